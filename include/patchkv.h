@@ -379,6 +379,118 @@ PATCHKV_API int patchkv_checkpoint_to_host(patchkv_ctx* ctx, const patchkv_geom*
                                            const uint64_t* host_layer_capacity, uint64_t* host_layer_bytes,
                                            void* stream);
 
+/* ---- live cache: quantised pages and attention ---------------------------------------------------------------
+ * The paper stops where the suffix is back in its pages; the decode steps and the recompute of the repair rows that
+ * follow have to attend over those pages.  These entry points do that over the bf16 pool a restore has filled, and over
+ * a cache whose pages are kept in the checkpoint's own quantised representations (Section IV-D: K8/V8, K8/V4, K4/V4),
+ * with the calls that write rows into such a cache and read them back.  One layer per call.
+ *
+ * A quantised page is one PKV1 block record of page_tokens tokens: [K codes][K scales][V codes][V scales] as above,
+ * every page of a pool at the same tag.  (A page can therefore be offloaded, or fetched, as a plain copy of a record.)
+ * Of patchkv_geom these calls read n_layers, n_kv_heads (H), head_dim (D, even), page_tokens (P) and group (G, divides
+ * D); block_tokens and the rotary fields are ignored: K is stored and used as given.
+ *
+ * Every geometry is taken.  The fast kernels want D = 64 or 128 and, for quantised pages, G a multiple of 32 and P a
+ * multiple of 16; other geometries, and rows or strides that are not multiples of 16 bytes, go to element-wise kernels with the same
+ * definition and no claim to speed. */
+enum { PATCHKV_ROWS_BF16 = 0, PATCHKV_ROWS_F16 = 1 };
+enum { PATCHKV_MAX_ATTENTION_DIM = 256 };
+
+/* A pool of quantised pages.  Page p of layer l starts at base + l*stride_layer + p*stride_page. */
+typedef struct {
+    uint32_t struct_size;
+    int32_t tag;            /* PATCHKV_TAG_INT8, _INT4 or _K4V4: the representation of every page */
+    int32_t n_pages;
+    int32_t reserved;
+    void* base;             /* DEVICE, 16-byte aligned */
+    int64_t stride_layer;   /* bytes, a non-negative multiple of 16 */
+    int64_t stride_page;    /* bytes, a multiple of 16, at least patchkv_record_bytes(tag, P, H, D, G) */
+} patchkv_qpool;
+
+/* A ragged batch of sequences.  Rows (new tokens, tokens to read, or query tokens) of all sequences are packed one behind
+ * the other; rows row_start[b] .. row_start[b+1]-1 belong to sequence b, and rows at and behind row_start[n_seqs] are
+ * neither read nor written.  Row i of a sequence with R rows stands at position pos[row] where pos is given, else at
+ * kv_len[b] - R + i: the last R positions.  A sequence may have no rows.
+ * The device arrays are read when the work runs, so a captured call can be replayed with other contents; n_rows,
+ * max_rows and max_kv_len are host-side bounds that size the launches. */
+typedef struct {
+    uint32_t struct_size;
+    int32_t n_seqs;
+    int32_t n_rows;               /* rows of the packed arrays, at least row_start[n_seqs] */
+    int32_t max_rows;             /* bound on the rows of one sequence (attention) */
+    int32_t max_kv_len;           /* bound on kv_len */
+    int32_t table_stride;         /* entries of block_table per sequence */
+    const int32_t* row_start;     /* DEVICE i32 [n_seqs + 1], ascending from >= 0 */
+    const int32_t* kv_len;        /* DEVICE i32 [n_seqs]: tokens of the sequence in the cache, those of this call included */
+    const int32_t* pos;           /* DEVICE i32 [n_rows], optional */
+    const int32_t* block_table;   /* DEVICE i32 [n_seqs][table_stride]: logical page -> physical page */
+} patchkv_batch;
+
+/* K and V rows outside the cache, element (row, head, channel) at row*stride_row + head*stride_head + channel. */
+typedef struct {
+    uint32_t struct_size;
+    int32_t type;                 /* PATCHKV_ROWS_* */
+    void* k;                      /* DEVICE [n_rows][H][D] */
+    void* v;                      /* DEVICE [n_rows][H][D] */
+    int64_t stride_row;           /* elements, the same for k and v */
+    int64_t stride_head;
+} patchkv_rows;
+
+/* Quantises the rows of the batch into their positions in the cache.  Per group of G channels: s = fp16(amax / qmax)
+ * (fp32 division, nearest even), code = clamp(rint(x / s), -qmax, qmax) with ties to even, s == 0 -> code 0; qmax = 127
+ * for 8 bits and 7 for 4: the quantiser of patchkv_quantize_gather.  Values must be finite; a group whose amax / qmax
+ * exceeds 65504 gets an infinite scale and zero codes.  Only the codes and scales of the rows' own slots are written.
+ * Positions of one sequence must be strictly ascending, and no two sequences may write the same slot.  A row whose
+ * position is outside [0, kv_len) or whose page is out of range, and a row whose position is not above that of the row
+ * in front of it, is skipped and PATCHKV_E_BOUNDS is latched.
+ * One launch, asynchronous on `stream`, no allocation, no workspace; it can be captured. */
+PATCHKV_API int patchkv_cache_append(patchkv_ctx* ctx, const patchkv_geom* geom, const patchkv_qpool* cache, int layer,
+                                     const patchkv_batch* batch, const patchkv_rows* rows, void* stream);
+
+/* Reads rows back: value = code * scale in fp32 (exact), rounded once to the rows' type (nearest even; beyond 65504 an
+ * fp16 row gets an infinity).  Positions may be in any order and may repeat.  A row that is out of range (as above) is
+ * left as it was and PATCHKV_E_BOUNDS is latched.  One launch, as patchkv_cache_append. */
+PATCHKV_API int patchkv_cache_read(patchkv_ctx* ctx, const patchkv_geom* geom, const patchkv_qpool* cache, int layer,
+                                   const patchkv_batch* batch, const patchkv_rows* rows, void* stream);
+
+/* Attention of the batch's query rows over the cache:
+ *   out[row][h] = sum_j softmax_j(scale * q[row][h] . k_j) v_j, query head h reading KV head h / (Hq / H),
+ * over the tokens j that the row at position p sees: j <= p, j < kv_len and, with a window, p - j < window or
+ * j < sinks.  A row that sees no token (a negative position, kv_len 0) gets zeros.  Tokens that a row does not see do
+ * not reach it, whatever their slots hold (NaN and infinities included). */
+typedef struct {
+    uint32_t struct_size;
+    int32_t type;                 /* PATCHKV_ROWS_*: type of q and out; over a bf16 pool only PATCHKV_ROWS_BF16 */
+    int32_t n_q_heads;            /* Hq, a multiple of H */
+    int32_t window;               /* 0: none; else the row's own position and the window - 1 before it */
+    int32_t sinks;                /* first tokens that stay visible behind a window, >= 0; without a window all are */
+    float scale;                  /* factor on the dot products, usually D^-1/2; finite */
+    const void* q;                /* DEVICE [n_rows][Hq][D] */
+    void* out;                    /* DEVICE [n_rows][Hq][D], must not overlap q */
+    int64_t q_stride_row;         /* elements; the channel stride is 1 */
+    int64_t q_stride_head;
+    int64_t out_stride_row;
+    int64_t out_stride_head;
+    void* workspace;              /* DEVICE, 16-byte aligned; the caller's for the time the call's work takes, contents
+                                     don't matter.  Calls that may overlap on the GPU need one each, and so do graphs */
+    uint64_t workspace_bytes;     /* at least patchkv_attention_workspace_bytes of the same arguments */
+} patchkv_attention_args;
+
+/* `pool` is a patchkv_pool (bf16) or NULL, `cache` a patchkv_qpool or NULL: exactly one of the two.  Asynchronous on
+ * `stream`, no allocation, no host synchronisation; can be captured.  Logits, softmax sums and output sums are held in
+ * fp32, the result is rounded once; the weights enter the second product as 16-bit numbers.
+ * A sequence whose row_start entries are descending or outside [0, n_rows], rows beyond max_rows of a sequence, tokens
+ * beyond max_kv_len or the block table, and tokens whose page is out of range are left out, and PATCHKV_E_BOUNDS is
+ * latched (left-out rows keep what `out` held). */
+PATCHKV_API int patchkv_attention(patchkv_ctx* ctx, const patchkv_geom* geom, const patchkv_pool* pool,
+                                  const patchkv_qpool* cache, int layer, const patchkv_batch* batch,
+                                  const patchkv_attention_args* args, void* stream);
+
+/* Workspace of such a call; 0 if it needs none (or the arguments are invalid).  Depends on the geometry, the tag
+ * (PATCHKV_TAG_BF16: a pool), n_seqs, n_rows, max_rows, max_kv_len, Hq, window and sinks.  Needs no GPU. */
+PATCHKV_API uint64_t patchkv_attention_workspace_bytes(const patchkv_geom* geom, int tag, const patchkv_batch* batch,
+                                                       int n_q_heads, int window, int sinks);
+
 /* Synchronises the context's device work and returns in *device_status the first device-side error latched
  * since the last query (PATCHKV_OK, PATCHKV_E_BOUNDS, PATCHKV_E_BADINPUT or PATCHKV_E_TIMEOUT), then clears it. */
 PATCHKV_API int patchkv_query_status(patchkv_ctx* ctx, int* device_status);

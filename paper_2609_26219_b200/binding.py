@@ -23,6 +23,7 @@ ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 LAYERS_INDEPENDENT, LAYERS_SHARED = 0, 1
 SCORE_ATTN_F16, SCORE_BLOCK_MASS, SCORE_TOKEN_MASS = 0, 1, 2
 MAX_SESSIONS = 8
+ROWS_BF16, ROWS_F16 = 0, 1
 FLAG_DIRECT_LOADS = 1
 FLAG_HOST_DIRECT = 2
 FLAG_HOST_STAGED = 4
@@ -73,6 +74,29 @@ class RestoreStats(C.Structure):
                 ("bytes_useful", C.c_uint64), ("n_block_layers", C.c_uint64), ("bytes_direct", C.c_uint64)]
 
 
+class QPool(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("tag", C.c_int32), ("n_pages", C.c_int32), ("reserved", C.c_int32),
+                ("base", C.c_void_p), ("stride_layer", C.c_int64), ("stride_page", C.c_int64)]
+
+
+class Batch(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("max_rows", C.c_int32),
+                ("max_kv_len", C.c_int32), ("table_stride", C.c_int32), ("row_start", C.c_void_p),
+                ("kv_len", C.c_void_p), ("pos", C.c_void_p), ("block_table", C.c_void_p)]
+
+
+class Rows(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("type", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("stride_row", C.c_int64), ("stride_head", C.c_int64)]
+
+
+class AttentionArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("type", C.c_int32), ("n_q_heads", C.c_int32), ("window", C.c_int32),
+                ("sinks", C.c_int32), ("scale", C.c_float), ("q", C.c_void_p), ("out", C.c_void_p),
+                ("q_stride_row", C.c_int64), ("q_stride_head", C.c_int64), ("out_stride_row", C.c_int64),
+                ("out_stride_head", C.c_int64), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
 _lib = None
 
 
@@ -104,6 +128,16 @@ def lib():
         l.patchkv_plan_precision.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_float, C.c_float,
                                              C.c_float, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p]
         l.patchkv_plan_precision.restype = C.c_int
+        l.patchkv_cache_append.argtypes = [C.c_void_p, C.POINTER(Geom), C.POINTER(QPool), C.c_int, C.POINTER(Batch),
+                                           C.POINTER(Rows), C.c_void_p]
+        l.patchkv_cache_append.restype = C.c_int
+        l.patchkv_cache_read.argtypes = l.patchkv_cache_append.argtypes
+        l.patchkv_cache_read.restype = C.c_int
+        l.patchkv_attention.argtypes = [C.c_void_p, C.POINTER(Geom), C.POINTER(Pool), C.POINTER(QPool), C.c_int,
+                                        C.POINTER(Batch), C.POINTER(AttentionArgs), C.c_void_p]
+        l.patchkv_attention.restype = C.c_int
+        l.patchkv_attention_workspace_bytes.argtypes = [C.POINTER(Geom), C.c_int, C.POINTER(Batch), C.c_int, C.c_int, C.c_int]
+        l.patchkv_attention_workspace_bytes.restype = C.c_uint64
         l.patchkv_query_status.argtypes = [C.c_void_p, C.POINTER(C.c_int)]
         l.patchkv_selftest_bounded_wait.argtypes = [C.c_void_p, C.c_uint32, C.c_void_p]
         l.patchkv_selftest_stall_next_launch.argtypes = [C.c_void_p, C.c_int32, C.c_uint32]
@@ -152,6 +186,54 @@ def make_session(*, n_suffix_tokens, delta, dst_shift, block_table, tags, blk_of
     return Session(C.sizeof(Session), n_suffix_tokens, delta, dst_shift, block_table.numel(), 0,
                    _ptr(block_table), _ptr(tags), _ptr(blk_off), _ptr(layer_payload), _ptr(layer_bytes),
                    _ptr(reuse_idx), _ptr(reuse_cnt))
+
+
+def make_qpool(pages: torch.Tensor, tag: int, n_pages: int, stride_layer: Optional[int] = None,
+               stride_page: Optional[int] = None) -> QPool:
+    """A pool of quantised pages.  pages: uint8 device tensor [n_pages][bytes] or [n_layers][n_pages][bytes]; the strides
+    (bytes) are the tensor's unless given.  A page holds record_bytes(tag, page_tokens, H, D, G) bytes."""
+    if pages.dtype != torch.uint8 or pages.dim() not in (2, 3) or pages.stride(-1) != 1:
+        raise ValueError("pages: a uint8 tensor [n_pages][bytes] or [n_layers][n_pages][bytes] with unit stride on the last axis")
+    if stride_page is None:
+        stride_page = pages.stride(-2)
+    if stride_layer is None:
+        stride_layer = pages.stride(0) if pages.dim() == 3 else 0
+    return QPool(C.sizeof(QPool), tag, n_pages, 0, pages.data_ptr(), int(stride_layer), int(stride_page))
+
+
+def make_batch(*, row_start: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, n_rows: int, max_rows: int,
+               max_kv_len: int, pos: Optional[torch.Tensor] = None) -> Batch:
+    """int32 device tensors: row_start [n_seqs + 1], kv_len [n_seqs], block_table [n_seqs][entries], pos [n_rows] or None;
+    all kept alive by the caller."""
+    n = kv_len.numel()
+    for name, t, size in (("row_start", row_start, n + 1), ("kv_len", kv_len, n), ("pos", pos, n_rows)):
+        if t is not None and (t.dtype != torch.int32 or t.numel() < size or not t.is_contiguous()):
+            raise ValueError(f"{name}: a contiguous int32 tensor of {size} entries")
+    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.shape[0] < n or not block_table.is_contiguous():
+        raise ValueError("block_table: a contiguous int32 tensor [n_seqs][entries]")
+    return Batch(C.sizeof(Batch), n, n_rows, max_rows, max_kv_len, block_table.shape[1], _ptr(row_start), _ptr(kv_len),
+                 _ptr(pos), _ptr(block_table))
+
+
+def _row_type(t: torch.Tensor, name: str) -> int:
+    if t.dtype not in (torch.bfloat16, torch.float16) or t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name}: a bfloat16 or float16 tensor [rows][heads][channels] with unit channel stride")
+    return ROWS_F16 if t.dtype == torch.float16 else ROWS_BF16
+
+
+def _make_rows(geom: Geom, batch: Batch, k: torch.Tensor, v: torch.Tensor) -> Rows:
+    kind = _row_type(k, "k")
+    if _row_type(v, "v") != kind or v.shape != k.shape or v.stride() != k.stride():
+        raise ValueError("k and v must agree in type, shape and strides")
+    if k.shape[0] < batch.n_rows or tuple(k.shape[1:]) != (geom.n_kv_heads, geom.head_dim):
+        raise ValueError("k and v: [n_rows][n_kv_heads][head_dim]")
+    return Rows(C.sizeof(Rows), kind, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1))
+
+
+def attention_workspace_bytes(geom: Geom, cache, batch: Batch, n_q_heads: int, window: int = 0, sinks: int = 0) -> int:
+    """Bytes of workspace Context.attention needs for such a call (`cache`: a QPool, or a Pool for the bf16 pool)."""
+    tag = cache.tag if isinstance(cache, QPool) else TAG_BF16
+    return int(lib().patchkv_attention_workspace_bytes(C.byref(geom), tag, C.byref(batch), n_q_heads, window, sinks))
 
 
 class Context:
@@ -231,6 +313,40 @@ class Context:
         return self._check(lib().patchkv_plan_precision(self._h, _ptr(attn), _ptr(resid), attn.numel(), block_tokens,
                                                         alpha, tau_L, tau_H, eps4, _ptr(tags), _ptr(risk),
                                                         _stream_handle(stream)), check)
+
+    def cache_append(self, geom: Geom, cache: QPool, layer: int, batch: Batch, k: torch.Tensor, v: torch.Tensor,
+                     stream=None, check: bool = True) -> int:
+        """Quantises the rows k, v [n_rows][H][D] (bf16 or fp16) into their positions in the cache."""
+        rows = _make_rows(geom, batch, k, v)
+        return self._check(lib().patchkv_cache_append(self._h, C.byref(geom), C.byref(cache), layer, C.byref(batch),
+                                                      C.byref(rows), _stream_handle(stream)), check)
+
+    def cache_read(self, geom: Geom, cache: QPool, layer: int, batch: Batch, k: torch.Tensor, v: torch.Tensor,
+                   stream=None, check: bool = True) -> int:
+        """Reads the batch's positions back into k, v [n_rows][H][D] (bf16 or fp16)."""
+        rows = _make_rows(geom, batch, k, v)
+        return self._check(lib().patchkv_cache_read(self._h, C.byref(geom), C.byref(cache), layer, C.byref(batch),
+                                                    C.byref(rows), _stream_handle(stream)), check)
+
+    def attention(self, geom: Geom, cache, layer: int, batch: Batch, q: torch.Tensor, out: torch.Tensor,
+                  scale: Optional[float] = None, window: int = 0, sinks: int = 0,
+                  workspace: Optional[torch.Tensor] = None, stream=None, check: bool = True) -> int:
+        """Attention of q [n_rows][Hq][D] over a QPool or the bf16 Pool into out (same shape and type).  scale None =
+        head_dim ** -0.5.  workspace: a uint8 device tensor of attention_workspace_bytes(...) bytes that nothing else uses
+        while the call's work runs; needed when that is not 0."""
+        kind = _row_type(q, "q")
+        if _row_type(out, "out") != kind or out.shape != q.shape:
+            raise ValueError("out must have the shape and type of q")
+        if q.shape[0] < batch.n_rows or q.shape[2] != geom.head_dim:
+            raise ValueError("q: [n_rows][n_q_heads][head_dim]")
+        a = AttentionArgs(C.sizeof(AttentionArgs), kind, q.shape[1], window, sinks,
+                          geom.head_dim ** -0.5 if scale is None else scale, q.data_ptr(), out.data_ptr(), q.stride(0),
+                          q.stride(1), out.stride(0), out.stride(1), _ptr(workspace),
+                          0 if workspace is None else workspace.numel() * workspace.element_size())
+        quantised = isinstance(cache, QPool)
+        return self._check(lib().patchkv_attention(self._h, C.byref(geom), None if quantised else C.byref(cache),
+                                                   C.byref(cache) if quantised else None, layer, C.byref(batch),
+                                                   C.byref(a), _stream_handle(stream)), check)
 
     def selftest_bounded_wait(self, max_polls: int, stream=None, check: bool = True) -> int:
         """Runs the kernels' bounded barrier wait on a barrier that nothing completes; query_status() then reports E_TIMEOUT."""

@@ -1,0 +1,194 @@
+// Attention over a cache of quantised pages or over the bf16 pool (patchkv_attention).
+#include <math.h>
+
+#include <algorithm>
+
+#include "attention.cuh"
+
+namespace patchkv {
+
+// ---------------------------------------------------------------- any geometry, any strides
+// One CTA per (row, query head): tiles of 128 tokens, a token per thread for the logits, channels across threads for the
+// second product.  Every token a row does not see is passed over, so nothing of its slot reaches the row.
+constexpr int kAnyThreads = 128;
+
+template <int TYPE>
+__global__ void __launch_bounds__(kAnyThreads) attention_any_kernel(const AttentionParams p) {
+    __shared__ float q[PATCHKV_MAX_ATTENTION_DIM];
+    __shared__ float w[kAnyThreads];
+    __shared__ long long off_k[kAnyThreads], off_v[kAnyThreads];
+    __shared__ float red[kAnyThreads / 32];
+    const int s = blockIdx.z, hq = blockIdx.y, h = hq / p.share;
+    int first, kv, rows;
+    const bool ordered = sequence_rows(p, s, &first, &kv, &rows);
+    if (threadIdx.x == 0 && (!ordered || rows > p.b.max_rows)) latch(p.status);
+    if (!ordered || (int)blockIdx.x >= rows) return;
+    const int r = first + blockIdx.x;
+    if (__ldg(p.b.kv_len + s) > kv && threadIdx.x == 0) latch(p.status);
+    const int pos = row_position(p.b, s, r);
+    const uint16_t* qs = p.q + (long long)r * p.q_stride_row + (long long)hq * p.q_stride_head;
+    for (int c = threadIdx.x; c < p.c.D; c += kAnyThreads)
+        q[c] = TYPE == PATCHKV_ROWS_F16 ? half_bits_to_float(qs[c]) : bf16_bits_to_float(qs[c]);
+    __syncthreads();
+    const int end = min(pos, kv - 1) + 1;                       // tokens [0, end), those outside the window by `sees`
+    float m = -INFINITY, l = 0.0f, acc[2] = {0.0f, 0.0f};
+    const int kf = k_format(p.c.tag), vf = v_format(p.c.tag);
+    int t0 = 0;
+    while (t0 < end) {
+        const int t = t0 + threadIdx.x;
+        float x = -INFINITY;
+        off_v[threadIdx.x] = -1;
+        if (t < end && sees(p, pos, t)) {
+            const int lp = div_page(p.c, t), slot = t - lp * p.c.P;
+            const int page = __ldg(p.b.block_table + (long long)s * p.b.table_stride + lp);
+            if (page < 0 || page >= p.c.n_pages) {
+                latch(p.status);
+            } else if (p.c.tag == PATCHKV_TAG_BF16) {
+                const long long o = (long long)page * p.c.stride_page + (long long)slot * p.c.stride_token + (long long)h * p.c.stride_head;
+                off_v[threadIdx.x] = o;
+                x = 0.0f;
+                for (int c = 0; c < p.c.D; c++) x = fmaf(q[c], bf16_bits_to_float(p.c.k[o + c]), x);
+            } else {
+                const uint8_t* pg = p.c.base + (long long)page * p.c.stride_page;
+                const unsigned long long e = ((unsigned long long)slot * p.c.H + h) * p.c.D;
+                off_v[threadIdx.x] = (long long)page;
+                off_k[threadIdx.x] = (long long)e;
+                x = 0.0f;
+                for (int c0 = 0; c0 < p.c.D; c0 += p.c.G) {
+                    float y = 0.0f;
+                    for (int c = c0; c < c0 + p.c.G; c++) y = fmaf(q[c], (float)code_at(pg, kf, e + c), y);
+                    x = fmaf(y, scale_at(pg + p.c.k_scales, (e + c0) / p.c.G), x);
+                }
+            }
+            x *= p.scale_log2;
+        }
+        float mt = x;
+        for (int d = 16; d; d >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xFFFFFFFFu, mt, d));
+        if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = mt;
+        __syncthreads();
+        mt = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+        const float mn = fmaxf(m, mt), ref = mn == -INFINITY ? 0.0f : mn;
+        const float e = off_v[threadIdx.x] >= 0 ? exp2f(x - ref) : 0.0f;
+        w[threadIdx.x] = e;
+        const float keep = exp2f(m - ref);
+        m = mn;
+        __syncthreads();
+        l *= keep;
+        acc[0] *= keep; acc[1] *= keep;
+        for (int j = 0; j < min(kAnyThreads, end - t0); j++) {
+            const long long o = off_v[j];
+            if (o < 0) continue;
+            l += w[j];
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+                const int c = threadIdx.x + k * kAnyThreads;
+                if (c >= p.c.D) continue;
+                if (p.c.tag == PATCHKV_TAG_BF16) {
+                    acc[k] = fmaf(w[j], bf16_bits_to_float(p.c.v[o + c]), acc[k]);
+                } else {
+                    const uint8_t* pg = p.c.base + o * p.c.stride_page;
+                    const unsigned long long ec = (unsigned long long)off_k[j] + c;
+                    acc[k] = fmaf(w[j], (float)code_at(pg + p.c.v_codes, vf, ec) * scale_at(pg + p.c.v_scales, ec / p.c.G), acc[k]);
+                }
+            }
+        }
+        __syncthreads();
+        t0 += kAnyThreads;
+        if (p.window > 0 && t0 >= p.sinks && t0 <= pos - p.window)       // skip what lies between the sinks and the window
+            t0 = pos - p.window + 1;
+    }
+    uint16_t* o = p.out + (long long)r * p.out_stride_row + (long long)hq * p.out_stride_head;
+    const float inv = l != 0.0f ? 1.0f / l : 0.0f;              // a row that sees nothing: zeros
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+        const int c = threadIdx.x + k * kAnyThreads;
+        if (c < p.c.D) {
+            const float y = acc[k] * inv;
+            o[c] = TYPE == PATCHKV_ROWS_F16 ? __half_as_ushort(__float2half_rn(y)) : __bfloat16_as_ushort(__float2bfloat16_rn(y));
+        }
+    }
+}
+
+namespace {
+
+// Checks everything but the workspace; with `ctx` null only what the workspace's size depends on.
+int check_attention(patchkv_ctx* ctx, const patchkv_geom* g, int tag, const patchkv_batch* b, int Hq, int window, int sinks) {
+    if (g->head_dim > PATCHKV_MAX_ATTENTION_DIM) return fail(ctx, PATCHKV_E_UNSUPPORTED, "attention: head_dim above 256");
+    if (Hq <= 0 || Hq % g->n_kv_heads) return fail(ctx, PATCHKV_E_INVALID, "attention: n_q_heads must be a positive multiple of n_kv_heads");
+    if (window < 0 || sinks < 0) return fail(ctx, PATCHKV_E_INVALID, "attention: negative window or sinks");
+    if (Hq > 65535 || b->n_seqs > 65535) return fail(ctx, PATCHKV_E_UNSUPPORTED, "attention: more than 65535 query heads or sequences");
+    if (tag < PATCHKV_TAG_BF16 || tag > PATCHKV_TAG_K4V4) return fail(ctx, PATCHKV_E_INVALID, "attention: unknown tag");
+    return PATCHKV_OK;
+}
+
+int fill_pool(patchkv_ctx* ctx, const patchkv_geom* g, const patchkv_pool* q, int layer, CacheDev* c) {
+    if (q->struct_size != sizeof(patchkv_pool)) return fail(ctx, PATCHKV_E_INVALID, "attention: wrong struct_size of the pool");
+    const uintptr_t k = reinterpret_cast<uintptr_t>(q->k_base), v = reinterpret_cast<uintptr_t>(q->v_base);
+    if (!k || !v || ((k | v) & 15u) || q->n_pages <= 0) return fail(ctx, PATCHKV_E_INVALID, "attention: pool base null or not 16-byte aligned, or no pages");
+    if (q->stride_layer < 0 || q->stride_page < 0 || q->stride_token < 0 || q->stride_head < 0)
+        return fail(ctx, PATCHKV_E_INVALID, "attention: negative pool stride");
+    memset(c, 0, sizeof(*c));
+    c->k = static_cast<const uint16_t*>(q->k_base) + (long long)layer * q->stride_layer;
+    c->v = static_cast<const uint16_t*>(q->v_base) + (long long)layer * q->stride_layer;
+    c->stride_page = q->stride_page; c->stride_token = q->stride_token; c->stride_head = q->stride_head;
+    c->n_pages = q->n_pages; c->H = g->n_kv_heads; c->D = g->head_dim; c->P = g->page_tokens; c->G = g->group;
+    c->P_shift = log2_exact(g->page_tokens);
+    c->tag = PATCHKV_TAG_BF16;
+    return PATCHKV_OK;
+}
+
+}  // namespace
+}  // namespace patchkv
+
+using namespace patchkv;
+
+extern "C" uint64_t patchkv_attention_workspace_bytes(const patchkv_geom* g, int tag, const patchkv_batch* b, int n_q_heads,
+                                                      int window, int sinks) {
+    BatchDev bd;
+    if (check_live_geometry(nullptr, "attention", g, 0) != PATCHKV_OK || fill_batch(nullptr, "attention", b, &bd) != PATCHKV_OK ||
+        check_attention(nullptr, g, tag, b, n_q_heads, window, sinks) != PATCHKV_OK)
+        return 0;
+    return 0;
+}
+
+extern "C" int patchkv_attention(patchkv_ctx* ctx, const patchkv_geom* g, const patchkv_pool* pool, const patchkv_qpool* cache,
+                                 int layer, const patchkv_batch* batch, const patchkv_attention_args* a, void* stream_) {
+    if (!ctx) return PATCHKV_E_INVALID;
+    std::lock_guard<std::mutex> lock(ctx->mu);
+    AttentionParams p;
+    if ((pool != nullptr) == (cache != nullptr)) return fail(ctx, PATCHKV_E_INVALID, "attention: give a pool or a cache, one of the two");
+    int rc = check_live_geometry(ctx, "attention", g, layer);
+    if (rc == PATCHKV_OK) rc = fill_batch(ctx, "attention", batch, &p.b);
+    if (rc == PATCHKV_OK) rc = pool ? fill_pool(ctx, g, pool, layer, &p.c) : fill_cache(ctx, "attention", g, cache, layer, &p.c);
+    if (rc != PATCHKV_OK) return rc;
+    if (!a || a->struct_size != sizeof(patchkv_attention_args)) return fail(ctx, PATCHKV_E_INVALID, "attention: null args or wrong struct_size");
+    rc = check_attention(ctx, g, p.c.tag, batch, a->n_q_heads, a->window, a->sinks);
+    if (rc != PATCHKV_OK) return rc;
+    if (a->type != PATCHKV_ROWS_BF16 && a->type != PATCHKV_ROWS_F16) return fail(ctx, PATCHKV_E_INVALID, "attention: unknown row type");
+    if (pool && a->type != PATCHKV_ROWS_BF16) return fail(ctx, PATCHKV_E_INVALID, "attention: over a bf16 pool q and out must be bf16");
+    if (!(fabsf(a->scale) <= 3.0e38f)) return fail(ctx, PATCHKV_E_INVALID, "attention: scale must be finite");
+    if (a->q_stride_row < 0 || a->q_stride_head < 0 || a->out_stride_row < 0 || a->out_stride_head < 0)
+        return fail(ctx, PATCHKV_E_INVALID, "attention: negative stride");
+    if (p.b.n_rows == 0 || p.b.n_seqs == 0 || p.b.max_rows == 0) return PATCHKV_OK;
+    const uintptr_t qa = reinterpret_cast<uintptr_t>(a->q), oa = reinterpret_cast<uintptr_t>(a->out);
+    if (!qa || !oa || (qa & 1) || (oa & 1)) return fail(ctx, PATCHKV_E_INVALID, "attention: null or misaligned q or out");
+    if (rows_overlap(p.b.n_rows, a->n_q_heads, p.c.D, a->out_stride_row, a->out_stride_head))
+        return fail(ctx, PATCHKV_E_INVALID, "attention: rows or heads of out overlap");
+    const uint64_t need = patchkv_attention_workspace_bytes(g, p.c.tag, batch, a->n_q_heads, a->window, a->sinks);
+    if (need && (!a->workspace || (reinterpret_cast<uintptr_t>(a->workspace) & 15) || a->workspace_bytes < need))
+        return fail(ctx, PATCHKV_E_INVALID, "attention: workspace null, misaligned or too small");
+    p.q = static_cast<const uint16_t*>(a->q); p.out = static_cast<uint16_t*>(a->out);
+    p.q_stride_row = a->q_stride_row; p.q_stride_head = a->q_stride_head;
+    p.out_stride_row = a->out_stride_row; p.out_stride_head = a->out_stride_head;
+    p.Hq = a->n_q_heads; p.share = a->n_q_heads / g->n_kv_heads;
+    p.window = a->window; p.sinks = a->sinks;
+    p.scale_log2 = (float)((double)a->scale * 1.4426950408889634);
+    p.status = ctx->d_status;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(ctx, PATCHKV_E_CUDA, "cudaSetDevice failed");
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    auto kernel = a->type == PATCHKV_ROWS_F16 ? attention_any_kernel<PATCHKV_ROWS_F16> : attention_any_kernel<PATCHKV_ROWS_BF16>;
+    kernel<<<dim3(std::min(p.b.max_rows, p.b.n_rows), p.Hq, p.b.n_seqs), kAnyThreads, 0, stream>>>(p);
+    PKV_CUDA(ctx, cudaGetLastError());
+    return PATCHKV_OK;
+}

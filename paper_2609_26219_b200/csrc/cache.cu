@@ -1,0 +1,352 @@
+// Rows into and out of a cache of quantised pages: patchkv_cache_append, patchkv_cache_read, and the checks that the
+// live-cache calls share.
+#include "live.cuh"
+
+namespace patchkv {
+
+constexpr int kRowThreads = 128;
+
+struct RowsDev {
+    uint16_t* k;
+    uint16_t* v;
+    long long stride_row, stride_head;
+};
+
+struct RowParams {
+    CacheDev c;
+    BatchDev b;
+    RowsDev rows;
+    int32_t* status;
+    int32_t vecs;               // 8-channel vectors of a row: H * D / 8
+    int32_t seg;                // lanes per scale group: G / 8
+};
+
+__device__ __forceinline__ void latch_bounds(int32_t* status) { atomicCAS(status, 0, (int)PATCHKV_E_BOUNDS); }
+
+// Page and slot of row r; false (latched once per row by the caller's `first` thread) when the row is skipped.
+template <bool WRITE>
+__device__ __forceinline__ bool find_slot(const RowParams& p, int r, bool first, uint8_t** page, int* slot) {
+    const int s = find_sequence(p.b, r);
+    if (s < 0) return false;                                // a row of no sequence: not an error
+    const int pos = row_position(p.b, s, r);
+    bool ok = !WRITE || !p.b.pos || r == __ldg(p.b.row_start + s) || __ldg(p.b.pos + r - 1) < pos;
+    const int pg = ok ? locate(p.b, p.c, s, pos, slot) : -1;
+    if (pg < 0) {
+        if (first) latch_bounds(p.status);
+        return false;
+    }
+    *page = p.c.base + (long long)pg * p.c.stride_page;
+    return true;
+}
+
+template <int TYPE>
+__device__ __forceinline__ float to_float(uint32_t h) {
+    return TYPE == PATCHKV_ROWS_F16 ? half_bits_to_float(h) : bf16_bits_to_float(h);
+}
+template <int TYPE>
+__device__ __forceinline__ uint32_t pack_pair(float lo, float hi) {
+    if (TYPE == PATCHKV_ROWS_F16) {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Eight channels -> codes and, from the group's first lane, its scale.  `seg` lanes share a group (a power of two).
+// The quotient: r = 1 / s rounded, t = x * r, one correction t + (x - t*s) * r.  s has 11 significant bits, so its
+// reciprocal is not the one case in which a correctly rounded r does not make the corrected quotient the correctly
+// rounded x / s (Markstein's theorem); x and s have 11 bits at most, so x / s is exactly a half-integer or at least 2^-12
+// away from one, and the fp32 rounding of the quotient (2^-17 at |x / s| <= 128) does not carry it across.
+template <int TYPE, int FMT>
+__device__ __forceinline__ void encode8(const uint4& w, uint8_t* codes, uint8_t* scale, int seg, bool live) {
+    float x[8];
+    const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        x[2 * i] = to_float<TYPE>(ws[i] & 0xFFFFu);
+        x[2 * i + 1] = to_float<TYPE>(ws[i] >> 16);
+    }
+    float amax = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; i++) amax = fmaxf(amax, fabsf(x[i]));
+    for (int d = 1; d < seg; d <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, d));
+    if (!live) return;
+    constexpr float qmax = FMT == FMT_INT8 ? 127.0f : 7.0f;
+    const __half s16 = __float2half_rn(__fdiv_rn(amax, qmax));
+    float s = __half2float(s16);
+    const bool usable = s > 0.0f && s <= 65504.0f;          // a zero or infinite scale: all codes zero
+    if (!usable) s = 1.0f;
+    const float r = __frcp_rn(s);
+    uint32_t kb[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const float xi = usable ? x[i] : 0.0f;
+        float t = __fmul_rn(xi, r);
+        t = __fmaf_rn(__fmaf_rn(-t, s, xi), r, t);
+        t = fminf(fmaxf(t, -qmax), qmax);                   // only a subnormal scale leaves |t| above qmax
+        kb[i] = __float_as_uint(__fadd_rn(t, 12582912.0f)); // 1.5 * 2^23: rounds to an integer, ties to even
+    }
+    const uint32_t w0 = __byte_perm(__byte_perm(kb[0], kb[1], 0x0040), __byte_perm(kb[2], kb[3], 0x0040), 0x5410);
+    const uint32_t w1 = __byte_perm(__byte_perm(kb[4], kb[5], 0x0040), __byte_perm(kb[6], kb[7], 0x0040), 0x5410);
+    if (FMT == FMT_INT8) {
+        *reinterpret_cast<uint2*>(codes) = make_uint2(w0, w1);
+    } else {
+        uint32_t a = w0 & 0x0F0F0F0Fu, b = w1 & 0x0F0F0F0Fu;
+        a = (a | (a >> 4)) & 0x00FF00FFu; a = (a | (a >> 8)) & 0x0000FFFFu;
+        b = (b | (b >> 4)) & 0x00FF00FFu; b = (b | (b >> 8)) & 0x0000FFFFu;
+        *reinterpret_cast<uint32_t*>(codes) = a | (b << 16);
+    }
+    if (scale) *reinterpret_cast<__half*>(scale) = s16;
+}
+
+// A thread takes eight channels of one row, K and V: the loads and stores of a warp are contiguous, the groups' maxima
+// go through shuffles, and the row's slot is looked up while the row is on its way.  Bound by memory.
+template <int TYPE, int KF, int VF>
+__global__ void __launch_bounds__(kRowThreads) cache_append_kernel(const RowParams p) {
+    pdl_trigger();
+    const uint32_t i = blockIdx.x * kRowThreads + threadIdx.x, q = i / (uint32_t)p.vecs;
+    const int r = (int)q, vec = (int)(i - q * (uint32_t)p.vecs);
+    bool live = r < p.b.n_rows;
+    const int e = vec * 8, h = e / p.c.D, c = e - h * p.c.D;
+    uint4 kw = make_uint4(0, 0, 0, 0), vw = kw;
+    uint8_t* page = nullptr;
+    int slot = 0;
+    pdl_wait();
+    live = live && find_slot<true>(p, r, vec == 0, &page, &slot);
+    if (live) {
+        const long long src = (long long)r * p.rows.stride_row + (long long)h * p.rows.stride_head + c;
+        kw = __ldg(reinterpret_cast<const uint4*>(p.rows.k + src));
+        vw = __ldg(reinterpret_cast<const uint4*>(p.rows.v + src));
+    }
+    const uint32_t at = (uint32_t)slot * p.c.H * p.c.D + e;
+    const bool first = (vec & (p.seg - 1)) == 0;
+    const uint32_t group = at / p.c.G;
+    encode8<TYPE, KF>(kw, page + (KF == FMT_INT8 ? at : at >> 1), first ? page + p.c.k_scales + 2 * group : nullptr, p.seg, live);
+    encode8<TYPE, VF>(vw, page + p.c.v_codes + (VF == FMT_INT8 ? at : at >> 1), first ? page + p.c.v_scales + 2 * group : nullptr,
+                      p.seg, live);
+}
+
+// Eight codes and their scale -> eight channels.  An integer u < 2^23 in the low bits of 2^23's pattern is the float
+// 2^23 + u, so the codes need no conversion instruction; code * scale is exact in fp32 and rounded once.
+template <int TYPE, int FMT>
+__device__ __forceinline__ uint4 decode8(const uint2& w, float s) {
+    float x[8];
+    if (FMT == FMT_INT8) {
+        const uint32_t a = w.x ^ 0x80808080u, b = w.y ^ 0x80808080u;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            x[i] = __uint_as_float(__byte_perm(a, 0x4B000000u, 0x7540 + i)) - 8388736.0f;
+            x[4 + i] = __uint_as_float(__byte_perm(b, 0x4B000000u, 0x7540 + i)) - 8388736.0f;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            x[i] = __uint_as_float((((w.x >> (4 * i)) & 15u) ^ 8u) | 0x4B000000u) - 8388616.0f;
+    }
+    uint4 o;
+    o.x = pack_pair<TYPE>(x[0] * s, x[1] * s);
+    o.y = pack_pair<TYPE>(x[2] * s, x[3] * s);
+    o.z = pack_pair<TYPE>(x[4] * s, x[5] * s);
+    o.w = pack_pair<TYPE>(x[6] * s, x[7] * s);
+    return o;
+}
+template <int FMT>
+__device__ __forceinline__ uint2 load_codes8(const uint8_t* codes, uint32_t at) {
+    if (FMT == FMT_INT8) return *reinterpret_cast<const uint2*>(codes + at);
+    return make_uint2(*reinterpret_cast<const uint32_t*>(codes + (at >> 1)), 0u);
+}
+
+template <int TYPE, int KF, int VF>
+__global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const RowParams p) {
+    pdl_trigger();
+    const uint32_t i = blockIdx.x * kRowThreads + threadIdx.x, q = i / (uint32_t)p.vecs;
+    const int r = (int)q, vec = (int)(i - q * (uint32_t)p.vecs);
+    if (r >= p.b.n_rows) return;
+    const int e = vec * 8, h = e / p.c.D, c = e - h * p.c.D;
+    uint8_t* page = nullptr;
+    int slot = 0;
+    pdl_wait();
+    if (!find_slot<false>(p, r, vec == 0, &page, &slot)) return;
+    const uint32_t at = (uint32_t)slot * p.c.H * p.c.D + e;
+    const uint32_t group = at / p.c.G;
+    const uint2 kc = load_codes8<KF>(page, at), vc = load_codes8<VF>(page + p.c.v_codes, at);
+    const float ks = __half2float(*reinterpret_cast<const __half*>(page + p.c.k_scales + 2 * group));
+    const float vs = __half2float(*reinterpret_cast<const __half*>(page + p.c.v_scales + 2 * group));
+    const long long dst = (long long)r * p.rows.stride_row + (long long)h * p.rows.stride_head + c;
+    *reinterpret_cast<uint4*>(p.rows.k + dst) = decode8<TYPE, KF>(kc, ks);
+    *reinterpret_cast<uint4*>(p.rows.v + dst) = decode8<TYPE, VF>(vc, vs);
+}
+
+// Any geometry, any strides: one thread per (row, section, head) walks the head's groups with byte accesses to the page.
+// (A byte may hold codes of two groups, so the head is the smallest piece that one thread can own.)
+template <int TYPE, bool WRITE>
+__global__ void __launch_bounds__(kRowThreads) cache_rows_any_kernel(const RowParams p) {
+    const uint32_t i = blockIdx.x * kRowThreads + threadIdx.x, per_row = 2u * p.c.H;
+    const int r = (int)(i / per_row), q = (int)(i - (uint32_t)r * per_row), h = q >> 1;
+    if (r >= p.b.n_rows) return;
+    uint8_t* page = nullptr;
+    int slot = 0;
+    if (!find_slot<WRITE>(p, r, q == 0, &page, &slot)) return;
+    const bool is_v = q & 1;
+    const int fmt = is_v ? v_format(p.c.tag) : k_format(p.c.tag);
+    uint8_t* codes = page + (is_v ? p.c.v_codes : 0u);
+    uint8_t* scales = page + (is_v ? p.c.v_scales : p.c.k_scales);
+    uint16_t* x = (is_v ? p.rows.v : p.rows.k) + (long long)r * p.rows.stride_row + (long long)h * p.rows.stride_head;
+    const unsigned long long e0 = ((unsigned long long)slot * p.c.H + h) * p.c.D;
+    const float qmax = fmt == FMT_INT8 ? 127.0f : 7.0f;
+    int low = 0;
+    for (int c0 = 0; c0 < p.c.D; c0 += p.c.G) {
+        const unsigned long long group = (e0 + c0) / p.c.G;
+        if (WRITE) {
+            float amax = 0.0f;
+            for (int c = c0; c < c0 + p.c.G; c++) amax = fmaxf(amax, fabsf(to_float<TYPE>(x[c])));
+            const uint32_t sb = pack_pair<PATCHKV_ROWS_F16>(__fdiv_rn(amax, qmax), 0.0f);
+            const float s = half_bits_to_float(sb & 0xFFFFu);
+            scales[2 * group] = (uint8_t)sb;
+            scales[2 * group + 1] = (uint8_t)(sb >> 8);
+            const bool usable = s > 0.0f && s <= 65504.0f;
+            for (int c = c0; c < c0 + p.c.G; c++) {
+                float t = usable ? rintf(__fdiv_rn(to_float<TYPE>(x[c]), s)) : 0.0f;
+                const int code = (int)fminf(fmaxf(t, -qmax), qmax);
+                if (fmt == FMT_INT8) codes[e0 + c] = (uint8_t)code;
+                else if ((c & 1) == 0) low = code & 15;                   // D is even: the pair is this thread's
+                else codes[(e0 + c) >> 1] = (uint8_t)(low | (code & 15) << 4);
+            }
+        } else {
+            const float s = scale_at(scales, group);
+            for (int c = c0; c < c0 + p.c.G; c++)
+                x[c] = (uint16_t)pack_pair<TYPE>((float)code_at(codes, fmt, e0 + c) * s, 0.0f);
+        }
+    }
+}
+
+bool rows_overlap(long long n, long long H, long long D, long long stride_row, long long stride_head) {
+    const bool by_row = (H == 1 || stride_head >= D) && (n == 1 || stride_row >= (H - 1) * stride_head + D);
+    const bool by_head = (n == 1 || stride_row >= D) && (H == 1 || stride_head >= (n - 1) * stride_row + D);
+    return !by_row && !by_head;
+}
+
+int check_live_geometry(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, int layer) {
+    const std::string w(who);
+    if (!g || g->struct_size != sizeof(patchkv_geom)) return fail(ctx, PATCHKV_E_INVALID, w + ": null geom or wrong struct_size");
+    if (g->n_layers <= 0 || g->n_kv_heads <= 0 || g->head_dim <= 0 || (g->head_dim & 1) || g->page_tokens <= 0 || g->group <= 0 ||
+        g->head_dim % g->group)
+        return fail(ctx, PATCHKV_E_INVALID, w + ": geometry needs L, H, P > 0, D even, G dividing D");
+    if (layer < 0 || layer >= g->n_layers) return fail(ctx, PATCHKV_E_INVALID, w + ": layer out of range");
+    // element indexes inside a page, and its byte offsets, are 32-bit
+    if ((unsigned long long)g->page_tokens * g->n_kv_heads > (1ull << 29) / g->head_dim)
+        return fail(ctx, PATCHKV_E_UNSUPPORTED, w + ": a page holds more than 2^29 elements");
+    return PATCHKV_OK;
+}
+
+int fill_cache(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, const patchkv_qpool* q, int layer, CacheDev* c) {
+    const std::string w(who);
+    if (!q || q->struct_size != sizeof(patchkv_qpool)) return fail(ctx, PATCHKV_E_INVALID, w + ": null cache or wrong struct_size");
+    if (q->tag < PATCHKV_TAG_INT8 || q->tag > PATCHKV_TAG_K4V4) return fail(ctx, PATCHKV_E_INVALID, w + ": tag of a quantised cache must be INT8, INT4 or K4V4");
+    if (!q->base || (reinterpret_cast<uintptr_t>(q->base) & 15u) || q->n_pages <= 0)
+        return fail(ctx, PATCHKV_E_INVALID, w + ": cache base null or not 16-byte aligned, or no pages");
+    const uint64_t elems = (uint64_t)g->page_tokens * g->n_kv_heads * g->head_dim;
+    if (q->stride_layer < 0 || (q->stride_layer & 15) || (q->stride_page & 15) || q->stride_page < 0 ||
+        (uint64_t)q->stride_page < record_bytes(q->tag, elems, g->group))
+        return fail(ctx, PATCHKV_E_INVALID, w + ": cache strides must be multiples of 16, a page at least one record");
+    memset(c, 0, sizeof(*c));
+    c->base = static_cast<uint8_t*>(q->base) + (long long)layer * q->stride_layer;
+    c->stride_page = q->stride_page;
+    const int kf = k_format(q->tag), vf = v_format(q->tag);
+    c->k_scales = (uint32_t)code_bytes(kf, elems);
+    c->v_codes = c->k_scales + (uint32_t)scale_bytes(kf, elems, g->group);
+    c->v_scales = c->v_codes + (uint32_t)code_bytes(vf, elems);
+    c->n_pages = q->n_pages; c->H = g->n_kv_heads; c->D = g->head_dim; c->P = g->page_tokens; c->G = g->group;
+    c->P_shift = log2_exact(g->page_tokens);
+    c->tag = q->tag;
+    return PATCHKV_OK;
+}
+
+int fill_batch(patchkv_ctx* ctx, const char* who, const patchkv_batch* b, BatchDev* o) {
+    const std::string w(who);
+    if (!b || b->struct_size != sizeof(patchkv_batch)) return fail(ctx, PATCHKV_E_INVALID, w + ": null batch or wrong struct_size");
+    if (b->n_seqs < 0 || b->n_rows < 0 || b->max_rows < 0 || b->max_kv_len < 0 || b->table_stride < 0)
+        return fail(ctx, PATCHKV_E_INVALID, w + ": negative count in the batch");
+    if (b->n_seqs > 0 && b->n_rows > 0 && (!b->row_start || !b->kv_len || (!b->block_table && b->table_stride > 0)))
+        return fail(ctx, PATCHKV_E_INVALID, w + ": null row_start, kv_len or block_table");
+    o->row_start = b->row_start; o->kv_len = b->kv_len; o->pos = b->pos; o->block_table = b->block_table;
+    o->n_seqs = b->n_seqs; o->n_rows = b->n_rows; o->max_rows = b->max_rows; o->max_kv_len = b->max_kv_len;
+    o->table_stride = b->table_stride;
+    return PATCHKV_OK;
+}
+
+namespace {
+
+template <int TYPE, int KF, int VF>
+cudaError_t launch_rows_fast(const RowParams& p, bool write, unsigned grid, cudaStream_t stream) {
+    return write ? launch_pdl(cache_append_kernel<TYPE, KF, VF>, dim3(grid), dim3(kRowThreads), 0, stream, p)
+                 : launch_pdl(cache_read_kernel<TYPE, KF, VF>, dim3(grid), dim3(kRowThreads), 0, stream, p);
+}
+template <int TYPE>
+cudaError_t launch_rows_tag(const RowParams& p, bool write, unsigned grid, cudaStream_t stream) {
+    if (p.c.tag == PATCHKV_TAG_INT8) return launch_rows_fast<TYPE, FMT_INT8, FMT_INT8>(p, write, grid, stream);
+    if (p.c.tag == PATCHKV_TAG_INT4) return launch_rows_fast<TYPE, FMT_INT8, FMT_INT4>(p, write, grid, stream);
+    return launch_rows_fast<TYPE, FMT_INT4, FMT_INT4>(p, write, grid, stream);
+}
+
+int cache_rows(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, const patchkv_qpool* cache, int layer,
+               const patchkv_batch* batch, const patchkv_rows* rows, bool write, cudaStream_t stream) {
+    const std::string w(who);
+    RowParams p;
+    int rc = check_live_geometry(ctx, who, g, layer);
+    if (rc == PATCHKV_OK) rc = fill_cache(ctx, who, g, cache, layer, &p.c);
+    if (rc == PATCHKV_OK) rc = fill_batch(ctx, who, batch, &p.b);
+    if (rc != PATCHKV_OK) return rc;
+    if (!rows || rows->struct_size != sizeof(patchkv_rows)) return fail(ctx, PATCHKV_E_INVALID, w + ": null rows or wrong struct_size");
+    if (rows->type != PATCHKV_ROWS_BF16 && rows->type != PATCHKV_ROWS_F16) return fail(ctx, PATCHKV_E_INVALID, w + ": unknown row type");
+    if (rows->stride_row < 0 || rows->stride_head < 0) return fail(ctx, PATCHKV_E_INVALID, w + ": negative row stride");
+    if (p.b.n_rows == 0 || p.b.n_seqs == 0) return PATCHKV_OK;
+    const uintptr_t ka = reinterpret_cast<uintptr_t>(rows->k), va = reinterpret_cast<uintptr_t>(rows->v);
+    if (!ka || !va || (ka & 1) || (va & 1)) return fail(ctx, PATCHKV_E_INVALID, w + ": null or misaligned rows");
+    if (!write && rows_overlap(p.b.n_rows, p.c.H, p.c.D, rows->stride_row, rows->stride_head))
+        return fail(ctx, PATCHKV_E_INVALID, w + ": rows or heads of the output overlap");
+    p.rows = {static_cast<uint16_t*>(rows->k), static_cast<uint16_t*>(rows->v), rows->stride_row, rows->stride_head};
+    p.status = ctx->d_status;
+    const long long elems = (long long)g->page_tokens * g->n_kv_heads * g->head_dim;
+    const int gs = log2_exact(g->group);
+    const bool fast = g->head_dim % 8 == 0 && gs >= 3 && gs <= 8 && elems % 32 == 0 && (elems / g->group) % 8 == 0 &&
+                      ((ka | va) & 15) == 0 && rows->stride_row % 8 == 0 && rows->stride_head % 8 == 0;
+    p.vecs = (int)((long long)g->n_kv_heads * g->head_dim / 8);
+    p.seg = g->group / 8;
+    const long long threads = (long long)p.b.n_rows * (fast ? p.vecs : 2 * g->n_kv_heads);
+    const long long grid = (threads + kRowThreads - 1) / kRowThreads;
+    if (grid * kRowThreads > (1ll << 32) - 1) return fail(ctx, PATCHKV_E_UNSUPPORTED, w + ": too many rows for one call");
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(ctx, PATCHKV_E_CUDA, "cudaSetDevice failed");
+    const bool f16 = rows->type == PATCHKV_ROWS_F16;
+    if (fast) {
+        PKV_CUDA(ctx, f16 ? launch_rows_tag<PATCHKV_ROWS_F16>(p, write, (unsigned)grid, stream)
+                          : launch_rows_tag<PATCHKV_ROWS_BF16>(p, write, (unsigned)grid, stream));
+        return PATCHKV_OK;
+    }
+    auto kernel = f16 ? (write ? cache_rows_any_kernel<PATCHKV_ROWS_F16, true> : cache_rows_any_kernel<PATCHKV_ROWS_F16, false>)
+                      : (write ? cache_rows_any_kernel<PATCHKV_ROWS_BF16, true> : cache_rows_any_kernel<PATCHKV_ROWS_BF16, false>);
+    kernel<<<(unsigned)grid, kRowThreads, 0, stream>>>(p);
+    PKV_CUDA(ctx, cudaGetLastError());
+    return PATCHKV_OK;
+}
+
+}  // namespace
+}  // namespace patchkv
+
+using namespace patchkv;
+
+extern "C" int patchkv_cache_append(patchkv_ctx* ctx, const patchkv_geom* geom, const patchkv_qpool* cache, int layer,
+                                    const patchkv_batch* batch, const patchkv_rows* rows, void* stream) {
+    if (!ctx) return PATCHKV_E_INVALID;
+    std::lock_guard<std::mutex> lock(ctx->mu);
+    return cache_rows(ctx, "cache_append", geom, cache, layer, batch, rows, true, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int patchkv_cache_read(patchkv_ctx* ctx, const patchkv_geom* geom, const patchkv_qpool* cache, int layer,
+                                  const patchkv_batch* batch, const patchkv_rows* rows, void* stream) {
+    if (!ctx) return PATCHKV_E_INVALID;
+    std::lock_guard<std::mutex> lock(ctx->mu);
+    return cache_rows(ctx, "cache_read", geom, cache, layer, batch, rows, false, static_cast<cudaStream_t>(stream));
+}
