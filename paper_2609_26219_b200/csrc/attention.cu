@@ -4,6 +4,7 @@
 #include <algorithm>
 
 #include "attention.cuh"
+#include "attention_split.cuh"
 
 namespace patchkv {
 
@@ -137,6 +138,83 @@ int fill_pool(patchkv_ctx* ctx, const patchkv_geom* g, const patchkv_pool* q, in
     return PATCHKV_OK;
 }
 
+constexpr int kSms = 148;                        // B200; only sizes launches, so that results don't depend on the context
+
+// Warps and ring depth of the split kernels: sixteen warps hide the latency of the page look-ups and of the operand
+// work best where 128 registers a thread are enough (8 columns), the ring takes what shared memory is left.
+template <int KF, int VF, int D, int NT>
+struct SplitShape {
+    static constexpr int kWarps = KF != FMT_BF16 && NT == 1 ? 16 : 8;
+    static constexpr int kBytes = kTile * ((KF == FMT_BF16 ? 2 * D : KF == FMT_INT8 ? D : D / 2) + (VF == FMT_BF16 ? 2 * D : VF == FMT_INT8 ? D : D / 2) + 32) + 256;
+    static constexpr int kFit = 220 * 1024 / (kWarps * kBytes);
+    static constexpr int kStages = kFit > 4 ? 4 : kFit;
+    static_assert(kStages >= 2, "the ring needs two stages");
+};
+
+int split_warps(int tag, int nt) { return tag != PATCHKV_TAG_BF16 && nt == 1 ? 16 : 8; }
+
+// How a call is served.
+struct AttentionPlan {
+    int nt;                     // column tiles of the split kernel; 0: the element-wise kernel
+    int heads, groups, warps_per_head;
+    int target, max_items;
+    long long item_stride;      // floats
+    uint64_t partial_bytes, items_bytes;
+};
+
+AttentionPlan plan_attention(const patchkv_geom* g, int tag, const patchkv_batch* b, int Hq) {
+    AttentionPlan a;
+    memset(&a, 0, sizeof(a));
+    const int D = g->head_dim, H = g->n_kv_heads;
+    const bool shape = (D == 64 || D == 128) && g->page_tokens % kTile == 0 && (tag == PATCHKV_TAG_BF16 || g->group % 32 == 0);
+    const long long cols = (long long)std::min(b->max_rows, b->n_rows) * (Hq / H);
+    if (!shape || cols == 0 || cols > 16) return a;
+    a.nt = cols <= 8 ? 1 : 2;
+    const int warps = split_warps(tag, a.nt);
+    a.heads = 1;
+    for (int h = 1; h <= warps; h *= 2)
+        if ((H + h - 1) / h * h <= (H + a.heads - 1) / a.heads * a.heads || h <= H) a.heads = h;
+    a.groups = (H + a.heads - 1) / a.heads;
+    a.warps_per_head = warps / a.heads;
+    // Pieces: as many CTAs as there are SMs, one per SM; a sequence leaves one piece partly filled.
+    const int slots = std::max(1, kSms / a.groups);
+    a.target = b->n_seqs >= 2 * slots ? 0 : std::max(slots - b->n_seqs, (slots + 1) / 2);
+    a.max_items = b->n_seqs + a.target;
+    if (a.target) {
+        a.item_stride = 4ll * (D / 16) * a.nt * 32 + 2 * 8 * a.nt;
+        a.items_bytes = ((uint64_t)b->n_seqs * 8 + 15) / 16 * 16;
+        a.partial_bytes = (uint64_t)a.max_items * H * a.item_stride * 4;
+    }
+    return a;
+}
+
+template <int KF, int VF, int D, int NT, bool G32>
+cudaError_t launch_split(const AttentionParams& p, const SplitPlan& pl, int groups, cudaStream_t stream) {
+    using S = SplitShape<KF, VF, D, NT>;
+    using K = SplitKernel<KF, VF, D, NT, S::kStages, S::kWarps, G32>;
+    constexpr int smem = K::kSmem > K::kMerge ? K::kSmem : K::kMerge;
+    auto kernel = attention_split_kernel<KF, VF, D, NT, S::kStages, S::kWarps, G32>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    e = launch_pdl(kernel, dim3(pl.max_items, groups), dim3(S::kWarps * 32), smem, stream, p, pl);
+    if (e != cudaSuccess || pl.target == 0) return e;
+    return launch_pdl(attention_join_kernel<KF == FMT_BF16, D, NT>, dim3(p.b.n_seqs, p.c.H, 4), dim3(kJoinThreads), 0, stream, p, pl);
+}
+template <int D, int NT>
+cudaError_t launch_split_tag(const AttentionParams& p, const SplitPlan& pl, int groups, cudaStream_t s) {
+    const bool g32 = p.c.G == 32;
+    switch (p.c.tag) {
+        case PATCHKV_TAG_BF16: return launch_split<FMT_BF16, FMT_BF16, D, NT, true>(p, pl, groups, s);
+        case PATCHKV_TAG_INT8: return g32 ? launch_split<FMT_INT8, FMT_INT8, D, NT, true>(p, pl, groups, s) : launch_split<FMT_INT8, FMT_INT8, D, NT, false>(p, pl, groups, s);
+        case PATCHKV_TAG_INT4: return g32 ? launch_split<FMT_INT8, FMT_INT4, D, NT, true>(p, pl, groups, s) : launch_split<FMT_INT8, FMT_INT4, D, NT, false>(p, pl, groups, s);
+        default: return g32 ? launch_split<FMT_INT4, FMT_INT4, D, NT, true>(p, pl, groups, s) : launch_split<FMT_INT4, FMT_INT4, D, NT, false>(p, pl, groups, s);
+    }
+}
+
+bool aligned_rows(const void* x, int64_t stride_row, int64_t stride_head) {
+    return (reinterpret_cast<uintptr_t>(x) & 15) == 0 && stride_row % 8 == 0 && stride_head % 8 == 0;
+}
+
 }  // namespace
 }  // namespace patchkv
 
@@ -148,7 +226,8 @@ extern "C" uint64_t patchkv_attention_workspace_bytes(const patchkv_geom* g, int
     if (check_live_geometry(nullptr, "attention", g, 0) != PATCHKV_OK || fill_batch(nullptr, "attention", b, &bd) != PATCHKV_OK ||
         check_attention(nullptr, g, tag, b, n_q_heads, window, sinks) != PATCHKV_OK)
         return 0;
-    return 0;
+    const AttentionPlan a = plan_attention(g, tag, b, n_q_heads);
+    return a.partial_bytes + a.items_bytes;
 }
 
 extern "C" int patchkv_attention(patchkv_ctx* ctx, const patchkv_geom* g, const patchkv_pool* pool, const patchkv_qpool* cache,
@@ -187,6 +266,25 @@ extern "C" int patchkv_attention(patchkv_ctx* ctx, const patchkv_geom* g, const 
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return fail(ctx, PATCHKV_E_CUDA, "cudaSetDevice failed");
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    p.f16 = a->type == PATCHKV_ROWS_F16;
+    const AttentionPlan plan = plan_attention(g, p.c.tag, batch, a->n_q_heads);
+    const bool aligned = aligned_rows(a->q, a->q_stride_row, a->q_stride_head) &&
+                         (!pool || (pool->stride_page % 8 == 0 && pool->stride_token % 8 == 0 && pool->stride_head % 8 == 0 && pool->stride_layer % 8 == 0));
+    if (plan.nt && aligned) {
+        SplitPlan pl;
+        memset(&pl, 0, sizeof(pl));
+        pl.items = static_cast<int32_t*>(a->workspace);
+        pl.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(a->workspace) + plan.items_bytes);
+        pl.regs = 4 * (p.c.D / 16) * plan.nt; pl.cols_max = 8 * plan.nt;
+        pl.item_stride = (int32_t)plan.item_stride;
+        pl.max_items = plan.max_items; pl.target = plan.target;
+        pl.heads = plan.heads; pl.head_groups = plan.groups; pl.warps_per_head = plan.warps_per_head;
+        cudaError_t e;
+        if (p.c.D == 128) e = plan.nt == 1 ? launch_split_tag<128, 1>(p, pl, plan.groups, stream) : launch_split_tag<128, 2>(p, pl, plan.groups, stream);
+        else e = plan.nt == 1 ? launch_split_tag<64, 1>(p, pl, plan.groups, stream) : launch_split_tag<64, 2>(p, pl, plan.groups, stream);
+        PKV_CUDA(ctx, e);
+        return PATCHKV_OK;
+    }
     auto kernel = a->type == PATCHKV_ROWS_F16 ? attention_any_kernel<PATCHKV_ROWS_F16> : attention_any_kernel<PATCHKV_ROWS_BF16>;
     kernel<<<dim3(std::min(p.b.max_rows, p.b.n_rows), p.Hq, p.b.n_seqs), kAnyThreads, 0, stream>>>(p);
     PKV_CUDA(ctx, cudaGetLastError());

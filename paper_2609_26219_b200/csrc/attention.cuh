@@ -13,6 +13,7 @@ struct AttentionParams {
     long long q_stride_row, q_stride_head, out_stride_row, out_stride_head;
     int32_t Hq, share;              // query heads, and query heads per KV head
     int32_t window, sinks;
+    int32_t f16;                    // type of q and out: fp16 (1) or bf16 (0)
     float scale_log2;               // scale * log2(e): the softmax runs on powers of two
     int32_t* status;
 };

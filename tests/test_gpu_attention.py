@@ -204,9 +204,9 @@ def test_nan_and_infinity_in_unseen_tokens(pk, ctx, tag, rows):
         s.k[page, slot], s.v[page, slot] = float("nan"), float("inf")
     else:
         kc, ks, vc, vs = s.lay.split(s.pages[page])
-        for x in (ks, vs):
+        for x, bad in ((ks, np.nan), (vs, np.inf)):        # an infinite K could be a logit of -infinity: a weight of zero
             n = 2 * 2 * 64 // 32
-            x[slot * n:(slot + 1) * n] = np.array([np.inf] * (n // 2), np.float16).view(np.uint8)
+            x[slot * n:(slot + 1) * n] = np.array([bad] * (n // 2), np.float16).view(np.uint8)
         s.dev.copy_(torch.from_numpy(s.pages))
     out = s.run(ctx)
     assert ctx.query_status() == 0
