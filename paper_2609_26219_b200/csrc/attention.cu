@@ -142,20 +142,19 @@ constexpr int kSms = 148;                        // B200; only sizes launches, s
 
 // Warps and ring depth of the split kernels: sixteen warps hide the latency of the page look-ups and of the operand
 // work best where 128 registers a thread are enough (8 columns), the ring takes what shared memory is left.
-template <int KF, int VF, int D, int NT>
+constexpr int split_warps(bool pool, int nc) { return !pool && nc <= 2 ? 16 : 8; }
+template <int KF, int VF, int D, int NC>
 struct SplitShape {
-    static constexpr int kWarps = KF != FMT_BF16 && NT == 1 ? 16 : 8;
+    static constexpr int kWarps = split_warps(KF == FMT_BF16, NC);
     static constexpr int kBytes = kTile * ((KF == FMT_BF16 ? 2 * D : KF == FMT_INT8 ? D : D / 2) + (VF == FMT_BF16 ? 2 * D : VF == FMT_INT8 ? D : D / 2) + 32) + 256;
     static constexpr int kFit = 220 * 1024 / (kWarps * kBytes);
     static constexpr int kStages = kFit > 4 ? 4 : kFit;
     static_assert(kStages >= 2, "the ring needs two stages");
 };
 
-int split_warps(int tag, int nt) { return tag != PATCHKV_TAG_BF16 && nt == 1 ? 16 : 8; }
-
 // How a call is served.
 struct AttentionPlan {
-    int nt;                     // column tiles of the split kernel; 0: the element-wise kernel
+    int nc;                     // columns of a lane of the split kernel; 0: the element-wise kernel
     int heads, groups, warps_per_head;
     int target, max_items;
     long long item_stride;      // floats
@@ -166,13 +165,14 @@ AttentionPlan plan_attention(const patchkv_geom* g, int tag, const patchkv_batch
     AttentionPlan a;
     memset(&a, 0, sizeof(a));
     const int D = g->head_dim, H = g->n_kv_heads;
-    const bool shape = (D == 64 || D == 128) && g->page_tokens % kTile == 0 && (tag == PATCHKV_TAG_BF16 || g->group % 32 == 0);
+    const bool pool = tag == PATCHKV_TAG_BF16;
+    const bool shape = (D == 64 || D == 128) && g->page_tokens % kTile == 0 && (pool || g->group % 32 == 0);
     const long long cols = (long long)std::min(b->max_rows, b->n_rows) * (Hq / H);
     if (!shape || cols == 0 || cols > 16) return a;
-    a.nt = cols <= 8 ? 1 : 2;
-    const int warps = split_warps(tag, a.nt);
+    a.nc = cols <= 4 ? 1 : cols <= 8 ? 2 : 4;
+    const int warps = split_warps(pool, a.nc);
     a.heads = 1;
-    for (int h = 1; h <= warps; h *= 2)
+    for (int h = 2; h <= warps; h *= 2)         // the most heads a CTA can take without more idle warps
         if ((H + h - 1) / h * h <= (H + a.heads - 1) / a.heads * a.heads || h <= H) a.heads = h;
     a.groups = (H + a.heads - 1) / a.heads;
     a.warps_per_head = warps / a.heads;
@@ -181,34 +181,41 @@ AttentionPlan plan_attention(const patchkv_geom* g, int tag, const patchkv_batch
     a.target = b->n_seqs >= 2 * slots ? 0 : std::max(slots - b->n_seqs, (slots + 1) / 2);
     a.max_items = b->n_seqs + a.target;
     if (a.target) {
-        a.item_stride = 4ll * (D / 16) * a.nt * 32 + 2 * 8 * a.nt;
+        a.item_stride = (a.nc == 1 ? 2 : 2 * a.nc) * (D / 16) * 32 + 2 * 4 * a.nc;
         a.items_bytes = ((uint64_t)b->n_seqs * 8 + 15) / 16 * 16;
         a.partial_bytes = (uint64_t)a.max_items * H * a.item_stride * 4;
     }
     return a;
 }
 
-template <int KF, int VF, int D, int NT, bool G32>
+template <int KF, int VF, int D, int NC, bool G32>
 cudaError_t launch_split(const AttentionParams& p, const SplitPlan& pl, int groups, cudaStream_t stream) {
-    using S = SplitShape<KF, VF, D, NT>;
-    using K = SplitKernel<KF, VF, D, NT, S::kStages, S::kWarps, G32>;
+    using S = SplitShape<KF, VF, D, NC>;
+    using K = SplitKernel<KF, VF, D, NC, S::kStages, S::kWarps, G32>;
     constexpr int smem = K::kSmem > K::kMerge ? K::kSmem : K::kMerge;
-    auto kernel = attention_split_kernel<KF, VF, D, NT, S::kStages, S::kWarps, G32>;
+    auto kernel = attention_split_kernel<KF, VF, D, NC, S::kStages, S::kWarps, G32>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     e = launch_pdl(kernel, dim3(pl.max_items, groups), dim3(S::kWarps * 32), smem, stream, p, pl);
     if (e != cudaSuccess || pl.target == 0) return e;
-    return launch_pdl(attention_join_kernel<KF == FMT_BF16, D, NT>, dim3(p.b.n_seqs, p.c.H, 4), dim3(kJoinThreads), 0, stream, p, pl);
+    return launch_pdl(attention_join_kernel<KF == FMT_BF16, D, NC>, dim3(p.b.n_seqs, p.c.H, (NC == 1 ? 2 : 2 * NC) * (D / 16) / 4), dim3(kJoinThreads), 0, stream, p, pl);
 }
-template <int D, int NT>
+template <int D, int NC, bool G32>
 cudaError_t launch_split_tag(const AttentionParams& p, const SplitPlan& pl, int groups, cudaStream_t s) {
-    const bool g32 = p.c.G == 32;
     switch (p.c.tag) {
-        case PATCHKV_TAG_BF16: return launch_split<FMT_BF16, FMT_BF16, D, NT, true>(p, pl, groups, s);
-        case PATCHKV_TAG_INT8: return g32 ? launch_split<FMT_INT8, FMT_INT8, D, NT, true>(p, pl, groups, s) : launch_split<FMT_INT8, FMT_INT8, D, NT, false>(p, pl, groups, s);
-        case PATCHKV_TAG_INT4: return g32 ? launch_split<FMT_INT8, FMT_INT4, D, NT, true>(p, pl, groups, s) : launch_split<FMT_INT8, FMT_INT4, D, NT, false>(p, pl, groups, s);
-        default: return g32 ? launch_split<FMT_INT4, FMT_INT4, D, NT, true>(p, pl, groups, s) : launch_split<FMT_INT4, FMT_INT4, D, NT, false>(p, pl, groups, s);
+        case PATCHKV_TAG_INT8: return launch_split<FMT_INT8, FMT_INT8, D, NC, G32>(p, pl, groups, s);
+        case PATCHKV_TAG_INT4: return launch_split<FMT_INT8, FMT_INT4, D, NC, G32>(p, pl, groups, s);
+        default: return launch_split<FMT_INT4, FMT_INT4, D, NC, G32>(p, pl, groups, s);
     }
+}
+template <int D, int NC>
+cudaError_t launch_split_group(const AttentionParams& p, const SplitPlan& pl, int groups, cudaStream_t s) {
+    if (p.c.tag == PATCHKV_TAG_BF16) return launch_split<FMT_BF16, FMT_BF16, D, NC, true>(p, pl, groups, s);
+    return p.c.G == 32 ? launch_split_tag<D, NC, true>(p, pl, groups, s) : launch_split_tag<D, NC, false>(p, pl, groups, s);
+}
+template <int D>
+cudaError_t launch_split_columns(const AttentionParams& p, const SplitPlan& pl, int nc, int groups, cudaStream_t s) {
+    return nc == 1 ? launch_split_group<D, 1>(p, pl, groups, s) : nc == 2 ? launch_split_group<D, 2>(p, pl, groups, s) : launch_split_group<D, 4>(p, pl, groups, s);
 }
 
 bool aligned_rows(const void* x, int64_t stride_row, int64_t stride_head) {
@@ -270,19 +277,16 @@ extern "C" int patchkv_attention(patchkv_ctx* ctx, const patchkv_geom* g, const 
     const AttentionPlan plan = plan_attention(g, p.c.tag, batch, a->n_q_heads);
     const bool aligned = aligned_rows(a->q, a->q_stride_row, a->q_stride_head) &&
                          (!pool || (pool->stride_page % 8 == 0 && pool->stride_token % 8 == 0 && pool->stride_head % 8 == 0 && pool->stride_layer % 8 == 0));
-    if (plan.nt && aligned) {
+    if (plan.nc && aligned) {
         SplitPlan pl;
         memset(&pl, 0, sizeof(pl));
         pl.items = static_cast<int32_t*>(a->workspace);
         pl.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(a->workspace) + plan.items_bytes);
-        pl.regs = 4 * (p.c.D / 16) * plan.nt; pl.cols_max = 8 * plan.nt;
         pl.item_stride = (int32_t)plan.item_stride;
         pl.max_items = plan.max_items; pl.target = plan.target;
-        pl.heads = plan.heads; pl.head_groups = plan.groups; pl.warps_per_head = plan.warps_per_head;
-        cudaError_t e;
-        if (p.c.D == 128) e = plan.nt == 1 ? launch_split_tag<128, 1>(p, pl, plan.groups, stream) : launch_split_tag<128, 2>(p, pl, plan.groups, stream);
-        else e = plan.nt == 1 ? launch_split_tag<64, 1>(p, pl, plan.groups, stream) : launch_split_tag<64, 2>(p, pl, plan.groups, stream);
-        PKV_CUDA(ctx, e);
+        pl.heads = plan.heads; pl.warps_per_head = plan.warps_per_head;
+        PKV_CUDA(ctx, p.c.D == 128 ? launch_split_columns<128>(p, pl, plan.nc, plan.groups, stream)
+                                   : launch_split_columns<64>(p, pl, plan.nc, plan.groups, stream));
         return PATCHKV_OK;
     }
     auto kernel = a->type == PATCHKV_ROWS_F16 ? attention_any_kernel<PATCHKV_ROWS_F16> : attention_any_kernel<PATCHKV_ROWS_BF16>;
