@@ -4,6 +4,7 @@
 #include <algorithm>
 
 #include "attention.cuh"
+#include "attention_rows.cuh"
 #include "attention_split.cuh"
 
 namespace patchkv {
@@ -154,21 +155,33 @@ struct SplitShape {
 
 // How a call is served.
 struct AttentionPlan {
-    int nc;                     // columns of a lane of the split kernel; 0: the element-wise kernel
+    int nc;                     // columns of a lane of the split kernel; 0: another kernel
+    int row_tiles, row_splits;  // CTAs along the query vectors of a sequence, and along the tokens, of the row kernel; 0: another
     int heads, groups, warps_per_head;
     int target, max_items;
     long long item_stride;      // floats
     uint64_t partial_bytes, items_bytes;
 };
 
-AttentionPlan plan_attention(const patchkv_geom* g, int tag, const patchkv_batch* b, int Hq) {
+AttentionPlan plan_attention(const patchkv_geom* g, int tag, const patchkv_batch* b, int Hq, int window, int sinks) {
     AttentionPlan a;
     memset(&a, 0, sizeof(a));
     const int D = g->head_dim, H = g->n_kv_heads;
     const bool pool = tag == PATCHKV_TAG_BF16;
     const bool shape = (D == 64 || D == 128) && g->page_tokens % kTile == 0 && (pool || g->group % 32 == 0);
     const long long cols = (long long)std::min(b->max_rows, b->n_rows) * (Hq / H);
-    if (!shape || cols == 0 || cols > 16) return a;
+    if (!shape || cols == 0) return a;
+    if (cols > 16) {
+        // Whole CTAs along the query vectors; where they leave SMs idle the tokens are split, two steps a piece at least.
+        const long long tiles = (cols + 2 * kRowTile - 1) / (2 * kRowTile), ctas = tiles * H * b->n_seqs;
+        if (ctas > 1 << 24 || cols > 1 << 30) return a;
+        long long steps = (b->max_kv_len + kRowTile - 1) / kRowTile;
+        if (window > 0) steps = std::min(steps, ((long long)window + sinks + b->max_rows) / kRowTile + 3);
+        a.row_tiles = (int)tiles;
+        a.row_splits = (int)std::max(1ll, std::min((long long)kSms / ctas, steps / 2));
+        if (a.row_splits > 1) a.partial_bytes = (uint64_t)a.row_splits * b->n_rows * Hq * (D + 2) * 4;
+        return a;
+    }
     a.nc = cols <= 4 ? 1 : cols <= 8 ? 2 : 4;
     const int warps = split_warps(pool, a.nc);
     a.heads = 1;
@@ -218,6 +231,25 @@ cudaError_t launch_split_columns(const AttentionParams& p, const SplitPlan& pl, 
     return nc == 1 ? launch_split_group<D, 1>(p, pl, groups, s) : nc == 2 ? launch_split_group<D, 2>(p, pl, groups, s) : launch_split_group<D, 4>(p, pl, groups, s);
 }
 
+template <int KF, int VF, int D>
+cudaError_t launch_rows(const AttentionParams& p, const RowsPlan& pl, cudaStream_t stream) {
+    auto kernel = attention_rows_kernel<KF, VF, D>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsSmem<D>::kLaunch);
+    if (e != cudaSuccess) return e;
+    e = launch_pdl(kernel, dim3(pl.tiles * p.c.H * p.b.n_seqs * pl.splits), dim3(kRowsThreads), RowsSmem<D>::kLaunch, stream, p, pl);
+    if (e != cudaSuccess || pl.splits == 1) return e;
+    return launch_pdl(attention_rows_join_kernel<D>, dim3((unsigned)(((long long)p.b.n_rows * p.Hq + 3) / 4)), dim3(128), 0, stream, p, pl);
+}
+template <int D>
+cudaError_t launch_rows_tag(const AttentionParams& p, const RowsPlan& pl, cudaStream_t s) {
+    switch (p.c.tag) {
+        case PATCHKV_TAG_BF16: return launch_rows<FMT_BF16, FMT_BF16, D>(p, pl, s);
+        case PATCHKV_TAG_INT8: return launch_rows<FMT_INT8, FMT_INT8, D>(p, pl, s);
+        case PATCHKV_TAG_INT4: return launch_rows<FMT_INT8, FMT_INT4, D>(p, pl, s);
+        default: return launch_rows<FMT_INT4, FMT_INT4, D>(p, pl, s);
+    }
+}
+
 bool aligned_rows(const void* x, int64_t stride_row, int64_t stride_head) {
     return (reinterpret_cast<uintptr_t>(x) & 15) == 0 && stride_row % 8 == 0 && stride_head % 8 == 0;
 }
@@ -233,7 +265,7 @@ extern "C" uint64_t patchkv_attention_workspace_bytes(const patchkv_geom* g, int
     if (check_live_geometry(nullptr, "attention", g, 0) != PATCHKV_OK || fill_batch(nullptr, "attention", b, &bd) != PATCHKV_OK ||
         check_attention(nullptr, g, tag, b, n_q_heads, window, sinks) != PATCHKV_OK)
         return 0;
-    const AttentionPlan a = plan_attention(g, tag, b, n_q_heads);
+    const AttentionPlan a = plan_attention(g, tag, b, n_q_heads, window, sinks);
     return a.partial_bytes + a.items_bytes;
 }
 
@@ -274,7 +306,7 @@ extern "C" int patchkv_attention(patchkv_ctx* ctx, const patchkv_geom* g, const 
     if (!guard.ok) return fail(ctx, PATCHKV_E_CUDA, "cudaSetDevice failed");
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     p.f16 = a->type == PATCHKV_ROWS_F16;
-    const AttentionPlan plan = plan_attention(g, p.c.tag, batch, a->n_q_heads);
+    const AttentionPlan plan = plan_attention(g, p.c.tag, batch, a->n_q_heads, a->window, a->sinks);
     const bool aligned = aligned_rows(a->q, a->q_stride_row, a->q_stride_head) &&
                          (!pool || (pool->stride_page % 8 == 0 && pool->stride_token % 8 == 0 && pool->stride_head % 8 == 0 && pool->stride_layer % 8 == 0));
     if (plan.nc && aligned) {
@@ -287,6 +319,11 @@ extern "C" int patchkv_attention(patchkv_ctx* ctx, const patchkv_geom* g, const 
         pl.heads = plan.heads; pl.warps_per_head = plan.warps_per_head;
         PKV_CUDA(ctx, p.c.D == 128 ? launch_split_columns<128>(p, pl, plan.nc, plan.groups, stream)
                                    : launch_split_columns<64>(p, pl, plan.nc, plan.groups, stream));
+        return PATCHKV_OK;
+    }
+    if (plan.row_tiles && aligned && aligned_rows(a->out, a->out_stride_row, a->out_stride_head)) {
+        const RowsPlan pl = {static_cast<float*>(a->workspace), plan.row_tiles, plan.row_splits};
+        PKV_CUDA(ctx, p.c.D == 128 ? launch_rows_tag<128>(p, pl, stream) : launch_rows_tag<64>(p, pl, stream));
         return PATCHKV_OK;
     }
     auto kernel = a->type == PATCHKV_ROWS_F16 ? attention_any_kernel<PATCHKV_ROWS_F16> : attention_any_kernel<PATCHKV_ROWS_BF16>;

@@ -692,7 +692,7 @@ __device__ __forceinline__ Item find_item(const AttentionParams& p, const SplitP
 }
 
 template <int KF, int VF, int D, int NC, int STAGES, int WARPS, bool G32>
-__global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const AttentionParams p, const SplitPlan pl) {
+__global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ SplitPlan pl) {
     using K = SplitKernel<KF, VF, D, NC, STAGES, WARPS, G32>;
     extern __shared__ __align__(16) uint8_t smem[];
     pdl_trigger();
