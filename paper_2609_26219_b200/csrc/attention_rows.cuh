@@ -14,6 +14,8 @@
 // As in the split kernel the softmax reference is only moved (and O rescaled) when a logit exceeds it by more than 8.
 #pragma once
 
+#include <stddef.h>
+
 #include "attention_split.cuh"
 
 namespace patchkv {
@@ -106,11 +108,11 @@ struct RowsSmem {
 };
 struct RowsBars {
     uint64_t q_ready[2], s_ready[2], p_ready[2], o_ready[2], k_full[2], k_empty[2], v_full[2], v_empty[2], drained;
-    uint32_t absent[4][4];                      // per step (mod 4): tokens whose page is out of range
+    alignas(16) uint32_t absent[4][4];                      // per step (mod 4): tokens whose page is out of range
     uint32_t tmem;
     int32_t abort, lo, hi, lost;                // lost: a value that is not finite was taken out of a tile that needs a mask
 };
-static_assert(sizeof(RowsBars) <= 512, "barrier area");
+static_assert(sizeof(RowsBars) <= 512 && offsetof(RowsBars, absent) % 16 == 0, "barrier area");
 
 // Steps of 128 tokens that the rows between positions lo and hi see (as tile_range, in other units).
 __device__ __forceinline__ TileRange step_range(const AttentionParams& p, int kv, int lo_pos, int hi_pos) {
@@ -260,26 +262,18 @@ struct RowsKernel {
                 fence_async_smem();
                 mbar_arrive(&bars.k_full[st]);
                 cp_wait<0>();
-                if (masked) {
-#pragma unroll
-                    for (int i = 0; i < kPass; i++)
-#pragma unroll
-                        for (int q = 0; q < 4; q++) {
-                            const uint32_t a = vb + swizzled(tok0 + i * kTok, q * kPer + c);
-                            uint4 x = lds128(a);
-                            if (finite_only<0x7F80u>(x)) { sts128(a, x.x, x.y, x.z, x.w); bars.lost = 1; }
-                        }
-                }
+                if (masked) clean<0x7F80u>(vb, tok0, c, 1, kPer);
                 fence_async_smem();
                 mbar_arrive(&bars.v_full[st]);
             } else {
 #pragma unroll
-                for (int i = 0; i < kPass; i++) store_operands<KF>(kb, tok0 + i * kTok, c, kw[i], ks[i], m0, m1, false);
+                for (int i = 0; i < kPass; i++) store_operands<KF>(kb, tok0 + i * kTok, c, kw[i], ks[i], m0, m1);
                 fence_async_smem();
                 mbar_arrive(&bars.k_full[st]);
                 if (!wait_warp(&bars.v_empty[st], parity)) return;
 #pragma unroll
-                for (int i = 0; i < kPass; i++) store_operands<VF>(vb, tok0 + i * kTok, c, vw[i], vs[i], m0, m1, masked);
+                for (int i = 0; i < kPass; i++) store_operands<VF>(vb, tok0 + i * kTok, c, vw[i], vs[i], m0, m1);
+                if (masked) clean<0x7C00u>(vb, tok0, c, 4, 1);
                 fence_async_smem();
                 mbar_arrive(&bars.v_full[st]);
             }
@@ -317,9 +311,20 @@ struct RowsKernel {
         }
         return found;
     }
+    // In a step that needs a mask a value that is not finite must not meet the weight 0 of a row that does not see it: it is taken out
+    // here and given to the rows that see it at the end.  Chunks of the thread: c * lead + q * apart, q = 0 .. 3.
+    template <uint32_t EXP>
+    __device__ __forceinline__ void clean(uint32_t mat, int tok0, int c, int lead, int apart) {
+#pragma unroll 1
+        for (int i = 0; i < kPer * 4; i++) {
+            const uint32_t a = mat + swizzled(tok0 + (i >> 2) * (32 / kPer), c * lead + (i & 3) * apart);
+            uint4 x = lds128(a);
+            if (finite_only<EXP>(x)) { sts128(a, x.x, x.y, x.z, x.w); bars.lost = 1; }
+        }
+    }
     // The 32 channels of a thread into its token's row.
     template <int F>
-    __device__ __forceinline__ void store_operands(uint32_t mat, int tok, int c, const uint32_t (&w)[8], uint32_t scale, uint32_t m0, uint32_t m1, bool clean) {
+    __device__ __forceinline__ void store_operands(uint32_t mat, int tok, int c, const uint32_t (&w)[8], uint32_t scale, uint32_t m0, uint32_t m1) {
         const uint32_t s = scale | scale << 16;
         const uint32_t flip = c & 2;                            // the two halves of the channels write different banks
 #pragma unroll
@@ -331,7 +336,6 @@ struct RowsKernel {
                 const uint2 a = operands8(flip ? w[(2 * i) ^ 4] : w[2 * i], s), b = operands8(flip ? w[(2 * i + 1) ^ 4] : w[2 * i + 1], s);
                 o = make_uint4(a.x, a.y, b.x, b.y);
             }
-            if (clean && finite_only<0x7C00u>(o)) bars.lost = 1;
             sts128(mat + swizzled(tok, 4 * c + (i ^ flip)), o.x, o.y, o.z, o.w);
         }
     }
@@ -379,6 +383,19 @@ struct RowsKernel {
         }
     }
 
+    // Bit c: this row sees column c0 + c.
+    __device__ __forceinline__ static uint32_t seen(int c0, int a, int b, int s, const uint4& absent, int k) {
+        auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u; };      // bits [0, n)
+        const uint32_t gone = k == 0 ? absent.x : k == 1 ? absent.y : k == 2 ? absent.z : absent.w;
+        return below(b + 1 - c0) & (~below(a - c0) | below(s - c0)) & ~gone;
+    }
+    // What a row does not see becomes the value whose weight is zero: times the factor minus infinity.
+    __device__ __forceinline__ static void mask_chunk(float (&x)[32], uint32_t seen, float factor) {
+        const float none = factor < 0.0f ? INFINITY : -INFINITY;
+#pragma unroll
+        for (int c = 0; c < 32; c++) x[c] = seen >> c & 1u ? x[c] : none;
+    }
+
     // ---- softmax: one thread per query vector
     __device__ __forceinline__ void softmax(int i, int first, int m, int m_end, uint32_t tmem, const RowsPlan& pl, int split) {
         const int r = threadIdx.x & 127;
@@ -391,7 +408,7 @@ struct RowsKernel {
             const uint16_t* q = p.q + (long long)row * p.q_stride_row + (long long)hq * p.q_stride_head;
             const uint32_t mat = smem + S::kQ + i * S::kMat;
             if constexpr (kPool) {
-#pragma unroll
+#pragma unroll 4
                 for (int c = 0; c < D / 8; c++) {
                     const uint4 x = live ? __ldg(reinterpret_cast<const uint4*>(q) + c) : make_uint4(0, 0, 0, 0);
                     sts128(mat + swizzled(r, c), x.x, x.y, x.z, x.w);
@@ -399,7 +416,7 @@ struct RowsKernel {
             } else {
                 // scaled so that the largest magnitude lies in [2^13, 2^14); a vector with a NaN or an infinity gives NaN
                 float amax = 0.0f, bad = 0.0f;
-#pragma unroll
+#pragma unroll 4
                 for (int c = 0; c < D / 8; c++) {
                     const uint4 x = live ? __ldg(reinterpret_cast<const uint4*>(q) + c) : make_uint4(0, 0, 0, 0);
                     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
@@ -414,7 +431,7 @@ struct RowsKernel {
                 const int shift = amax > 0.0f ? min(13 - e, 120) : 0;
                 const float up = bad == 0.0f ? exp2i(shift) : 0.0f;
                 factor = p.scale_log2 * exp2i(-shift) + bad;
-#pragma unroll
+#pragma unroll 2
                 for (int c = 0; c < D / 8; c++) {
                     const uint4 x = live && bad == 0.0f ? __ldg(reinterpret_cast<const uint4*>(q) + c) : make_uint4(0, 0, 0, 0);
                     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
@@ -433,55 +450,48 @@ struct RowsKernel {
         }
         fence_async_smem();
         mbar_arrive(&bars.q_ready[i]);
+        // A mask is minus infinity over the factor: a factor of zero is one that leaves no logit, a NaN enters at the end.
+        const bool broken = factor != factor;
+        if (broken) factor = 1.0f;
+        if (factor == 0.0f) factor = 1.17549435e-38f;
         const uint32_t lanes = (uint32_t)((threadIdx.x >> 5) & 3) << 21;              // the warp's quarter of the TMEM lanes
         const uint32_t s_at = tmem + lanes + i * kRowTile, o_at = tmem + lanes + 2 * kRowTile + i * kRowTile;
-        float ref = kNoMax, sum = 0.0f;
+        float ref = kNoMax;
+        f32x2 sum2 = pack2(0.0f, 0.0f);
         const int n = end - begin;
         for (int j = 0; j < n; j++) {
             const int t0 = range.tile(begin + j) * kRowTile;
             if (!wait_warp(&bars.s_ready[i], j & 1)) return;
             tc_after();
-            const bool clear = whole(t0);
             // Columns of the step this row sees: [a, b] and [0, s); what its pages don't hold is in `absent`.
+            const uint4 absent = lds128(smem_u32(bars.absent[j & 3]));
+            const bool plain = whole(t0) && (absent.x | absent.y | absent.z | absent.w) == 0;
             const int b = min(pos, kv - 1) - t0, a = p.window > 0 ? max(pos - p.window + 1, 0) - t0 : -t0, s = p.sinks - t0;
-            uint32_t absent[4] = {0, 0, 0, 0};
-#pragma unroll
-            for (int k = 0; k < 4; k++) absent[k] = bars.absent[j & 3][k];
-            const bool plain = clear && (absent[0] | absent[1] | absent[2] | absent[3]) == 0;
-            auto load = [&](float (&x)[32], int k) {
-                tc_ld32(x, s_at + 32 * k);
-                tc_wait_ld();
-                if (!plain) {
-#pragma unroll
-                    for (int c = 0; c < 32; c++) {
-                        const int col = 32 * k + c;
-                        const bool in = col <= b && (col >= a || col < s) && !(absent[k] >> c & 1u);
-                        if (!in) x[c] = -INFINITY;
-                    }
-                }
-            };
+            // The loops over the step's four chunks stay loops: three roles run different code on an SM, and unrolled it does not
+            // stay in the instruction cache (1270 us for 8192 rows of prompt, most of it waiting for instructions).
             float top = -INFINITY;
-#pragma unroll
+#pragma unroll 1
             for (int k = 0; k < 4; k++) {
                 float x[32];
-                load(x, k);
-                if (!plain || factor < 0.0f) {                  // masked entries stay -inf under a negative factor
+                tc_ld32(x, s_at + 32 * k);
+                tc_wait_ld();
+                if (!plain) mask_chunk(x, seen(32 * k, a, b, s, absent, k), factor);
+                float y[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                if (factor < 0.0f)
 #pragma unroll
-                    for (int c = 0; c < 32; c++) top = fmaxf(top, x[c] == -INFINITY ? -INFINITY : x[c] * factor);
-                } else {
-                    float y = x[0];
+                    for (int c = 0; c < 32; c++) x[c] = -x[c];
 #pragma unroll
-                    for (int c = 1; c < 32; c++) y = fmaxf(y, x[c]);
-                    top = fmaxf(top, y * factor);
-                }
+                for (int c = 0; c < 32; c += 2) y[(c >> 1) & 3] = fmaxf(y[(c >> 1) & 3], fmaxf(x[c], x[c + 1]));
+                top = fmaxf(top, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
             }
+            top = top == -INFINITY ? top : top * fabsf(factor);
             const bool move = top > ref + 8.0f;
             if (__any_sync(0xFFFFFFFFu, move)) {
                 const float to = move ? top : ref, keep = fast_exp2(ref - to);
                 ref = to;
-                sum *= keep;
+                sum2 = mul2(sum2, pack2(keep, keep));
                 if (j > 0)                                      // the products of the steps before are done: s_ready came behind them
-#pragma unroll
+#pragma unroll 1
                     for (int k = 0; k < D / 32; k++) {
                         float o[32];
                         tc_ld32(o, o_at + 32 * k);
@@ -492,20 +502,23 @@ struct RowsKernel {
                     }
             }
             // P lies over the first half of S: a chunk of 32 logits is read before the chunk of 16 columns over it is written
-#pragma unroll
+            const f32x2 factor2 = pack2(factor, factor), ref2 = pack2(-ref, -ref);
+#pragma unroll 1
             for (int k = 0; k < 4; k++) {
                 float x[32];
-                load(x, k);
+                tc_ld32(x, s_at + 32 * k);
+                tc_wait_ld();
+                if (!plain) mask_chunk(x, seen(32 * k, a, b, s, absent, k), factor);
                 uint32_t w[16];
 #pragma unroll
-                for (int c = 0; c < 32; c++) {
-                    float y = fmaf(x[c], factor, -ref);
-                    if (!plain) y = x[c] == -INFINITY ? -INFINITY : y;
-                    x[c] = fast_exp2(y);
-                    sum += x[c];
+                for (int c = 0; c < 16; c++) {
+                    float u, v;
+                    unpack2(fma2(pack2(x[2 * c], x[2 * c + 1]), factor2, ref2), u, v);
+                    u = fast_exp2(u);
+                    v = fast_exp2(v);
+                    sum2 = add2(sum2, pack2(u, v));
+                    w[c] = kPool ? bf162_bits(u, v) : half2_bits(u, v);
                 }
-#pragma unroll
-                for (int c = 0; c < 16; c++) w[c] = kPool ? bf162_bits(x[2 * c], x[2 * c + 1]) : half2_bits(x[2 * c], x[2 * c + 1]);
                 tc_st16(s_at + 16 * k, w);
             }
             tc_wait_st();
@@ -514,12 +527,16 @@ struct RowsKernel {
         }
         if (n > 0 && !wait_warp(&bars.o_ready[i], 0)) return;
         tc_after();
+        float sum, sum_odd;
+        unpack2(sum2, sum, sum_odd);
+        sum += sum_odd;
+        if (broken && sum != 0.0f) sum = __uint_as_float(0x7FC00000u);
         const bool lost = *reinterpret_cast<volatile int32_t*>(&bars.lost) != 0;
         const float inv = pl.splits > 1 ? 1.0f : (sum != 0.0f ? 1.0f / sum : 0.0f);
         const long long vec = (long long)row * p.Hq + hq;
         float* part = pl.partial + ((long long)split * p.b.n_rows * p.Hq + vec) * D;
         uint16_t* out = p.out + (long long)row * p.out_stride_row + (long long)hq * p.out_stride_head;
-#pragma unroll
+#pragma unroll 1
         for (int k = 0; k < D / 32; k++) {
             float o[32];
             if (n > 0) {
