@@ -161,7 +161,11 @@ struct AttentionPlan {
     int target, max_items;
     long long item_stride;      // floats
     uint64_t partial_bytes, items_bytes;
+    int image_steps;            // steps of a sequence whose operands are laid out in the workspace first; 0: none
+    uint64_t image_bytes, meta_bytes;
 };
+
+constexpr uint64_t kMaxImageBytes = 1ull << 30;
 
 AttentionPlan plan_attention(const patchkv_geom* g, int tag, const patchkv_batch* b, int Hq, int window, int sinks) {
     AttentionPlan a;
@@ -179,6 +183,13 @@ AttentionPlan plan_attention(const patchkv_geom* g, int tag, const patchkv_batch
         if (window > 0) steps = std::min(steps, ((long long)window + sinks + b->max_rows) / kRowTile + 3);
         a.row_tiles = (int)tiles;
         a.row_splits = (int)std::max(1ll, std::min((long long)kSms / ctas, steps / 2));
+        // Images pay where a token is needed by several CTAs, up to a gigabyte of workspace.
+        const uint64_t all_steps = ((uint64_t)b->max_kv_len + kRowTile - 1) / kRowTile, images = all_steps * H * b->n_seqs;
+        if (tiles > 1 && images > 0 && images <= kMaxImageBytes / (4ull * kRowTile * D)) {
+            a.image_steps = (int)all_steps;
+            a.image_bytes = images * 4 * kRowTile * D;
+            a.meta_bytes = images * 32;
+        }
         if (a.row_splits > 1) a.partial_bytes = (uint64_t)a.row_splits * b->n_rows * Hq * (D + 2) * 4;
         return a;
     }
@@ -231,12 +242,24 @@ cudaError_t launch_split_columns(const AttentionParams& p, const SplitPlan& pl, 
     return nc == 1 ? launch_split_group<D, 1>(p, pl, groups, s) : nc == 2 ? launch_split_group<D, 2>(p, pl, groups, s) : launch_split_group<D, 4>(p, pl, groups, s);
 }
 
-template <int KF, int VF, int D>
-cudaError_t launch_rows(const AttentionParams& p, const RowsPlan& pl, cudaStream_t stream) {
-    auto kernel = attention_rows_kernel<KF, VF, D>;
+template <int KF, int VF, int D, bool IMAGE>
+cudaError_t launch_rows_kernel(const AttentionParams& p, const RowsPlan& pl, cudaStream_t stream) {
+    auto kernel = attention_rows_kernel<KF, VF, D, IMAGE>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsSmem<D>::kLaunch);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(kernel, dim3(pl.tiles * p.c.H * p.b.n_seqs * pl.splits), dim3(kRowsThreads), RowsSmem<D>::kLaunch, stream, p, pl);
+    return launch_pdl(kernel, dim3(pl.tiles * p.c.H * p.b.n_seqs * pl.splits), dim3(rows_threads(IMAGE)), RowsSmem<D>::kLaunch, stream, p, pl);
+}
+template <int KF, int VF, int D>
+cudaError_t launch_rows(const AttentionParams& p, const RowsPlan& pl, cudaStream_t stream) {
+    cudaError_t e;
+    if (pl.images) {
+        e = launch_pdl(attention_image_kernel<KF, VF, D>, dim3(pl.steps, p.c.H, p.b.n_seqs), dim3(kImageThreads), 0, stream, p, pl);
+        if (e != cudaSuccess) return e;
+        constexpr int F = KF == FMT_BF16 ? FMT_BF16 : FMT_INT8;
+        e = launch_rows_kernel<F, F, D, true>(p, pl, stream);
+    } else {
+        e = launch_rows_kernel<KF, VF, D, false>(p, pl, stream);
+    }
     if (e != cudaSuccess || pl.splits == 1) return e;
     return launch_pdl(attention_rows_join_kernel<D>, dim3((unsigned)(((long long)p.b.n_rows * p.Hq + 3) / 4)), dim3(128), 0, stream, p, pl);
 }
@@ -266,7 +289,7 @@ extern "C" uint64_t patchkv_attention_workspace_bytes(const patchkv_geom* g, int
         check_attention(nullptr, g, tag, b, n_q_heads, window, sinks) != PATCHKV_OK)
         return 0;
     const AttentionPlan a = plan_attention(g, tag, b, n_q_heads, window, sinks);
-    return a.partial_bytes + a.items_bytes;
+    return a.partial_bytes + a.items_bytes + a.image_bytes + a.meta_bytes;
 }
 
 extern "C" int patchkv_attention(patchkv_ctx* ctx, const patchkv_geom* g, const patchkv_pool* pool, const patchkv_qpool* cache,
@@ -322,7 +345,9 @@ extern "C" int patchkv_attention(patchkv_ctx* ctx, const patchkv_geom* g, const 
         return PATCHKV_OK;
     }
     if (plan.row_tiles && aligned && aligned_rows(a->out, a->out_stride_row, a->out_stride_head)) {
-        const RowsPlan pl = {static_cast<float*>(a->workspace), plan.row_tiles, plan.row_splits};
+        uint8_t* ws = static_cast<uint8_t*>(a->workspace);
+        const RowsPlan pl = {reinterpret_cast<float*>(ws + plan.image_bytes + plan.meta_bytes), plan.row_tiles, plan.row_splits,
+                             plan.image_steps ? ws : nullptr, reinterpret_cast<uint32_t*>(ws + plan.image_bytes), plan.image_steps};
         PKV_CUDA(ctx, p.c.D == 128 ? launch_rows_tag<128>(p, pl, stream) : launch_rows_tag<64>(p, pl, stream));
         return PATCHKV_OK;
     }

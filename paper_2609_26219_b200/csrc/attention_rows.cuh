@@ -4,12 +4,17 @@
 // the other, vector m = row * share + head, so that no row of the tiles is left empty whatever share is.  It walks the
 // tokens in tiles of 128:
 //   S = Q K^T    tcgen05.mma, 128 x 128 x D, both operands in shared memory, S in TMEM
-//   P = 2^(S - ref)   a thread per row; P goes back to TMEM as 16-bit numbers over its S
+//   P = 2^(S - ref)   two threads per row, 64 columns each; P goes back to TMEM as 16-bit numbers over its S
 //   O += P V     tcgen05.mma, 128 x D x 128, P from TMEM, V from shared memory, O in TMEM
-// Roles: a warpgroup per tile for the softmax, one thread that issues the products, four warps that bring K and V.  The two tiles
-// take turns: while one is in its softmax the tensor cores work for the other.
-// K and V are brought by warps and not by TMA because the codes have to become operands on the way: fp16(code * scale), one
-// rounding of 2^-12; bf16 pages are copied with cp.async.  Queries over quantised pages are fp16 scaled by a power of two per
+// Roles: two warpgroups per tile for the softmax, one warp that issues the products, four warps that bring K and V.  The two tiles
+// take turns: while one is in its softmax the tensor cores work for the other.  (With one softmax thread per row the chain
+// softmax - P V - Q K^T of a tile took 5700 cycles a step, 3000 of them in that thread and 90 per product in an issuing thread
+// the compiler did not know to be alone; the products need 2050.)
+// The codes have to become operands on the way: fp16(code * scale), one rounding of 2^-12.  Where several CTAs need the same tokens
+// (two tiles of CTAs or more) a first kernel does that once per token and leaves images of the two shared-memory matrices of
+// each step in the workspace, which a CTA then fetches with one bulk copy each; converting in every CTA kept four warps busy for
+// 6000 cycles a step, three times what the products take.  Where one CTA is all there is, its own four warps convert (bf16
+// pages: cp.async), and the cache is read once, as it is.  Queries over quantised pages are fp16 scaled by a power of two per
 // row, so a bf16 query loses nothing.  The weights are fp16 there, bf16 over bf16 pages; sums are fp32 throughout.
 // As in the split kernel the softmax reference is only moved (and O rescaled) when a logit exceeds it by more than 8.
 #pragma once
@@ -21,14 +26,21 @@
 namespace patchkv {
 
 constexpr int kRowTile = 128;                   // query vectors of a tile, and tokens of a step
-constexpr int kRowsThreads = 13 * 32;           // two softmax warpgroups, four producer warps, the issuing warp
-constexpr int kProducer0 = 256, kIssuer = 384;  // first threads of the roles
+constexpr int kProducer0 = 512;                 // four softmax warpgroups, then the warps that bring K and V (four, or one that copies
+__host__ __device__ constexpr int rows_issuer(bool image) { return image ? 544 : 640; }             // images), then the issuing warp
+__host__ __device__ constexpr int rows_threads(bool image) { return rows_issuer(image) + 32; }
 
 struct RowsPlan {
     float* partial;                             // [split][n_rows * Hq][D], then (m, l) [split][n_rows * Hq]
     int32_t tiles;                              // CTAs along the query vectors of a sequence
     int32_t splits;                             // pieces of the token range (1: no partial results)
+    uint8_t* images;                            // [sequence][step][KV head]: K matrix, V matrix; null: no images
+    uint32_t* meta;                             // of each image: 4 words of absent tokens, 1 word `lost`, 3 unused
+    int32_t steps;                              // of a sequence in the two
 };
+__device__ __forceinline__ long long image_index(const AttentionParams& p, const RowsPlan& pl, int seq, int step, int head) {
+    return ((long long)seq * pl.steps + step) * p.c.H + head;
+}
 
 // ---- tcgen05 --------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void tc_alloc(uint32_t* slot, uint32_t cols) {
@@ -65,20 +77,27 @@ __device__ __forceinline__ void tc_ld32(float (&v)[32], uint32_t addr) {
           "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(addr) : "memory");
 }
-__device__ __forceinline__ void tc_st32(uint32_t addr, const float (&v)[32]) {
-    const uint32_t* r = reinterpret_cast<const uint32_t*>(v);
+__device__ __forceinline__ void tc_ld16(uint32_t (&r)[16], uint32_t addr) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,"
-        "%27,%28,%29,%30,%31,%32};" ::"r"(addr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
-        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
-        "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(addr) : "memory");
+}
+// One lane of the warp, always the same one.
+__device__ __forceinline__ bool elect_lane() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
 }
 __device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t (&r)[16]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr), "r"(r[0]), "r"(r[1]),
         "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]),
         "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void bulk_g2s_at(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
 }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
@@ -103,16 +122,17 @@ template <int D>
 struct RowsSmem {
     static constexpr int kMat = kRowTile * D * 2;               // one 128-row matrix
     static constexpr int kQ = 0, kK = 2 * kMat, kV = 4 * kMat, kBars = 6 * kMat;
-    static constexpr int kBytes = kBars + 512 + 1024;           // 1024: the matrices start on a multiple of that
+    static constexpr int kBytes = kBars + 3072 + 1024;          // 1024: the matrices start on a multiple of that
     static constexpr int kLaunch = kBytes > 120 * 1024 ? kBytes : 120 * 1024;   // one CTA per SM: it takes all of TMEM
 };
 struct RowsBars {
-    uint64_t q_ready[2], s_ready[2], p_ready[2], o_ready[2], k_full[2], k_empty[2], v_full[2], v_empty[2], drained;
-    alignas(16) uint32_t absent[4][4];                      // per step (mod 4): tokens whose page is out of range
+    uint64_t q_ready[2], max_ready[2], s_ready[2], p_ready[2], o_ready[2], k_full[2], k_empty[2], v_full[2], v_empty[2], drained;
+    alignas(16) uint32_t absent[4][8];          // per step (mod 4): tokens whose page is out of range; word 4: `lost` of an image
+    float top[2][2][kRowTile];                  // largest logit of a row in each half of the columns; at the end its sums
     uint32_t tmem;
     int32_t abort, lo, hi, lost;                // lost: a value that is not finite was taken out of a tile that needs a mask
 };
-static_assert(sizeof(RowsBars) <= 512 && offsetof(RowsBars, absent) % 16 == 0, "barrier area");
+static_assert(sizeof(RowsBars) <= 3072 && offsetof(RowsBars, absent) % 16 == 0, "barrier area");
 
 // Steps of 128 tokens that the rows between positions lo and hi see (as tile_range, in other units).
 __device__ __forceinline__ TileRange step_range(const AttentionParams& p, int kv, int lo_pos, int hi_pos) {
@@ -146,17 +166,50 @@ __device__ __forceinline__ uint2 operands8(uint32_t w, uint32_t s) {
     return o;
 }
 
-struct StepPlace { TileRange range; int seq, head, kv, lo, hi, begin, end; };
+// Sets fp16 (EXP 0x7C00) or bf16 (0x7F80) numbers that are not finite to zero; true when there was one.
+template <uint32_t EXP>
+__device__ __forceinline__ bool finite_only(uint4& x) {
+    bool found = false;
+    uint32_t* w = &x.x;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        if ((w[i] & EXP) == EXP) { w[i] &= 0xFFFF0000u; found = true; }
+        if ((w[i] >> 16 & EXP) == EXP) { w[i] &= 0x0000FFFFu; found = true; }
+    }
+    return found;
+}
+// 32 channels of a token (piece c of its row) as fp16 in channel order.
+template <int F>
+__device__ __forceinline__ void image_operands(uint4 (&o)[4], const uint8_t* row, int c, uint32_t s, uint32_t m0, uint32_t m1) {
+    const uint4 a = __ldg(reinterpret_cast<const uint4*>(row + c * (F == FMT_INT8 ? 32 : 16)));
+    if (F == FMT_INT8) {
+        const uint4 b = __ldg(reinterpret_cast<const uint4*>(row + c * 32 + 16));
+        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const uint2 x = operands8(w[2 * i], s), y = operands8(w[2 * i + 1], s);
+            o[i] = make_uint4(x.x, x.y, y.x, y.y);
+        }
+    } else {
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; i++) {                           // 0 4, 1 5, 2 6, 3 7 -> 0 1, 2 3, 4 5, 6 7
+            const uint4 x = operands4(w[i], s, m0, m1);
+            o[i] = make_uint4(__byte_perm(x.x, x.y, 0x5410), __byte_perm(x.z, x.w, 0x5410), __byte_perm(x.x, x.y, 0x7632), __byte_perm(x.z, x.w, 0x7632));
+        }
+    }
+}
+struct StepPlace { TileRange range; int seq, head, kv, lo, hi, begin, end; bool order4; };
 __device__ __forceinline__ bool whole_step(const AttentionParams& p, int kv, int lo, int hi, int t0) {
     return t0 + kRowTile - 1 <= min(lo, kv - 1) && (p.window == 0 || hi - t0 < p.window || t0 + kRowTile <= p.sinks);
 }
-// Values that are not finite were taken out of the masked steps; a row that sees such a value gets it here.  (Rare: element by
-// element, from the pages.)
-template <int VF, int D>
-__device__ __noinline__ void add_lost(const AttentionParams& p, const StepPlace& at, float (&o)[32], int c0, int pos) {
+// Values that are not finite were taken out of the masked steps (of an image: of all); a row that sees such a value gets it here.
+// (Rare: element by element, from the pages.)
+__device__ __noinline__ void add_lost(const AttentionParams& p, const RowsPlan& pl, const StepPlace& at, float (&o)[32], int c0, int pos) {
+    const int vf = v_format(p.c.tag), D = p.c.D;
     for (int j = at.begin; j < at.end; j++) {
-        const int t0 = at.range.tile(j) * kRowTile;
-        if (whole_step(p, at.kv, at.lo, at.hi, t0)) continue;
+        const int step = at.range.tile(j), t0 = step * kRowTile;
+        if (pl.images ? pl.meta[image_index(p, pl, at.seq, step, at.head) * 8 + 4] == 0 : whole_step(p, at.kv, at.lo, at.hi, t0)) continue;
         for (int t = t0; t < t0 + kRowTile; t++) {
             if (t > min(pos, at.kv - 1) || !sees(p, pos, t)) continue;
             const int lp = div_page(p.c, t), slot = t - lp * p.c.P;
@@ -165,13 +218,13 @@ __device__ __noinline__ void add_lost(const AttentionParams& p, const StepPlace&
             for (int c = 0; c < 32; c++) {
                 float v;
                 // column c of the accumulator is channel `ch`
-                const int e = c & 7, ch = c0 + (VF == FMT_INT4 ? (c & ~7) + (e & 1 ? 4 + (e >> 1) : e >> 1) : c);
-                if (VF == FMT_BF16) {
+                const int e = c & 7, ch = c0 + (at.order4 ? (c & ~7) + (e & 1 ? 4 + (e >> 1) : e >> 1) : c);
+                if (vf == FMT_BF16) {
                     v = bf16_bits_to_float(p.c.v[(long long)page * p.c.stride_page + (long long)slot * p.c.stride_token + (long long)at.head * p.c.stride_head + ch]);
                 } else {
                     const uint8_t* pg = p.c.base + (long long)page * p.c.stride_page;
                     const unsigned long long el = ((unsigned long long)slot * p.c.H + at.head) * D + ch;
-                    v = (float)code_at(pg + p.c.v_codes, VF, el) * scale_at(pg + p.c.v_scales, el / p.c.G);
+                    v = (float)code_at(pg + p.c.v_codes, vf, el) * scale_at(pg + p.c.v_scales, el / p.c.G);
                     v = __half2float(__float2half_rn(v));   // as the operand was: beyond 65504 an infinity
                 }
                 if (!(fabsf(v) <= 3.4e38f)) o[c] += v;
@@ -180,8 +233,9 @@ __device__ __noinline__ void add_lost(const AttentionParams& p, const StepPlace&
     }
 }
 
-// KF / VF: page formats (both FMT_BF16 for the bf16 pool).
-template <int KF, int VF, int D>
+// KF / VF: page formats (both FMT_BF16 for the bf16 pool).  IMAGE: operands come as images, in channel order (KF = VF = FMT_INT8
+// stands for fp16 images, FMT_BF16 for bf16).
+template <int KF, int VF, int D, bool IMAGE>
 struct RowsKernel {
     static constexpr bool kPool = KF == FMT_BF16;
     using S = RowsSmem<D>;
@@ -202,81 +256,146 @@ struct RowsKernel {
     __device__ __forceinline__ bool whole(int t0) const { return whole_step(p, kv, lo, hi, t0); }
 
     // ---- the warps that bring K and V
+    // A warp takes 32 tokens of a step; kPer lanes share a token, 32 / kPer tokens at a time (a pass).
+    static constexpr int kTok = 32 / kPer, kPass = kPer;
+    struct Pages { int page, t0; };                             // lane 0: page of the warp's first 16 tokens, lane 1: of the other 16
+
+    // Address of the thread's token of pass i (quantised: its page, and its row in *row); live: some row sees it and it has a page.
+    __device__ __forceinline__ long long token_at(const Pages& g, int tok, uint32_t* row, bool* live) const {
+        const int w32 = tok & ~31, t = g.t0 + tok;
+        const int page = __shfl_sync(0xFFFFFFFFu, g.page, (tok - w32) >> 4);
+        const int slot = t - div_page(p.c, t) * p.c.P;
+        *live = page >= 0 && any_sees(t);
+        *row = (uint32_t)slot * p.c.H + head;
+        if (!*live) return 0;
+        return (long long)page * p.c.stride_page + (kPool ? (long long)slot * p.c.stride_token + (long long)head * p.c.stride_head : 0ll);
+    }
+    // Tokens of the warp that some row sees but whose page is out of range.
+    __device__ __forceinline__ uint32_t missing(const Pages& g, int w) const {
+        const int lane = threadIdx.x & 31, page = __shfl_sync(0xFFFFFFFFu, g.page, lane >> 4);
+        const uint32_t gone = __ballot_sync(0xFFFFFFFFu, page < 0 && any_sees(g.t0 + 32 * w + lane));
+        if (gone && lane == 0) latch(p.status);
+        return gone;
+    }
+    // The thread's 32 channels of pass i, K or V: codes and their scale.
+    template <int F>
+    __device__ __forceinline__ void load_piece(const Pages& g, int tok, int c, bool is_v, uint32_t (&w)[8], uint32_t& scale) const {
+        uint32_t row;
+        bool live;
+        const uint8_t* pg = p.c.base + token_at(g, tok, &row, &live);
+#pragma unroll
+        for (int i = 0; i < 8; i++) w[i] = 0;
+        scale = 0;
+        if (!live) return;
+        const uint8_t* codes = pg + (is_v ? p.c.v_codes : 0u) + row * (F == FMT_INT8 ? D : D / 2) + c * (F == FMT_INT8 ? 32 : 16);
+        const uint4 a = __ldg(reinterpret_cast<const uint4*>(codes));
+        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+        if (F == FMT_INT8) {
+            const uint4 b = __ldg(reinterpret_cast<const uint4*>(codes + 16));
+            w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+        }
+        const uint32_t s = (row * (D / p.c.G) + c * 32 / p.c.G) * 2 + (is_v ? p.c.v_scales : p.c.k_scales);
+        scale = __ldg(reinterpret_cast<const uint16_t*>(pg + s));
+    }
+
+    // Images: one lane copies.  Returns with the copies in flight counted in `sent` (bit 2 st + (0 for K, 1 for V): a copy into stage st
+    // has been issued), so that after an abort they can be waited for.
+    __device__ __forceinline__ void fetch_images(const RowsPlan& pl) {
+        int j = begin;
+        uint32_t k_uses = 0, v_uses = 0;                        // copies issued
+        for (; j < end; j++) {
+            const int n = j - begin, st = n & 1;
+            const uint32_t parity = ((n >> 1) & 1) ^ 1;
+            const long long at = image_index(p, pl, seq, range.tile(j), head);
+            const uint8_t* image = pl.images + at * (2 * S::kMat);
+            if (!wait_warp(&bars.k_empty[st], parity)) break;
+            if (elect_lane()) {
+                mbar_arrive_expect_tx(&bars.k_full[st], S::kMat + 32);
+                bulk_g2s_at(smem + S::kK + st * S::kMat, image, S::kMat, &bars.k_full[st]);
+                bulk_g2s_at(smem_u32(bars.absent[n & 3]), pl.meta + at * 8, 32, &bars.k_full[st]);
+            }
+            __syncwarp();
+            k_uses++;
+            if (!wait_warp(&bars.v_empty[st], parity)) break;
+            if (elect_lane()) {
+                mbar_arrive_expect_tx(&bars.v_full[st], S::kMat);
+                bulk_g2s_at(smem + S::kV + st * S::kMat, image + S::kMat, S::kMat, &bars.v_full[st]);
+            }
+            __syncwarp();
+            v_uses++;
+        }
+        // The last copies (after an abort they may have no reader) must have landed before the CTA goes.
+        for (int back = 1; back <= 2; back++) {
+            const uint32_t k = k_uses - back, v = v_uses - back;
+            for (uint32_t i = 0; k_uses >= (uint32_t)back && i < kWaitLimit && !mbar_try_wait(&bars.k_full[k & 1], (k >> 1) & 1); i++) __nanosleep(40);
+            for (uint32_t i = 0; v_uses >= (uint32_t)back && i < kWaitLimit && !mbar_try_wait(&bars.v_full[v & 1], (v >> 1) & 1); i++) __nanosleep(40);
+        }
+    }
+
     __device__ __forceinline__ void produce() {
         const int w = (threadIdx.x - kProducer0) >> 5, lane = threadIdx.x & 31;
-        // A warp takes 32 tokens of a step; kPer lanes share a token, 32 / kPer tokens at a time.
-        constexpr int kTok = 32 / kPer, kPass = kPer;
         const int c = lane % kPer, tok0 = 32 * w + lane / kPer;
         uint32_t m0, m1;                                        // 1024 + 8 and 1024 + 8 * 16 in every half: magic and offset
         asm volatile("mov.b32 %0, 0x64086408;" : "=r"(m0));
         asm volatile("mov.b32 %0, 0x64806480;" : "=r"(m1));
-        int next_page = page_of(begin, 32 * w + (lane & 1) * 16);
-        for (int j = begin; j < end; j++) {
-            const int n = j - begin, st = n & 1, t0 = range.tile(j) * kRowTile;
-            const uint32_t parity = ((n >> 1) & 1) ^ 1;
-            const int page_lane = next_page;                    // lane 0: the warp's first 16 tokens, lane 1: the other 16
-            if (j + 1 < end) next_page = page_of(j + 1, 32 * w + (lane & 1) * 16);
-            const bool masked = !whole(t0);
-            uint32_t kw[kPass][8], vw[kPass][8], ks[kPass], vs[kPass];
-            bool live[kPass];
-            long long at[kPass];
-            uint32_t gone = 0;
+        if (begin >= end) return;
+        auto pages_of = [&](int j) { return Pages{page_of(j, 32 * w + (lane & 1) * 16), j < end ? range.tile(j) * kRowTile : 0}; };
+        Pages now = pages_of(begin), next = pages_of(begin + 1);
+        // One set of registers for the codes in flight: as soon as K's have become operands V's are asked for, then the next K's.
+        uint32_t code[kPass][8], scale[kPass];
+        if constexpr (!kPool)
 #pragma unroll
-            for (int i = 0; i < kPass; i++) {
-                const int tok = tok0 + i * kTok, t = t0 + tok;
-                const int page = __shfl_sync(0xFFFFFFFFu, page_lane, (tok - 32 * w) >> 4);
-                live[i] = any_sees(t);
-                if (live[i] && page < 0) { live[i] = false; gone |= 1u << (tok & 31); latch(p.status); }
-                const int slot = t - div_page(p.c, t) * p.c.P;
-                at[i] = kPool ? (long long)page * p.c.stride_page + (long long)slot * p.c.stride_token + (long long)head * p.c.stride_head
-                              : (long long)page * p.c.stride_page;
-                if constexpr (!kPool) {
-                    const uint8_t* pg = p.c.base + at[i];
-                    const uint32_t row = (uint32_t)slot * p.c.H + head;
-                    load_codes<KF>(kw[i], pg + row * (KF == FMT_INT8 ? D : D / 2), c, live[i]);
-                    load_codes<VF>(vw[i], pg + p.c.v_codes + row * (VF == FMT_INT8 ? D : D / 2), c, live[i]);
-                    const uint32_t s = (row * (D / p.c.G) + c * 32 / p.c.G) * 2;
-                    ks[i] = live[i] ? __ldg(reinterpret_cast<const uint16_t*>(pg + p.c.k_scales + s)) : 0u;
-                    vs[i] = live[i] ? __ldg(reinterpret_cast<const uint16_t*>(pg + p.c.v_scales + s)) : 0u;
-                }
-            }
-            gone = __reduce_or_sync(0xFFFFFFFFu, gone);
+            for (int i = 0; i < kPass; i++) load_piece<KF>(now, tok0 + i * kTok, c, false, code[i], scale[i]);
+#pragma unroll 1
+        for (int j = begin; j < end; j++) {
+            const int n = j - begin, st = n & 1;
+            const uint32_t parity = ((n >> 1) & 1) ^ 1;
+            const bool masked = !whole(now.t0);
+            const uint32_t gone = missing(now, w);
             if (lane == 0) bars.absent[n & 3][w] = gone;
             const uint32_t kb = smem + S::kK + st * S::kMat, vb = smem + S::kV + st * S::kMat;
             if (!wait_warp(&bars.k_empty[st], parity)) return;
             if constexpr (kPool) {
+                // chunks kPer apart: a row's lanes read a contiguous run
+                auto copy = [&](const uint16_t* from, uint32_t mat) {
 #pragma unroll
-                for (int i = 0; i < kPass; i++)
+                    for (int i = 0; i < kPass; i++) {
+                        uint32_t row;
+                        bool live;
+                        const uint16_t* x = from + token_at(now, tok0 + i * kTok, &row, &live) + 8 * c;
 #pragma unroll
-                    for (int q = 0; q < 4; q++)                 // chunks kPer apart: a row's lanes read a contiguous run
-                        cp16(kb + swizzled(tok0 + i * kTok, q * kPer + c), p.c.k + (live[i] ? at[i] + 8 * (q * kPer + c) : 0), live[i]);
-                cp_commit();
+                        for (int q = 0; q < 4; q++) cp16(mat + swizzled(tok0 + i * kTok, q * kPer + c), live ? x + 8 * q * kPer : from, live);
+                    }
+                    cp_commit();
+                };
+                copy(p.c.k, kb);
                 if (!wait_warp(&bars.v_empty[st], parity)) return;
-#pragma unroll
-                for (int i = 0; i < kPass; i++)
-#pragma unroll
-                    for (int q = 0; q < 4; q++)
-                        cp16(vb + swizzled(tok0 + i * kTok, q * kPer + c), p.c.v + (live[i] ? at[i] + 8 * (q * kPer + c) : 0), live[i]);
-                cp_commit();
+                copy(p.c.v, vb);
                 cp_wait<1>();
                 fence_async_smem();
                 mbar_arrive(&bars.k_full[st]);
                 cp_wait<0>();
                 if (masked) clean<0x7F80u>(vb, tok0, c, 1, kPer);
-                fence_async_smem();
-                mbar_arrive(&bars.v_full[st]);
             } else {
 #pragma unroll
-                for (int i = 0; i < kPass; i++) store_operands<KF>(kb, tok0 + i * kTok, c, kw[i], ks[i], m0, m1);
+                for (int i = 0; i < kPass; i++) {
+                    store_operands<KF>(kb, tok0 + i * kTok, c, code[i], scale[i], m0, m1);
+                    load_piece<VF>(now, tok0 + i * kTok, c, true, code[i], scale[i]);
+                }
                 fence_async_smem();
                 mbar_arrive(&bars.k_full[st]);
                 if (!wait_warp(&bars.v_empty[st], parity)) return;
 #pragma unroll
-                for (int i = 0; i < kPass; i++) store_operands<VF>(vb, tok0 + i * kTok, c, vw[i], vs[i], m0, m1);
+                for (int i = 0; i < kPass; i++) {
+                    store_operands<VF>(vb, tok0 + i * kTok, c, code[i], scale[i], m0, m1);
+                    load_piece<KF>(next, tok0 + i * kTok, c, false, code[i], scale[i]);
+                }
                 if (masked) clean<0x7C00u>(vb, tok0, c, 4, 1);
-                fence_async_smem();
-                mbar_arrive(&bars.v_full[st]);
             }
+            fence_async_smem();
+            mbar_arrive(&bars.v_full[st]);
+            now = next;
+            next = pages_of(j + 2);
         }
     }
     // Page of token `tok` of step j; -1 when it is out of range or lies behind the cache.
@@ -286,30 +405,6 @@ struct RowsKernel {
         if (t >= kv) return -1;
         const int pg = __ldg(p.b.block_table + (long long)seq * p.b.table_stride + div_page(p.c, t));
         return pg >= 0 && pg < p.c.n_pages ? pg : -1;
-    }
-    template <int F>
-    __device__ __forceinline__ static void load_codes(uint32_t (&w)[8], const uint8_t* row, int c, bool live) {
-#pragma unroll
-        for (int i = 0; i < 8; i++) w[i] = 0;
-        if (!live) return;
-        const uint4 a = __ldg(reinterpret_cast<const uint4*>(row + c * (F == FMT_INT8 ? 32 : 16)));
-        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-        if (F == FMT_INT8) {
-            const uint4 b = __ldg(reinterpret_cast<const uint4*>(row + c * 32 + 16));
-            w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
-        }
-    }
-    // Sets fp16 (EXP 0x7C00) or bf16 (0x7F80) numbers that are not finite to zero; true when there was one.
-    template <uint32_t EXP>
-    __device__ __forceinline__ static bool finite_only(uint4& x) {
-        bool found = false;
-        uint32_t* w = &x.x;
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            if ((w[i] & EXP) == EXP) { w[i] &= 0xFFFF0000u; found = true; }
-            if ((w[i] >> 16 & EXP) == EXP) { w[i] &= 0x0000FFFFu; found = true; }
-        }
-        return found;
     }
     // In a step that needs a mask a value that is not finite must not meet the weight 0 of a row that does not see it: it is taken out
     // here and given to the rows that see it at the end.  Chunks of the thread: c * lead + q * apart, q = 0 .. 3.
@@ -340,85 +435,95 @@ struct RowsKernel {
         }
     }
 
-    // ---- the thread that issues the products
+    // ---- the warp that issues the products (one lane of it; the whole warp waits, so that all else is known to be uniform)
     __device__ __forceinline__ void issue(int tiles, uint32_t tmem) {
         constexpr uint32_t kQk = instr_desc(kPool, false, kRowTile), kPv = instr_desc(kPool, true, D);
-        auto logits = [&](int i, int st) {
-            const uint32_t q = smem + S::kQ + i * S::kMat, k = smem + S::kK + st * S::kMat;
+        const uint64_t q_desc = smem_desc(smem + S::kQ, 16), k_desc = smem_desc(smem + S::kK, 16), v_desc = smem_desc(smem + S::kV, kRowTile * 128);
+        constexpr uint32_t kMat16 = S::kMat >> 4;
+        auto logits = [&](int i, int st, uint64_t* k_free) {
+            const uint64_t q = q_desc + i * kMat16, k = k_desc + st * kMat16;
+            if (elect_lane()) {
 #pragma unroll
-            for (int x = 0; x < D / 16; x++) {                  // 16 channels: 32 bytes inside a 128-byte row, then the next half
-                const uint32_t o = (x >> 2) * (kRowTile * 128) + (x & 3) * 32;
-                tc_mma_ss(tmem + i * kRowTile, smem_desc(q + o, 16), smem_desc(k + o, 16), kQk, x != 0);
+                for (int x = 0; x < D / 16; x++) {              // 16 channels: 32 bytes inside a 128-byte row, then the next half
+                    const uint32_t o = (x >> 2) * (kRowTile * 8) + (x & 3) * 2;
+                    tc_mma_ss(tmem + i * kRowTile, q + o, k + o, kQk, x != 0);
+                }
+                tc_commit(&bars.s_ready[i]);
+                if (k_free) tc_commit(k_free);
             }
-            tc_commit(&bars.s_ready[i]);
+            __syncwarp();
         };
-        for (int i = 0; i < tiles; i++) if (!wait(&bars.q_ready[i], 0)) return;
-        if (!wait(&bars.k_full[0], 0)) return;
+        for (int i = 0; i < tiles; i++) if (!wait_warp(&bars.q_ready[i], 0)) return;
+        if (!wait_warp(&bars.k_full[0], 0)) return;
         tc_after();
-        for (int i = 0; i < tiles; i++) logits(i, 0);
-        tc_commit(&bars.k_empty[0]);
+        for (int i = 0; i < tiles; i++) logits(i, 0, i == tiles - 1 ? &bars.k_empty[0] : nullptr);
         const int n = end - begin;
+#pragma unroll 1
         for (int j = 0; j < n; j++) {
             const int st = j & 1;
+            if (!wait_warp(&bars.v_full[st], (j >> 1) & 1)) return;
+            if (j + 1 < n && !wait_warp(&bars.k_full[st ^ 1], ((j + 1) >> 1) & 1)) return;
+#pragma unroll 1
             for (int i = 0; i < tiles; i++) {
-                if (i == 0 && !wait(&bars.v_full[st], (j >> 1) & 1)) return;
-                if (!wait(&bars.p_ready[i], j & 1)) return;
+                if (!wait_warp(&bars.p_ready[i], j & 1)) return;
                 tc_after();
-                const uint32_t v = smem + S::kV + st * S::kMat;
+                const uint64_t v = v_desc + st * kMat16;
+                const uint32_t o = tmem + (2 + i) * kRowTile, a = tmem + i * kRowTile;
+                if (elect_lane()) {
+                    tc_mma_ts(o, a, v, kPv, j != 0);
 #pragma unroll
-                for (int x = 0; x < kRowTile / 16; x++)         // 16 tokens: two groups of 8 rows
-                    tc_mma_ts(tmem + 2 * kRowTile + i * kRowTile, tmem + i * kRowTile + 8 * x, smem_desc(v + x * 2048, kRowTile * 128), kPv, j != 0 || x != 0);
-                if (i == tiles - 1) tc_commit(&bars.v_empty[st]);
-                if (j + 1 < n) {
-                    if (i == 0) {
-                        if (!wait(&bars.k_full[st ^ 1], ((j + 1) >> 1) & 1)) return;
-                        tc_after();
-                    }
-                    logits(i, st ^ 1);
-                    if (i == tiles - 1) tc_commit(&bars.k_empty[st ^ 1]);
-                } else {
-                    tc_commit(&bars.o_ready[i]);
+                    for (int x = 1; x < kRowTile / 16; x++)       // 16 tokens: 8 columns of P, two groups of 8 rows of V
+                        tc_mma_ts(o, a + 8 * x + (x >= 4 ? 32 : 0), v + x * 128, kPv, true);
+                    if (i == tiles - 1) tc_commit(&bars.v_empty[st]);
+                    if (j + 1 == n) tc_commit(&bars.o_ready[i]);
                 }
+                __syncwarp();
+                if (j + 1 < n) logits(i, st ^ 1, i == tiles - 1 ? &bars.k_empty[st ^ 1] : nullptr);
             }
         }
     }
 
+    // Tokens on pages out of range count when some row sees them (with images nobody has looked at that yet).
+    __device__ __forceinline__ void latch_absent(int c0, int t0, const uint2& absent) const {
+        const int lane = threadIdx.x & 31;
+        if ((absent.x >> lane & 1u && any_sees(t0 + c0 + lane)) || (absent.y >> lane & 1u && any_sees(t0 + c0 + 32 + lane))) latch(p.status);
+    }
+
     // Bit c: this row sees column c0 + c.
-    __device__ __forceinline__ static uint32_t seen(int c0, int a, int b, int s, const uint4& absent, int k) {
+    __device__ __forceinline__ static uint32_t seen(int c0, int a, int b, int s, uint32_t gone) {
         auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u; };      // bits [0, n)
-        const uint32_t gone = k == 0 ? absent.x : k == 1 ? absent.y : k == 2 ? absent.z : absent.w;
         return below(b + 1 - c0) & (~below(a - c0) | below(s - c0)) & ~gone;
     }
     // What a row does not see becomes the value whose weight is zero: times the factor minus infinity.
-    __device__ __forceinline__ static void mask_chunk(float (&x)[32], uint32_t seen, float factor) {
-        const float none = factor < 0.0f ? INFINITY : -INFINITY;
+    __device__ __forceinline__ static void mask_chunk(float (&x)[32], uint32_t seen, float none) {
 #pragma unroll
         for (int c = 0; c < 32; c++) x[c] = seen >> c & 1u ? x[c] : none;
     }
 
-    // ---- softmax: one thread per query vector
-    __device__ __forceinline__ void softmax(int i, int first, int m, int m_end, uint32_t tmem, const RowsPlan& pl, int split) {
+    // ---- softmax: two threads per query vector, one per half of a step's tokens (and of the channels at the ends)
+    __device__ __forceinline__ void softmax(int i, int half, int first, int m, int m_end, uint32_t tmem, const RowsPlan& pl, int split) {
         const int r = threadIdx.x & 127;
         const bool live = m < m_end;
         const int row = live ? first + m / p.share : first, hq = live ? head * p.share + m % p.share : 0;
         const int pos = live ? max(-1, row_position(p.b, seq, row)) : -1;
-        // the query into shared memory
+        // the query into shared memory; each half writes its channels
         float factor = p.scale_log2;
         {
-            const uint16_t* q = p.q + (long long)row * p.q_stride_row + (long long)hq * p.q_stride_head;
+            const uint4* q = reinterpret_cast<const uint4*>(p.q + (long long)row * p.q_stride_row + (long long)hq * p.q_stride_head);
             const uint32_t mat = smem + S::kQ + i * S::kMat;
+            constexpr int kHalf = D / 16;                       // 16-byte chunks of a half
             if constexpr (kPool) {
 #pragma unroll 4
-                for (int c = 0; c < D / 8; c++) {
-                    const uint4 x = live ? __ldg(reinterpret_cast<const uint4*>(q) + c) : make_uint4(0, 0, 0, 0);
+                for (int c = half * kHalf; c < (half + 1) * kHalf; c++) {
+                    const uint4 x = live ? __ldg(q + c) : make_uint4(0, 0, 0, 0);
                     sts128(mat + swizzled(r, c), x.x, x.y, x.z, x.w);
                 }
             } else {
                 // scaled so that the largest magnitude lies in [2^13, 2^14); a vector with a NaN or an infinity gives NaN
                 float amax = 0.0f, bad = 0.0f;
 #pragma unroll 4
-                for (int c = 0; c < D / 8; c++) {
-                    const uint4 x = live ? __ldg(reinterpret_cast<const uint4*>(q) + c) : make_uint4(0, 0, 0, 0);
+                for (int c = 0; c < 2 * kHalf; c++) {
+                    const uint4 x = live ? __ldg(q + c) : make_uint4(0, 0, 0, 0);
                     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
                     for (int k = 0; k < 4; k++) {
@@ -429,11 +534,11 @@ struct RowsKernel {
                 }
                 const int e = (int)(__float_as_uint(amax) >> 23) - 127;
                 const int shift = amax > 0.0f ? min(13 - e, 120) : 0;
-                const float up = bad == 0.0f ? exp2i(shift) : 0.0f;
+                const float up = exp2i(shift);
                 factor = p.scale_log2 * exp2i(-shift) + bad;
 #pragma unroll 2
-                for (int c = 0; c < D / 8; c++) {
-                    const uint4 x = live && bad == 0.0f ? __ldg(reinterpret_cast<const uint4*>(q) + c) : make_uint4(0, 0, 0, 0);
+                for (int c = half * kHalf; c < (half + 1) * kHalf; c++) {
+                    const uint4 x = live && bad == 0.0f ? __ldg(q + c) : make_uint4(0, 0, 0, 0);
                     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
                     float f[8];
 #pragma unroll
@@ -455,69 +560,79 @@ struct RowsKernel {
         if (broken) factor = 1.0f;
         if (factor == 0.0f) factor = 1.17549435e-38f;
         const uint32_t lanes = (uint32_t)((threadIdx.x >> 5) & 3) << 21;              // the warp's quarter of the TMEM lanes
-        const uint32_t s_at = tmem + lanes + i * kRowTile, o_at = tmem + lanes + 2 * kRowTile + i * kRowTile;
+        const uint32_t s_at = tmem + lanes + i * kRowTile + 64 * half, o_at = tmem + lanes + (2 + i) * kRowTile + half * (D / 2);
+        const float none = factor < 0.0f ? INFINITY : -INFINITY;                      // times the factor: minus infinity
         float ref = kNoMax;
+        uint32_t lost_seen = 0;
         f32x2 sum2 = pack2(0.0f, 0.0f);
         const int n = end - begin;
+#pragma unroll 1
         for (int j = 0; j < n; j++) {
             const int t0 = range.tile(begin + j) * kRowTile;
             if (!wait_warp(&bars.s_ready[i], j & 1)) return;
             tc_after();
             // Columns of the step this row sees: [a, b] and [0, s); what its pages don't hold is in `absent`.
-            const uint4 absent = lds128(smem_u32(bars.absent[j & 3]));
-            const bool plain = whole(t0) && (absent.x | absent.y | absent.z | absent.w) == 0;
+            const uint2 absent = lds64(smem_u32(&bars.absent[j & 3][2 * half]));
+            const bool plain = whole(t0) && (absent.x | absent.y) == 0;
+            if (IMAGE && !plain && (absent.x | absent.y) != 0) latch_absent(64 * half, t0, absent);
+            if (IMAGE) lost_seen |= bars.absent[j & 3][4];
             const int b = min(pos, kv - 1) - t0, a = p.window > 0 ? max(pos - p.window + 1, 0) - t0 : -t0, s = p.sinks - t0;
-            // The loops over the step's four chunks stay loops: three roles run different code on an SM, and unrolled it does not
-            // stay in the instruction cache (1270 us for 8192 rows of prompt, most of it waiting for instructions).
-            float top = -INFINITY;
+            // Two passes over the thread's 64 logits, 32 at a time out of TMEM: 80 registers a thread are what 21 warps leave, and
+            // four warps on each scheduler hide the loads.  The loops stay loops: three roles run different code on an SM,
+            // and unrolled it does not stay in the instruction cache.
+            float y[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll 1
-            for (int k = 0; k < 4; k++) {
+            for (int k = 0; k < 2; k++) {
                 float x[32];
                 tc_ld32(x, s_at + 32 * k);
                 tc_wait_ld();
-                if (!plain) mask_chunk(x, seen(32 * k, a, b, s, absent, k), factor);
-                float y[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                if (factor < 0.0f)
+                if (!plain) mask_chunk(x, seen(64 * half + 32 * k, a, b, s, k ? absent.y : absent.x), none);
+                if (factor >= 0.0f) {
 #pragma unroll
-                    for (int c = 0; c < 32; c++) x[c] = -x[c];
+                    for (int c = 0; c < 32; c += 2) y[(c >> 1) & 3] = fmaxf(y[(c >> 1) & 3], fmaxf(x[c], x[c + 1]));
+                } else {
 #pragma unroll
-                for (int c = 0; c < 32; c += 2) y[(c >> 1) & 3] = fmaxf(y[(c >> 1) & 3], fmaxf(x[c], x[c + 1]));
-                top = fmaxf(top, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
+                    for (int c = 0; c < 32; c += 2) y[(c >> 1) & 3] = fmaxf(y[(c >> 1) & 3], fmaxf(-x[c], -x[c + 1]));
+                }
             }
-            top = top == -INFINITY ? top : top * fabsf(factor);
-            const bool move = top > ref + 8.0f;
-            if (__any_sync(0xFFFFFFFFu, move)) {
-                const float to = move ? top : ref, keep = fast_exp2(ref - to);
+            bars.top[i][half][r] = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0) mbar_arrive(&bars.max_ready[i]);
+            if (!wait_warp(&bars.max_ready[i], j & 1)) return;
+            const float most = fmaxf(bars.top[i][0][r], bars.top[i][1][r]);
+            const float top = most == -INFINITY ? most : most * fabsf(factor);
+            if (__any_sync(0xFFFFFFFFu, top > ref + 8.0f)) {                         // the same in both halves
+                const float to = top > ref + 8.0f ? top : ref, keep = fast_exp2(ref - to);
                 ref = to;
                 sum2 = mul2(sum2, pack2(keep, keep));
                 if (j > 0)                                      // the products of the steps before are done: s_ready came behind them
 #pragma unroll 1
                     for (int k = 0; k < D / 32; k++) {
-                        float o[32];
-                        tc_ld32(o, o_at + 32 * k);
+                        uint32_t w[16];
+                        tc_ld16(w, o_at + 16 * k);
                         tc_wait_ld();
 #pragma unroll
-                        for (int c = 0; c < 32; c++) o[c] *= keep;
-                        tc_st32(o_at + 32 * k, o);
+                        for (int c = 0; c < 16; c++) w[c] = __float_as_uint(__uint_as_float(w[c]) * keep);
+                        tc_st16(o_at + 16 * k, w);
                     }
             }
-            // P lies over the first half of S: a chunk of 32 logits is read before the chunk of 16 columns over it is written
+            // P lies over the first 32 of the thread's own 64 columns of S, each chunk of 16 on columns that have been read.
             const f32x2 factor2 = pack2(factor, factor), ref2 = pack2(-ref, -ref);
 #pragma unroll 1
-            for (int k = 0; k < 4; k++) {
+            for (int k = 0; k < 2; k++) {
                 float x[32];
                 tc_ld32(x, s_at + 32 * k);
                 tc_wait_ld();
-                if (!plain) mask_chunk(x, seen(32 * k, a, b, s, absent, k), factor);
+                if (!plain) mask_chunk(x, seen(64 * half + 32 * k, a, b, s, k ? absent.y : absent.x), none);
                 uint32_t w[16];
 #pragma unroll
                 for (int c = 0; c < 16; c++) {
-                    float u, v;
-                    unpack2(fma2(pack2(x[2 * c], x[2 * c + 1]), factor2, ref2), u, v);
-                    u = fast_exp2(u);
-                    v = fast_exp2(v);
-                    sum2 = add2(sum2, pack2(u, v));
-                    w[c] = kPool ? bf162_bits(u, v) : half2_bits(u, v);
+                    float e, f;
+                    unpack2(fma2(pack2(x[2 * c], x[2 * c + 1]), factor2, ref2), e, f);
+                    e = fast_exp2(e);
+                    f = fast_exp2(f);
+                    sum2 = add2(sum2, pack2(e, f));
+                    w[c] = kPool ? bf162_bits(e, f) : half2_bits(e, f);
                 }
                 tc_st16(s_at + 16 * k, w);
             }
@@ -530,17 +645,22 @@ struct RowsKernel {
         float sum, sum_odd;
         unpack2(sum2, sum, sum_odd);
         sum += sum_odd;
+        bars.top[i][half][r] = sum;                             // (nobody reads a maximum any more: o_ready came behind all of P)
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(&bars.max_ready[i]);
+        if (!wait_warp(&bars.max_ready[i], n & 1)) return;
+        sum = bars.top[i][0][r] + bars.top[i][1][r];
         if (broken && sum != 0.0f) sum = __uint_as_float(0x7FC00000u);
-        const bool lost = *reinterpret_cast<volatile int32_t*>(&bars.lost) != 0;
+        const bool lost = IMAGE ? lost_seen != 0 : *reinterpret_cast<volatile int32_t*>(&bars.lost) != 0;
         const float inv = pl.splits > 1 ? 1.0f : (sum != 0.0f ? 1.0f / sum : 0.0f);
         const long long vec = (long long)row * p.Hq + hq;
         float* part = pl.partial + ((long long)split * p.b.n_rows * p.Hq + vec) * D;
         uint16_t* out = p.out + (long long)row * p.out_stride_row + (long long)hq * p.out_stride_head;
 #pragma unroll 1
-        for (int k = 0; k < D / 32; k++) {
+        for (int k = half * (D / 64); k < (half + 1) * (D / 64); k++) {
             float o[32];
             if (n > 0) {
-                tc_ld32(o, o_at + 32 * k);
+                tc_ld32(o, tmem + lanes + (2 + i) * kRowTile + 32 * k);
                 tc_wait_ld();
             } else {
 #pragma unroll
@@ -550,7 +670,7 @@ struct RowsKernel {
                 float fixed[32];
 #pragma unroll
                 for (int c = 0; c < 32; c++) fixed[c] = o[c];
-                add_lost<VF, D>(p, {range, seq, head, kv, lo, hi, begin, end}, fixed, 32 * k, pos);
+                add_lost(p, pl, {range, seq, head, kv, lo, hi, begin, end, VF == FMT_INT4}, fixed, 32 * k, pos);
 #pragma unroll
                 for (int c = 0; c < 32; c++) o[c] = fixed[c];
             }
@@ -575,17 +695,18 @@ struct RowsKernel {
                 }
             }
         }
-        if (live && pl.splits > 1) {
+        if (live && half == 0 && pl.splits > 1) {
             float* ml = pl.partial + (long long)pl.splits * p.b.n_rows * p.Hq * D + ((long long)split * p.b.n_rows * p.Hq + vec) * 2;
             *reinterpret_cast<float2*>(ml) = make_float2(ref, sum);
         }
     }
 };
 
-template <int KF, int VF, int D>
-__global__ void __launch_bounds__(kRowsThreads, 1) attention_rows_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ RowsPlan pl) {
-    using K = RowsKernel<KF, VF, D>;
+template <int KF, int VF, int D, bool IMAGE>
+__global__ void __launch_bounds__(rows_threads(IMAGE), 1) attention_rows_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ RowsPlan pl) {
+    using K = RowsKernel<KF, VF, D, IMAGE>;
     using S = RowsSmem<D>;
+    constexpr int kIssuer = rows_issuer(IMAGE), kThreads = rows_threads(IMAGE);
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     RowsBars& bars = *reinterpret_cast<RowsBars*>(raw + (base - smem_u32(raw)) + S::kBars);
@@ -593,9 +714,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attention_rows_kernel(const _
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0);
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; i++) {
-            mbar_init(&bars.q_ready[i], kRowTile); mbar_init(&bars.p_ready[i], kRowTile);
+            mbar_init(&bars.q_ready[i], 2 * kRowTile); mbar_init(&bars.p_ready[i], 2 * kRowTile);
+            mbar_init(&bars.max_ready[i], 8);
             mbar_init(&bars.s_ready[i], 1); mbar_init(&bars.o_ready[i], 1);
-            mbar_init(&bars.k_full[i], 128); mbar_init(&bars.v_full[i], 128);
+            mbar_init(&bars.k_full[i], IMAGE ? 1 : 128); mbar_init(&bars.v_full[i], IMAGE ? 1 : 128);
             mbar_init(&bars.k_empty[i], 1); mbar_init(&bars.v_empty[i], 1);
         }
         mbar_init(&bars.drained, 1);
@@ -618,7 +740,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attention_rows_kernel(const _
     if (m0 >= m_end) return;
     __syncthreads();
     // positions of the CTA's rows
-    for (int r = m0 / p.share + threadIdx.x; r <= (m_end - 1) / p.share; r += kRowsThreads) {
+    for (int r = m0 / p.share + threadIdx.x; r <= (m_end - 1) / p.share; r += kThreads) {
         const int x = row_position(p.b, seq, first + r);
         atomicMin(&bars.lo, max(-1, x));
         atomicMax(&bars.hi, x);
@@ -636,15 +758,20 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attention_rows_kernel(const _
     k.end = (int)((long long)k.range.count * (split + 1) / pl.splits);
     const int tiles = m_end - m0 > kRowTile ? 2 : 1;
     if (warp < kProducer0 / 32) {
-        const int i = warp >> 2;
-        if (i < tiles) k.softmax(i, first, m0 + threadIdx.x, m_end, tmem, pl, split);
+        const int i = warp >> 3, half = warp >> 2 & 1;          // tile, half of its columns
+        if (i < tiles) k.softmax(i, half, first, m0 + i * kRowTile + (threadIdx.x & 127), m_end, tmem, pl, split);
     } else if (warp < kIssuer / 32) {
-        k.produce();
-        cp_wait<0>();
-    } else if ((threadIdx.x & 31) == 0 && k.end > k.begin) {
+        if constexpr (IMAGE) {
+            k.fetch_images(pl);
+        } else {
+            k.produce();
+            cp_wait<0>();
+        }
+    } else if (k.end > k.begin) {
         k.issue(tiles, tmem);
-        if (bars.abort) {                                       // what was issued must have ended before TMEM goes
-            tc_commit(&bars.drained);
+        if (__any_sync(0xFFFFFFFFu, *reinterpret_cast<volatile int32_t*>(&bars.abort))) {      // what was issued must have ended before TMEM goes
+            if (elect_lane()) tc_commit(&bars.drained);
+            __syncwarp();
             for (uint32_t i = 0; i < kWaitLimit && !mbar_try_wait(&bars.drained, 0); i++) __nanosleep(40);
         }
     }
@@ -654,6 +781,80 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attention_rows_kernel(const _
     tc_after();
     if (warp == kIssuer / 32) tc_free(tmem, 512);
     if (threadIdx.x == 0 && bars.abort) atomicCAS(p.status, 0, (int)PATCHKV_E_TIMEOUT);
+}
+
+// Images of the two matrices of a step (grid: step, KV head, sequence): the operands of 128 tokens in channel order, laid out and
+// swizzled as in shared memory, tokens behind the cache or on a page out of range zero.  Values that are not finite are set to
+// zero in V and noted.  Bound by memory: reads the cache once, writes 4 bytes per element pair.
+constexpr int kImageThreads = 256;
+template <int KF, int VF, int D>
+__global__ void __launch_bounds__(kImageThreads) attention_image_kernel(const AttentionParams p, const RowsPlan pl) {
+    using S = RowsSmem<D>;
+    constexpr bool kPool = KF == FMT_BF16;
+    constexpr int kPer = D / 32, kTokens = kImageThreads / kPer;        // 32 channels a thread; tokens per pass
+    __shared__ uint32_t meta[8];
+    pdl_trigger();
+    pdl_wait();
+    const int step = blockIdx.x, head = blockIdx.y, seq = blockIdx.z, t0 = step * kRowTile;
+    int first, kv, rows, lo = 0, hi;
+    if (!sequence_rows(p, seq, &first, &kv, &rows) || rows == 0) return;
+    hi = kv - 1;
+    if (!p.b.pos) {                                             // the last positions: what no row sees needs no image
+        const int a = __ldg(p.b.kv_len + seq) - rows;
+        lo = max(-1, a);
+        hi = a + min(rows, p.b.max_rows) - 1;
+    }
+    const TileRange range = step_range(p, kv, p.b.pos ? 0 : lo, hi);
+    if (t0 > min(hi, kv - 1) || (!p.b.pos && step >= range.sink_tiles && step < range.first)) return;
+    if (threadIdx.x < 8) meta[threadIdx.x] = 0;
+    __syncthreads();
+    const int c = threadIdx.x % kPer;
+    uint32_t m0 = 0x64086408u, m1 = 0x64806480u;
+    uint8_t* k_image = pl.images + image_index(p, pl, seq, step, head) * (2 * S::kMat);
+    uint8_t* v_image = k_image + S::kMat;
+#pragma unroll
+    for (int i = 0; i < kRowTile / kTokens; i++) {
+        const int tok = threadIdx.x / kPer + i * kTokens, t = t0 + tok;
+        int page = -1, slot = 0;
+        if (t < kv) {
+            const int lp = div_page(p.c, t);
+            slot = t - lp * p.c.P;
+            page = __ldg(p.b.block_table + (long long)seq * p.b.table_stride + lp);
+            if (page < 0 || page >= p.c.n_pages) {
+                page = -1;
+                if (c == 0) atomicOr(&meta[tok >> 5], 1u << (tok & 31));
+            }
+        }
+        uint4 ko[4], vo[4];
+        if (page < 0) {
+#pragma unroll
+            for (int q = 0; q < 4; q++) ko[q] = vo[q] = make_uint4(0, 0, 0, 0);
+        } else if constexpr (kPool) {
+            const long long o = (long long)page * p.c.stride_page + (long long)slot * p.c.stride_token + (long long)head * p.c.stride_head + 32 * c;
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                ko[q] = __ldg(reinterpret_cast<const uint4*>(p.c.k + o) + q);
+                vo[q] = __ldg(reinterpret_cast<const uint4*>(p.c.v + o) + q);
+            }
+        } else {
+            const uint8_t* pg = p.c.base + (long long)page * p.c.stride_page;
+            const uint32_t row = (uint32_t)slot * p.c.H + head, sc = (row * (D / p.c.G) + c * 32 / p.c.G) * 2;
+            uint32_t ks = __ldg(reinterpret_cast<const uint16_t*>(pg + p.c.k_scales + sc)), vs = __ldg(reinterpret_cast<const uint16_t*>(pg + p.c.v_scales + sc));
+            ks |= ks << 16; vs |= vs << 16;
+            image_operands<KF>(ko, pg + row * (KF == FMT_INT8 ? D : D / 2), c, ks, m0, m1);
+            image_operands<VF>(vo, pg + p.c.v_codes + row * (VF == FMT_INT8 ? D : D / 2), c, vs, m0, m1);
+        }
+        bool lost = false;
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            lost = finite_only<kPool ? 0x7F80u : 0x7C00u>(vo[q]) || lost;
+            *reinterpret_cast<uint4*>(k_image + swizzled(tok, 4 * c + q)) = ko[q];
+            *reinterpret_cast<uint4*>(v_image + swizzled(tok, 4 * c + q)) = vo[q];
+        }
+        if (lost) meta[4] = 1;
+    }
+    __syncthreads();
+    if (threadIdx.x < 8) pl.meta[image_index(p, pl, seq, step, head) * 8 + threadIdx.x] = meta[threadIdx.x];
 }
 
 // Joins the pieces of split rows: a warp per query vector.
