@@ -83,6 +83,14 @@ __device__ __forceinline__ void tc_ld16(uint32_t (&r)[16], uint32_t addr) {
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
           "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(addr) : "memory");
 }
+__device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,"
+        "%27,%28,%29,%30,%31,%32};" ::"r"(addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+        "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
 // One lane of the warp, always the same one.
 __device__ __forceinline__ bool elect_lane() {
     uint32_t yes;
@@ -126,9 +134,10 @@ struct RowsSmem {
     static constexpr int kLaunch = kBytes > 120 * 1024 ? kBytes : 120 * 1024;   // one CTA per SM: it takes all of TMEM
 };
 struct RowsBars {
-    uint64_t q_ready[2], max_ready[2], s_ready[2], p_ready[2], o_ready[2], k_full[2], k_empty[2], v_full[2], v_empty[2], drained;
+    uint64_t q_ready[2], met[2], s_ready[2], p_ready[2], o_ready[2], k_full[2], k_empty[2], v_full[2], v_empty[2], drained;
     alignas(16) uint32_t absent[4][8];          // per step (mod 4): tokens whose page is out of range; word 4: `lost` of an image
     float top[2][2][kRowTile];                  // largest logit of a row in each half of the columns; at the end its sums
+    int32_t exceeded[2];                        // last step in which a tile's weights were too large
     uint32_t tmem;
     int32_t abort, lo, hi, lost;                // lost: a value that is not finite was taken out of a tile that needs a mask
 };
@@ -251,6 +260,12 @@ struct RowsKernel {
     __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, &bars.abort); }
     // The same for a whole warp: all of its lanes go on, or none.
     __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, wait(bar, parity)); }
+    // The eight softmax warps of a tile meet; what they wrote to shared memory before is visible behind it.
+    __device__ __forceinline__ bool meet(uint64_t* bar, uint32_t& phase) {
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
+        return wait_warp(bar, phase++ & 1);
+    }
     // Seen by some row (or by none): only then does a token's slot take part.
     __device__ __forceinline__ bool any_sees(int t) const { return t <= min(hi, kv - 1) && sees(p, lo, t); }
     __device__ __forceinline__ bool whole(int t0) const { return whole_step(p, kv, lo, hi, t0); }
@@ -563,7 +578,7 @@ struct RowsKernel {
         const uint32_t s_at = tmem + lanes + i * kRowTile + 64 * half, o_at = tmem + lanes + (2 + i) * kRowTile + half * (D / 2);
         const float none = factor < 0.0f ? INFINITY : -INFINITY;                      // times the factor: minus infinity
         float ref = kNoMax;
-        uint32_t lost_seen = 0;
+        uint32_t lost_seen = 0, phase = 0;
         f32x2 sum2 = pack2(0.0f, 0.0f);
         const int n = end - begin;
 #pragma unroll 1
@@ -577,68 +592,81 @@ struct RowsKernel {
             if (IMAGE && !plain && (absent.x | absent.y) != 0) latch_absent(64 * half, t0, absent);
             if (IMAGE) lost_seen |= bars.absent[j & 3][4];
             const int b = min(pos, kv - 1) - t0, a = p.window > 0 ? max(pos - p.window + 1, 0) - t0 : -t0, s = p.sinks - t0;
-            // Two passes over the thread's 64 logits, 32 at a time out of TMEM: 80 registers a thread are what 21 warps leave, and
-            // four warps on each scheduler hide the loads.  The loops stay loops: three roles run different code on an SM,
-            // and unrolled it does not stay in the instruction cache.
-            float y[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            // Weights are made against the reference as it stands, and checked afterwards; nothing is stored before both
+            // threads of every row know that no weight exceeds 2^8.  Else (a row's first step, and rarely) the largest logits
+            // are found first, the references moved, and the weights made again.  The loops stay loops: the roles run
+            // different code on an SM, and unrolled it does not stay in the instruction cache.
+            bool search = j == 0;
+            uint32_t w[32];
+            f32x2 total;
+            for (;;) {
+                if (search) {
+                    float y = -INFINITY;
 #pragma unroll 1
-            for (int k = 0; k < 2; k++) {
-                float x[32];
-                tc_ld32(x, s_at + 32 * k);
-                tc_wait_ld();
-                if (!plain) mask_chunk(x, seen(64 * half + 32 * k, a, b, s, k ? absent.y : absent.x), none);
-                if (factor >= 0.0f) {
-#pragma unroll
-                    for (int c = 0; c < 32; c += 2) y[(c >> 1) & 3] = fmaxf(y[(c >> 1) & 3], fmaxf(x[c], x[c + 1]));
-                } else {
-#pragma unroll
-                    for (int c = 0; c < 32; c += 2) y[(c >> 1) & 3] = fmaxf(y[(c >> 1) & 3], fmaxf(-x[c], -x[c + 1]));
-                }
-            }
-            bars.top[i][half][r] = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
-            __syncwarp();
-            if ((threadIdx.x & 31) == 0) mbar_arrive(&bars.max_ready[i]);
-            if (!wait_warp(&bars.max_ready[i], j & 1)) return;
-            const float most = fmaxf(bars.top[i][0][r], bars.top[i][1][r]);
-            const float top = most == -INFINITY ? most : most * fabsf(factor);
-            if (__any_sync(0xFFFFFFFFu, top > ref + 8.0f)) {                         // the same in both halves
-                const float to = top > ref + 8.0f ? top : ref, keep = fast_exp2(ref - to);
-                ref = to;
-                sum2 = mul2(sum2, pack2(keep, keep));
-                if (j > 0)                                      // the products of the steps before are done: s_ready came behind them
-#pragma unroll 1
-                    for (int k = 0; k < D / 32; k++) {
-                        uint32_t w[16];
-                        tc_ld16(w, o_at + 16 * k);
+                    for (int k = 0; k < 4; k++) {
+                        uint32_t x[16];
+                        tc_ld16(x, s_at + 16 * k);
                         tc_wait_ld();
+                        const uint32_t in = plain ? 0xFFFFFFFFu : seen(64 * half + 16 * k, a, b, s, (k & 2 ? absent.y : absent.x) >> (16 * (k & 1)));
 #pragma unroll
-                        for (int c = 0; c < 16; c++) w[c] = __float_as_uint(__uint_as_float(w[c]) * keep);
-                        tc_st16(o_at + 16 * k, w);
+                        for (int c = 0; c < 16; c++) {
+                            const float z = factor < 0.0f ? -__uint_as_float(x[c]) : __uint_as_float(x[c]);
+                            if (in >> c & 1u) y = fmaxf(y, z);
+                        }
                     }
-            }
-            // P lies over the first 32 of the thread's own 64 columns of S, each chunk of 16 on columns that have been read.
-            const f32x2 factor2 = pack2(factor, factor), ref2 = pack2(-ref, -ref);
+                    bars.top[i][half][r] = y;
+                    if (!meet(&bars.met[i], phase)) return;
+                    const float most = fmaxf(bars.top[i][0][r], bars.top[i][1][r]);
+                    const float top = most == -INFINITY ? most : most * fabsf(factor);
+                    const float to = top > ref + 8.0f ? top : ref, keep = fast_exp2(ref - to);
+                    ref = to;
+                    sum2 = mul2(sum2, pack2(keep, keep));
+                    if (j > 0)                                  // the products of the steps before are done: s_ready came behind them
 #pragma unroll 1
-            for (int k = 0; k < 2; k++) {
-                float x[32];
-                tc_ld32(x, s_at + 32 * k);
-                tc_wait_ld();
-                if (!plain) mask_chunk(x, seen(64 * half + 32 * k, a, b, s, k ? absent.y : absent.x), none);
-                uint32_t w[16];
+                        for (int k = 0; k < D / 32; k++) {
+                            uint32_t o[16];
+                            tc_ld16(o, o_at + 16 * k);
+                            tc_wait_ld();
 #pragma unroll
-                for (int c = 0; c < 16; c++) {
-                    float e, f;
-                    unpack2(fma2(pack2(x[2 * c], x[2 * c + 1]), factor2, ref2), e, f);
-                    e = fast_exp2(e);
-                    f = fast_exp2(f);
-                    sum2 = add2(sum2, pack2(e, f));
-                    w[c] = kPool ? bf162_bits(e, f) : half2_bits(e, f);
+                            for (int c = 0; c < 16; c++) o[c] = __float_as_uint(__uint_as_float(o[c]) * keep);
+                            tc_st16(o_at + 16 * k, o);
+                        }
                 }
-                tc_st16(s_at + 16 * k, w);
+                const f32x2 factor2 = pack2(factor, factor), ref2 = pack2(-ref, -ref);
+                total = sum2;
+#pragma unroll
+                for (int k = 0; k < 2; k++) {
+                    float x[32];
+                    tc_ld32(x, s_at + 32 * k);
+                    tc_wait_ld();
+                    if (!plain) mask_chunk(x, seen(64 * half + 32 * k, a, b, s, k ? absent.y : absent.x), none);
+#pragma unroll
+                    for (int c = 0; c < 16; c++) {
+                        float e, f;
+                        unpack2(fma2(pack2(x[2 * c], x[2 * c + 1]), factor2, ref2), e, f);
+                        e = fast_exp2(e);
+                        f = fast_exp2(f);
+                        total = add2(total, pack2(e, f));
+                        w[16 * k + c] = kPool ? bf162_bits(e, f) : half2_bits(e, f);
+                    }
+                }
+                if (search) break;
+                uint32_t most = 0;                              // weights are not negative: their bit patterns order them
+#pragma unroll
+                for (int c = 0; c < 32; c++) most = __vmaxu2(most, w[c]);
+                constexpr uint32_t kLimit = kPool ? 0x4380u : 0x5C00u;                  // 2^8
+                if (__any_sync(0xFFFFFFFFu, max(most & 0xFFFFu, most >> 16) > kLimit)) *reinterpret_cast<volatile int32_t*>(&bars.exceeded[i]) = j;
+                if (!meet(&bars.met[i], phase)) return;
+                search = *reinterpret_cast<volatile int32_t*>(&bars.exceeded[i]) == j;
+                if (!search) break;
             }
+            sum2 = total;
+            // P lies over the first 32 of the thread's own 64 columns of S.
+            tc_st32(s_at, w);
             tc_wait_st();
             tc_before();
-            mbar_arrive(&bars.p_ready[i]);
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0) mbar_arrive(&bars.p_ready[i]);
         }
         if (n > 0 && !wait_warp(&bars.o_ready[i], 0)) return;
         tc_after();
@@ -646,9 +674,7 @@ struct RowsKernel {
         unpack2(sum2, sum, sum_odd);
         sum += sum_odd;
         bars.top[i][half][r] = sum;                             // (nobody reads a maximum any more: o_ready came behind all of P)
-        __syncwarp();
-        if ((threadIdx.x & 31) == 0) mbar_arrive(&bars.max_ready[i]);
-        if (!wait_warp(&bars.max_ready[i], n & 1)) return;
+        if (!meet(&bars.met[i], phase)) return;
         sum = bars.top[i][0][r] + bars.top[i][1][r];
         if (broken && sum != 0.0f) sum = __uint_as_float(0x7FC00000u);
         const bool lost = IMAGE ? lost_seen != 0 : *reinterpret_cast<volatile int32_t*>(&bars.lost) != 0;
@@ -714,8 +740,9 @@ __global__ void __launch_bounds__(rows_threads(IMAGE), 1) attention_rows_kernel(
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0);
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; i++) {
-            mbar_init(&bars.q_ready[i], 2 * kRowTile); mbar_init(&bars.p_ready[i], 2 * kRowTile);
-            mbar_init(&bars.max_ready[i], 8);
+            mbar_init(&bars.q_ready[i], 2 * kRowTile);
+            mbar_init(&bars.p_ready[i], 8); mbar_init(&bars.met[i], 8);              // the eight warps of a tile
+            bars.exceeded[i] = -1;
             mbar_init(&bars.s_ready[i], 1); mbar_init(&bars.o_ready[i], 1);
             mbar_init(&bars.k_full[i], IMAGE ? 1 : 128); mbar_init(&bars.v_full[i], IMAGE ? 1 : 128);
             mbar_init(&bars.k_empty[i], 1); mbar_init(&bars.v_empty[i], 1);
