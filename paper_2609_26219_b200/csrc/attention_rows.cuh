@@ -4,12 +4,11 @@
 // the other, vector m = row * share + head, so that no row of the tiles is left empty whatever share is.  It walks the
 // tokens in tiles of 128:
 //   S = Q K^T    tcgen05.mma, 128 x 128 x D, both operands in shared memory, S in TMEM
-//   P = 2^(S - ref)   two threads per row, 64 columns each; P goes back to TMEM as 16-bit numbers over its S
+//   P = 2^(S - ref)   a thread per row; P goes back to TMEM as 16-bit numbers over its S
 //   O += P V     tcgen05.mma, 128 x D x 128, P from TMEM, V from shared memory, O in TMEM
-// Roles: two warpgroups per tile for the softmax, one warp that issues the products, four warps that bring K and V.  The two tiles
-// take turns: while one is in its softmax the tensor cores work for the other.  (With one softmax thread per row the chain
-// softmax - P V - Q K^T of a tile took 5700 cycles a step, 3000 of them in that thread and 90 per product in an issuing thread
-// the compiler did not know to be alone; the products need 2050.)
+// Roles: a warpgroup per tile for the softmax, one warp that issues the products, the warps that bring K and V.  The two tiles
+// take turns: while one is in its softmax the tensor cores work for the other.  A step's products take 2050 cycles and its
+// exponentials as long; what a step takes is the chain of one tile, softmax - P V - Q K^T, and most of the work went into the first.
 // The codes have to become operands on the way: fp16(code * scale), one rounding of 2^-12.  Where several CTAs need the same tokens
 // (two tiles of CTAs or more) a first kernel does that once per token and leaves images of the two shared-memory matrices of
 // each step in the workspace, which a CTA then fetches with one bulk copy each; converting in every CTA kept four warps busy for
@@ -26,8 +25,8 @@
 namespace patchkv {
 
 constexpr int kRowTile = 128;                   // query vectors of a tile, and tokens of a step
-constexpr int kProducer0 = 512;                 // four softmax warpgroups, then the warps that bring K and V (four, or one that copies
-__host__ __device__ constexpr int rows_issuer(bool image) { return image ? 544 : 640; }             // images), then the issuing warp
+constexpr int kProducer0 = 256;                 // two softmax warpgroups, then the warps that bring K and V (four, or one that copies
+__host__ __device__ constexpr int rows_issuer(bool image) { return image ? 288 : 384; }             // images), then the issuing warp
 __host__ __device__ constexpr int rows_threads(bool image) { return rows_issuer(image) + 32; }
 
 struct RowsPlan {
@@ -83,13 +82,18 @@ __device__ __forceinline__ void tc_ld16(uint32_t (&r)[16], uint32_t addr) {
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
           "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t (&r)[32]) {
+__device__ __forceinline__ void tc_st64(uint32_t addr, const uint32_t (&r)[64]) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,"
-        "%27,%28,%29,%30,%31,%32};" ::"r"(addr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
-        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
-        "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+        "tcgen05.st.sync.aligned.32x32b.x64.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,"
+        "%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,"
+        "%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63,%64};" ::"r"(addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
+        "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]),
+        "r"(r[31]), "r"(r[32]), "r"(r[33]), "r"(r[34]), "r"(r[35]), "r"(r[36]), "r"(r[37]), "r"(r[38]), "r"(r[39]), "r"(r[40]),
+        "r"(r[41]), "r"(r[42]), "r"(r[43]), "r"(r[44]), "r"(r[45]), "r"(r[46]), "r"(r[47]), "r"(r[48]), "r"(r[49]), "r"(r[50]),
+        "r"(r[51]), "r"(r[52]), "r"(r[53]), "r"(r[54]), "r"(r[55]), "r"(r[56]), "r"(r[57]), "r"(r[58]), "r"(r[59]), "r"(r[60]),
+        "r"(r[61]), "r"(r[62]), "r"(r[63]) : "memory");
 }
 // One lane of the warp, always the same one.
 __device__ __forceinline__ bool elect_lane() {
@@ -130,18 +134,16 @@ template <int D>
 struct RowsSmem {
     static constexpr int kMat = kRowTile * D * 2;               // one 128-row matrix
     static constexpr int kQ = 0, kK = 2 * kMat, kV = 4 * kMat, kBars = 6 * kMat;
-    static constexpr int kBytes = kBars + 3072 + 1024;          // 1024: the matrices start on a multiple of that
+    static constexpr int kBytes = kBars + 512 + 1024;           // 1024: the matrices start on a multiple of that
     static constexpr int kLaunch = kBytes > 120 * 1024 ? kBytes : 120 * 1024;   // one CTA per SM: it takes all of TMEM
 };
 struct RowsBars {
-    uint64_t q_ready[2], met[2], s_ready[2], p_ready[2], o_ready[2], k_full[2], k_empty[2], v_full[2], v_empty[2], drained;
+    uint64_t q_ready[2], s_ready[2], p_ready[2], o_ready[2], k_full[2], k_empty[2], v_full[2], v_empty[2], drained;
     alignas(16) uint32_t absent[4][8];          // per step (mod 4): tokens whose page is out of range; word 4: `lost` of an image
-    float top[2][2][kRowTile];                  // largest logit of a row in each half of the columns; at the end its sums
-    int32_t exceeded[2];                        // last step in which a tile's weights were too large
     uint32_t tmem;
     int32_t abort, lo, hi, lost;                // lost: a value that is not finite was taken out of a tile that needs a mask
 };
-static_assert(sizeof(RowsBars) <= 3072 && offsetof(RowsBars, absent) % 16 == 0, "barrier area");
+static_assert(sizeof(RowsBars) <= 512 && offsetof(RowsBars, absent) % 16 == 0, "barrier area");
 
 // Steps of 128 tokens that the rows between positions lo and hi see (as tile_range, in other units).
 __device__ __forceinline__ TileRange step_range(const AttentionParams& p, int kv, int lo_pos, int hi_pos) {
@@ -260,12 +262,6 @@ struct RowsKernel {
     __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) { return mbar_wait(bar, parity, &bars.abort); }
     // The same for a whole warp: all of its lanes go on, or none.
     __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, wait(bar, parity)); }
-    // The eight softmax warps of a tile meet; what they wrote to shared memory before is visible behind it.
-    __device__ __forceinline__ bool meet(uint64_t* bar, uint32_t& phase) {
-        __syncwarp();
-        if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
-        return wait_warp(bar, phase++ & 1);
-    }
     // Seen by some row (or by none): only then does a token's slot take part.
     __device__ __forceinline__ bool any_sees(int t) const { return t <= min(hi, kv - 1) && sees(p, lo, t); }
     __device__ __forceinline__ bool whole(int t0) const { return whole_step(p, kv, lo, hi, t0); }
@@ -488,7 +484,7 @@ struct RowsKernel {
                     tc_mma_ts(o, a, v, kPv, j != 0);
 #pragma unroll
                     for (int x = 1; x < kRowTile / 16; x++)       // 16 tokens: 8 columns of P, two groups of 8 rows of V
-                        tc_mma_ts(o, a + 8 * x + (x >= 4 ? 32 : 0), v + x * 128, kPv, true);
+                        tc_mma_ts(o, a + 8 * x, v + x * 128, kPv, true);
                     if (i == tiles - 1) tc_commit(&bars.v_empty[st]);
                     if (j + 1 == n) tc_commit(&bars.o_ready[i]);
                 }
@@ -499,9 +495,12 @@ struct RowsKernel {
     }
 
     // Tokens on pages out of range count when some row sees them (with images nobody has looked at that yet).
-    __device__ __forceinline__ void latch_absent(int c0, int t0, const uint2& absent) const {
+    __device__ __forceinline__ void latch_absent(int t0, const uint4& absent) const {
         const int lane = threadIdx.x & 31;
-        if ((absent.x >> lane & 1u && any_sees(t0 + c0 + lane)) || (absent.y >> lane & 1u && any_sees(t0 + c0 + 32 + lane))) latch(p.status);
+        const uint32_t gone[4] = {absent.x, absent.y, absent.z, absent.w};
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+            if (gone[k] >> lane & 1u && any_sees(t0 + 32 * k + lane)) latch(p.status);
     }
 
     // Bit c: this row sees column c0 + c.
@@ -509,121 +508,134 @@ struct RowsKernel {
         auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u; };      // bits [0, n)
         return below(b + 1 - c0) & (~below(a - c0) | below(s - c0)) & ~gone;
     }
-    // What a row does not see becomes the value whose weight is zero: times the factor minus infinity.
-    __device__ __forceinline__ static void mask_chunk(float (&x)[32], uint32_t seen, float none) {
+    // ---- softmax: a thread per query vector
+    // The query into shared memory: cp.async, then (quantised pages) in place to fp16, scaled so that the largest magnitude lies in
+    // [2^13, 2^14).  A vector with a NaN or an infinity gives NaN.  Returns the factor of its logits.
+    __device__ __forceinline__ float load_query(int i, int r, bool live, int row, int hq) {
+        const uint16_t* q = p.q + (long long)row * p.q_stride_row + (long long)hq * p.q_stride_head;
+        const uint32_t mat = smem + S::kQ + i * S::kMat;
+#pragma unroll 1
+        for (int c = 0; c < D / 8; c++) cp16(mat + swizzled(r, c), q + 8 * c, live);
+        cp_commit();
+        cp_wait<0>();
+        if (kPool) return p.scale_log2;
+        float amax = 0.0f, bad = 0.0f;
+#pragma unroll 1
+        for (int c = 0; c < D / 8; c++) {
+            const uint4 v = lds128(mat + swizzled(r, c));
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int c = 0; c < 32; c++) x[c] = seen >> c & 1u ? x[c] : none;
+            for (int k = 0; k < 4; k++) {
+                const float a = p.f16 ? low_half(w[k]) : bf16_bits_to_float(w[k] & 0xFFFFu), b = p.f16 ? high_half(w[k]) : __uint_as_float(w[k] & 0xFFFF0000u);
+                amax = fmaxf(amax, fmaxf(fabsf(a), fabsf(b)));
+                bad = fmaf(a, 0.0f, fmaf(b, 0.0f, bad));
+            }
+        }
+        const int e = (int)(__float_as_uint(amax) >> 23) - 127;
+        const int shift = amax > 0.0f ? min(13 - e, 120) : 0;
+        const float up = exp2i(shift);
+#pragma unroll 1
+        for (int c = 0; c < D / 8; c++) {
+            uint4 v = lds128(mat + swizzled(r, c));
+            if (bad != 0.0f) v = make_uint4(0, 0, 0, 0);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            float f[8];
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                f[2 * k] = (p.f16 ? low_half(w[k]) : bf16_bits_to_float(w[k] & 0xFFFFu)) * up;
+                f[2 * k + 1] = (p.f16 ? high_half(w[k]) : __uint_as_float(w[k] & 0xFFFF0000u)) * up;
+            }
+            if (KF == FMT_INT4)                                 // the order operands4 leaves the channels in
+                sts128(mat + swizzled(r, c), half2_bits(f[0], f[4]), half2_bits(f[1], f[5]), half2_bits(f[2], f[6]), half2_bits(f[3], f[7]));
+            else
+                sts128(mat + swizzled(r, c), half2_bits(f[0], f[1]), half2_bits(f[2], f[3]), half2_bits(f[4], f[5]), half2_bits(f[6], f[7]));
+        }
+        return p.scale_log2 * exp2i(-shift) + bad;
     }
 
-    // ---- softmax: two threads per query vector, one per half of a step's tokens (and of the channels at the ends)
-    __device__ __forceinline__ void softmax(int i, int half, int first, int m, int m_end, uint32_t tmem, const RowsPlan& pl, int split) {
+    // 32 logits -> 16 words of weights against the reference; their sum onto `total`.
+    __device__ __forceinline__ static void weigh(const float (&x)[32], uint32_t* w, f32x2 factor2, f32x2 ref2, f32x2& total) {
+#pragma unroll
+        for (int c = 0; c < 16; c++) {
+            float e, f;
+            unpack2(fma2(pack2(x[2 * c], x[2 * c + 1]), factor2, ref2), e, f);
+            e = fast_exp2(e);
+            f = fast_exp2(f);
+            total = add2(total, pack2(e, f));
+            w[c] = kPool ? bf162_bits(e, f) : half2_bits(e, f);
+        }
+    }
+
+    __device__ __forceinline__ void softmax(int i, int first, int m, int m_end, uint32_t tmem, const RowsPlan& pl, int split) {
         const int r = threadIdx.x & 127;
         const bool live = m < m_end;
         const int row = live ? first + m / p.share : first, hq = live ? head * p.share + m % p.share : 0;
         const int pos = live ? max(-1, row_position(p.b, seq, row)) : -1;
-        // the query into shared memory; each half writes its channels
-        float factor = p.scale_log2;
-        {
-            const uint4* q = reinterpret_cast<const uint4*>(p.q + (long long)row * p.q_stride_row + (long long)hq * p.q_stride_head);
-            const uint32_t mat = smem + S::kQ + i * S::kMat;
-            constexpr int kHalf = D / 16;                       // 16-byte chunks of a half
-            if constexpr (kPool) {
-#pragma unroll 4
-                for (int c = half * kHalf; c < (half + 1) * kHalf; c++) {
-                    const uint4 x = live ? __ldg(q + c) : make_uint4(0, 0, 0, 0);
-                    sts128(mat + swizzled(r, c), x.x, x.y, x.z, x.w);
-                }
-            } else {
-                // scaled so that the largest magnitude lies in [2^13, 2^14); a vector with a NaN or an infinity gives NaN
-                float amax = 0.0f, bad = 0.0f;
-#pragma unroll 4
-                for (int c = 0; c < 2 * kHalf; c++) {
-                    const uint4 x = live ? __ldg(q + c) : make_uint4(0, 0, 0, 0);
-                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                    for (int k = 0; k < 4; k++) {
-                        const float a = p.f16 ? low_half(w[k]) : bf16_bits_to_float(w[k] & 0xFFFFu), b = p.f16 ? high_half(w[k]) : __uint_as_float(w[k] & 0xFFFF0000u);
-                        amax = fmaxf(amax, fmaxf(fabsf(a), fabsf(b)));
-                        bad = fmaf(a, 0.0f, fmaf(b, 0.0f, bad));
-                    }
-                }
-                const int e = (int)(__float_as_uint(amax) >> 23) - 127;
-                const int shift = amax > 0.0f ? min(13 - e, 120) : 0;
-                const float up = exp2i(shift);
-                factor = p.scale_log2 * exp2i(-shift) + bad;
-#pragma unroll 2
-                for (int c = half * kHalf; c < (half + 1) * kHalf; c++) {
-                    const uint4 x = live && bad == 0.0f ? __ldg(q + c) : make_uint4(0, 0, 0, 0);
-                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-                    float f[8];
-#pragma unroll
-                    for (int k = 0; k < 4; k++) {
-                        f[2 * k] = (p.f16 ? low_half(w[k]) : bf16_bits_to_float(w[k] & 0xFFFFu)) * up;
-                        f[2 * k + 1] = (p.f16 ? high_half(w[k]) : __uint_as_float(w[k] & 0xFFFF0000u)) * up;
-                    }
-                    if (KF == FMT_INT4)                         // the order operands4 leaves the channels in
-                        sts128(mat + swizzled(r, c), half2_bits(f[0], f[4]), half2_bits(f[1], f[5]), half2_bits(f[2], f[6]), half2_bits(f[3], f[7]));
-                    else
-                        sts128(mat + swizzled(r, c), half2_bits(f[0], f[1]), half2_bits(f[2], f[3]), half2_bits(f[4], f[5]), half2_bits(f[6], f[7]));
-                }
-            }
-        }
+        float factor = load_query(i, r, live, row, hq);
         fence_async_smem();
-        mbar_arrive(&bars.q_ready[i]);
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(&bars.q_ready[i]);
         // A mask is minus infinity over the factor: a factor of zero is one that leaves no logit, a NaN enters at the end.
         const bool broken = factor != factor;
         if (broken) factor = 1.0f;
         if (factor == 0.0f) factor = 1.17549435e-38f;
         const uint32_t lanes = (uint32_t)((threadIdx.x >> 5) & 3) << 21;              // the warp's quarter of the TMEM lanes
-        const uint32_t s_at = tmem + lanes + i * kRowTile + 64 * half, o_at = tmem + lanes + (2 + i) * kRowTile + half * (D / 2);
-        const float none = factor < 0.0f ? INFINITY : -INFINITY;                      // times the factor: minus infinity
+        const uint32_t s_at = tmem + lanes + i * kRowTile, o_at = tmem + lanes + (2 + i) * kRowTile;
         float ref = kNoMax;
-        uint32_t lost_seen = 0, phase = 0;
+        uint32_t lost_seen = 0;
         f32x2 sum2 = pack2(0.0f, 0.0f);
+        const f32x2 factor2 = pack2(factor, factor);
         const int n = end - begin;
 #pragma unroll 1
         for (int j = 0; j < n; j++) {
             const int t0 = range.tile(begin + j) * kRowTile;
             if (!wait_warp(&bars.s_ready[i], j & 1)) return;
             tc_after();
-            // Columns of the step this row sees: [a, b] and [0, s); what its pages don't hold is in `absent`.
-            const uint2 absent = lds64(smem_u32(&bars.absent[j & 3][2 * half]));
-            const bool plain = whole(t0) && (absent.x | absent.y) == 0;
-            if (IMAGE && !plain && (absent.x | absent.y) != 0) latch_absent(64 * half, t0, absent);
+            const uint4 absent = lds128(smem_u32(bars.absent[j & 3]));
             if (IMAGE) lost_seen |= bars.absent[j & 3][4];
-            const int b = min(pos, kv - 1) - t0, a = p.window > 0 ? max(pos - p.window + 1, 0) - t0 : -t0, s = p.sinks - t0;
-            // Weights are made against the reference as it stands, and checked afterwards; nothing is stored before both
-            // threads of every row know that no weight exceeds 2^8.  Else (a row's first step, and rarely) the largest logits
-            // are found first, the references moved, and the weights made again.  The loops stay loops: the roles run
-            // different code on an SM, and unrolled it does not stay in the instruction cache.
-            bool search = j == 0;
-            uint32_t w[32];
+            const bool gaps = (absent.x | absent.y | absent.z | absent.w) != 0;
+            if (gaps || !whole(t0)) {
+                // What a row does not see becomes the logit whose product with the factor is minus infinity, in TMEM: steps that
+                // need a mask are few, and the code below stays free of it.
+                if (IMAGE && gaps) latch_absent(t0, absent);
+                const int b = min(pos, kv - 1) - t0, a = p.window > 0 ? max(pos - p.window + 1, 0) - t0 : -t0, s = p.sinks - t0;
+                const uint32_t none = factor < 0.0f ? 0x7F800000u : 0xFF800000u;
+#pragma unroll 1
+                for (int k = 0; k < 8; k++) {
+                    const uint32_t gone = (k < 2 ? absent.x : k < 4 ? absent.y : k < 6 ? absent.z : absent.w) >> (16 * (k & 1));
+                    const uint32_t in = seen(16 * k, a, b, s, gone);
+                    uint32_t x[16];
+                    tc_ld16(x, s_at + 16 * k);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int c = 0; c < 16; c++) x[c] = in >> c & 1u ? x[c] : none;
+                    tc_st16(s_at + 16 * k, x);
+                }
+                tc_wait_st();
+            }
+            // Weights are made against the reference as it stands, and checked: nothing is stored before it is known that none exceeds
+            // 2^8.  Else (a row's first step, and rarely) the largest logits are found, the references of the warp's rows moved,
+            // and the weights made again.
+            uint32_t w[64];
             f32x2 total;
+            bool search = j == 0;
             for (;;) {
                 if (search) {
                     float y = -INFINITY;
 #pragma unroll 1
-                    for (int k = 0; k < 4; k++) {
+                    for (int k = 0; k < 8; k++) {
                         uint32_t x[16];
                         tc_ld16(x, s_at + 16 * k);
                         tc_wait_ld();
-                        const uint32_t in = plain ? 0xFFFFFFFFu : seen(64 * half + 16 * k, a, b, s, (k & 2 ? absent.y : absent.x) >> (16 * (k & 1)));
 #pragma unroll
-                        for (int c = 0; c < 16; c++) {
-                            const float z = factor < 0.0f ? -__uint_as_float(x[c]) : __uint_as_float(x[c]);
-                            if (in >> c & 1u) y = fmaxf(y, z);
-                        }
+                        for (int c = 0; c < 16; c++) y = fmaxf(y, __uint_as_float(x[c]) * factor);
                     }
-                    bars.top[i][half][r] = y;
-                    if (!meet(&bars.met[i], phase)) return;
-                    const float most = fmaxf(bars.top[i][0][r], bars.top[i][1][r]);
-                    const float top = most == -INFINITY ? most : most * fabsf(factor);
-                    const float to = top > ref + 8.0f ? top : ref, keep = fast_exp2(ref - to);
+                    const float to = y > ref + 8.0f ? y : ref, keep = fast_exp2(ref - to);
                     ref = to;
                     sum2 = mul2(sum2, pack2(keep, keep));
                     if (j > 0)                                  // the products of the steps before are done: s_ready came behind them
 #pragma unroll 1
-                        for (int k = 0; k < D / 32; k++) {
+                        for (int k = 0; k < D / 16; k++) {
                             uint32_t o[16];
                             tc_ld16(o, o_at + 16 * k);
                             tc_wait_ld();
@@ -632,37 +644,42 @@ struct RowsKernel {
                             tc_st16(o_at + 16 * k, o);
                         }
                 }
-                const f32x2 factor2 = pack2(factor, factor), ref2 = pack2(-ref, -ref);
+                const f32x2 ref2 = pack2(-ref, -ref);
                 total = sum2;
-#pragma unroll
-                for (int k = 0; k < 2; k++) {
-                    float x[32];
-                    tc_ld32(x, s_at + 32 * k);
+                float x[32];
+                if constexpr (IMAGE) {                          // registers for two chunks: one on its way while the other is weighed
+                    float z[32];
+                    tc_ld32(x, s_at);
                     tc_wait_ld();
-                    if (!plain) mask_chunk(x, seen(64 * half + 32 * k, a, b, s, k ? absent.y : absent.x), none);
+                    tc_ld32(z, s_at + 32);
+                    weigh(x, w, factor2, ref2, total);
+                    tc_wait_ld();
+                    tc_ld32(x, s_at + 64);
+                    weigh(z, w + 16, factor2, ref2, total);
+                    tc_wait_ld();
+                    tc_ld32(z, s_at + 96);
+                    weigh(x, w + 32, factor2, ref2, total);
+                    tc_wait_ld();
+                    weigh(z, w + 48, factor2, ref2, total);
+                } else {
 #pragma unroll
-                    for (int c = 0; c < 16; c++) {
-                        float e, f;
-                        unpack2(fma2(pack2(x[2 * c], x[2 * c + 1]), factor2, ref2), e, f);
-                        e = fast_exp2(e);
-                        f = fast_exp2(f);
-                        total = add2(total, pack2(e, f));
-                        w[16 * k + c] = kPool ? bf162_bits(e, f) : half2_bits(e, f);
+                    for (int k = 0; k < 4; k++) {
+                        tc_ld32(x, s_at + 32 * k);
+                        tc_wait_ld();
+                        weigh(x, w + 16 * k, factor2, ref2, total);
                     }
                 }
                 if (search) break;
-                uint32_t most = 0;                              // weights are not negative: their bit patterns order them
+                uint32_t most[4] = {0, 0, 0, 0};                // weights are not negative: their bit patterns order them
 #pragma unroll
-                for (int c = 0; c < 32; c++) most = __vmaxu2(most, w[c]);
+                for (int c = 0; c < 64; c++) most[c & 3] = __vmaxu2(most[c & 3], w[c]);
+                const uint32_t top = __vmaxu2(__vmaxu2(most[0], most[1]), __vmaxu2(most[2], most[3]));
                 constexpr uint32_t kLimit = kPool ? 0x4380u : 0x5C00u;                  // 2^8
-                if (__any_sync(0xFFFFFFFFu, max(most & 0xFFFFu, most >> 16) > kLimit)) *reinterpret_cast<volatile int32_t*>(&bars.exceeded[i]) = j;
-                if (!meet(&bars.met[i], phase)) return;
-                search = *reinterpret_cast<volatile int32_t*>(&bars.exceeded[i]) == j;
+                search = __any_sync(0xFFFFFFFFu, max(top & 0xFFFFu, top >> 16) > kLimit);
                 if (!search) break;
             }
             sum2 = total;
-            // P lies over the first 32 of the thread's own 64 columns of S.
-            tc_st32(s_at, w);
+            tc_st64(s_at, w);                                   // over the first half of S
             tc_wait_st();
             tc_before();
             __syncwarp();
@@ -673,9 +690,6 @@ struct RowsKernel {
         float sum, sum_odd;
         unpack2(sum2, sum, sum_odd);
         sum += sum_odd;
-        bars.top[i][half][r] = sum;                             // (nobody reads a maximum any more: o_ready came behind all of P)
-        if (!meet(&bars.met[i], phase)) return;
-        sum = bars.top[i][0][r] + bars.top[i][1][r];
         if (broken && sum != 0.0f) sum = __uint_as_float(0x7FC00000u);
         const bool lost = IMAGE ? lost_seen != 0 : *reinterpret_cast<volatile int32_t*>(&bars.lost) != 0;
         const float inv = pl.splits > 1 ? 1.0f : (sum != 0.0f ? 1.0f / sum : 0.0f);
@@ -683,10 +697,10 @@ struct RowsKernel {
         float* part = pl.partial + ((long long)split * p.b.n_rows * p.Hq + vec) * D;
         uint16_t* out = p.out + (long long)row * p.out_stride_row + (long long)hq * p.out_stride_head;
 #pragma unroll 1
-        for (int k = half * (D / 64); k < (half + 1) * (D / 64); k++) {
+        for (int k = 0; k < D / 32; k++) {
             float o[32];
             if (n > 0) {
-                tc_ld32(o, tmem + lanes + (2 + i) * kRowTile + 32 * k);
+                tc_ld32(o, o_at + 32 * k);
                 tc_wait_ld();
             } else {
 #pragma unroll
@@ -721,7 +735,7 @@ struct RowsKernel {
                 }
             }
         }
-        if (live && half == 0 && pl.splits > 1) {
+        if (live && pl.splits > 1) {
             float* ml = pl.partial + (long long)pl.splits * p.b.n_rows * p.Hq * D + ((long long)split * p.b.n_rows * p.Hq + vec) * 2;
             *reinterpret_cast<float2*>(ml) = make_float2(ref, sum);
         }
@@ -740,9 +754,7 @@ __global__ void __launch_bounds__(rows_threads(IMAGE), 1) attention_rows_kernel(
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0);
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; i++) {
-            mbar_init(&bars.q_ready[i], 2 * kRowTile);
-            mbar_init(&bars.p_ready[i], 8); mbar_init(&bars.met[i], 8);              // the eight warps of a tile
-            bars.exceeded[i] = -1;
+            mbar_init(&bars.q_ready[i], 4); mbar_init(&bars.p_ready[i], 4);          // the four warps of a tile
             mbar_init(&bars.s_ready[i], 1); mbar_init(&bars.o_ready[i], 1);
             mbar_init(&bars.k_full[i], IMAGE ? 1 : 128); mbar_init(&bars.v_full[i], IMAGE ? 1 : 128);
             mbar_init(&bars.k_empty[i], 1); mbar_init(&bars.v_empty[i], 1);
@@ -785,8 +797,8 @@ __global__ void __launch_bounds__(rows_threads(IMAGE), 1) attention_rows_kernel(
     k.end = (int)((long long)k.range.count * (split + 1) / pl.splits);
     const int tiles = m_end - m0 > kRowTile ? 2 : 1;
     if (warp < kProducer0 / 32) {
-        const int i = warp >> 3, half = warp >> 2 & 1;          // tile, half of its columns
-        if (i < tiles) k.softmax(i, half, first, m0 + i * kRowTile + (threadIdx.x & 127), m_end, tmem, pl, split);
+        const int i = warp >> 2;
+        if (i < tiles) k.softmax(i, first, m0 + (int)threadIdx.x, m_end, tmem, pl, split);
     } else if (warp < kIssuer / 32) {
         if constexpr (IMAGE) {
             k.fetch_images(pl);
