@@ -512,15 +512,24 @@ struct RowsKernel {
     // The query into shared memory: cp.async, then (quantised pages) in place to fp16, scaled so that the largest magnitude lies in
     // [2^13, 2^14).  A vector with a NaN or an infinity gives NaN.  Returns the factor of its logits.
     __device__ __forceinline__ float load_query(int i, int r, bool live, int row, int hq) {
-        const uint16_t* q = p.q + (long long)row * p.q_stride_row + (long long)hq * p.q_stride_head;
+        const long long mine = (long long)row * p.q_stride_row + (long long)hq * p.q_stride_head;
         const uint32_t mat = smem + S::kQ + i * S::kMat;
-#pragma unroll 1
-        for (int c = 0; c < D / 8; c++) cp16(mat + swizzled(r, c), q + 8 * c, live);
+        // The warp's 32 rows, a run of D / 8 lanes each: row by row of a thread is 32 cache lines an instruction.
+        constexpr int kRun = D / 8;
+        const int lane = threadIdx.x & 31;
+#pragma unroll 4
+        for (int k = 0; k < kRun; k++) {
+            const int from = k * (32 / kRun) + lane / kRun;
+            const long long at = __shfl_sync(0xFFFFFFFFu, mine, from);
+            const bool there = __shfl_sync(0xFFFFFFFFu, (int)live, from) != 0;
+            cp16(mat + swizzled((r & ~31) + from, lane % kRun), p.q + at + 8 * (lane % kRun), there);
+        }
         cp_commit();
         cp_wait<0>();
+        __syncwarp();
         if (kPool) return p.scale_log2;
         float amax = 0.0f, bad = 0.0f;
-#pragma unroll 1
+#pragma unroll 4
         for (int c = 0; c < D / 8; c++) {
             const uint4 v = lds128(mat + swizzled(r, c));
             const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -534,7 +543,7 @@ struct RowsKernel {
         const int e = (int)(__float_as_uint(amax) >> 23) - 127;
         const int shift = amax > 0.0f ? min(13 - e, 120) : 0;
         const float up = exp2i(shift);
-#pragma unroll 1
+#pragma unroll 2
         for (int c = 0; c < D / 8; c++) {
             uint4 v = lds128(mat + swizzled(r, c));
             if (bad != 0.0f) v = make_uint4(0, 0, 0, 0);
@@ -614,8 +623,8 @@ struct RowsKernel {
                 tc_wait_st();
             }
             // Weights are made against the reference as it stands, and checked: nothing is stored before it is known that none exceeds
-            // 2^8.  Else (a row's first step, and rarely) the largest logits are found, the references of the warp's rows moved,
-            // and the weights made again.
+            // 2^8.  Else (a row's first step, and rarely) the largest logits are found, the references of the warp's rows moved to
+            // 4 above them (so that it is rare), and the weights made again.
             uint32_t w[64];
             f32x2 total;
             bool search = j == 0;
@@ -630,7 +639,7 @@ struct RowsKernel {
 #pragma unroll
                         for (int c = 0; c < 16; c++) y = fmaxf(y, __uint_as_float(x[c]) * factor);
                     }
-                    const float to = y > ref + 8.0f ? y : ref, keep = fast_exp2(ref - to);
+                    const float to = y > ref + 8.0f ? y + 4.0f : ref, keep = fast_exp2(ref - to);
                     ref = to;
                     sum2 = mul2(sum2, pack2(keep, keep));
                     if (j > 0)                                  // the products of the steps before are done: s_ready came behind them
@@ -690,12 +699,11 @@ struct RowsKernel {
         float sum, sum_odd;
         unpack2(sum2, sum, sum_odd);
         sum += sum_odd;
-        if (broken && sum != 0.0f) sum = __uint_as_float(0x7FC00000u);
+        if (broken && sum > 1.0e-30f) sum = __uint_as_float(0x7FC00000u);
         const bool lost = IMAGE ? lost_seen != 0 : *reinterpret_cast<volatile int32_t*>(&bars.lost) != 0;
         const float inv = pl.splits > 1 ? 1.0f : (sum != 0.0f ? 1.0f / sum : 0.0f);
         const long long vec = (long long)row * p.Hq + hq;
         float* part = pl.partial + ((long long)split * p.b.n_rows * p.Hq + vec) * D;
-        uint16_t* out = p.out + (long long)row * p.out_stride_row + (long long)hq * p.out_stride_head;
 #pragma unroll 1
         for (int k = 0; k < D / 32; k++) {
             float o[32];
@@ -714,7 +722,6 @@ struct RowsKernel {
 #pragma unroll
                 for (int c = 0; c < 32; c++) o[c] = fixed[c];
             }
-            if (!live) continue;
 #pragma unroll
             for (int c = 0; c < 32; c += 8) {
                 float y[8];
@@ -724,15 +731,29 @@ struct RowsKernel {
                     y[e] = o[c + from] * inv;
                 }
                 if (pl.splits > 1) {
+                    if (!live) continue;
                     float4* d = reinterpret_cast<float4*>(part + 32 * k + c);
                     d[0] = make_float4(y[0], y[1], y[2], y[3]);
                     d[1] = make_float4(y[4], y[5], y[6], y[7]);
-                } else {
-                    uint4 z;
-                    if (p.f16) z = make_uint4(half2_bits(y[0], y[1]), half2_bits(y[2], y[3]), half2_bits(y[4], y[5]), half2_bits(y[6], y[7]));
-                    else z = make_uint4(bf162_bits(y[0], y[1]), bf162_bits(y[2], y[3]), bf162_bits(y[4], y[5]), bf162_bits(y[6], y[7]));
-                    *reinterpret_cast<uint4*>(out + 32 * k + c) = z;
+                } else {                                        // by way of the query's place in shared memory
+                    const uint32_t at = smem + S::kQ + i * S::kMat + swizzled(r, 4 * k + c / 8);
+                    if (p.f16) sts128(at, half2_bits(y[0], y[1]), half2_bits(y[2], y[3]), half2_bits(y[4], y[5]), half2_bits(y[6], y[7]));
+                    else sts128(at, bf162_bits(y[0], y[1]), bf162_bits(y[2], y[3]), bf162_bits(y[4], y[5]), bf162_bits(y[6], y[7]));
                 }
+            }
+        }
+        if (pl.splits == 1) {
+            __syncwarp();
+            const long long mine = (long long)row * p.out_stride_row + (long long)hq * p.out_stride_head;
+            constexpr int kRun = D / 8;
+            const int lane = threadIdx.x & 31;
+#pragma unroll 4
+            for (int k = 0; k < kRun; k++) {
+                const int from = k * (32 / kRun) + lane / kRun;
+                const long long at = __shfl_sync(0xFFFFFFFFu, mine, from);
+                const bool there = __shfl_sync(0xFFFFFFFFu, (int)live, from) != 0;
+                const uint4 z = lds128(smem + S::kQ + i * S::kMat + swizzled((r & ~31) + from, lane % kRun));
+                if (there) *reinterpret_cast<uint4*>(p.out + at + 8 * (lane % kRun)) = z;
             }
         }
         if (live && pl.splits > 1) {
