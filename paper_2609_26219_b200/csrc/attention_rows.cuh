@@ -509,8 +509,8 @@ struct RowsKernel {
         return below(b + 1 - c0) & (~below(a - c0) | below(s - c0)) & ~gone;
     }
     // ---- softmax: a thread per query vector
-    // The query into shared memory: cp.async, then (quantised pages) in place to fp16, scaled so that the largest magnitude lies in
-    // [2^13, 2^14).  A vector with a NaN or an infinity gives NaN.  Returns the factor of its logits.
+    // The query into shared memory: cp.async, then (bf16 over quantised pages) in place to fp16, scaled so that the largest magnitude
+    // lies in [2^13, 2^14).  A vector with a NaN or an infinity gives NaN.  Returns the factor of its logits.
     __device__ __forceinline__ float load_query(int i, int r, bool live, int row, int hq) {
         const long long mine = (long long)row * p.q_stride_row + (long long)hq * p.q_stride_head;
         const uint32_t mat = smem + S::kQ + i * S::kMat;
@@ -528,48 +528,67 @@ struct RowsKernel {
         cp_wait<0>();
         __syncwarp();
         if (kPool) return p.scale_log2;
-        float amax = 0.0f, bad = 0.0f;
+        // Magnitudes are ordered as their bit patterns.
+        uint32_t most = 0;
 #pragma unroll 4
         for (int c = 0; c < D / 8; c++) {
             const uint4 v = lds128(mat + swizzled(r, c));
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int k = 0; k < 4; k++) {
-                const float a = p.f16 ? low_half(w[k]) : bf16_bits_to_float(w[k] & 0xFFFFu), b = p.f16 ? high_half(w[k]) : __uint_as_float(w[k] & 0xFFFF0000u);
-                amax = fmaxf(amax, fmaxf(fabsf(a), fabsf(b)));
-                bad = fmaf(a, 0.0f, fmaf(b, 0.0f, bad));
-            }
+            most = __vmaxu2(__vmaxu2(most, v.x & 0x7FFF7FFFu), __vmaxu2(v.y & 0x7FFF7FFFu, __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu)));
         }
-        const int e = (int)(__float_as_uint(amax) >> 23) - 127;
-        const int shift = amax > 0.0f ? min(13 - e, 120) : 0;
+        most = max(most & 0xFFFFu, most >> 16);
+        const bool bad = most >= (p.f16 ? 0x7C00u : 0x7F80u);
+        // fp16 stays as it is
+        const int shift = p.f16 || most == 0 ? 0 : min(13 - ((int)(most >> 7) - 127), 120);
         const float up = exp2i(shift);
+        if (!p.f16 || KF == FMT_INT4 || __any_sync(0xFFFFFFFFu, bad))
 #pragma unroll 2
-        for (int c = 0; c < D / 8; c++) {
-            uint4 v = lds128(mat + swizzled(r, c));
-            if (bad != 0.0f) v = make_uint4(0, 0, 0, 0);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-            float f[8];
+            for (int c = 0; c < D / 8; c++) {
+                uint4 v = lds128(mat + swizzled(r, c));
+                if (bad) v = make_uint4(0, 0, 0, 0);
+                uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                if (!p.f16)
 #pragma unroll
-            for (int k = 0; k < 4; k++) {
-                f[2 * k] = (p.f16 ? low_half(w[k]) : bf16_bits_to_float(w[k] & 0xFFFFu)) * up;
-                f[2 * k + 1] = (p.f16 ? high_half(w[k]) : __uint_as_float(w[k] & 0xFFFF0000u)) * up;
+                    for (int k = 0; k < 4; k++) w[k] = half2_bits(__uint_as_float(w[k] << 16) * up, __uint_as_float(w[k] & 0xFFFF0000u) * up);
+                if (KF == FMT_INT4)                             // the order operands4 leaves the channels in: 0 4, 1 5, 2 6, 3 7
+                    sts128(mat + swizzled(r, c), __byte_perm(w[0], w[2], 0x5410), __byte_perm(w[0], w[2], 0x7632), __byte_perm(w[1], w[3], 0x5410), __byte_perm(w[1], w[3], 0x7632));
+                else
+                    sts128(mat + swizzled(r, c), w[0], w[1], w[2], w[3]);
             }
-            if (KF == FMT_INT4)                                 // the order operands4 leaves the channels in
-                sts128(mat + swizzled(r, c), half2_bits(f[0], f[4]), half2_bits(f[1], f[5]), half2_bits(f[2], f[6]), half2_bits(f[3], f[7]));
-            else
-                sts128(mat + swizzled(r, c), half2_bits(f[0], f[1]), half2_bits(f[2], f[3]), half2_bits(f[4], f[5]), half2_bits(f[6], f[7]));
-        }
-        return p.scale_log2 * exp2i(-shift) + bad;
+        return bad ? __uint_as_float(0x7FC00000u) : p.scale_log2 * exp2i(-shift);
     }
 
-    // 32 logits -> 16 words of weights against the reference; their sum onto `total`.
+    // 2^y for two y <= 2^7 on the fma pipe: y = n + f with n whole and |f| <= 1/2, 2^f by a polynomial (fitted for the least relative
+    // error on that interval: 2.6e-6), times 2^n put together as bits.  Below -126 the result is about 2^-126; NaN stays NaN.
+    __device__ __forceinline__ static void exp2_pair(f32x2 y2, float& a, float& b) {
+        float u, v;
+        unpack2(y2, u, v);
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(u) : "f"(-126.0f));
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(-126.0f));
+        const f32x2 y = pack2(u, v), magic = pack2(12582912.0f, 12582912.0f);       // 1.5 * 2^23
+        const f32x2 t = add2(y, magic), f = sub2(y, sub2(t, magic));
+        f32x2 e = fma2(f, pack2(0.009570097550749779f, 0.009570097550749779f), pack2(0.05591786280274391f, 0.05591786280274391f));
+        e = fma2(e, f, pack2(0.240247443318367f, 0.240247443318367f));
+        e = fma2(e, f, pack2(0.6931217908859253f, 0.6931217908859253f));
+        e = fma2(e, f, pack2(0.9999992847442627f, 0.9999992847442627f));
+        float n0, n1;
+        unpack2(t, n0, n1);
+        unpack2(mul2(e, pack2(__uint_as_float((__float_as_uint(n0) << 23) + 0x3F800000u), __uint_as_float((__float_as_uint(n1) << 23) + 0x3F800000u))), a, b);
+    }
+
+    // 32 logits -> 16 words of weights against the reference; their sum onto `total`.  The exponential unit does 16 a cycle and SM, a
+    // step's 32768 would keep it as busy as the products keep the tensor cores: kOnFma of 16 pairs are computed instead.
+    static constexpr int kOnFma = 4;
     __device__ __forceinline__ static void weigh(const float (&x)[32], uint32_t* w, f32x2 factor2, f32x2 ref2, f32x2& total) {
 #pragma unroll
         for (int c = 0; c < 16; c++) {
             float e, f;
             unpack2(fma2(pack2(x[2 * c], x[2 * c + 1]), factor2, ref2), e, f);
-            e = fast_exp2(e);
-            f = fast_exp2(f);
+            if (c % 4 < kOnFma / 4) {
+                exp2_pair(pack2(e, f), e, f);
+            } else {
+                e = fast_exp2(e);
+                f = fast_exp2(f);
+            }
             total = add2(total, pack2(e, f));
             w[c] = kPool ? bf162_bits(e, f) : half2_bits(e, f);
         }
@@ -699,7 +718,9 @@ struct RowsKernel {
         float sum, sum_odd;
         unpack2(sum2, sum, sum_odd);
         sum += sum_odd;
-        if (broken && sum > 1.0e-30f) sum = __uint_as_float(0x7FC00000u);
+        // (A row that sees a token has a weight of 2^-4 at least; what it does not see weighs up to 2^-126 in the computed pairs.)
+        if (sum < 1.0e-30f) sum = 0.0f;
+        if (broken && sum != 0.0f) sum = __uint_as_float(0x7FC00000u);
         const bool lost = IMAGE ? lost_seen != 0 : *reinterpret_cast<volatile int32_t*>(&bars.lost) != 0;
         const float inv = pl.splits > 1 ? 1.0f : (sum != 0.0f ? 1.0f / sum : 0.0f);
         const long long vec = (long long)row * p.Hq + hq;
