@@ -97,6 +97,7 @@ class AttentionArgs(C.Structure):
                 ("out_stride_head", C.c_int64), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
 
 
+_SIZEOF_ROWS, _SIZEOF_ATTENTION = C.sizeof(Rows), C.sizeof(AttentionArgs)
 _lib = None
 
 
@@ -215,19 +216,31 @@ def make_batch(*, row_start: torch.Tensor, kv_len: torch.Tensor, block_table: to
                  _ptr(pos), _ptr(block_table))
 
 
+_ROW_TYPES = {torch.bfloat16: ROWS_BF16, torch.float16: ROWS_F16}
+
+
 def _row_type(t: torch.Tensor, name: str) -> int:
-    if t.dtype not in (torch.bfloat16, torch.float16) or t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+    kind = _ROW_TYPES.get(t.dtype)
+    if kind is None or t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
         raise ValueError(f"{name}: a bfloat16 or float16 tensor [rows][heads][channels] with unit channel stride")
-    return ROWS_F16 if t.dtype == torch.float16 else ROWS_BF16
+    return kind
 
 
 def _make_rows(geom: Geom, batch: Batch, k: torch.Tensor, v: torch.Tensor) -> Rows:
     kind = _row_type(k, "k")
-    if _row_type(v, "v") != kind or v.shape != k.shape or v.stride() != k.stride():
+    shape, strides = k.shape, k.stride()
+    if v.dtype is not k.dtype or v.shape != shape or v.stride() != strides:
         raise ValueError("k and v must agree in type, shape and strides")
-    if k.shape[0] < batch.n_rows or tuple(k.shape[1:]) != (geom.n_kv_heads, geom.head_dim):
+    if shape[0] < batch.n_rows or shape[1] != geom.n_kv_heads or shape[2] != geom.head_dim:
         raise ValueError("k and v: [n_rows][n_kv_heads][head_dim]")
-    return Rows(C.sizeof(Rows), kind, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1))
+    return Rows(_SIZEOF_ROWS, kind, k.data_ptr(), v.data_ptr(), strides[0], strides[1])
+
+
+def _stream_of(stream, device: int) -> Optional[int]:
+    """The raw handle of `stream`, or of the stream that is current on the context's device (which need not be the current one)."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device)
+    return _stream_handle(stream)
 
 
 def attention_workspace_bytes(geom: Geom, cache, batch: Batch, n_q_heads: int, window: int = 0, sinks: int = 0) -> int:
@@ -318,15 +331,15 @@ class Context:
                      stream=None, check: bool = True) -> int:
         """Quantises the rows k, v [n_rows][H][D] (bf16 or fp16) into their positions in the cache."""
         rows = _make_rows(geom, batch, k, v)
-        return self._check(lib().patchkv_cache_append(self._h, C.byref(geom), C.byref(cache), layer, C.byref(batch),
-                                                      C.byref(rows), _stream_handle(stream)), check)
+        rc = lib().patchkv_cache_append(self._h, geom, cache, layer, batch, rows, _stream_of(stream, self.device))
+        return rc if rc == OK else self._check(rc, check)
 
     def cache_read(self, geom: Geom, cache: QPool, layer: int, batch: Batch, k: torch.Tensor, v: torch.Tensor,
                    stream=None, check: bool = True) -> int:
         """Reads the batch's positions back into k, v [n_rows][H][D] (bf16 or fp16)."""
         rows = _make_rows(geom, batch, k, v)
-        return self._check(lib().patchkv_cache_read(self._h, C.byref(geom), C.byref(cache), layer, C.byref(batch),
-                                                    C.byref(rows), _stream_handle(stream)), check)
+        rc = lib().patchkv_cache_read(self._h, geom, cache, layer, batch, rows, _stream_of(stream, self.device))
+        return rc if rc == OK else self._check(rc, check)
 
     def attention(self, geom: Geom, cache, layer: int, batch: Batch, q: torch.Tensor, out: torch.Tensor,
                   scale: Optional[float] = None, window: int = 0, sinks: int = 0,
@@ -335,18 +348,17 @@ class Context:
         head_dim ** -0.5.  workspace: a uint8 device tensor of attention_workspace_bytes(...) bytes that nothing else uses
         while the call's work runs; needed when that is not 0."""
         kind = _row_type(q, "q")
-        if _row_type(out, "out") != kind or out.shape != q.shape:
-            raise ValueError("out must have the shape and type of q")
-        if q.shape[0] < batch.n_rows or q.shape[2] != geom.head_dim:
+        shape, qs, os_ = q.shape, q.stride(), out.stride()
+        if out.dtype is not q.dtype or out.shape != shape or (os_[2] != 1 and shape[2] > 1):
+            raise ValueError("out must have the shape and type of q, and unit channel stride")
+        if shape[0] < batch.n_rows or shape[2] != geom.head_dim:
             raise ValueError("q: [n_rows][n_q_heads][head_dim]")
-        a = AttentionArgs(C.sizeof(AttentionArgs), kind, q.shape[1], window, sinks,
-                          geom.head_dim ** -0.5 if scale is None else scale, q.data_ptr(), out.data_ptr(), q.stride(0),
-                          q.stride(1), out.stride(0), out.stride(1), _ptr(workspace),
-                          0 if workspace is None else workspace.numel() * workspace.element_size())
-        quantised = isinstance(cache, QPool)
-        return self._check(lib().patchkv_attention(self._h, C.byref(geom), None if quantised else C.byref(cache),
-                                                   C.byref(cache) if quantised else None, layer, C.byref(batch),
-                                                   C.byref(a), _stream_handle(stream)), check)
+        ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+        a = AttentionArgs(_SIZEOF_ATTENTION, kind, shape[1], window, sinks, geom.head_dim ** -0.5 if scale is None else scale,
+                          q.data_ptr(), out.data_ptr(), qs[0], qs[1], os_[0], os_[1], ws, ws_bytes)
+        pool, pages = (None, cache) if isinstance(cache, QPool) else (cache, None)
+        rc = lib().patchkv_attention(self._h, geom, pool, pages, layer, batch, a, _stream_of(stream, self.device))
+        return rc if rc == OK else self._check(rc, check)
 
     def selftest_bounded_wait(self, max_polls: int, stream=None, check: bool = True) -> int:
         """Runs the kernels' bounded barrier wait on a barrier that nothing completes; query_status() then reports E_TIMEOUT."""

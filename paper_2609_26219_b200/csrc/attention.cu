@@ -2,6 +2,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "attention.cuh"
 #include "attention_rows.cuh"
@@ -212,13 +213,26 @@ AttentionPlan plan_attention(const patchkv_geom* g, int tag, const patchkv_batch
     return a;
 }
 
+// Opts a kernel into `bytes` of dynamic shared memory, once per device (a bit each; the attribute is per device and sticks).
+cudaError_t allow_smem(const void* kernel, int bytes, std::atomic<uint64_t>* done) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (bit && (done->load(std::memory_order_acquire) & bit)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) done->fetch_or(bit, std::memory_order_release);
+    return e;
+}
+
 template <int KF, int VF, int D, int NC, bool G32>
 cudaError_t launch_split(const AttentionParams& p, const SplitPlan& pl, int groups, cudaStream_t stream) {
     using S = SplitShape<KF, VF, D, NC>;
     using K = SplitKernel<KF, VF, D, NC, S::kStages, S::kWarps, G32>;
     constexpr int smem = K::kSmem > K::kMerge ? K::kSmem : K::kMerge;
     auto kernel = attention_split_kernel<KF, VF, D, NC, S::kStages, S::kWarps, G32>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    static std::atomic<uint64_t> allowed{0};
+    cudaError_t e = allow_smem((const void*)kernel, smem, &allowed);
     if (e != cudaSuccess) return e;
     e = launch_pdl(kernel, dim3(pl.max_items, groups), dim3(S::kWarps * 32), smem, stream, p, pl);
     if (e != cudaSuccess || pl.target == 0) return e;
@@ -245,7 +259,8 @@ cudaError_t launch_split_columns(const AttentionParams& p, const SplitPlan& pl, 
 template <int KF, int VF, int D, bool IMAGE>
 cudaError_t launch_rows_kernel(const AttentionParams& p, const RowsPlan& pl, cudaStream_t stream) {
     auto kernel = attention_rows_kernel<KF, VF, D, IMAGE>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, RowsSmem<D>::kLaunch);
+    static std::atomic<uint64_t> allowed{0};
+    const cudaError_t e = allow_smem((const void*)kernel, RowsSmem<D>::kLaunch, &allowed);
     if (e != cudaSuccess) return e;
     return launch_pdl(kernel, dim3(pl.tiles * p.c.H * p.b.n_seqs * pl.splits), dim3(rows_threads(IMAGE)), RowsSmem<D>::kLaunch, stream, p, pl);
 }
