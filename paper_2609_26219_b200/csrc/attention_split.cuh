@@ -168,7 +168,8 @@ struct SplitKernel {
     static constexpr int kStage = kScales + (kPool ? 0 : 2 * kTile * 8);                    // 8 bytes of scales per token, K then V
     static constexpr int kChunks = D / 32, kMT = D / 16;
     static constexpr int kRegs = (NC == 1 ? 2 : 4 * NT) * kMT;                              // accumulators of a lane that hold a column
-    static constexpr int kSmem = WARPS * STAGES * kStage;
+    static constexpr int kCold = 4 * (4 + 4 * NC);                                          // a warp's numbers that only masks need
+    static constexpr int kSmem = WARPS * (STAGES * kStage + kCold);
     static constexpr int kMerge = WARPS * (kRegs * 32 + 2 * 4 * NC) * 4;                    // the warps' results, in the same memory
 
     const AttentionParams& p;
@@ -177,26 +178,27 @@ struct SplitKernel {
     uint32_t qf[NT][kMT][2];
     float bias[kPool ? 1 : NT][kPool ? 1 : kChunks][2];
     float factor[NC], ref[NC], sum[NC];
-    int pos[NC];
     float acc[NT][kMT][4];
-    int v_exp;                                  // V scales are multiplied by 2^v_exp, as the product of two halves
-    uint32_t v_up0, v_up1;
-    int kv, lo_pos, hi_pos;
-    uint32_t k_off, v_off, k_step, v_step, s_off;    // the lane's places in a tile's rows, relative to its first
+    uint32_t v_up0, v_up1, v_most;              // V scales are multiplied by a power of two: two halves, and the bits of the first scale too large for it
+    uint32_t cold;                              // shared memory: kv, smallest and largest position, and the positions of the columns
+    uint32_t k_off, v_off, s_off;               // the lane's places in a tile's rows, relative to its first
     uint32_t flip0, flip1;                      // 8 in every half's low nibble, 8 in the next one (constants the compiler must keep in registers)
 
     __device__ __forceinline__ SplitKernel(const AttentionParams& p_) : p(p_) {}
 
-    __device__ __forceinline__ bool visible(int ps, int tok) const {
-        return tok <= ps && tok < kv && sees(p, ps, tok);
-    }
+    // 128 registers a thread are what sixteen warps leave: what only tiles with a mask need lives in shared memory.
+    __device__ __forceinline__ int kv() const { return (int)lds32(cold); }
+    __device__ __forceinline__ int lo_pos() const { return (int)lds32(cold + 4); }
+    __device__ __forceinline__ int hi_pos() const { return (int)lds32(cold + 8); }
+    __device__ __forceinline__ int pos(int c) const { return (int)lds32(cold + 16 + 4 * column_of(c, t)); }
+    __device__ __forceinline__ int v_exp() const { return 30 - (int)(v_most >> 10); }
     __device__ __forceinline__ int scales_per_row() const { return G32 ? kChunks : D / p.c.G; }
 
-    __device__ __forceinline__ void start(int lane_, uint32_t ring_) {
-        lane = lane_; g = lane >> 2; t = lane & 3; ring = ring_;
+    __device__ __forceinline__ void start(int lane_, uint32_t ring_, uint32_t cold_) {
+        lane = lane_; g = lane >> 2; t = lane & 3; ring = ring_; cold = cold_;
         constexpr int kc = kKRow / 16, vc = kVRow / 16;       // 16-byte chunks of a row, a power of two
-        k_off = (lane / kc) * p.c.H * kKRow + (lane % kc) * 16; k_step = (32 / kc) * p.c.H * kKRow;
-        v_off = (lane / vc) * p.c.H * kVRow + (lane % vc) * 16; v_step = (32 / vc) * p.c.H * kVRow;
+        k_off = (lane / kc) * p.c.H * kKRow + (lane % kc) * 16;
+        v_off = (lane / vc) * p.c.H * kVRow + (lane % vc) * 16;
         if (!kPool) {
             s_off = (lane & 15) * p.c.H * scales_per_row() * 2 + (lane < 16 ? p.c.k_scales : p.c.v_scales);
             v_off += p.c.v_codes;
@@ -214,9 +216,9 @@ struct SplitKernel {
                 for (int j = 0; j < 4; j++) acc[nt][i][j] = 0.0f;
     }
     __device__ __forceinline__ void set_v_exp(int e) {       // -1 <= e <= 29: exact, a scale only grows
-        v_exp = e;
         v_up0 = both(exp2i(min(e, 15)));
         v_up1 = both(exp2i(max(e - 15, 0)));
+        v_most = (uint32_t)(30 - e) << 10;                   // exponent field x: s < 2^(x - 14), so s * 2^e stays at 2^15 at most
     }
 
     // Queries as B operands, and the per-column numbers of the lane's logit columns.
@@ -310,46 +312,43 @@ struct SplitKernel {
         }
     }
 
-    // Whole tiles need no mask: seen by the earliest row and inside the latest row's window, or among the sinks.
-    __device__ __forceinline__ bool whole_tile(int t0) const {
-        return t0 + kTile - 1 <= min(lo_pos, kv - 1) && (p.window == 0 || hi_pos - t0 < p.window || t0 + kTile <= p.sinks);
-    }
-
-    // Enqueues tile `tile` of the head into stage `st`; page < 0: zeros.  A token that no row sees is filled with zeros (of
-    // quantised pages: its scales): nothing of its slot takes part.
-    __device__ __forceinline__ void fetch(int st, int tile, int page, int head) {
-        const uint32_t base = ring + st * kStage;
-        const int t0 = tile * kTile, slot0 = t0 - div_page(p.c, t0) * p.c.P;
-        const int end = min(hi_pos, kv - 1);
-        const bool all = page >= 0 && whole_tile(t0);
+    // Enqueues a tile into the stage at `base`: `at` is the place of its page (of a pool: of its first token), in bytes; row0 its first
+    // (token, head) row there, H apart per token.  A token that no row sees is filled with zeros (of quantised pages: its
+    // scales), and so is a tile without a page: nothing of its slot takes part.
+    __device__ __forceinline__ void fetch(uint32_t base, long long at, uint32_t row0, bool whole, bool present, int t0) {
         if constexpr (kPool) {
-            const long long o = page < 0 ? 0 : (long long)page * p.c.stride_page + (long long)slot0 * p.c.stride_token + (long long)head * p.c.stride_head;
             constexpr int kc = kKRow / 16;
+            const uint8_t* k = reinterpret_cast<const uint8_t*>(p.c.k) + at + (lane % kc) * 16;
+            const uint8_t* v = reinterpret_cast<const uint8_t*>(p.c.v) + at + (lane % kc) * 16;
+            const uint32_t dst = base + (lane / kc) * kKStride + (lane % kc) * 16;
 #pragma unroll
             for (int i = 0; i < kTile * kc / 32; i++) {
-                const int tok = lane / kc + i * (32 / kc), c = lane % kc;
-                const bool live = all || (page >= 0 && t0 + tok <= end && sees(p, lo_pos, t0 + tok));
-                const long long a = o + (live ? tok * p.c.stride_token + 8 * c : 0);
-                cp16(base + tok * kKStride + 16 * c, p.c.k + a, live);
-                cp16(base + kV + tok * kVStride + 16 * c, p.c.v + a, live);
+                const int tok = lane / kc + i * (32 / kc);
+                const bool live = whole || (present && t0 + tok <= min(hi_pos(), kv() - 1) && sees(p, lo_pos(), t0 + tok));
+                const long long o = live ? 2 * tok * p.c.stride_token : 0;
+                cp16(dst + i * (32 / kc) * kKStride, k + o, live);
+                cp16(dst + kV + i * (32 / kc) * kVStride, v + o, live);
             }
         } else {
-            const uint8_t* pg = p.c.base + (page < 0 ? 0ll : (long long)page * p.c.stride_page);
-            const uint32_t row0 = (uint32_t)slot0 * p.c.H + head;          // (token, head) rows of a page, H apart per token
+            const uint8_t* pg = p.c.base + at;
             constexpr int kc = kKRow / 16, vc = kVRow / 16;
             const uint8_t* ks = pg + (row0 * kKRow + k_off);
             const uint8_t* vs = pg + (row0 * kVRow + v_off);
+            const uint8_t* sc = pg + (row0 * (uint32_t)scales_per_row() * 2 + s_off);
             const uint32_t kd = base + (lane / kc) * kKStride + (lane % kc) * 16, vd = base + kV + (lane / vc) * kVStride + (lane % vc) * 16;
+            const uint32_t sd = base + kScales + lane * 8;
+            bool live = true, all = true;
+            if (!whole) {
+                const int tok = t0 + (lane & 15);
+                live = present && tok <= min(hi_pos(), kv() - 1) && sees(p, lo_pos(), tok);
+                all = present;
+            }
 #pragma unroll
-            for (int i = 0; i < kTile * kc / 32; i++) cp16(kd + i * (32 / kc) * kKStride, ks + i * k_step, page >= 0);
+            for (int i = 0; i < kTile * kc / 32; i++) cp16(kd + i * (32 / kc) * kKStride, ks + i * (32 / kc) * kKRow * p.c.H, all);
 #pragma unroll
-            for (int i = 0; i < kTile * vc / 32; i++) cp16(vd + i * (32 / vc) * kVStride, vs + i * v_step, page >= 0);
-            const int tok = t0 + (lane & 15);
-            const bool live = all || (page >= 0 && tok <= end && sees(p, lo_pos, tok));
-            const uint32_t e = row0 * (uint32_t)scales_per_row() * 2 + s_off;
-            const uint32_t dst = base + kScales + lane * 8;
-            if (D == 128 && G32) cp_small<8>(dst, pg + e, live);
-            else cp_small<4>(dst, pg + (e & ~3u), live);                   // a lone fp16: its word, picked apart below
+            for (int i = 0; i < kTile * vc / 32; i++) cp16(vd + i * (32 / vc) * kVStride, vs + i * (32 / vc) * kVRow * p.c.H, all);
+            if (D == 128 && G32) cp_small<8>(sd, sc, live);
+            else cp_small<4>(sd, reinterpret_cast<const uint8_t*>(reinterpret_cast<uintptr_t>(sc) & ~(uintptr_t)3), live);   // a lone fp16: its word, picked apart below
         }
     }
 
@@ -369,10 +368,7 @@ struct SplitKernel {
     }
 
     // One tile: logits, weights, and the weighted values.
-    __device__ __forceinline__ void tile(int st, int tl, bool present, int head) {
-        const uint32_t base = ring + st * kStage;
-        const int t0 = tl * kTile;
-        const int slot0 = t0 - div_page(p.c, t0) * p.c.P;
+    __device__ __forceinline__ void tile(uint32_t base, bool whole, bool present, int t0, uint32_t row0) {
         float x[NC][2];                                                    // tokens g and g + 8
         if constexpr (kPool) {
             float y[NT][4];
@@ -393,8 +389,8 @@ struct SplitKernel {
         } else {
             uint32_t odd_a = 0, odd_b = 0;
             if (!G32 && p.c.G == D) {                                      // which half of the word a lone scale is
-                odd_a = ((slot0 + g) * p.c.H + head) & 1;
-                odd_b = ((slot0 + g + 8) * p.c.H + head) & 1;
+                odd_a = (row0 + g * p.c.H) & 1;
+                odd_b = (row0 + (g + 8) * p.c.H) & 1;
             }
             const uint2 sa = lds64(base + kScales + 8 * g), sb = lds64(base + kScales + 8 * (g + 8));
             const uint32_t ra = base + g * kKStride + 4 * t, rb = ra + 8 * kKStride;
@@ -436,24 +432,61 @@ struct SplitKernel {
                 }
             }
         }
-        const bool whole = present && whole_tile(t0);
+#pragma unroll
+        for (int c = 0; c < NC; c++) { x[c][0] *= factor[c]; x[c][1] *= factor[c]; }
+        if (!whole)
+#pragma unroll
+            for (int c = 0; c < NC; c++)
+#pragma unroll
+                for (int i = 0; i < 2; i++) {
+                    const int tok = t0 + g + 8 * i, ps = pos(c);
+                    if (!(present && tok <= ps && tok < kv() && sees(p, ps, tok))) x[c][i] = -INFINITY;
+                }
         float most = kNoMax;
 #pragma unroll
-        for (int c = 0; c < NC; c++)
+        for (int c = 0; c < NC; c++) most = fmaxf(most, fmaxf(x[c][0], x[c][1]) - ref[c]);
+        // V scales of the lane's channels (one group: channels [g * D / 8, (g + 1) * D / 8)) for tokens 2t, 2t+1, 2t+8, 2t+9
+        uint32_t sp[2] = {0, 0}, top = 0;
+        if constexpr (!kPool) {
+            uint32_t s[4];
+            const int group = g * (D / 8) / (G32 ? 32 : p.c.G);
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                x[c][i] *= factor[c];
-                if (!whole && !(present && visible(pos[c], t0 + g + 8 * i))) x[c][i] = -INFINITY;
-                most = fmaxf(most, x[c][i] - ref[c]);
+            for (int i = 0; i < 4; i++) {
+                const int tok = 2 * t + (i & 1) + 8 * (i >> 1);
+                uint32_t at = base + kScales + 128 + 8 * tok + 2 * group;
+                if (!G32 && p.c.G == D) at += 2 * ((row0 + tok * p.c.H) & 1);
+                s[i] = lds16(at);
             }
-        if (__any_sync(0xFFFFFFFFu, most > 8.0f)) {
+            sp[0] = s[0] | s[1] << 16;
+            sp[1] = s[2] | s[3] << 16;
+            const uint32_t mag = __vmaxu2(sp[0] & 0x7FFF7FFFu, sp[1] & 0x7FFF7FFFu);
+            top = max(mag & 0xFFFFu, mag >> 16);
+        }
+        // One vote for the two references that may have to move.
+        if (__any_sync(0xFFFFFFFFu, most > 8.0f || (!kPool && top >= v_most))) {
 #pragma unroll
             for (int c = 0; c < NC; c++) {
                 float m = fmaxf(x[c][0], x[c][1]);
                 m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 4));
                 m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
                 m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
-                if (m > ref[c]) rescale(c, m);
+                if (m > ref[c] + 8.0f) rescale(c, m);
+            }
+            if constexpr (!kPool) {
+                uint32_t m = top >= 0x7C00u ? 0u : top;             // a scale that is not finite always gets here
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+                const int from = v_exp(), to = min(from, 29 - (int)(m >> 10));
+                if (to < from) {
+                    const float keep = exp2i(to - from);
+                    set_v_exp(to);
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                        for (int i = 0; i < kMT; i++)
+#pragma unroll
+                            for (int k = 0; k < 4; k++) acc[nt][i][k] *= keep;
+                }
             }
         }
         uint32_t pf[NT][2];
@@ -492,36 +525,7 @@ struct SplitKernel {
                 for (int nt = 0; nt < NT; nt++) mma_bf16(acc[nt][i], r[0], r[1], r[2], r[3], pf[nt][0], pf[nt][1]);
             }
         } else {
-            // scales of the lane's channels (one group: channels [g * D / 8, (g + 1) * D / 8)) for tokens 2t, 2t+1, 2t+8, 2t+9
-            const int group = g * (D / 8) / (G32 ? 32 : p.c.G);
-            uint32_t s[4];
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const int tok = 2 * t + (i & 1) + 8 * (i >> 1);
-                uint32_t at = base + kScales + 128 + 8 * tok + 2 * group;
-                if (!G32 && p.c.G == D) at += 2 * (((slot0 + tok) * p.c.H + head) & 1);
-                s[i] = lds16(at);
-            }
-            uint32_t sp[2] = {s[0] | s[1] << 16, s[2] | s[3] << 16};
-            const uint32_t mag = __vmaxu2(sp[0] & 0x7FFF7FFFu, sp[1] & 0x7FFF7FFFu), top = max(mag & 0xFFFFu, mag >> 16);
-            // exponent field e: s < 2^(e - 14); the power of two keeps s * 2^v_exp at 2^15 at most
-            if (__any_sync(0xFFFFFFFFu, (int)(top >> 10) + v_exp > 29)) {   // a scale that is not finite always gets here
-                uint32_t m = top >= 0x7C00u ? 0u : top;
-#pragma unroll
-                for (int d = 1; d < 32; d <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-                const int to = min(v_exp, 29 - (int)(m >> 10));
-                if (to < v_exp) {
-                    const float keep = exp2i(to - v_exp);
-                    set_v_exp(to);
-#pragma unroll
-                    for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                        for (int i = 0; i < kMT; i++)
-#pragma unroll
-                            for (int k = 0; k < 4; k++) acc[nt][i][k] *= keep;
-                }
-                if (!whole && __any_sync(0xFFFFFFFFu, top >= 0x7C00u)) { values_one_by_one(base, x, (uint32_t)(slot0 * p.c.H + head)); return; }
-            }
+            if (!whole && __any_sync(0xFFFFFFFFu, top >= 0x7C00u)) { values_one_by_one(base, x, row0); return; }
             uint32_t S[2], S16[2], off[2];
 #pragma unroll
             for (int k = 0; k < 2; k++) {
@@ -603,7 +607,7 @@ struct SplitKernel {
                         const uint32_t byte = base + kV + tok * kVStride + (VF == FMT_INT8 ? ch : ch >> 1);
                         uint32_t u = lds32(byte & ~3u) >> ((byte & 3u) * 8);
                         if (VF == FMT_INT4) u = ((u >> ((ch & 1) * 4)) & 15u) ^ 8u; else u = (u & 255u) ^ 128u;
-                        v = ((float)u - (VF == FMT_INT4 ? 8.0f : 128.0f)) * half_bits_to_float(lds16(at)) * 5.9604644775390625e-08f * exp2i(v_exp);
+                        v = ((float)u - (VF == FMT_INT4 ? 8.0f : 128.0f)) * half_bits_to_float(lds16(at)) * 5.9604644775390625e-08f * exp2i(v_exp());
                     }
 #pragma unroll
                     for (int c = 0; c < NC; c++)
@@ -705,50 +709,63 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
     const bool live = head < p.c.H;
     const int cols = min(it.rows * p.share, 4 * NC);
     K k(p);
-    k.start(lane, smem_u32(smem) + warp * STAGES * K::kStage);
-    k.kv = it.kv; k.lo_pos = it.lo; k.hi_pos = it.hi;
+    k.start(lane, smem_u32(smem) + warp * STAGES * K::kStage, smem_u32(smem) + WARPS * STAGES * K::kStage + warp * K::kCold);
     const TileRange range = tile_range(p, it.kv, it.lo, it.hi);
     if (live) {
         const int step = pl.warps_per_head, n = it.begin + sub < it.end ? (it.end - it.begin - sub + step - 1) / step : 0;
-        // pages of the warp's next 64 tiles: a lane each of the current 32 and the 32 behind them
-        auto page_of = [&](int i) {
-            if (i >= n) return -1;
-            const int lp = div_page(p.c, range.tile(it.begin + sub + i * step) * kTile);
-            int pg = __ldg(p.b.block_table + (long long)it.seq * p.b.table_stride + lp);
-            if (pg < 0 || pg >= p.c.n_pages) { latch(p.status); pg = -1; }
-            return pg;
+        uint32_t* cold = reinterpret_cast<uint32_t*>(smem + WARPS * STAGES * K::kStage + warp * K::kCold);
+        if (lane == 0) { cold[0] = it.kv; cold[1] = it.lo; cold[2] = it.hi; }
+        if (lane < 4 * NC) cold[4 + lane] = lane < cols ? row_position(p.b, it.seq, it.first + lane / p.share) : -1;
+        __syncwarp();
+        // The warp's next 32 tiles, a lane each: place, first row and flags.  Whole tiles need no mask: seen by the earliest row and
+        // inside the latest row's window, or among the sinks.
+        struct Place { long long at; uint32_t row0, flags; };        // flags: bit 0 whole, bit 1 has a page
+        auto place_of = [&](int i) {
+            Place o = {0, 0, 0};
+            if (i < n) {
+                const int t0 = range.tile(it.begin + sub + i * step) * kTile, lp = div_page(p.c, t0), slot0 = t0 - lp * p.c.P;
+                const int pg = __ldg(p.b.block_table + (long long)it.seq * p.b.table_stride + lp);
+                o.row0 = (uint32_t)slot0 * p.c.H + head;
+                if (pg < 0 || pg >= p.c.n_pages) {
+                    latch(p.status);
+                } else {
+                    o.at = K::kPool ? 2 * ((long long)pg * p.c.stride_page + (long long)slot0 * p.c.stride_token + (long long)head * p.c.stride_head)
+                                    : (long long)pg * p.c.stride_page;
+                    const int lo = k.lo_pos(), hi = k.hi_pos();
+                    o.flags = t0 + kTile - 1 <= min(lo, k.kv() - 1) && (p.window == 0 || hi - t0 < p.window || t0 + kTile <= p.sinks) ? 3 : 2;
+                }
+            }
+            return o;
         };
-        int pages = page_of(lane), pages_next = page_of(lane + 32);
+        Place here = place_of(lane);
         // One copy of the tile's code, stage and all else in registers: the instruction cache is cold at every launch, and a
         // short context runs each instruction a few times only.
-        uint32_t present = 0;                                // bit k: the tile fetched k ago has a valid page
-        int fetch_stage = 0;
+        uint32_t whole = 0, present = 0, odd = 0;            // bit j: flags (and row0 & 1) of the tile fetched j ago
+        uint32_t fetch_base = k.ring, base = k.ring;
         auto fetch = [&](int i) {
-            // i runs through 0, 1, 2 ...; the pages in registers are those of the 32-block of i
-            const int pg = __shfl_sync(0xFFFFFFFFu, pages, i & 31);
-            if (i < n) k.fetch(fetch_stage, range.tile(it.begin + sub + i * step), pg, head);
+            // i runs through 0, 1, 2 ...; `here` is the 32-block of i
+            const uint32_t flags = __shfl_sync(0xFFFFFFFFu, here.flags, i & 31), row0 = __shfl_sync(0xFFFFFFFFu, here.row0, i & 31);
+            const long long at = __shfl_sync(0xFFFFFFFFu, here.at, i & 31);
+            if (i < n) k.fetch(fetch_base, at, row0, flags & 1, flags >> 1, flags & 1 ? 0 : range.tile(it.begin + sub + i * step) * kTile);
             cp_commit();
-            if ((i & 31) == 31) { pages = pages_next; pages_next = page_of(i + 33 + lane); }
-            present = present << 1 | (pg >= 0 ? 1u : 0u);
-            fetch_stage = fetch_stage == STAGES - 1 ? 0 : fetch_stage + 1;
+            if ((i & 31) == 31) here = place_of(i + 1 + lane);
+            whole = whole << 1 | (flags & 1);
+            present = present << 1 | flags >> 1;
+            if (!G32) odd = odd << 1 | (row0 & 1);
+            fetch_base = fetch_base == k.ring + (STAGES - 1) * K::kStage ? k.ring : fetch_base + K::kStage;
         };
 #pragma unroll 1
         for (int i = 0; i < STAGES - 1; i++) fetch(i);
-#pragma unroll
-        for (int c = 0; c < NC; c++) {
-            const int col = column_of(c, k.t);
-            k.pos[c] = col < cols ? row_position(p.b, it.seq, it.first + col / p.share) : -1;
-        }
         k.load_queries(it.first, cols, head);
-        int stage = 0;
 #pragma unroll 1
         for (int i = 0; i < n; i++) {
             fetch(i + STAGES - 1);
             cp_wait<STAGES - 1>();
             __syncwarp();
-            k.tile(stage, range.tile(it.begin + sub + i * step), present >> (STAGES - 1) & 1u, head);
+            const bool w = whole >> (STAGES - 1) & 1;
+            k.tile(base, w, present >> (STAGES - 1) & 1, w ? 0 : range.tile(it.begin + sub + i * step) * kTile, odd >> (STAGES - 1) & 1);
             __syncwarp();                                    // the stage may be filled again
-            stage = stage == STAGES - 1 ? 0 : stage + 1;
+            base = base == k.ring + (STAGES - 1) * K::kStage ? k.ring : base + K::kStage;
         }
         cp_wait<0>();
     }
@@ -762,7 +779,7 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
     float* res = reinterpret_cast<float*>(smem);
     float* ml = res + WARPS * K::kRegs * 32;
     if (live) {
-        const float down = K::kPool ? 1.0f : 16777216.0f * exp2i(-k.v_exp);
+        const float down = K::kPool ? 1.0f : 16777216.0f * exp2i(-k.v_exp());
         int r = 0;
 #pragma unroll
         for (int nt = 0; nt < K::NT; nt++)
