@@ -354,7 +354,8 @@ extern "C" int patchkv_attention(patchkv_ctx* ctx, const patchkv_geom* g, const 
         pl.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(a->workspace) + plan.items_bytes);
         pl.item_stride = (int32_t)plan.item_stride;
         pl.max_items = plan.max_items; pl.target = plan.target;
-        pl.heads = plan.heads; pl.warps_per_head = plan.warps_per_head;
+        pl.heads_log2 = log2_exact(plan.heads); pl.per_head_log2 = log2_exact(plan.warps_per_head);
+        pl.share_magic = (65536u + p.share - 1) / p.share;
         PKV_CUDA(ctx, p.c.D == 128 ? launch_split_columns<128>(p, pl, plan.nc, plan.groups, stream)
                                    : launch_split_columns<64>(p, pl, plan.nc, plan.groups, stream));
         return PATCHKV_OK;

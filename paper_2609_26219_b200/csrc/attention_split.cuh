@@ -33,7 +33,8 @@ struct SplitPlan {
     int32_t item_stride;                        // floats per (item, head)
     int32_t max_items;                          // grid bound
     int32_t target;                             // pieces the whole batch is cut into (0: one piece per sequence, no combine)
-    int32_t heads, warps_per_head;              // heads of a CTA (a power of two), warps that share a head's tiles
+    int32_t heads_log2, per_head_log2;          // heads of a CTA, warps that share a head's tiles: powers of two
+    uint32_t share_magic;                       // row of a column n < 16: n * share_magic >> 16
 };
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool live) {
@@ -222,84 +223,75 @@ struct SplitKernel {
     }
 
     // Queries as B operands, and the per-column numbers of the lane's logit columns.
-    __device__ __forceinline__ void load_queries(int first, int cols, int head) {
-        if constexpr (kPool) {
+    __device__ __forceinline__ void load_queries(int first, int cols, int head, uint32_t share_magic) {
 #pragma unroll
-            for (int nt = 0; nt < NT; nt++) {
-                const int n = column_of(2 * nt + (g & 1), g >> 1), row = n / p.share;
-                const uint16_t* q = p.q + (long long)(first + row) * p.q_stride_row + (long long)(head * p.share + n - row * p.share) * p.q_stride_head;
+        for (int nt = 0; nt < NT; nt++) {
+            const int n = column_of(2 * nt + (g & 1), g >> 1), row = (int)(n * share_magic >> 16);
+            const bool live = n < cols && (g & 1) < NC;
+            const uint16_t* q = p.q + (long long)(first + row) * p.q_stride_row + (long long)(head * p.share + n - row * p.share) * p.q_stride_head;
+            if constexpr (kPool) {
 #pragma unroll
                 for (int k = 0; k < kMT; k++)
 #pragma unroll
-                    for (int e = 0; e < 2; e++)
-                        qf[nt][k][e] = n < cols && (g & 1) < NC ? __ldg(reinterpret_cast<const uint32_t*>(q + 16 * k + 8 * e + 2 * t)) : 0u;
-            }
-#pragma unroll
-            for (int c = 0; c < NC; c++) factor[c] = p.scale_log2;
-        } else {
-#pragma unroll
-            for (int nt = 0; nt < NT; nt++) {
-                const int n = column_of(2 * nt + (g & 1), g >> 1), row = n / p.share;
-                const bool live = n < cols && (g & 1) < NC;
-                const uint16_t* q = p.q + (long long)(first + row) * p.q_stride_row + (long long)(head * p.share + n - row * p.share) * p.q_stride_head;
-                float x[kChunks][8];                          // 8 channels of each chunk, in the order the codes of a word come out
-                float amax = 0.0f;
+                    for (int e = 0; e < 2; e++) qf[nt][k][e] = live ? __ldg(reinterpret_cast<const uint32_t*>(q + 16 * k + 8 * e + 2 * t)) : 0u;
+                factor[2 * nt] = p.scale_log2;
+                if (NC > 1) factor[2 * nt + (NC > 1)] = p.scale_log2;
+            } else {
+                uint32_t w[kChunks][4];                       // 8 channels of each chunk, in the order the codes of a word come out
 #pragma unroll
                 for (int j = 0; j < kChunks; j++) {
-                    uint32_t w[4] = {0, 0, 0, 0};
+                    uint4 v = make_uint4(0, 0, 0, 0);
                     if (live) {
                         if (kK4) {
-                            const uint4 v = __ldg(reinterpret_cast<const uint4*>(q + 32 * j + 8 * t));
-                            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+                            v = __ldg(reinterpret_cast<const uint4*>(q + 32 * j + 8 * t));
                         } else {
                             const uint2 a = __ldg(reinterpret_cast<const uint2*>(q + 32 * j + 4 * t));
                             const uint2 b = __ldg(reinterpret_cast<const uint2*>(q + 32 * j + 16 + 4 * t));
-                            w[0] = a.x; w[1] = a.y; w[2] = b.x; w[3] = b.y;
+                            v = make_uint4(a.x, a.y, b.x, b.y);
                         }
                     }
-#pragma unroll
-                    for (int i = 0; i < 8; i++) {
-                        const uint32_t h = i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xFFFFu;
-                        x[j][i] = p.f16 ? half_bits_to_float(h) : bf16_bits_to_float(h);
-                        amax = fmaxf(amax, fabsf(x[j][i]));
-                    }
+                    w[j][0] = v.x; w[j][1] = v.y; w[j][2] = v.z; w[j][3] = v.w;
                 }
-                amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
-                amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
-                // largest magnitude into [2^13, 2^14); zeros as they are.  A column with a NaN or an infinity has no result but
-                // NaN: its factor is NaN.
-                const int e = (int)(__float_as_uint(amax) >> 23) - 127;
-                const int shift = amax > 0.0f ? min(13 - e, 120) : 0;
-                const float up = exp2i(shift);
-                float bad = 0.0f;                             // NaN when a channel is not finite
+                // Largest magnitude (ordered as the bit patterns are) into [2^13, 2^14); zeros as they are.  A column with a NaN or an
+                // infinity has no result but NaN: its factor is NaN.
+                uint32_t most = 0;
 #pragma unroll
                 for (int j = 0; j < kChunks; j++)
 #pragma unroll
-                    for (int i = 0; i < 8; i++) bad = fmaf(x[j][i], 0.0f, bad);
-                bad += __shfl_xor_sync(0xFFFFFFFFu, bad, 1);
-                bad += __shfl_xor_sync(0xFFFFFFFFu, bad, 2);
-                const float down = p.scale_log2 * exp2i(-shift) * 16777216.0f + bad;
-                if (bad != 0.0f)
-#pragma unroll
-                    for (int j = 0; j < kChunks; j++)
-#pragma unroll
-                        for (int i = 0; i < 8; i++) x[j][i] = 0.0f;
+                    for (int i = 0; i < 4; i++) most = __vmaxu2(most, w[j][i] & 0x7FFF7FFFu);
+                most = max(most & 0xFFFFu, most >> 16);
+                most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
+                most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
+                const bool bad = most >= (p.f16 ? 0x7C00u : 0x7F80u);
+                const float amax = p.f16 ? half_bits_to_float(most) : bf16_bits_to_float(most);
+                const int shift = most == 0 ? 0 : min(13 - ((int)(__float_as_uint(amax) >> 23) - 127), 120);
+                const float up = bad ? 0.0f : exp2i(shift);
+                const float down = bad ? __uint_as_float(0x7FC00000u) : p.scale_log2 * exp2i(-shift) * 16777216.0f;
 #pragma unroll
                 for (int j = 0; j < kChunks; j++) {
-                    float a = 0.0f;
+                    float x[8], a = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        x[2 * i] = p.f16 ? low_half(w[j][i]) : __uint_as_float(w[j][i] << 16);
+                        x[2 * i + 1] = p.f16 ? high_half(w[j][i]) : __uint_as_float(w[j][i] & 0xFFFF0000u);
+                    }
+                    if (bad)
+#pragma unroll
+                        for (int i = 0; i < 8; i++) x[i] = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 8; i++) { x[i] *= up; a += x[i]; }
 #pragma unroll
                     for (int m = 0; m < 2; m++) {
                         uint32_t* f = qf[nt][2 * j + m];
                         if (kK4) {                            // nibbles of a word: (0, 4) (1, 5) / (2, 6) (3, 7), odd ones 16 times up
-                            f[0] = half2_bits(x[j][2 * m] * up, x[j][2 * m + 4] * up);
-                            f[1] = half2_bits(x[j][2 * m + 1] * (up * 0.0625f), x[j][2 * m + 5] * (up * 0.0625f));
+                            f[0] = half2_bits(x[2 * m], x[2 * m + 4]);
+                            f[1] = half2_bits(x[2 * m + 1] * 0.0625f, x[2 * m + 5] * 0.0625f);
                         } else {
-                            f[0] = half2_bits(x[j][4 * m] * up, x[j][4 * m + 1] * up);
-                            f[1] = half2_bits(x[j][4 * m + 2] * up, x[j][4 * m + 3] * up);
+                            f[0] = half2_bits(x[4 * m], x[4 * m + 1]);
+                            f[1] = half2_bits(x[4 * m + 2], x[4 * m + 3]);
                         }
-                        a += low_half(f[0]) + high_half(f[0]);
-                        a = fmaf(low_half(f[1]) + high_half(f[1]), kK4 ? 16.0f : 1.0f, a);
                     }
+                    // the chunk's sum (what rounding to half took away lies 2^-25 below the largest)
                     a += __shfl_xor_sync(0xFFFFFFFFu, a, 1);
                     a += __shfl_xor_sync(0xFFFFFFFFu, a, 2);
                     a *= kK4 ? -4.76837158203125e-07f : -7.62939453125e-06f;        // -8 * 2^-24, -128 * 2^-24
@@ -655,14 +647,14 @@ __device__ __forceinline__ Item find_item(const AttentionParams& p, const SplitP
         int tiles = tiles_of(0), total = __reduce_add_sync(0xFFFFFFFFu, max(tiles, 0));
 #pragma unroll 1
         for (int s0 = 32; s0 < p.b.n_seqs; s0 += 32) total += __reduce_add_sync(0xFFFFFFFFu, max(tiles_of(s0), 0));
-        const int least = pl.warps_per_head;                 // a piece gives every warp a tile
-        const int piece = max((total + pl.target - 1) / pl.target, least);
+        const int least = 1 << pl.per_head_log2;             // a piece gives every warp a tile
+        const int piece = max((int)((uint32_t)(total + pl.target - 1) / (uint32_t)pl.target), least);
         int at = 0;
         it.seq = -1;
 #pragma unroll 1
         for (int s0 = 0; s0 < p.b.n_seqs && it.seq < 0; s0 += 32) {
             if (s0) tiles = tiles_of(s0);
-            const int n = tiles < 0 ? 0 : max(1, (tiles + piece - 1) / piece);
+            const int n = tiles < 0 ? 0 : max(1, (int)((uint32_t)(tiles + piece - 1) / (uint32_t)piece));
             int inc = n;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -705,17 +697,17 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const Item it = find_item(p, pl, blockIdx.x);
     if (!it.ok) return;                                      // the same in every warp
-    const int local = warp & (pl.heads - 1), sub = warp / pl.heads, head = blockIdx.y * pl.heads + local;
+    const int heads = 1 << pl.heads_log2, local = warp & (heads - 1), sub = warp >> pl.heads_log2, head = blockIdx.y * heads + local;
     const bool live = head < p.c.H;
     const int cols = min(it.rows * p.share, 4 * NC);
     K k(p);
     k.start(lane, smem_u32(smem) + warp * STAGES * K::kStage, smem_u32(smem) + WARPS * STAGES * K::kStage + warp * K::kCold);
     const TileRange range = tile_range(p, it.kv, it.lo, it.hi);
     if (live) {
-        const int step = pl.warps_per_head, n = it.begin + sub < it.end ? (it.end - it.begin - sub + step - 1) / step : 0;
+        const int step = 1 << pl.per_head_log2, n = it.begin + sub < it.end ? (it.end - it.begin - sub + step - 1) >> pl.per_head_log2 : 0;
         uint32_t* cold = reinterpret_cast<uint32_t*>(smem + WARPS * STAGES * K::kStage + warp * K::kCold);
         if (lane == 0) { cold[0] = it.kv; cold[1] = it.lo; cold[2] = it.hi; }
-        if (lane < 4 * NC) cold[4 + lane] = lane < cols ? row_position(p.b, it.seq, it.first + lane / p.share) : -1;
+        if (lane < 4 * NC) cold[4 + lane] = lane < cols ? row_position(p.b, it.seq, it.first + (int)(lane * pl.share_magic >> 16)) : -1;
         __syncwarp();
         // The warp's next 32 tiles, a lane each: place, first row and flags.  Whole tiles need no mask: seen by the earliest row and
         // inside the latest row's window, or among the sinks.
@@ -756,7 +748,7 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
         };
 #pragma unroll 1
         for (int i = 0; i < STAGES - 1; i++) fetch(i);
-        k.load_queries(it.first, cols, head);
+        k.load_queries(it.first, cols, head, pl.share_magic);
 #pragma unroll 1
         for (int i = 0; i < n; i++) {
             fetch(i + STAGES - 1);
@@ -773,59 +765,62 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
         pl.items[2 * it.seq] = it.first_item;
         pl.items[2 * it.seq + 1] = it.splits;
     }
-    // Results of a head's warps: through shared memory as [warp][register][lane], with m and l per column; each of the warps then
-    // sums up its share of the registers.  V's power of two is taken out here.
-    __syncthreads();
+    // V's power of two out of the result; l over the lanes.
+    const float down = K::kPool ? 1.0f : 16777216.0f * exp2i(-k.v_exp());
+#pragma unroll
+    for (int c = 0; c < NC; c++) {
+        k.sum[c] += __shfl_xor_sync(0xFFFFFFFFu, k.sum[c], 4);
+        k.sum[c] += __shfl_xor_sync(0xFFFFFFFFu, k.sum[c], 8);
+        k.sum[c] += __shfl_xor_sync(0xFFFFFFFFu, k.sum[c], 16);
+    }
+    // The warps of a head agree on a reference (m and l per column through shared memory), bring their results to it, and each
+    // sums up its share of the registers, which lie as [warp][register][lane].
+    float weight[NC];
+    __syncthreads();                                         // the rings are done with
     float* res = reinterpret_cast<float*>(smem);
     float* ml = res + WARPS * K::kRegs * 32;
-    if (live) {
-        const float down = K::kPool ? 1.0f : 16777216.0f * exp2i(-k.v_exp());
+    if (lane < 4)
+#pragma unroll
+        for (int c = 0; c < NC; c++) *reinterpret_cast<float2*>(ml + (warp * 4 * NC + column_of(c, lane)) * 2) = make_float2(k.ref[c], k.sum[c]);
+    __syncthreads();
+    float m[NC], l[NC];
+#pragma unroll
+    for (int c = 0; c < NC; c++) {
+        m[c] = k.ref[c];
+        l[c] = 0.0f;
+        const float* o = ml + (local * 4 * NC + column_of(c, k.t)) * 2;
+        for (int w = 0; w < WARPS >> pl.heads_log2; w++) m[c] = fmaxf(m[c], o[(w << pl.heads_log2) * 8 * NC]);
+        for (int w = 0; w < WARPS >> pl.heads_log2; w++)
+            l[c] = fmaf(fast_exp2(o[(w << pl.heads_log2) * 8 * NC] - m[c]), o[(w << pl.heads_log2) * 8 * NC + 1], l[c]);
+        weight[c] = fast_exp2(k.ref[c] - m[c]) * down;
+    }
+    {
         int r = 0;
 #pragma unroll
         for (int nt = 0; nt < K::NT; nt++)
 #pragma unroll
             for (int i = 0; i < K::kMT; i++)
 #pragma unroll
-                for (int j = 0; j < 4; j += NC == 1 ? 2 : 1) res[(warp * K::kRegs + r++) * 32 + lane] = k.acc[nt][i][j] * down;
-#pragma unroll
-        for (int c = 0; c < NC; c++) {
-            float s = k.sum[c];
-            s += __shfl_xor_sync(0xFFFFFFFFu, s, 4);
-            s += __shfl_xor_sync(0xFFFFFFFFu, s, 8);
-            s += __shfl_xor_sync(0xFFFFFFFFu, s, 16);
-            if (lane < 4) {
-                float* o = ml + (warp * 4 * NC + column_of(c, lane)) * 2;
-                o[0] = k.ref[c];
-                o[1] = s;
-            }
-        }
+                for (int j = 0; j < 4; j += NC == 1 ? 2 : 1) res[(warp * K::kRegs + r++) * 32 + lane] = k.acc[nt][i][j] * weight[(2 * nt + (j & 1)) % NC];
     }
     __syncthreads();
     if (!live) return;
-    // weights of the head's warps for the lane's columns
-    float m[NC], l[NC];
-#pragma unroll
-    for (int c = 0; c < NC; c++) {
-        m[c] = kNoMax;
-        l[c] = 0.0f;
-        for (int w = local; w < WARPS; w += pl.heads) m[c] = fmaxf(m[c], ml[(w * 4 * NC + column_of(c, k.t)) * 2]);
-        for (int w = local; w < WARPS; w += pl.heads) {
-            const float* o = ml + (w * 4 * NC + column_of(c, k.t)) * 2;
-            l[c] = fmaf(fast_exp2(o[0] - m[c]), o[1], l[c]);
-        }
-    }
     float* out = pl.partial + ((long long)blockIdx.x * p.c.H + head) * pl.item_stride;
-    for (int r = sub; r < K::kRegs; r += pl.warps_per_head) {
-        int ch, col;
-        place<K::kPool, D, NC>(r, lane, &ch, &col);
-        const int c = 2 * (col >> 3) + ((col >> 2) & 1);
-        float mc = m[0], lc = l[0];
-#pragma unroll
-        for (int j = 1; j < NC; j++) if (c == j) { mc = m[j]; lc = l[j]; }
+    const float* mine = res + local * K::kRegs * 32 + lane;
+#pragma unroll 4
+    for (int r = sub; r < K::kRegs; r += 1 << pl.per_head_log2) {
         float y = 0.0f;
-        for (int w = local; w < WARPS; w += pl.heads) y = fmaf(fast_exp2(ml[(w * 4 * NC + col) * 2] - mc), res[(w * K::kRegs + r) * 32 + lane], y);
-        if (pl.target) out[r * 32 + lane] = y;
-        else if (col < cols) store_out(p, it.first, head, ch, col, lc != 0.0f ? y / lc : 0.0f);
+        for (int w = 0; w < WARPS >> pl.heads_log2; w++) y += mine[((w << pl.heads_log2) * K::kRegs + r) * 32];
+        if (pl.target) {
+            out[r * 32 + lane] = y;
+        } else {
+            int ch, col;
+            place<K::kPool, D, NC>(r, lane, &ch, &col);
+            float lc = l[0];
+#pragma unroll
+            for (int j = 1; j < NC; j++) if (2 * (col >> 3) + ((col >> 2) & 1) == j) lc = l[j];
+            if (col < cols) store_out(p, it.first, head, ch, col, lc != 0.0f ? y / lc : 0.0f);
+        }
     }
     if (pl.target && sub == 0 && lane < 4)
 #pragma unroll
