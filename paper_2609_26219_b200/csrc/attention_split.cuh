@@ -618,8 +618,8 @@ __device__ __forceinline__ void place(int r, int lane, int* channel, int* col) {
     *col = 8 * nt + 4 * f + t;
 }
 
-__device__ __forceinline__ void store_out(const AttentionParams& p, int first, int head, int c, int n, float y) {
-    const int row = n / p.share;
+__device__ __forceinline__ void store_out(const AttentionParams& p, uint32_t share_magic, int first, int head, int c, int n, float y) {
+    const int row = (int)(n * share_magic >> 16);
     uint16_t* o = p.out + (long long)(first + row) * p.out_stride_row + (long long)(head * p.share + n - row * p.share) * p.out_stride_head + c;
     *o = (uint16_t)(p.f16 ? half2_bits(y, 0.0f) : bf162_bits(y, 0.0f));
 }
@@ -695,8 +695,15 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
     pdl_wait();
     // the warp's number through a shuffle: the compiler then knows that it is the same in all lanes
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    const Item it = find_item(p, pl, blockIdx.x);
-    if (!it.ok) return;                                      // the same in every warp
+    // One warp looks the piece up (sixteen at once would share its schedulers for three microseconds), the others read it.
+    __shared__ Item found;
+    if (warp == 0) {
+        const Item x = find_item(p, pl, blockIdx.x);
+        if (lane == 0) found = x;
+    }
+    __syncthreads();
+    const Item it = found;
+    if (!it.ok) return;
     const int heads = 1 << pl.heads_log2, local = warp & (heads - 1), sub = warp >> pl.heads_log2, head = blockIdx.y * heads + local;
     const bool live = head < p.c.H;
     const int cols = min(it.rows * p.share, 4 * NC);
@@ -819,7 +826,7 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
             float lc = l[0];
 #pragma unroll
             for (int j = 1; j < NC; j++) if (2 * (col >> 3) + ((col >> 2) & 1) == j) lc = l[j];
-            if (col < cols) store_out(p, it.first, head, ch, col, lc != 0.0f ? y / lc : 0.0f);
+            if (col < cols) store_out(p, pl.share_magic, it.first, head, ch, col, lc != 0.0f ? y / lc : 0.0f);
         }
     }
     if (pl.target && sub == 0 && lane < 4)
@@ -832,7 +839,7 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
 // are found first, a column per warp.
 constexpr int kJoinWarps = 16, kJoinThreads = 32 * kJoinWarps, kMaxPieces = 160;
 template <bool POOL, int D, int NC>
-__global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const AttentionParams p, const SplitPlan pl) {
+__global__ void __launch_bounds__(kJoinThreads, 1) attention_join_kernel(const AttentionParams p, const SplitPlan pl) {
     constexpr int kRegs = (NC == 1 ? 2 : 2 * NC) * (D / 16), kCols = 4 * NC;
     __shared__ float4 acc[kJoinWarps][32];
     __shared__ float weight[kMaxPieces][kCols];
@@ -849,14 +856,22 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Atte
     const int at = blockIdx.z * 32 + lane;                   // numbers 4 at .. 4 at + 3: one register of four lanes, four columns
     int ch0, col0;
     place<POOL, D, NC>(at >> 3, 0, &ch0, &col0);
+    // the warp's pieces are asked for first, so that they are on their way while the weights are found
+    constexpr int kMine = kMaxPieces / kJoinWarps;
+    float4 x[kMine];
+#pragma unroll
+    for (int i = 0; i < kMine; i++) {
+        x[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (col0 < cols && warp + i * kJoinWarps < n) x[i] = __ldg(reinterpret_cast<const float4*>(part + (warp + i * kJoinWarps) * step) + at);
+    }
     for (int c = warp; c < cols; c += kJoinWarps) {
         float m[kMaxPieces / 32], l[kMaxPieces / 32], top = kNoMax, sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < kMaxPieces / 32; i++) {
             m[i] = kNoMax; l[i] = 0.0f;
             if (32 * i + lane < n) {
-                const float2 x = __ldg(reinterpret_cast<const float2*>(part + (32 * i + lane) * step + kRegs * 32 + 2 * c));
-                m[i] = x.x; l[i] = x.y;
+                const float2 z = __ldg(reinterpret_cast<const float2*>(part + (32 * i + lane) * step + kRegs * 32 + 2 * c));
+                m[i] = z.x; l[i] = z.y;
             }
             top = fmaxf(top, m[i]);
         }
@@ -875,13 +890,14 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Atte
     __syncthreads();
     float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (col0 < cols) {
-#pragma unroll 5
-        for (int i = warp; i < n; i += kJoinWarps) {
-            const float4 x = __ldg(reinterpret_cast<const float4*>(part + i * step) + at);
-            y.x = fmaf(weight[i][col0], x.x, y.x);
-            if (col0 + 1 < cols) y.y = fmaf(weight[i][col0 + 1], x.y, y.y);
-            if (col0 + 2 < cols) y.z = fmaf(weight[i][col0 + 2], x.z, y.z);
-            if (col0 + 3 < cols) y.w = fmaf(weight[i][col0 + 3], x.w, y.w);
+#pragma unroll
+        for (int i = 0; i < kMine; i++) {
+            const int k = warp + i * kJoinWarps;
+            if (k >= n) break;
+            y.x = fmaf(weight[k][col0], x[i].x, y.x);
+            if (col0 + 1 < cols) y.y = fmaf(weight[k][col0 + 1], x[i].y, y.y);
+            if (col0 + 2 < cols) y.z = fmaf(weight[k][col0 + 2], x[i].z, y.z);
+            if (col0 + 3 < cols) y.w = fmaf(weight[k][col0 + 3], x[i].w, y.w);
         }
     }
     acc[warp][lane] = y;
@@ -894,7 +910,7 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const Atte
     float v = 0.0f;
 #pragma unroll
     for (int w = 0; w < kJoinWarps; w++) v += reinterpret_cast<const float*>(acc[w])[threadIdx.x];
-    store_out(p, first, h, c, col, norm[col] != 0.0f ? v / norm[col] : 0.0f);
+    store_out(p, pl.share_magic, first, h, c, col, norm[col] != 0.0f ? v / norm[col] : 0.0f);
 }
 
 }  // namespace patchkv
