@@ -169,7 +169,7 @@ struct SplitKernel {
     static constexpr int kStage = kScales + (kPool ? 0 : 2 * kTile * 8);                    // 8 bytes of scales per token, K then V
     static constexpr int kChunks = D / 32, kMT = D / 16;
     static constexpr int kRegs = (NC == 1 ? 2 : 4 * NT) * kMT;                              // accumulators of a lane that hold a column
-    static constexpr int kCold = 4 * (4 + 4 * NC);                                          // a warp's numbers that only masks need
+    static constexpr int kCold = 4 * (12 + 4 * NC);                                         // a warp's numbers that only masks need
     static constexpr int kSmem = WARPS * (STAGES * kStage + kCold);
     static constexpr int kMerge = WARPS * (kRegs * 32 + 2 * 4 * NC) * 4;                    // the warps' results, in the same memory
 
@@ -191,7 +191,16 @@ struct SplitKernel {
     __device__ __forceinline__ int kv() const { return (int)lds32(cold); }
     __device__ __forceinline__ int lo_pos() const { return (int)lds32(cold + 4); }
     __device__ __forceinline__ int hi_pos() const { return (int)lds32(cold + 8); }
-    __device__ __forceinline__ int pos(int c) const { return (int)lds32(cold + 16 + 4 * column_of(c, t)); }
+    __device__ __forceinline__ int pos(int c) const { return (int)lds32(cold + 48 + 4 * column_of(c, t)); }
+    // First token of the warp's tile i.
+    __device__ __forceinline__ int first_token(int i) const {
+        const int v = (int)lds32(cold + 12) + (i << lds32(cold + 16)), sinks = (int)lds32(cold + 20);
+        return (v < sinks ? v : (int)lds32(cold + 24) + v - sinks) * kTile;
+    }
+    __device__ __forceinline__ const int32_t* table() const {
+        const uint2 x = lds64(cold + 32);
+        return reinterpret_cast<const int32_t*>((uint64_t)x.y << 32 | x.x);
+    }
     __device__ __forceinline__ int v_exp() const { return 30 - (int)(v_most >> 10); }
     __device__ __forceinline__ int scales_per_row() const { return G32 ? kChunks : D / p.c.G; }
 
@@ -655,6 +664,7 @@ __device__ __forceinline__ Item find_item(const AttentionParams& p, const SplitP
         for (int s0 = 0; s0 < p.b.n_seqs && it.seq < 0; s0 += 32) {
             if (s0) tiles = tiles_of(s0);
             const int n = tiles < 0 ? 0 : max(1, (int)((uint32_t)(tiles + piece - 1) / (uint32_t)piece));
+            const int even = n ? (int)((uint32_t)(tiles + n - 1) / (uint32_t)n) : 0;      // the sequence's pieces of equal length
             int inc = n;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -668,8 +678,9 @@ __device__ __forceinline__ Item find_item(const AttentionParams& p, const SplitP
                 it.splits = __shfl_sync(0xFFFFFFFFu, n, src);
                 it.first_item = at + __shfl_sync(0xFFFFFFFFu, inc - n, src);
                 it.split = item - it.first_item;
-                it.begin = it.split * piece;
-                it.end = it.begin + piece;
+                const int length = __shfl_sync(0xFFFFFFFFu, even, src);
+                it.begin = it.split * length;
+                it.end = it.begin + length;
             }
             at += __shfl_sync(0xFFFFFFFFu, inc, 31);
         }
@@ -709,12 +720,17 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
     const int cols = min(it.rows * p.share, 4 * NC);
     K k(p);
     k.start(lane, smem_u32(smem) + warp * STAGES * K::kStage, smem_u32(smem) + WARPS * STAGES * K::kStage + warp * K::kCold);
-    const TileRange range = tile_range(p, it.kv, it.lo, it.hi);
     if (live) {
         const int step = 1 << pl.per_head_log2, n = it.begin + sub < it.end ? (it.end - it.begin - sub + step - 1) >> pl.per_head_log2 : 0;
         uint32_t* cold = reinterpret_cast<uint32_t*>(smem + WARPS * STAGES * K::kStage + warp * K::kCold);
-        if (lane == 0) { cold[0] = it.kv; cold[1] = it.lo; cold[2] = it.hi; }
-        if (lane < 4 * NC) cold[4 + lane] = lane < cols ? row_position(p.b, it.seq, it.first + (int)(lane * pl.share_magic >> 16)) : -1;
+        if (lane == 0) {
+            const TileRange range = tile_range(p, it.kv, it.lo, it.hi);
+            const uint64_t table = reinterpret_cast<uint64_t>(p.b.block_table + (long long)it.seq * p.b.table_stride);
+            cold[0] = it.kv; cold[1] = it.lo; cold[2] = it.hi;
+            cold[3] = it.begin + sub; cold[4] = pl.per_head_log2; cold[5] = range.sink_tiles; cold[6] = range.first;
+            cold[8] = (uint32_t)table; cold[9] = (uint32_t)(table >> 32);
+        }
+        if (lane < 4 * NC) cold[12 + lane] = lane < cols ? row_position(p.b, it.seq, it.first + (int)(lane * pl.share_magic >> 16)) : -1;
         __syncwarp();
         // The warp's next 32 tiles, a lane each: place, first row and flags.  Whole tiles need no mask: seen by the earliest row and
         // inside the latest row's window, or among the sinks.
@@ -722,8 +738,8 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
         auto place_of = [&](int i) {
             Place o = {0, 0, 0};
             if (i < n) {
-                const int t0 = range.tile(it.begin + sub + i * step) * kTile, lp = div_page(p.c, t0), slot0 = t0 - lp * p.c.P;
-                const int pg = __ldg(p.b.block_table + (long long)it.seq * p.b.table_stride + lp);
+                const int t0 = k.first_token(i), lp = div_page(p.c, t0), slot0 = t0 - lp * p.c.P;
+                const int pg = __ldg(k.table() + lp);
                 o.row0 = (uint32_t)slot0 * p.c.H + head;
                 if (pg < 0 || pg >= p.c.n_pages) {
                     latch(p.status);
@@ -745,7 +761,7 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
             // i runs through 0, 1, 2 ...; `here` is the 32-block of i
             const uint32_t flags = __shfl_sync(0xFFFFFFFFu, here.flags, i & 31), row0 = __shfl_sync(0xFFFFFFFFu, here.row0, i & 31);
             const long long at = __shfl_sync(0xFFFFFFFFu, here.at, i & 31);
-            if (i < n) k.fetch(fetch_base, at, row0, flags & 1, flags >> 1, flags & 1 ? 0 : range.tile(it.begin + sub + i * step) * kTile);
+            if (i < n) k.fetch(fetch_base, at, row0, flags & 1, flags >> 1, flags & 1 ? 0 : k.first_token(i));
             cp_commit();
             if ((i & 31) == 31) here = place_of(i + 1 + lane);
             whole = whole << 1 | (flags & 1);
@@ -762,7 +778,7 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
             cp_wait<STAGES - 1>();
             __syncwarp();
             const bool w = whole >> (STAGES - 1) & 1;
-            k.tile(base, w, present >> (STAGES - 1) & 1, w ? 0 : range.tile(it.begin + sub + i * step) * kTile, odd >> (STAGES - 1) & 1);
+            k.tile(base, w, present >> (STAGES - 1) & 1, w ? 0 : k.first_token(i), odd >> (STAGES - 1) & 1);
             __syncwarp();                                    // the stage may be filled again
             base = base == k.ring + (STAGES - 1) * K::kStage ? k.ring : base + K::kStage;
         }
