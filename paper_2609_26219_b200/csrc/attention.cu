@@ -236,7 +236,9 @@ cudaError_t launch_split(const AttentionParams& p, const SplitPlan& pl, int grou
     if (e != cudaSuccess) return e;
     e = launch_pdl(kernel, dim3(pl.max_items, groups), dim3(S::kWarps * 32), smem, stream, p, pl);
     if (e != cudaSuccess || pl.target == 0) return e;
-    return launch_pdl(attention_join_kernel<KF == FMT_BF16, D, NC>, dim3(p.b.n_seqs, p.c.H, (NC == 1 ? 2 : 2 * NC) * (D / 16) / 4), dim3(kJoinThreads), 0, stream, p, pl);
+    const dim3 grid(p.b.n_seqs, p.c.H, (NC == 1 ? 2 : 2 * NC) * (D / 16) / 4);
+    if (pl.max_items > 16 * p.b.n_seqs) return launch_pdl(attention_join_kernel<KF == FMT_BF16, D, NC, 16>, grid, dim3(512), 0, stream, p, pl);
+    return launch_pdl(attention_join_kernel<KF == FMT_BF16, D, NC, 4>, grid, dim3(128), 0, stream, p, pl);
 }
 template <int D, int NC, bool G32>
 cudaError_t launch_split_tag(const AttentionParams& p, const SplitPlan& pl, int groups, cudaStream_t s) {

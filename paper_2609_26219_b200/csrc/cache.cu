@@ -19,6 +19,7 @@ struct RowParams {
     int32_t* status;
     int32_t vecs;               // 8-channel vectors of a row: H * D / 8
     int32_t seg;                // lanes per scale group: G / 8
+    int32_t G_shift, D_shift;   // log2 of G; of D when it is a power of two, else -1
 };
 
 __device__ __forceinline__ void latch_bounds(int32_t* status) { atomicCAS(status, 0, (int)PATCHKV_E_BOUNDS); }
@@ -100,31 +101,54 @@ __device__ __forceinline__ void encode8(const uint4& w, uint8_t* codes, uint8_t*
     if (scale) *reinterpret_cast<__half*>(scale) = s16;
 }
 
-// A thread takes eight channels of one row, K and V: the loads and stores of a warp are contiguous, the groups' maxima
-// go through shuffles, and the row's slot is looked up while the row is on its way.  Bound by memory.
+// A warp takes a row, a lane eight channels of K and of V at a time, kBatch times 32 vectors at once: the row's slot is looked up once
+// per row (with a thread per vector that look-up was most of the instructions: 170 us to read 2 x 64k tokens, 27 us for
+// 16k rows), loads and stores of a warp are contiguous, the groups' maxima go through shuffles.  Bound by memory.
+constexpr int kBatch = 4;
+
+// Element offset of vector `vec` inside a row of the caller's tensors.
+__device__ __forceinline__ long long row_element(const RowParams& p, int vec) {
+    const int e = vec * 8;
+    if (p.rows.stride_head == p.c.D) return e;
+    const int h = p.D_shift >= 0 ? e >> p.D_shift : e / p.c.D;
+    return (long long)h * p.rows.stride_head + (e - h * p.c.D);
+}
+
 template <int TYPE, int KF, int VF>
-__global__ void __launch_bounds__(kRowThreads) cache_append_kernel(const RowParams p) {
+__global__ void __launch_bounds__(kRowThreads) cache_append_kernel(const __grid_constant__ RowParams p) {
     pdl_trigger();
-    const uint32_t i = blockIdx.x * kRowThreads + threadIdx.x, q = i / (uint32_t)p.vecs;
-    const int r = (int)q, vec = (int)(i - q * (uint32_t)p.vecs);
-    bool live = r < p.b.n_rows;
-    const int e = vec * 8, h = e / p.c.D, c = e - h * p.c.D;
-    uint4 kw = make_uint4(0, 0, 0, 0), vw = kw;
+    const int r = (int)((blockIdx.x * kRowThreads + threadIdx.x) >> 5), lane = threadIdx.x & 31;
+    if (r >= p.b.n_rows) return;
+    pdl_wait();
     uint8_t* page = nullptr;
     int slot = 0;
-    pdl_wait();
-    live = live && find_slot<true>(p, r, vec == 0, &page, &slot);
-    if (live) {
-        const long long src = (long long)r * p.rows.stride_row + (long long)h * p.rows.stride_head + c;
-        kw = __ldg(reinterpret_cast<const uint4*>(p.rows.k + src));
-        vw = __ldg(reinterpret_cast<const uint4*>(p.rows.v + src));
+    bool found = false;
+    for (int v0 = 0; v0 < p.vecs; v0 += 32 * kBatch) {
+        uint4 kw[kBatch], vw[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; i++) {
+            const int vec = v0 + 32 * i + lane;
+            kw[i] = vw[i] = make_uint4(0, 0, 0, 0);
+            if (vec < p.vecs) {
+                const long long src = (long long)r * p.rows.stride_row + row_element(p, vec);
+                kw[i] = __ldg(reinterpret_cast<const uint4*>(p.rows.k + src));
+                vw[i] = __ldg(reinterpret_cast<const uint4*>(p.rows.v + src));
+            }
+        }
+        if (v0 == 0) found = find_slot<true>(p, r, lane == 0, &page, &slot);      // while the row is on its way
+        if (!found) return;                                  // the same for all lanes
+#pragma unroll
+        for (int i = 0; i < kBatch; i++) {
+            if (v0 + 32 * i >= p.vecs) break;
+            const int vec = v0 + 32 * i + lane;
+            const uint32_t at = ((uint32_t)slot * p.vecs + vec) * 8;
+            const bool first = (vec & (p.seg - 1)) == 0;
+            const uint32_t group = at >> p.G_shift;
+            encode8<TYPE, KF>(kw[i], page + (KF == FMT_INT8 ? at : at >> 1), first ? page + p.c.k_scales + 2 * group : nullptr, p.seg, vec < p.vecs);
+            encode8<TYPE, VF>(vw[i], page + p.c.v_codes + (VF == FMT_INT8 ? at : at >> 1), first ? page + p.c.v_scales + 2 * group : nullptr,
+                              p.seg, vec < p.vecs);
+        }
     }
-    const uint32_t at = (uint32_t)slot * p.c.H * p.c.D + e;
-    const bool first = (vec & (p.seg - 1)) == 0;
-    const uint32_t group = at / p.c.G;
-    encode8<TYPE, KF>(kw, page + (KF == FMT_INT8 ? at : at >> 1), first ? page + p.c.k_scales + 2 * group : nullptr, p.seg, live);
-    encode8<TYPE, VF>(vw, page + p.c.v_codes + (VF == FMT_INT8 ? at : at >> 1), first ? page + p.c.v_scales + 2 * group : nullptr,
-                      p.seg, live);
 }
 
 // Eight codes and their scale -> eight channels.  An integer u < 2^23 in the low bits of 2^23's pattern is the float
@@ -158,24 +182,36 @@ __device__ __forceinline__ uint2 load_codes8(const uint8_t* codes, uint32_t at) 
 }
 
 template <int TYPE, int KF, int VF>
-__global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const RowParams p) {
+__global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_constant__ RowParams p) {
     pdl_trigger();
-    const uint32_t i = blockIdx.x * kRowThreads + threadIdx.x, q = i / (uint32_t)p.vecs;
-    const int r = (int)q, vec = (int)(i - q * (uint32_t)p.vecs);
+    const int r = (int)((blockIdx.x * kRowThreads + threadIdx.x) >> 5), lane = threadIdx.x & 31;
     if (r >= p.b.n_rows) return;
-    const int e = vec * 8, h = e / p.c.D, c = e - h * p.c.D;
     uint8_t* page = nullptr;
     int slot = 0;
     pdl_wait();
-    if (!find_slot<false>(p, r, vec == 0, &page, &slot)) return;
-    const uint32_t at = (uint32_t)slot * p.c.H * p.c.D + e;
-    const uint32_t group = at / p.c.G;
-    const uint2 kc = load_codes8<KF>(page, at), vc = load_codes8<VF>(page + p.c.v_codes, at);
-    const float ks = __half2float(*reinterpret_cast<const __half*>(page + p.c.k_scales + 2 * group));
-    const float vs = __half2float(*reinterpret_cast<const __half*>(page + p.c.v_scales + 2 * group));
-    const long long dst = (long long)r * p.rows.stride_row + (long long)h * p.rows.stride_head + c;
-    *reinterpret_cast<uint4*>(p.rows.k + dst) = decode8<TYPE, KF>(kc, ks);
-    *reinterpret_cast<uint4*>(p.rows.v + dst) = decode8<TYPE, VF>(vc, vs);
+    if (!find_slot<false>(p, r, lane == 0, &page, &slot)) return;
+    for (int v0 = 0; v0 < p.vecs; v0 += 32 * kBatch) {
+        uint2 kc[kBatch], vc[kBatch];
+        uint16_t ks[kBatch], vs[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; i++) {
+            const int vec = min(v0 + 32 * i + lane, p.vecs - 1);
+            const uint32_t at = ((uint32_t)slot * p.vecs + vec) * 8, group = at >> p.G_shift;
+            kc[i] = load_codes8<KF>(page, at);
+            vc[i] = load_codes8<VF>(page + p.c.v_codes, at);
+            ks[i] = *reinterpret_cast<const uint16_t*>(page + p.c.k_scales + 2 * group);
+            vs[i] = *reinterpret_cast<const uint16_t*>(page + p.c.v_scales + 2 * group);
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; i++) {
+            const int vec = v0 + 32 * i + lane;
+            if (vec < p.vecs) {
+                const long long dst = (long long)r * p.rows.stride_row + row_element(p, vec);
+                *reinterpret_cast<uint4*>(p.rows.k + dst) = decode8<TYPE, KF>(kc[i], half_bits_to_float(ks[i]));
+                *reinterpret_cast<uint4*>(p.rows.v + dst) = decode8<TYPE, VF>(vc[i], half_bits_to_float(vs[i]));
+            }
+        }
+    }
 }
 
 // Any geometry, any strides: one thread per (row, section, head) walks the head's groups with byte accesses to the page.
@@ -314,7 +350,8 @@ int cache_rows(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, const p
                       ((ka | va) & 15) == 0 && rows->stride_row % 8 == 0 && rows->stride_head % 8 == 0;
     p.vecs = (int)((long long)g->n_kv_heads * g->head_dim / 8);
     p.seg = g->group / 8;
-    const long long threads = (long long)p.b.n_rows * (fast ? p.vecs : 2 * g->n_kv_heads);
+    p.G_shift = gs; p.D_shift = log2_exact(g->head_dim);
+    const long long threads = (long long)p.b.n_rows * (fast ? 32 : 2 * g->n_kv_heads);
     const long long grid = (threads + kRowThreads - 1) / kRowThreads;
     if (grid * kRowThreads > (1ll << 32) - 1) return fail(ctx, PATCHKV_E_UNSUPPORTED, w + ": too many rows for one call");
     DeviceGuard guard(ctx->device);
