@@ -1,5 +1,7 @@
 // Rows into and out of a cache of quantised pages: patchkv_cache_append, patchkv_cache_read, and the checks that the
 // live-cache calls share.
+#include <math.h>
+
 #include "live.cuh"
 
 namespace patchkv {
@@ -19,6 +21,7 @@ struct RowParams {
     int32_t* status;
     int32_t vecs;               // 8-channel vectors of a row: H * D / 8
     int32_t seg;                // lanes per scale group: G / 8
+    int32_t parts;              // warps that share a row (32 vectors each at a time)
     int32_t G_shift, D_shift;   // log2 of G; of D when it is a power of two, else -1
 };
 
@@ -55,38 +58,44 @@ __device__ __forceinline__ uint32_t pack_pair(float lo, float hi) {
 }
 
 // Eight channels -> codes and, from the group's first lane, its scale.  `seg` lanes share a group (a power of two).
-// The quotient: r = 1 / s rounded, t = x * r, one correction t + (x - t*s) * r.  s has 11 significant bits, so its
-// reciprocal is not the one case in which a correctly rounded r does not make the corrected quotient the correctly
-// rounded x / s (Markstein's theorem); x and s have 11 bits at most, so x / s is exactly a half-integer or at least 2^-12
-// away from one, and the fp32 rounding of the quotient (2^-17 at |x / s| <= 128) does not carry it across.
+//   Group maximum: magnitudes are ordered as their 16-bit patterns, two at a time.
+//   s = fp16(amax / qmax): q0 = amax * y, q = q0 + (amax - q0 * qmax) * y with y = fp32(1 / qmax), fused, is the correctly rounded fp32
+//   quotient for every bf16 and fp16 amax and qmax 7 or 127 (gone through in exact arithmetic).
+//   code = rint(x / s): t = x * r with r = 1 / s to an ulp or two, corrected to t' = t + (x - t * s) * r, the remainder exact.  x and s have 11
+//   bits at most, so x / s is a half-integer or 2^-12 away from one: t' is within 2^-15 of it, and where x / s is a half-integer h
+//   the correction differs from h - t by 2^-22 of itself, which rounds away: t' = h.  Adding 1.5 * 2^23 rounds to the integer,
+//   ties to even.  |x / s| <= qmax (1 + 2^-11) unless s is subnormal; then the quotients are clamped.
 template <int TYPE, int FMT>
 __device__ __forceinline__ void encode8(const uint4& w, uint8_t* codes, uint8_t* scale, int seg, bool live) {
-    float x[8];
     const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        x[2 * i] = to_float<TYPE>(ws[i] & 0xFFFFu);
-        x[2 * i + 1] = to_float<TYPE>(ws[i] >> 16);
-    }
-    float amax = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; i++) amax = fmaxf(amax, fabsf(x[i]));
-    for (int d = 1; d < seg; d <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, d));
+    uint32_t most = __vmaxu2(__vmaxu2(ws[0] & 0x7FFF7FFFu, ws[1] & 0x7FFF7FFFu), __vmaxu2(ws[2] & 0x7FFF7FFFu, ws[3] & 0x7FFF7FFFu));
+    for (int d = 1; d < seg; d <<= 1) most = __vmaxu2(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
     if (!live) return;
-    constexpr float qmax = FMT == FMT_INT8 ? 127.0f : 7.0f;
-    const __half s16 = __float2half_rn(__fdiv_rn(amax, qmax));
-    float s = __half2float(s16);
-    const bool usable = s > 0.0f && s <= 65504.0f;          // a zero or infinite scale: all codes zero
-    if (!usable) s = 1.0f;
-    const float r = __frcp_rn(s);
+    constexpr float qmax = FMT == FMT_INT8 ? 127.0f : 7.0f, y = 1.0f / qmax;
+    const float amax = to_float<TYPE>(max(most & 0xFFFFu, most >> 16));
+    const float q0 = __fmul_rn(amax, y), q = __fmaf_rn(__fmaf_rn(-q0, qmax, amax), y, q0);
+    const uint32_t s16 = pack_pair<PATCHKV_ROWS_F16>(amax > 3.0e38f ? INFINITY : q, 0.0f) & 0xFFFFu;
+    const bool usable = s16 != 0 && s16 < 0x7C00u;          // a zero or infinite scale: all codes zero
+    const float s = half_bits_to_float(usable ? s16 : 0x3C00u);
+    float r;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(s));
+    if (!usable) r = 0.0f;
+    const f32x2 r2 = pack2(r, r), s2 = pack2(-s, -s), magic = pack2(12582912.0f, 12582912.0f);
     uint32_t kb[8];
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const float xi = usable ? x[i] : 0.0f;
-        float t = __fmul_rn(xi, r);
-        t = __fmaf_rn(__fmaf_rn(-t, s, xi), r, t);
-        t = fminf(fmaxf(t, -qmax), qmax);                   // only a subnormal scale leaves |t| above qmax
-        kb[i] = __float_as_uint(__fadd_rn(t, 12582912.0f)); // 1.5 * 2^23: rounds to an integer, ties to even
+    for (int i = 0; i < 4; i++) {
+        const f32x2 x = usable ? pack2(to_float<TYPE>(ws[i] & 0xFFFFu), to_float<TYPE>(ws[i] >> 16)) : pack2(0.0f, 0.0f);
+        f32x2 t = mul2(x, r2);
+        t = fma2(fma2(t, s2, x), r2, t);
+        if (s16 < 0x0400u) {                                // subnormal
+            float a, b;
+            unpack2(t, a, b);
+            t = pack2(fminf(fmaxf(a, -qmax), qmax), fminf(fmaxf(b, -qmax), qmax));
+        }
+        float a, b;
+        unpack2(add2(t, magic), a, b);
+        kb[2 * i] = __float_as_uint(a);
+        kb[2 * i + 1] = __float_as_uint(b);
     }
     const uint32_t w0 = __byte_perm(__byte_perm(kb[0], kb[1], 0x0040), __byte_perm(kb[2], kb[3], 0x0040), 0x5410);
     const uint32_t w1 = __byte_perm(__byte_perm(kb[4], kb[5], 0x0040), __byte_perm(kb[6], kb[7], 0x0040), 0x5410);
@@ -98,7 +107,7 @@ __device__ __forceinline__ void encode8(const uint4& w, uint8_t* codes, uint8_t*
         b = (b | (b >> 4)) & 0x00FF00FFu; b = (b | (b >> 8)) & 0x0000FFFFu;
         *reinterpret_cast<uint32_t*>(codes) = a | (b << 16);
     }
-    if (scale) *reinterpret_cast<__half*>(scale) = s16;
+    if (scale) *reinterpret_cast<uint16_t*>(scale) = (uint16_t)s16;
 }
 
 // A warp takes a row, a lane eight channels of K and of V at a time, kBatch times 32 vectors at once: the row's slot is looked up once
@@ -106,6 +115,13 @@ __device__ __forceinline__ void encode8(const uint4& w, uint8_t* codes, uint8_t*
 // 16k rows), loads and stores of a warp are contiguous, the groups' maxima go through shuffles.  Bound by memory.
 constexpr int kBatch = 4;
 
+// Row and first vector of a warp.
+__device__ __forceinline__ bool warp_place(const RowParams& p, int* r, int* v_first) {
+    const uint32_t w = (blockIdx.x * kRowThreads + threadIdx.x) >> 5, q = p.parts == 1 ? w : w / (uint32_t)p.parts;
+    *r = (int)q;
+    *v_first = (int)(w - q * p.parts) * 32;
+    return *r < p.b.n_rows;
+}
 // Element offset of vector `vec` inside a row of the caller's tensors.
 __device__ __forceinline__ long long row_element(const RowParams& p, int vec) {
     const int e = vec * 8;
@@ -117,17 +133,18 @@ __device__ __forceinline__ long long row_element(const RowParams& p, int vec) {
 template <int TYPE, int KF, int VF>
 __global__ void __launch_bounds__(kRowThreads) cache_append_kernel(const __grid_constant__ RowParams p) {
     pdl_trigger();
-    const int r = (int)((blockIdx.x * kRowThreads + threadIdx.x) >> 5), lane = threadIdx.x & 31;
-    if (r >= p.b.n_rows) return;
+    int r, v_first;
+    if (!warp_place(p, &r, &v_first)) return;
     pdl_wait();
     uint8_t* page = nullptr;
     int slot = 0;
     bool found = false;
-    for (int v0 = 0; v0 < p.vecs; v0 += 32 * kBatch) {
+    const int lane = threadIdx.x & 31, stride = 32 * p.parts;
+    for (int v0 = v_first; v0 < p.vecs; v0 += stride * kBatch) {
         uint4 kw[kBatch], vw[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; i++) {
-            const int vec = v0 + 32 * i + lane;
+            const int vec = v0 + stride * i + lane;
             kw[i] = vw[i] = make_uint4(0, 0, 0, 0);
             if (vec < p.vecs) {
                 const long long src = (long long)r * p.rows.stride_row + row_element(p, vec);
@@ -135,12 +152,12 @@ __global__ void __launch_bounds__(kRowThreads) cache_append_kernel(const __grid_
                 vw[i] = __ldg(reinterpret_cast<const uint4*>(p.rows.v + src));
             }
         }
-        if (v0 == 0) found = find_slot<true>(p, r, lane == 0, &page, &slot);      // while the row is on its way
+        if (v0 == v_first) found = find_slot<true>(p, r, lane == 0 && v_first == 0, &page, &slot);      // while the row is on its way
         if (!found) return;                                  // the same for all lanes
 #pragma unroll
         for (int i = 0; i < kBatch; i++) {
-            if (v0 + 32 * i >= p.vecs) break;
-            const int vec = v0 + 32 * i + lane;
+            if (v0 + stride * i >= p.vecs) break;
+            const int vec = v0 + stride * i + lane;
             const uint32_t at = ((uint32_t)slot * p.vecs + vec) * 8;
             const bool first = (vec & (p.seg - 1)) == 0;
             const uint32_t group = at >> p.G_shift;
@@ -184,18 +201,19 @@ __device__ __forceinline__ uint2 load_codes8(const uint8_t* codes, uint32_t at) 
 template <int TYPE, int KF, int VF>
 __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_constant__ RowParams p) {
     pdl_trigger();
-    const int r = (int)((blockIdx.x * kRowThreads + threadIdx.x) >> 5), lane = threadIdx.x & 31;
-    if (r >= p.b.n_rows) return;
+    int r, v_first;
+    if (!warp_place(p, &r, &v_first)) return;
+    const int lane = threadIdx.x & 31, stride = 32 * p.parts;
     uint8_t* page = nullptr;
     int slot = 0;
     pdl_wait();
-    if (!find_slot<false>(p, r, lane == 0, &page, &slot)) return;
-    for (int v0 = 0; v0 < p.vecs; v0 += 32 * kBatch) {
+    if (!find_slot<false>(p, r, lane == 0 && v_first == 0, &page, &slot)) return;
+    for (int v0 = v_first; v0 < p.vecs; v0 += stride * kBatch) {
         uint2 kc[kBatch], vc[kBatch];
         uint16_t ks[kBatch], vs[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; i++) {
-            const int vec = min(v0 + 32 * i + lane, p.vecs - 1);
+            const int vec = min(v0 + stride * i + lane, p.vecs - 1);
             const uint32_t at = ((uint32_t)slot * p.vecs + vec) * 8, group = at >> p.G_shift;
             kc[i] = load_codes8<KF>(page, at);
             vc[i] = load_codes8<VF>(page + p.c.v_codes, at);
@@ -204,7 +222,7 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
         }
 #pragma unroll
         for (int i = 0; i < kBatch; i++) {
-            const int vec = v0 + 32 * i + lane;
+            const int vec = v0 + stride * i + lane;
             if (vec < p.vecs) {
                 const long long dst = (long long)r * p.rows.stride_row + row_element(p, vec);
                 *reinterpret_cast<uint4*>(p.rows.k + dst) = decode8<TYPE, KF>(kc[i], half_bits_to_float(ks[i]));
@@ -351,7 +369,10 @@ int cache_rows(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, const p
     p.vecs = (int)((long long)g->n_kv_heads * g->head_dim / 8);
     p.seg = g->group / 8;
     p.G_shift = gs; p.D_shift = log2_exact(g->head_dim);
-    const long long threads = (long long)p.b.n_rows * (fast ? 32 : 2 * g->n_kv_heads);
+    // Few rows: a warp for every 32 vectors of a row (8 rows of 128 vectors, append and read: 7.2 us in one warp each, 4.7 in four).
+    const int groups = (p.vecs + 31) / 32;
+    p.parts = (long long)p.b.n_rows * groups <= 16 * 148 ? groups : 1;
+    const long long threads = (long long)p.b.n_rows * (fast ? 32 * p.parts : 2 * g->n_kv_heads);
     const long long grid = (threads + kRowThreads - 1) / kRowThreads;
     if (grid * kRowThreads > (1ll << 32) - 1) return fail(ctx, PATCHKV_E_UNSUPPORTED, w + ": too many rows for one call");
     DeviceGuard guard(ctx->device);
