@@ -19,8 +19,8 @@ struct RowParams {
     BatchDev b;
     RowsDev rows;
     int32_t* status;
-    int32_t vecs;               // 8-channel vectors of a row: H * D / 8
-    int32_t seg;                // lanes per scale group: G / 8
+    int32_t vecs;               // vectors of a row: H * D / 8, or / 32
+    int32_t seg;                // lanes per scale group: G / 8, or / 32
     int32_t parts;              // warps that share a row (32 vectors each at a time)
     int32_t G_shift, D_shift;   // log2 of G; of D when it is a power of two, else -1
 };
@@ -57,7 +57,7 @@ __device__ __forceinline__ uint32_t pack_pair(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Eight channels -> codes and, from the group's first lane, its scale.  `seg` lanes share a group (a power of two).
+// CH = 8 or 32 channels (w) -> codes and, from the group's first lane, its scale.  `seg` lanes share a group (a power of two).
 //   Group maximum: magnitudes are ordered as their 16-bit patterns, two at a time.
 //   s = fp16(amax / qmax): q0 = amax * y, q = q0 + (amax - q0 * qmax) * y with y = fp32(1 / qmax), fused, is the correctly rounded fp32
 //   quotient for every bf16 and fp16 amax and qmax 7 or 127 (gone through in exact arithmetic).
@@ -65,10 +65,12 @@ __device__ __forceinline__ uint32_t pack_pair(float lo, float hi) {
 //   bits at most, so x / s is a half-integer or 2^-12 away from one: t' is within 2^-15 of it, and where x / s is a half-integer h
 //   the correction differs from h - t by 2^-22 of itself, which rounds away: t' = h.  Adding 1.5 * 2^23 rounds to the integer,
 //   ties to even.  |x / s| <= qmax (1 + 2^-11) unless s is subnormal; then the quotients are clamped.
-template <int TYPE, int FMT>
-__device__ __forceinline__ void encode8(const uint4& w, uint8_t* codes, uint8_t* scale, int seg, bool live) {
-    const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-    uint32_t most = __vmaxu2(__vmaxu2(ws[0] & 0x7FFF7FFFu, ws[1] & 0x7FFF7FFFu), __vmaxu2(ws[2] & 0x7FFF7FFFu, ws[3] & 0x7FFF7FFFu));
+template <int TYPE, int FMT, int CH>
+__device__ __forceinline__ void encode(const uint4 (&w)[CH / 8], uint8_t* codes, uint8_t* scale, int seg, bool live) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < CH / 8; i++)
+        most = __vmaxu2(most, __vmaxu2(__vmaxu2(w[i].x & 0x7FFF7FFFu, w[i].y & 0x7FFF7FFFu), __vmaxu2(w[i].z & 0x7FFF7FFFu, w[i].w & 0x7FFF7FFFu)));
     for (int d = 1; d < seg; d <<= 1) most = __vmaxu2(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
     if (!live) return;
     constexpr float qmax = FMT == FMT_INT8 ? 127.0f : 7.0f, y = 1.0f / qmax;
@@ -79,42 +81,53 @@ __device__ __forceinline__ void encode8(const uint4& w, uint8_t* codes, uint8_t*
     const float s = half_bits_to_float(usable ? s16 : 0x3C00u);
     float r;
     asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(s));
-    if (!usable) r = 0.0f;
     const f32x2 r2 = pack2(r, r), s2 = pack2(-s, -s), magic = pack2(12582912.0f, 12582912.0f);
-    uint32_t kb[8];
+    uint32_t out[CH / 8][2];
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-        const f32x2 x = usable ? pack2(to_float<TYPE>(ws[i] & 0xFFFFu), to_float<TYPE>(ws[i] >> 16)) : pack2(0.0f, 0.0f);
-        f32x2 t = mul2(x, r2);
-        t = fma2(fma2(t, s2, x), r2, t);
-        if (s16 < 0x0400u) {                                // subnormal
+    for (int k = 0; k < CH / 8; k++) {
+        const uint32_t ws[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+        uint32_t kb[8];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const f32x2 x = pack2(to_float<TYPE>(ws[i] & 0xFFFFu), to_float<TYPE>(ws[i] >> 16));
+            f32x2 t = mul2(x, r2);
+            t = fma2(fma2(t, s2, x), r2, t);
             float a, b;
-            unpack2(t, a, b);
-            t = pack2(fminf(fmaxf(a, -qmax), qmax), fminf(fmaxf(b, -qmax), qmax));
+            if (s16 < 0x0400u) {                            // subnormal
+                unpack2(t, a, b);
+                t = pack2(fminf(fmaxf(a, -qmax), qmax), fminf(fmaxf(b, -qmax), qmax));
+            }
+            unpack2(add2(t, magic), a, b);
+            kb[2 * i] = __float_as_uint(a);
+            kb[2 * i + 1] = __float_as_uint(b);
         }
-        float a, b;
-        unpack2(add2(t, magic), a, b);
-        kb[2 * i] = __float_as_uint(a);
-        kb[2 * i + 1] = __float_as_uint(b);
+        const uint32_t w0 = __byte_perm(__byte_perm(kb[0], kb[1], 0x0040), __byte_perm(kb[2], kb[3], 0x0040), 0x5410);
+        const uint32_t w1 = __byte_perm(__byte_perm(kb[4], kb[5], 0x0040), __byte_perm(kb[6], kb[7], 0x0040), 0x5410);
+        if (FMT == FMT_INT8) {
+            out[k][0] = w0; out[k][1] = w1;
+        } else {
+            uint32_t a = w0 & 0x0F0F0F0Fu, b = w1 & 0x0F0F0F0Fu;
+            a = (a | (a >> 4)) & 0x00FF00FFu; b = (b | (b >> 4)) & 0x00FF00FFu;
+            out[k][0] = __byte_perm(a, b, 0x6420);
+        }
+        if (!usable) out[k][0] = out[k][1] = 0;
     }
-    const uint32_t w0 = __byte_perm(__byte_perm(kb[0], kb[1], 0x0040), __byte_perm(kb[2], kb[3], 0x0040), 0x5410);
-    const uint32_t w1 = __byte_perm(__byte_perm(kb[4], kb[5], 0x0040), __byte_perm(kb[6], kb[7], 0x0040), 0x5410);
-    if (FMT == FMT_INT8) {
-        *reinterpret_cast<uint2*>(codes) = make_uint2(w0, w1);
+    if constexpr (CH == 8) {
+        if (FMT == FMT_INT8) *reinterpret_cast<uint2*>(codes) = make_uint2(out[0][0], out[0][1]);
+        else *reinterpret_cast<uint32_t*>(codes) = out[0][0];
+    } else if constexpr (FMT == FMT_INT8) {
+        reinterpret_cast<uint4*>(codes)[0] = make_uint4(out[0][0], out[0][1], out[1][0], out[1][1]);
+        reinterpret_cast<uint4*>(codes)[1] = make_uint4(out[2][0], out[2][1], out[3][0], out[3][1]);
     } else {
-        uint32_t a = w0 & 0x0F0F0F0Fu, b = w1 & 0x0F0F0F0Fu;
-        a = (a | (a >> 4)) & 0x00FF00FFu; a = (a | (a >> 8)) & 0x0000FFFFu;
-        b = (b | (b >> 4)) & 0x00FF00FFu; b = (b | (b >> 8)) & 0x0000FFFFu;
-        *reinterpret_cast<uint32_t*>(codes) = a | (b << 16);
+        *reinterpret_cast<uint4*>(codes) = make_uint4(out[0][0], out[1][0], out[2][0], out[3][0]);
     }
     if (scale) *reinterpret_cast<uint16_t*>(scale) = (uint16_t)s16;
 }
 
-// A warp takes a row, a lane eight channels of K and of V at a time, kBatch times 32 vectors at once: the row's slot is looked up once
-// per row (with a thread per vector that look-up was most of the instructions: 170 us to read 2 x 64k tokens, 27 us for
-// 16k rows), loads and stores of a warp are contiguous, the groups' maxima go through shuffles.  Bound by memory.
-constexpr int kBatch = 4;
-
+// A warp takes a row (or a share of one), a lane a vector of K and of V, several times 32 of them at once: the row's slot is looked up
+// once, loads and stores of a warp are contiguous, the groups' maxima go through shuffles.  (With a thread per vector of a row
+// the look-up was most of the instructions: 170 us to read 2 x 64k tokens, 116 so.)  Bound by memory, the append of few bits by
+// its instructions too: a vector there is 32 channels of one group, so that its scale is found once, or 8 where groups are smaller.
 // Row and first vector of a warp.
 __device__ __forceinline__ bool warp_place(const RowParams& p, int* r, int* v_first) {
     const uint32_t w = (blockIdx.x * kRowThreads + threadIdx.x) >> 5, q = p.parts == 1 ? w : w / (uint32_t)p.parts;
@@ -122,16 +135,16 @@ __device__ __forceinline__ bool warp_place(const RowParams& p, int* r, int* v_fi
     *v_first = (int)(w - q * p.parts) * 32;
     return *r < p.b.n_rows;
 }
-// Element offset of vector `vec` inside a row of the caller's tensors.
-__device__ __forceinline__ long long row_element(const RowParams& p, int vec) {
-    const int e = vec * 8;
+// Element offset of channel e of a row (counted over its heads) inside a row of the caller's tensors.
+__device__ __forceinline__ long long row_element(const RowParams& p, int e) {
     if (p.rows.stride_head == p.c.D) return e;
     const int h = p.D_shift >= 0 ? e >> p.D_shift : e / p.c.D;
     return (long long)h * p.rows.stride_head + (e - h * p.c.D);
 }
 
-template <int TYPE, int KF, int VF>
+template <int TYPE, int KF, int VF, int CH>
 __global__ void __launch_bounds__(kRowThreads) cache_append_kernel(const __grid_constant__ RowParams p) {
+    constexpr int kBatch = CH == 8 ? 4 : 1;
     pdl_trigger();
     int r, v_first;
     if (!warp_place(p, &r, &v_first)) return;
@@ -141,15 +154,19 @@ __global__ void __launch_bounds__(kRowThreads) cache_append_kernel(const __grid_
     bool found = false;
     const int lane = threadIdx.x & 31, stride = 32 * p.parts;
     for (int v0 = v_first; v0 < p.vecs; v0 += stride * kBatch) {
-        uint4 kw[kBatch], vw[kBatch];
+        uint4 kw[kBatch][CH / 8], vw[kBatch][CH / 8];
 #pragma unroll
         for (int i = 0; i < kBatch; i++) {
             const int vec = v0 + stride * i + lane;
-            kw[i] = vw[i] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int q = 0; q < CH / 8; q++) kw[i][q] = vw[i][q] = make_uint4(0, 0, 0, 0);
             if (vec < p.vecs) {
-                const long long src = (long long)r * p.rows.stride_row + row_element(p, vec);
-                kw[i] = __ldg(reinterpret_cast<const uint4*>(p.rows.k + src));
-                vw[i] = __ldg(reinterpret_cast<const uint4*>(p.rows.v + src));
+                const long long src = (long long)r * p.rows.stride_row + row_element(p, vec * CH);
+#pragma unroll
+                for (int q = 0; q < CH / 8; q++) {
+                    kw[i][q] = __ldg(reinterpret_cast<const uint4*>(p.rows.k + src) + q);
+                    vw[i][q] = __ldg(reinterpret_cast<const uint4*>(p.rows.v + src) + q);
+                }
             }
         }
         if (v0 == v_first) found = find_slot<true>(p, r, lane == 0 && v_first == 0, &page, &slot);      // while the row is on its way
@@ -158,12 +175,12 @@ __global__ void __launch_bounds__(kRowThreads) cache_append_kernel(const __grid_
         for (int i = 0; i < kBatch; i++) {
             if (v0 + stride * i >= p.vecs) break;
             const int vec = v0 + stride * i + lane;
-            const uint32_t at = ((uint32_t)slot * p.vecs + vec) * 8;
+            const uint32_t at = ((uint32_t)slot * p.vecs + vec) * CH;
             const bool first = (vec & (p.seg - 1)) == 0;
             const uint32_t group = at >> p.G_shift;
-            encode8<TYPE, KF>(kw[i], page + (KF == FMT_INT8 ? at : at >> 1), first ? page + p.c.k_scales + 2 * group : nullptr, p.seg, vec < p.vecs);
-            encode8<TYPE, VF>(vw[i], page + p.c.v_codes + (VF == FMT_INT8 ? at : at >> 1), first ? page + p.c.v_scales + 2 * group : nullptr,
-                              p.seg, vec < p.vecs);
+            encode<TYPE, KF, CH>(kw[i], page + (KF == FMT_INT8 ? at : at >> 1), first ? page + p.c.k_scales + 2 * group : nullptr, p.seg, vec < p.vecs);
+            encode<TYPE, VF, CH>(vw[i], page + p.c.v_codes + (VF == FMT_INT8 ? at : at >> 1), first ? page + p.c.v_scales + 2 * group : nullptr,
+                                 p.seg, vec < p.vecs);
         }
     }
 }
@@ -208,6 +225,7 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
     int slot = 0;
     pdl_wait();
     if (!find_slot<false>(p, r, lane == 0 && v_first == 0, &page, &slot)) return;
+    constexpr int kBatch = 4;
     for (int v0 = v_first; v0 < p.vecs; v0 += stride * kBatch) {
         uint2 kc[kBatch], vc[kBatch];
         uint16_t ks[kBatch], vs[kBatch];
@@ -224,7 +242,7 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
         for (int i = 0; i < kBatch; i++) {
             const int vec = v0 + stride * i + lane;
             if (vec < p.vecs) {
-                const long long dst = (long long)r * p.rows.stride_row + row_element(p, vec);
+                const long long dst = (long long)r * p.rows.stride_row + row_element(p, vec * 8);
                 *reinterpret_cast<uint4*>(p.rows.k + dst) = decode8<TYPE, KF>(kc[i], half_bits_to_float(ks[i]));
                 *reinterpret_cast<uint4*>(p.rows.v + dst) = decode8<TYPE, VF>(vc[i], half_bits_to_float(vs[i]));
             }
@@ -334,7 +352,8 @@ namespace {
 
 template <int TYPE, int KF, int VF>
 cudaError_t launch_rows_fast(const RowParams& p, bool write, unsigned grid, cudaStream_t stream) {
-    return write ? launch_pdl(cache_append_kernel<TYPE, KF, VF>, dim3(grid), dim3(kRowThreads), 0, stream, p)
+    if (write && p.seg << 5 == p.c.G) return launch_pdl(cache_append_kernel<TYPE, KF, VF, 32>, dim3(grid), dim3(kRowThreads), 0, stream, p);
+    return write ? launch_pdl(cache_append_kernel<TYPE, KF, VF, 8>, dim3(grid), dim3(kRowThreads), 0, stream, p)
                  : launch_pdl(cache_read_kernel<TYPE, KF, VF>, dim3(grid), dim3(kRowThreads), 0, stream, p);
 }
 template <int TYPE>
@@ -366,8 +385,9 @@ int cache_rows(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, const p
     const int gs = log2_exact(g->group);
     const bool fast = g->head_dim % 8 == 0 && gs >= 3 && gs <= 8 && elems % 32 == 0 && (elems / g->group) % 8 == 0 &&
                       ((ka | va) & 15) == 0 && rows->stride_row % 8 == 0 && rows->stride_head % 8 == 0;
-    p.vecs = (int)((long long)g->n_kv_heads * g->head_dim / 8);
-    p.seg = g->group / 8;
+    const int channels = write && g->group % 32 == 0 ? 32 : 8;         // of a vector
+    p.vecs = (int)((long long)g->n_kv_heads * g->head_dim / channels);
+    p.seg = g->group / channels;
     p.G_shift = gs; p.D_shift = log2_exact(g->head_dim);
     // Few rows: a warp for every 32 vectors of a row (8 rows of 128 vectors, append and read: 7.2 us in one warp each, 4.7 in four).
     const int groups = (p.vecs + 31) / 32;
