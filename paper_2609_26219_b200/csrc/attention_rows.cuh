@@ -557,13 +557,16 @@ struct RowsKernel {
         return bad ? __uint_as_float(0x7FC00000u) : p.scale_log2 * exp2i(-shift);
     }
 
-    // 2^y for two y <= 2^7 on the fma pipe: y = n + f with n whole and |f| <= 1/2, 2^f by a polynomial (fitted for the least relative
-    // error on that interval: 2.6e-6), times 2^n put together as bits.  Below -126 the result is about 2^-126; NaN stays NaN.
+    // 2^y for two y on the fma pipe: y = n + f with n whole and |f| <= 1/2, 2^f by a polynomial (fitted for the least relative
+    // error on that interval: 2.6e-6), times 2^n put together as bits.  Below -126 the result is about 2^-126, above 126 (a row that has
+    // had no token yet: its reference is far below all logits) 2^126, which the check behind finds; NaN stays NaN.
     __device__ __forceinline__ static void exp2_pair(f32x2 y2, float& a, float& b) {
         float u, v;
         unpack2(y2, u, v);
         asm("max.NaN.f32 %0, %0, %1;" : "+f"(u) : "f"(-126.0f));
         asm("max.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(-126.0f));
+        asm("min.NaN.f32 %0, %0, %1;" : "+f"(u) : "f"(126.0f));
+        asm("min.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(126.0f));
         const f32x2 y = pack2(u, v), magic = pack2(12582912.0f, 12582912.0f);       // 1.5 * 2^23
         const f32x2 t = add2(y, magic), f = sub2(y, sub2(t, magic));
         f32x2 e = fma2(f, pack2(0.009570097550749779f, 0.009570097550749779f), pack2(0.05591786280274391f, 0.05591786280274391f));

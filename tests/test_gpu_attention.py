@@ -74,7 +74,10 @@ class Setup:
 
     def workspace(self, window=0, sinks=0):
         n = self.pk.attention_workspace_bytes(self.geom, self.cache, self.batch, self.q.shape[1], window, sinks)
-        return torch.randint(0, 256, (max(n, 16),), dtype=torch.uint8, device=DEV)
+        whole = torch.randint(0, 256, (max(n, 16) + 4096,), dtype=torch.uint8, device=DEV)
+        whole[max(n, 16):] = 0xA5
+        self.behind = whole[max(n, 16):]
+        return whole[:max(n, 16)]
 
     def run(self, ctx, window=0, sinks=0, scale=None, q=None, out=None, **kw):
         q = self.q.to(DEV) if q is None else q
@@ -99,6 +102,8 @@ class Setup:
     def check(self, ctx, window=0, sinks=0, scale=None, **kw):
         out = self.run(ctx, window, sinks, scale, **kw)
         assert ctx.query_status() == 0
+        if hasattr(self, "behind"):
+            assert (self.behind == 0xA5).all()           # nothing is written behind the workspace
         want, tol = self.reference(window, sinks, scale)
         n = want.shape[0]
         got = out[:n].double().cpu().numpy()
@@ -121,8 +126,10 @@ BATCHES = {
     "scattered": Case([500, 100], [20, 4], [[0, 1, 15, 16, 17, 63, 64, 65, 127, 128, 129, 200, 255, 256, 300, 301, 302, 303, 498, 499],
                                           [99, 0, 50, 99]]),
     "more_rows_than_tokens": Case([5], [9]),
+    "scattered_many": Case([700, 300], [150, 90], [[(i * 37) % 700 for i in range(150)], [(i * 11) % 300 for i in range(90)]]),
 }
-MASKS = {"causal": (0, 0), "window": (37, 0), "sinks": (100, 4), "one": (1, 0), "sinks_over": (16, 50)}
+MASKS = {"causal": (0, 0), "window": (37, 0), "sinks": (100, 4), "one": (1, 0), "sinks_over": (16, 50),
+         "wide": (2 ** 31 - 1, 2 ** 31 - 1)}
 
 
 @pytest.mark.parametrize("tag", TAGS)
@@ -518,3 +525,97 @@ def test_refusals(pk, ctx):
     assert call(args(), batch=none) == 0
     torch.cuda.synchronize()
     assert ctx.query_status() == 0 and (out == 5).all()
+
+
+@pytest.mark.parametrize("tag", [0, 1, 3])
+@pytest.mark.parametrize("n_seqs", [33, 100, 400])
+def test_many_sequences(pk, ctx, tag, n_seqs):
+    """More sequences than a warp has lanes, than SMs, and than pieces are worth."""
+    rng = np.random.default_rng(n_seqs)
+    kv = [int(x) for x in rng.integers(0, 90, n_seqs)]
+    kv[n_seqs // 2] = 3000
+    rows = [int(x) for x in rng.integers(0, 3, n_seqs)]
+    Setup(pk, tag, 1, 2, 64, 16, 32, Case(kv, rows)).check(ctx, 200, 3)
+
+
+@pytest.mark.parametrize("tag", TAGS)
+@pytest.mark.parametrize("rows", [1, 30, 200])
+def test_pages_behind_the_window_may_be_gone(pk, ctx, tag, rows):
+    """Table entries of tokens that no row sees may be anything; nothing is read there and nothing latched."""
+    s = Setup(pk, tag, 2, 4, 64, 16, 32, Case([900], [rows]))
+    first = (900 - rows - 100 + 1) // 16                 # page of the first token in the earliest row's window
+    s.keep["table"][0, 1:first] = torch.arange(first - 1, dtype=torch.int32, device=DEV) * -7 - 1
+    s.check(ctx, 100, 5)
+
+
+@pytest.mark.parametrize("tag", TAGS)
+@pytest.mark.parametrize("rows", [1, 30, 200])
+def test_a_broken_query_spoils_only_itself(pk, ctx, tag, rows):
+    s = Setup(pk, tag, 2, 4, 64, 16, 32, Case([300, 0], [rows, rows]))
+    good, tol = s.reference()
+    s.q[0, 1, 3], s.q[rows - 1, 2, 60], s.q[rows, 0, 0] = float("nan"), float("inf"), float("nan")
+    out = s.run(ctx)
+    assert ctx.query_status() == 0
+    got = out.double().cpu().numpy()
+    assert np.isnan(got[0, 1]).all() and not np.isfinite(got[rows - 1, 2]).any()
+    for r, h in ((0, 1), (rows - 1, 2)):
+        got[r, h] = good[r, h]
+    assert np.all(np.abs(got - good) <= tol)             # the second sequence has no tokens: zeros, whatever its queries
+
+
+def test_two_graphs_with_workspaces_of_their_own(pk, ctx):
+    s = [Setup(pk, 3, 2, 8, 128, 16, 32, Case([3000], [r]), seed=r) for r in (1, 90)]
+    q = [x.q.to(DEV) for x in s]
+    out, ws, graphs = [torch.zeros_like(x) for x in q], [x.workspace() for x in s], []
+    for i in (0, 1):
+        s[i].run(ctx, q=q[i], out=out[i], workspace=ws[i])
+        g = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g):
+            ctx.attention(s[i].geom, s[i].cache, 0, s[i].batch, q[i], out[i], workspace=ws[i])
+        graphs.append(g)
+    want = [x.clone() for x in out]
+    streams = [torch.cuda.Stream() for _ in s]
+    for _ in range(10):
+        for g, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                g.replay()
+    torch.cuda.synchronize()
+    assert ctx.query_status() == 0
+    assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
+
+
+def test_first_call_of_a_process_may_be_captured():
+    """Nothing of the calls has to be warmed up outside a capture: a fresh process captures its first ones."""
+    import subprocess
+    import sys
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = """
+import torch
+from paper_2609_26219_b200 import binding as pk
+dev = "cuda:0"
+ctx = pk.Context(device=0)
+g = pk.make_geom(1, 2, 64, 64, pk.ROPE_HALF, 1e4, 16, 16, 32)
+pages = torch.zeros((64, pk.record_bytes(3, 16, 2, 64, 32)), dtype=torch.uint8, device=dev)
+cache = pk.make_qpool(pages, 3, 64)
+for rows in (1, 40, 300):
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=dev)
+    b = dict(row_start=i32([0, rows]), kv_len=i32([700]), block_table=torch.arange(64, dtype=torch.int32, device=dev)[None], n_rows=rows, max_rows=rows, max_kv_len=700)
+    batch = pk.make_batch(**b)
+    k = torch.ones((rows, 2, 64), dtype=torch.bfloat16, device=dev)
+    q = torch.ones((rows, 4, 64), dtype=torch.bfloat16, device=dev)
+    out = torch.zeros_like(q)
+    ws = torch.empty(max(16, pk.attention_workspace_bytes(g, cache, batch, 4)), dtype=torch.uint8, device=dev)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        ctx.cache_append(g, cache, 0, batch, k, k)
+        ctx.attention(g, cache, 0, batch, q, out, workspace=ws)
+    graph.replay()
+    assert ctx.query_status() == 0
+    assert torch.isfinite(out).all() and float(out[0].float().mean()) > 0
+print("ok")
+"""
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip().endswith("ok"), r.stderr[-2000:]
