@@ -15,7 +15,7 @@
 // 6000 cycles a step, three times what the products take.  Where one CTA is all there is, its own four warps convert (bf16
 // pages: cp.async), and the cache is read once, as it is.  Queries over quantised pages are fp16 scaled by a power of two per
 // row, so a bf16 query loses nothing.  The weights are fp16 there, bf16 over bf16 pages; sums are fp32 throughout.
-// As in the split kernel the softmax reference is only moved (and O rescaled) when a logit exceeds it by more than 8.
+// As in the split kernel the softmax reference is only moved (and O rescaled) when a logit exceeds it by more than 15.
 #pragma once
 
 #include <stddef.h>
@@ -25,6 +25,7 @@
 namespace patchkv {
 
 constexpr int kRowTile = 128;                   // query vectors of a tile, and tokens of a step
+constexpr float kTop = kSplitTop, kPeak = kSplitPeak;
 constexpr int kProducer0 = 256;                 // two softmax warpgroups, then the warps that bring K and V (four, or one that copies
 __host__ __device__ constexpr int rows_issuer(bool image) { return image ? 288 : 384; }             // images), then the issuing warp
 __host__ __device__ constexpr int rows_threads(bool image) { return rows_issuer(image) + 32; }
@@ -645,8 +646,9 @@ struct RowsKernel {
                 tc_wait_st();
             }
             // Weights are made against the reference as it stands, and checked: nothing is stored before it is known that none exceeds
-            // 2^8.  Else (a row's first step, and rarely) the largest logits are found, the references of the warp's rows moved to
-            // 4 above them (so that it is rare), and the weights made again.
+            // 2^15.  Else (a row's first step, and rarely) the largest logits are found, the references of the warp's rows moved to
+            // 8 below them, and the weights made again.  (fp16 then holds weights down to 2^-22 of the largest to all its bits; the
+            // many small weights of a long context matter: with a largest weight of 2^-4 its error was 7.7e-4 instead of 4e-4.)
             uint32_t w[64];
             f32x2 total;
             bool search = j == 0;
@@ -661,7 +663,7 @@ struct RowsKernel {
 #pragma unroll
                         for (int c = 0; c < 16; c++) y = fmaxf(y, __uint_as_float(x[c]) * factor);
                     }
-                    const float to = y > ref + 8.0f ? y + 4.0f : ref, keep = fast_exp2(ref - to);
+                    const float to = y > ref + kTop ? y - kPeak : ref, keep = fast_exp2(ref - to);
                     ref = to;
                     sum2 = mul2(sum2, pack2(keep, keep));
                     if (j > 0)                                  // the products of the steps before are done: s_ready came behind them
@@ -705,7 +707,7 @@ struct RowsKernel {
 #pragma unroll
                 for (int c = 0; c < 64; c++) most[c & 3] = __vmaxu2(most[c & 3], w[c]);
                 const uint32_t top = __vmaxu2(__vmaxu2(most[0], most[1]), __vmaxu2(most[2], most[3]));
-                constexpr uint32_t kLimit = kPool ? 0x4380u : 0x5C00u;                  // 2^8
+                constexpr uint32_t kLimit = kPool ? 0x4700u : 0x7800u;                  // 2^15
                 search = __any_sync(0xFFFFFFFFu, max(top & 0xFFFFu, top >> 16) > kLimit);
                 if (!search) break;
             }
@@ -721,7 +723,7 @@ struct RowsKernel {
         float sum, sum_odd;
         unpack2(sum2, sum, sum_odd);
         sum += sum_odd;
-        // (A row that sees a token has a weight of 2^-4 at least; what it does not see weighs up to 2^-126 in the computed pairs.)
+        // (A row that sees a token has a weight of 2^8 and more; what it does not see weighs up to 2^-126 in the computed pairs.)
         if (sum < 1.0e-30f) sum = 0.0f;
         if (broken && sum != 0.0f) sum = __uint_as_float(0x7FC00000u);
         const bool lost = IMAGE ? lost_seen != 0 : *reinterpret_cast<volatile int32_t*>(&bars.lost) != 0;

@@ -15,8 +15,8 @@
 //      the chunk's q), then enters the logit with the token's fp32 scale: no rounding of K at all.
 //   V: v = (u * 2^-24) * S - offset * S in one half fma, S the token's scale times a power of two that follows the
 //      largest V scale seen: one rounding of 2^-12, as p's own to fp16.
-// Softmax on powers of two against a reference that is only moved when a logit exceeds it by more than 8 (p <= 256): one
-// vote per tile instead of a maximum across lanes.
+// Softmax on powers of two against a reference that is only moved when a logit exceeds it by more than 15 (p <= 2^15), to 8 below
+// the largest (fp16 then holds weights down to 2^-22 of it to all its bits): one vote per tile instead of a maximum across lanes.
 #pragma once
 
 #include "attention.cuh"
@@ -25,6 +25,7 @@ namespace patchkv {
 
 constexpr int kTile = 16;                       // tokens a warp takes at a time: one mma K (M) step
 constexpr float kNoMax = -3.0e38f;
+constexpr float kSplitTop = 15.0f, kSplitPeak = 8.0f;   // logits reach that far above the reference at most; it is put that far below the largest
 
 // What the combine kernel needs of a split launch, and where partial results lie.
 struct SplitPlan {
@@ -464,14 +465,14 @@ struct SplitKernel {
             top = max(mag & 0xFFFFu, mag >> 16);
         }
         // One vote for the two references that may have to move.
-        if (__any_sync(0xFFFFFFFFu, most > 8.0f || (!kPool && top >= v_most))) {
+        if (__any_sync(0xFFFFFFFFu, most > kSplitTop || (!kPool && top >= v_most))) {
 #pragma unroll
             for (int c = 0; c < NC; c++) {
                 float m = fmaxf(x[c][0], x[c][1]);
                 m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 4));
                 m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
                 m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
-                if (m > ref[c] + 8.0f) rescale(c, m);
+                if (m > ref[c] + kSplitTop) rescale(c, m - kSplitPeak);
             }
             if constexpr (!kPool) {
                 uint32_t m = top >= 0x7C00u ? 0u : top;             // a scale that is not finite always gets here
