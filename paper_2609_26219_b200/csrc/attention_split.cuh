@@ -232,8 +232,8 @@ struct SplitKernel {
         v_most = (uint32_t)(30 - e) << 10;                   // exponent field x: s < 2^(x - 14), so s * 2^e stays at 2^15 at most
     }
 
-    // Queries as B operands, and the per-column numbers of the lane's logit columns.
-    __device__ __forceinline__ void load_queries(int first, int cols, int head, uint32_t share_magic) {
+    // Asks for the queries: 32-bit words of column n = column_of(2 nt + (g & 1), g / 2), into the operands' own registers.
+    __device__ __forceinline__ void ask_queries(int first, int cols, int head, uint32_t share_magic) {
 #pragma unroll
         for (int nt = 0; nt < NT; nt++) {
             const int n = column_of(2 * nt + (g & 1), g >> 1), row = (int)(n * share_magic >> 16);
@@ -244,12 +244,9 @@ struct SplitKernel {
                 for (int k = 0; k < kMT; k++)
 #pragma unroll
                     for (int e = 0; e < 2; e++) qf[nt][k][e] = live ? __ldg(reinterpret_cast<const uint32_t*>(q + 16 * k + 8 * e + 2 * t)) : 0u;
-                factor[2 * nt] = p.scale_log2;
-                if (NC > 1) factor[2 * nt + (NC > 1)] = p.scale_log2;
             } else {
-                uint32_t w[kChunks][4];                       // 8 channels of each chunk, in the order the codes of a word come out
 #pragma unroll
-                for (int j = 0; j < kChunks; j++) {
+                for (int j = 0; j < kChunks; j++) {           // 8 channels of each chunk, in the order the codes of a word come out
                     uint4 v = make_uint4(0, 0, 0, 0);
                     if (live) {
                         if (kK4) {
@@ -260,7 +257,23 @@ struct SplitKernel {
                             v = make_uint4(a.x, a.y, b.x, b.y);
                         }
                     }
-                    w[j][0] = v.x; w[j][1] = v.y; w[j][2] = v.z; w[j][3] = v.w;
+                    qf[nt][2 * j][0] = v.x; qf[nt][2 * j][1] = v.y; qf[nt][2 * j + 1][0] = v.z; qf[nt][2 * j + 1][1] = v.w;
+                }
+            }
+        }
+    }
+    // Queries as B operands, and the per-column numbers of the lane's logit columns.
+    __device__ __forceinline__ void load_queries() {
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++) {
+            if constexpr (kPool) {
+                factor[2 * nt] = p.scale_log2;
+                if (NC > 1) factor[2 * nt + (NC > 1)] = p.scale_log2;
+            } else {
+                uint32_t w[kChunks][4];
+#pragma unroll
+                for (int j = 0; j < kChunks; j++) {
+                    w[j][0] = qf[nt][2 * j][0]; w[j][1] = qf[nt][2 * j][1]; w[j][2] = qf[nt][2 * j + 1][0]; w[j][3] = qf[nt][2 * j + 1][1];
                 }
                 // Largest magnitude (ordered as the bit patterns are) into [2^13, 2^14); zeros as they are.  A column with a NaN or an
                 // infinity has no result but NaN: its factor is NaN.
@@ -644,6 +657,20 @@ __device__ __forceinline__ Item find_item(const AttentionParams& p, const SplitP
     it.splits = 1; it.split = 0; it.first_item = item;
     if (pl.target == 0) {
         it.seq = item;
+    } else if (p.b.n_seqs == 1) {                            // no search
+        int lo, hi;
+        it.seq = 0;
+        if (!sequence_rows(p, 0, &it.first, &it.kv, &it.rows)) { if (lane == 0 && item == 0) latch(p.status); return it; }
+        if (it.rows == 0) return it;
+        position_range(p, 0, it.first, it.rows, &lo, &hi);
+        const int tiles = tile_range(p, it.kv, lo, hi).count;
+        const int piece = max((int)((uint32_t)(tiles + pl.target - 1) / (uint32_t)pl.target), 1 << pl.per_head_log2);
+        it.splits = max(1, (int)((uint32_t)(tiles + piece - 1) / (uint32_t)piece));
+        if (item >= it.splits) return it;
+        it.split = item;
+        it.first_item = 0;
+        it.begin = item * piece;
+        it.end = it.begin + piece;
     } else {
         // tiles of sequence s0 + lane; -1 for one without rows
         auto tiles_of = [&](int s0) {
@@ -722,6 +749,7 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
     K k(p);
     k.start(lane, smem_u32(smem) + warp * STAGES * K::kStage, smem_u32(smem) + WARPS * STAGES * K::kStage + warp * K::kCold);
     if (live) {
+        k.ask_queries(it.first, cols, head, pl.share_magic);
         const int step = 1 << pl.per_head_log2, n = it.begin + sub < it.end ? (it.end - it.begin - sub + step - 1) >> pl.per_head_log2 : 0;
         uint32_t* cold = reinterpret_cast<uint32_t*>(smem + WARPS * STAGES * K::kStage + warp * K::kCold);
         if (lane == 0) {
@@ -772,7 +800,7 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
         };
 #pragma unroll 1
         for (int i = 0; i < STAGES - 1; i++) fetch(i);
-        k.load_queries(it.first, cols, head, pl.share_magic);
+        k.load_queries();
 #pragma unroll 1
         for (int i = 0; i < n; i++) {
             fetch(i + STAGES - 1);
