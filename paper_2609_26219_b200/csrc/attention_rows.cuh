@@ -647,8 +647,10 @@ struct RowsKernel {
             }
             // Weights are made against the reference as it stands, and checked: nothing is stored before it is known that none exceeds
             // 2^15.  Else (a row's first step, and rarely) the largest logits are found, the references of the warp's rows moved to
-            // 8 below them, and the weights made again.  (fp16 then holds weights down to 2^-22 of the largest to all its bits; the
-            // many small weights of a long context matter: with a largest weight of 2^-4 its error was 7.7e-4 instead of 4e-4.)
+            // 3 below them, and the weights made again.  fp16 then holds weights down to 2^-17 of the largest to all its bits (the many
+            // small weights of a long context matter: with a largest weight of 2^-4 fp16 results were 7.7e-4 off, 7.0e-4
+            // so, what is left being K's rounding), and a logit may still grow by 12: a step made twice costs 4500 cycles, and at 8
+            // below prompt_8k took 566 us instead of 517.
             uint32_t w[64];
             f32x2 total;
             bool search = j == 0;
@@ -723,7 +725,7 @@ struct RowsKernel {
         float sum, sum_odd;
         unpack2(sum2, sum, sum_odd);
         sum += sum_odd;
-        // (A row that sees a token has a weight of 2^8 and more; what it does not see weighs up to 2^-126 in the computed pairs.)
+        // (A row that sees a token has a weight of 2^3 and more; what it does not see weighs up to 2^-126 in the computed pairs.)
         if (sum < 1.0e-30f) sum = 0.0f;
         if (broken && sum != 0.0f) sum = __uint_as_float(0x7FC00000u);
         const bool lost = IMAGE ? lost_seen != 0 : *reinterpret_cast<volatile int32_t*>(&bars.lost) != 0;

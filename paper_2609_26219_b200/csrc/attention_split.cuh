@@ -15,8 +15,8 @@
 //      the chunk's q), then enters the logit with the token's fp32 scale: no rounding of K at all.
 //   V: v = (u * 2^-24) * S - offset * S in one half fma, S the token's scale times a power of two that follows the
 //      largest V scale seen: one rounding of 2^-12, as p's own to fp16.
-// Softmax on powers of two against a reference that is only moved when a logit exceeds it by more than 15 (p <= 2^15), to 8 below
-// the largest (fp16 then holds weights down to 2^-22 of it to all its bits): one vote per tile instead of a maximum across lanes.
+// Softmax on powers of two against a reference that is only moved when a logit exceeds it by more than 15 (p <= 2^15), to 3 below
+// the largest (fp16 then holds weights down to 2^-17 of it to all its bits): one vote per tile instead of a maximum across lanes.
 #pragma once
 
 #include "attention.cuh"
@@ -25,7 +25,7 @@ namespace patchkv {
 
 constexpr int kTile = 16;                       // tokens a warp takes at a time: one mma K (M) step
 constexpr float kNoMax = -3.0e38f;
-constexpr float kSplitTop = 15.0f, kSplitPeak = 8.0f;   // logits reach that far above the reference at most; it is put that far below the largest
+constexpr float kSplitTop = 15.0f, kSplitPeak = 3.0f;   // logits reach that far above the reference at most; it is put that far below the largest
 
 // What the combine kernel needs of a split launch, and where partial results lie.
 struct SplitPlan {
