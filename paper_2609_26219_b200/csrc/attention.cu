@@ -258,9 +258,9 @@ cudaError_t launch_split_columns(const AttentionParams& p, const SplitPlan& pl, 
     return nc == 1 ? launch_split_group<D, 1>(p, pl, groups, s) : nc == 2 ? launch_split_group<D, 2>(p, pl, groups, s) : launch_split_group<D, 4>(p, pl, groups, s);
 }
 
-template <int KF, int VF, int D, bool IMAGE>
+template <int KF, int VF, int D, bool IMAGE, bool ONE>
 cudaError_t launch_rows_kernel(const AttentionParams& p, const RowsPlan& pl, cudaStream_t stream) {
-    auto kernel = attention_rows_kernel<KF, VF, D, IMAGE>;
+    auto kernel = attention_rows_kernel<KF, VF, D, IMAGE, ONE>;
     static std::atomic<uint64_t> allowed{0};
     const cudaError_t e = allow_smem((const void*)kernel, RowsSmem<D>::kLaunch, &allowed);
     if (e != cudaSuccess) return e;
@@ -273,9 +273,10 @@ cudaError_t launch_rows(const AttentionParams& p, const RowsPlan& pl, cudaStream
         e = launch_pdl(attention_image_kernel<KF, VF, D>, dim3(pl.steps, p.c.H, p.b.n_seqs), dim3(kImageThreads), 0, stream, p, pl);
         if (e != cudaSuccess) return e;
         constexpr int F = KF == FMT_BF16 ? FMT_BF16 : FMT_INT8;
-        e = launch_rows_kernel<F, F, D, true>(p, pl, stream);
+        e = launch_rows_kernel<F, F, D, true, false>(p, pl, stream);
     } else {
-        e = launch_rows_kernel<KF, VF, D, false>(p, pl, stream);
+        e = (long long)std::min(p.b.max_rows, p.b.n_rows) * p.share <= kRowTile ? launch_rows_kernel<KF, VF, D, false, true>(p, pl, stream)
+                                                                                : launch_rows_kernel<KF, VF, D, false, false>(p, pl, stream);
     }
     if (e != cudaSuccess || pl.splits == 1) return e;
     return launch_pdl(attention_rows_join_kernel<D>, dim3((unsigned)(((long long)p.b.n_rows * p.Hq + 3) / 4)), dim3(128), 0, stream, p, pl);

@@ -268,14 +268,16 @@ struct RowsKernel {
     __device__ __forceinline__ bool whole(int t0) const { return whole_step(p, kv, lo, hi, t0); }
 
     // ---- the warps that bring K and V
-    // A warp takes 32 tokens of a step; kPer lanes share a token, 32 / kPer tokens at a time (a pass).
-    static constexpr int kTok = 32 / kPer, kPass = kPer;
+    // A warp takes TOK = 32 tokens of a step, or 16 where a call has one tile only and the second tile's softmax warps bring too; kPer lanes share a
+    // token, 32 / kPer tokens at a time (a pass).
+    static constexpr int kTok = 32 / kPer;
     struct Pages { int page, t0; };                             // lane 0: page of the warp's first 16 tokens, lane 1: of the other 16
 
     // Address of the thread's token of pass i (quantised: its page, and its row in *row); live: some row sees it and it has a page.
+    template <int TOK>
     __device__ __forceinline__ long long token_at(const Pages& g, int tok, uint32_t* row, bool* live) const {
-        const int w32 = tok & ~31, t = g.t0 + tok;
-        const int page = __shfl_sync(0xFFFFFFFFu, g.page, (tok - w32) >> 4);
+        const int t = g.t0 + tok;
+        const int page = __shfl_sync(0xFFFFFFFFu, g.page, TOK == 16 ? 0 : tok >> 4 & 1);
         const int slot = t - div_page(p.c, t) * p.c.P;
         *live = page >= 0 && any_sees(t);
         *row = (uint32_t)slot * p.c.H + head;
@@ -283,18 +285,19 @@ struct RowsKernel {
         return (long long)page * p.c.stride_page + (kPool ? (long long)slot * p.c.stride_token + (long long)head * p.c.stride_head : 0ll);
     }
     // Tokens of the warp that some row sees but whose page is out of range.
+    template <int TOK>
     __device__ __forceinline__ uint32_t missing(const Pages& g, int w) const {
         const int lane = threadIdx.x & 31, page = __shfl_sync(0xFFFFFFFFu, g.page, lane >> 4);
-        const uint32_t gone = __ballot_sync(0xFFFFFFFFu, page < 0 && any_sees(g.t0 + 32 * w + lane));
+        const uint32_t gone = __ballot_sync(0xFFFFFFFFu, lane < TOK && page < 0 && any_sees(g.t0 + TOK * w + lane));
         if (gone && lane == 0) latch(p.status);
         return gone;
     }
     // The thread's 32 channels of pass i, K or V: codes and their scale.
-    template <int F>
+    template <int F, int TOK>
     __device__ __forceinline__ void load_piece(const Pages& g, int tok, int c, bool is_v, uint32_t (&w)[8], uint32_t& scale) const {
         uint32_t row;
         bool live;
-        const uint8_t* pg = p.c.base + token_at(g, tok, &row, &live);
+        const uint8_t* pg = p.c.base + token_at<TOK>(g, tok, &row, &live);
 #pragma unroll
         for (int i = 0; i < 8; i++) w[i] = 0;
         scale = 0;
@@ -344,27 +347,32 @@ struct RowsKernel {
         }
     }
 
-    __device__ __forceinline__ void produce() {
-        const int w = (threadIdx.x - kProducer0) >> 5, lane = threadIdx.x & 31;
-        const int c = lane % kPer, tok0 = 32 * w + lane / kPer;
+    template <int TOK>
+    __device__ __forceinline__ void produce(int w) {
+        constexpr int kPass = TOK / kTok;
+        const int lane = threadIdx.x & 31;
+        const int c = lane % kPer, tok0 = TOK * w + lane / kPer;
         uint32_t m0, m1;                                        // 1024 + 8 and 1024 + 8 * 16 in every half: magic and offset
         asm volatile("mov.b32 %0, 0x64086408;" : "=r"(m0));
         asm volatile("mov.b32 %0, 0x64806480;" : "=r"(m1));
         if (begin >= end) return;
-        auto pages_of = [&](int j) { return Pages{page_of(j, 32 * w + (lane & 1) * 16), j < end ? range.tile(j) * kRowTile : 0}; };
+        auto pages_of = [&](int j) { return Pages{page_of(j, TOK * w + (TOK == 32 ? (lane & 1) * 16 : 0)), j < end ? range.tile(j) * kRowTile : 0}; };
         Pages now = pages_of(begin), next = pages_of(begin + 1);
         // One set of registers for the codes in flight: as soon as K's have become operands V's are asked for, then the next K's.
         uint32_t code[kPass][8], scale[kPass];
         if constexpr (!kPool)
 #pragma unroll
-            for (int i = 0; i < kPass; i++) load_piece<KF>(now, tok0 + i * kTok, c, false, code[i], scale[i]);
+            for (int i = 0; i < kPass; i++) load_piece<KF, TOK>(now, tok0 + i * kTok, c, false, code[i], scale[i]);
 #pragma unroll 1
         for (int j = begin; j < end; j++) {
             const int n = j - begin, st = n & 1;
             const uint32_t parity = ((n >> 1) & 1) ^ 1;
             const bool masked = !whole(now.t0);
-            const uint32_t gone = missing(now, w);
-            if (lane == 0) bars.absent[n & 3][w] = gone;
+            const uint32_t gone = missing<TOK>(now, w);
+            if (lane == 0) {
+                if (TOK == 32) bars.absent[n & 3][w] = gone;
+                else reinterpret_cast<uint16_t*>(bars.absent[n & 3])[w] = (uint16_t)gone;
+            }
             const uint32_t kb = smem + S::kK + st * S::kMat, vb = smem + S::kV + st * S::kMat;
             if (!wait_warp(&bars.k_empty[st], parity)) return;
             if constexpr (kPool) {
@@ -374,7 +382,7 @@ struct RowsKernel {
                     for (int i = 0; i < kPass; i++) {
                         uint32_t row;
                         bool live;
-                        const uint16_t* x = from + token_at(now, tok0 + i * kTok, &row, &live) + 8 * c;
+                        const uint16_t* x = from + token_at<TOK>(now, tok0 + i * kTok, &row, &live) + 8 * c;
 #pragma unroll
                         for (int q = 0; q < 4; q++) cp16(mat + swizzled(tok0 + i * kTok, q * kPer + c), live ? x + 8 * q * kPer : from, live);
                     }
@@ -387,12 +395,12 @@ struct RowsKernel {
                 fence_async_smem();
                 mbar_arrive(&bars.k_full[st]);
                 cp_wait<0>();
-                if (masked) clean<0x7F80u>(vb, tok0, c, 1, kPer);
+                if (masked) clean<0x7F80u, kPass>(vb, tok0, c, 1, kPer);
             } else {
 #pragma unroll
                 for (int i = 0; i < kPass; i++) {
                     store_operands<KF>(kb, tok0 + i * kTok, c, code[i], scale[i], m0, m1);
-                    load_piece<VF>(now, tok0 + i * kTok, c, true, code[i], scale[i]);
+                    load_piece<VF, TOK>(now, tok0 + i * kTok, c, true, code[i], scale[i]);
                 }
                 fence_async_smem();
                 mbar_arrive(&bars.k_full[st]);
@@ -400,9 +408,9 @@ struct RowsKernel {
 #pragma unroll
                 for (int i = 0; i < kPass; i++) {
                     store_operands<VF>(vb, tok0 + i * kTok, c, code[i], scale[i], m0, m1);
-                    load_piece<KF>(next, tok0 + i * kTok, c, false, code[i], scale[i]);
+                    load_piece<KF, TOK>(next, tok0 + i * kTok, c, false, code[i], scale[i]);
                 }
-                if (masked) clean<0x7C00u>(vb, tok0, c, 4, 1);
+                if (masked) clean<0x7C00u, kPass>(vb, tok0, c, 4, 1);
             }
             fence_async_smem();
             mbar_arrive(&bars.v_full[st]);
@@ -420,10 +428,10 @@ struct RowsKernel {
     }
     // In a step that needs a mask a value that is not finite must not meet the weight 0 of a row that does not see it: it is taken out
     // here and given to the rows that see it at the end.  Chunks of the thread: c * lead + q * apart, q = 0 .. 3.
-    template <uint32_t EXP>
+    template <uint32_t EXP, int PASSES>
     __device__ __forceinline__ void clean(uint32_t mat, int tok0, int c, int lead, int apart) {
 #pragma unroll 1
-        for (int i = 0; i < kPer * 4; i++) {
+        for (int i = 0; i < PASSES * 4; i++) {
             const uint32_t a = mat + swizzled(tok0 + (i >> 2) * (32 / kPer), c * lead + (i & 3) * apart);
             uint4 x = lds128(a);
             if (finite_only<EXP>(x)) { sts128(a, x.x, x.y, x.z, x.w); bars.lost = 1; }
@@ -650,7 +658,7 @@ struct RowsKernel {
             // 3 below them, and the weights made again.  fp16 then holds weights down to 2^-17 of the largest to all its bits (the many
             // small weights of a long context matter: with a largest weight of 2^-4 fp16 results were 7.7e-4 off, 7.0e-4
             // so, what is left being K's rounding), and a logit may still grow by 12: a step made twice costs 4500 cycles, and at 8
-            // below prompt_8k took 566 us instead of 517.
+            // below 8192 rows over 8192 tokens (32 query heads) took 566 us instead of 517.
             uint32_t w[64];
             f32x2 total;
             bool search = j == 0;
@@ -791,7 +799,8 @@ struct RowsKernel {
     }
 };
 
-template <int KF, int VF, int D, bool IMAGE>
+// ONE: no sequence has more than one tile of vectors; the second tile's warps then help to bring K and V.
+template <int KF, int VF, int D, bool IMAGE, bool ONE>
 __global__ void __launch_bounds__(rows_threads(IMAGE), 1) attention_rows_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ RowsPlan pl) {
     using K = RowsKernel<KF, VF, D, IMAGE>;
     using S = RowsSmem<D>;
@@ -805,7 +814,7 @@ __global__ void __launch_bounds__(rows_threads(IMAGE), 1) attention_rows_kernel(
         for (int i = 0; i < 2; i++) {
             mbar_init(&bars.q_ready[i], 4); mbar_init(&bars.p_ready[i], 4);          // the four warps of a tile
             mbar_init(&bars.s_ready[i], 1); mbar_init(&bars.o_ready[i], 1);
-            mbar_init(&bars.k_full[i], IMAGE ? 1 : 128); mbar_init(&bars.v_full[i], IMAGE ? 1 : 128);
+            mbar_init(&bars.k_full[i], IMAGE ? 1 : ONE ? 256 : 128); mbar_init(&bars.v_full[i], IMAGE ? 1 : ONE ? 256 : 128);
             mbar_init(&bars.k_empty[i], 1); mbar_init(&bars.v_empty[i], 1);
         }
         mbar_init(&bars.drained, 1);
@@ -826,6 +835,7 @@ __global__ void __launch_bounds__(rows_threads(IMAGE), 1) attention_rows_kernel(
     rows = min(rows, p.b.max_rows);
     const int m0 = tile * 2 * kRowTile, m_end = min(rows * p.share, m0 + 2 * kRowTile);
     if (m0 >= m_end) return;
+    const int tiles = !ONE && m_end - m0 > kRowTile ? 2 : 1;
     __syncthreads();
     // positions of the CTA's rows
     for (int r = m0 / p.share + threadIdx.x; r <= (m_end - 1) / p.share; r += kThreads) {
@@ -844,15 +854,13 @@ __global__ void __launch_bounds__(rows_threads(IMAGE), 1) attention_rows_kernel(
     k.range = step_range(p, kv, k.lo, k.hi);
     k.begin = (int)((long long)k.range.count * split / pl.splits);
     k.end = (int)((long long)k.range.count * (split + 1) / pl.splits);
-    const int tiles = m_end - m0 > kRowTile ? 2 : 1;
-    if (warp < kProducer0 / 32) {
-        const int i = warp >> 2;
-        if (i < tiles) k.softmax(i, first, m0 + (int)threadIdx.x, m_end, tmem, pl, split);
+    if (warp < (ONE ? 4 : kProducer0 / 32)) {
+        if (warp < 4 * tiles) k.softmax(warp >> 2, first, m0 + (int)threadIdx.x, m_end, tmem, pl, split);
     } else if (warp < kIssuer / 32) {
         if constexpr (IMAGE) {
             k.fetch_images(pl);
         } else {
-            k.produce();
+            k.template produce<ONE ? 16 : 32>(warp - (ONE ? 4 : 8));
             cp_wait<0>();
         }
     } else if (k.end > k.begin) {
