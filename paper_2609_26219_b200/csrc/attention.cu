@@ -166,7 +166,7 @@ struct AttentionPlan {
     uint64_t image_bytes, meta_bytes;
 };
 
-constexpr uint64_t kMaxImageBytes = 1ull << 30;
+constexpr uint64_t kMaxImageBytes = 3ull << 29;
 
 AttentionPlan plan_attention(const patchkv_geom* g, int tag, const patchkv_batch* b, int Hq, int window, int sinks) {
     AttentionPlan a;
@@ -184,11 +184,12 @@ AttentionPlan plan_attention(const patchkv_geom* g, int tag, const patchkv_batch
         if (window > 0) steps = std::min(steps, ((long long)window + sinks + b->max_rows) / kRowTile + 3);
         a.row_tiles = (int)tiles;
         a.row_splits = (int)std::max(1ll, std::min((long long)kSms / ctas, steps / 2));
-        // Images pay where a token is needed by several CTAs, up to a gigabyte of workspace.
+        // Images pay where a token is needed by several CTAs, up to 1.5 GiB of workspace.
         const uint64_t all_steps = ((uint64_t)b->max_kv_len + kRowTile - 1) / kRowTile, images = all_steps * H * b->n_seqs;
-        if (tiles > 1 && images > 0 && images <= kMaxImageBytes / (4ull * kRowTile * D)) {
+        const uint64_t image = (pool ? 4ull : 6ull) * kRowTile * D;         // room for fp16 queries' two matrices of K
+        if (tiles > 1 && images > 0 && images <= kMaxImageBytes / image) {
             a.image_steps = (int)all_steps;
-            a.image_bytes = images * 4 * kRowTile * D;
+            a.image_bytes = images * image;
             a.meta_bytes = images * 32;
         }
         if (a.row_splits > 1) a.partial_bytes = (uint64_t)a.row_splits * b->n_rows * Hq * (D + 2) * 4;
@@ -258,36 +259,41 @@ cudaError_t launch_split_columns(const AttentionParams& p, const SplitPlan& pl, 
     return nc == 1 ? launch_split_group<D, 1>(p, pl, groups, s) : nc == 2 ? launch_split_group<D, 2>(p, pl, groups, s) : launch_split_group<D, 4>(p, pl, groups, s);
 }
 
-template <int KF, int VF, int D, bool IMAGE, bool ONE>
+template <int KF, int VF, int D, bool IMAGE, bool ONE, bool FINE>
 cudaError_t launch_rows_kernel(const AttentionParams& p, const RowsPlan& pl, cudaStream_t stream) {
-    auto kernel = attention_rows_kernel<KF, VF, D, IMAGE, ONE>;
+    auto kernel = attention_rows_kernel<KF, VF, D, IMAGE, ONE, FINE>;
     static std::atomic<uint64_t> allowed{0};
     const cudaError_t e = allow_smem((const void*)kernel, RowsSmem<D>::kLaunch, &allowed);
     if (e != cudaSuccess) return e;
     return launch_pdl(kernel, dim3(pl.tiles * p.c.H * p.b.n_seqs * pl.splits), dim3(rows_threads(IMAGE)), RowsSmem<D>::kLaunch, stream, p, pl);
 }
-template <int KF, int VF, int D>
+template <int KF, int VF, int D, bool FINE>
 cudaError_t launch_rows(const AttentionParams& p, const RowsPlan& pl, cudaStream_t stream) {
     cudaError_t e;
     if (pl.images) {
-        e = launch_pdl(attention_image_kernel<KF, VF, D>, dim3(pl.steps, p.c.H, p.b.n_seqs), dim3(kImageThreads), 0, stream, p, pl);
+        e = launch_pdl(attention_image_kernel<KF, VF, D, FINE>, dim3(pl.steps, p.c.H, p.b.n_seqs), dim3(kImageThreads), 0, stream, p, pl);
         if (e != cudaSuccess) return e;
         constexpr int F = KF == FMT_BF16 ? FMT_BF16 : FMT_INT8;
-        e = launch_rows_kernel<F, F, D, true, false>(p, pl, stream);
+        e = launch_rows_kernel<F, F, D, true, false, FINE>(p, pl, stream);
+    } else if ((long long)std::min(p.b.max_rows, p.b.n_rows) * p.share <= kRowTile) {
+        e = launch_rows_kernel<KF, VF, D, false, true, FINE>(p, pl, stream);
     } else {
-        e = (long long)std::min(p.b.max_rows, p.b.n_rows) * p.share <= kRowTile ? launch_rows_kernel<KF, VF, D, false, true>(p, pl, stream)
-                                                                                : launch_rows_kernel<KF, VF, D, false, false>(p, pl, stream);
+        e = launch_rows_kernel<KF, VF, D, false, false, FINE>(p, pl, stream);
     }
     if (e != cudaSuccess || pl.splits == 1) return e;
     return launch_pdl(attention_rows_join_kernel<D>, dim3((unsigned)(((long long)p.b.n_rows * p.Hq + 3) / 4)), dim3(128), 0, stream, p, pl);
 }
+template <int KF, int VF, int D>
+cudaError_t launch_rows_type(const AttentionParams& p, const RowsPlan& pl, cudaStream_t s) {
+    return p.f16 ? launch_rows<KF, VF, D, true>(p, pl, s) : launch_rows<KF, VF, D, false>(p, pl, s);
+}
 template <int D>
 cudaError_t launch_rows_tag(const AttentionParams& p, const RowsPlan& pl, cudaStream_t s) {
     switch (p.c.tag) {
-        case PATCHKV_TAG_BF16: return launch_rows<FMT_BF16, FMT_BF16, D>(p, pl, s);
-        case PATCHKV_TAG_INT8: return launch_rows<FMT_INT8, FMT_INT8, D>(p, pl, s);
-        case PATCHKV_TAG_INT4: return launch_rows<FMT_INT8, FMT_INT4, D>(p, pl, s);
-        default: return launch_rows<FMT_INT4, FMT_INT4, D>(p, pl, s);
+        case PATCHKV_TAG_BF16: return launch_rows<FMT_BF16, FMT_BF16, D, false>(p, pl, s);
+        case PATCHKV_TAG_INT8: return launch_rows_type<FMT_INT8, FMT_INT8, D>(p, pl, s);
+        case PATCHKV_TAG_INT4: return launch_rows_type<FMT_INT8, FMT_INT4, D>(p, pl, s);
+        default: return launch_rows_type<FMT_INT4, FMT_INT4, D>(p, pl, s);
     }
 }
 

@@ -15,6 +15,8 @@
 // 6000 cycles a step, three times what the products take.  Where one CTA is all there is, its own four warps convert (bf16
 // pages: cp.async), and the cache is read once, as it is.  Queries over quantised pages are fp16 scaled by a power of two per
 // row, so a bf16 query loses nothing.  The weights are fp16 there, bf16 over bf16 pages; sums are fp32 throughout.
+// fp16 queries (FINE) get K as the sum of two fp16 matrices, 22 bits, for one more product per 16 channels: one matrix alone
+// rounds code * scale to 11 bits, which in channels far larger than the others was most of an fp16 result's error.
 // As in the split kernel the softmax reference is only moved (and O rescaled) when a logit exceeds it by more than 15.
 #pragma once
 
@@ -34,7 +36,7 @@ struct RowsPlan {
     float* partial;                             // [split][n_rows * Hq][D], then (m, l) [split][n_rows * Hq]
     int32_t tiles;                              // CTAs along the query vectors of a sequence
     int32_t splits;                             // pieces of the token range (1: no partial results)
-    uint8_t* images;                            // [sequence][step][KV head]: K matrix, V matrix; null: no images
+    uint8_t* images;                            // [sequence][step][KV head]: K matrix (FINE: and what it leaves of K), V matrix; null: no images
     uint32_t* meta;                             // of each image: 4 words of absent tokens, 1 word `lost`, 3 unused
     int32_t steps;                              // of a sequence in the two
 };
@@ -169,6 +171,30 @@ __device__ __forceinline__ uint4 operands4(uint32_t w, uint32_t s, uint32_t m0, 
     asm("{\n\t.reg .b32 a;\n\tfma.rn.f16x2 a, %1, %2, %3;\n\tmul.rn.f16x2 %0, a, %4;\n\t}" : "=r"(o.w) : "r"(and_xor<0x00F000F0u>(v, m1)), "r"(0x2C002C00u), "r"(0xD480D480u), "r"(s));
     return o;
 }
+// The same and what the rounding took away: code * scale = hi + lo but for bits below 2^-24.  Where 128 * scale may pass fp16's
+// range, scales of 512 and more, lo is zero: an infinite hi keeps its sign, and infinity - infinity is never formed.
+__device__ __forceinline__ uint32_t rest_mask(uint32_t s) { return (s & 0x7FFFu) < 0x6000u ? 0xFFFFFFFFu : 0u; }
+__device__ __forceinline__ uint32_t rest(uint32_t code, uint32_t s, uint32_t hi, uint32_t keep) { return hfma2(code, s, hi ^ 0x80008000u) & keep; }
+__device__ __forceinline__ uint32_t hsub2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ void operands4(uint32_t w, uint32_t s, uint32_t m0, uint32_t m1, uint4& hi, uint4& lo) {
+    const uint32_t v = w >> 8;
+    const uint32_t a = hsub2(and_xor<0x000F000Fu>(w, m0), 0x64086408u), b = hfma2(and_xor<0x00F000F0u>(w, m1), 0x2C002C00u, 0xD480D480u);
+    const uint32_t c = hsub2(and_xor<0x000F000Fu>(v, m0), 0x64086408u), d = hfma2(and_xor<0x00F000F0u>(v, m1), 0x2C002C00u, 0xD480D480u);
+    const uint32_t keep = rest_mask(s);
+    hi = make_uint4(hmul2(a, s), hmul2(b, s), hmul2(c, s), hmul2(d, s));
+    lo = make_uint4(rest(a, s, hi.x, keep), rest(b, s, hi.y, keep), rest(c, s, hi.z, keep), rest(d, s, hi.w, keep));
+}
+__device__ __forceinline__ void operands8(uint32_t w, uint32_t s, uint2& hi, uint2& lo) {
+    const uint32_t u = w ^ 0x80808080u;
+    const uint32_t a = hsub2(__byte_perm(u, 0x64646464u, 0x4140), 0x64806480u), b = hsub2(__byte_perm(u, 0x64646464u, 0x4342), 0x64806480u);
+    const uint32_t keep = rest_mask(s);
+    hi = make_uint2(hmul2(a, s), hmul2(b, s));
+    lo = make_uint2(rest(a, s, hi.x, keep), rest(b, s, hi.y, keep));
+}
 // Four fp16 operands of a word of 8-bit codes, in order: 1024 + u, minus 1152, times the scale.
 __device__ __forceinline__ uint2 operands8(uint32_t w, uint32_t s) {
     const uint32_t u = w ^ 0x80808080u;
@@ -211,6 +237,35 @@ __device__ __forceinline__ void image_operands(uint4 (&o)[4], const uint8_t* row
         }
     }
 }
+// K of an image: also what the rounding took away.
+template <int F>
+__device__ __forceinline__ void image_operands(uint4 (&hi)[4], uint4 (&lo)[4], const uint8_t* row, int c, uint32_t s, uint32_t m0, uint32_t m1) {
+    const uint4 a = __ldg(reinterpret_cast<const uint4*>(row + c * (F == FMT_INT8 ? 32 : 16)));
+    auto ordered = [](const uint4& x) {                         // 0 4, 1 5, 2 6, 3 7 -> 0 1, 2 3, 4 5, 6 7
+        return make_uint4(__byte_perm(x.x, x.y, 0x5410), __byte_perm(x.z, x.w, 0x5410), __byte_perm(x.x, x.y, 0x7632), __byte_perm(x.z, x.w, 0x7632));
+    };
+    if (F == FMT_INT8) {
+        const uint4 b = __ldg(reinterpret_cast<const uint4*>(row + c * 32 + 16));
+        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            uint2 x, y, p, q;
+            operands8(w[2 * i], s, x, p);
+            operands8(w[2 * i + 1], s, y, q);
+            hi[i] = make_uint4(x.x, x.y, y.x, y.y);
+            lo[i] = make_uint4(p.x, p.y, q.x, q.y);
+        }
+    } else {
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            uint4 x, y;
+            operands4(w[i], s, m0, m1, x, y);
+            hi[i] = ordered(x);
+            lo[i] = ordered(y);
+        }
+    }
+}
 struct StepPlace { TileRange range; int seq, head, kv, lo, hi, begin, end; bool order4; };
 __device__ __forceinline__ bool whole_step(const AttentionParams& p, int kv, int lo, int hi, int t0) {
     return t0 + kRowTile - 1 <= min(lo, kv - 1) && (p.window == 0 || hi - t0 < p.window || t0 + kRowTile <= p.sinks);
@@ -247,11 +302,14 @@ __device__ __noinline__ void add_lost(const AttentionParams& p, const RowsPlan& 
 
 // KF / VF: page formats (both FMT_BF16 for the bf16 pool).  IMAGE: operands come as images, in channel order (KF = VF = FMT_INT8
 // stands for fp16 images, FMT_BF16 for bf16).
-template <int KF, int VF, int D, bool IMAGE>
+template <int KF, int VF, int D, bool IMAGE, bool FINE>
 struct RowsKernel {
     static constexpr bool kPool = KF == FMT_BF16;
     using S = RowsSmem<D>;
     static constexpr int kPer = D / 32;                         // 32-channel pieces (= threads) of a token's row
+    // K's ring: two stages, or one of two matrices (the next K has the whole softmax of a step to arrive).
+    __device__ __forceinline__ static int k_stage(int n) { return FINE ? 0 : n & 1; }
+    __device__ __forceinline__ static uint32_t k_turn(int n) { return (FINE ? n : n >> 1) & 1; }
 
     const AttentionParams& p;
     RowsBars& bars;
@@ -321,20 +379,22 @@ struct RowsKernel {
         for (; j < end; j++) {
             const int n = j - begin, st = n & 1;
             const uint32_t parity = ((n >> 1) & 1) ^ 1;
+            constexpr uint32_t kBytes = (FINE ? 2 : 1) * S::kMat;
             const long long at = image_index(p, pl, seq, range.tile(j), head);
-            const uint8_t* image = pl.images + at * (2 * S::kMat);
-            if (!wait_warp(&bars.k_empty[st], parity)) break;
+            const uint8_t* image = pl.images + at * (kBytes + S::kMat);
+            uint64_t* full = &bars.k_full[k_stage(n)];
+            if (!wait_warp(&bars.k_empty[k_stage(n)], k_turn(n) ^ 1)) break;
             if (elect_lane()) {
-                mbar_arrive_expect_tx(&bars.k_full[st], S::kMat + 32);
-                bulk_g2s_at(smem + S::kK + st * S::kMat, image, S::kMat, &bars.k_full[st]);
-                bulk_g2s_at(smem_u32(bars.absent[n & 3]), pl.meta + at * 8, 32, &bars.k_full[st]);
+                mbar_arrive_expect_tx(full, kBytes + 32);
+                bulk_g2s_at(smem + S::kK + k_stage(n) * S::kMat, image, kBytes, full);
+                bulk_g2s_at(smem_u32(bars.absent[n & 3]), pl.meta + at * 8, 32, full);
             }
             __syncwarp();
             k_uses++;
             if (!wait_warp(&bars.v_empty[st], parity)) break;
             if (elect_lane()) {
                 mbar_arrive_expect_tx(&bars.v_full[st], S::kMat);
-                bulk_g2s_at(smem + S::kV + st * S::kMat, image + S::kMat, S::kMat, &bars.v_full[st]);
+                bulk_g2s_at(smem + S::kV + st * S::kMat, image + kBytes, S::kMat, &bars.v_full[st]);
             }
             __syncwarp();
             v_uses++;
@@ -342,7 +402,7 @@ struct RowsKernel {
         // The last copies (after an abort they may have no reader) must have landed before the CTA goes.
         for (int back = 1; back <= 2; back++) {
             const uint32_t k = k_uses - back, v = v_uses - back;
-            for (uint32_t i = 0; k_uses >= (uint32_t)back && i < kWaitLimit && !mbar_try_wait(&bars.k_full[k & 1], (k >> 1) & 1); i++) __nanosleep(40);
+            for (uint32_t i = 0; k_uses >= (uint32_t)back && (!FINE || back == 1) && i < kWaitLimit && !mbar_try_wait(&bars.k_full[k_stage((int)k)], k_turn((int)k)); i++) __nanosleep(40);
             for (uint32_t i = 0; v_uses >= (uint32_t)back && i < kWaitLimit && !mbar_try_wait(&bars.v_full[v & 1], (v >> 1) & 1); i++) __nanosleep(40);
         }
     }
@@ -373,8 +433,9 @@ struct RowsKernel {
                 if (TOK == 32) bars.absent[n & 3][w] = gone;
                 else reinterpret_cast<uint16_t*>(bars.absent[n & 3])[w] = (uint16_t)gone;
             }
-            const uint32_t kb = smem + S::kK + st * S::kMat, vb = smem + S::kV + st * S::kMat;
-            if (!wait_warp(&bars.k_empty[st], parity)) return;
+            const uint32_t kb = smem + S::kK + k_stage(n) * S::kMat, vb = smem + S::kV + st * S::kMat;
+            uint64_t* k_full = &bars.k_full[k_stage(n)];
+            if (!wait_warp(&bars.k_empty[k_stage(n)], k_turn(n) ^ 1)) return;
             if constexpr (kPool) {
                 // chunks kPer apart: a row's lanes read a contiguous run
                 auto copy = [&](const uint16_t* from, uint32_t mat) {
@@ -393,21 +454,21 @@ struct RowsKernel {
                 copy(p.c.v, vb);
                 cp_wait<1>();
                 fence_async_smem();
-                mbar_arrive(&bars.k_full[st]);
+                mbar_arrive(k_full);
                 cp_wait<0>();
                 if (masked) clean<0x7F80u, kPass>(vb, tok0, c, 1, kPer);
             } else {
 #pragma unroll
                 for (int i = 0; i < kPass; i++) {
-                    store_operands<KF>(kb, tok0 + i * kTok, c, code[i], scale[i], m0, m1);
+                    store_operands<KF, FINE>(kb, tok0 + i * kTok, c, code[i], scale[i], m0, m1);
                     load_piece<VF, TOK>(now, tok0 + i * kTok, c, true, code[i], scale[i]);
                 }
                 fence_async_smem();
-                mbar_arrive(&bars.k_full[st]);
+                mbar_arrive(k_full);
                 if (!wait_warp(&bars.v_empty[st], parity)) return;
 #pragma unroll
                 for (int i = 0; i < kPass; i++) {
-                    store_operands<VF>(vb, tok0 + i * kTok, c, code[i], scale[i], m0, m1);
+                    store_operands<VF, false>(vb, tok0 + i * kTok, c, code[i], scale[i], m0, m1);
                     load_piece<KF, TOK>(next, tok0 + i * kTok, c, false, code[i], scale[i]);
                 }
                 if (masked) clean<0x7C00u, kPass>(vb, tok0, c, 4, 1);
@@ -438,20 +499,26 @@ struct RowsKernel {
         }
     }
     // The 32 channels of a thread into its token's row.
-    template <int F>
+    template <int F, bool REST>
     __device__ __forceinline__ void store_operands(uint32_t mat, int tok, int c, const uint32_t (&w)[8], uint32_t scale, uint32_t m0, uint32_t m1) {
         const uint32_t s = scale | scale << 16;
         const uint32_t flip = c & 2;                            // the two halves of the channels write different banks
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            uint4 o;
+            uint4 o, lo;
             if constexpr (F == FMT_INT4) {
-                o = operands4(flip ? w[i ^ 2] : w[i], s, m0, m1);
+                const uint32_t x = flip ? w[i ^ 2] : w[i];
+                if (REST) operands4(x, s, m0, m1, o, lo); else o = operands4(x, s, m0, m1);
             } else {
-                const uint2 a = operands8(flip ? w[(2 * i) ^ 4] : w[2 * i], s), b = operands8(flip ? w[(2 * i + 1) ^ 4] : w[2 * i + 1], s);
+                const uint32_t x = flip ? w[(2 * i) ^ 4] : w[2 * i], y = flip ? w[(2 * i + 1) ^ 4] : w[2 * i + 1];
+                uint2 a, b, c2, d2;
+                if (REST) { operands8(x, s, a, c2); operands8(y, s, b, d2); lo = make_uint4(c2.x, c2.y, d2.x, d2.y); }
+                else { a = operands8(x, s); b = operands8(y, s); }
                 o = make_uint4(a.x, a.y, b.x, b.y);
             }
-            sts128(mat + swizzled(tok, 4 * c + (i ^ flip)), o.x, o.y, o.z, o.w);
+            const uint32_t at = mat + swizzled(tok, 4 * c + (i ^ flip));
+            sts128(at, o.x, o.y, o.z, o.w);
+            if (REST) sts128(at + S::kMat, lo.x, lo.y, lo.z, lo.w);
         }
     }
 
@@ -467,6 +534,7 @@ struct RowsKernel {
                 for (int x = 0; x < D / 16; x++) {              // 16 channels: 32 bytes inside a 128-byte row, then the next half
                     const uint32_t o = (x >> 2) * (kRowTile * 8) + (x & 3) * 2;
                     tc_mma_ss(tmem + i * kRowTile, q + o, k + o, kQk, x != 0);
+                    if (FINE) tc_mma_ss(tmem + i * kRowTile, q + o, k + o + kMat16, kQk, true);
                 }
                 tc_commit(&bars.s_ready[i]);
                 if (k_free) tc_commit(k_free);
@@ -482,7 +550,7 @@ struct RowsKernel {
         for (int j = 0; j < n; j++) {
             const int st = j & 1;
             if (!wait_warp(&bars.v_full[st], (j >> 1) & 1)) return;
-            if (j + 1 < n && !wait_warp(&bars.k_full[st ^ 1], ((j + 1) >> 1) & 1)) return;
+            if (j + 1 < n && !wait_warp(&bars.k_full[k_stage(j + 1)], k_turn(j + 1))) return;
 #pragma unroll 1
             for (int i = 0; i < tiles; i++) {
                 if (!wait_warp(&bars.p_ready[i], j & 1)) return;
@@ -498,7 +566,7 @@ struct RowsKernel {
                     if (j + 1 == n) tc_commit(&bars.o_ready[i]);
                 }
                 __syncwarp();
-                if (j + 1 < n) logits(i, st ^ 1, i == tiles - 1 ? &bars.k_empty[st ^ 1] : nullptr);
+                if (j + 1 < n) logits(i, k_stage(j + 1), i == tiles - 1 ? &bars.k_empty[k_stage(j + 1)] : nullptr);
             }
         }
     }
@@ -800,9 +868,9 @@ struct RowsKernel {
 };
 
 // ONE: no sequence has more than one tile of vectors; the second tile's warps then help to bring K and V.
-template <int KF, int VF, int D, bool IMAGE, bool ONE>
+template <int KF, int VF, int D, bool IMAGE, bool ONE, bool FINE>
 __global__ void __launch_bounds__(rows_threads(IMAGE), 1) attention_rows_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ RowsPlan pl) {
-    using K = RowsKernel<KF, VF, D, IMAGE>;
+    using K = RowsKernel<KF, VF, D, IMAGE, FINE>;
     using S = RowsSmem<D>;
     constexpr int kIssuer = rows_issuer(IMAGE), kThreads = rows_threads(IMAGE);
     extern __shared__ uint8_t raw[];
@@ -883,7 +951,7 @@ __global__ void __launch_bounds__(rows_threads(IMAGE), 1) attention_rows_kernel(
 // swizzled as in shared memory, tokens behind the cache or on a page out of range zero.  Values that are not finite are set to
 // zero in V and noted.  Bound by memory: reads the cache once, writes 4 bytes per element pair.
 constexpr int kImageThreads = 256;
-template <int KF, int VF, int D>
+template <int KF, int VF, int D, bool FINE>
 __global__ void __launch_bounds__(kImageThreads) attention_image_kernel(const AttentionParams p, const RowsPlan pl) {
     using S = RowsSmem<D>;
     constexpr bool kPool = KF == FMT_BF16;
@@ -906,8 +974,8 @@ __global__ void __launch_bounds__(kImageThreads) attention_image_kernel(const At
     __syncthreads();
     const int c = threadIdx.x % kPer;
     uint32_t m0 = 0x64086408u, m1 = 0x64806480u;
-    uint8_t* k_image = pl.images + image_index(p, pl, seq, step, head) * (2 * S::kMat);
-    uint8_t* v_image = k_image + S::kMat;
+    uint8_t* k_image = pl.images + image_index(p, pl, seq, step, head) * ((FINE ? 3 : 2) * S::kMat);
+    uint8_t* v_image = k_image + (FINE ? 2 : 1) * S::kMat;
 #pragma unroll
     for (int i = 0; i < kRowTile / kTokens; i++) {
         const int tok = threadIdx.x / kPer + i * kTokens, t = t0 + tok;
@@ -921,10 +989,10 @@ __global__ void __launch_bounds__(kImageThreads) attention_image_kernel(const At
                 if (c == 0) atomicOr(&meta[tok >> 5], 1u << (tok & 31));
             }
         }
-        uint4 ko[4], vo[4];
+        uint4 ko[4], kr[4], vo[4];
         if (page < 0) {
 #pragma unroll
-            for (int q = 0; q < 4; q++) ko[q] = vo[q] = make_uint4(0, 0, 0, 0);
+            for (int q = 0; q < 4; q++) ko[q] = kr[q] = vo[q] = make_uint4(0, 0, 0, 0);
         } else if constexpr (kPool) {
             const long long o = (long long)page * p.c.stride_page + (long long)slot * p.c.stride_token + (long long)head * p.c.stride_head + 32 * c;
 #pragma unroll
@@ -937,7 +1005,8 @@ __global__ void __launch_bounds__(kImageThreads) attention_image_kernel(const At
             const uint32_t row = (uint32_t)slot * p.c.H + head, sc = (row * (D / p.c.G) + c * 32 / p.c.G) * 2;
             uint32_t ks = __ldg(reinterpret_cast<const uint16_t*>(pg + p.c.k_scales + sc)), vs = __ldg(reinterpret_cast<const uint16_t*>(pg + p.c.v_scales + sc));
             ks |= ks << 16; vs |= vs << 16;
-            image_operands<KF>(ko, pg + row * (KF == FMT_INT8 ? D : D / 2), c, ks, m0, m1);
+            if (FINE) image_operands<KF>(ko, kr, pg + row * (KF == FMT_INT8 ? D : D / 2), c, ks, m0, m1);
+            else image_operands<KF>(ko, pg + row * (KF == FMT_INT8 ? D : D / 2), c, ks, m0, m1);
             image_operands<VF>(vo, pg + p.c.v_codes + row * (VF == FMT_INT8 ? D : D / 2), c, vs, m0, m1);
         }
         bool lost = false;
@@ -945,6 +1014,7 @@ __global__ void __launch_bounds__(kImageThreads) attention_image_kernel(const At
         for (int q = 0; q < 4; q++) {
             lost = finite_only<kPool ? 0x7F80u : 0x7C00u>(vo[q]) || lost;
             *reinterpret_cast<uint4*>(k_image + swizzled(tok, 4 * c + q)) = ko[q];
+            if (FINE) *reinterpret_cast<uint4*>(k_image + S::kMat + swizzled(tok, 4 * c + q)) = kr[q];
             *reinterpret_cast<uint4*>(v_image + swizzled(tok, 4 * c + q)) = vo[q];
         }
         if (lost) meta[4] = 1;

@@ -126,13 +126,14 @@ def random_rows(rng, n, H, D, dtype, outliers=True):
     return torch.from_numpy(x).to(dtype)
 
 
-def attention64(q, k_of, v_of, case: Case, share: int, scale: float, window: int, sinks: int, out_type, bf16_pool: bool):
+def attention64(q, k_of, v_of, case: Case, share: int, scale: float, window: int, sinks: int, out_type, bf16_pool: bool,
+                k_rounding: float = 2.0 ** -11):
     """q float64 [n][Hq][D]; k_of(b), v_of(b): float64 [kv][H][D] of a sequence.  Returns (out, tol).
 
     tol is an elementwise bound on what the library may be off, from its number formats alone:
       the result's rounding                          u_out |o|
       the weights as 16-bit numbers                  u_p sum p|v|       (u_p 2^-8 over bf16 pages, 2^-11 else)
-      quantised values as fp16 operands              2^-11 sum p|v|     and logits off by d = 2^-11 scale max_j sum |q||k|,
+      quantised values as fp16 operands              2^-11 sum p|v|     and logits off by d = k_rounding scale max_j sum |q||k|,
                                                      which change a weight by a factor within e^(2d)
       fp32 sums (and exp2, 2^-22) over D, then the tokens in pieces: (D + 64) 2^-23 on the logits' terms likewise
       weights below fp16's normal range              n 2^-24 max|v|
@@ -159,7 +160,7 @@ def attention64(q, k_of, v_of, case: Case, share: int, scale: float, window: int
                 w /= np.where(live, w.sum(1), 1.0)[:, None]
                 o, a = w @ vv, w @ np.abs(vv)
                 big = np.abs(scale) * np.where(see, np.abs(qq) @ np.abs(kk).T, 0.0).max(1)[:, None]
-                d = ((0.0 if bf16_pool else 2.0 ** -11) + (D + 64) * 2.0 ** -23) * big
+                d = ((0.0 if bf16_pool else k_rounding) + (D + 64) * 2.0 ** -23) * big
                 u = (2.0 ** -8 if bf16_pool else 2.0 ** -11 + 2.0 ** -11) + np.expm1(2 * d) + 2.0 ** -18
                 floor = see.sum(1)[:, None] * 2.0 ** -24 * np.abs(vv).max()
                 out[r:r + R, h] = o

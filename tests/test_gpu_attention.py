@@ -199,6 +199,43 @@ def test_value_ranges(pk, ctx, tag, rows, size):
     s.check(ctx)
 
 
+@pytest.mark.parametrize("tag", [1, 2, 3])
+@pytest.mark.parametrize("rows", [1, 40, 100, 300])
+@pytest.mark.parametrize("D", [64, 128])
+def test_fp16_queries_see_whole_keys(pk, ctx, tag, rows, D):
+    """Over quantised pages an fp16 query's logits are those of code * scale, not of its fp16 rounding: the bound has no term
+    for K.  With a scale of 2^-14 or more the product is a multiple of 2^-24 of at most 19 bits, so two fp16 numbers hold it.
+    One channel of K is far larger than the others, where rounding it would show."""
+    s = Setup(pk, tag, 2, 4, D, 16, 32, Case([333], [rows]), dtype=F16)
+    rng = np.random.default_rng(5)
+    for j in range(333):
+        k, v = (random_rows(rng, 1, 2, D, BF16, outliers=False).double().numpy()[0] for _ in range(2))
+        k[:, 7] *= 300
+        s.lay.put(s.pages[s.table[0, j // 16]], j % 16, k, v)
+    s.dev.copy_(torch.from_numpy(s.pages))
+    s.q[:, :, 7] *= 0.02
+    got = s.check(ctx)[:rows].double().cpu().numpy()
+    want, tol = attention64(s.q[:rows].double().numpy(), lambda b: s.kv(b)[0], lambda b: s.kv(b)[1], s.case, 2, D ** -0.5, 0, 0, F16,
+                            False, k_rounding=0.0)
+    assert np.all(np.abs(got - want) <= tol), np.max(np.abs(got - want) / tol)
+
+
+@pytest.mark.parametrize("tag", [1, 2, 3])
+@pytest.mark.parametrize("rows", [1, 40, 300])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_keys_beyond_fp16(pk, ctx, tag, rows, dtype):
+    """A key of finite scales whose values pass fp16's range, far on the negative side: a weight of zero, as for one within it."""
+    s = Setup(pk, tag, 2, 4, 64, 16, 32, Case([310], [rows]), dtype=dtype)
+    s.q = -s.q.abs() - 0.5
+    outs = []
+    for size in (4000.0, 120000.0):
+        s.lay.put(s.pages[s.table[0, 0]], 5, np.full((2, 64), size), np.ones((2, 64)))
+        s.dev.copy_(torch.from_numpy(s.pages))
+        outs.append(s.run(ctx))
+    assert ctx.query_status() == 0
+    assert torch.isfinite(outs[0]).all() and torch.equal(*outs)
+
+
 @pytest.mark.parametrize("tag", TAGS)
 @pytest.mark.parametrize("rows", [2, 60, 300])
 def test_nan_and_infinity_in_unseen_tokens(pk, ctx, tag, rows):
