@@ -14,7 +14,8 @@
 //      largest; each 32-channel chunk is summed on its own in fp32 from a start value that takes the offset out again (-8 * sum of
 //      the chunk's q), then enters the logit with the token's fp32 scale: no rounding of K at all.
 //   V: v = (u * 2^-24) * S - offset * S in one half fma, S the token's scale times a power of two that follows the
-//      largest V scale seen: one rounding of 2^-12, as p's own to fp16.
+//      largest V scale seen: one rounding of 2^-12, as p's own to fp16.  For fp16 results, whose own rounding is no larger
+//      than those two, p is the sum of two fp16 numbers, for one more product per operand.
 // Softmax on powers of two against a reference that is only moved when a logit exceeds it by more than 15 (p <= 2^15), to 3 below
 // the largest (fp16 then holds weights down to 2^-17 of it to all its bits): one vote per tile instead of a maximum across lanes.
 #pragma once
@@ -504,7 +505,8 @@ struct SplitKernel {
                 }
             }
         }
-        uint32_t pf[NT][2];
+        uint32_t pf[NT][2], pr[NT][2];                              // weights, and for fp16 results what their rounding took
+        const bool fine = !kPool && p.f16;
 #pragma unroll
         for (int c = 0; c < NC; c++) {
 #pragma unroll
@@ -516,7 +518,10 @@ struct SplitKernel {
 #pragma unroll
             for (int i = 0; i < 2; i++) {
                 const float lo = x[2 * nt][i], hi = NC > 1 ? x[(2 * nt + 1) % NC][i] : 0.0f;
-                pf[nt][i] = transpose8x8(kPool ? bf162_bits(lo, hi) : half2_bits(lo, hi));
+                const uint32_t w = kPool ? bf162_bits(lo, hi) : half2_bits(lo, hi);
+                pf[nt][i] = transpose8x8(w);
+                pr[nt][i] = 0;
+                if (fine) pr[nt][i] = transpose8x8(half2_bits(lo - low_half(w), hi - high_half(w)));
             }
         if constexpr (kPool) {
             const uint32_t a = base + kV + ((lane & 7) + ((lane >> 4) << 3)) * kVStride + (lane & 8) * 2;
@@ -578,7 +583,10 @@ struct SplitKernel {
                             const uint32_t a2 = hfma2(and_xor<0x000F000Fu>(b, flip0), S[1], off[1]);
                             const uint32_t a3 = hfma2(and_xor<0x00F000F0u>(b, flip1), S16[1], off[1]);
 #pragma unroll
-                            for (int nt = 0; nt < NT; nt++) mma_f16(acc[nt][4 * k + 2 * h + m], a0, a1, a2, a3, pf[nt][0], pf[nt][1]);
+                            for (int nt = 0; nt < NT; nt++) {
+                                mma_f16(acc[nt][4 * k + 2 * h + m], a0, a1, a2, a3, pf[nt][0], pf[nt][1]);
+                                if (fine) mma_f16(acc[nt][4 * k + 2 * h + m], a0, a1, a2, a3, pr[nt][0], pr[nt][1]);
+                            }
                             a >>= 8; b >>= 8;
                         }
                     } else {
@@ -587,7 +595,10 @@ struct SplitKernel {
                         const uint32_t a2 = hfma2(and_xor<0x00FF00FFu>(b, flip1), S[1], off[1]);
                         const uint32_t a3 = hfma2(and_xor<0x00FF00FFu>(b >> 8, flip1), S[1], off[1]);
 #pragma unroll
-                        for (int nt = 0; nt < NT; nt++) mma_f16(acc[nt][2 * k + h], a0, a1, a2, a3, pf[nt][0], pf[nt][1]);
+                        for (int nt = 0; nt < NT; nt++) {
+                            mma_f16(acc[nt][2 * k + h], a0, a1, a2, a3, pf[nt][0], pf[nt][1]);
+                            if (fine) mma_f16(acc[nt][2 * k + h], a0, a1, a2, a3, pr[nt][0], pr[nt][1]);
+                        }
                     }
                 }
             }
