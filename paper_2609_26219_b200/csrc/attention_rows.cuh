@@ -725,7 +725,7 @@ struct RowsKernel {
             // 2^15.  Else (a row's first step, and rarely) the largest logits are found, the references of the warp's rows moved to
             // 3 below them, and the weights made again.  fp16 then holds weights down to 2^-17 of the largest to all its bits (the many
             // small weights of a long context matter: with a largest weight of 2^-4 fp16 results were 7.7e-4 off, 7.0e-4
-            // so, what is left being K's rounding), and a logit may still grow by 12: a step made twice costs 4500 cycles, and at 8
+            // so, with K as one fp16 matrix), and a logit may still grow by 12: a step made twice costs 4500 cycles, and at 8
             // below 8192 rows over 8192 tokens (32 query heads) took 566 us instead of 517.
             uint32_t w[64];
             f32x2 total;
