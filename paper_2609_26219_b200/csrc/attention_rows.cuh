@@ -635,13 +635,15 @@ struct RowsKernel {
     }
 
     // 2^y for two y on the fma pipe: y = n + f with n whole and |f| <= 1/2, 2^f by a polynomial (fitted for the least relative
-    // error on that interval: 2.6e-6), times 2^n put together as bits.  Below -126 the result is about 2^-126, above 126 (a row that has
-    // had no token yet: its reference is far below all logits) 2^126, which the check behind finds; NaN stays NaN.
+    // error on that interval: 2.6e-6), times 2^n put together as bits.  At -127, where all below is put, those bits are +0: a masked
+    // logit has the weight 0, as from ex2.  (2^-126 instead is a normal bf16 number, and times a finite 3e38 in a slot that the row
+    // does not see it shows.)  Above 126 (a row that has had no token yet: its reference is far below all logits) the result is
+    // 2^126, which the check behind finds; NaN stays NaN.
     __device__ __forceinline__ static void exp2_pair(f32x2 y2, float& a, float& b) {
         float u, v;
         unpack2(y2, u, v);
-        asm("max.NaN.f32 %0, %0, %1;" : "+f"(u) : "f"(-126.0f));
-        asm("max.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(-126.0f));
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(u) : "f"(-127.0f));
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(-127.0f));
         asm("min.NaN.f32 %0, %0, %1;" : "+f"(u) : "f"(126.0f));
         asm("min.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(126.0f));
         const f32x2 y = pack2(u, v), magic = pack2(12582912.0f, 12582912.0f);       // 1.5 * 2^23
@@ -801,8 +803,6 @@ struct RowsKernel {
         float sum, sum_odd;
         unpack2(sum2, sum, sum_odd);
         sum += sum_odd;
-        // (A row that sees a token has a weight of 2^3 and more; what it does not see weighs up to 2^-126 in the computed pairs.)
-        if (sum < 1.0e-30f) sum = 0.0f;
         if (broken && sum != 0.0f) sum = __uint_as_float(0x7FC00000u);
         const bool lost = IMAGE ? lost_seen != 0 : *reinterpret_cast<volatile int32_t*>(&bars.lost) != 0;
         const float inv = pl.splits > 1 ? 1.0f : (sum != 0.0f ? 1.0f / sum : 0.0f);

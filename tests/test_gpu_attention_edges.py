@@ -1,0 +1,31 @@
+"""patchkv_attention where it is easy to get wrong: what unseen slots hold, rows that see nothing or lie far apart, batches
+whose entries are out of order, values of very different size.  Bounds as in test_gpu_attention."""
+import numpy as np
+import pytest
+
+from live_common import Case
+from test_gpu_attention import Setup, ctx, pk  # noqa: F401  (fixtures)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("rows", [2, 60, 300])
+@pytest.mark.parametrize("window", [0, 24])
+def test_huge_values_in_unseen_pool_tokens(pk, ctx, rows, window):
+    """A finite value of 3e38 in a token that a row does not see, later than the row or behind its window, is not part of its result: a weight
+    of zero is zero, not a small number.  Two neighbouring tokens at every place of eight."""
+    s = Setup(pk, 0, 2, 4, 64, 16, 32, Case([400], [rows]))
+    first, clean = 400 - rows, max(1, rows // 2)            # rows [clean, ...) see the later tokens
+    at = list(range(first + clean, 400)) + list(range(0, first - window) if window else [])
+    at = [t for t in at if t % 8 in (0, 1)] or [first + clean]
+    s.v = s.v.clone()
+    for t in at:
+        s.v[s.table[0, t // 16], t % 16] = 3.0e38
+        s.host[1][s.table[0, t // 16], t % 16] = 0.0
+    s.cache = pk.make_pool(s.k, s.v, s.n_pages, (0, 2048, 128, 64))
+    out = s.run(ctx, window)
+    assert ctx.query_status() == 0
+    seen = Case([400], [clean], [list(range(first, first + clean))])
+    s.q = s.q[:clean]
+    want, tol = s.reference(window, case=seen)
+    assert np.all(np.abs(out[:clean].double().cpu().numpy() - want) <= tol)
