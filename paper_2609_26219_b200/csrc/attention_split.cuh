@@ -135,23 +135,25 @@ __device__ __forceinline__ TileRange tile_range(const AttentionParams& p, int kv
     r.count = r.sink_tiles + max(0, last - r.first);
     return r;
 }
-// Smallest (but -1 for any below) and largest position of the first max_rows of a sequence's rows.
-__device__ __forceinline__ void position_range(const AttentionParams& p, int s, int first, int rows, int* lo, int* hi) {
+// Smallest and largest position of the first max_rows of a sequence's rows, those below 0 left out: they see nothing, and a window
+// need not reach back for them.  `blind`: there is such a row (a tile then needs its mask).
+__device__ __forceinline__ void position_range(const AttentionParams& p, int s, int first, int rows, int* lo, int* hi, bool* blind) {
     const int n = min(rows, p.b.max_rows);
     if (!p.b.pos) {
         const int a = __ldg(p.b.kv_len + s) - rows;
-        *lo = max(-1, a);
+        *lo = max(0, a);
         *hi = a + n - 1;
+        *blind = a < 0;
         return;
     }
     *lo = 0x7FFFFFFF;
     *hi = -1;
+    *blind = false;
     for (int i = 0; i < n; i++) {
         const int x = __ldg(p.b.pos + first + i);
-        *lo = min(*lo, x);
+        if (x >= 0) *lo = min(*lo, x); else *blind = true;
         *hi = max(*hi, x);
     }
-    *lo = max(-1, *lo);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -183,7 +185,7 @@ struct SplitKernel {
     float factor[NC], ref[NC], sum[NC];
     float acc[NT][kMT][4];
     uint32_t v_up0, v_up1, v_most;              // V scales are multiplied by a power of two: two halves, and the bits of the first scale too large for it
-    uint32_t cold;                              // shared memory: kv, smallest and largest position, and the positions of the columns
+    uint32_t cold;                              // shared memory: kv, smallest and largest position (not below 0), and the positions of the columns
     uint32_t k_off, v_off, s_off;               // the lane's places in a tile's rows, relative to its first
     uint32_t flip0, flip1;                      // 8 in every half's low nibble, 8 in the next one (constants the compiler must keep in registers)
 
@@ -192,6 +194,7 @@ struct SplitKernel {
     // 128 registers a thread are what sixteen warps leave: what only tiles with a mask need lives in shared memory.
     __device__ __forceinline__ int kv() const { return (int)lds32(cold); }
     __device__ __forceinline__ int lo_pos() const { return (int)lds32(cold + 4); }
+    __device__ __forceinline__ int lo_whole() const { return (int)lds32(cold + 28); }       // lo_pos, or -1 with a row below 0
     __device__ __forceinline__ int hi_pos() const { return (int)lds32(cold + 8); }
     __device__ __forceinline__ int pos(int c) const { return (int)lds32(cold + 48 + 4 * column_of(c, t)); }
     // First token of the warp's tile i.
@@ -660,7 +663,7 @@ __device__ __forceinline__ void store_out(const AttentionParams& p, uint32_t sha
 
 // The piece of the batch that item `item` stands for: sequence and virtual tiles [begin, end).  All lanes of a warp agree.
 // With a target, the batch's tiles are cut into about that many pieces of equal length, none across two sequences.
-struct Item { int seq, split, splits, first_item, begin, end, first, rows, kv, lo, hi; bool ok; };
+struct Item { int seq, split, splits, first_item, begin, end, first, rows, kv, lo, hi; bool blind, ok; };
 __device__ __forceinline__ Item find_item(const AttentionParams& p, const SplitPlan& pl, int item) {
     const int lane = threadIdx.x & 31;
     Item it;
@@ -673,7 +676,7 @@ __device__ __forceinline__ Item find_item(const AttentionParams& p, const SplitP
         it.seq = 0;
         if (!sequence_rows(p, 0, &it.first, &it.kv, &it.rows)) { if (lane == 0 && item == 0) latch(p.status); return it; }
         if (it.rows == 0) return it;
-        position_range(p, 0, it.first, it.rows, &lo, &hi);
+        position_range(p, 0, it.first, it.rows, &lo, &hi, &it.blind);
         const int tiles = tile_range(p, it.kv, lo, hi).count;
         const int piece = max((int)((uint32_t)(tiles + pl.target - 1) / (uint32_t)pl.target), 1 << pl.per_head_log2);
         it.splits = max(1, (int)((uint32_t)(tiles + piece - 1) / (uint32_t)piece));
@@ -686,10 +689,11 @@ __device__ __forceinline__ Item find_item(const AttentionParams& p, const SplitP
         // tiles of sequence s0 + lane; -1 for one without rows
         auto tiles_of = [&](int s0) {
             int first, kv, rows, lo, hi;
+            bool blind;
             if (s0 + lane >= p.b.n_seqs) return -1;
             if (!sequence_rows(p, s0 + lane, &first, &kv, &rows)) { if (item == 0) latch(p.status); return -1; }
             if (rows == 0) return -1;
-            position_range(p, s0 + lane, first, rows, &lo, &hi);
+            position_range(p, s0 + lane, first, rows, &lo, &hi, &blind);
             return tile_range(p, kv, lo, hi).count;
         };
         int tiles = tiles_of(0), total = __reduce_add_sync(0xFFFFFFFFu, max(tiles, 0));
@@ -728,7 +732,7 @@ __device__ __forceinline__ Item find_item(const AttentionParams& p, const SplitP
     const bool ordered = sequence_rows(p, it.seq, &it.first, &it.kv, &it.rows);
     if (lane == 0 && (!ordered || it.rows > p.b.max_rows || __ldg(p.b.kv_len + it.seq) > it.kv)) latch(p.status);
     if (!ordered || it.rows == 0) return it;
-    position_range(p, it.seq, it.first, it.rows, &it.lo, &it.hi);
+    position_range(p, it.seq, it.first, it.rows, &it.lo, &it.hi, &it.blind);
     it.rows = min(it.rows, p.b.max_rows);
     const int count = tile_range(p, it.kv, it.lo, it.hi).count;
     if (pl.target == 0) { it.begin = 0; it.end = count; }
@@ -768,6 +772,7 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
             const uint64_t table = reinterpret_cast<uint64_t>(p.b.block_table + (long long)it.seq * p.b.table_stride);
             cold[0] = it.kv; cold[1] = it.lo; cold[2] = it.hi;
             cold[3] = it.begin + sub; cold[4] = pl.per_head_log2; cold[5] = range.sink_tiles; cold[6] = range.first;
+            cold[7] = it.blind ? -1 : it.lo;
             cold[8] = (uint32_t)table; cold[9] = (uint32_t)(table >> 32);
         }
         if (lane < 4 * NC) cold[12 + lane] = lane < cols ? row_position(p.b, it.seq, it.first + (int)(lane * pl.share_magic >> 16)) : -1;
@@ -786,7 +791,7 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
                 } else {
                     o.at = K::kPool ? 2 * ((long long)pg * p.c.stride_page + (long long)slot0 * p.c.stride_token + (long long)head * p.c.stride_head)
                                     : (long long)pg * p.c.stride_page;
-                    const int lo = k.lo_pos(), hi = k.hi_pos();
+                    const int lo = k.lo_whole(), hi = k.hi_pos();
                     o.flags = t0 + kTile - 1 <= min(lo, k.kv() - 1) && (p.window == 0 || hi - t0 < p.window || t0 + kTile <= p.sinks) ? 3 : 2;
                 }
             }

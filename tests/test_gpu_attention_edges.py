@@ -2,9 +2,10 @@
 whose entries are out of order, values of very different size.  Bounds as in test_gpu_attention."""
 import numpy as np
 import pytest
+import torch
 
 from live_common import Case
-from test_gpu_attention import Setup, ctx, pk  # noqa: F401  (fixtures)
+from test_gpu_attention import DEV, TAGS, Setup, ctx, pk  # noqa: F401  (fixtures)
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +30,16 @@ def test_huge_values_in_unseen_pool_tokens(pk, ctx, rows, window):
     s.q = s.q[:clean]
     want, tol = s.reference(window, case=seen)
     assert np.all(np.abs(out[:clean].double().cpu().numpy() - want) <= tol)
+
+
+@pytest.mark.parametrize("tag", TAGS)
+@pytest.mark.parametrize("rows", [2, 30, 200])
+def test_rows_that_see_nothing_do_not_widen_the_window(pk, ctx, tag, rows):
+    """Rows at negative positions (padding) beside windowed ones: pages that only they could have seen may be gone."""
+    pos = list(range(900 - rows + 1, 900))
+    pos.insert(rows // 2, -1)
+    s = Setup(pk, tag, 2, 4, 64, 16, 32, Case([900], [rows], [pos]))
+    first = (pos[0] - 99) // 16                             # page of the first token in the earliest row's window
+    s.keep["table"][0, 1:first] = torch.arange(first - 1, dtype=torch.int32, device=DEV) * -7 - 1
+    out = s.check(ctx, 100, 5)
+    assert (out[rows // 2] == 0).all()
