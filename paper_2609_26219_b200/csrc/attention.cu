@@ -2,7 +2,6 @@
 #include <math.h>
 
 #include <algorithm>
-#include <atomic>
 
 #include "attention.cuh"
 #include "attention_rows.cuh"
@@ -142,18 +141,6 @@ int fill_pool(patchkv_ctx* ctx, const patchkv_geom* g, const patchkv_pool* q, in
 
 constexpr int kSms = 148;                        // B200; only sizes launches, so that results don't depend on the context
 
-// Warps and ring depth of the split kernels: sixteen warps hide the latency of the page look-ups and of the operand
-// work best where 128 registers a thread are enough (8 columns), the ring takes what shared memory is left.
-constexpr int split_warps(bool pool, int nc) { return !pool && nc <= 2 ? 16 : 8; }
-template <int KF, int VF, int D, int NC>
-struct SplitShape {
-    static constexpr int kWarps = split_warps(KF == FMT_BF16, NC);
-    static constexpr int kBytes = kTile * ((KF == FMT_BF16 ? 2 * D : KF == FMT_INT8 ? D : D / 2) + (VF == FMT_BF16 ? 2 * D : VF == FMT_INT8 ? D : D / 2) + 32) + 256;
-    static constexpr int kFit = 220 * 1024 / (kWarps * kBytes);
-    static constexpr int kStages = kFit > 4 ? 4 : kFit;
-    static_assert(kStages >= 2, "the ring needs two stages");
-};
-
 // How a call is served.
 struct AttentionPlan {
     int nc;                     // columns of a lane of the split kernel; 0: another kernel
@@ -212,89 +199,6 @@ AttentionPlan plan_attention(const patchkv_geom* g, int tag, const patchkv_batch
         a.partial_bytes = (uint64_t)a.max_items * H * a.item_stride * 4;
     }
     return a;
-}
-
-// Opts a kernel into `bytes` of dynamic shared memory, once per device (a bit each; the attribute is per device and sticks).
-cudaError_t allow_smem(const void* kernel, int bytes, std::atomic<uint64_t>* done) {
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
-    if (bit && (done->load(std::memory_order_acquire) & bit)) return cudaSuccess;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == cudaSuccess) done->fetch_or(bit, std::memory_order_release);
-    return e;
-}
-
-template <int KF, int VF, int D, int NC, bool G32>
-cudaError_t launch_split(const AttentionParams& p, const SplitPlan& pl, int groups, cudaStream_t stream) {
-    using S = SplitShape<KF, VF, D, NC>;
-    using K = SplitKernel<KF, VF, D, NC, S::kStages, S::kWarps, G32>;
-    constexpr int smem = K::kSmem > K::kMerge ? K::kSmem : K::kMerge;
-    auto kernel = attention_split_kernel<KF, VF, D, NC, S::kStages, S::kWarps, G32>;
-    static std::atomic<uint64_t> allowed{0};
-    cudaError_t e = allow_smem((const void*)kernel, smem, &allowed);
-    if (e != cudaSuccess) return e;
-    e = launch_pdl(kernel, dim3(pl.max_items, groups), dim3(S::kWarps * 32), smem, stream, p, pl);
-    if (e != cudaSuccess || pl.target == 0) return e;
-    const dim3 grid(p.b.n_seqs, p.c.H, (NC == 1 ? 2 : 2 * NC) * (D / 16) / 4);
-    if (pl.max_items > 16 * p.b.n_seqs) return launch_pdl(attention_join_kernel<KF == FMT_BF16, D, NC, 16>, grid, dim3(512), 0, stream, p, pl);
-    return launch_pdl(attention_join_kernel<KF == FMT_BF16, D, NC, 4>, grid, dim3(128), 0, stream, p, pl);
-}
-template <int D, int NC, bool G32>
-cudaError_t launch_split_tag(const AttentionParams& p, const SplitPlan& pl, int groups, cudaStream_t s) {
-    switch (p.c.tag) {
-        case PATCHKV_TAG_INT8: return launch_split<FMT_INT8, FMT_INT8, D, NC, G32>(p, pl, groups, s);
-        case PATCHKV_TAG_INT4: return launch_split<FMT_INT8, FMT_INT4, D, NC, G32>(p, pl, groups, s);
-        default: return launch_split<FMT_INT4, FMT_INT4, D, NC, G32>(p, pl, groups, s);
-    }
-}
-template <int D, int NC>
-cudaError_t launch_split_group(const AttentionParams& p, const SplitPlan& pl, int groups, cudaStream_t s) {
-    if (p.c.tag == PATCHKV_TAG_BF16) return launch_split<FMT_BF16, FMT_BF16, D, NC, true>(p, pl, groups, s);
-    return p.c.G == 32 ? launch_split_tag<D, NC, true>(p, pl, groups, s) : launch_split_tag<D, NC, false>(p, pl, groups, s);
-}
-template <int D>
-cudaError_t launch_split_columns(const AttentionParams& p, const SplitPlan& pl, int nc, int groups, cudaStream_t s) {
-    return nc == 1 ? launch_split_group<D, 1>(p, pl, groups, s) : nc == 2 ? launch_split_group<D, 2>(p, pl, groups, s) : launch_split_group<D, 4>(p, pl, groups, s);
-}
-
-template <int KF, int VF, int D, bool IMAGE, bool ONE, bool FINE>
-cudaError_t launch_rows_kernel(const AttentionParams& p, const RowsPlan& pl, cudaStream_t stream) {
-    auto kernel = attention_rows_kernel<KF, VF, D, IMAGE, ONE, FINE>;
-    static std::atomic<uint64_t> allowed{0};
-    const cudaError_t e = allow_smem((const void*)kernel, RowsSmem<D>::kLaunch, &allowed);
-    if (e != cudaSuccess) return e;
-    return launch_pdl(kernel, dim3(pl.tiles * p.c.H * p.b.n_seqs * pl.splits), dim3(rows_threads(IMAGE)), RowsSmem<D>::kLaunch, stream, p, pl);
-}
-template <int KF, int VF, int D, bool FINE>
-cudaError_t launch_rows(const AttentionParams& p, const RowsPlan& pl, cudaStream_t stream) {
-    cudaError_t e;
-    if (pl.images) {
-        e = launch_pdl(attention_image_kernel<KF, VF, D, FINE>, dim3(pl.steps, p.c.H, p.b.n_seqs), dim3(kImageThreads), 0, stream, p, pl);
-        if (e != cudaSuccess) return e;
-        constexpr int F = KF == FMT_BF16 ? FMT_BF16 : FMT_INT8;
-        e = launch_rows_kernel<F, F, D, true, false, FINE>(p, pl, stream);
-    } else if ((long long)std::min(p.b.max_rows, p.b.n_rows) * p.share <= kRowTile) {
-        e = launch_rows_kernel<KF, VF, D, false, true, FINE>(p, pl, stream);
-    } else {
-        e = launch_rows_kernel<KF, VF, D, false, false, FINE>(p, pl, stream);
-    }
-    if (e != cudaSuccess || pl.splits == 1) return e;
-    return launch_pdl(attention_rows_join_kernel<D>, dim3((unsigned)(((long long)p.b.n_rows * p.Hq + 3) / 4)), dim3(128), 0, stream, p, pl);
-}
-template <int KF, int VF, int D>
-cudaError_t launch_rows_type(const AttentionParams& p, const RowsPlan& pl, cudaStream_t s) {
-    return p.f16 ? launch_rows<KF, VF, D, true>(p, pl, s) : launch_rows<KF, VF, D, false>(p, pl, s);
-}
-template <int D>
-cudaError_t launch_rows_tag(const AttentionParams& p, const RowsPlan& pl, cudaStream_t s) {
-    switch (p.c.tag) {
-        case PATCHKV_TAG_BF16: return launch_rows<FMT_BF16, FMT_BF16, D, false>(p, pl, s);
-        case PATCHKV_TAG_INT8: return launch_rows_type<FMT_INT8, FMT_INT8, D>(p, pl, s);
-        case PATCHKV_TAG_INT4: return launch_rows_type<FMT_INT8, FMT_INT4, D>(p, pl, s);
-        default: return launch_rows_type<FMT_INT4, FMT_INT4, D>(p, pl, s);
-    }
 }
 
 bool aligned_rows(const void* x, int64_t stride_row, int64_t stride_head) {
@@ -365,15 +269,15 @@ extern "C" int patchkv_attention(patchkv_ctx* ctx, const patchkv_geom* g, const 
         pl.max_items = plan.max_items; pl.target = plan.target;
         pl.heads_log2 = log2_exact(plan.heads); pl.per_head_log2 = log2_exact(plan.warps_per_head);
         pl.share_magic = (65536u + p.share - 1) / p.share;
-        PKV_CUDA(ctx, p.c.D == 128 ? launch_split_columns<128>(p, pl, plan.nc, plan.groups, stream)
-                                   : launch_split_columns<64>(p, pl, plan.nc, plan.groups, stream));
+        PKV_CUDA(ctx, p.c.D == 128 ? launch_split<128>(p, pl, plan.nc, plan.groups, stream)
+                                   : launch_split<64>(p, pl, plan.nc, plan.groups, stream));
         return PATCHKV_OK;
     }
     if (plan.row_tiles && aligned && aligned_rows(a->out, a->out_stride_row, a->out_stride_head)) {
         uint8_t* ws = static_cast<uint8_t*>(a->workspace);
         const RowsPlan pl = {reinterpret_cast<float*>(ws + plan.image_bytes + plan.meta_bytes), plan.row_tiles, plan.row_splits,
                              plan.image_steps ? ws : nullptr, reinterpret_cast<uint32_t*>(ws + plan.image_bytes), plan.image_steps};
-        PKV_CUDA(ctx, p.c.D == 128 ? launch_rows_tag<128>(p, pl, stream) : launch_rows_tag<64>(p, pl, stream));
+        PKV_CUDA(ctx, p.c.D == 128 ? launch_rows<128>(p, pl, stream) : launch_rows<64>(p, pl, stream));
         return PATCHKV_OK;
     }
     auto kernel = a->type == PATCHKV_ROWS_F16 ? attention_any_kernel<PATCHKV_ROWS_F16> : attention_any_kernel<PATCHKV_ROWS_BF16>;

@@ -40,6 +40,9 @@ struct RowsPlan {
     uint32_t* meta;                             // of each image: 4 words of absent tokens, 1 word `lost`, 3 unused
     int32_t steps;                              // of a sequence in the two
 };
+// The image, row and join kernels of a call for head dimension D, 64 or 128 (attention_rows_launch.cuh).
+template <int D>
+cudaError_t launch_rows(const AttentionParams& p, const RowsPlan& pl, cudaStream_t s);
 __device__ __forceinline__ long long image_index(const AttentionParams& p, const RowsPlan& pl, int seq, int step, int head) {
     return ((long long)seq * pl.steps + step) * p.c.H + head;
 }
@@ -273,7 +276,7 @@ __device__ __forceinline__ bool whole_step(const AttentionParams& p, int kv, int
 }
 // Values that are not finite were taken out of the masked steps (of an image: of all); a row that sees such a value gets it here.
 // (Rare: element by element, from the pages.)
-__device__ __noinline__ void add_lost(const AttentionParams& p, const RowsPlan& pl, const StepPlace& at, float (&o)[32], int c0, int pos) {
+inline __device__ __noinline__ void add_lost(const AttentionParams& p, const RowsPlan& pl, const StepPlace& at, float (&o)[32], int c0, int pos) {
     const int vf = v_format(p.c.tag), D = p.c.D;
     for (int j = at.begin; j < at.end; j++) {
         const int step = at.range.tile(j), t0 = step * kRowTile;

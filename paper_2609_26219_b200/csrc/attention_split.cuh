@@ -38,6 +38,13 @@ struct SplitPlan {
     int32_t heads_log2, per_head_log2;          // heads of a CTA, warps that share a head's tiles: powers of two
     uint32_t share_magic;                       // row of a column n < 16: n * share_magic >> 16
 };
+// The split kernels for head dimension D (64, 128) and 4 * nc columns, and the join where there is one (attention_split_launch.cuh).
+template <int D>
+cudaError_t launch_split(const AttentionParams& p, const SplitPlan& pl, int nc, int groups, cudaStream_t s);
+
+// Warps and ring depth of the kernels: sixteen warps hide the latency of the page look-ups and of the operand
+// work best where 128 registers a thread are enough (8 columns), the ring takes what shared memory is left.
+constexpr int split_warps(bool pool, int nc) { return !pool && nc <= 2 ? 16 : 8; }
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool live) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
