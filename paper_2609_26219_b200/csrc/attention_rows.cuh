@@ -147,8 +147,8 @@ struct RowsBars {
     uint64_t q_ready[2], s_ready[2], p_ready[2], o_ready[2], k_full[2], k_empty[2], v_full[2], v_empty[2], drained;
     alignas(16) uint32_t absent[4][8];          // per step (mod 4): tokens whose page is out of range; word 4: `lost` of an image
     uint32_t tmem;
-    int32_t abort, lo, hi, blind, lost;         // smallest and largest position not below 0; a row is; a value that is not finite was
-                                                // taken out of a tile that needs a mask
+    int32_t abort, lo, hi, least, lost;         // smallest and largest position not below 0; smallest of all; a value that is not finite
+                                                // was taken out of a tile that needs a mask
 };
 static_assert(sizeof(RowsBars) <= 512 && offsetof(RowsBars, absent) % 16 == 0, "barrier area");
 
@@ -270,9 +270,10 @@ __device__ __forceinline__ void image_operands(uint4 (&hi)[4], uint4 (&lo)[4], c
         }
     }
 }
-struct StepPlace { TileRange range; int seq, head, kv, lo, hi, begin, end; bool blind, order4; };
-__device__ __forceinline__ bool whole_step(const AttentionParams& p, int kv, int lo, int hi, bool blind, int t0) {
-    return !blind && t0 + kRowTile - 1 <= min(lo, kv - 1) && (p.window == 0 || hi - t0 < p.window || t0 + kRowTile <= p.sinks);
+struct StepPlace { TileRange range; int seq, head, kv, last, hi, begin, end; bool order4; };
+// A step that every row sees whole: up to token `last`, which is the earliest row's position or the cache's end.
+__device__ __forceinline__ bool whole_step(const AttentionParams& p, int last, int hi, int t0) {
+    return t0 + kRowTile - 1 <= last && (p.window == 0 || hi - t0 < p.window || t0 + kRowTile <= p.sinks);
 }
 // Values that are not finite were taken out of the masked steps (of an image: of all); a row that sees such a value gets it here.
 // (Rare: element by element, from the pages.)
@@ -280,7 +281,7 @@ inline __device__ __noinline__ void add_lost(const AttentionParams& p, const Row
     const int vf = v_format(p.c.tag), D = p.c.D;
     for (int j = at.begin; j < at.end; j++) {
         const int step = at.range.tile(j), t0 = step * kRowTile;
-        if (pl.images ? pl.meta[image_index(p, pl, at.seq, step, at.head) * 8 + 4] == 0 : whole_step(p, at.kv, at.lo, at.hi, at.blind, t0)) continue;
+        if (pl.images ? pl.meta[image_index(p, pl, at.seq, step, at.head) * 8 + 4] == 0 : whole_step(p, at.last, at.hi, t0)) continue;
         for (int t = t0; t < t0 + kRowTile; t++) {
             if (t > min(pos, at.kv - 1) || !sees(p, pos, t)) continue;
             const int lp = div_page(p.c, t), slot = t - lp * p.c.P;
@@ -318,8 +319,7 @@ struct RowsKernel {
     const AttentionParams& p;
     RowsBars& bars;
     uint32_t smem;
-    int seq, head, kv, lo, hi, begin, end;                      // steps [begin, end) of the range
-    bool blind;
+    int seq, head, kv, last, hi, begin, end;                    // steps [begin, end) of the range
     TileRange range;
 
     __device__ __forceinline__ RowsKernel(const AttentionParams& p_, RowsBars& b) : p(p_), bars(b) {}
@@ -327,8 +327,8 @@ struct RowsKernel {
     // The same for a whole warp: all of its lanes go on, or none.
     __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, wait(bar, parity)); }
     // Seen by some row (or by none): only then does a token's slot take part.
-    __device__ __forceinline__ bool any_sees(int t) const { return t <= min(hi, kv - 1) && sees(p, lo, t); }
-    __device__ __forceinline__ bool whole(int t0) const { return whole_step(p, kv, lo, hi, blind, t0); }
+    __device__ __forceinline__ bool any_sees(int t) const { return t <= min(hi, kv - 1) && sees(p, bars.lo, t); }
+    __device__ __forceinline__ bool whole(int t0) const { return whole_step(p, last, hi, t0); }
 
     // ---- the warps that bring K and V
     // A warp takes TOK = 32 tokens of a step, or 16 where a call has one tile only and the second tile's softmax warps bring too; kPer lanes share a
@@ -827,7 +827,7 @@ struct RowsKernel {
                 float fixed[32];
 #pragma unroll
                 for (int c = 0; c < 32; c++) fixed[c] = o[c];
-                add_lost(p, pl, {range, seq, head, kv, lo, hi, begin, end, blind, VF == FMT_INT4}, fixed, 32 * k, pos);
+                add_lost(p, pl, {range, seq, head, kv, last, hi, begin, end, VF == FMT_INT4}, fixed, 32 * k, pos);
 #pragma unroll
                 for (int c = 0; c < 32; c++) o[c] = fixed[c];
             }
@@ -891,8 +891,8 @@ __global__ void __launch_bounds__(rows_threads(IMAGE), 1) attention_rows_kernel(
             mbar_init(&bars.k_empty[i], 1); mbar_init(&bars.v_empty[i], 1);
         }
         mbar_init(&bars.drained, 1);
-        bars.abort = 0; bars.blind = 0; bars.lost = 0;
-        bars.lo = 0x7FFFFFFF; bars.hi = -1;
+        bars.abort = 0; bars.lost = 0;
+        bars.lo = bars.least = 0x7FFFFFFF; bars.hi = -1;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     pdl_wait();
@@ -911,10 +911,23 @@ __global__ void __launch_bounds__(rows_threads(IMAGE), 1) attention_rows_kernel(
     const int tiles = !ONE && m_end - m0 > kRowTile ? 2 : 1;
     __syncthreads();
     // positions of the CTA's rows (one below 0 sees nothing: no window need reach back for it)
-    for (int r = m0 / p.share + threadIdx.x; r <= (m_end - 1) / p.share; r += kThreads) {
-        const int x = row_position(p.b, seq, first + r);
-        if (x >= 0) atomicMin(&bars.lo, x); else bars.blind = 1;
-        atomicMax(&bars.hi, x);
+    {
+        uint32_t low = 0x7FFFFFFFu;                             // below 0 is above that
+        int least = 0x7FFFFFFF, most = -1;
+        for (int r = m0 / p.share + threadIdx.x; r <= (m_end - 1) / p.share; r += kThreads) {
+            const int x = row_position(p.b, seq, first + r);
+            low = min(low, (uint32_t)x);
+            least = min(least, x);
+            most = max(most, x);
+        }
+        low = __reduce_min_sync(0xFFFFFFFFu, low);
+        least = __reduce_min_sync(0xFFFFFFFFu, least);
+        most = __reduce_max_sync(0xFFFFFFFFu, most);
+        if ((threadIdx.x & 31) == 0) {
+            atomicMin(&bars.lo, (int)low);
+            atomicMin(&bars.least, least);
+            atomicMax(&bars.hi, most);
+        }
     }
     if (warp == kIssuer / 32) tc_alloc(&bars.tmem, 512);
     tc_before();
@@ -923,8 +936,9 @@ __global__ void __launch_bounds__(rows_threads(IMAGE), 1) attention_rows_kernel(
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&bars.tmem);
     K k(p, bars);
     k.smem = base; k.seq = seq; k.head = head; k.kv = kv;
-    k.lo = bars.lo; k.hi = bars.hi; k.blind = bars.blind != 0;
-    k.range = step_range(p, kv, k.lo, k.hi);
+    k.hi = bars.hi;
+    k.last = min(bars.least, kv - 1);
+    k.range = step_range(p, kv, bars.lo, k.hi);
     k.begin = (int)((long long)k.range.count * split / pl.splits);
     k.end = (int)((long long)k.range.count * (split + 1) / pl.splits);
     if (warp < (ONE ? 4 : kProducer0 / 32)) {
