@@ -147,6 +147,7 @@ struct RowsBars {
     uint64_t q_ready[2], s_ready[2], p_ready[2], o_ready[2], k_full[2], k_empty[2], v_full[2], v_empty[2], drained;
     alignas(16) uint32_t absent[4][8];          // per step (mod 4): tokens whose page is out of range; word 4: `lost` of an image
     uint32_t tmem;
+    int32_t first_row, last_row;                // the CTA's rows
     int32_t abort, lo, hi, least, lost;         // smallest and largest position not below 0; smallest of all; a value that is not finite
                                                 // was taken out of a tile that needs a mask
 };
@@ -270,6 +271,15 @@ __device__ __forceinline__ void image_operands(uint4 (&hi)[4], uint4 (&lo)[4], c
         }
     }
 }
+// Whether one of the rows at given positions sees token t (they may lie further apart than the window).  Asked only of tokens
+// between the rows' positions that have no page.
+inline __device__ __noinline__ bool some_row_sees(const AttentionParams& p, int first, int last, int t) {
+    for (int r = first; r <= last; r++) {
+        const int x = __ldg(p.b.pos + r);
+        if (x >= t && sees(p, x, t)) return true;
+    }
+    return false;
+}
 struct StepPlace { TileRange range; int seq, head, kv, last, hi, begin, end; bool order4; };
 // A step that every row sees whole: up to token `last`, which is the earliest row's position or the cache's end.
 __device__ __forceinline__ bool whole_step(const AttentionParams& p, int last, int hi, int t0) {
@@ -328,6 +338,10 @@ struct RowsKernel {
     __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, wait(bar, parity)); }
     // Seen by some row (or by none): only then does a token's slot take part.
     __device__ __forceinline__ bool any_sees(int t) const { return t <= min(hi, kv - 1) && sees(p, bars.lo, t); }
+    // The same exactly, for what counts as an error.
+    __device__ __forceinline__ bool really_seen(int t) const {
+        return any_sees(t) && (!p.b.pos || p.window == 0 || some_row_sees(p, bars.first_row, bars.last_row, t));
+    }
     __device__ __forceinline__ bool whole(int t0) const { return whole_step(p, last, hi, t0); }
 
     // ---- the warps that bring K and V
@@ -352,7 +366,7 @@ struct RowsKernel {
     __device__ __forceinline__ uint32_t missing(const Pages& g, int w) const {
         const int lane = threadIdx.x & 31, page = __shfl_sync(0xFFFFFFFFu, g.page, lane >> 4);
         const uint32_t gone = __ballot_sync(0xFFFFFFFFu, lane < TOK && page < 0 && any_sees(g.t0 + TOK * w + lane));
-        if (gone && lane == 0) latch(p.status);
+        if (gone >> lane & 1u && really_seen(g.t0 + TOK * w + lane)) latch(p.status);
         return gone;
     }
     // The thread's 32 channels of pass i, K or V: codes and their scale.
@@ -582,7 +596,7 @@ struct RowsKernel {
         const uint32_t gone[4] = {absent.x, absent.y, absent.z, absent.w};
 #pragma unroll
         for (int k = 0; k < 4; k++)
-            if (gone[k] >> lane & 1u && any_sees(t0 + 32 * k + lane)) latch(p.status);
+            if (gone[k] >> lane & 1u && really_seen(t0 + 32 * k + lane)) latch(p.status);
     }
 
     // Bit c: this row sees column c0 + c.
@@ -923,6 +937,7 @@ __global__ void __launch_bounds__(rows_threads(IMAGE), 1) attention_rows_kernel(
         low = __reduce_min_sync(0xFFFFFFFFu, low);
         least = __reduce_min_sync(0xFFFFFFFFu, least);
         most = __reduce_max_sync(0xFFFFFFFFu, most);
+        if (threadIdx.x == 0) { bars.first_row = first + m0 / p.share; bars.last_row = first + (m_end - 1) / p.share; }
         if ((threadIdx.x & 31) == 0) {
             atomicMin(&bars.lo, (int)low);
             atomicMin(&bars.least, least);

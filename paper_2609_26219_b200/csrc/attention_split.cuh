@@ -213,6 +213,17 @@ struct SplitKernel {
         const int v = (int)lds32(cold + 12) + (i << lds32(cold + 16)), sinks = (int)lds32(cold + 20);
         return (v < sinks ? v : (int)lds32(cold + 24) + v - sinks) * kTile;
     }
+    // Whether one of the rows sees a token of the tile: rows at given positions may lie further apart than the window.
+    __device__ __forceinline__ bool some_row_sees(int t0) const {
+        if (!p.b.pos || p.window == 0 || t0 < p.sinks) return true;
+        bool seen = false;
+#pragma unroll 1
+        for (int c = 0; c < 4 * NC; c++) {
+            const int x = (int)lds32(cold + 48 + 4 * c);
+            seen = seen || (x >= t0 && x - (t0 + kTile - 1) < p.window);
+        }
+        return seen;
+    }
     __device__ __forceinline__ const int32_t* table() const {
         const uint2 x = lds64(cold + 32);
         return reinterpret_cast<const int32_t*>((uint64_t)x.y << 32 | x.x);
@@ -787,7 +798,7 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
         struct Place { long long at; uint32_t row0, flags; };        // flags: bit 0 whole, bit 1 has a page
         auto place_of = [&](int i) {
             Place o = {0, 0, 0};
-            if (i < n) {
+            if (i < n && k.some_row_sees(k.first_token(i))) {
                 const int t0 = k.first_token(i), lp = div_page(p.c, t0), slot0 = t0 - lp * p.c.P;
                 const int pg = __ldg(k.table() + lp);
                 o.row0 = (uint32_t)slot0 * p.c.H + head;

@@ -43,3 +43,19 @@ def test_rows_that_see_nothing_do_not_widen_the_window(pk, ctx, tag, rows):
     s.keep["table"][0, 1:first] = torch.arange(first - 1, dtype=torch.int32, device=DEV) * -7 - 1
     out = s.check(ctx, 100, 5)
     assert (out[rows // 2] == 0).all()
+
+
+@pytest.mark.parametrize("tag", TAGS)
+@pytest.mark.parametrize("near", [1, 20, 80, 200])
+@pytest.mark.parametrize("splits", [False, True])
+def test_pages_between_rows_may_be_gone(pk, ctx, tag, near, splits):
+    """Rows further apart than the window: pages between their windows may be gone; one that a row sees may not."""
+    total = 4000 if splits else 1400
+    pos = list(range(100, 100 + near)) + list(range(total - near, total))
+    s = Setup(pk, tag, 2, 4, 64, 16, 32, Case([total], [2 * near], [pos]))
+    a, b = (100 + near - 1) // 16 + 1, (total - near - 63) // 16
+    s.keep["table"][0, a:b] = s.n_pages + 5
+    s.check(ctx, 64, 3)
+    s.keep["table"][0, b] = -1
+    s.run(ctx, 64, 3)
+    assert ctx.query_status() == pk.E_BOUNDS
