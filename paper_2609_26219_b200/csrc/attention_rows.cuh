@@ -1057,17 +1057,18 @@ __global__ void __launch_bounds__(kImageThreads) attention_image_kernel(const At
     if (threadIdx.x < 8) pl.meta[image_index(p, pl, seq, step, head) * 8 + threadIdx.x] = meta[threadIdx.x];
 }
 
-// Joins the pieces of split rows: a warp per query vector.
+// Joins the pieces of split rows: a warp per query vector, sequence by sequence as they were made (a search for a row's sequence would
+// lose those in front of row_start entries that descend).
 template <int D>
 __global__ void __launch_bounds__(128) attention_rows_join_kernel(const AttentionParams p, const RowsPlan pl) {
     pdl_wait();
-    const long long n = (long long)p.b.n_rows * p.Hq, vec = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31;
-    if (vec >= n) return;
-    const int row = (int)(vec / p.Hq), hq = (int)(vec - (long long)row * p.Hq);
-    const int s = find_sequence(p.b, row);
     int first, kv, rows;
-    if (s < 0 || !sequence_rows(p, s, &first, &kv, &rows) || row - first >= p.b.max_rows) return;
+    if (!sequence_rows(p, blockIdx.y, &first, &kv, &rows)) return;
+    const long long n = (long long)p.b.n_rows * p.Hq, at = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (at >= (long long)min(rows, p.b.max_rows) * p.Hq) return;
+    const int row = first + (int)(at / p.Hq), hq = (int)(at % p.Hq);
+    const long long vec = (long long)row * p.Hq + hq;
     const float* ml = pl.partial + pl.splits * n * D;
     float top = kNoMax, sum = 0.0f, y[D / 32];
     for (int i = 0; i < pl.splits; i++) top = fmaxf(top, __ldg(ml + (i * n + vec) * 2));

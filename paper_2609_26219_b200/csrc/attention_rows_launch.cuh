@@ -31,7 +31,8 @@ cudaError_t launch_rows_one(const AttentionParams& p, const RowsPlan& pl, cudaSt
         e = launch_rows_kernel<KF, VF, D, false, false, FINE>(p, pl, stream);
     }
     if (e != cudaSuccess || pl.splits == 1) return e;
-    return launch_pdl(attention_rows_join_kernel<D>, dim3((unsigned)(((long long)p.b.n_rows * p.Hq + 3) / 4)), dim3(128), 0, stream, p, pl);
+    const long long vectors = (long long)std::min(p.b.max_rows, p.b.n_rows) * p.Hq;          // of a sequence at most
+    return launch_pdl(attention_rows_join_kernel<D>, dim3((unsigned)((vectors + 3) / 4), p.b.n_seqs), dim3(128), 0, stream, p, pl);
 }
 template <int KF, int VF, int D>
 cudaError_t launch_rows_type(const AttentionParams& p, const RowsPlan& pl, cudaStream_t s) {

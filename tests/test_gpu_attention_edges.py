@@ -59,3 +59,17 @@ def test_pages_between_rows_may_be_gone(pk, ctx, tag, near, splits):
     s.keep["table"][0, b] = -1
     s.run(ctx, 64, 3)
     assert ctx.query_status() == pk.E_BOUNDS
+
+
+@pytest.mark.parametrize("tag", TAGS)
+@pytest.mark.parametrize("rows", [1, 40, 300])
+def test_a_sequence_before_descending_entries_keeps_its_rows(pk, ctx, tag, rows):
+    """row_start that descends leaves out the sequence whose entries those are and no other, also where the tokens are split."""
+    s = Setup(pk, tag, 1, 2, 64, 16, 32, Case([3000, 50], [rows, rows]))
+    s.keep["start"][2] = 0
+    out = s.run(ctx)
+    assert ctx.query_status() == pk.E_BOUNDS
+    assert (out[rows:] == 5).all()
+    s.q = s.q[:rows]
+    want, tol = s.reference(case=Case([3000], [rows]))
+    assert np.all(np.abs(out[:rows].double().cpu().numpy() - want) <= tol)
