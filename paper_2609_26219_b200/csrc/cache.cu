@@ -33,7 +33,9 @@ __device__ __forceinline__ bool find_slot(const RowParams& p, int r, bool first,
     const int s = find_sequence(p.b, r);
     if (s < 0) return false;                                // a row of no sequence: not an error
     const int pos = row_position(p.b, s, r);
-    bool ok = !WRITE || !p.b.pos || r == __ldg(p.b.row_start + s) || __ldg(p.b.pos + r - 1) < pos;
+    // (A sequence that starts below row 0 has no row in front of row 0 to look at.)
+    bool ok = __ldg(p.b.row_start + s) >= 0;
+    if (WRITE && ok && p.b.pos && r > __ldg(p.b.row_start + s)) ok = __ldg(p.b.pos + r - 1) < pos;
     const int pg = ok ? locate(p.b, p.c, s, pos, slot) : -1;
     if (pg < 0) {
         if (first) latch_bounds(p.status);

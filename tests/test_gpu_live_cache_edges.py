@@ -1,0 +1,35 @@
+"""patchkv_cache_append and patchkv_cache_read on batches whose row_start entries are out of order, and every fp16 value."""
+import numpy as np
+import pytest
+import torch
+
+from live_common import BF16, Case, Layout, build_tables, device_batch, random_rows
+from test_gpu_live_cache import DEV, ctx, geom_of, pk  # noqa: F401  (fixtures)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("H,D,G", [(4, 64, 32), (2, 10, 5)])
+def test_a_sequence_that_starts_below_row_0_is_left_out(pk, ctx, H, D, G):
+    """No position in front of the first one is looked at for its rows: they are skipped and latched.  (The array of positions
+    has an entry in front of it here, one that would let row 0 pass.)"""
+    lay, case = Layout(3, H, D, 16, G), Case([40, 40], [3, 2], [[0, 5, 39], [1, 2]])
+    rng = np.random.default_rng(5)
+    table, n_pages = build_tables(case, 16, rng)
+    batch, keep = device_batch(pk, case, table, DEV)
+    padded = torch.cat([torch.tensor([-5], dtype=torch.int32, device=DEV), keep["pos"]])
+    batch.pos = padded[1:].data_ptr()
+    keep["start"][0] = -1
+    pages = rng.integers(0, 256, (n_pages, lay.page_bytes()), dtype=np.uint8)
+    dev = torch.from_numpy(pages).to(DEV)
+    k, v = random_rows(rng, 5, H, D, BF16), random_rows(rng, 5, H, D, BF16)
+    cache, g = pk.make_qpool(dev, 3, n_pages), geom_of(pk, lay)
+    ctx.cache_append(g, cache, 0, batch, k.to(DEV), v.to(DEV))
+    assert ctx.query_status() == pk.E_BOUNDS
+    for r, pos in ((3, 1), (4, 2)):                         # the other sequence's rows
+        lay.put(pages[table[1, 0]], pos, k[r].double().numpy(), v[r].double().numpy())
+    assert np.array_equal(dev.cpu().numpy(), pages)
+    ko, vo = torch.full_like(k, 9.0, device=DEV), torch.full_like(v, 9.0, device=DEV)
+    ctx.cache_read(g, cache, 0, batch, ko, vo)
+    assert ctx.query_status() == pk.E_BOUNDS
+    assert (ko[:3] == 9).all() and (vo[:3] == 9).all() and not (ko[3:] == 9).all(2).any()
