@@ -441,8 +441,9 @@ typedef struct {
  * for 8 bits and 7 for 4: the quantiser of patchkv_quantize_gather.  Values must be finite; a group whose amax / qmax
  * exceeds 65504 gets an infinite scale and zero codes.  Only the codes and scales of the rows' own slots are written.
  * Positions of one sequence must be strictly ascending, and no two sequences may write the same slot.  A row whose
- * position is outside [0, kv_len) or whose page is out of range, and a row whose position is not above that of the row
- * in front of it, is skipped and PATCHKV_E_BOUNDS is latched.
+ * position is outside [0, kv_len) or whose page is out of range, a row whose position is not above that of the row
+ * in front of it, and the rows of a sequence whose row_start entries descend or lie outside [0, n_rows], are skipped and
+ * PATCHKV_E_BOUNDS is latched (entries that descend may take rows of other sequences with them).
  * One launch, asynchronous on `stream`, no allocation, no workspace; it can be captured. */
 PATCHKV_API int patchkv_cache_append(patchkv_ctx* ctx, const patchkv_geom* geom, const patchkv_qpool* cache, int layer,
                                      const patchkv_batch* batch, const patchkv_rows* rows, void* stream);

@@ -32,10 +32,10 @@ template <bool WRITE>
 __device__ __forceinline__ bool find_slot(const RowParams& p, int r, bool first, uint8_t** page, int* slot) {
     const int s = find_sequence(p.b, r);
     if (s < 0) return false;                                // a row of no sequence: not an error
-    const int pos = row_position(p.b, s, r);
+    const int pos = row_position(p.b, s, r), a = __ldg(p.b.row_start + s);
     // (A sequence that starts below row 0 has no row in front of row 0 to look at.)
-    bool ok = __ldg(p.b.row_start + s) >= 0;
-    if (WRITE && ok && p.b.pos && r > __ldg(p.b.row_start + s)) ok = __ldg(p.b.pos + r - 1) < pos;
+    bool ok = a >= 0 && __ldg(p.b.row_start + s + 1) <= p.b.n_rows;
+    if (WRITE && ok && p.b.pos && r > a) ok = __ldg(p.b.pos + r - 1) < pos;
     const int pg = ok ? locate(p.b, p.c, s, pos, slot) : -1;
     if (pg < 0) {
         if (first) latch_bounds(p.status);
@@ -43,6 +43,15 @@ __device__ __forceinline__ bool find_slot(const RowParams& p, int r, bool first,
     }
     *page = p.c.base + (long long)pg * p.c.stride_page;
     return true;
+}
+
+// Entries of row_start that descend or lie outside [0, n_rows] are an error, although the rows of such a sequence may be found in
+// none.  The launch's threads share the sequences; at a kernel's end, so that nothing waits for these loads.
+__device__ __forceinline__ void check_entries(const BatchDev& b, int32_t* status, uint32_t thread, uint32_t threads) {
+    for (uint32_t s = thread; s < (uint32_t)b.n_seqs; s += threads) {
+        const int a = __ldg(b.row_start + s), e = __ldg(b.row_start + s + 1);
+        if (a < 0 || e < a || e > b.n_rows) latch_bounds(status);
+    }
 }
 
 template <int TYPE>
@@ -172,7 +181,7 @@ __global__ void __launch_bounds__(kRowThreads) cache_append_kernel(const __grid_
             }
         }
         if (v0 == v_first) found = find_slot<true>(p, r, lane == 0 && v_first == 0, &page, &slot);      // while the row is on its way
-        if (!found) return;                                  // the same for all lanes
+        if (!found) break;                                   // the same for all lanes
 #pragma unroll
         for (int i = 0; i < kBatch; i++) {
             if (v0 + stride * i >= p.vecs) break;
@@ -185,6 +194,7 @@ __global__ void __launch_bounds__(kRowThreads) cache_append_kernel(const __grid_
                                  p.seg, vec < p.vecs);
         }
     }
+    check_entries(p.b, p.status, blockIdx.x * kRowThreads + threadIdx.x, (uint32_t)p.b.n_rows * p.parts * 32);
 }
 
 // Eight codes and their scale -> eight channels.  An integer u < 2^23 in the low bits of 2^23's pattern is the float
@@ -226,9 +236,9 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
     uint8_t* page = nullptr;
     int slot = 0;
     pdl_wait();
-    if (!find_slot<false>(p, r, lane == 0 && v_first == 0, &page, &slot)) return;
+    const bool found = find_slot<false>(p, r, lane == 0 && v_first == 0, &page, &slot);
     constexpr int kBatch = 4;
-    for (int v0 = v_first; v0 < p.vecs; v0 += stride * kBatch) {
+    for (int v0 = found ? v_first : p.vecs; v0 < p.vecs; v0 += stride * kBatch) {
         uint2 kc[kBatch], vc[kBatch];
         uint16_t ks[kBatch], vs[kBatch];
 #pragma unroll
@@ -250,6 +260,7 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
             }
         }
     }
+    check_entries(p.b, p.status, blockIdx.x * kRowThreads + threadIdx.x, (uint32_t)p.b.n_rows * p.parts * 32);
 }
 
 // Any geometry, any strides: one thread per (row, section, head) walks the head's groups with byte accesses to the page.
@@ -259,6 +270,7 @@ __global__ void __launch_bounds__(kRowThreads) cache_rows_any_kernel(const RowPa
     const uint32_t i = blockIdx.x * kRowThreads + threadIdx.x, per_row = 2u * p.c.H;
     const int r = (int)(i / per_row), q = (int)(i - (uint32_t)r * per_row), h = q >> 1;
     if (r >= p.b.n_rows) return;
+    check_entries(p.b, p.status, i, (uint32_t)p.b.n_rows * per_row);
     uint8_t* page = nullptr;
     int slot = 0;
     if (!find_slot<WRITE>(p, r, q == 0, &page, &slot)) return;

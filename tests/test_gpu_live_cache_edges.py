@@ -33,3 +33,28 @@ def test_a_sequence_that_starts_below_row_0_is_left_out(pk, ctx, H, D, G):
     ctx.cache_read(g, cache, 0, batch, ko, vo)
     assert ctx.query_status() == pk.E_BOUNDS
     assert (ko[:3] == 9).all() and (vo[:3] == 9).all() and not (ko[3:] == 9).all(2).any()
+
+
+@pytest.mark.parametrize("H,D,G", [(4, 64, 32), (2, 10, 5)])
+@pytest.mark.parametrize("start", [[0, 3, 0], [0, 3, 2, 5], [0, 2, 9]])
+def test_entries_out_of_order_are_latched(pk, ctx, H, D, G, start):
+    """row_start that descends or runs past n_rows is an error of both calls; nothing but slots of the batch is written."""
+    lay = Layout(3, H, D, 16, G)
+    rng = np.random.default_rng(5)
+    n_seqs, n = len(start) - 1, 5
+    table, n_pages = build_tables(Case([40] * n_seqs, [1] * n_seqs), 16, rng)
+    batch, keep = device_batch(pk, Case([40] * n_seqs, [1] * n_seqs), table, DEV, n_rows=n)
+    keep["start"].copy_(torch.tensor(start, dtype=torch.int32))
+    pages = rng.integers(0, 256, (n_pages, lay.page_bytes()), dtype=np.uint8)
+    dev = torch.from_numpy(pages).to(DEV)
+    k, v = random_rows(rng, n, H, D, BF16).to(DEV), random_rows(rng, n, H, D, BF16).to(DEV)
+    cache, g = pk.make_qpool(dev, 3, n_pages), geom_of(pk, lay)
+    ctx.cache_append(g, cache, 0, batch, k, v)
+    assert ctx.query_status() == pk.E_BOUNDS
+    unused = sorted(set(range(n_pages)) - set(table.reshape(-1).tolist()))
+    assert np.array_equal(dev.cpu().numpy()[unused], pages[unused])
+    ctx.cache_read(g, cache, 0, batch, k, v)
+    assert ctx.query_status() == pk.E_BOUNDS
+    keep["start"].copy_(torch.arange(n_seqs + 1, dtype=torch.int32))
+    ctx.cache_append(g, cache, 0, batch, k, v)              # in order again: no error
+    assert ctx.query_status() == 0
