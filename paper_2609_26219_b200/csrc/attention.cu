@@ -26,7 +26,7 @@ __global__ void __launch_bounds__(kAnyThreads) attention_any_kernel(const Attent
     if (threadIdx.x == 0 && (!ordered || rows > p.b.max_rows)) latch(p.status);
     if (!ordered || (int)blockIdx.x >= rows) return;
     const int r = first + blockIdx.x;
-    if (__ldg(p.b.kv_len + s) > kv && threadIdx.x == 0) latch(p.status);
+    if (p.b.kv_len[s] > kv && threadIdx.x == 0) latch(p.status);
     const int pos = row_position(p.b, s, r);
     const uint16_t* qs = p.q + (long long)r * p.q_stride_row + (long long)hq * p.q_stride_head;
     for (int c = threadIdx.x; c < p.c.D; c += kAnyThreads)
@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(kAnyThreads) attention_any_kernel(const Attent
         off_v[threadIdx.x] = -1;
         if (t < end && sees(p, pos, t)) {
             const int lp = div_page(p.c, t), slot = t - lp * p.c.P;
-            const int page = __ldg(p.b.block_table + (long long)s * p.b.table_stride + lp);
+            const int page = p.b.block_table[(long long)s * p.b.table_stride + lp];
             if (page < 0 || page >= p.c.n_pages) {
                 latch(p.status);
             } else if (p.c.tag == PATCHKV_TAG_BF16) {

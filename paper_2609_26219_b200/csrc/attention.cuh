@@ -27,10 +27,10 @@ __device__ __forceinline__ bool sees(const AttentionParams& p, int pos, int t) {
 
 // First row of a sequence and the tokens it may use; false when its row_start entries are out of order or out of range.
 __device__ __forceinline__ bool sequence_rows(const AttentionParams& p, int s, int* first, int* kv, int* rows = nullptr) {
-    const int a = __ldg(p.b.row_start + s), e = __ldg(p.b.row_start + s + 1);
+    const int a = p.b.row_start[s], e = p.b.row_start[s + 1];
     *first = a;
     const long long cap = (long long)p.b.table_stride * p.c.P;
-    long long n = min(__ldg(p.b.kv_len + s), p.b.max_kv_len);
+    long long n = min(p.b.kv_len[s], p.b.max_kv_len);
     if (n > cap) n = cap;
     *kv = n < 0 ? 0 : (int)n;
     if (rows) *rows = e - a;

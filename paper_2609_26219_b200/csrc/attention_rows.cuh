@@ -224,9 +224,9 @@ __device__ __forceinline__ bool finite_only(uint4& x) {
 // 32 channels of a token (piece c of its row) as fp16 in channel order.
 template <int F>
 __device__ __forceinline__ void image_operands(uint4 (&o)[4], const uint8_t* row, int c, uint32_t s, uint32_t m0, uint32_t m1) {
-    const uint4 a = __ldg(reinterpret_cast<const uint4*>(row + c * (F == FMT_INT8 ? 32 : 16)));
+    const uint4 a = *reinterpret_cast<const uint4*>(row + c * (F == FMT_INT8 ? 32 : 16));
     if (F == FMT_INT8) {
-        const uint4 b = __ldg(reinterpret_cast<const uint4*>(row + c * 32 + 16));
+        const uint4 b = *reinterpret_cast<const uint4*>(row + c * 32 + 16);
         const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
         for (int i = 0; i < 4; i++) {
@@ -245,12 +245,12 @@ __device__ __forceinline__ void image_operands(uint4 (&o)[4], const uint8_t* row
 // K of an image: also what the rounding took away.
 template <int F>
 __device__ __forceinline__ void image_operands(uint4 (&hi)[4], uint4 (&lo)[4], const uint8_t* row, int c, uint32_t s, uint32_t m0, uint32_t m1) {
-    const uint4 a = __ldg(reinterpret_cast<const uint4*>(row + c * (F == FMT_INT8 ? 32 : 16)));
+    const uint4 a = *reinterpret_cast<const uint4*>(row + c * (F == FMT_INT8 ? 32 : 16));
     auto ordered = [](const uint4& x) {                         // 0 4, 1 5, 2 6, 3 7 -> 0 1, 2 3, 4 5, 6 7
         return make_uint4(__byte_perm(x.x, x.y, 0x5410), __byte_perm(x.z, x.w, 0x5410), __byte_perm(x.x, x.y, 0x7632), __byte_perm(x.z, x.w, 0x7632));
     };
     if (F == FMT_INT8) {
-        const uint4 b = __ldg(reinterpret_cast<const uint4*>(row + c * 32 + 16));
+        const uint4 b = *reinterpret_cast<const uint4*>(row + c * 32 + 16);
         const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
         for (int i = 0; i < 4; i++) {
@@ -275,7 +275,7 @@ __device__ __forceinline__ void image_operands(uint4 (&hi)[4], uint4 (&lo)[4], c
 // between the rows' positions that have no page.
 inline __device__ __noinline__ bool some_row_sees(const AttentionParams& p, int first, int last, int t) {
     for (int r = first; r <= last; r++) {
-        const int x = __ldg(p.b.pos + r);
+        const int x = p.b.pos[r];
         if (x >= t && sees(p, x, t)) return true;
     }
     return false;
@@ -295,7 +295,7 @@ inline __device__ __noinline__ void add_lost(const AttentionParams& p, const Row
         for (int t = t0; t < t0 + kRowTile; t++) {
             if (t > min(pos, at.kv - 1) || !sees(p, pos, t)) continue;
             const int lp = div_page(p.c, t), slot = t - lp * p.c.P;
-            const int page = __ldg(p.b.block_table + (long long)at.seq * p.b.table_stride + lp);
+            const int page = p.b.block_table[(long long)at.seq * p.b.table_stride + lp];
             if (page < 0 || page >= p.c.n_pages) continue;
             for (int c = 0; c < 32; c++) {
                 float v;
@@ -380,14 +380,14 @@ struct RowsKernel {
         scale = 0;
         if (!live) return;
         const uint8_t* codes = pg + (is_v ? p.c.v_codes : 0u) + row * (F == FMT_INT8 ? D : D / 2) + c * (F == FMT_INT8 ? 32 : 16);
-        const uint4 a = __ldg(reinterpret_cast<const uint4*>(codes));
+        const uint4 a = *reinterpret_cast<const uint4*>(codes);
         w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
         if (F == FMT_INT8) {
-            const uint4 b = __ldg(reinterpret_cast<const uint4*>(codes + 16));
+            const uint4 b = *reinterpret_cast<const uint4*>(codes + 16);
             w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
         }
         const uint32_t s = (row * (D / p.c.G) + c * 32 / p.c.G) * 2 + (is_v ? p.c.v_scales : p.c.k_scales);
-        scale = __ldg(reinterpret_cast<const uint16_t*>(pg + s));
+        scale = *reinterpret_cast<const uint16_t*>(pg + s);
     }
 
     // Images: one lane copies.  Returns with the copies in flight counted in `sent` (bit 2 st + (0 for K, 1 for V): a copy into stage st
@@ -503,7 +503,7 @@ struct RowsKernel {
         if (j >= end) return -1;
         const int t = range.tile(j) * kRowTile + tok;
         if (t >= kv) return -1;
-        const int pg = __ldg(p.b.block_table + (long long)seq * p.b.table_stride + div_page(p.c, t));
+        const int pg = p.b.block_table[(long long)seq * p.b.table_stride + div_page(p.c, t)];
         return pg >= 0 && pg < p.c.n_pages ? pg : -1;
     }
     // In a step that needs a mask a value that is not finite must not meet the weight 0 of a row that does not see it: it is taken out
@@ -917,7 +917,7 @@ __global__ void __launch_bounds__(rows_threads(IMAGE), 1) attention_rows_kernel(
     const int seq = id % p.b.n_seqs, tile = pl.tiles - 1 - id / p.b.n_seqs;
     int first, kv, rows;
     const bool ordered = sequence_rows(p, seq, &first, &kv, &rows);
-    if (threadIdx.x == 0 && (!ordered || rows > p.b.max_rows || (rows > 0 && __ldg(p.b.kv_len + seq) > kv))) latch(p.status);
+    if (threadIdx.x == 0 && (!ordered || rows > p.b.max_rows || (rows > 0 && p.b.kv_len[seq] > kv))) latch(p.status);
     if (!ordered) return;
     rows = min(rows, p.b.max_rows);
     const int m0 = tile * 2 * kRowTile, m_end = min(rows * p.share, m0 + 2 * kRowTile);
@@ -998,7 +998,7 @@ __global__ void __launch_bounds__(kImageThreads) attention_image_kernel(const At
     if (!sequence_rows(p, seq, &first, &kv, &rows) || rows == 0) return;
     hi = kv - 1;
     if (!p.b.pos) {                                             // the last positions: what no row sees needs no image
-        const int a = __ldg(p.b.kv_len + seq) - rows;
+        const int a = p.b.kv_len[seq] - rows;
         lo = max(-1, a);
         hi = a + min(rows, p.b.max_rows) - 1;
     }
@@ -1017,7 +1017,7 @@ __global__ void __launch_bounds__(kImageThreads) attention_image_kernel(const At
         if (t < kv) {
             const int lp = div_page(p.c, t);
             slot = t - lp * p.c.P;
-            page = __ldg(p.b.block_table + (long long)seq * p.b.table_stride + lp);
+            page = p.b.block_table[(long long)seq * p.b.table_stride + lp];
             if (page < 0 || page >= p.c.n_pages) {
                 page = -1;
                 if (c == 0) atomicOr(&meta[tok >> 5], 1u << (tok & 31));
@@ -1031,13 +1031,13 @@ __global__ void __launch_bounds__(kImageThreads) attention_image_kernel(const At
             const long long o = (long long)page * p.c.stride_page + (long long)slot * p.c.stride_token + (long long)head * p.c.stride_head + 32 * c;
 #pragma unroll
             for (int q = 0; q < 4; q++) {
-                ko[q] = __ldg(reinterpret_cast<const uint4*>(p.c.k + o) + q);
-                vo[q] = __ldg(reinterpret_cast<const uint4*>(p.c.v + o) + q);
+                ko[q] = *(reinterpret_cast<const uint4*>(p.c.k + o) + q);
+                vo[q] = *(reinterpret_cast<const uint4*>(p.c.v + o) + q);
             }
         } else {
             const uint8_t* pg = p.c.base + (long long)page * p.c.stride_page;
             const uint32_t row = (uint32_t)slot * p.c.H + head, sc = (row * (D / p.c.G) + c * 32 / p.c.G) * 2;
-            uint32_t ks = __ldg(reinterpret_cast<const uint16_t*>(pg + p.c.k_scales + sc)), vs = __ldg(reinterpret_cast<const uint16_t*>(pg + p.c.v_scales + sc));
+            uint32_t ks = *reinterpret_cast<const uint16_t*>(pg + p.c.k_scales + sc), vs = *reinterpret_cast<const uint16_t*>(pg + p.c.v_scales + sc);
             ks |= ks << 16; vs |= vs << 16;
             if (FINE) image_operands<KF>(ko, kr, pg + row * (KF == FMT_INT8 ? D : D / 2), c, ks, m0, m1);
             else image_operands<KF>(ko, pg + row * (KF == FMT_INT8 ? D : D / 2), c, ks, m0, m1);
@@ -1071,16 +1071,16 @@ __global__ void __launch_bounds__(128) attention_rows_join_kernel(const Attentio
     const long long vec = (long long)row * p.Hq + hq;
     const float* ml = pl.partial + pl.splits * n * D;
     float top = kNoMax, sum = 0.0f, y[D / 32];
-    for (int i = 0; i < pl.splits; i++) top = fmaxf(top, __ldg(ml + (i * n + vec) * 2));
+    for (int i = 0; i < pl.splits; i++) top = fmaxf(top, ml[(i * n + vec) * 2]);
 #pragma unroll
     for (int k = 0; k < D / 32; k++) y[k] = 0.0f;
 #pragma unroll 4
     for (int i = 0; i < pl.splits; i++) {
-        const float2 x = __ldg(reinterpret_cast<const float2*>(ml + (i * n + vec) * 2));
+        const float2 x = *reinterpret_cast<const float2*>(ml + (i * n + vec) * 2);
         const float f = fast_exp2(x.x - top);
         sum = fmaf(f, x.y, sum);
 #pragma unroll
-        for (int k = 0; k < D / 32; k++) y[k] = fmaf(f, __ldg(pl.partial + (i * n + vec) * D + lane + 32 * k), y[k]);
+        for (int k = 0; k < D / 32; k++) y[k] = fmaf(f, pl.partial[(i * n + vec) * D + lane + 32 * k], y[k]);
     }
     uint16_t* o = p.out + (long long)row * p.out_stride_row + (long long)hq * p.out_stride_head;
 #pragma unroll

@@ -147,7 +147,7 @@ __device__ __forceinline__ TileRange tile_range(const AttentionParams& p, int kv
 __device__ __forceinline__ void position_range(const AttentionParams& p, int s, int first, int rows, int* lo, int* hi, int* least) {
     const int n = min(rows, p.b.max_rows);
     if (!p.b.pos) {
-        const int a = __ldg(p.b.kv_len + s) - rows;
+        const int a = p.b.kv_len[s] - rows;
         *least = max(-1, a);
         *lo = max(0, a);
         *hi = a + n - 1;
@@ -158,7 +158,7 @@ __device__ __forceinline__ void position_range(const AttentionParams& p, int s, 
     *hi = -1;
 #pragma unroll 1
     for (int i = 0; i < n; i++) {
-        const int x = __ldg(p.b.pos + first + i);
+        const int x = p.b.pos[first + i];
         low = min(low, (uint32_t)x);
         *least = min(*least, x);
         *hi = max(*hi, x);
@@ -269,17 +269,17 @@ struct SplitKernel {
 #pragma unroll
                 for (int k = 0; k < kMT; k++)
 #pragma unroll
-                    for (int e = 0; e < 2; e++) qf[nt][k][e] = live ? __ldg(reinterpret_cast<const uint32_t*>(q + 16 * k + 8 * e + 2 * t)) : 0u;
+                    for (int e = 0; e < 2; e++) qf[nt][k][e] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * k + 8 * e + 2 * t) : 0u;
             } else {
 #pragma unroll
                 for (int j = 0; j < kChunks; j++) {           // 8 channels of each chunk, in the order the codes of a word come out
                     uint4 v = make_uint4(0, 0, 0, 0);
                     if (live) {
                         if (kK4) {
-                            v = __ldg(reinterpret_cast<const uint4*>(q + 32 * j + 8 * t));
+                            v = *reinterpret_cast<const uint4*>(q + 32 * j + 8 * t);
                         } else {
-                            const uint2 a = __ldg(reinterpret_cast<const uint2*>(q + 32 * j + 4 * t));
-                            const uint2 b = __ldg(reinterpret_cast<const uint2*>(q + 32 * j + 16 + 4 * t));
+                            const uint2 a = *reinterpret_cast<const uint2*>(q + 32 * j + 4 * t);
+                            const uint2 b = *reinterpret_cast<const uint2*>(q + 32 * j + 16 + 4 * t);
                             v = make_uint4(a.x, a.y, b.x, b.y);
                         }
                     }
@@ -736,7 +736,7 @@ __device__ __forceinline__ Item find_item(const AttentionParams& p, const SplitP
         if (it.seq < 0) return it;
     }
     const bool ordered = sequence_rows(p, it.seq, &it.first, &it.kv, &it.rows);
-    if (lane == 0 && (!ordered || it.rows > p.b.max_rows || __ldg(p.b.kv_len + it.seq) > it.kv)) latch(p.status);
+    if (lane == 0 && (!ordered || it.rows > p.b.max_rows || p.b.kv_len[it.seq] > it.kv)) latch(p.status);
     if (!ordered || it.rows == 0) return it;
     position_range(p, it.seq, it.first, it.rows, &it.lo, &it.hi, &it.least);
     it.rows = min(it.rows, p.b.max_rows);
@@ -800,7 +800,7 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
             Place o = {0, 0, 0};
             if (i < n && k.some_row_sees(k.first_token(i))) {
                 const int t0 = k.first_token(i), lp = div_page(p.c, t0), slot0 = t0 - lp * p.c.P;
-                const int pg = __ldg(k.table() + lp);
+                const int pg = *(k.table() + lp);
                 o.row0 = (uint32_t)slot0 * p.c.H + head;
                 if (pg < 0 || pg >= p.c.n_pages) {
                     latch(p.status);
@@ -936,7 +936,7 @@ __global__ void __launch_bounds__(32 * WARPS) attention_join_kernel(const Attent
     const int at = blockIdx.z * 32 + lane;                   // numbers 4 at .. 4 at + 3: one register of four lanes, four columns
     int ch0, col0;
     place<POOL, D, NC>(at >> 3, 0, &ch0, &col0);
-    auto piece = [&](int i) { return __ldg(reinterpret_cast<const float4*>(part + i * step) + at); };
+    auto piece = [&](int i) { return *(reinterpret_cast<const float4*>(part + i * step) + at); };
     float4 x[kFirst];
 #pragma unroll
     for (int i = 0; i < kFirst; i++)
@@ -947,7 +947,7 @@ __global__ void __launch_bounds__(32 * WARPS) attention_join_kernel(const Attent
         for (int i = 0; i < kMaxPieces / 32; i++) {
             m[i] = kNoMax; l[i] = 0.0f;
             if (32 * i + lane < n) {
-                const float2 z = __ldg(reinterpret_cast<const float2*>(part + (32 * i + lane) * step + kRegs * 32 + 2 * c));
+                const float2 z = *reinterpret_cast<const float2*>(part + (32 * i + lane) * step + kRegs * 32 + 2 * c);
                 m[i] = z.x; l[i] = z.y;
             }
             top = fmaxf(top, m[i]);

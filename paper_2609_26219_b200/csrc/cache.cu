@@ -32,10 +32,10 @@ template <bool WRITE>
 __device__ __forceinline__ bool find_slot(const RowParams& p, int r, bool first, uint8_t** page, int* slot) {
     const int s = find_sequence(p.b, r);
     if (s < 0) return false;                                // a row of no sequence: not an error
-    const int pos = row_position(p.b, s, r), a = __ldg(p.b.row_start + s);
+    const int pos = row_position(p.b, s, r), a = p.b.row_start[s];
     // (A sequence that starts below row 0 has no row in front of row 0 to look at.)
-    bool ok = a >= 0 && __ldg(p.b.row_start + s + 1) <= p.b.n_rows;
-    if (WRITE && ok && p.b.pos && r > a) ok = __ldg(p.b.pos + r - 1) < pos;
+    bool ok = a >= 0 && p.b.row_start[s + 1] <= p.b.n_rows;
+    if (WRITE && ok && p.b.pos && r > a) ok = p.b.pos[r - 1] < pos;
     const int pg = ok ? locate(p.b, p.c, s, pos, slot) : -1;
     if (pg < 0) {
         if (first) latch_bounds(p.status);
@@ -49,7 +49,7 @@ __device__ __forceinline__ bool find_slot(const RowParams& p, int r, bool first,
 // none.  The launch's threads share the sequences; at a kernel's end, so that nothing waits for these loads.
 __device__ __forceinline__ void check_entries(const BatchDev& b, int32_t* status, uint32_t thread, uint32_t threads) {
     for (uint32_t s = thread; s < (uint32_t)b.n_seqs; s += threads) {
-        const int a = __ldg(b.row_start + s), e = __ldg(b.row_start + s + 1);
+        const int a = b.row_start[s], e = b.row_start[s + 1];
         if (a < 0 || e < a || e > b.n_rows) latch_bounds(status);
     }
 }
@@ -175,8 +175,8 @@ __global__ void __launch_bounds__(kRowThreads) cache_append_kernel(const __grid_
                 const long long src = (long long)r * p.rows.stride_row + row_element(p, vec * CH);
 #pragma unroll
                 for (int q = 0; q < CH / 8; q++) {
-                    kw[i][q] = __ldg(reinterpret_cast<const uint4*>(p.rows.k + src) + q);
-                    vw[i][q] = __ldg(reinterpret_cast<const uint4*>(p.rows.v + src) + q);
+                    kw[i][q] = *(reinterpret_cast<const uint4*>(p.rows.k + src) + q);
+                    vw[i][q] = *(reinterpret_cast<const uint4*>(p.rows.v + src) + q);
                 }
             }
         }

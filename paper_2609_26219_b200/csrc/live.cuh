@@ -1,4 +1,6 @@
 // What the live-cache calls (cache.cu, attention.cu) share: the batch and the page pool as a kernel sees them.
+// All their kernels read global memory with plain loads: launched as dependents, they are resident while the kernel in front of
+// them writes what they will read, which the read-only path rules out (and the compiler may move such loads across the wait).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -37,23 +39,23 @@ __device__ __forceinline__ int find_sequence(const BatchDev& b, int r) {
     int lo = 0, hi = b.n_seqs;          // answer in [lo, hi]
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
-        if (__ldg(b.row_start + mid + 1) > r) hi = mid; else lo = mid + 1;
+        if (b.row_start[mid + 1] > r) hi = mid; else lo = mid + 1;
     }
-    return lo < b.n_seqs && __ldg(b.row_start + lo) <= r ? lo : -1;
+    return lo < b.n_seqs && b.row_start[lo] <= r ? lo : -1;
 }
 
 // Position of row r of sequence s (which ends at row `end`).
 __device__ __forceinline__ int row_position(const BatchDev& b, int s, int r) {
-    return b.pos ? __ldg(b.pos + r) : __ldg(b.kv_len + s) - (__ldg(b.row_start + s + 1) - r);
+    return b.pos ? b.pos[r] : b.kv_len[s] - (b.row_start[s + 1] - r);
 }
 
 // Page and slot of a position inside [0, kv_len); page -1 when it is out of range.
 __device__ __forceinline__ int locate(const BatchDev& b, const CacheDev& c, int s, int pos, int* slot) {
-    if (pos < 0 || pos >= __ldg(b.kv_len + s)) return -1;
+    if (pos < 0 || pos >= b.kv_len[s]) return -1;
     const int lp = div_page(c, pos);
     *slot = pos - lp * c.P;
     if (lp >= b.table_stride) return -1;
-    const int page = __ldg(b.block_table + (long long)s * b.table_stride + lp);
+    const int page = b.block_table[(long long)s * b.table_stride + lp];
     return page >= 0 && page < c.n_pages ? page : -1;
 }
 
