@@ -167,7 +167,7 @@ AttentionPlan plan_attention(const patchkv_geom* g, int tag, const patchkv_batch
         // Whole CTAs along the query vectors; where they leave SMs idle the tokens are split, two steps a piece at least.
         const long long tiles = (cols + 2 * kRowTile - 1) / (2 * kRowTile), ctas = tiles * H * b->n_seqs;
         if (ctas > 1 << 24 || cols > 1 << 30) return a;
-        long long steps = (b->max_kv_len + kRowTile - 1) / kRowTile;
+        long long steps = ((long long)b->max_kv_len + kRowTile - 1) / kRowTile;
         if (window > 0) steps = std::min(steps, ((long long)window + sinks + b->max_rows) / kRowTile + 3);
         a.row_tiles = (int)tiles;
         a.row_splits = (int)std::max(1ll, std::min((long long)kSms / ctas, steps / 2));

@@ -1,4 +1,5 @@
 """CPU checks of the live-cache calls: what their kernels may use, and workspace sizes at the ends of the range."""
+import ctypes
 import os
 
 import pytest
@@ -14,3 +15,20 @@ def test_no_read_only_loads(name):
     loads that ask for memory that does not change while the kernel is there are not theirs to make."""
     text = open(os.path.join(CSRC, name)).read()
     assert "__ldg" not in text and "global.nc" not in text and "__restrict__" not in text
+
+
+def size(pk, geom, tag, hq, window=0, sinks=0, **batch):
+    fields = dict(struct_size=ctypes.sizeof(pk.Batch), n_seqs=1, n_rows=1, max_rows=1, max_kv_len=16384, table_stride=4,
+                  row_start=16, kv_len=16, block_table=16)
+    b = pk.Batch(**{**fields, **batch})
+    return pk.lib().patchkv_attention_workspace_bytes(ctypes.byref(geom), tag, ctypes.byref(b), hq, window, sinks)
+
+
+@pytest.mark.parametrize("rows", [40, 60])
+def test_workspace_of_the_longest_bound(pk, rows):
+    """max_kv_len is a bound, and 2^31 - 1 is one: the tokens are split as for any long context."""
+    g = pk.make_geom(1, 2, 64, 64, 0, 1e4, 16, 16, 32)
+    long = size(pk, g, 3, 4, n_rows=rows, max_rows=rows, max_kv_len=1 << 24)
+    assert long > 0
+    for kv in (2 ** 31 - 1, 2 ** 31 - 127, 2 ** 31 - 128):
+        assert size(pk, g, 3, 4, n_rows=rows, max_rows=rows, max_kv_len=kv) == long
