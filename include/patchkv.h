@@ -492,7 +492,8 @@ PATCHKV_API int patchkv_attention(patchkv_ctx* ctx, const patchkv_geom* geom, co
                                   const patchkv_attention_args* args, void* stream);
 
 /* Workspace of such a call; 0 if it needs none (or the arguments are invalid).  Depends on the geometry, the tag
- * (PATCHKV_TAG_BF16: a pool), n_seqs, n_rows, max_rows, max_kv_len, Hq, window and sinks.  Needs no GPU. */
+ * (PATCHKV_TAG_BF16: a pool), n_seqs, n_rows, max_rows, max_kv_len, Hq, window and sinks; the batch's arrays
+ * may be null.  Needs no GPU. */
 PATCHKV_API uint64_t patchkv_attention_workspace_bytes(const patchkv_geom* geom, int tag, const patchkv_batch* batch,
                                                        int n_q_heads, int window, int sinks);
 

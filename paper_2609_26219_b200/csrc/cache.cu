@@ -354,7 +354,7 @@ int fill_batch(patchkv_ctx* ctx, const char* who, const patchkv_batch* b, BatchD
     if (!b || b->struct_size != sizeof(patchkv_batch)) return fail(ctx, PATCHKV_E_INVALID, w + ": null batch or wrong struct_size");
     if (b->n_seqs < 0 || b->n_rows < 0 || b->max_rows < 0 || b->max_kv_len < 0 || b->table_stride < 0)
         return fail(ctx, PATCHKV_E_INVALID, w + ": negative count in the batch");
-    if (b->n_seqs > 0 && b->n_rows > 0 && (!b->row_start || !b->kv_len || (!b->block_table && b->table_stride > 0)))
+    if (ctx && b->n_seqs > 0 && b->n_rows > 0 && (!b->row_start || !b->kv_len || (!b->block_table && b->table_stride > 0)))
         return fail(ctx, PATCHKV_E_INVALID, w + ": null row_start, kv_len or block_table");
     o->row_start = b->row_start; o->kv_len = b->kv_len; o->pos = b->pos; o->block_table = b->block_table;
     o->n_seqs = b->n_seqs; o->n_rows = b->n_rows; o->max_rows = b->max_rows; o->max_kv_len = b->max_kv_len;

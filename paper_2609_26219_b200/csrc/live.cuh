@@ -72,7 +72,7 @@ __device__ __forceinline__ float scale_at(const uint8_t* scales, unsigned long l
     return half_bits_to_float((uint32_t)scales[2 * i] | (uint32_t)scales[2 * i + 1] << 8);
 }
 
-// Host side: validation, and the device form of the structs.
+// Host side: validation, and the device form of the structs.  Without a context (a size is asked for) arrays may be null.
 int fill_batch(patchkv_ctx* ctx, const char* who, const patchkv_batch* b, BatchDev* out);
 int fill_cache(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, const patchkv_qpool* q, int layer, CacheDev* out);
 int check_live_geometry(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, int layer);

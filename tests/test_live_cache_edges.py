@@ -32,3 +32,13 @@ def test_workspace_of_the_longest_bound(pk, rows):
     assert long > 0
     for kv in (2 ** 31 - 1, 2 ** 31 - 127, 2 ** 31 - 128):
         assert size(pk, g, 3, 4, n_rows=rows, max_rows=rows, max_kv_len=kv) == long
+
+
+@pytest.mark.parametrize("rows", [1, 40, 300])
+def test_workspace_size_needs_no_arrays(pk, rows):
+    """The size follows from numbers alone, so it can be asked for before the device arrays exist."""
+    g = pk.make_geom(1, 2, 64, 64, 0, 1e4, 16, 16, 32)
+    for tag in (0, 3):
+        want = size(pk, g, tag, 4, n_rows=rows, max_rows=rows)
+        assert want > 0
+        assert size(pk, g, tag, 4, n_rows=rows, max_rows=rows, row_start=None, kv_len=None, block_table=None) == want
