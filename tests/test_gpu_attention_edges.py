@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from live_common import Case
+from live_common import BF16, F16, Case, attention64
 from test_gpu_attention import DEV, TAGS, Setup, ctx, pk  # noqa: F401  (fixtures)
 
 pytestmark = pytest.mark.gpu
@@ -73,3 +73,35 @@ def test_a_sequence_before_descending_entries_keeps_its_rows(pk, ctx, tag, rows)
     s.q = s.q[:rows]
     want, tol = s.reference(case=Case([3000], [rows]))
     assert np.all(np.abs(out[:rows].double().cpu().numpy() - want) <= tol)
+
+
+@pytest.mark.parametrize("tag", TAGS)
+@pytest.mark.parametrize("rows", [1, 40, 130, 300])
+def test_a_loose_bound_on_the_lengths(pk, ctx, tag, rows):
+    """max_kv_len of 2^31 - 1: the same results.  Images of that many steps would pass what they may take, so 300 rows run as several CTAs
+    that convert the codes themselves."""
+    case = Case([700, 350], [rows, max(1, rows // 3)])
+    Setup(pk, tag, 2, 8, 64, 16, 32, case, max_kv=2 ** 31 - 1).check(ctx, 300, 4)
+    Setup(pk, tag, 1, 4, 128, 16, 32, case, dtype=F16 if tag else BF16, max_kv=2 ** 31 - 1).check(ctx)
+
+
+@pytest.mark.parametrize("tag", [0, 3])
+@pytest.mark.parametrize("rows", [1, 40])
+def test_long_caches(pk, ctx, tag, rows):
+    """Tens of thousands of tokens: many tiles a piece, and look-ups past the first 32 of a warp."""
+    s = Setup(pk, tag, 1, 2, 64, 16, 32, Case([40001], [rows]))
+    s.check(ctx)
+    s.check(ctx, 20000, 5000)
+
+
+@pytest.mark.parametrize("tag", [1, 2, 3])
+@pytest.mark.parametrize("rows", [1, 8])
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("scale", [0.125, 1.0, 5.0])
+def test_few_columns_see_whole_keys(pk, ctx, tag, rows, dtype, scale):
+    """Up to 16 columns the logits are those of code * scale, of any size: the bound has no term for a rounding of K."""
+    s = Setup(pk, tag, 2, 4, 64, 16, 32, Case([300], [rows]), dtype=dtype)
+    got = s.check(ctx, scale=scale)[:rows].double().cpu().numpy()
+    want, tol = attention64(s.q[:rows].double().numpy(), lambda b: s.kv(b)[0], lambda b: s.kv(b)[1], s.case, 2, scale, 0, 0, dtype,
+                            False, k_rounding=0.0)
+    assert np.all(np.abs(got - want) <= tol), np.max(np.abs(got - want) / tol)

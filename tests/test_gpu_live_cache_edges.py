@@ -3,8 +3,8 @@ import numpy as np
 import pytest
 import torch
 
-from live_common import BF16, Case, Layout, build_tables, device_batch, random_rows
-from test_gpu_live_cache import DEV, ctx, geom_of, pk  # noqa: F401  (fixtures)
+from live_common import BF16, F16, Case, Layout, build_tables, device_batch, random_rows
+from test_gpu_live_cache import DEV, ctx, geom_of, pk, reference_append  # noqa: F401  (fixtures)
 
 pytestmark = pytest.mark.gpu
 
@@ -58,3 +58,27 @@ def test_entries_out_of_order_are_latched(pk, ctx, H, D, G, start):
     keep["start"].copy_(torch.arange(n_seqs + 1, dtype=torch.int32))
     ctx.cache_append(g, cache, 0, batch, k, v)              # in order again: no error
     assert ctx.query_status() == 0
+
+
+@pytest.mark.parametrize("bits_tag", [1, 3])
+def test_every_fp16_value_as_group_maximum(pk, ctx, bits_tag):
+    """Every positive finite fp16 value as the maximum of a group, with neighbours that fall on and next to the half-way points
+    of its codes."""
+    lay = Layout(bits_tag, 4, 64, 16, 32)
+    top = 127 if bits_tag == 1 else 7
+    m = torch.arange(1, 0x7C00, dtype=torch.int16).view(F16)
+    n = -(-m.numel() // 8)
+    m = torch.cat([m, m[:n * 8 - m.numel()]]).view(n, 8, 1)
+    s = (m.double() / top).half().double()
+    half = (torch.floor(torch.arange(31, dtype=torch.float64) * (top / 31.0)) + 0.5) * s
+    x = torch.cat([m.double(), torch.minimum(half, m.double())], -1).to(F16).view(n, 4, 64)
+    rng = np.random.default_rng(3)
+    case = Case([n], [n])
+    table, n_pages = build_tables(case, 16, rng)
+    batch, keep = device_batch(pk, case, table, DEV)
+    pages = np.zeros((n_pages, lay.page_bytes()), np.uint8)
+    dev = torch.from_numpy(pages).to(DEV)
+    reference_append(lay, pages, case, table, x, x)
+    ctx.cache_append(geom_of(pk, lay), pk.make_qpool(dev, bits_tag, n_pages), 0, batch, x.to(DEV), x.to(DEV))
+    assert ctx.query_status() == 0
+    assert np.array_equal(dev.cpu().numpy(), pages)
