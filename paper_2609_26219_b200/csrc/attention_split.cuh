@@ -14,8 +14,10 @@
 //      largest; each 32-channel chunk is summed on its own in fp32 from a start value that takes the offset out again (-8 * sum of
 //      the chunk's q), then enters the logit with the token's fp32 scale: no rounding of K at all.
 //   V: v = (u * 2^-24) * S - offset * S in one half fma, S the token's scale times a power of two that follows the
-//      largest V scale seen: one rounding of 2^-12, as p's own to fp16.  For fp16 results, whose own rounding is no larger
-//      than those two, p is the sum of two fp16 numbers, for one more product per operand.
+//      V scales: one rounding, of 2^-12, as p's own to fp16, or of 2^-25 where v is subnormal.  For the latter to stay below
+//      2^-12 of a group's largest value S has to be 2^8 at least (8-bit codes: 2^4), and it is 2^15 at most: the power of two
+//      moves both ways, and a tile whose scales have a wider range goes through again for the smaller ones.  For fp16 results,
+//      whose own rounding is no larger than those two, p is the sum of two fp16 numbers, for one more product per operand.
 // Softmax on powers of two against a reference that is only moved when a logit exceeds it by more than 15 (p <= 2^15), to 3 below
 // the largest (fp16 then holds weights down to 2^-17 of it to all its bits): one vote per tile instead of a maximum across lanes.
 #pragma once
@@ -111,6 +113,11 @@ __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
 __device__ __forceinline__ uint32_t bf162_bits(float lo, float hi) {
     uint32_t d;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+__device__ __forceinline__ uint32_t add_u16x2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("add.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
 }
 __device__ __forceinline__ uint32_t both(float x) { return half2_bits(x, x); }
@@ -252,7 +259,7 @@ struct SplitKernel {
 #pragma unroll
                 for (int j = 0; j < 4; j++) acc[nt][i][j] = 0.0f;
     }
-    __device__ __forceinline__ void set_v_exp(int e) {       // -1 <= e <= 29: exact, a scale only grows
+    __device__ __forceinline__ void set_v_exp(int e) {       // -1 <= e <= 29: exact
         v_up0 = both(exp2i(min(e, 15)));
         v_up1 = both(exp2i(max(e - 15, 0)));
         v_most = (uint32_t)(30 - e) << 10;                   // exponent field x: s < 2^(x - 14), so s * 2^e stays at 2^15 at most
@@ -408,8 +415,19 @@ struct SplitKernel {
         for (int i = 0; i < kMT; i++) { acc[c >> 1][i][c & 1] *= keep; acc[c >> 1][i][2 + (c & 1)] *= keep; }
     }
 
-    // One tile: logits, weights, and the weighted values.
-    __device__ __forceinline__ void tile(uint32_t base, bool whole, bool present, int t0, uint32_t row0) {
+    // V scales of one pass have bit patterns in [v_most - kSpread, v_most): S in [2^8, 2^15), or [2^4, 2^15) (file header).
+    static constexpr int kSpread = (VF == FMT_INT8 ? 11 : 7) << 10;
+    // Largest magnitude of four halves, and the smallest that is not zero, minus 1.
+    __device__ __forceinline__ static void magnitudes(const uint32_t (&s)[2], uint32_t* top, int* low) {
+        const uint32_t a = s[0] & 0x7FFF7FFFu, b = s[1] & 0x7FFF7FFFu, most = __vmaxu2(a, b);
+        const uint32_t least = __vminu2(add_u16x2(a, 0xFFFFFFFFu), add_u16x2(b, 0xFFFFFFFFu));
+        *top = max(most & 0xFFFFu, most >> 16);
+        *low = (int)min(least & 0xFFFFu, least >> 16);
+    }
+
+    // One tile: logits, weights, and the weighted values.  `below`: 0, or the tile once more for its V scales below that bit pattern;
+    // returns the next such, 0 when all are done.
+    __device__ __forceinline__ uint32_t tile(uint32_t base, bool whole, bool present, int t0, uint32_t row0, uint32_t below) {
         float x[NC][2];                                                    // tokens g and g + 8
         if constexpr (kPool) {
             float y[NT][4];
@@ -487,7 +505,8 @@ struct SplitKernel {
 #pragma unroll
         for (int c = 0; c < NC; c++) most = fmaxf(most, fmaxf(x[c][0], x[c][1]) - ref[c]);
         // V scales of the lane's channels (one group: channels [g * D / 8, (g + 1) * D / 8)) for tokens 2t, 2t+1, 2t+8, 2t+9
-        uint32_t sp[2] = {0, 0}, top = 0;
+        uint32_t sp[2] = {0, 0}, top = 0, next = 0;
+        int low = 0;
         if constexpr (!kPool) {
             uint32_t s[4];
             const int group = g * (D / 8) / (G32 ? 32 : p.c.G);
@@ -500,11 +519,10 @@ struct SplitKernel {
             }
             sp[0] = s[0] | s[1] << 16;
             sp[1] = s[2] | s[3] << 16;
-            const uint32_t mag = __vmaxu2(sp[0] & 0x7FFF7FFFu, sp[1] & 0x7FFF7FFFu);
-            top = max(mag & 0xFFFFu, mag >> 16);
+            magnitudes(sp, &top, &low);
         }
         // One vote for the two references that may have to move.
-        if (__any_sync(0xFFFFFFFFu, most > kSplitTop || (!kPool && top >= v_most))) {
+        if (__any_sync(0xFFFFFFFFu, most > kSplitTop || (!kPool && (top >= v_most || low < (int)v_most - kSpread || below)))) {
 #pragma unroll
             for (int c = 0; c < NC; c++) {
                 float m = fmaxf(x[c][0], x[c][1]);
@@ -514,11 +532,16 @@ struct SplitKernel {
                 if (m > ref[c] + kSplitTop) rescale(c, m - kSplitPeak);
             }
             if constexpr (!kPool) {
-                uint32_t m = top >= 0x7C00u ? 0u : top;             // a scale that is not finite always gets here
+                if (below) {                                        // the weights are in the sums already
 #pragma unroll
-                for (int d = 1; d < 32; d <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-                const int from = v_exp(), to = min(from, 29 - (int)(m >> 10));
-                if (to < from) {
+                    for (int c = 0; c < NC; c++) sum[c] -= fast_exp2(x[c][0] - ref[c]) + fast_exp2(x[c][1] - ref[c]);
+#pragma unroll
+                    for (int k = 0; k < 2; k++) sp[k] &= __vcmpltu2(sp[k] & 0x7FFF7FFFu, below * 0x00010001u);
+                    magnitudes(sp, &top, &low);
+                }
+                const uint32_t m = __reduce_max_sync(0xFFFFFFFFu, top >= 0x7C00u ? 0u : top);   // a scale that is not finite always gets here
+                if (m >= v_most || (m && __any_sync(0xFFFFFFFFu, low < (int)v_most - kSpread))) {
+                    const int from = v_exp(), to = 29 - (int)(m >> 10);
                     const float keep = exp2i(to - from);
                     set_v_exp(to);
 #pragma unroll
@@ -527,6 +550,11 @@ struct SplitKernel {
                         for (int i = 0; i < kMT; i++)
 #pragma unroll
                             for (int k = 0; k < 4; k++) acc[nt][i][k] *= keep;
+                }
+                if (__any_sync(0xFFFFFFFFu, low < (int)v_most - kSpread)) {
+                    next = v_most - kSpread;
+#pragma unroll
+                    for (int k = 0; k < 2; k++) sp[k] &= __vcmpgeu2(sp[k] & 0x7FFF7FFFu, next * 0x00010001u);
                 }
             }
         }
@@ -560,7 +588,7 @@ struct SplitKernel {
 #pragma unroll
                     for (int k = 0; k < 4; k++) bad |= ((r[k] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
                 }
-                if (__any_sync(0xFFFFFFFFu, bad != 0)) { values_one_by_one(base, x, 0u); return; }
+                if (__any_sync(0xFFFFFFFFu, bad != 0)) { values_one_by_one(base, x, 0u); return 0; }
             }
 #pragma unroll
             for (int i = 0; i < kMT; i++) {
@@ -570,7 +598,7 @@ struct SplitKernel {
                 for (int nt = 0; nt < NT; nt++) mma_bf16(acc[nt][i], r[0], r[1], r[2], r[3], pf[nt][0], pf[nt][1]);
             }
         } else {
-            if (!whole && __any_sync(0xFFFFFFFFu, top >= 0x7C00u)) { values_one_by_one(base, x, row0); return; }
+            if (!whole && __any_sync(0xFFFFFFFFu, top >= 0x7C00u)) { values_one_by_one(base, x, row0); return 0; }
             uint32_t S[2], S16[2], off[2];
 #pragma unroll
             for (int k = 0; k < 2; k++) {
@@ -628,6 +656,7 @@ struct SplitKernel {
                 }
             }
         }
+        return next;
     }
 
     // Channel of accumulator (i, e) of this lane.
@@ -839,7 +868,9 @@ __global__ void __launch_bounds__(WARPS * 32) attention_split_kernel(const __gri
             cp_wait<STAGES - 1>();
             __syncwarp();
             const bool w = whole >> (STAGES - 1) & 1;
-            k.tile(base, w, present >> (STAGES - 1) & 1, w ? 0 : k.first_token(i), odd >> (STAGES - 1) & 1);
+            uint32_t below = 0;
+            do below = k.tile(base, w, present >> (STAGES - 1) & 1, w ? 0 : k.first_token(i), odd >> (STAGES - 1) & 1, below);
+            while (!K::kPool && below);
             __syncwarp();                                    // the stage may be filled again
             base = base == k.ring + (STAGES - 1) * K::kStage ? k.ring : base + K::kStage;
         }

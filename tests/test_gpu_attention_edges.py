@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from live_common import BF16, F16, Case, attention64
+from live_common import BF16, F16, Case, attention64, random_rows
 from test_gpu_attention import DEV, TAGS, Setup, ctx, pk  # noqa: F401  (fixtures)
 
 pytestmark = pytest.mark.gpu
@@ -105,3 +105,58 @@ def test_few_columns_see_whole_keys(pk, ctx, tag, rows, dtype, scale):
     want, tol = attention64(s.q[:rows].double().numpy(), lambda b: s.kv(b)[0], lambda b: s.kv(b)[1], s.case, 2, scale, 0, 0, dtype,
                             False, k_rounding=0.0)
     assert np.all(np.abs(got - want) <= tol), np.max(np.abs(got - want) / tol)
+
+
+@pytest.mark.parametrize("tag", [1, 2, 3])
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("rows", [1, 4])
+@pytest.mark.parametrize("at", [0, 37])
+@pytest.mark.parametrize("size", [300.0, 2.0e4])
+def test_a_token_of_large_values_and_no_weight(pk, ctx, tag, dtype, rows, at, size):
+    """One token's values are far larger than all others and its weight is zero (its logit 150 and more below the others, in
+    powers of two): the others keep their bits.  The bound is that of the batch without the token."""
+    n, D = 200, 64
+    s = Setup(pk, tag, 1, 2, D, 16, 32, Case([n], [rows], [[n - 1] * rows]), dtype=dtype)
+    s.q = (s.q.abs() + 0.5).to(dtype)
+    rng = np.random.default_rng(8)
+    for j in range(n):
+        k, v = (random_rows(rng, 1, 1, D, BF16, outliers=False).double().numpy()[0] for _ in range(2))
+        if j == at:
+            k, v = np.full((1, D), -40.0), np.full((1, D), size)
+        s.lay.put(s.pages[s.table[0, j // 16]], j % 16, k, v)
+    s.dev.copy_(torch.from_numpy(s.pages))
+    got = s.run(ctx)[:rows].double().cpu().numpy()
+    assert ctx.query_status() == 0
+    rest = [j for j in range(n) if j != at]
+    K, V = (x[rest] for x in s.kv(0))
+    x = s.q[:rows].double().numpy() @ s.kv(0)[0][at, 0] * D ** -0.5
+    assert (x < -104 - 40).all()                            # e^-104 is below 2^-150; logits of the others are above -40
+    want, tol = attention64(s.q[:rows].double().numpy(), lambda b: K, lambda b: V, Case([n - 1], [rows], [[n - 2] * rows]), 2,
+                            D ** -0.5, 0, 0, dtype, False, k_rounding=0.0)
+    assert np.all(np.abs(got - want) <= tol), np.max(np.abs(got - want) / tol)
+
+
+@pytest.mark.parametrize("tag", [2, 3])
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("D,G", [(64, 32), (128, 64)])
+@pytest.mark.parametrize("size", [2.0 ** -10, 2.0 ** -15])
+def test_groups_of_small_values_keep_their_bits(pk, ctx, tag, dtype, D, G, size):
+    """The values of one scale group are far smaller than the other's, in every token: bounded group by group."""
+    n = 100
+    s = Setup(pk, tag, 1, 2, D, 16, G, Case([n], [2]), dtype=dtype)
+    rng = np.random.default_rng(8)
+    for j in range(n):
+        k, v = (random_rows(rng, 1, 1, D, BF16, outliers=False).double().numpy()[0] for _ in range(2))
+        v *= 16
+        v[:, G:] *= size
+        s.lay.put(s.pages[s.table[0, j // 16]], j % 16, k, v)
+    s.dev.copy_(torch.from_numpy(s.pages))
+    got = s.run(ctx).double().cpu().numpy()
+    assert ctx.query_status() == 0
+    K, V = s.kv(0)
+    for c in (slice(0, G), slice(G, D)):
+        only = np.zeros_like(V)
+        only[..., c] = V[..., c]
+        want, tol = attention64(s.q.double().numpy(), lambda b: K, lambda b: only, s.case, 2, D ** -0.5, 0, 0, dtype, False, k_rounding=0.0)
+        err = np.abs(got - want)[..., c]
+        assert np.all(err <= tol[..., c]), np.max(err / tol[..., c])
