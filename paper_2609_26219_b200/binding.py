@@ -196,6 +196,8 @@ def make_qpool(pages: torch.Tensor, tag: int, n_pages: int, stride_layer: Option
     if pages.dtype != torch.uint8 or pages.dim() not in (2, 3) or pages.stride(-1) != 1:
         raise ValueError("pages: a uint8 tensor [n_pages][bytes] or [n_layers][n_pages][bytes] with unit stride on the last axis")
     if stride_page is None:
+        if n_pages > pages.shape[-2]:
+            raise ValueError(f"n_pages {n_pages}: the tensor has {pages.shape[-2]}")
         stride_page = pages.stride(-2)
     if stride_layer is None:
         stride_layer = pages.stride(0) if pages.dim() == 3 else 0

@@ -3,6 +3,7 @@ import ctypes
 import os
 
 import pytest
+import torch
 
 from test_live_cache import pk  # noqa: F401  (fixture)
 
@@ -42,3 +43,13 @@ def test_workspace_size_needs_no_arrays(pk, rows):
         want = size(pk, g, tag, 4, n_rows=rows, max_rows=rows)
         assert want > 0
         assert size(pk, g, tag, 4, n_rows=rows, max_rows=rows, row_start=None, kv_len=None, block_table=None) == want
+
+
+def test_a_pool_has_no_more_pages_than_its_tensor(pk):
+    """With the tensor's own strides; a pool laid out by given strides may have any number."""
+    pages = torch.zeros((2, 3, 64), dtype=torch.uint8)
+    for t in (pages, pages[0]):
+        assert pk.make_qpool(t, 3, 3).n_pages == 3
+        with pytest.raises(ValueError):
+            pk.make_qpool(t, 3, 4)
+    assert pk.make_qpool(pages.view(1, -1), 3, 6, stride_page=64).n_pages == 6
