@@ -220,14 +220,16 @@ struct SplitKernel {
         const int v = (int)lds32(cold + 12) + (i << lds32(cold + 16)), sinks = (int)lds32(cold + 20);
         return (v < sinks ? v : (int)lds32(cold + 24) + v - sinks) * kTile;
     }
-    // Whether one of the rows sees a token of the tile: rows at given positions may lie further apart than the window.
+    // Whether one of the rows sees a token of the tile: rows at given positions may lie further apart than the window, or behind the
+    // cache's end.
     __device__ __forceinline__ bool some_row_sees(int t0) const {
         if (!p.b.pos || p.window == 0 || t0 < p.sinks) return true;
+        const int last = min(t0 + kTile, kv()) - 1;
         bool seen = false;
 #pragma unroll 1
         for (int c = 0; c < 4 * NC; c++) {
             const int x = (int)lds32(cold + 48 + 4 * c);
-            seen = seen || (x >= t0 && x - (t0 + kTile - 1) < p.window);
+            seen = seen || (x >= t0 && x - last < p.window);
         }
         return seen;
     }

@@ -62,6 +62,18 @@ def test_pages_between_rows_may_be_gone(pk, ctx, tag, near, splits):
 
 
 @pytest.mark.parametrize("tag", TAGS)
+@pytest.mark.parametrize("rows", [1, 3, 40, 300])
+@pytest.mark.parametrize("window", [1, 4, 20])
+def test_rows_behind_the_cache(pk, ctx, tag, rows, window):
+    """Positions at and behind kv_len: a window that ends behind the last token shows nothing, and asks for no page."""
+    pos = [405 + window - 1 + i for i in range(rows)]       # kv_len 405 ends inside a tile and a page; the windows start at 405 and later
+    s = Setup(pk, tag, 2, 4, 64, 32, 32, Case([405], [rows], [pos]))
+    s.keep["table"][0] = -1
+    out = s.check(ctx, window)
+    assert (out[:rows] == 0).all()
+
+
+@pytest.mark.parametrize("tag", TAGS)
 @pytest.mark.parametrize("rows", [1, 40, 300])
 def test_a_sequence_before_descending_entries_keeps_its_rows(pk, ctx, tag, rows):
     """row_start that descends leaves out the sequence whose entries those are and no other, also where the tokens are split."""
