@@ -171,10 +171,13 @@ AttentionPlan plan_attention(const patchkv_geom* g, int tag, const patchkv_batch
         if (window > 0) steps = std::min(steps, ((long long)window + sinks + b->max_rows) / kRowTile + 3);
         a.row_tiles = (int)tiles;
         a.row_splits = (int)std::max(1ll, std::min((long long)kSms / ctas, steps / 2));
-        // Images pay where a token is needed by several CTAs, up to 1.5 GiB of workspace.
+        // Images pay where a token is needed by several CTAs of vectors: by two where they save converting codes, by eight over bf16 pages, which
+        // they only copy.  With and without, 8 KV heads, 32 query heads, D 128, 64k tokens: 4-bit pages and 2, 4, 8 CTAs
+        // 232 and 241, 362 and 479, 602 and 942 us; bf16 pages 245 and 172, 374 and 353, 633 and 674, and with 32 of them
+        // 2091 and 2626 us.  Up to 1.5 GiB of workspace.
         const uint64_t all_steps = ((uint64_t)b->max_kv_len + kRowTile - 1) / kRowTile, images = all_steps * H * b->n_seqs;
         const uint64_t image = (pool ? 4ull : 6ull) * kRowTile * D;         // room for fp16 queries' two matrices of K
-        if (tiles > 1 && images > 0 && images <= kMaxImageBytes / image) {
+        if (tiles >= (pool ? 8 : 2) && images > 0 && images <= kMaxImageBytes / image) {
             a.image_steps = (int)all_steps;
             a.image_bytes = images * image;
             a.meta_bytes = images * 32;

@@ -15,9 +15,19 @@ pytestmark = pytest.mark.gpu
 def test_huge_values_in_unseen_pool_tokens(pk, ctx, rows, window):
     """A finite value of 3e38 in a token that a row does not see, later than the row or behind its window, is not part of its result: a weight
     of zero is zero, not a small number.  Two neighbouring tokens at every place of eight."""
-    s = Setup(pk, 0, 2, 4, 64, 16, 32, Case([400], [rows]))
-    first, clean = 400 - rows, max(1, rows // 2)            # rows [clean, ...) see the later tokens
-    at = list(range(first + clean, 400)) + list(range(0, first - window) if window else [])
+    huge_values(pk, ctx, 400, rows, window)
+
+
+@pytest.mark.parametrize("window", [0, 24])
+def test_huge_values_in_unseen_pool_tokens_with_images(pk, ctx, window):
+    """The same from images of the pool's tokens, which enough rows get."""
+    huge_values(pk, ctx, 1300, 1200, window)
+
+
+def huge_values(pk, ctx, total, rows, window):
+    s = Setup(pk, 0, 2, 4, 64, 16, 32, Case([total], [rows]))
+    first, clean = total - rows, max(1, rows // 2)          # rows [clean, ...) see the later tokens
+    at = list(range(first + clean, total)) + list(range(0, first - window) if window else [])
     at = [t for t in at if t % 8 in (0, 1)] or [first + clean]
     s.v = s.v.clone()
     for t in at:
@@ -26,7 +36,7 @@ def test_huge_values_in_unseen_pool_tokens(pk, ctx, rows, window):
     s.cache = pk.make_pool(s.k, s.v, s.n_pages, (0, 2048, 128, 64))
     out = s.run(ctx, window)
     assert ctx.query_status() == 0
-    seen = Case([400], [clean], [list(range(first, first + clean))])
+    seen = Case([total], [clean], [list(range(first, first + clean))])
     s.q = s.q[:clean]
     want, tol = s.reference(window, case=seen)
     assert np.all(np.abs(out[:clean].double().cpu().numpy() - want) <= tol)
@@ -172,3 +182,15 @@ def test_groups_of_small_values_keep_their_bits(pk, ctx, tag, dtype, D, G, size)
         want, tol = attention64(s.q.double().numpy(), lambda b: K, lambda b: only, s.case, 2, D ** -0.5, 0, 0, dtype, False, k_rounding=0.0)
         err = np.abs(got - want)[..., c]
         assert np.all(err <= tol[..., c]), np.max(err / tol[..., c])
+
+
+@pytest.mark.parametrize("rows", [500, 1100])
+@pytest.mark.parametrize("name", ["causal", "window", "scattered", "gone"])
+def test_pool_rows_without_and_with_images(pk, ctx, rows, name):
+    """4 and 9 CTAs of vectors over the bf16 pool: fewer than eight read the pages themselves, more get images of them."""
+    total = 1500
+    pos = [[(i * 37) % total for i in range(rows)]] if name == "scattered" else None
+    s = Setup(pk, 0, 1, 2, 64, 16, 32, Case([total], [rows], pos))
+    if name == "gone":
+        s.keep["table"][0, 1:(total - rows - 100) // 16] = -1
+    s.check(ctx, *{"window": (70, 0), "gone": (100, 3)}.get(name, (0, 0)))

@@ -53,3 +53,13 @@ def test_a_pool_has_no_more_pages_than_its_tensor(pk):
         with pytest.raises(ValueError):
             pk.make_qpool(t, 3, 4)
     assert pk.make_qpool(pages.view(1, -1), 3, 6, stride_page=64).n_pages == 6
+
+
+def test_images_where_they_pay(pk):
+    """Operands are laid out in the workspace for two CTAs of query vectors over quantised pages, for eight over bf16 pages."""
+    g = pk.make_geom(1, 1, 64, 64, 0, 1e4, 16, 16, 32)
+    kv, image = 16384, 16384 * 64 * 2
+    for tag, tiles in ((0, 8), (1, 2), (2, 2), (3, 2)):
+        without, with_ = (size(pk, g, tag, 1, n_rows=n, max_rows=n, max_kv_len=kv) for n in ((tiles - 1) * 256, (tiles - 1) * 256 + 1))
+        assert with_ - without > image and without < image * 74
+        assert size(pk, g, tag, 1, n_rows=256 * 148, max_rows=256 * 148, max_kv_len=kv) >= 2 * image
