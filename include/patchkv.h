@@ -479,8 +479,8 @@ typedef struct {
 
 /* `pool` is a patchkv_pool (bf16) or NULL, `cache` a patchkv_qpool or NULL: exactly one of the two.  Asynchronous on
  * `stream`, no allocation, no host synchronisation; can be captured.  Logits, softmax sums and output sums are held in
- * fp32, the result is rounded once; the weights enter the second product as 16-bit numbers (bf16 over a pool, else fp16;
- * two of them for fp16 results of the calls below 17 pairs).
+ * fp32, the result is rounded once; the weights enter the second product as 16-bit numbers (bf16 over a pool, else fp16; in
+ * calls of up to 16 pairs as two of them over a pool and for fp16 results), quantised values rounded once to fp16.
  * Calls with more than 16 (row, query head) pairs per KV head and sequence round quantised values to fp16 first (K for fp16
  * queries to two fp16 numbers): a magnitude above 65504 is an infinity to them.
  * A sequence whose row_start entries are descending or outside [0, n_rows], rows beyond max_rows of a sequence, tokens

@@ -3,8 +3,9 @@
 // A column is a (row, query head of one KV head) pair; up to 16 of them ride on one pass over a KV head.
 // Both products run on warp-level mma with the cache as the M side, so a cached number becomes a matrix operand once and
 // all columns use it: logits^T[16 tokens][columns] = K * q^T, out^T[channels][columns] += V^T * p^T.  The matrix pipe is
-// far from its limit here (tcgen05 would want 128 rows); what bounds the kernel is the bytes of the cache and, for 4-bit
-// pages, the instructions that turn codes into operands, which is where the work below went.
+// far from its limit here (31 % with 8 columns); what bounds the kernel is the bytes of the cache and, for 4-bit pages, the instructions
+// that turn codes into operands, which is where the work below went.  (tcgen05 with 128 tokens as its M side and 8 or 16
+// columns as N would take the same operands from shared memory; it has not been tried.)
 //
 // Codes as operands.  The bit pattern u < 2048 is the half u * 2^-24, so a code plus its offset (u = q + 8 or q + 128) is an exact
 // operand once it stands in the low bits of its half: one logic instruction per register.  (e4m3 operands would take half
@@ -16,8 +17,10 @@
 //   V: v = (u * 2^-24) * S - offset * S in one half fma, S the token's scale times a power of two that follows the
 //      V scales: one rounding, of 2^-12, as p's own to fp16, or of 2^-25 where v is subnormal.  For the latter to stay below
 //      2^-12 of a group's largest value S has to be 2^8 at least (8-bit codes: 2^4), and it is 2^15 at most: the power of two
-//      moves both ways, and a tile whose scales have a wider range goes through again for the smaller ones.  For fp16 results,
-//      whose own rounding is no larger than those two, p is the sum of two fp16 numbers, for one more product per operand.
+//      moves both ways, and a tile whose scales have a wider range goes through again for the smaller ones.
+//   p: where its rounding would be as large as the result's own, for fp16 results and over bf16 pages, it is the sum of two such
+//      numbers, for one more product per operand (bf16 pages, 8 x 16k tokens: 2.0e-3 -> 1.7e-3 off, which is the result's rounding, 99.1 ->
+//      99.3 us; the matrix pipe has room).
 // Softmax on powers of two against a reference that is only moved when a logit exceeds it by more than 15 (p <= 2^15), to 3 below
 // the largest (fp16 then holds weights down to 2^-17 of it to all its bits): one vote per tile instead of a maximum across lanes.
 #pragma once
@@ -560,8 +563,8 @@ struct SplitKernel {
                 }
             }
         }
-        uint32_t pf[NT][2], pr[NT][2];                              // weights, and for fp16 results what their rounding took
-        const bool fine = !kPool && p.f16;
+        uint32_t pf[NT][2], pr[NT][2];                              // weights, and where that shows what their rounding took
+        const bool fine = kPool || p.f16;
 #pragma unroll
         for (int c = 0; c < NC; c++) {
 #pragma unroll
@@ -576,7 +579,8 @@ struct SplitKernel {
                 const uint32_t w = kPool ? bf162_bits(lo, hi) : half2_bits(lo, hi);
                 pf[nt][i] = transpose8x8(w);
                 pr[nt][i] = 0;
-                if (fine) pr[nt][i] = transpose8x8(half2_bits(lo - low_half(w), hi - high_half(w)));
+                if constexpr (kPool) pr[nt][i] = transpose8x8(bf162_bits(lo - __uint_as_float(w << 16), hi - __uint_as_float(w & 0xFFFF0000u)));
+                else if (fine) pr[nt][i] = transpose8x8(half2_bits(lo - low_half(w), hi - high_half(w)));
             }
         if constexpr (kPool) {
             const uint32_t a = base + kV + ((lane & 7) + ((lane >> 4) << 3)) * kVStride + (lane & 8) * 2;
@@ -597,7 +601,10 @@ struct SplitKernel {
                 uint32_t r[4];
                 ldmatrix4_trans(r, a + 32 * i);
 #pragma unroll
-                for (int nt = 0; nt < NT; nt++) mma_bf16(acc[nt][i], r[0], r[1], r[2], r[3], pf[nt][0], pf[nt][1]);
+                for (int nt = 0; nt < NT; nt++) {
+                    mma_bf16(acc[nt][i], r[0], r[1], r[2], r[3], pf[nt][0], pf[nt][1]);
+                    mma_bf16(acc[nt][i], r[0], r[1], r[2], r[3], pr[nt][0], pr[nt][1]);
+                }
             }
         } else {
             if (!whole && __any_sync(0xFFFFFFFFu, top >= 0x7C00u)) { values_one_by_one(base, x, row0); return 0; }

@@ -194,3 +194,20 @@ def test_pool_rows_without_and_with_images(pk, ctx, rows, name):
     if name == "gone":
         s.keep["table"][0, 1:(total - rows - 100) // 16] = -1
     s.check(ctx, *{"window": (70, 0), "gone": (100, 3)}.get(name, (0, 0)))
+
+
+@pytest.mark.parametrize("rows", [1, 4, 8])
+@pytest.mark.parametrize("scale", [0.125, 0.25])
+def test_few_columns_over_the_pool_keep_their_weights(pk, ctx, rows, scale):
+    """Up to 16 columns the weights over bf16 pages are sums of two bf16 numbers.  What is left is half a step of the result and,
+    of sum p|v|: 2^-16 for the weights (two roundings of 2^-9, the second of what the first left, doubled), 2^-18 for exp2 and the
+    sums, and what fp32 dot products of D = 64 put the logits off."""
+    s = Setup(pk, 0, 2, 4, 64, 16, 32, Case([300], [rows]))
+    got = s.check(ctx, scale=scale)[:rows].double().cpu().numpy()
+    q, K, V = s.q[:rows].double().numpy(), s.kv(0)[0], s.kv(0)[1]
+    want, _ = attention64(q, lambda b: K, lambda b: V, s.case, 2, scale, 0, 0, BF16, True)
+    mass, _ = attention64(q, lambda b: K, lambda b: np.abs(V), s.case, 2, scale, 0, 0, BF16, True)
+    big = scale * np.einsum("rhd,khd->rhk", np.abs(q), np.abs(K).repeat(2, 1)).max(2)[..., None]
+    half_step = 2.0 ** (np.floor(np.log2(np.abs(want))) - 8)
+    tol = half_step + (2.0 ** -16 + 2.0 ** -18 + np.expm1(2 * (64 + 64) * 2.0 ** -23 * big)) * mass
+    assert np.all(np.abs(got - want) <= tol), np.max(np.abs(got - want) / tol)
