@@ -497,6 +497,141 @@ PATCHKV_API int patchkv_attention(patchkv_ctx* ctx, const patchkv_geom* geom, co
 PATCHKV_API uint64_t patchkv_attention_workspace_bytes(const patchkv_geom* geom, int tag, const patchkv_batch* batch,
                                                        int n_q_heads, int window, int sinks);
 
+/* ---- around the attention: rotary positions, attention weight, eviction -----------------------------------------
+ * What a program does with the live cache besides attending: new rows get their rotary positions on their way in
+ * (patchkv_rotary_append), cached tokens are weighed by the attention they receive (patchkv_attention_mass: A_i of Eqs. 10 and
+ * 13, from the live cache instead of from attention that was stored), and a cache that has grown too long is cut down to the tokens
+ * that matter (patchkv_evict_select, patchkv_cache_gather).  Batches, caches, errors and captures as above. */
+
+/* Rotates query and key rows and writes keys and values into their positions of the cache.
+ *   q_out[row][h] = R(t) q[row][h],   K of the row's position <- R(t) k[row][h],   V of it <- v[row][h]
+ * t is rope_pos[row] where that is given (a cache that was cut down keeps the positions its keys were rotated to), else the
+ * row's position in the cache.  R turns the first rotary_dim channels of a head by t * theta_i, pairs as rope_style says,
+ * theta_i = inv_freq[i] or rope_base^(-2i/Dr) (frequencies scaled for long contexts come as inv_freq), |theta_i| <= 65536;
+ * (a, b) -> (a c - b s, a s + b c) with c, s = factor * (cos, sin) of (double)t * theta_i, evaluated in double.  rotary_dim 0: nothing
+ * is rotated.  Queries, and keys of a bf16 pool, are formed in fp32 with c and s rounded to fp32, and rounded once; channels behind
+ * rotary_dim are copied bit for bit.  Keys of quantised pages are formed in double and quantised from there as
+ * patchkv_cache_append quantises, without a rounding in between; values are quantised from their 16 bits.
+ * Rows, positions and skipped rows as for patchkv_cache_append; the q_out of a skipped row, and of a row of no sequence, is left
+ * as it was.  One launch, no allocation, no workspace; can be captured (inv_freq is read by the call, not by its replays).
+ * Every geometry is taken.  The fast kernel wants D a power of two from 16 to 256, rotary_dim a multiple of 32 (HALF) or 16,
+ * for quantised pages G a multiple of 16 and page sections of whole 16 bytes, and rows and strides of whole 16 bytes. */
+typedef struct {
+    uint32_t struct_size;
+    int32_t type;                 /* PATCHKV_ROWS_*: type of q, q_out, k and v; into a bf16 pool only PATCHKV_ROWS_BF16 */
+    int32_t n_q_heads;            /* 0: no queries */
+    float factor;                 /* on cos and sin, 1 for a rotation (some long-context scalings have another); finite */
+    const void* q;                /* DEVICE [n_rows][Hq][D] */
+    void* q_out;                  /* DEVICE [n_rows][Hq][D]; q itself with the same strides, or no overlap with q, k and v */
+    int64_t q_stride_row;         /* elements; the channel stride is 1 */
+    int64_t q_stride_head;
+    int64_t q_out_stride_row;
+    int64_t q_out_stride_head;
+    const void* k;                /* DEVICE [n_rows][H][D] */
+    const void* v;                /* DEVICE [n_rows][H][D] */
+    int64_t k_stride_row;
+    int64_t k_stride_head;
+    int64_t v_stride_row;
+    int64_t v_stride_head;
+    const int32_t* rope_pos;      /* DEVICE i32 [n_rows], optional: the rotary positions */
+} patchkv_rotary_args;
+
+PATCHKV_API int patchkv_rotary_append(patchkv_ctx* ctx, const patchkv_geom* geom, const patchkv_pool* pool,
+                                      const patchkv_qpool* cache, int layer, const patchkv_batch* batch,
+                                      const patchkv_rotary_args* args, void* stream);
+
+/* The attention weight that each cached token receives from the batch's query rows:
+ *   mass[b][j] <- decay * mass_in[b][j] + sum over rows and query heads of softmax_j(scale * q . k_j)
+ * for every token j < kv_len[b] (a sequence without rows has an empty sum); entries at and behind kv_len[b] are left as they were.
+ * What a row sees, and what is left out or skipped, is as for patchkv_attention with the
+ * same arguments; a row that sees no token adds nothing; a NaN or an infinity in a query makes the masses that it sees NaN.
+ * Sums are formed in fp32 in an order that the arguments fix, so that equal calls give equal bits.
+ *   PATCHKV_MASS_F32: decay any finite number; 0 does not read mass_in, and neither does a null mass_in.
+ *   PATCHKV_MASS_U64: units of 2^-24 as patchkv_select_repair_tokens reads them (kind TOKEN_MASS); the call's sum is rounded
+ *     once, ties to even, and added: decay must be 0 or 1.  A sum that is not finite counts as 0 and latches PATCHKV_E_BADINPUT.
+ * Quantised keys enter as they are in calls of up to 16 (row, query head) pairs per KV head and sequence, and with 22 bits in larger
+ * ones (a magnitude above 65504 is an infinity to those). */
+enum { PATCHKV_MASS_F32 = 0, PATCHKV_MASS_U64 = 1 };
+typedef struct {
+    uint32_t struct_size;
+    int32_t type;                 /* PATCHKV_ROWS_*: type of q; over a bf16 pool only PATCHKV_ROWS_BF16 */
+    int32_t n_q_heads;            /* Hq, a multiple of H */
+    int32_t window;               /* as for patchkv_attention */
+    int32_t sinks;
+    float scale;
+    float decay;
+    int32_t mass_type;            /* PATCHKV_MASS_* */
+    const void* q;                /* DEVICE [n_rows][Hq][D] */
+    int64_t q_stride_row;         /* elements; the channel stride is 1 */
+    int64_t q_stride_head;
+    const void* mass_in;          /* DEVICE [n_seqs][mass_stride], optional; may be mass */
+    void* mass;                   /* DEVICE [n_seqs][mass_stride] */
+    int64_t mass_stride;          /* elements, at least max_kv_len */
+    void* workspace;              /* as for patchkv_attention */
+    uint64_t workspace_bytes;     /* at least patchkv_attention_mass_workspace_bytes of the same arguments */
+} patchkv_mass_args;
+
+PATCHKV_API int patchkv_attention_mass(patchkv_ctx* ctx, const patchkv_geom* geom, const patchkv_pool* pool,
+                                       const patchkv_qpool* cache, int layer, const patchkv_batch* batch,
+                                       const patchkv_mass_args* args, void* stream);
+PATCHKV_API uint64_t patchkv_attention_mass_workspace_bytes(const patchkv_geom* geom, int tag, const patchkv_batch* batch,
+                                                            int n_q_heads, int window, int sinks);
+
+/* Chooses the tokens of each sequence that stay.  Of n = kv_len[b] tokens with a budget of B = budget[b] (or max_keep): all where
+ * n <= B; else the last min(recent, B) tokens, the first min(sinks, what is left of B), and of the rest those of largest mass until
+ * there are B; of equal masses the lower index.
+ *   keep[b][0 .. kept[b]-1] = their indices, ascending; the entries behind, up to max_keep, are set to -1
+ *   mass_out[b][i] = mass[b][keep[b][i]], where mass_out is given; the entries behind are left as they were
+ * A mass that is negative, infinite or NaN counts as zero and latches PATCHKV_E_BADINPUT.  Lengths above max_len and budgets
+ * above max_keep are cut there and latch PATCHKV_E_BOUNDS; those below 0 count as 0.  One launch on `stream`, no allocation, no workspace;
+ * can be captured. */
+typedef struct {
+    uint32_t struct_size;
+    int32_t n_seqs;
+    int32_t max_len;              /* bound on kv_len, at most 2^24 */
+    int32_t max_keep;             /* bound on the budgets, and the budget where `budget` is null */
+    int32_t recent;               /* last tokens that stay */
+    int32_t sinks;                /* first tokens that stay */
+    const float* mass;            /* DEVICE fp32 [n_seqs][mass_stride] */
+    int64_t mass_stride;          /* elements, at least max_len */
+    const int32_t* kv_len;        /* DEVICE i32 [n_seqs] */
+    const int32_t* budget;        /* DEVICE i32 [n_seqs], optional */
+    int32_t* keep;                /* DEVICE i32 [n_seqs][keep_stride] (out) */
+    int64_t keep_stride;          /* elements, at least max_keep */
+    int32_t* kept;                /* DEVICE i32 [n_seqs] (out); may be neither kv_len nor budget */
+    float* mass_out;              /* DEVICE fp32 [n_seqs][mass_out_stride] (out), optional; must not overlap mass */
+    int64_t mass_out_stride;      /* elements, at least max_keep */
+} patchkv_evict_args;
+
+PATCHKV_API int patchkv_evict_select(patchkv_ctx* ctx, const patchkv_evict_args* args, void* stream);
+
+/* Moves the kept rows of one layer to other pages: the token at position keep[b][i] (its page by src_table) goes to position i (its
+ * page by dst_table), for i < kept[b].  Quantised rows are moved bit for bit.  With rotate (bf16 pools) K is turned by i - keep[b][i]
+ * positions as patchkv_rotary_append turns it with factor 1 (a row that stays at its position is copied bit for bit): the keys are
+ * then those of a context of the kept tokens alone, whose positions are those in the cache; without it they stay where they were
+ * rotated to, and later rows need rope_pos.
+ * A slot that is written may not be the slot of another row that is read: the pages of dst_table must hold none that src_table reads,
+ * but for rows that stay where they are (same page and slot).  A sequence is therefore cut down into spare pages, which its old ones replace
+ * as spares for the next.  Rows whose positions or pages are out of range are skipped and PATCHKV_E_BOUNDS is latched; kept[b] above
+ * max_keep is cut there and latches it too.  One launch, no allocation, no workspace; can be captured. */
+typedef struct {
+    uint32_t struct_size;
+    int32_t n_seqs;
+    int32_t max_keep;             /* bound on kept */
+    int32_t rotate;               /* 0 or 1; 1 only over a bf16 pool */
+    int32_t src_stride;           /* entries of src_table per sequence */
+    int32_t dst_stride;           /* entries of dst_table per sequence */
+    const int32_t* keep;          /* DEVICE i32 [n_seqs][keep_stride] */
+    int64_t keep_stride;
+    const int32_t* kept;          /* DEVICE i32 [n_seqs] */
+    const int32_t* kv_len;        /* DEVICE i32 [n_seqs]: tokens of the sequence before */
+    const int32_t* src_table;     /* DEVICE i32 [n_seqs][src_stride] */
+    const int32_t* dst_table;     /* DEVICE i32 [n_seqs][dst_stride] */
+} patchkv_gather_args;
+
+PATCHKV_API int patchkv_cache_gather(patchkv_ctx* ctx, const patchkv_geom* geom, const patchkv_pool* pool,
+                                     const patchkv_qpool* cache, int layer, const patchkv_gather_args* args, void* stream);
+
 /* Synchronises the context's device work and returns in *device_status the first device-side error latched
  * since the last query (PATCHKV_OK, PATCHKV_E_BOUNDS, PATCHKV_E_BADINPUT or PATCHKV_E_TIMEOUT), then clears it. */
 PATCHKV_API int patchkv_query_status(patchkv_ctx* ctx, int* device_status);

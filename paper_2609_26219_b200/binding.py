@@ -24,6 +24,7 @@ LAYERS_INDEPENDENT, LAYERS_SHARED = 0, 1
 SCORE_ATTN_F16, SCORE_BLOCK_MASS, SCORE_TOKEN_MASS = 0, 1, 2
 MAX_SESSIONS = 8
 ROWS_BF16, ROWS_F16 = 0, 1
+MASS_F32, MASS_U64 = 0, 1
 FLAG_DIRECT_LOADS = 1
 FLAG_HOST_DIRECT = 2
 FLAG_HOST_STAGED = 4
@@ -97,6 +98,35 @@ class AttentionArgs(C.Structure):
                 ("out_stride_head", C.c_int64), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
 
 
+class RotaryArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("type", C.c_int32), ("n_q_heads", C.c_int32), ("factor", C.c_float),
+                ("q", C.c_void_p), ("q_out", C.c_void_p), ("q_stride_row", C.c_int64), ("q_stride_head", C.c_int64),
+                ("q_out_stride_row", C.c_int64), ("q_out_stride_head", C.c_int64), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_stride_row", C.c_int64), ("k_stride_head", C.c_int64), ("v_stride_row", C.c_int64),
+                ("v_stride_head", C.c_int64), ("rope_pos", C.c_void_p)]
+
+
+class MassArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("type", C.c_int32), ("n_q_heads", C.c_int32), ("window", C.c_int32),
+                ("sinks", C.c_int32), ("scale", C.c_float), ("decay", C.c_float), ("mass_type", C.c_int32),
+                ("q", C.c_void_p), ("q_stride_row", C.c_int64), ("q_stride_head", C.c_int64), ("mass_in", C.c_void_p),
+                ("mass", C.c_void_p), ("mass_stride", C.c_int64), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+class EvictArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_seqs", C.c_int32), ("max_len", C.c_int32), ("max_keep", C.c_int32),
+                ("recent", C.c_int32), ("sinks", C.c_int32), ("mass", C.c_void_p), ("mass_stride", C.c_int64),
+                ("kv_len", C.c_void_p), ("budget", C.c_void_p), ("keep", C.c_void_p), ("keep_stride", C.c_int64),
+                ("kept", C.c_void_p), ("mass_out", C.c_void_p), ("mass_out_stride", C.c_int64)]
+
+
+class GatherArgs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_seqs", C.c_int32), ("max_keep", C.c_int32), ("rotate", C.c_int32),
+                ("src_stride", C.c_int32), ("dst_stride", C.c_int32), ("keep", C.c_void_p), ("keep_stride", C.c_int64),
+                ("kept", C.c_void_p), ("kv_len", C.c_void_p), ("src_table", C.c_void_p), ("dst_table", C.c_void_p)]
+
+
+_SIZEOF_ROTARY, _SIZEOF_MASS, _SIZEOF_EVICT, _SIZEOF_GATHER = (C.sizeof(x) for x in (RotaryArgs, MassArgs, EvictArgs, GatherArgs))
 _SIZEOF_ROWS, _SIZEOF_ATTENTION = C.sizeof(Rows), C.sizeof(AttentionArgs)
 _lib = None
 
@@ -139,6 +169,19 @@ def lib():
         l.patchkv_attention.restype = C.c_int
         l.patchkv_attention_workspace_bytes.argtypes = [C.POINTER(Geom), C.c_int, C.POINTER(Batch), C.c_int, C.c_int, C.c_int]
         l.patchkv_attention_workspace_bytes.restype = C.c_uint64
+        l.patchkv_rotary_append.argtypes = [C.c_void_p, C.POINTER(Geom), C.POINTER(Pool), C.POINTER(QPool), C.c_int,
+                                            C.POINTER(Batch), C.POINTER(RotaryArgs), C.c_void_p]
+        l.patchkv_rotary_append.restype = C.c_int
+        l.patchkv_attention_mass.argtypes = [C.c_void_p, C.POINTER(Geom), C.POINTER(Pool), C.POINTER(QPool), C.c_int,
+                                             C.POINTER(Batch), C.POINTER(MassArgs), C.c_void_p]
+        l.patchkv_attention_mass.restype = C.c_int
+        l.patchkv_attention_mass_workspace_bytes.argtypes = l.patchkv_attention_workspace_bytes.argtypes
+        l.patchkv_attention_mass_workspace_bytes.restype = C.c_uint64
+        l.patchkv_evict_select.argtypes = [C.c_void_p, C.POINTER(EvictArgs), C.c_void_p]
+        l.patchkv_evict_select.restype = C.c_int
+        l.patchkv_cache_gather.argtypes = [C.c_void_p, C.POINTER(Geom), C.POINTER(Pool), C.POINTER(QPool), C.c_int,
+                                           C.POINTER(GatherArgs), C.c_void_p]
+        l.patchkv_cache_gather.restype = C.c_int
         l.patchkv_query_status.argtypes = [C.c_void_p, C.POINTER(C.c_int)]
         l.patchkv_selftest_bounded_wait.argtypes = [C.c_void_p, C.c_uint32, C.c_void_p]
         l.patchkv_selftest_stall_next_launch.argtypes = [C.c_void_p, C.c_int32, C.c_uint32]
@@ -251,6 +294,34 @@ def attention_workspace_bytes(geom: Geom, cache, batch: Batch, n_q_heads: int, w
     return int(lib().patchkv_attention_workspace_bytes(C.byref(geom), tag, C.byref(batch), n_q_heads, window, sinks))
 
 
+def attention_mass_workspace_bytes(geom: Geom, cache, batch: Batch, n_q_heads: int, window: int = 0, sinks: int = 0) -> int:
+    """Bytes of workspace Context.attention_mass needs for such a call (`cache`: a QPool, or a Pool for the bf16 pool)."""
+    tag = cache.tag if isinstance(cache, QPool) else TAG_BF16
+    return int(lib().patchkv_attention_mass_workspace_bytes(C.byref(geom), tag, C.byref(batch), n_q_heads, window, sinks))
+
+
+_MASS_TYPES = {torch.float32: MASS_F32, torch.int64: MASS_U64}
+
+
+def _table_rows(t: torch.Tensor, name: str, rows: int) -> int:
+    """Row stride of an int32 tensor [at least rows][entries] with unit stride on the last axis."""
+    if t.dtype is not torch.int32 or t.dim() != 2 or t.shape[0] < rows or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{name}: an int32 tensor [n_seqs][entries] with unit stride on the last axis")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _counts(t: torch.Tensor, name: str, n: int) -> int:
+    if t.dtype is not torch.int32 or t.dim() != 1 or t.shape[0] < n or (t.stride(0) != 1 and n > 1):
+        raise ValueError(f"{name}: a contiguous int32 tensor of {n} entries")
+    return t.data_ptr()
+
+
+def _mass_rows(t: torch.Tensor, name: str, kinds, rows: int) -> int:
+    if t.dtype not in kinds or t.dim() != 2 or t.shape[0] < rows or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{name}: a tensor [n_seqs][tokens] of {', '.join(str(k) for k in kinds)} with unit stride on the last axis")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
 class Context:
     """Owns one patchkv_ctx.  Methods are the C entry points with the `patchkv_` prefix dropped."""
 
@@ -360,6 +431,90 @@ class Context:
                           q.data_ptr(), out.data_ptr(), qs[0], qs[1], os_[0], os_[1], ws, ws_bytes)
         pool, pages = (None, cache) if isinstance(cache, QPool) else (cache, None)
         rc = lib().patchkv_attention(self._h, geom, pool, pages, layer, batch, a, _stream_of(stream, self.device))
+        return rc if rc == OK else self._check(rc, check)
+
+    def rotary_append(self, geom: Geom, cache, layer: int, batch: Batch, k: torch.Tensor, v: torch.Tensor,
+                      q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                      rope_pos: Optional[torch.Tensor] = None, rope_factor: float = 1.0, stream=None, check: bool = True) -> int:
+        """Rotates q [n_rows][Hq][D] into q_out (None: into q itself) and k [n_rows][H][D], and writes k and v into their
+        positions of a QPool or of the bf16 Pool.  rope_pos: int32 [n_rows], the rotary positions where they are not those in
+        the cache; rope_factor multiplies cos and sin.  Without q only the cache is written."""
+        kind = _row_type(k, "k")
+        if _row_type(v, "v") != kind or v.shape != k.shape:
+            raise ValueError("k and v must agree in type and shape")
+        if k.shape[0] < batch.n_rows or k.shape[1] != geom.n_kv_heads or k.shape[2] != geom.head_dim:
+            raise ValueError("k and v: [n_rows][n_kv_heads][head_dim]")
+        ks, vs, qs, os_, heads, qp, op = k.stride(), v.stride(), (0, 0), (0, 0), 0, None, None
+        if q is not None:
+            if q_out is None:
+                q_out = q
+            if _row_type(q, "q") != kind or _row_type(q_out, "q_out") != kind or q_out.shape != q.shape:
+                raise ValueError("q and q_out must agree in shape, and in type with k")
+            if q.shape[0] < batch.n_rows or q.shape[2] != geom.head_dim:
+                raise ValueError("q: [n_rows][n_q_heads][head_dim]")
+            qs, os_, heads, qp, op = q.stride(), q_out.stride(), q.shape[1], q.data_ptr(), q_out.data_ptr()
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        a = RotaryArgs(_SIZEOF_ROTARY, kind, heads, rope_factor, qp, op, qs[0], qs[1], os_[0], os_[1], k.data_ptr(), v.data_ptr(),
+                       ks[0], ks[1], vs[0], vs[1], None if rope_pos is None else _counts(rope_pos, "rope_pos", batch.n_rows))
+        pool, pages = (None, cache) if isinstance(cache, QPool) else (cache, None)
+        rc = lib().patchkv_rotary_append(self._h, geom, pool, pages, layer, batch, a, _stream_of(stream, self.device))
+        return rc if rc == OK else self._check(rc, check)
+
+    def attention_mass(self, geom: Geom, cache, layer: int, batch: Batch, q: torch.Tensor, mass: torch.Tensor,
+                       mass_in: Optional[torch.Tensor] = None, decay: float = 1.0, scale: Optional[float] = None, window: int = 0,
+                       sinks: int = 0, workspace: Optional[torch.Tensor] = None, stream=None, check: bool = True) -> int:
+        """mass [n_seqs][tokens] (fp32, or int64 in units of 2^-24) = decay * mass_in + the attention weight that each token gets
+        from q [n_rows][Hq][D].  mass_in: like mass (same strides), may be mass; None: zeros.  The rest as for attention, the
+        workspace of attention_mass_workspace_bytes(...) bytes."""
+        kind = _row_type(q, "q")
+        if q.shape[0] < batch.n_rows or q.shape[2] != geom.head_dim:
+            raise ValueError("q: [n_rows][n_q_heads][head_dim]")
+        stride = _mass_rows(mass, "mass", _MASS_TYPES, batch.n_seqs)
+        if mass.shape[1] < batch.max_kv_len:
+            raise ValueError("mass: [n_seqs][at least max_kv_len]")
+        if mass_in is not None and (mass_in.dtype is not mass.dtype or mass_in.shape != mass.shape or mass_in.stride() != mass.stride()):
+            raise ValueError("mass_in must agree with mass in type, shape and strides")
+        ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+        qs = q.stride()
+        a = MassArgs(_SIZEOF_MASS, kind, q.shape[1], window, sinks, geom.head_dim ** -0.5 if scale is None else scale, decay,
+                     _MASS_TYPES[mass.dtype], q.data_ptr(), qs[0], qs[1], None if mass_in is None else mass_in.data_ptr(),
+                     mass.data_ptr(), stride, ws, ws_bytes)
+        pool, pages = (None, cache) if isinstance(cache, QPool) else (cache, None)
+        rc = lib().patchkv_attention_mass(self._h, geom, pool, pages, layer, batch, a, _stream_of(stream, self.device))
+        return rc if rc == OK else self._check(rc, check)
+
+    def evict_select(self, mass: torch.Tensor, kv_len: torch.Tensor, keep: torch.Tensor, kept: torch.Tensor, sinks: int = 0,
+                     recent: int = 0, budget: Optional[torch.Tensor] = None, mass_out: Optional[torch.Tensor] = None, stream=None,
+                     check: bool = True) -> int:
+        """Chooses the tokens that stay: mass fp32 [n_seqs][tokens], kv_len int32 [n_seqs] -> keep int32 [n_seqs][max_keep]
+        (ascending, then -1), kept int32 [n_seqs], and mass_out fp32 [n_seqs][max_keep], the masses of the kept.  The
+        budget of a sequence is budget[b] (int32), or max_keep; n_seqs is kv_len's size."""
+        n = kv_len.numel()
+        ms, keep_stride = _mass_rows(mass, "mass", (torch.float32,), n), _table_rows(keep, "keep", n)
+        out, out_stride = None, 0
+        if mass_out is not None:
+            out, out_stride = mass_out.data_ptr(), _mass_rows(mass_out, "mass_out", (torch.float32,), n)
+            if mass_out.shape[1] < keep.shape[1]:
+                raise ValueError("mass_out: [n_seqs][at least max_keep]")
+        a = EvictArgs(_SIZEOF_EVICT, n, mass.shape[1], keep.shape[1], recent, sinks, mass.data_ptr(), ms, _counts(kv_len, "kv_len", n),
+                      None if budget is None else _counts(budget, "budget", n), keep.data_ptr(), keep_stride,
+                      _counts(kept, "kept", n), out, out_stride)
+        rc = lib().patchkv_evict_select(self._h, a, _stream_of(stream, self.device))
+        return rc if rc == OK else self._check(rc, check)
+
+    def cache_gather(self, geom: Geom, cache, layer: int, keep: torch.Tensor, kept: torch.Tensor, kv_len: torch.Tensor,
+                     src_table: torch.Tensor, dst_table: torch.Tensor, rotate: bool = False, stream=None, check: bool = True) -> int:
+        """Moves the rows keep[b][i] (positions by src_table) of a QPool or the bf16 Pool to positions i by dst_table; rotate (Pool
+        only) turns K by i - keep[b][i].  int32 tensors; pages of dst_table may not be among those that src_table reads."""
+        n = kept.numel()
+        a = GatherArgs(_SIZEOF_GATHER, n, keep.shape[1], 1 if rotate else 0, _table_rows(src_table, "src_table", n), _table_rows(dst_table, "dst_table", n),
+                       keep.data_ptr(), _table_rows(keep, "keep", n), _counts(kept, "kept", n), _counts(kv_len, "kv_len", n),
+                       src_table.data_ptr(), dst_table.data_ptr())
+        if n > 1 and (src_table.stride(0) != src_table.shape[1] or dst_table.stride(0) != dst_table.shape[1]):
+            raise ValueError("src_table, dst_table: contiguous")
+        pool, pages = (None, cache) if isinstance(cache, QPool) else (cache, None)
+        rc = lib().patchkv_cache_gather(self._h, geom, pool, pages, layer, a, _stream_of(stream, self.device))
         return rc if rc == OK else self._check(rc, check)
 
     def selftest_bounded_wait(self, max_polls: int, stream=None, check: bool = True) -> int:

@@ -123,22 +123,6 @@ int check_attention(patchkv_ctx* ctx, const patchkv_geom* g, int tag, const patc
     return PATCHKV_OK;
 }
 
-int fill_pool(patchkv_ctx* ctx, const patchkv_geom* g, const patchkv_pool* q, int layer, CacheDev* c) {
-    if (q->struct_size != sizeof(patchkv_pool)) return fail(ctx, PATCHKV_E_INVALID, "attention: wrong struct_size of the pool");
-    const uintptr_t k = reinterpret_cast<uintptr_t>(q->k_base), v = reinterpret_cast<uintptr_t>(q->v_base);
-    if (!k || !v || ((k | v) & 15u) || q->n_pages <= 0) return fail(ctx, PATCHKV_E_INVALID, "attention: pool base null or not 16-byte aligned, or no pages");
-    if (q->stride_layer < 0 || q->stride_page < 0 || q->stride_token < 0 || q->stride_head < 0)
-        return fail(ctx, PATCHKV_E_INVALID, "attention: negative pool stride");
-    memset(c, 0, sizeof(*c));
-    c->k = static_cast<const uint16_t*>(q->k_base) + (long long)layer * q->stride_layer;
-    c->v = static_cast<const uint16_t*>(q->v_base) + (long long)layer * q->stride_layer;
-    c->stride_page = q->stride_page; c->stride_token = q->stride_token; c->stride_head = q->stride_head;
-    c->n_pages = q->n_pages; c->H = g->n_kv_heads; c->D = g->head_dim; c->P = g->page_tokens; c->G = g->group;
-    c->P_shift = log2_exact(g->page_tokens);
-    c->tag = PATCHKV_TAG_BF16;
-    return PATCHKV_OK;
-}
-
 constexpr int kSms = 148;                        // B200; only sizes launches, so that results don't depend on the context
 
 // How a call is served.
@@ -231,7 +215,7 @@ extern "C" int patchkv_attention(patchkv_ctx* ctx, const patchkv_geom* g, const 
     if ((pool != nullptr) == (cache != nullptr)) return fail(ctx, PATCHKV_E_INVALID, "attention: give a pool or a cache, one of the two");
     int rc = check_live_geometry(ctx, "attention", g, layer);
     if (rc == PATCHKV_OK) rc = fill_batch(ctx, "attention", batch, &p.b);
-    if (rc == PATCHKV_OK) rc = pool ? fill_pool(ctx, g, pool, layer, &p.c) : fill_cache(ctx, "attention", g, cache, layer, &p.c);
+    if (rc == PATCHKV_OK) rc = pool ? fill_pool(ctx, "attention", g, pool, layer, &p.c) : fill_cache(ctx, "attention", g, cache, layer, &p.c);
     if (rc != PATCHKV_OK) return rc;
     if (!a || a->struct_size != sizeof(patchkv_attention_args)) return fail(ctx, PATCHKV_E_INVALID, "attention: null args or wrong struct_size");
     rc = check_attention(ctx, g, p.c.tag, batch, a->n_q_heads, a->window, a->sinks);

@@ -1,0 +1,458 @@
+// Cutting a cache down: which tokens stay (patchkv_evict_select), and their rows' way into other pages (patchkv_cache_gather).
+#include <cooperative_groups.h>
+
+#include "attention_launch.cuh"
+#include "rotary.cuh"
+
+namespace patchkv {
+
+namespace cg = cooperative_groups;
+
+// ---------------------------------------------------------------- which tokens stay
+constexpr int kSelectThreads = 1024, kSelectWarps = kSelectThreads / 32, kSelectBins = 2048, kSelectCached = 32768;
+
+struct EvictParams {
+    const float* mass;
+    const int32_t* kv_len;
+    const int32_t* budget;
+    int32_t* keep;
+    int32_t* kept;
+    float* mass_out;
+    long long mass_stride, keep_stride, out_stride;
+    int32_t max_len, max_keep, recent, sinks;
+    int32_t* status;
+};
+
+// A cluster takes a sequence, each of its CTAs a run of the tokens, whose masses stay in shared memory as keys: bit patterns, which
+// order numbers that are not negative.  The key of the last token that stays is found digit by digit (11, 11 and 10 bits): every CTA counts
+// its keys by digit, the counts are added up in the first CTA's shared memory, which finds the digit.  Then each warp counts what of its
+// run stays, and a prefix over warps and CTAs gives every kept token its place.  All counts are whole numbers: the order of the
+// atomics does not matter.
+__global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const EvictParams p) {
+    extern __shared__ uint32_t cached[];
+    __shared__ int bins[kSelectBins];
+    __shared__ int warp_sums[33];
+    __shared__ int found[2];                    // digit, and how many keys lie above it (first CTA)
+    __shared__ int2 warp_count[kSelectWarps];   // tokens that stay in any case, and those at the border
+    __shared__ int2 cta_count[16];              // of every CTA of the cluster
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
+    const int s = blockIdx.x / ctas, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    pdl_trigger();
+    pdl_wait();
+    int n = p.kv_len[s], B = p.budget ? p.budget[s] : p.max_keep;
+    if (rank == 0 && tid == 0 && (n > p.max_len || B > p.max_keep)) atomicCAS(p.status, 0, (int)PATCHKV_E_BOUNDS);
+    n = max(0, min(n, p.max_len));
+    B = max(0, min(B, p.max_keep));
+    const int kept = min(n, B), last = n <= B ? n : min(p.recent, B), first = n <= B ? 0 : min(p.sinks, B - last);
+    const int wanted = kept - last - first;     // of the middle, tokens [first, n - last)
+    // this CTA's run, a whole number of steps of a warp for each warp
+    const int run = (n + ctas * kSelectThreads - 1) / (ctas * kSelectThreads) * kSelectThreads, base = rank * run;
+    const float* mass = p.mass + (long long)s * p.mass_stride;
+    auto key_of = [&](int i, bool report) {     // of token base + i
+        const float x = mass[base + i];
+        const uint32_t bits = __float_as_uint(x);
+        if (bits < 0x7F800000u) return bits;
+        if (bits != 0x80000000u && report) atomicCAS(p.status, 0, (int)PATCHKV_E_BADINPUT);
+        return 0u;
+    };
+    auto key = [&](int i) { return i < kSelectCached ? cached[i] : key_of(i, false); };
+    for (int i = tid; i < run; i += kSelectThreads) {
+        const uint32_t k = base + i < n ? key_of(i, true) : 0u;
+        if (i < kSelectCached) cached[i] = k;
+    }
+    uint32_t border = 0;                        // key of the last token that stays, so far as it is known
+    int need = wanted;                          // how many of those keys that agree with it so far stay
+    if (wanted > 0) {
+#pragma unroll 1
+        for (int pass = 0; pass < 3; pass++) {
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 0 ? 32 : pass == 1 ? 21 : 10;
+            for (int i = tid; i < kSelectBins; i += kSelectThreads) bins[i] = 0;
+            cluster.sync();                     // the keys are there, and all bins are empty
+            for (int i = tid; i < run; i += kSelectThreads) {
+                const int t = base + i;
+                if (t < first || t >= n - last) continue;
+                const uint32_t k = key(i);
+                if (above == 32 || (k >> above) == (border >> above)) atomicAdd(&bins[(k >> shift) & (kSelectBins - 1) & ((1u << (above - shift)) - 1u)], 1);
+            }
+            if (rank != 0) {
+                __syncthreads();
+                int* to = cluster.map_shared_rank(bins, 0);
+                for (int i = tid; i < kSelectBins; i += kSelectThreads)
+                    if (bins[i]) atomicAdd(&to[i], bins[i]);
+            }
+            cluster.sync();
+            if (rank == 0) {                    // bins from the top: thread i has the bins 2047 - 2i and 2046 - 2i
+                const int a = bins[kSelectBins - 1 - 2 * tid], b = bins[kSelectBins - 2 - 2 * tid];
+                int total;
+                const int before = cta_exclusive_scan(a + b, warp_sums, &total);
+                if (before < need && need <= before + a + b) {
+                    const bool second = need > before + a;
+                    found[0] = kSelectBins - 1 - 2 * tid - second;
+                    found[1] = before + (second ? a : 0);
+                }
+            }
+            cluster.sync();
+            const int* from = cluster.map_shared_rank(found, 0);
+            border |= (uint32_t)from[0] << shift;
+            need -= from[1];
+        }
+    } else {
+        __syncthreads();
+    }
+    // What stays: in any case (bit 0), or if it is among the first `need` at the border (bit 1).
+    auto standing = [&](int i) {
+        const int t = base + i;
+        if (t >= n) return 0;
+        if (t < first || t >= n - last) return 1;
+        if (wanted == 0) return 0;
+        const uint32_t k = key(i);
+        return k > border ? 1 : k == border ? 2 : 0;
+    };
+    const int begin = warp * (run / kSelectWarps), end = begin + run / kSelectWarps;
+    int2 mine = make_int2(0, 0);
+    for (int i = begin + lane; i < end; i += 32) {
+        const int x = standing(i);
+        mine.x += __popc(__ballot_sync(0xFFFFFFFFu, x & 1));
+        mine.y += __popc(__ballot_sync(0xFFFFFFFFu, x & 2));
+    }
+    if (lane == 0) warp_count[warp] = mine;
+    __syncthreads();
+    if (warp == 0) {
+        int2 c = warp_count[lane], sum = c;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int a = __shfl_up_sync(0xFFFFFFFFu, sum.x, d), b = __shfl_up_sync(0xFFFFFFFFu, sum.y, d);
+            if (lane >= d) { sum.x += a; sum.y += b; }
+        }
+        warp_count[lane] = make_int2(sum.x - c.x, sum.y - c.y);
+        const int2 all = make_int2(__shfl_sync(0xFFFFFFFFu, sum.x, 31), __shfl_sync(0xFFFFFFFFu, sum.y, 31));
+        if (lane < ctas) cluster.map_shared_rank(cta_count, lane)[rank] = all;
+    }
+    cluster.sync();
+    int2 at = warp_count[warp];
+    for (int i = 0; i < rank; i++) { at.x += cta_count[i].x; at.y += cta_count[i].y; }
+    int32_t* keep = p.keep + (long long)s * p.keep_stride;
+    float* out = p.mass_out ? p.mass_out + (long long)s * p.out_stride : nullptr;
+    const uint32_t below = (1u << lane) - 1u;
+    for (int i = begin + lane; i < end; i += 32) {
+        const int x = standing(i);
+        const uint32_t sure = __ballot_sync(0xFFFFFFFFu, x & 1), edge = __ballot_sync(0xFFFFFFFFu, x & 2);
+        const int ties = at.y + __popc(edge & below), place = at.x + __popc(sure & below) + min(ties, need);
+        if ((x & 1) || ((x & 2) && ties < need)) {
+            keep[place] = base + i;
+            if (out) out[place] = __uint_as_float(key(i));
+        }
+        at.x += __popc(sure);
+        at.y += __popc(edge);
+    }
+    for (int i = kept + rank * kSelectThreads + tid; i < p.max_keep; i += ctas * kSelectThreads) keep[i] = -1;
+    if (rank == 0 && tid == 0) p.kept[s] = kept;
+    cluster.sync();                             // nobody's shared memory goes while it may still be read
+}
+
+// ---------------------------------------------------------------- their rows
+constexpr int kGatherThreads = 128;
+
+struct MoveParams {
+    CacheDev c;
+    uint16_t* k_pool;
+    uint16_t* v_pool;
+    const int32_t* keep;
+    const int32_t* kept;
+    const int32_t* kv_len;
+    const int32_t* src_table;
+    const int32_t* dst_table;
+    long long keep_stride;
+    int32_t* status;
+    int32_t n_seqs, max_keep, src_stride, dst_stride, rotate, Dr, half;
+    int32_t parts, passes, U_shift;             // pools: warps that share a row; passes over K or V; 16-channel units of a head
+    uint32_t k_row, s_row, v_row;               // quantised pages: bytes of a row's K codes, scales (of K or V) and V codes
+    Frequencies f;
+};
+
+struct Move { int from, to, slot, to_slot, turn; };         // pages and slots; positions moved
+// Where row i of sequence s comes from and goes to; false when it is skipped (latched by the caller's `report` thread).
+__device__ __forceinline__ bool find_move(const MoveParams& p, int s, int i, bool report, Move* m) {
+    const int old = p.keep[(long long)s * p.keep_stride + i];
+    bool ok = old >= 0 && old < p.kv_len[s];
+    if (ok) {
+        const int lp = div_page(p.c, old), tp = div_page(p.c, i);
+        ok = lp < p.src_stride && tp < p.dst_stride;
+        if (ok) {
+            m->from = p.src_table[(long long)s * p.src_stride + lp];
+            m->to = p.dst_table[(long long)s * p.dst_stride + tp];
+            m->slot = old - lp * p.c.P;
+            m->to_slot = i - tp * p.c.P;
+            m->turn = i - old;
+            ok = m->from >= 0 && m->from < p.c.n_pages && m->to >= 0 && m->to < p.c.n_pages;
+        }
+    }
+    if (!ok && report) atomicCAS(p.status, 0, (int)PATCHKV_E_BOUNDS);
+    return ok;
+}
+__device__ __forceinline__ int rows_of(const MoveParams& p, int s) {
+    const int n = p.kept[s];
+    if (n > p.max_keep && blockIdx.x == 0 && threadIdx.x == 0) atomicCAS(p.status, 0, (int)PATCHKV_E_BOUNDS);
+    return min(n, p.max_keep);
+}
+
+// Rows of a bf16 pool (grid: warps, sequence): a warp takes a row, or every `parts`-th pass of one; a pass is 32 units of 16 channels, keys and
+// then values, laid out over the lanes as in rotary_append_kernel.
+template <bool HALF>
+__global__ void __launch_bounds__(kGatherThreads) gather_pool_kernel(const __grid_constant__ MoveParams p) {
+    __shared__ float2 table[kGatherThreads / 32][PATCHKV_MAX_ROTARY_DIM / 2];
+    pdl_trigger();
+    pdl_wait();
+    const int s = blockIdx.y, lane = threadIdx.x & 31;
+    const uint32_t wid = (blockIdx.x * kGatherThreads + threadIdx.x) >> 5;
+    const int i = (int)(wid / (uint32_t)p.parts), part = (int)(wid - (uint32_t)i * p.parts);
+    if (i >= rows_of(p, s)) return;
+    Move m;
+    if (!find_move(p, s, i, lane == 0 && part == 0, &m)) return;
+    const int u = lane & ((1 << p.U_shift) - 1), sub = lane >> p.U_shift, total = 2 * p.passes;
+    const long long from = (long long)m.from * p.c.stride_page + (long long)m.slot * p.c.stride_token + 16 * u;
+    const long long to = (long long)m.to * p.c.stride_page + (long long)m.to_slot * p.c.stride_token + 16 * u;
+    struct Unit { uint4 a, b; };
+    auto head_of = [&](int pass) { return ((pass < p.passes ? pass : pass - p.passes) << (5 - p.U_shift)) + sub; };
+    auto load = [&](int pass) {
+        Unit x = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+        const int h = head_of(pass);
+        if (pass >= total || h >= p.c.H) return x;
+        const uint4* a = reinterpret_cast<const uint4*>((pass < p.passes ? p.c.k : p.c.v) + from + (long long)h * p.c.stride_head);
+        x.a = a[0];
+        x.b = a[1];
+        return x;
+    };
+    Unit next = load(part);
+    const bool rotate = p.rotate && m.turn != 0;
+    float2* tab = table[threadIdx.x >> 5];
+    if (rotate && part < p.passes)
+        for (int j = lane; j < p.Dr >> 1; j += 32) {
+            double c, sn;
+            cos_sin((double)m.turn * p.f.theta[j], &c, &sn);
+            tab[j] = make_float2((float)c, (float)sn);
+        }
+    __syncwarp();
+    const int away = p.Dr >> 5;
+    const bool turns = rotate && 16 * u < p.Dr, upper = HALF && u >= away;
+    const int partner = HALF && turns ? (upper ? lane - away : lane + away) : lane;
+    const float2* mine = tab + (!turns ? 0 : HALF ? 16 * (upper ? u - away : u) : 8 * u);
+#pragma unroll 1
+    for (int pass = part; pass < total; pass += p.parts) {
+        const Unit x = next;
+        next = load(pass + p.parts);
+        const int h = head_of(pass);
+        uint32_t w[8] = {x.a.x, x.a.y, x.a.z, x.a.w, x.b.x, x.b.y, x.b.z, x.b.w};
+        if (rotate && pass < p.passes) {
+            uint32_t o[8];
+#pragma unroll
+            for (int k = 0; k < 8; k++) o[k] = HALF ? __shfl_sync(0xFFFFFFFFu, w[k], partner) : 0u;
+            if (turns)
+#pragma unroll
+                for (int k = 0; k < 8; k++) {
+                    const float a = bf16_bits_to_float(w[k] & 0xFFFFu), b = __uint_as_float(w[k] & 0xFFFF0000u);
+                    __nv_bfloat162 y;
+                    if (HALF) {
+                        const float a2 = bf16_bits_to_float(o[k] & 0xFFFFu), b2 = __uint_as_float(o[k] & 0xFFFF0000u);
+                        const float2 t0 = mine[2 * k], t1 = mine[2 * k + 1];
+                        y = __floats2bfloat162_rn(fmaf(a2, upper ? t0.y : -t0.y, a * t0.x), fmaf(b2, upper ? t1.y : -t1.y, b * t1.x));
+                    } else {
+                        const float2 t = mine[k];
+                        y = __floats2bfloat162_rn(fmaf(-b, t.y, a * t.x), fmaf(b, t.x, a * t.y));
+                    }
+                    w[k] = *reinterpret_cast<const uint32_t*>(&y);
+                }
+        }
+        if (h < p.c.H) {
+            uint4* a = reinterpret_cast<uint4*>((pass < p.passes ? p.k_pool : p.v_pool) + to + (long long)h * p.c.stride_head);
+            a[0] = make_uint4(w[0], w[1], w[2], w[3]);
+            a[1] = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+    }
+}
+
+// Rows of quantised pages (grid: warps, sequence): a row's codes and scales are a run of bytes in each of the page's four sections.
+// A warp takes a row, codes by 16 bytes and scales by 4.
+__global__ void __launch_bounds__(kGatherThreads) gather_codes_kernel(const __grid_constant__ MoveParams p) {
+    pdl_trigger();
+    pdl_wait();
+    const int s = blockIdx.y, lane = threadIdx.x & 31, i = (int)((blockIdx.x * kGatherThreads + threadIdx.x) >> 5);
+    if (i >= rows_of(p, s)) return;
+    Move m;
+    if (!find_move(p, s, i, lane == 0, &m)) return;
+    const uint8_t* from = p.c.base + (long long)m.from * p.c.stride_page;
+    uint8_t* to = p.c.base + (long long)m.to * p.c.stride_page;
+    const uint32_t ks = p.c.k_scales + m.slot * p.s_row, kd = p.c.k_scales + m.to_slot * p.s_row;
+    const uint32_t vs = p.c.v_scales + m.slot * p.s_row, vd = p.c.v_scales + m.to_slot * p.s_row;
+    const uint32_t k16 = p.k_row / 16, v16 = p.v_row / 16, s4 = p.s_row / 4, steps = max(max(k16, v16), s4);
+#pragma unroll 1
+    for (uint32_t j = lane; j < steps; j += 32) {
+        uint4 k = make_uint4(0, 0, 0, 0), v = k;
+        uint32_t a = 0, b = 0;
+        if (j < k16) k = *(reinterpret_cast<const uint4*>(from + m.slot * p.k_row) + j);
+        if (j < v16) v = *(reinterpret_cast<const uint4*>(from + p.c.v_codes + m.slot * p.v_row) + j);
+        if (j < s4) { a = *(reinterpret_cast<const uint32_t*>(from + ks) + j); b = *(reinterpret_cast<const uint32_t*>(from + vs) + j); }
+        if (j < k16) *(reinterpret_cast<uint4*>(to + m.to_slot * p.k_row) + j) = k;
+        if (j < v16) *(reinterpret_cast<uint4*>(to + p.c.v_codes + m.to_slot * p.v_row) + j) = v;
+        if (j < s4) { *(reinterpret_cast<uint32_t*>(to + kd) + j) = a; *(reinterpret_cast<uint32_t*>(to + vd) + j) = b; }
+    }
+}
+
+// Any geometry, any strides: a thread per row and head (grid: threads, sequence), byte by byte and pair by pair.
+__global__ void __launch_bounds__(kGatherThreads) gather_any_kernel(const __grid_constant__ MoveParams p) {
+    const int s = blockIdx.y;
+    const uint32_t id = blockIdx.x * kGatherThreads + threadIdx.x;
+    const int i = (int)(id / (uint32_t)p.c.H), h = (int)(id - (uint32_t)i * p.c.H), D = p.c.D;
+    if (i >= rows_of(p, s)) return;
+    Move m;
+    if (!find_move(p, s, i, h == 0, &m)) return;
+    if (p.c.tag == PATCHKV_TAG_BF16) {
+        const long long from = (long long)m.from * p.c.stride_page + (long long)m.slot * p.c.stride_token + (long long)h * p.c.stride_head;
+        const long long to = (long long)m.to * p.c.stride_page + (long long)m.to_slot * p.c.stride_token + (long long)h * p.c.stride_head;
+        const int Dr = p.rotate && m.turn != 0 ? p.Dr : 0;
+        for (int j = 0; j < Dr >> 1; j++) {
+            const int c0 = p.half ? j : 2 * j, c1 = p.half ? j + (Dr >> 1) : 2 * j + 1;
+            double c, sn;
+            cos_sin((double)m.turn * p.f.theta[j], &c, &sn);
+            const float cf = (float)c, sf = (float)sn, a = bf16_bits_to_float(p.c.k[from + c0]), b = bf16_bits_to_float(p.c.k[from + c1]);
+            p.k_pool[to + c0] = __bfloat16_as_ushort(__float2bfloat16_rn(fmaf(-b, sf, a * cf)));
+            p.k_pool[to + c1] = __bfloat16_as_ushort(__float2bfloat16_rn(fmaf(b, cf, a * sf)));
+        }
+        for (int c = Dr; c < D; c++) p.k_pool[to + c] = p.c.k[from + c];
+        for (int c = 0; c < D; c++) p.v_pool[to + c] = p.c.v[from + c];
+        return;
+    }
+    const uint8_t* from = p.c.base + (long long)m.from * p.c.stride_page;
+    uint8_t* to = p.c.base + (long long)m.to * p.c.stride_page;
+    const uint32_t section[4] = {0, p.c.k_scales, p.c.v_codes, p.c.v_scales}, row[4] = {p.k_row, p.s_row, p.v_row, p.s_row};
+    for (int q = 0; q < 4; q++)
+        for (uint32_t j = row[q] / p.c.H * h; j < row[q] / p.c.H * (h + 1); j++)        // a head's bytes: whole ones, D is even
+            to[section[q] + m.to_slot * row[q] + j] = from[section[q] + m.slot * row[q] + j];
+}
+
+namespace {
+
+int evict_select(patchkv_ctx* ctx, const patchkv_evict_args* a, cudaStream_t stream) {
+    if (!a || a->struct_size != sizeof(patchkv_evict_args)) return fail(ctx, PATCHKV_E_INVALID, "evict_select: null args or wrong struct_size");
+    if (a->n_seqs < 0 || a->max_len < 0 || a->max_keep < 0 || a->recent < 0 || a->sinks < 0)
+        return fail(ctx, PATCHKV_E_INVALID, "evict_select: negative count");
+    if (a->max_len > 1 << 24) return fail(ctx, PATCHKV_E_UNSUPPORTED, "evict_select: max_len above 2^24");
+    if (a->n_seqs > 65535) return fail(ctx, PATCHKV_E_UNSUPPORTED, "evict_select: more than 65535 sequences");
+    if (a->mass_stride < a->max_len || a->keep_stride < a->max_keep || (a->mass_out && a->mass_out_stride < a->max_keep))
+        return fail(ctx, PATCHKV_E_INVALID, "evict_select: a stride is smaller than its row");
+    if (a->n_seqs == 0) return PATCHKV_OK;
+    if (!a->kv_len || !a->kept || (a->max_keep > 0 && !a->keep) || (a->max_len > 0 && !a->mass))
+        return fail(ctx, PATCHKV_E_INVALID, "evict_select: null mass, kv_len, keep or kept");
+    if (((reinterpret_cast<uintptr_t>(a->mass) | reinterpret_cast<uintptr_t>(a->kv_len) | reinterpret_cast<uintptr_t>(a->budget) |
+          reinterpret_cast<uintptr_t>(a->keep) | reinterpret_cast<uintptr_t>(a->kept) | reinterpret_cast<uintptr_t>(a->mass_out)) & 3) != 0)
+        return fail(ctx, PATCHKV_E_INVALID, "evict_select: misaligned array");
+    if (a->kept == a->kv_len || a->kept == a->budget || a->mass_out == a->mass)
+        return fail(ctx, PATCHKV_E_INVALID, "evict_select: an output is an input");
+    const EvictParams p = {a->mass, a->kv_len, a->budget, a->keep, a->kept, a->mass_out, a->mass_stride, a->keep_stride, a->mass_out_stride,
+                           a->max_len, a->max_keep, a->recent, a->sinks, ctx->d_status};
+    // CTAs of a cluster: one for every 4096 tokens, up to eight.
+    int ctas = 1;
+    while (ctas < 8 && (long long)ctas * 4096 < a->max_len) ctas *= 2;
+    const int run = (a->max_len + ctas * kSelectThreads - 1) / (ctas * kSelectThreads) * kSelectThreads;
+    const int smem = std::min(run, kSelectCached) * 4;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(ctx, PATCHKV_E_CUDA, "cudaSetDevice failed");
+    static std::atomic<uint64_t> allowed{0};
+    PKV_CUDA(ctx, allow_smem((const void*)evict_select_kernel, kSelectCached * 4, &allowed));
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = dim3(a->n_seqs * ctas); cfg.blockDim = dim3(kSelectThreads); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    PKV_CUDA(ctx, cudaLaunchKernelEx(&cfg, evict_select_kernel, p));
+    return PATCHKV_OK;
+}
+
+int cache_gather(patchkv_ctx* ctx, const patchkv_geom* g, const patchkv_pool* pool, const patchkv_qpool* cache, int layer,
+                 const patchkv_gather_args* a, cudaStream_t stream) {
+    MoveParams p;
+    if ((pool != nullptr) == (cache != nullptr)) return fail(ctx, PATCHKV_E_INVALID, "cache_gather: give a pool or a cache, one of the two");
+    int rc = check_live_geometry(ctx, "cache_gather", g, layer);
+    if (rc == PATCHKV_OK) rc = pool ? fill_pool(ctx, "cache_gather", g, pool, layer, &p.c) : fill_cache(ctx, "cache_gather", g, cache, layer, &p.c);
+    if (rc != PATCHKV_OK) return rc;
+    if (!a || a->struct_size != sizeof(patchkv_gather_args)) return fail(ctx, PATCHKV_E_INVALID, "cache_gather: null args or wrong struct_size");
+    if (a->n_seqs < 0 || a->max_keep < 0 || a->src_stride < 0 || a->dst_stride < 0) return fail(ctx, PATCHKV_E_INVALID, "cache_gather: negative count");
+    if (a->n_seqs > 65535) return fail(ctx, PATCHKV_E_UNSUPPORTED, "cache_gather: more than 65535 sequences");
+    if (a->rotate != 0 && a->rotate != 1) return fail(ctx, PATCHKV_E_INVALID, "cache_gather: rotate must be 0 or 1");
+    if (a->rotate && !pool) return fail(ctx, PATCHKV_E_UNSUPPORTED, "cache_gather: keys of quantised pages are moved as they are; rotate needs a bf16 pool");
+    if (a->keep_stride < a->max_keep) return fail(ctx, PATCHKV_E_INVALID, "cache_gather: keep_stride is smaller than max_keep");
+    if (a->n_seqs == 0 || a->max_keep == 0) return PATCHKV_OK;
+    if (!a->keep || !a->kept || !a->kv_len || (a->src_stride > 0 && !a->src_table) || (a->dst_stride > 0 && !a->dst_table))
+        return fail(ctx, PATCHKV_E_INVALID, "cache_gather: null keep, kept, kv_len or table");
+    p.Dr = 0;
+    if (a->rotate) {
+        rc = fill_frequencies(ctx, "cache_gather", g, &p.f);
+        if (rc != PATCHKV_OK) return rc;
+        p.Dr = g->rotary_dim;
+    }
+    const bool half = a->rotate && g->rope_style == PATCHKV_ROPE_HALF;
+    p.k_pool = const_cast<uint16_t*>(p.c.k); p.v_pool = const_cast<uint16_t*>(p.c.v);
+    p.keep = a->keep; p.kept = a->kept; p.kv_len = a->kv_len; p.src_table = a->src_table; p.dst_table = a->dst_table;
+    p.keep_stride = a->keep_stride;
+    p.status = ctx->d_status;
+    p.n_seqs = a->n_seqs; p.max_keep = a->max_keep; p.src_stride = a->src_stride; p.dst_stride = a->dst_stride;
+    p.rotate = a->rotate; p.half = half;
+    const int H = g->n_kv_heads, D = g->head_dim, ds = log2_exact(D);
+    p.k_row = (uint32_t)code_bytes(k_format(p.c.tag), (uint64_t)H * D);
+    p.v_row = (uint32_t)code_bytes(v_format(p.c.tag), (uint64_t)H * D);
+    p.s_row = 2u * (uint32_t)(H * (D / g->group));
+    p.parts = 1; p.passes = 0; p.U_shift = 0;
+    bool fast;
+    long long threads;                                      // of a sequence
+    if (pool) {
+        fast = ds >= 4 && ds <= 8 && p.Dr % (half ? 32 : 16) == 0 && p.c.stride_page % 8 == 0 && p.c.stride_token % 8 == 0 &&
+               p.c.stride_head % 8 == 0 && pool->stride_layer % 8 == 0;
+        if (fast) {
+            p.U_shift = ds - 4;
+            const int per_pass = 32 >> p.U_shift;           // heads
+            p.passes = (H + per_pass - 1) / per_pass;
+            if ((long long)a->n_seqs * a->max_keep * 2 * p.passes <= 16 * 148) p.parts = 2 * p.passes;      // few rows: a warp for each pass
+        }
+        threads = (long long)a->max_keep * (fast ? 32 * p.parts : H);
+    } else {
+        fast = p.k_row % 16 == 0 && p.v_row % 16 == 0 && p.s_row % 4 == 0 && p.c.k_scales % 16 == 0 && p.c.v_codes % 16 == 0 && p.c.v_scales % 16 == 0;
+        threads = (long long)a->max_keep * (fast ? 32 : H);
+    }
+    const long long grid = (threads + kGatherThreads - 1) / kGatherThreads;
+    if (grid * kGatherThreads > (1ll << 32) - 1) return fail(ctx, PATCHKV_E_UNSUPPORTED, "cache_gather: too many rows for one call");
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(ctx, PATCHKV_E_CUDA, "cudaSetDevice failed");
+    const dim3 blocks((unsigned)grid, a->n_seqs), block(kGatherThreads);
+    if (!fast) {
+        gather_any_kernel<<<blocks, block, 0, stream>>>(p);
+        PKV_CUDA(ctx, cudaGetLastError());
+    } else if (!pool) {
+        PKV_CUDA(ctx, launch_pdl(gather_codes_kernel, blocks, block, 0, stream, p));
+    } else {
+        PKV_CUDA(ctx, half ? launch_pdl(gather_pool_kernel<true>, blocks, block, 0, stream, p) : launch_pdl(gather_pool_kernel<false>, blocks, block, 0, stream, p));
+    }
+    return PATCHKV_OK;
+}
+
+}  // namespace
+}  // namespace patchkv
+
+using namespace patchkv;
+
+extern "C" int patchkv_evict_select(patchkv_ctx* ctx, const patchkv_evict_args* args, void* stream) {
+    if (!ctx) return PATCHKV_E_INVALID;
+    std::lock_guard<std::mutex> lock(ctx->mu);
+    return evict_select(ctx, args, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int patchkv_cache_gather(patchkv_ctx* ctx, const patchkv_geom* geom, const patchkv_pool* pool, const patchkv_qpool* cache,
+                                    int layer, const patchkv_gather_args* args, void* stream) {
+    if (!ctx) return PATCHKV_E_INVALID;
+    std::lock_guard<std::mutex> lock(ctx->mu);
+    return cache_gather(ctx, geom, pool, cache, layer, args, static_cast<cudaStream_t>(stream));
+}

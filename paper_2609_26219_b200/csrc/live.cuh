@@ -75,6 +75,7 @@ __device__ __forceinline__ float scale_at(const uint8_t* scales, unsigned long l
 // Host side: validation, and the device form of the structs.  Without a context (a size is asked for) arrays may be null.
 int fill_batch(patchkv_ctx* ctx, const char* who, const patchkv_batch* b, BatchDev* out);
 int fill_cache(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, const patchkv_qpool* q, int layer, CacheDev* out);
+int fill_pool(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, const patchkv_pool* q, int layer, CacheDev* out);
 int check_live_geometry(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, int layer);
 // Whether two of the n * H vectors of D elements at these strides share an element (rows within heads or heads within rows).
 bool rows_overlap(long long n, long long H, long long D, long long stride_row, long long stride_head);

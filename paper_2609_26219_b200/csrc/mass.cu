@@ -1,0 +1,182 @@
+// The attention weight that cached tokens receive (patchkv_attention_mass).
+#include <math.h>
+
+#include <algorithm>
+
+#include "mass.cuh"
+
+namespace patchkv {
+
+// ---------------------------------------------------------------- any geometry, any strides
+constexpr int kMassThreads = 128;
+
+// scale * log2(e) * q . k of a token at a place of the cache (pools: element offset; quantised pages: page and element index).
+struct KeyPlace { long long at; unsigned long long e; };
+__device__ __forceinline__ bool find_key(const AttentionParams& p, int s, int t, int h, KeyPlace* k) {
+    const int lp = div_page(p.c, t), slot = t - lp * p.c.P;
+    const int page = p.b.block_table[(long long)s * p.b.table_stride + lp];
+    if (page < 0 || page >= p.c.n_pages) return false;
+    if (p.c.tag == PATCHKV_TAG_BF16) {
+        k->at = (long long)page * p.c.stride_page + (long long)slot * p.c.stride_token + (long long)h * p.c.stride_head;
+    } else {
+        k->at = (long long)page * p.c.stride_page;
+        k->e = ((unsigned long long)slot * p.c.H + h) * p.c.D;
+    }
+    return true;
+}
+__device__ __forceinline__ float logit(const AttentionParams& p, const KeyPlace& k, const float* q) {
+    float x = 0.0f;
+    if (p.c.tag == PATCHKV_TAG_BF16) {
+        for (int c = 0; c < p.c.D; c++) x = fmaf(q[c], bf16_bits_to_float(p.c.k[k.at + c]), x);
+    } else {
+        const uint8_t* pg = p.c.base + k.at;
+        const int fmt = k_format(p.c.tag);
+        for (int c0 = 0; c0 < p.c.D; c0 += p.c.G) {
+            float y = 0.0f;
+            for (int c = c0; c < c0 + p.c.G; c++) y = fmaf(q[c], (float)code_at(pg, fmt, k.e + c), y);
+            x = fmaf(y, scale_at(pg + p.c.k_scales, (k.e + c0) / p.c.G), x);
+        }
+    }
+    return x * p.scale_log2;
+}
+__device__ __forceinline__ void load_query(const AttentionParams& p, int r, int hq, float* q) {
+    const uint16_t* qs = p.q + (long long)r * p.q_stride_row + (long long)hq * p.q_stride_head;
+    for (int c = threadIdx.x; c < p.c.D; c += kMassThreads) q[c] = p.f16 ? half_bits_to_float(qs[c]) : bf16_bits_to_float(qs[c]);
+}
+
+// One CTA per (row, query head): log2 of the sum of 2^logit over the tokens that the row sees; infinity for a row that sees none, so that
+// its weights are zero.
+__global__ void __launch_bounds__(kMassThreads) mass_sums_any_kernel(const AttentionParams p, float* sums) {
+    __shared__ float q[PATCHKV_MAX_ATTENTION_DIM];
+    __shared__ float2 red[kMassThreads];
+    const int s = blockIdx.z, hq = blockIdx.y, h = hq / p.share;
+    int first, kv, rows;
+    const bool ordered = sequence_rows(p, s, &first, &kv, &rows);
+    if (threadIdx.x == 0 && (!ordered || rows > p.b.max_rows || (rows > 0 && p.b.kv_len[s] > kv))) latch(p.status);
+    if (!ordered || (int)blockIdx.x >= min(rows, p.b.max_rows)) return;
+    const int r = first + blockIdx.x, pos = row_position(p.b, s, r);
+    load_query(p, r, hq, q);
+    __syncthreads();
+    float m = -INFINITY, l = 0.0f;
+    for (int t = threadIdx.x; t <= min(pos, kv - 1); t += kMassThreads) {
+        if (!sees(p, pos, t)) continue;
+        KeyPlace k;
+        if (!find_key(p, s, t, h, &k)) { latch(p.status); continue; }
+        const float x = logit(p, k, q), to = fmaxf(m, x);
+        if (to == -INFINITY) continue;
+        l = l * exp2f(m - to) + exp2f(x - to);
+        m = to;
+    }
+    red[threadIdx.x] = make_float2(m, l);
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int i = 0; i < kMassThreads; i++) m = fmaxf(m, red[i].x);
+    l = 0.0f;
+    if (m != -INFINITY)
+        for (int i = 0; i < kMassThreads; i++) l += red[i].y * exp2f(red[i].x - m);
+    sums[(long long)r * p.Hq + hq] = l == 0.0f ? INFINITY : m + log2f(l);
+}
+
+// A thread per token: the weights of all rows and heads, in order.
+__global__ void __launch_bounds__(kMassThreads) mass_columns_any_kernel(const AttentionParams p, const WeightParams m, const float* sums) {
+    __shared__ float q[PATCHKV_MAX_ATTENTION_DIM];
+    const int s = blockIdx.y, t = blockIdx.x * kMassThreads + threadIdx.x;
+    int first, kv, rows;
+    if (!sequence_rows(p, s, &first, &kv, &rows)) return;
+    rows = min(rows, p.b.max_rows);
+    float total = 0.0f;
+    for (int hq = 0; hq < p.Hq; hq++) {
+        KeyPlace k;
+        const bool there = t < kv && find_key(p, s, t, hq / p.share, &k);
+        float sum = 0.0f;
+        for (int i = 0; i < rows; i++) {
+            const int r = first + i, pos = row_position(p.b, s, r);
+            __syncthreads();
+            load_query(p, r, hq, q);
+            __syncthreads();
+            if (there && t <= pos && sees(p, pos, t)) sum += exp2f(logit(p, k, q) - sums[(long long)r * p.Hq + hq]);
+        }
+        total += sum;
+    }
+    if (t < kv) store_mass(p, m, s, t, total);
+}
+
+namespace {
+
+int check_mass(patchkv_ctx* ctx, const patchkv_geom* g, int tag, const patchkv_batch* b, int Hq, int window, int sinks) {
+    if (g->head_dim > PATCHKV_MAX_ATTENTION_DIM) return fail(ctx, PATCHKV_E_UNSUPPORTED, "attention_mass: head_dim above 256");
+    if (Hq <= 0 || Hq % g->n_kv_heads) return fail(ctx, PATCHKV_E_INVALID, "attention_mass: n_q_heads must be a positive multiple of n_kv_heads");
+    if (window < 0 || sinks < 0) return fail(ctx, PATCHKV_E_INVALID, "attention_mass: negative window or sinks");
+    if (Hq > 65535 || b->n_seqs > 65535) return fail(ctx, PATCHKV_E_UNSUPPORTED, "attention_mass: more than 65535 query heads or sequences");
+    if (tag < PATCHKV_TAG_BF16 || tag > PATCHKV_TAG_K4V4) return fail(ctx, PATCHKV_E_INVALID, "attention_mass: unknown tag");
+    return PATCHKV_OK;
+}
+
+}  // namespace
+}  // namespace patchkv
+
+using namespace patchkv;
+
+extern "C" uint64_t patchkv_attention_mass_workspace_bytes(const patchkv_geom* g, int tag, const patchkv_batch* b, int n_q_heads,
+                                                           int window, int sinks) {
+    BatchDev bd;
+    if (check_live_geometry(nullptr, "attention_mass", g, 0) != PATCHKV_OK || fill_batch(nullptr, "attention_mass", b, &bd) != PATCHKV_OK ||
+        check_mass(nullptr, g, tag, b, n_q_heads, window, sinks) != PATCHKV_OK)
+        return 0;
+    return ((uint64_t)b->n_rows * n_q_heads * 4 + 15) / 16 * 16;
+}
+
+extern "C" int patchkv_attention_mass(patchkv_ctx* ctx, const patchkv_geom* g, const patchkv_pool* pool, const patchkv_qpool* cache,
+                                      int layer, const patchkv_batch* batch, const patchkv_mass_args* a, void* stream_) {
+    if (!ctx) return PATCHKV_E_INVALID;
+    std::lock_guard<std::mutex> lock(ctx->mu);
+    AttentionParams p;
+    if ((pool != nullptr) == (cache != nullptr)) return fail(ctx, PATCHKV_E_INVALID, "attention_mass: give a pool or a cache, one of the two");
+    int rc = check_live_geometry(ctx, "attention_mass", g, layer);
+    if (rc == PATCHKV_OK) rc = fill_batch(ctx, "attention_mass", batch, &p.b);
+    if (rc == PATCHKV_OK) rc = pool ? fill_pool(ctx, "attention_mass", g, pool, layer, &p.c) : fill_cache(ctx, "attention_mass", g, cache, layer, &p.c);
+    if (rc != PATCHKV_OK) return rc;
+    if (!a || a->struct_size != sizeof(patchkv_mass_args)) return fail(ctx, PATCHKV_E_INVALID, "attention_mass: null args or wrong struct_size");
+    rc = check_mass(ctx, g, p.c.tag, batch, a->n_q_heads, a->window, a->sinks);
+    if (rc != PATCHKV_OK) return rc;
+    if (a->type != PATCHKV_ROWS_BF16 && a->type != PATCHKV_ROWS_F16) return fail(ctx, PATCHKV_E_INVALID, "attention_mass: unknown row type");
+    if (pool && a->type != PATCHKV_ROWS_BF16) return fail(ctx, PATCHKV_E_INVALID, "attention_mass: over a bf16 pool q must be bf16");
+    if (!(fabsf(a->scale) <= 3.0e38f)) return fail(ctx, PATCHKV_E_INVALID, "attention_mass: scale must be finite");
+    if (!(fabsf(a->decay) <= 3.0e38f)) return fail(ctx, PATCHKV_E_INVALID, "attention_mass: decay must be finite");
+    if (a->mass_type != PATCHKV_MASS_F32 && a->mass_type != PATCHKV_MASS_U64) return fail(ctx, PATCHKV_E_INVALID, "attention_mass: unknown mass type");
+    if (a->mass_type == PATCHKV_MASS_U64 && a->decay != 0.0f && a->decay != 1.0f)
+        return fail(ctx, PATCHKV_E_INVALID, "attention_mass: decay of whole masses must be 0 or 1");
+    if (a->q_stride_row < 0 || a->q_stride_head < 0) return fail(ctx, PATCHKV_E_INVALID, "attention_mass: negative stride");
+    if (a->mass_stride < batch->max_kv_len) return fail(ctx, PATCHKV_E_INVALID, "attention_mass: mass_stride is smaller than max_kv_len");
+    if (p.b.n_seqs == 0 || p.b.max_kv_len == 0) return PATCHKV_OK;
+    const uintptr_t unit = a->mass_type == PATCHKV_MASS_U64 ? 7 : 3;
+    if (!a->mass || (reinterpret_cast<uintptr_t>(a->mass) & unit) || (reinterpret_cast<uintptr_t>(a->mass_in) & unit))
+        return fail(ctx, PATCHKV_E_INVALID, "attention_mass: null or misaligned mass");
+    if (!p.b.row_start || !p.b.kv_len) return fail(ctx, PATCHKV_E_INVALID, "attention_mass: null row_start or kv_len");
+    const uintptr_t qa = reinterpret_cast<uintptr_t>(a->q);
+    const bool any_rows = p.b.n_rows > 0 && p.b.max_rows > 0;
+    if (any_rows && (!qa || (qa & 1))) return fail(ctx, PATCHKV_E_INVALID, "attention_mass: null or misaligned q");
+    const uint64_t need = patchkv_attention_mass_workspace_bytes(g, p.c.tag, batch, a->n_q_heads, a->window, a->sinks);
+    if (need && (!a->workspace || (reinterpret_cast<uintptr_t>(a->workspace) & 15) || a->workspace_bytes < need))
+        return fail(ctx, PATCHKV_E_INVALID, "attention_mass: workspace null, misaligned or too small");
+    p.q = static_cast<const uint16_t*>(a->q); p.out = nullptr;
+    p.q_stride_row = a->q_stride_row; p.q_stride_head = a->q_stride_head;
+    p.out_stride_row = p.out_stride_head = 0;
+    p.Hq = a->n_q_heads; p.share = a->n_q_heads / g->n_kv_heads;
+    p.window = a->window; p.sinks = a->sinks;
+    p.scale_log2 = (float)((double)a->scale * 1.4426950408889634);
+    p.status = ctx->d_status;
+    p.f16 = a->type == PATCHKV_ROWS_F16;
+    const WeightParams m = {a->mass_in, a->mass, a->mass_stride, a->decay, a->mass_type == PATCHKV_MASS_U64};
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(ctx, PATCHKV_E_CUDA, "cudaSetDevice failed");
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    float* sums = static_cast<float*>(a->workspace);
+    if (any_rows) {
+        mass_sums_any_kernel<<<dim3(std::min(p.b.max_rows, p.b.n_rows), p.Hq, p.b.n_seqs), kMassThreads, 0, stream>>>(p, sums);
+        PKV_CUDA(ctx, cudaGetLastError());
+    }
+    mass_columns_any_kernel<<<dim3((p.b.max_kv_len + kMassThreads - 1) / kMassThreads, p.b.n_seqs), kMassThreads, 0, stream>>>(p, m, sums);
+    PKV_CUDA(ctx, cudaGetLastError());
+    return PATCHKV_OK;
+}

@@ -1,0 +1,393 @@
+// Rows that get their rotary positions on their way into the cache: patchkv_rotary_append.
+#include "cache_rows.cuh"
+#include "rotary.cuh"
+
+namespace patchkv {
+
+constexpr int kRotaryThreads = 128;
+
+struct RotaryParams {
+    CacheDev c;
+    BatchDev b;
+    const uint16_t* q;
+    uint16_t* q_out;
+    const uint16_t* k;
+    const uint16_t* v;
+    uint16_t* k_pool;           // of a bf16 pool
+    uint16_t* v_pool;
+    long long q_stride_row, q_stride_head, out_stride_row, out_stride_head, k_stride_row, k_stride_head, v_stride_row, v_stride_head;
+    const int32_t* rope_pos;
+    int32_t* status;
+    double factor;
+    int32_t Hq, Dr, half;
+    int32_t parts;              // warps that share a row
+    int32_t q_passes, kv_passes;    // passes of a warp over the queries, and over K or V
+    int32_t U_shift;            // log2 of the 16-channel units of a head
+    int32_t seg, G_shift;       // lanes per scale group; log2 of G
+    Frequencies f;
+};
+
+// 16 channels (a lane's) of keys -> codes and, from the group's first lane, its scale: the quantiser's definition in 64 bits, as the rotated
+// key is not a 16-bit number.  (In fp32 a key within 2^-24 of the border of two codes would fall on either side, and a code is a step
+// of up to a seventh of the group's largest value.)  code = rint(x / s): t = x * r with r = 1 / s to 2^-46, corrected once by its
+// remainder; where x / s is a half-integer the remainder is exact and the correction gives it.  Adding 1.5 * 2^52 rounds, ties to even.
+template <int FMT>
+__device__ __forceinline__ void encode64(double (&x)[16], uint8_t* codes, uint8_t* scale, int seg, bool live) {
+    double amax = 0.0;
+#pragma unroll
+    for (int i = 0; i < 16; i++) amax = fmax(amax, fabs(x[i]));
+    for (int d = 1; d < seg; d <<= 1) amax = fmax(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, d));
+    if (!live) return;
+    constexpr double qmax = FMT == FMT_INT8 ? 127.0 : 7.0;
+    const uint32_t s16 = __half_as_ushort(__double2half(amax * (1.0 / qmax)));
+    const bool usable = s16 != 0 && s16 < 0x7C00u;          // a zero or infinite scale: all codes zero
+    const float sf = half_bits_to_float(usable ? s16 : 0x3C00u);
+    float rf;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(rf) : "f"(sf));
+    const double s = sf;
+    double r = rf;
+    r = fma(fma(-s, r, 1.0), r, r);
+    uint32_t code[16];
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+        double t = x[i] * r;
+        t = fma(fma(-t, s, x[i]), r, t);
+        if (s16 < 0x0400u) t = fmin(fmax(t, -qmax), qmax);  // a subnormal scale; else |t| <= qmax (1 + 2^-11)
+        code[i] = usable ? (uint32_t)__double2loint(t + 6755399441055744.0) : 0u;
+    }
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+        w[i] = __byte_perm(__byte_perm(code[4 * i], code[4 * i + 1], 0x0040), __byte_perm(code[4 * i + 2], code[4 * i + 3], 0x0040), 0x5410);
+    if (FMT == FMT_INT8) {
+        *reinterpret_cast<uint4*>(codes) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            w[i] &= 0x0F0F0F0Fu;
+            w[i] = (w[i] | w[i] >> 4) & 0x00FF00FFu;
+        }
+        *reinterpret_cast<uint2*>(codes) = make_uint2(__byte_perm(w[0], w[1], 0x6420), __byte_perm(w[2], w[3], 0x6420));
+    }
+    if (scale) *reinterpret_cast<uint16_t*>(scale) = (uint16_t)s16;
+}
+
+// A warp takes a row, or every `parts`-th pass of one; a pass is 32 units of 16 channels: queries, then keys, then values.  A lane has the
+// same channels of a head in every pass, so it keeps the cosines and sines of its channels in registers; in the half layout the
+// other channel of a pair lies Dr / 32 lanes away and comes by shuffle.  Bound by memory: the next pass is asked for before one is worked on.
+template <int TYPE, int KF, int VF, bool HALF>
+__global__ void __launch_bounds__(kRotaryThreads) rotary_append_kernel(const __grid_constant__ RotaryParams p) {
+    constexpr bool kPool = KF == FMT_BF16;
+    __shared__ double2 table[kRotaryThreads / 32][PATCHKV_MAX_ROTARY_DIM / 2];
+    pdl_trigger();
+    const uint32_t wid = (blockIdx.x * kRotaryThreads + threadIdx.x) >> 5;
+    const int r = (int)(wid / (uint32_t)p.parts), part = (int)(wid - (uint32_t)r * p.parts), lane = threadIdx.x & 31;
+    if (r >= p.b.n_rows) return;
+    pdl_wait();
+    const int u = lane & ((1 << p.U_shift) - 1), sub = lane >> p.U_shift, total = p.q_passes + 2 * p.kv_passes;
+    struct Unit { uint4 a, b; };
+    // Kind of a pass (0 queries, 1 keys, 2 values) and the lane's head in it.
+    auto kind_of = [&](int pass, int* h) {
+        const int kind = pass < p.q_passes ? 0 : pass < p.q_passes + p.kv_passes ? 1 : 2;
+        pass -= kind == 0 ? 0 : kind == 1 ? p.q_passes : p.q_passes + p.kv_passes;
+        *h = (pass << (5 - p.U_shift)) + sub;
+        return kind;
+    };
+    auto load = [&](int pass) {
+        Unit x = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+        if (pass >= total) return x;
+        int h;
+        const int kind = kind_of(pass, &h);
+        if (h >= (kind == 0 ? p.Hq : p.c.H)) return x;
+        const uint16_t* from = kind == 0 ? p.q + (long long)r * p.q_stride_row + (long long)h * p.q_stride_head
+                             : kind == 1 ? p.k + (long long)r * p.k_stride_row + (long long)h * p.k_stride_head
+                                         : p.v + (long long)r * p.v_stride_row + (long long)h * p.v_stride_head;
+        x.a = *(reinterpret_cast<const uint4*>(from + 16 * u));
+        x.b = *(reinterpret_cast<const uint4*>(from + 16 * u) + 1);
+        return x;
+    };
+    Unit next = load(part);
+    int slot = 0, pos = 0;
+    const int pg = find_page<true>(p, r, lane == 0 && part == 0, &slot, &pos);
+    if (pg >= 0) {
+        double2* tab = table[threadIdx.x >> 5];
+        if (part < p.q_passes + p.kv_passes) {              // a warp of values alone needs no angles
+            if (p.rope_pos) pos = p.rope_pos[r];
+            for (int i = lane; i < p.Dr >> 1; i += 32) {
+                double c, s;
+                cos_sin((double)pos * p.f.theta[i], &c, &s);
+                tab[i] = make_double2(p.factor * c, p.factor * s);
+            }
+        }
+        __syncwarp();
+        const int away = p.Dr >> 5;                         // lanes between the channels of a pair
+        const bool turns = 16 * u < p.Dr, upper = HALF && u >= away;
+        const int partner = HALF && turns ? (upper ? lane - away : lane + away) : lane;
+        const double2* mine = tab + (!turns ? 0 : HALF ? 16 * (upper ? u - away : u) : 8 * u);
+        constexpr int kAngles = HALF ? 16 : 8;
+        float cf[kAngles], sf[kAngles];
+#pragma unroll
+        for (int i = 0; i < kAngles; i++) {
+            cf[i] = turns ? (float)mine[i].x : 1.0f;
+            sf[i] = turns ? (float)mine[i].y : 0.0f;
+            if (HALF && !upper) sf[i] = -sf[i];
+        }
+        const long long row = kPool ? (long long)pg * p.c.stride_page + (long long)slot * p.c.stride_token : (long long)pg * p.c.stride_page;
+#pragma unroll 1
+        for (int pass = part; pass < total; pass += p.parts) {
+            const Unit x = next;
+            next = load(pass + p.parts);
+            int h;
+            const int kind = kind_of(pass, &h);
+            const bool live = h < (kind == 0 ? p.Hq : p.c.H);
+            const uint32_t w[8] = {x.a.x, x.a.y, x.a.z, x.a.w, x.b.x, x.b.y, x.b.z, x.b.w};
+            const uint32_t at = ((uint32_t)slot * p.c.H + h) * p.c.D + 16 * u, group = at >> p.G_shift;
+            const bool first = (u & (p.seg - 1)) == 0;
+            if (kind == 2) {
+                if constexpr (kPool) {
+                    if (live) {
+                        uint4* to = reinterpret_cast<uint4*>(p.v_pool + row + (long long)h * p.c.stride_head + 16 * u);
+                        to[0] = x.a;
+                        to[1] = x.b;
+                    }
+                } else {
+                    const uint4 v[2] = {x.a, x.b};
+                    uint8_t* page = p.c.base + row;
+                    encode<TYPE, VF, 16>(v, page + p.c.v_codes + (VF == FMT_INT8 ? at : at >> 1), first ? page + p.c.v_scales + 2 * group : nullptr, p.seg, live);
+                }
+                continue;
+            }
+            uint32_t o[8];                                  // the words of the other channels
+#pragma unroll
+            for (int i = 0; i < 8; i++) o[i] = HALF ? __shfl_sync(0xFFFFFFFFu, w[i], partner) : 0u;
+            if (kPool || kind == 0) {
+                uint32_t y[8];
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const float a = to_float<TYPE>(w[i] & 0xFFFFu), b = to_float<TYPE>(w[i] >> 16);
+                    if (HALF) {
+                        const float a2 = to_float<TYPE>(o[i] & 0xFFFFu), b2 = to_float<TYPE>(o[i] >> 16);
+                        y[i] = pack_pair<TYPE>(fmaf(a2, sf[2 * i], a * cf[2 * i]), fmaf(b2, sf[2 * i + 1], b * cf[2 * i + 1]));
+                    } else {
+                        y[i] = pack_pair<TYPE>(fmaf(-b, sf[i], a * cf[i]), fmaf(b, cf[i], a * sf[i]));
+                    }
+                    if (!turns) y[i] = w[i];
+                }
+                if (live) {
+                    uint16_t* to = kind == 0 ? p.q_out + (long long)r * p.out_stride_row + (long long)h * p.out_stride_head
+                                             : p.k_pool + row + (long long)h * p.c.stride_head;
+                    reinterpret_cast<uint4*>(to + 16 * u)[0] = make_uint4(y[0], y[1], y[2], y[3]);
+                    reinterpret_cast<uint4*>(to + 16 * u)[1] = make_uint4(y[4], y[5], y[6], y[7]);
+                }
+            } else if constexpr (!kPool) {
+                double z[16];
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const double a = to_float<TYPE>(w[i] & 0xFFFFu), b = to_float<TYPE>(w[i] >> 16);
+                    if (!turns) {
+                        z[2 * i] = a;
+                        z[2 * i + 1] = b;
+                    } else if (HALF) {
+                        const double a2 = to_float<TYPE>(o[i] & 0xFFFFu), b2 = to_float<TYPE>(o[i] >> 16);
+                        const double2 t0 = mine[2 * i], t1 = mine[2 * i + 1];
+                        z[2 * i] = fma(a2, upper ? t0.y : -t0.y, a * t0.x);
+                        z[2 * i + 1] = fma(b2, upper ? t1.y : -t1.y, b * t1.x);
+                    } else {
+                        const double2 t = mine[i];
+                        z[2 * i] = fma(-b, t.y, a * t.x);
+                        z[2 * i + 1] = fma(b, t.x, a * t.y);
+                    }
+                }
+                uint8_t* page = p.c.base + row;
+                encode64<KF>(z, page + (KF == FMT_INT8 ? at : at >> 1), first ? page + p.c.k_scales + 2 * group : nullptr, p.seg, live);
+            }
+        }
+    }
+    check_entries(p.b, p.status, blockIdx.x * kRotaryThreads + threadIdx.x, (uint32_t)p.b.n_rows * p.parts * 32);
+}
+
+// Any geometry, any strides: one thread per (row, head) of the queries, keys and values.
+template <int TYPE>
+__global__ void __launch_bounds__(kRotaryThreads) rotary_any_kernel(const __grid_constant__ RotaryParams p) {
+    const uint32_t i = blockIdx.x * kRotaryThreads + threadIdx.x, per_row = (uint32_t)p.Hq + 2u * p.c.H;
+    const int r = (int)(i / per_row), q = (int)(i - (uint32_t)r * per_row);
+    if (r >= p.b.n_rows) return;
+    check_entries(p.b, p.status, i, (uint32_t)p.b.n_rows * per_row);
+    int slot = 0, pos = 0;
+    const int pg = find_page<true>(p, r, q == 0, &slot, &pos);
+    if (pg < 0) return;
+    if (p.rope_pos) pos = p.rope_pos[r];
+    const int kind = q < p.Hq ? 0 : q < p.Hq + p.c.H ? 1 : 2, h = q - (kind == 0 ? 0 : kind == 1 ? p.Hq : p.Hq + p.c.H), D = p.c.D;
+    const uint16_t* x = kind == 0 ? p.q + (long long)r * p.q_stride_row + (long long)h * p.q_stride_head
+                      : kind == 1 ? p.k + (long long)r * p.k_stride_row + (long long)h * p.k_stride_head
+                                  : p.v + (long long)r * p.v_stride_row + (long long)h * p.v_stride_head;
+    const int Dr = kind == 2 ? 0 : p.Dr;
+    const bool half = p.half, pool = p.c.tag == PATCHKV_TAG_BF16;
+    if (kind == 0 || pool) {
+        const long long row = (long long)pg * p.c.stride_page + (long long)slot * p.c.stride_token + (long long)h * p.c.stride_head;
+        uint16_t* y = kind == 0 ? p.q_out + (long long)r * p.out_stride_row + (long long)h * p.out_stride_head : (kind == 1 ? p.k_pool : p.v_pool) + row;
+        for (int j = 0; j < Dr >> 1; j++) {
+            const int c0 = half ? j : 2 * j, c1 = half ? j + (Dr >> 1) : 2 * j + 1;
+            double c, s;
+            cos_sin((double)pos * p.f.theta[j], &c, &s);
+            const float cf = (float)(p.factor * c), sf = (float)(p.factor * s), a = to_float<TYPE>(x[c0]), b = to_float<TYPE>(x[c1]);
+            y[c0] = (uint16_t)pack_pair<TYPE>(fmaf(-b, sf, a * cf), 0.0f);
+            y[c1] = (uint16_t)pack_pair<TYPE>(fmaf(b, cf, a * sf), 0.0f);
+        }
+        for (int c = Dr; c < D; c++) y[c] = x[c];
+        return;
+    }
+    const int fmt = kind == 2 ? v_format(p.c.tag) : k_format(p.c.tag);
+    uint8_t* page = p.c.base + (long long)pg * p.c.stride_page;
+    uint8_t* codes = page + (kind == 2 ? p.c.v_codes : 0u);
+    uint8_t* scales = page + (kind == 2 ? p.c.v_scales : p.c.k_scales);
+    const unsigned long long e0 = ((unsigned long long)slot * p.c.H + h) * D;
+    auto value = [&](int ch) {                              // the rotated key, or the value
+        if (ch >= Dr) return (double)to_float<TYPE>(x[ch]);
+        const int n = Dr >> 1, j = half ? ch % n : ch >> 1, second = half ? ch >= n : ch & 1;
+        double c, s;
+        cos_sin((double)pos * p.f.theta[j], &c, &s);
+        const double a = to_float<TYPE>(x[half ? j : 2 * j]), b = to_float<TYPE>(x[half ? j + n : 2 * j + 1]);
+        c *= p.factor;
+        s *= p.factor;
+        return second ? fma(b, c, a * s) : fma(-b, s, a * c);
+    };
+    const double qmax = fmt == FMT_INT8 ? 127.0 : 7.0;
+    int low = 0;
+    for (int c0 = 0; c0 < D; c0 += p.c.G) {
+        const unsigned long long group = (e0 + c0) / p.c.G;
+        double amax = 0.0;
+        for (int c = c0; c < c0 + p.c.G; c++) amax = fmax(amax, fabs(value(c)));
+        const float sf = __half2float(__double2half(amax / qmax));
+        const uint32_t sb = pack_pair<PATCHKV_ROWS_F16>(sf, 0.0f);      // its bits: exact (stored byte by byte from
+                                                                        // the 64-bit conversion itself the low byte came out wrong)
+        const double s = sf;
+        scales[2 * group] = (uint8_t)sb;
+        scales[2 * group + 1] = (uint8_t)(sb >> 8);
+        const bool usable = s > 0.0 && s <= 65504.0;
+        for (int c = c0; c < c0 + p.c.G; c++) {
+            const int code = usable ? (int)fmin(fmax(rint(value(c) / s), -qmax), qmax) : 0;
+            if (fmt == FMT_INT8) codes[e0 + c] = (uint8_t)code;
+            else if ((c & 1) == 0) low = code & 15;         // D is even: the pair is this thread's
+            else codes[(e0 + c) >> 1] = (uint8_t)(low | (code & 15) << 4);
+        }
+    }
+}
+
+int fill_frequencies(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, Frequencies* f) {
+    const std::string w(who);
+    if (g->rotary_dim < 0 || g->rotary_dim > g->head_dim || (g->rotary_dim & 1)) return fail(ctx, PATCHKV_E_INVALID, w + ": rotary_dim must be even and at most head_dim");
+    if (g->rope_style != PATCHKV_ROPE_HALF && g->rope_style != PATCHKV_ROPE_INTERLEAVED) return fail(ctx, PATCHKV_E_INVALID, w + ": unknown rope_style");
+    if (g->rotary_dim > PATCHKV_MAX_ROTARY_DIM) return fail(ctx, PATCHKV_E_UNSUPPORTED, w + ": rotary_dim above 256");
+    if (!g->inv_freq && g->rotary_dim > 0 && !(g->rope_base > 0.0 && g->rope_base <= 1e300)) return fail(ctx, PATCHKV_E_INVALID, w + ": rope_base must be positive and finite");
+    const int n = g->rotary_dim / 2;
+    for (int i = 0; i < n; i++) {
+        f->theta[i] = g->inv_freq ? (double)g->inv_freq[i] : pow(g->rope_base, -2.0 * (double)i / (double)g->rotary_dim);
+        if (!(fabs(f->theta[i]) <= 65536.0)) return fail(ctx, PATCHKV_E_INVALID, w + ": a frequency is above 65536 or not a number");
+    }
+    return PATCHKV_OK;
+}
+
+namespace {
+
+template <int TYPE, int KF, int VF>
+cudaError_t launch_rotary_style(const RotaryParams& p, bool half, unsigned grid, cudaStream_t stream) {
+    return half ? launch_pdl(rotary_append_kernel<TYPE, KF, VF, true>, dim3(grid), dim3(kRotaryThreads), 0, stream, p)
+                : launch_pdl(rotary_append_kernel<TYPE, KF, VF, false>, dim3(grid), dim3(kRotaryThreads), 0, stream, p);
+}
+template <int TYPE>
+cudaError_t launch_rotary_tag(const RotaryParams& p, bool half, unsigned grid, cudaStream_t stream) {
+    if (p.c.tag == PATCHKV_TAG_INT8) return launch_rotary_style<TYPE, FMT_INT8, FMT_INT8>(p, half, grid, stream);
+    if (p.c.tag == PATCHKV_TAG_INT4) return launch_rotary_style<TYPE, FMT_INT8, FMT_INT4>(p, half, grid, stream);
+    return launch_rotary_style<TYPE, FMT_INT4, FMT_INT4>(p, half, grid, stream);
+}
+
+bool vectors(const void* x, int64_t stride_row, int64_t stride_head) {
+    return (reinterpret_cast<uintptr_t>(x) & 15) == 0 && stride_row % 8 == 0 && stride_head % 8 == 0;
+}
+
+}  // namespace
+}  // namespace patchkv
+
+using namespace patchkv;
+
+extern "C" int patchkv_rotary_append(patchkv_ctx* ctx, const patchkv_geom* g, const patchkv_pool* pool, const patchkv_qpool* cache,
+                                     int layer, const patchkv_batch* batch, const patchkv_rotary_args* a, void* stream_) {
+    if (!ctx) return PATCHKV_E_INVALID;
+    std::lock_guard<std::mutex> lock(ctx->mu);
+    RotaryParams p;
+    if ((pool != nullptr) == (cache != nullptr)) return fail(ctx, PATCHKV_E_INVALID, "rotary_append: give a pool or a cache, one of the two");
+    int rc = check_live_geometry(ctx, "rotary_append", g, layer);
+    if (rc == PATCHKV_OK) rc = fill_frequencies(ctx, "rotary_append", g, &p.f);
+    if (rc == PATCHKV_OK) rc = fill_batch(ctx, "rotary_append", batch, &p.b);
+    if (rc == PATCHKV_OK) rc = pool ? fill_pool(ctx, "rotary_append", g, pool, layer, &p.c) : fill_cache(ctx, "rotary_append", g, cache, layer, &p.c);
+    if (rc != PATCHKV_OK) return rc;
+    if (!a || a->struct_size != sizeof(patchkv_rotary_args)) return fail(ctx, PATCHKV_E_INVALID, "rotary_append: null args or wrong struct_size");
+    if (a->type != PATCHKV_ROWS_BF16 && a->type != PATCHKV_ROWS_F16) return fail(ctx, PATCHKV_E_INVALID, "rotary_append: unknown row type");
+    if (pool && a->type != PATCHKV_ROWS_BF16) return fail(ctx, PATCHKV_E_INVALID, "rotary_append: rows into a bf16 pool must be bf16");
+    if (!(fabsf(a->factor) <= 3.0e38f)) return fail(ctx, PATCHKV_E_INVALID, "rotary_append: factor must be finite");
+    if (a->n_q_heads < 0 || a->n_q_heads > 65535) return fail(ctx, PATCHKV_E_INVALID, "rotary_append: n_q_heads must lie in [0, 65535]");
+    if (a->q_stride_row < 0 || a->q_stride_head < 0 || a->q_out_stride_row < 0 || a->q_out_stride_head < 0 || a->k_stride_row < 0 ||
+        a->k_stride_head < 0 || a->v_stride_row < 0 || a->v_stride_head < 0)
+        return fail(ctx, PATCHKV_E_INVALID, "rotary_append: negative stride");
+    if (p.b.n_rows == 0 || p.b.n_seqs == 0) return PATCHKV_OK;
+    const uintptr_t ka = reinterpret_cast<uintptr_t>(a->k), va = reinterpret_cast<uintptr_t>(a->v), qa = reinterpret_cast<uintptr_t>(a->q),
+                    oa = reinterpret_cast<uintptr_t>(a->q_out);
+    if (!ka || !va || ((ka | va) & 1)) return fail(ctx, PATCHKV_E_INVALID, "rotary_append: null or misaligned k or v");
+    if (a->n_q_heads > 0) {
+        if (!qa || !oa || ((qa | oa) & 1)) return fail(ctx, PATCHKV_E_INVALID, "rotary_append: null or misaligned q or q_out");
+        if (rows_overlap(p.b.n_rows, a->n_q_heads, p.c.D, a->q_out_stride_row, a->q_out_stride_head))
+            return fail(ctx, PATCHKV_E_INVALID, "rotary_append: rows or heads of q_out overlap");
+        if (qa == oa && (a->q_stride_row != a->q_out_stride_row || a->q_stride_head != a->q_out_stride_head))
+            return fail(ctx, PATCHKV_E_INVALID, "rotary_append: q in place needs the same strides");
+    }
+    p.q = static_cast<const uint16_t*>(a->q); p.q_out = static_cast<uint16_t*>(a->q_out);
+    p.k = static_cast<const uint16_t*>(a->k); p.v = static_cast<const uint16_t*>(a->v);
+    p.k_pool = const_cast<uint16_t*>(p.c.k); p.v_pool = const_cast<uint16_t*>(p.c.v);
+    p.q_stride_row = a->q_stride_row; p.q_stride_head = a->q_stride_head;
+    p.out_stride_row = a->q_out_stride_row; p.out_stride_head = a->q_out_stride_head;
+    p.k_stride_row = a->k_stride_row; p.k_stride_head = a->k_stride_head;
+    p.v_stride_row = a->v_stride_row; p.v_stride_head = a->v_stride_head;
+    p.rope_pos = a->rope_pos;
+    p.status = ctx->d_status;
+    p.factor = a->factor;
+    p.Hq = a->n_q_heads; p.Dr = g->rotary_dim;
+    const bool half = g->rope_style == PATCHKV_ROPE_HALF, f16 = a->type == PATCHKV_ROWS_F16;
+    const int D = g->head_dim, ds = log2_exact(D), gs = log2_exact(g->group);
+    bool fast = ds >= 4 && ds <= 8 && g->rotary_dim % (half ? 32 : 16) == 0 && vectors(a->k, a->k_stride_row, a->k_stride_head) &&
+                vectors(a->v, a->v_stride_row, a->v_stride_head);
+    if (p.Hq) fast = fast && vectors(a->q, a->q_stride_row, a->q_stride_head) && vectors(a->q_out, a->q_out_stride_row, a->q_out_stride_head);
+    const long long elems = (long long)g->page_tokens * g->n_kv_heads * D;
+    if (pool) fast = fast && p.c.stride_page % 8 == 0 && p.c.stride_token % 8 == 0 && p.c.stride_head % 8 == 0 && pool->stride_layer % 8 == 0;
+    else fast = fast && gs >= 4 && elems % 32 == 0 && (elems / g->group) % 8 == 0;
+    p.seg = fast && !pool ? g->group / 16 : 1;
+    p.G_shift = gs < 0 ? 0 : gs;
+    p.U_shift = fast ? ds - 4 : 0;
+    p.half = half;
+    p.parts = 1;
+    if (fast) {
+        const int per_pass = 32 >> p.U_shift;               // heads
+        p.q_passes = (p.Hq + per_pass - 1) / per_pass;
+        p.kv_passes = (g->n_kv_heads + per_pass - 1) / per_pass;
+        // Few rows: a warp for each pass of a row.
+        const int passes = p.q_passes + 2 * p.kv_passes;
+        if ((long long)p.b.n_rows * passes <= 16 * 148) p.parts = passes;
+    }
+    const long long threads = (long long)p.b.n_rows * (fast ? 32 * p.parts : p.Hq + 2 * g->n_kv_heads);
+    const long long grid = (threads + kRotaryThreads - 1) / kRotaryThreads;
+    if (grid * kRotaryThreads > (1ll << 32) - 1) return fail(ctx, PATCHKV_E_UNSUPPORTED, "rotary_append: too many rows for one call");
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(ctx, PATCHKV_E_CUDA, "cudaSetDevice failed");
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    if (fast) {
+        const cudaError_t e = pool ? launch_rotary_style<PATCHKV_ROWS_BF16, FMT_BF16, FMT_BF16>(p, half, (unsigned)grid, stream)
+                            : f16 ? launch_rotary_tag<PATCHKV_ROWS_F16>(p, half, (unsigned)grid, stream)
+                                  : launch_rotary_tag<PATCHKV_ROWS_BF16>(p, half, (unsigned)grid, stream);
+        PKV_CUDA(ctx, e);
+        return PATCHKV_OK;
+    }
+    if (f16) rotary_any_kernel<PATCHKV_ROWS_F16><<<(unsigned)grid, kRotaryThreads, 0, stream>>>(p);
+    else rotary_any_kernel<PATCHKV_ROWS_BF16><<<(unsigned)grid, kRotaryThreads, 0, stream>>>(p);
+    PKV_CUDA(ctx, cudaGetLastError());
+    return PATCHKV_OK;
+}

@@ -1,0 +1,48 @@
+// Cosines and sines of rotary positions (rotary.cu, evict.cu).
+#pragma once
+
+#include <math.h>
+
+#include "common.cuh"
+
+namespace patchkv {
+
+// Frequencies of the rotary pairs in 64 bits, as the restore path defines them: inv_freq[i], or rope_base^(-2i/Dr).
+struct Frequencies { double theta[PATCHKV_MAX_ROTARY_DIM / 2]; };
+
+// Checks the rotary fields of a geometry and fills the frequencies.
+int fill_frequencies(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, Frequencies* f);
+
+// cos and sin of an angle in radians, |angle| < 2^48, to 2^-52 or so.  The angle comes to [-pi/4, pi/4] by multiples of pi/2 taken off in
+// two parts (the first product and difference are exact in the fused operation: both are multiples of 2^-52 below 1), then the two
+// Taylor series, cut where the next term is below 2^-53.  64 bits because a position of 10^5 leaves an fp32 angle 2^-7 off, and so that a
+// key next to the border of two codes falls on the side that the formula says; some 25 operations of the fp64 pipe for both.
+__device__ __forceinline__ void cos_sin(double angle, double* c, double* s) {
+    constexpr double kRound = 6755399441055744.0;           // 1.5 * 2^52: adding it rounds to an integer, in the low word
+    const double t = fma(angle, 0.63661977236758134308, kRound);      // 2 / pi
+    const int quarter = __double2loint(t);
+    const double k = t - kRound;
+    double r = fma(k, -1.57079632679489655800, angle);      // pi / 2 in 53 bits, and what that leaves of it
+    r = fma(k, -6.12323399573676603587e-17, r);
+    const double z = r * r;
+    double p = -1.0 / 1307674368000.0, q = 1.0 / 20922789888000.0;    // 1 / 15!, 1 / 16!
+    p = fma(p, z, 1.0 / 6227020800.0);
+    q = fma(q, z, -1.0 / 87178291200.0);
+    p = fma(p, z, -1.0 / 39916800.0);
+    q = fma(q, z, 1.0 / 479001600.0);
+    p = fma(p, z, 1.0 / 362880.0);
+    q = fma(q, z, -1.0 / 3628800.0);
+    p = fma(p, z, -1.0 / 5040.0);
+    q = fma(q, z, 1.0 / 40320.0);
+    p = fma(p, z, 1.0 / 120.0);
+    q = fma(q, z, -1.0 / 720.0);
+    p = fma(p, z, -1.0 / 6.0);
+    q = fma(q, z, 1.0 / 24.0);
+    q = fma(q, z, -0.5);
+    const double sn = fma(p * z, r, r), cs = fma(q, z, 1.0);
+    const double a = quarter & 1 ? sn : cs, b = quarter & 1 ? cs : sn;
+    *c = (quarter + 1) & 2 ? -a : a;
+    *s = quarter & 2 ? -b : b;
+}
+
+}  // namespace patchkv
