@@ -574,6 +574,8 @@ typedef struct {
 PATCHKV_API int patchkv_attention_mass(patchkv_ctx* ctx, const patchkv_geom* geom, const patchkv_pool* pool,
                                        const patchkv_qpool* cache, int layer, const patchkv_batch* batch,
                                        const patchkv_mass_args* args, void* stream);
+/* Workspace of such a call, as patchkv_attention_workspace_bytes; it depends on whether pos is given, too (the batch's other arrays may
+ * be null). */
 PATCHKV_API uint64_t patchkv_attention_mass_workspace_bytes(const patchkv_geom* geom, int tag, const patchkv_batch* batch,
                                                             int n_q_heads, int window, int sinks);
 

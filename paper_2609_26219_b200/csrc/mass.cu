@@ -3,7 +3,7 @@
 
 #include <algorithm>
 
-#include "mass.cuh"
+#include "mass_split.cuh"
 
 namespace patchkv {
 
@@ -112,6 +112,45 @@ int check_mass(patchkv_ctx* ctx, const patchkv_geom* g, int tag, const patchkv_b
     return PATCHKV_OK;
 }
 
+constexpr int kSms = 148;                        // B200; only sizes launches, so that results don't depend on the context
+
+// How a call is served, and its workspace.
+struct MassPlan {
+    int nc;                     // columns of a lane of the split kernel; 0: another kernel
+    int heads, groups, warps_per_head, target, max_items, cols, tokens;
+    uint64_t items_bytes, sums_bytes, bytes;
+};
+
+MassPlan plan_mass(const patchkv_geom* g, int tag, const patchkv_batch* b, int Hq, int window, int sinks) {
+    MassPlan a;
+    memset(&a, 0, sizeof(a));
+    const int D = g->head_dim, H = g->n_kv_heads;
+    const bool pool = tag == PATCHKV_TAG_BF16;
+    const bool shape = (D == 64 || D == 128) && g->page_tokens % kTile == 0 && (pool || g->group % 32 == 0);
+    const long long cols = (long long)std::min(b->max_rows, b->n_rows) * (Hq / H);
+    a.bytes = ((uint64_t)b->n_rows * Hq * 4 + 15) / 16 * 16;
+    if (!shape || cols == 0 || cols > 16) return a;
+    a.nc = cols <= 4 ? 1 : cols <= 8 ? 2 : 4;
+    a.cols = (int)cols;
+    const int warps = split_warps(pool, a.nc);
+    a.heads = 1;                                // heads of a CTA, and pieces of the batch, as the attention has them
+    for (int h = 2; h <= warps; h *= 2)
+        if ((H + h - 1) / h * h <= (H + a.heads - 1) / a.heads * a.heads || h <= H) a.heads = h;
+    a.groups = (H + a.heads - 1) / a.heads;
+    a.warps_per_head = warps / a.heads;
+    const int slots = std::max(1, kSms / a.groups);
+    a.target = b->n_seqs >= 2 * slots ? 0 : std::max(slots - b->n_seqs, (slots + 1) / 2);
+    a.max_items = b->n_seqs + a.target;
+    // Tiles that a sequence's rows can see: with a window, and rows one behind the other, not all of them.
+    long long tiles = ((long long)b->max_kv_len + kTile - 1) / kTile;
+    if (window > 0 && !b->pos) tiles = std::min(tiles, ((long long)window + b->max_rows + kTile - 1) / kTile + 1 + ((long long)sinks + kTile - 1) / kTile);
+    a.tokens = (int)(tiles * kTile);
+    a.items_bytes = ((uint64_t)b->n_seqs * 8 + 15) / 16 * 16;
+    a.sums_bytes = (uint64_t)a.max_items * H * 4 * a.nc * 8;
+    a.bytes = a.items_bytes + a.sums_bytes + (uint64_t)b->n_seqs * H * a.cols * a.tokens * 4;
+    return a;
+}
+
 }  // namespace
 }  // namespace patchkv
 
@@ -123,7 +162,7 @@ extern "C" uint64_t patchkv_attention_mass_workspace_bytes(const patchkv_geom* g
     if (check_live_geometry(nullptr, "attention_mass", g, 0) != PATCHKV_OK || fill_batch(nullptr, "attention_mass", b, &bd) != PATCHKV_OK ||
         check_mass(nullptr, g, tag, b, n_q_heads, window, sinks) != PATCHKV_OK)
         return 0;
-    return ((uint64_t)b->n_rows * n_q_heads * 4 + 15) / 16 * 16;
+    return plan_mass(g, tag, b, n_q_heads, window, sinks).bytes;
 }
 
 extern "C" int patchkv_attention_mass(patchkv_ctx* ctx, const patchkv_geom* g, const patchkv_pool* pool, const patchkv_qpool* cache,
@@ -171,6 +210,23 @@ extern "C" int patchkv_attention_mass(patchkv_ctx* ctx, const patchkv_geom* g, c
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return fail(ctx, PATCHKV_E_CUDA, "cudaSetDevice failed");
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    const MassPlan plan = plan_mass(g, p.c.tag, batch, a->n_q_heads, a->window, a->sinks);
+    const bool aligned = (qa & 15) == 0 && a->q_stride_row % 8 == 0 && a->q_stride_head % 8 == 0 &&
+                         (!pool || (pool->stride_page % 8 == 0 && pool->stride_token % 8 == 0 && pool->stride_head % 8 == 0 && pool->stride_layer % 8 == 0));
+    if (plan.nc && aligned) {
+        uint8_t* ws = static_cast<uint8_t*>(a->workspace);
+        WeighPlan pl;
+        memset(&pl, 0, sizeof(pl));
+        pl.s.items = reinterpret_cast<int32_t*>(ws);
+        pl.s.max_items = plan.max_items; pl.s.target = plan.target;
+        pl.s.heads_log2 = log2_exact(plan.heads); pl.s.per_head_log2 = log2_exact(plan.warps_per_head);
+        pl.s.share_magic = (65536u + p.share - 1) / p.share;
+        pl.sums = reinterpret_cast<float2*>(ws + plan.items_bytes);
+        pl.logits = reinterpret_cast<float*>(ws + plan.items_bytes + plan.sums_bytes);
+        pl.tokens = plan.tokens; pl.cols = plan.cols;
+        PKV_CUDA(ctx, p.c.D == 128 ? launch_weigh<128>(p, m, pl, plan.nc, plan.groups, stream) : launch_weigh<64>(p, m, pl, plan.nc, plan.groups, stream));
+        return PATCHKV_OK;
+    }
     float* sums = static_cast<float*>(a->workspace);
     if (any_rows) {
         mass_sums_any_kernel<<<dim3(std::min(p.b.max_rows, p.b.n_rows), p.Hq, p.b.n_seqs), kMassThreads, 0, stream>>>(p, sums);
