@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpatchkv.so")
 SOURCES = ["context.cu", "restore.cu", "select.cu", "host_restore.cu", "writer.cu", "cache.cu", "rotary.cu", "evict.cu", "attention.cu", "mass.cu",
            "attention_split_64.cu", "attention_split_128.cu", "attention_rows_64.cu", "attention_rows_128.cu",
-           "mass_split_64.cu", "mass_split_128.cu"]
+           "mass_split_64.cu", "mass_split_128.cu", "mass_rows_64.cu", "mass_rows_128.cu"]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler",
          "-fPIC,-fvisibility=hidden", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 

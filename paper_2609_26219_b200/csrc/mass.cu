@@ -3,6 +3,7 @@
 
 #include <algorithm>
 
+#include "mass_rows.cuh"
 #include "mass_split.cuh"
 
 namespace patchkv {
@@ -119,7 +120,13 @@ struct MassPlan {
     int nc;                     // columns of a lane of the split kernel; 0: another kernel
     int heads, groups, warps_per_head, target, max_items, cols, tokens;
     uint64_t items_bytes, sums_bytes, bytes;
+    int row_tiles, row_splits, per, chunk, steps;       // the row kernels (0 tiles: another): CTAs along the vectors and the tokens, vector tiles of a
+                                // CTA, CTAs along the vectors of a launch of the second pass, steps of a sequence that have images
+    uint64_t ranges_bytes, acc_bytes, partial_bytes, image_bytes, meta_bytes;
 };
+
+constexpr uint64_t kMaxMassImages = 3ull << 29, kMaxMassPartial = 1ull << 28;
+uint64_t round16(uint64_t x) { return (x + 15) / 16 * 16; }
 
 MassPlan plan_mass(const patchkv_geom* g, int tag, const patchkv_batch* b, int Hq, int window, int sinks) {
     MassPlan a;
@@ -128,8 +135,36 @@ MassPlan plan_mass(const patchkv_geom* g, int tag, const patchkv_batch* b, int H
     const bool pool = tag == PATCHKV_TAG_BF16;
     const bool shape = (D == 64 || D == 128) && g->page_tokens % kTile == 0 && (pool || g->group % 32 == 0);
     const long long cols = (long long)std::min(b->max_rows, b->n_rows) * (Hq / H);
-    a.bytes = ((uint64_t)b->n_rows * Hq * 4 + 15) / 16 * 16;
-    if (!shape || cols == 0 || cols > 16) return a;
+    a.bytes = round16((uint64_t)b->n_rows * Hq * 4);
+    if (!shape || cols == 0) return a;
+    if (cols > 16) {
+        // Whole CTAs along the query vectors; where they leave SMs idle the tokens are split, two steps a piece at least.
+        const long long tiles = (cols + 2 * kRowTile - 1) / (2 * kRowTile), ctas = tiles * H * b->n_seqs;
+        if (ctas > 1 << 24 || cols > 1 << 30) return a;
+        const long long all = ((long long)b->max_kv_len + kRowTile - 1) / kRowTile;
+        long long steps = all;                  // that the rows of a CTA see at most
+        const long long cta_rows = std::min((long long)b->max_rows, 2ll * kRowTile / (Hq / H) + 2);
+        if (window > 0 && !b->pos) steps = std::min(all, ((long long)window + sinks + cta_rows) / kRowTile + 3);
+        a.row_tiles = (int)tiles;
+        a.row_splits = (int)std::max(1ll, std::min((long long)kSms / ctas, steps / 2));
+        a.per = cols <= kRowTile ? 1 : 2;
+        a.tokens = (int)(steps * kRowTile);
+        const uint64_t tile_bytes = (uint64_t)b->n_seqs * H * a.per * a.tokens * 4;
+        a.chunk = (int)std::min<uint64_t>(tiles, std::max<uint64_t>(1, kMaxMassPartial / std::max<uint64_t>(tile_bytes, 1)));
+        a.sums_bytes = (uint64_t)a.row_splits * (a.per == 1 ? 2 : 1) * b->n_rows * Hq * 8;
+        a.ranges_bytes = (uint64_t)b->n_seqs * tiles * 16;
+        a.acc_bytes = a.chunk < tiles ? round16((uint64_t)b->n_seqs * b->max_kv_len * 8) : 0;
+        a.partial_bytes = a.chunk * tile_bytes;
+        // Images pay where several CTAs would make the same operands from codes.
+        const uint64_t images = (uint64_t)all * H * b->n_seqs, image = 4ull * kRowTile * D;
+        if (!pool && tiles >= 2 && images > 0 && images <= kMaxMassImages / image) {
+            a.steps = (int)all;
+            a.image_bytes = images * image;
+            a.meta_bytes = images * 32;
+        }
+        a.bytes = round16(a.sums_bytes) + a.ranges_bytes + a.acc_bytes + a.partial_bytes + a.image_bytes + a.meta_bytes;
+        return a;
+    }
     a.nc = cols <= 4 ? 1 : cols <= 8 ? 2 : 4;
     a.cols = (int)cols;
     const int warps = split_warps(pool, a.nc);
@@ -225,6 +260,23 @@ extern "C" int patchkv_attention_mass(patchkv_ctx* ctx, const patchkv_geom* g, c
         pl.logits = reinterpret_cast<float*>(ws + plan.items_bytes + plan.sums_bytes);
         pl.tokens = plan.tokens; pl.cols = plan.cols;
         PKV_CUDA(ctx, p.c.D == 128 ? launch_weigh<128>(p, m, pl, plan.nc, plan.groups, stream) : launch_weigh<64>(p, m, pl, plan.nc, plan.groups, stream));
+        return PATCHKV_OK;
+    }
+    if (plan.row_tiles && aligned) {
+        uint8_t* ws = static_cast<uint8_t*>(a->workspace);
+        WeighRowsPlan pl;
+        memset(&pl, 0, sizeof(pl));
+        auto take = [&](uint64_t bytes) { uint8_t* at = bytes ? ws : nullptr; ws += round16(bytes); return at; };
+        pl.images = take(plan.image_bytes);
+        pl.meta = reinterpret_cast<uint32_t*>(take(plan.meta_bytes));
+        pl.sums = reinterpret_cast<float2*>(take(plan.sums_bytes));
+        pl.ranges = reinterpret_cast<int4*>(take(plan.ranges_bytes));
+        pl.acc = reinterpret_cast<double*>(take(plan.acc_bytes));
+        pl.partial = reinterpret_cast<float*>(take(plan.partial_bytes));
+        pl.tiles = plan.row_tiles; pl.splits = plan.row_splits; pl.per = plan.per;
+        pl.slots = plan.row_splits * (plan.per == 1 ? 2 : 1);
+        pl.chunk_tiles = plan.chunk; pl.tokens = plan.tokens; pl.steps = plan.steps;
+        PKV_CUDA(ctx, p.c.D == 128 ? launch_weigh_rows<128>(p, m, pl, stream) : launch_weigh_rows<64>(p, m, pl, stream));
         return PATCHKV_OK;
     }
     float* sums = static_cast<float*>(a->workspace);
