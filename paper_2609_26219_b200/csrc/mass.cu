@@ -120,8 +120,8 @@ struct MassPlan {
     int nc;                     // columns of a lane of the split kernel; 0: another kernel
     int heads, groups, warps_per_head, target, max_items, cols, tokens;
     uint64_t items_bytes, sums_bytes, bytes;
-    int row_tiles, row_splits, per, chunk, steps;       // the row kernels (0 tiles: another): CTAs along the vectors and the tokens, vector tiles of a
-                                // CTA, CTAs along the vectors of a launch of the second pass, steps of a sequence that have images
+    int row_tiles, row_splits, one, chunk, steps;       // the row kernels (0 tiles: another): CTAs along the vectors and the tokens, whether there is one tile
+                                // of vectors, CTAs along the vectors of a launch of the second pass, steps of a sequence that have images
     uint64_t ranges_bytes, acc_bytes, partial_bytes, image_bytes, meta_bytes;
 };
 
@@ -147,11 +147,11 @@ MassPlan plan_mass(const patchkv_geom* g, int tag, const patchkv_batch* b, int H
         if (window > 0 && !b->pos) steps = std::min(all, ((long long)window + sinks + cta_rows) / kRowTile + 3);
         a.row_tiles = (int)tiles;
         a.row_splits = (int)std::max(1ll, std::min((long long)kSms / ctas, steps / 2));
-        a.per = cols <= kRowTile ? 1 : 2;
+        a.one = cols <= kRowTile;
         a.tokens = (int)(steps * kRowTile);
-        const uint64_t tile_bytes = (uint64_t)b->n_seqs * H * a.per * a.tokens * 4;
+        const uint64_t tile_bytes = (uint64_t)b->n_seqs * H * a.tokens * 4;
         a.chunk = (int)std::min<uint64_t>(tiles, std::max<uint64_t>(1, kMaxMassPartial / std::max<uint64_t>(tile_bytes, 1)));
-        a.sums_bytes = (uint64_t)a.row_splits * (a.per == 1 ? 2 : 1) * b->n_rows * Hq * 8;
+        a.sums_bytes = (uint64_t)a.row_splits * weigh_slots(a.one) * b->n_rows * Hq * 8;
         a.ranges_bytes = (uint64_t)b->n_seqs * tiles * 16;
         a.acc_bytes = a.chunk < tiles ? round16((uint64_t)b->n_seqs * b->max_kv_len * 8) : 0;
         a.partial_bytes = a.chunk * tile_bytes;
@@ -273,8 +273,8 @@ extern "C" int patchkv_attention_mass(patchkv_ctx* ctx, const patchkv_geom* g, c
         pl.ranges = reinterpret_cast<int4*>(take(plan.ranges_bytes));
         pl.acc = reinterpret_cast<double*>(take(plan.acc_bytes));
         pl.partial = reinterpret_cast<float*>(take(plan.partial_bytes));
-        pl.tiles = plan.row_tiles; pl.splits = plan.row_splits; pl.per = plan.per;
-        pl.slots = plan.row_splits * (plan.per == 1 ? 2 : 1);
+        pl.tiles = plan.row_tiles; pl.splits = plan.row_splits; pl.one = plan.one;
+        pl.slots = plan.row_splits * weigh_slots(plan.one);
         pl.chunk_tiles = plan.chunk; pl.tokens = plan.tokens; pl.steps = plan.steps;
         PKV_CUDA(ctx, p.c.D == 128 ? launch_weigh_rows<128>(p, m, pl, stream) : launch_weigh_rows<64>(p, m, pl, stream));
         return PATCHKV_OK;

@@ -5,9 +5,10 @@
 //   first pass    S = Q K^T, a lane of TMEM per query vector; a thread adds up 2^(S - ref) over the tokens of its row
 //   second pass   S = K Q^T, a lane per token; a thread adds up 2^(S - log2 of the row's sum) over the vectors of the CTA
 // In both the sum runs along a thread's own lane, so nothing is exchanged, and nothing comes behind the sums: the products of the next
-// steps run while a step is added up (two places in TMEM for each of the two warpgroups).  With one tile of vectors the warpgroups
-// take turns at the steps.  A second pass leaves a number for each token, head and tile of vectors, which the last
-// kernel adds up in an order that the arguments fix.
+// steps run while a step is added up.  Four warpgroups do that, two (a pair) for each tile, half of the columns each, with two places
+// in TMEM for each pair; with one tile of vectors the pairs take turns at the steps.  (Two warpgroups, a tile each, took 3000 cycles a step:
+// two warps a scheduler do not hide one another's latencies.)  The second pass leaves a number for each token, head and CTA, which
+// the last kernel adds up in an order that the arguments fix.
 // Keys are operands without a rounding: bf16 as they are, quantised ones as the sum of two fp16 matrices (22 bits), for two products per
 // 16 channels.  One fp16 matrix alone would put a logit 2^-12 of its terms off and the masses 1e-4.  With many tiles of vectors the operands are
 // laid out in the workspace first (images), as for the attention; else each CTA makes them from the pages, eight warps of it.
@@ -21,13 +22,13 @@
 namespace patchkv {
 
 struct WeighRowsPlan {
-    float2* sums;               // [slot][n_rows * Hq]: reference and sum of a vector over a piece of the tokens
+    float2* sums;               // [slot][n_rows * Hq]: reference and sum of a vector over some of the tokens
     int4* ranges;               // [sequence][tile]: sink steps, first step and count of the steps that a CTA's rows see
-    float* partial;             // [sequence][KV head][tile of the chunk][vector tile][tokens]: what a tile's vectors give to a token
+    float* partial;             // [sequence][KV head][tile of the chunk][tokens]: what a CTA's vectors give to a token
     int32_t tiles, splits;      // CTAs along the vectors of a sequence, and along the tokens
     int32_t slots;              // entries of a vector in `sums`
     int32_t chunk, chunk_tiles; // the second pass: first tile, and number of tiles, of this launch
-    int32_t per;                // vector tiles of a CTA: 1 or 2
+    int32_t one;                // no sequence has more than 128 vectors
     int32_t tokens;             // of a tile in `partial`: 128 for each of its steps
     uint8_t* images;            // [sequence][step][KV head]: the matrix of K and what it leaves of K; null: no images
     uint32_t* meta;             // of each image: 4 words of absent tokens, 4 unused
@@ -38,17 +39,20 @@ struct WeighRowsPlan {
 template <int D>
 cudaError_t launch_weigh_rows(const AttentionParams& p, const WeightParams& m, WeighRowsPlan pl, cudaStream_t s);
 
-constexpr int kWeighProducers = 256;
-__host__ __device__ constexpr int weigh_issuer(bool image) { return image ? 288 : 256 + kWeighProducers; }
+constexpr int kWeighConsumers = 512, kWeighProducers = 256;
+__host__ __device__ constexpr int weigh_issuer(bool image) { return kWeighConsumers + (image ? 32 : kWeighProducers); }
+__host__ __device__ constexpr int weigh_slots(bool one) { return one ? 4 : 2; }     // sums of a vector and a piece: a warpgroup each
 __host__ __device__ constexpr int weigh_threads(bool image) { return weigh_issuer(image) + 32; }
 
 struct WeighBars {
     RowsBars r;
-    uint64_t s_full[2][2], s_empty[2][2], k_full[4], k_empty[4];    // [warpgroup][place in TMEM]; stages of the ring of keys
+    uint64_t s_full[2][2], s_empty[2][2], k_full[4], k_empty[4];    // [pair][place in TMEM]; stages of the ring of keys
+    uint64_t part_full[2][4];                                       // second pass: [pair][step mod 4] the other warpgroups' sums are there
     alignas(16) uint32_t absent[8][8];                              // per step (mod 8)
     float factor[256];                                              // of the vectors' logits
     int32_t pos[256];
-    alignas(16) float4 column[128];                                 // second pass: of a pair of vectors their factors and -log2 of their sums
+    alignas(16) float4 column[128];                                 // second pass: of two vectors their factors and -log2 of their sums
+    float part[4][3][kRowTile];                                     // [step mod 4][warpgroup 1 .. 3]
 };
 template <int D>
 struct WeighSmem {
@@ -76,8 +80,8 @@ __device__ __forceinline__ void weigh_exp2_pair(f32x2 y2, float& a, float& b) {
     unpack2(t, n0, n1);
     unpack2(mul2(e, pack2(__uint_as_float((__float_as_uint(n0) << 23) + 0x3F800000u), __uint_as_float((__float_as_uint(n1) << 23) + 0x3F800000u))), a, b);
 }
-// The 256 threads of the two warpgroups.
-__device__ __forceinline__ void sync_consumers() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+// The threads of the four warpgroups.
+__device__ __forceinline__ void sync_consumers() { asm volatile("bar.sync 1, %0;" ::"n"(kWeighConsumers) : "memory"); }
 
 // KF: format of the keys; IMAGE: they come as images (KF = FMT_INT8 stands for those).  ONE: no sequence has more than one tile of vectors.
 // COLUMNS: the second pass.
@@ -177,7 +181,7 @@ struct WeighRows : RowsKernel<KF, KF, D, IMAGE, KF != FMT_BF16> {
         }
     }
 
-    // ---- the warp that issues the products.  Step j of tile i goes to warpgroup i, or with one tile to warpgroup j & 1.
+    // ---- the warp that issues the products.  Step j of tile i goes to pair i, or with one tile to pair j & 1.
     __device__ __forceinline__ void issue(int tiles, uint32_t tmem) {
         constexpr uint32_t kDesc = instr_desc(KF == FMT_BF16, false, kRowTile), kMat16 = S::kMat >> 4;
         const uint64_t q_desc = smem_desc(this->smem + S::kQ, 16), k_desc = smem_desc(this->smem + S::kK, 16);
@@ -189,11 +193,11 @@ struct WeighRows : RowsKernel<KF, KF, D, IMAGE, KF != FMT_BF16> {
             if (!this->wait_warp(&w.k_full[st], turn(j))) return;
 #pragma unroll 1
             for (int i = 0; i < tiles; i++) {
-                const int wg = ONE ? j & 1 : i, u = ONE ? j >> 1 : j;
-                if (!this->wait_warp(&w.s_empty[wg][u & 1], ((u >> 1) & 1) ^ 1)) return;
+                const int pair = ONE ? j & 1 : i, u = ONE ? j >> 1 : j;
+                if (!this->wait_warp(&w.s_empty[pair][u & 1], ((u >> 1) & 1) ^ 1)) return;
                 tc_after();
                 const uint64_t q = q_desc + i * kMat16, k = k_desc + st * (kStage >> 4);
-                const uint32_t d = tmem + (2 * wg + (u & 1)) * kRowTile;
+                const uint32_t d = tmem + (2 * pair + (u & 1)) * kRowTile;
                 if (elect_lane()) {
 #pragma unroll
                     for (int x = 0; x < D / 16; x++) {              // 16 channels: 32 bytes inside a 128-byte row, then the next half
@@ -201,7 +205,7 @@ struct WeighRows : RowsKernel<KF, KF, D, IMAGE, KF != FMT_BF16> {
                         tc_mma_ss(d, COLUMNS ? k + o : q + o, COLUMNS ? q + o : k + o, kDesc, x != 0);
                         if (FINE) tc_mma_ss(d, COLUMNS ? k + o + kMat16 : q + o, COLUMNS ? q + o : k + o + kMat16, kDesc, true);
                     }
-                    tc_commit(&w.s_full[wg][u & 1]);
+                    tc_commit(&w.s_full[pair][u & 1]);
                     if (i == tiles - 1) tc_commit(&w.k_empty[st]);
                 }
                 __syncwarp();
@@ -209,7 +213,7 @@ struct WeighRows : RowsKernel<KF, KF, D, IMAGE, KF != FMT_BF16> {
         }
     }
 
-    // ---- the warpgroups
+    // ---- the warpgroups: pair wg >> 1, columns 64 (wg & 1) .. + 63 of a place
     static constexpr int kOnFma = 5;                                // of 16 pairs of exponentials, those that are computed (0 .. 16)
     __device__ __forceinline__ static void exp2_both(int c, f32x2 y, float& a, float& b) {
         if (c * kOnFma % 16 < kOnFma) {
@@ -220,7 +224,7 @@ struct WeighRows : RowsKernel<KF, KF, D, IMAGE, KF != FMT_BF16> {
             b = fast_exp2(b);
         }
     }
-    __device__ __forceinline__ void add_row(const float (&x)[32], f32x2 factor2, f32x2 ref2, f32x2 (&total)[2]) {
+    __device__ __forceinline__ static void add_row(const float (&x)[32], f32x2 factor2, f32x2 ref2, f32x2 (&total)[2]) {
 #pragma unroll
         for (int c = 0; c < 16; c++) {
             float a, b;
@@ -228,56 +232,61 @@ struct WeighRows : RowsKernel<KF, KF, D, IMAGE, KF != FMT_BF16> {
             total[c & 1] = add2(total[c & 1], pack2(a, b));
         }
     }
-    // A warpgroup's vectors: queries into shared memory, their factors and positions.
+    // Queries into shared memory, their factors and positions: a tile by the first warpgroup of a pair.
     __device__ __forceinline__ void queries(int wg, int tiles, int first, int m0, int m_end) {
-        if (wg < tiles) {
-            const int m = m0 + (int)threadIdx.x, r = threadIdx.x & 127;
+        const int i = wg >> 1, r = threadIdx.x & 127;
+        if (!(wg & 1) && i < tiles) {
+            const int m = m0 + 128 * i + r;
             const bool live = m < m_end;
             const int row = live ? first + m / this->p.share : first, hq = live ? this->head * this->p.share + m % this->p.share : 0;
-            w.pos[threadIdx.x] = live ? max(-1, row_position(this->p.b, this->seq, row)) : -1;
-            w.factor[threadIdx.x] = this->load_query(wg, r, live, row, hq);
+            w.pos[128 * i + r] = live ? max(-1, row_position(this->p.b, this->seq, row)) : -1;
+            w.factor[128 * i + r] = this->load_query(i, r, live, row, hq);
             fence_async_smem();
             __syncwarp();
-            if ((threadIdx.x & 31) == 0) mbar_arrive(&w.r.q_ready[wg]);
+            if ((threadIdx.x & 31) == 0) mbar_arrive(&w.r.q_ready[i]);
         }
         sync_consumers();
     }
-    __device__ __forceinline__ void release(int wg, int u) {
+    __device__ __forceinline__ void release(int pair, int u) {
         tc_before();
         __syncwarp();
-        if ((threadIdx.x & 31) == 0) mbar_arrive(&w.s_empty[wg][u & 1]);
+        if ((threadIdx.x & 31) == 0) mbar_arrive(&w.s_empty[pair][u & 1]);
+    }
+    __device__ __forceinline__ long long vector_index(int first, int m) const {
+        return (long long)(first + m / this->p.share) * this->p.Hq + this->head * this->p.share + m % this->p.share;
     }
 
     // First pass: a thread per query vector.
     __device__ __forceinline__ void rows(int wg, int tiles, int first, int m0, int m_end, uint32_t tmem, const WeighRowsPlan& pl, int split) {
         queries(wg, tiles, first, m0, m_end);
-        if (!ONE && wg >= tiles) return;
-        const int r = threadIdx.x & 127, i = ONE ? 0 : wg, m = m0 + 128 * i + r, pos = w.pos[128 * i + r], kv = this->kv;
+        const int pair = wg >> 1, half = wg & 1;
+        if (!ONE && pair >= tiles) return;
+        const int r = threadIdx.x & 127, i = ONE ? 0 : pair, m = m0 + 128 * i + r, pos = w.pos[128 * i + r], kv = this->kv;
         float factor = w.factor[128 * i + r];
         const bool broken = factor != factor;
         if (broken) factor = 1.0f;
         if (factor == 0.0f) factor = 1.17549435e-38f;               // a mask is minus infinity over the factor
-        const uint32_t lanes = (uint32_t)((threadIdx.x >> 5) & 3) << 21;
+        const uint32_t at = tmem + ((uint32_t)((threadIdx.x >> 5) & 3) << 21) + 64 * half;
         float ref = kNoMax;
         f32x2 sum2[2] = {pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)};
         const f32x2 factor2 = pack2(factor, factor);
         const int n = this->end - this->begin;
 #pragma unroll 1
-        for (int u = 0, j = ONE ? wg : 0; j < n; u++, j += ONE ? 2 : 1) {
+        for (int u = 0, j = ONE ? pair : 0; j < n; u++, j += ONE ? 2 : 1) {
             const int t0 = this->range.tile(this->begin + j) * kRowTile;
-            const uint32_t s_at = tmem + lanes + (2 * wg + (u & 1)) * kRowTile;
-            if (!this->wait_warp(&w.s_full[wg][u & 1], (u >> 1) & 1)) return;
+            const uint32_t s_at = at + (2 * pair + (u & 1)) * kRowTile;
+            if (!this->wait_warp(&w.s_full[pair][u & 1], (u >> 1) & 1)) return;
             tc_after();
             const uint4 absent = lds128(smem_u32(w.absent[j & 7]));
             const bool gaps = (absent.x | absent.y | absent.z | absent.w) != 0;
             if (gaps || !this->whole(t0)) {                         // what a row does not see becomes minus infinity, in TMEM
-                if (IMAGE && gaps) this->latch_absent(t0, absent);
-                const int b = min(pos, kv - 1) - t0, a = this->p.window > 0 ? max(pos - this->p.window + 1, 0) - t0 : -t0, s = this->p.sinks - t0;
+                if (IMAGE && gaps && !half) this->latch_absent(t0, absent);
+                const int c0 = 64 * half, b = min(pos, kv - 1) - t0, a = this->p.window > 0 ? max(pos - this->p.window + 1, 0) - t0 : -t0, s = this->p.sinks - t0;
                 const uint32_t none = factor < 0.0f ? 0x7F800000u : 0xFF800000u;
 #pragma unroll 1
-                for (int k = 0; k < 8; k++) {
-                    const uint32_t gone = (k < 2 ? absent.x : k < 4 ? absent.y : k < 6 ? absent.z : absent.w) >> (16 * (k & 1));
-                    const uint32_t in = B::seen(16 * k, a, b, s, gone);
+                for (int k = 0; k < 4; k++) {
+                    const uint32_t gone = (half ? (k < 2 ? absent.z : absent.w) : (k < 2 ? absent.x : absent.y)) >> (16 * (k & 1));
+                    const uint32_t in = B::seen(c0 + 16 * k, a, b, s, gone);
                     uint32_t x[16];
                     tc_ld16(x, s_at + 16 * k);
                     tc_wait_ld();
@@ -295,7 +304,7 @@ struct WeighRows : RowsKernel<KF, KF, D, IMAGE, KF != FMT_BF16> {
                 if (search) {
                     float y = -INFINITY;
 #pragma unroll 1
-                    for (int k = 0; k < 8; k++) {
+                    for (int k = 0; k < 4; k++) {
                         uint32_t x[16];
                         tc_ld16(x, s_at + 16 * k);
                         tc_wait_ld();
@@ -310,19 +319,13 @@ struct WeighRows : RowsKernel<KF, KF, D, IMAGE, KF != FMT_BF16> {
                 const f32x2 ref2 = pack2(-ref, -ref);
                 total[0] = sum2[0];
                 total[1] = sum2[1];
-                float x[32], z[32];
-                tc_ld32(x, s_at);
-                tc_wait_ld();
-                tc_ld32(z, s_at + 32);
-                add_row(x, factor2, ref2, total);
-                tc_wait_ld();
-                tc_ld32(x, s_at + 64);
-                add_row(z, factor2, ref2, total);
-                tc_wait_ld();
-                tc_ld32(z, s_at + 96);
-                add_row(x, factor2, ref2, total);
-                tc_wait_ld();
-                add_row(z, factor2, ref2, total);
+#pragma unroll
+                for (int k = 0; k < 2; k++) {
+                    float x[32];
+                    tc_ld32(x, s_at + 32 * k);
+                    tc_wait_ld();
+                    add_row(x, factor2, ref2, total);
+                }
                 if (search) break;
                 float a, b;
                 unpack2(add2(total[0], total[1]), a, b);
@@ -331,109 +334,124 @@ struct WeighRows : RowsKernel<KF, KF, D, IMAGE, KF != FMT_BF16> {
             }
             sum2[0] = total[0];
             sum2[1] = total[1];
-            release(wg, u);
+            release(pair, u);
         }
         if (m >= m_end) return;
         float a, b;
         unpack2(add2(sum2[0], sum2[1]), a, b);
         a += b;
         if (broken && a != 0.0f) a = __uint_as_float(0x7FC00000u);
-        const long long vec = (long long)(first + m / this->p.share) * this->p.Hq + this->head * this->p.share + m % this->p.share;
-        const int slot = ONE ? 2 * split + wg : split;
-        pl.sums[(long long)slot * this->p.b.n_rows * this->p.Hq + vec] = make_float2(ref, a);
+        const int slot = ONE ? 4 * split + wg : 2 * split + half;
+        pl.sums[(long long)slot * this->p.b.n_rows * this->p.Hq + vector_index(first, m)] = make_float2(ref, a);
     }
 
-    // Second pass: a thread per token, the vectors of a tile along its lane.
-    __device__ __forceinline__ void add_column(const float (&x)[32], int at, f32x2 (&total)[2]) const {
+    // Second pass: a thread per token, the vectors of a tile along its lane; `in`: the vectors that see it, where not all do.
+    template <bool MASK>
+    __device__ __forceinline__ void add_column(const float (&x)[32], const float4* column, uint32_t in, f32x2 (&total)[2]) const {
 #pragma unroll
         for (int c = 0; c < 16; c++) {
-            const uint4 v = lds128(smem_u32(&w.column[at + c]));
+            const uint4 v = lds128(smem_u32(column + c));
             float a, b;
             exp2_both(c, fma2(pack2(x[2 * c], x[2 * c + 1]), pack2(__uint_as_float(v.x), __uint_as_float(v.y)), pack2(__uint_as_float(v.z), __uint_as_float(v.w))), a, b);
+            if (MASK) {
+                a = in >> (2 * c) & 1u ? a : 0.0f;
+                b = in >> (2 * c + 1) & 1u ? b : 0.0f;
+            }
             total[c & 1] = add2(total[c & 1], pack2(a, b));
         }
     }
-    // The same for a step in which not every row sees every token: one vector at a time.
-    __device__ __noinline__ float masked_columns(uint32_t s_at, int i, int t, bool there) const {
-        float total = 0.0f;
-#pragma unroll 1
-        for (int k = 0; k < 8; k++) {
-            uint32_t x[16];
-            tc_ld16(x, s_at + 16 * k);
+    template <bool MASK>
+    __device__ __forceinline__ float column_sum(uint32_t s_at, int first, unsigned long long in) const {
+        f32x2 total[2] = {pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)};
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            float x[32];
+            tc_ld32(x, s_at + 32 * k);
             tc_wait_ld();
-#pragma unroll 2
-            for (int c = 0; c < 16; c++) {
-                const int m = 128 * i + 16 * k + c, pos = w.pos[m];
-                const float* v = reinterpret_cast<const float*>(&w.column[m >> 1]) + (m & 1);
-                const bool in = there && t <= pos && sees(this->p, pos, t);
-                total += in ? fast_exp2(fmaf(__uint_as_float(x[c]), v[0], v[2])) : 0.0f;
-            }
+            add_column<MASK>(x, w.column + first / 2 + 16 * k, (uint32_t)(in >> (32 * k)), total);
         }
-        return total;
+        float a, b;
+        unpack2(add2(total[0], total[1]), a, b);
+        return a + b;
+    }
+    // Which of 64 vectors from number `first` of the CTA see token t.  A row's vectors lie together.
+    __device__ __forceinline__ unsigned long long seeing(int first, int m0, int t) const {
+        unsigned long long in = 0;
+        const int share = this->p.share;
+        int left = share - (m0 + first) % share;                    // of the row's vectors, from this one on
+#pragma unroll 1
+        for (int c = 0; c < 64; c += left, left = share) {
+            const int pos = w.pos[first + c];
+            if (t <= pos && sees(this->p, pos, t)) in |= (left < 64 ? (1ull << left) - 1ull : ~0ull) << c;
+        }
+        return in;
     }
     __device__ __forceinline__ void columns(int wg, int tiles, int first, int m0, int m_end, uint32_t tmem, const WeighRowsPlan& pl, int tile) {
-        {
-            // -log2 of the row's sum; minus infinity for a row that sees nothing and for vectors behind the last
-            const int m = m0 + (int)threadIdx.x;
-            float low = -INFINITY;
-            if (m < m_end) {
-                const long long vec = (long long)(first + m / this->p.share) * this->p.Hq + this->head * this->p.share + m % this->p.share;
-                const long long step = (long long)this->p.b.n_rows * this->p.Hq;
-                float top = kNoMax, sum = 0.0f;
-                for (int i = 0; i < pl.slots; i++) top = fmaxf(top, pl.sums[i * step + vec].x);
-                for (int i = 0; i < pl.slots; i++) {
-                    const float2 z = pl.sums[i * step + vec];
-                    sum = fmaf(z.y, fast_exp2(z.x - top), sum);
-                }
-                if (sum != 0.0f) low = -(top + log2f(sum));
+        const int pair = wg >> 1, half = wg & 1, r = threadIdx.x & 127, i = ONE ? 0 : pair, kv = this->kv;
+        // -log2 of the rows' sums; minus infinity for a row that sees nothing and for vectors behind the last
+        float low = -INFINITY;
+        const int m = m0 + 128 * pair + r;
+        if (!half && pair < tiles && m < m_end) {
+            const long long vec = vector_index(first, m), step = (long long)this->p.b.n_rows * this->p.Hq;
+            float top = kNoMax, sum = 0.0f;
+            for (int k = 0; k < pl.slots; k++) top = fmaxf(top, pl.sums[k * step + vec].x);
+            for (int k = 0; k < pl.slots; k++) {
+                const float2 z = pl.sums[k * step + vec];
+                sum = fmaf(z.y, fast_exp2(z.x - top), sum);
             }
-            queries(wg, tiles, first, m0, m_end);
-            float factor = m < m_end ? w.factor[threadIdx.x] : 0.0f;
+            if (sum != 0.0f) low = -(top + log2f(sum));
+        }
+        queries(wg, tiles, first, m0, m_end);
+        if (!half && pair < tiles) {
+            float factor = w.factor[128 * pair + r];
+            if (!(m < m_end)) factor = 0.0f;
             if (factor != factor) factor = 1.0f;
-            float* v = reinterpret_cast<float*>(&w.column[threadIdx.x >> 1]) + (threadIdx.x & 1);
+            float* v = reinterpret_cast<float*>(&w.column[64 * pair + (r >> 1)]) + (r & 1);
             v[0] = factor;
             v[2] = low;
-            sync_consumers();
         }
-        if (!ONE && wg >= tiles) return;
-        const int r = threadIdx.x & 127, i = ONE ? 0 : wg, kv = this->kv;
-        const uint32_t lanes = (uint32_t)((threadIdx.x >> 5) & 3) << 21;
+        sync_consumers();
+        if (!ONE && pair >= tiles) return;
+        const uint32_t at = tmem + ((uint32_t)((threadIdx.x >> 5) & 3) << 21) + 64 * half;
         const int n = this->end - this->begin;
-        float* out = pl.partial + ((((long long)this->seq * this->p.c.H + this->head) * pl.chunk_tiles + tile) * pl.per + i) * pl.tokens;
+        const bool leader = ONE ? half == 0 : wg == 0;              // adds up the other warpgroups' sums of a step, one step later
+        float* out = pl.partial + (((long long)this->seq * this->p.c.H + this->head) * pl.chunk_tiles + tile) * pl.tokens + (long long)this->begin * kRowTile + r;
+        float sum = 0.0f;
+        int u = 0, before = -1;                                     // step whose sum the leader still has
+        auto finish = [&]() {
+            const int v = u - 1;
+            if (!this->wait_warp(&w.part_full[ONE ? pair : 0][v & 3], (v >> 2) & 1)) return false;
+            if (ONE) sum += w.part[v & 3][2 * pair][r];
+            else for (int k = 0; k < 2 * tiles - 1; k++) sum += w.part[v & 3][k][r];
+            out[(long long)before * kRowTile] = sum;
+            return true;
+        };
 #pragma unroll 1
-        for (int u = 0, j = ONE ? wg : 0; j < n; u++, j += ONE ? 2 : 1) {
+        for (int j = ONE ? pair : 0; j < n; u++, j += ONE ? 2 : 1) {
             const int t0 = this->range.tile(this->begin + j) * kRowTile, t = t0 + r;
-            const uint32_t s_at = tmem + lanes + (2 * wg + (u & 1)) * kRowTile;
-            if (!this->wait_warp(&w.s_full[wg][u & 1], (u >> 1) & 1)) return;
+            const uint32_t s_at = at + (2 * pair + (u & 1)) * kRowTile;
+            if (leader && u && !finish()) return;
+            if (!this->wait_warp(&w.s_full[pair][u & 1], (u >> 1) & 1)) return;
             tc_after();
             const uint4 absent = lds128(smem_u32(w.absent[j & 7]));
             const bool gaps = (absent.x | absent.y | absent.z | absent.w) != 0;
-            float sum;
             if (gaps || !this->whole(t0)) {
                 const uint32_t word = r < 32 ? absent.x : r < 64 ? absent.y : r < 96 ? absent.z : absent.w;
-                sum = masked_columns(s_at, i, t, t < kv && !(word >> (r & 31) & 1u));
+                const bool there = t < kv && !(word >> (r & 31) & 1u);
+                sum = column_sum<true>(s_at, 128 * i + 64 * half, there ? seeing(128 * i + 64 * half, m0, t) : 0ull);
             } else {
-                f32x2 total[2] = {pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)};
-                float x[32], z[32];
-                tc_ld32(x, s_at);
-                tc_wait_ld();
-                tc_ld32(z, s_at + 32);
-                add_column(x, 64 * i, total);
-                tc_wait_ld();
-                tc_ld32(x, s_at + 64);
-                add_column(z, 64 * i + 16, total);
-                tc_wait_ld();
-                tc_ld32(z, s_at + 96);
-                add_column(x, 64 * i + 32, total);
-                tc_wait_ld();
-                add_column(z, 64 * i + 48, total);
-                float a, b;
-                unpack2(add2(total[0], total[1]), a, b);
-                sum = a + b;
+                sum = column_sum<false>(s_at, 128 * i + 64 * half, 0ull);
             }
-            release(wg, u);
-            out[(long long)(this->begin + j) * kRowTile + r] = sum;
+            release(pair, u);
+            if (leader) {
+                before = j;
+            } else {
+                w.part[u & 3][ONE ? 2 * pair : wg - 1][r] = sum;
+                __syncwarp();
+                if ((threadIdx.x & 31) == 0) mbar_arrive(&w.part_full[ONE ? pair : 0][u & 3]);
+            }
         }
+        if (leader && u) finish();
     }
 };
 
@@ -449,7 +467,7 @@ __global__ void __launch_bounds__(weigh_threads(IMAGE), 1) weigh_rows_kernel(con
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; i++) {
             mbar_init(&bars.r.q_ready[i], 4);
-            for (int k = 0; k < 2; k++) { mbar_init(&bars.s_full[i][k], 1); mbar_init(&bars.s_empty[i][k], 4); }
+            for (int k = 0; k < 2; k++) { mbar_init(&bars.s_full[i][k], 1); mbar_init(&bars.s_empty[i][k], 8); }
         }
         for (int i = 0; i < 4; i++) { mbar_init(&bars.k_full[i], IMAGE ? 1 : kWeighProducers); mbar_init(&bars.k_empty[i], 1); }
         mbar_init(&bars.r.drained, 1);
@@ -471,6 +489,10 @@ __global__ void __launch_bounds__(weigh_threads(IMAGE), 1) weigh_rows_kernel(con
     const int m0 = tile * 2 * kRowTile, m_end = min(rows * p.share, m0 + 2 * kRowTile);
     if (m0 >= m_end) return;
     const int tiles = !ONE && m_end - m0 > kRowTile ? 2 : 1;
+    if (COLUMNS && threadIdx.x == 0) {          // warps of the warpgroups that are not leaders
+        for (int i = 0; i < 2; i++) for (int k = 0; k < 4; k++) mbar_init(&bars.part_full[i][k], ONE ? 4 : 4 * (2 * tiles - 1));
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
     __syncthreads();
     {   // positions of the CTA's rows (one below 0 sees nothing: no window need reach back for it)
         uint32_t low = 0x7FFFFFFFu;
@@ -503,15 +525,15 @@ __global__ void __launch_bounds__(weigh_threads(IMAGE), 1) weigh_rows_kernel(con
     k.range = step_range(p, kv, bars.r.lo, k.hi);
     k.begin = (int)((long long)k.range.count * split / pl.splits);
     k.end = (int)((long long)k.range.count * (split + 1) / pl.splits);
-    if (!COLUMNS && head == 0 && split == 0 && threadIdx.x == 0) pl.ranges[(long long)seq * pl.tiles + tile] = make_int4(k.range.sink_tiles, k.range.first, k.range.count, tiles);
-    if (warp < 8) {
+    if (!COLUMNS && head == 0 && split == 0 && threadIdx.x == 0) pl.ranges[(long long)seq * pl.tiles + tile] = make_int4(k.range.sink_tiles, k.range.first, k.range.count, 0);
+    if (warp < kWeighConsumers / 32) {
         if (COLUMNS) k.columns(warp >> 2, tiles, first, m0, m_end, tmem, pl, local);
         else k.rows(warp >> 2, tiles, first, m0, m_end, tmem, pl, split);
     } else if (warp < kIssuer / 32) {
         if constexpr (IMAGE) {
             k.fetch_images(pl);
         } else {
-            k.produce(warp - 8);
+            k.produce(warp - kWeighConsumers / 32);
             cp_wait<0>();
         }
     } else if (k.end > k.begin) {
@@ -604,11 +626,11 @@ static __global__ void __launch_bounds__(kWeighJoin) weigh_rows_join_kernel(cons
         const int4 range = pl.ranges[(long long)s * pl.tiles + tile];
         const int v = step < range.x ? step : step - range.y + range.x;
         if (!(step < range.x || (step >= range.y && v < range.z))) continue;
-        const float* from = pl.partial + (((long long)s * p.c.H * pl.chunk_tiles + tile - pl.chunk) * pl.per) * pl.tokens + (long long)v * kRowTile + r;
-        const int per = min(pl.per, range.w);
-        for (int i = 0; i < per; i++)
+        const float* from = pl.partial + ((long long)s * p.c.H * pl.chunk_tiles + tile - pl.chunk) * pl.tokens + (long long)v * kRowTile + r;
+        float heads = 0.0f;
 #pragma unroll 8
-            for (int h = 0; h < p.c.H; h++) sum += from[((long long)h * pl.chunk_tiles * pl.per + i) * pl.tokens];
+        for (int h = 0; h < p.c.H; h++) heads += from[(long long)h * pl.chunk_tiles * pl.tokens];
+        sum += heads;
     }
     part[threadIdx.x] = sum;
     __syncthreads();

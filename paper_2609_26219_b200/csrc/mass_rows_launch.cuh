@@ -38,7 +38,7 @@ cudaError_t launch_weigh_rows_format(const AttentionParams& p, const WeightParam
             const cudaError_t e = launch_pdl(weigh_image_kernel<KF, D>, dim3(pl.steps, p.c.H, p.b.n_seqs), dim3(kImageThreads), 0, s, p, pl);
             return e != cudaSuccess ? e : launch_weigh_rows_passes<FMT_INT8, D, true, false>(p, m, pl, s);
         }
-    return pl.per == 1 ? launch_weigh_rows_passes<KF, D, false, true>(p, m, pl, s) : launch_weigh_rows_passes<KF, D, false, false>(p, m, pl, s);
+    return pl.one ? launch_weigh_rows_passes<KF, D, false, true>(p, m, pl, s) : launch_weigh_rows_passes<KF, D, false, false>(p, m, pl, s);
 }
 template <int D>
 cudaError_t launch_weigh_rows(const AttentionParams& p, const WeightParams& m, WeighRowsPlan pl, cudaStream_t s) {
