@@ -514,8 +514,9 @@ PATCHKV_API uint64_t patchkv_attention_workspace_bytes(const patchkv_geom* geom,
  * patchkv_cache_append quantises, without a rounding in between; values are quantised from their 16 bits.
  * Rows, positions and skipped rows as for patchkv_cache_append; the q_out of a skipped row, and of a row of no sequence, is left
  * as it was.  One launch, no allocation, no workspace; can be captured (inv_freq is read by the call, not by its replays).
- * Every geometry is taken.  The fast kernel wants D a power of two from 16 to 256, rotary_dim a multiple of 32 (HALF) or 16,
- * for quantised pages G a multiple of 16 and page sections of whole 16 bytes, and rows and strides of whole 16 bytes. */
+ * Every geometry is taken.  The fast kernel wants D a power of two from 16 to 256, rotary_dim a multiple of 16,
+ * for quantised pages G a power of two from 16 on (HALF: at least rotary_dim, or dividing its half) and page sections of whole 16 bytes,
+ * and rows and strides of whole 16 bytes. */
 typedef struct {
     uint32_t struct_size;
     int32_t type;                 /* PATCHKV_ROWS_*: type of q, q_out, k and v; into a bf16 pool only PATCHKV_ROWS_BF16 */

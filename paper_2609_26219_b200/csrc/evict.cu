@@ -201,7 +201,7 @@ __device__ __forceinline__ int rows_of(const MoveParams& p, int s) {
 // then values, laid out over the lanes as in rotary_append_kernel.
 template <bool HALF>
 __global__ void __launch_bounds__(kGatherThreads) gather_pool_kernel(const __grid_constant__ MoveParams p) {
-    __shared__ float2 table[kGatherThreads / 32][PATCHKV_MAX_ROTARY_DIM / 2];
+    __shared__ __align__(16) float cosine[kGatherThreads / 32][PATCHKV_MAX_ROTARY_DIM / 2], sine[kGatherThreads / 32][PATCHKV_MAX_ROTARY_DIM / 2];
     pdl_trigger();
     pdl_wait();
     const int s = blockIdx.y, lane = threadIdx.x & 31;
@@ -211,63 +211,50 @@ __global__ void __launch_bounds__(kGatherThreads) gather_pool_kernel(const __gri
     Move m;
     if (!find_move(p, s, i, lane == 0 && part == 0, &m)) return;
     const int u = lane & ((1 << p.U_shift) - 1), sub = lane >> p.U_shift, total = 2 * p.passes;
-    const long long from = (long long)m.from * p.c.stride_page + (long long)m.slot * p.c.stride_token + 16 * u;
-    const long long to = (long long)m.to * p.c.stride_page + (long long)m.to_slot * p.c.stride_token + 16 * u;
+    const long long from = (long long)m.from * p.c.stride_page + (long long)m.slot * p.c.stride_token;
+    const long long to = (long long)m.to * p.c.stride_page + (long long)m.to_slot * p.c.stride_token;
+    const bool rotate = p.rotate && m.turn != 0, turns = rotate && 16 * u < p.Dr;
+    const int ch0 = first_run(HALF && rotate, p.Dr, u), ch1 = second_run(HALF && rotate, p.Dr, u);
     struct Unit { uint4 a, b; };
     auto head_of = [&](int pass) { return ((pass < p.passes ? pass : pass - p.passes) << (5 - p.U_shift)) + sub; };
     auto load = [&](int pass) {
         Unit x = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
         const int h = head_of(pass);
         if (pass >= total || h >= p.c.H) return x;
-        const uint4* a = reinterpret_cast<const uint4*>((pass < p.passes ? p.c.k : p.c.v) + from + (long long)h * p.c.stride_head);
-        x.a = a[0];
-        x.b = a[1];
+        const uint16_t* a = (pass < p.passes ? p.c.k : p.c.v) + from + (long long)h * p.c.stride_head;
+        x.a = *reinterpret_cast<const uint4*>(a + ch0);
+        x.b = *reinterpret_cast<const uint4*>(a + ch1);
         return x;
     };
     Unit next = load(part);
-    const bool rotate = p.rotate && m.turn != 0;
-    float2* tab = table[threadIdx.x >> 5];
+    const int warp = threadIdx.x >> 5;
     if (rotate && part < p.passes)
         for (int j = lane; j < p.Dr >> 1; j += 32) {
             double c, sn;
             cos_sin((double)m.turn * p.f.theta[j], &c, &sn);
-            tab[j] = make_float2((float)c, (float)sn);
+            cosine[warp][j] = (float)c;
+            sine[warp][j] = (float)sn;
         }
     __syncwarp();
-    const int away = p.Dr >> 5;
-    const bool turns = rotate && 16 * u < p.Dr, upper = HALF && u >= away;
-    const int partner = HALF && turns ? (upper ? lane - away : lane + away) : lane;
-    const float2* mine = tab + (!turns ? 0 : HALF ? 16 * (upper ? u - away : u) : 8 * u);
+    float c[8], sn[8];
+    {
+        const float4* a = reinterpret_cast<const float4*>(&cosine[warp][turns ? 8 * u : 0]);
+        const float4* b = reinterpret_cast<const float4*>(&sine[warp][turns ? 8 * u : 0]);
+        const float4 c0 = a[0], c1 = a[1], s0 = b[0], s1 = b[1];
+        c[0] = c0.x; c[1] = c0.y; c[2] = c0.z; c[3] = c0.w; c[4] = c1.x; c[5] = c1.y; c[6] = c1.z; c[7] = c1.w;
+        sn[0] = s0.x; sn[1] = s0.y; sn[2] = s0.z; sn[3] = s0.w; sn[4] = s1.x; sn[5] = s1.y; sn[6] = s1.z; sn[7] = s1.w;
+    }
 #pragma unroll 1
     for (int pass = part; pass < total; pass += p.parts) {
         const Unit x = next;
         next = load(pass + p.parts);
         const int h = head_of(pass);
         uint32_t w[8] = {x.a.x, x.a.y, x.a.z, x.a.w, x.b.x, x.b.y, x.b.z, x.b.w};
-        if (rotate && pass < p.passes) {
-            uint32_t o[8];
-#pragma unroll
-            for (int k = 0; k < 8; k++) o[k] = HALF ? __shfl_sync(0xFFFFFFFFu, w[k], partner) : 0u;
-            if (turns)
-#pragma unroll
-                for (int k = 0; k < 8; k++) {
-                    const float a = bf16_bits_to_float(w[k] & 0xFFFFu), b = __uint_as_float(w[k] & 0xFFFF0000u);
-                    __nv_bfloat162 y;
-                    if (HALF) {
-                        const float a2 = bf16_bits_to_float(o[k] & 0xFFFFu), b2 = __uint_as_float(o[k] & 0xFFFF0000u);
-                        const float2 t0 = mine[2 * k], t1 = mine[2 * k + 1];
-                        y = __floats2bfloat162_rn(fmaf(a2, upper ? t0.y : -t0.y, a * t0.x), fmaf(b2, upper ? t1.y : -t1.y, b * t1.x));
-                    } else {
-                        const float2 t = mine[k];
-                        y = __floats2bfloat162_rn(fmaf(-b, t.y, a * t.x), fmaf(b, t.x, a * t.y));
-                    }
-                    w[k] = *reinterpret_cast<const uint32_t*>(&y);
-                }
-        }
+        if (turns && pass < p.passes) turn_words<PATCHKV_ROWS_BF16, HALF>(w, c, sn);
         if (h < p.c.H) {
-            uint4* a = reinterpret_cast<uint4*>((pass < p.passes ? p.k_pool : p.v_pool) + to + (long long)h * p.c.stride_head);
-            a[0] = make_uint4(w[0], w[1], w[2], w[3]);
-            a[1] = make_uint4(w[4], w[5], w[6], w[7]);
+            uint16_t* a = (pass < p.passes ? p.k_pool : p.v_pool) + to + (long long)h * p.c.stride_head;
+            *reinterpret_cast<uint4*>(a + ch0) = make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint4*>(a + ch1) = make_uint4(w[4], w[5], w[6], w[7]);
         }
     }
 }
@@ -410,7 +397,7 @@ int cache_gather(patchkv_ctx* ctx, const patchkv_geom* g, const patchkv_pool* po
     bool fast;
     long long threads;                                      // of a sequence
     if (pool) {
-        fast = ds >= 4 && ds <= 8 && p.Dr % (half ? 32 : 16) == 0 && p.c.stride_page % 8 == 0 && p.c.stride_token % 8 == 0 &&
+        fast = ds >= 4 && ds <= 8 && p.Dr % 16 == 0 && p.c.stride_page % 8 == 0 && p.c.stride_token % 8 == 0 &&
                p.c.stride_head % 8 == 0 && pool->stride_layer % 8 == 0;
         if (fast) {
             p.U_shift = ds - 4;

@@ -23,23 +23,21 @@ struct RotaryParams {
     int32_t parts;              // warps that share a row
     int32_t q_passes, kv_passes;    // passes of a warp over the queries, and over K or V
     int32_t U_shift;            // log2 of the 16-channel units of a head
-    int32_t seg, G_shift;       // lanes per scale group; log2 of G
+    int32_t G_shift;            // log2 of G
     Frequencies f;
 };
 
-// 16 channels (a lane's) of keys -> codes and, from the group's first lane, its scale: the quantiser's definition in 64 bits, as the rotated
-// key is not a 16-bit number.  (In fp32 a key within 2^-24 of the border of two codes would fall on either side, and a code is a step
-// of up to a seventh of the group's largest value.)  code = rint(x / s): t = x * r with r = 1 / s to 2^-46, corrected once by its
-// remainder; where x / s is a half-integer the remainder is exact and the correction gives it.  Adding 1.5 * 2^52 rounds, ties to even.
+// Eight channels of keys -> codes and, from the group's first lane, its scale: the quantiser's definition in 64 bits, as a rotated key is not a
+// 16-bit number.  (In fp32 a key within 2^-24 of the border of two codes would fall on either side, and a code is a step of up to a seventh
+// of the group's largest value.)  code = rint(x / s): t = x * r with r = 1 / s to 2^-46, corrected once by its remainder; where x / s is a
+// half-integer the remainder is exact and the correction gives it.  Adding 1.5 * 2^52 rounds, ties to even.
 template <int FMT>
-__device__ __forceinline__ void encode64(double (&x)[16], uint8_t* codes, uint8_t* scale, int seg, bool live) {
-    double amax = 0.0;
-#pragma unroll
-    for (int i = 0; i < 16; i++) amax = fmax(amax, fabs(x[i]));
-    for (int d = 1; d < seg; d <<= 1) amax = fmax(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, d));
-    if (!live) return;
+__device__ __forceinline__ uint32_t scale64(double amax) {
+    return __half_as_ushort(__double2half(amax * (1.0 / (FMT == FMT_INT8 ? 127.0 : 7.0))));
+}
+template <int FMT>
+__device__ __forceinline__ void codes64(const double* x, uint32_t s16, uint8_t* codes) {
     constexpr double qmax = FMT == FMT_INT8 ? 127.0 : 7.0;
-    const uint32_t s16 = __half_as_ushort(__double2half(amax * (1.0 / qmax)));
     const bool usable = s16 != 0 && s16 < 0x7C00u;          // a zero or infinite scale: all codes zero
     const float sf = half_bits_to_float(usable ? s16 : 0x3C00u);
     float rf;
@@ -47,44 +45,46 @@ __device__ __forceinline__ void encode64(double (&x)[16], uint8_t* codes, uint8_
     const double s = sf;
     double r = rf;
     r = fma(fma(-s, r, 1.0), r, r);
-    uint32_t code[16];
+    uint32_t code[8];
 #pragma unroll
-    for (int i = 0; i < 16; i++) {
+    for (int i = 0; i < 8; i++) {
         double t = x[i] * r;
         t = fma(fma(-t, s, x[i]), r, t);
         if (s16 < 0x0400u) t = fmin(fmax(t, -qmax), qmax);  // a subnormal scale; else |t| <= qmax (1 + 2^-11)
         code[i] = usable ? (uint32_t)__double2loint(t + 6755399441055744.0) : 0u;
     }
-    uint32_t w[4];
+    uint32_t w[2];
 #pragma unroll
-    for (int i = 0; i < 4; i++)
+    for (int i = 0; i < 2; i++)
         w[i] = __byte_perm(__byte_perm(code[4 * i], code[4 * i + 1], 0x0040), __byte_perm(code[4 * i + 2], code[4 * i + 3], 0x0040), 0x5410);
     if (FMT == FMT_INT8) {
-        *reinterpret_cast<uint4*>(codes) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint2*>(codes) = make_uint2(w[0], w[1]);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
+        for (int i = 0; i < 2; i++) {
             w[i] &= 0x0F0F0F0Fu;
             w[i] = (w[i] | w[i] >> 4) & 0x00FF00FFu;
         }
-        *reinterpret_cast<uint2*>(codes) = make_uint2(__byte_perm(w[0], w[1], 0x6420), __byte_perm(w[2], w[3], 0x6420));
+        *reinterpret_cast<uint32_t*>(codes) = __byte_perm(w[0], w[1], 0x6420);
     }
-    if (scale) *reinterpret_cast<uint16_t*>(scale) = (uint16_t)s16;
 }
 
 // A warp takes a row, or every `parts`-th pass of one; a pass is 32 units of 16 channels: queries, then keys, then values.  A lane has the
-// same channels of a head in every pass, so it keeps the cosines and sines of its channels in registers; in the half layout the
-// other channel of a pair lies Dr / 32 lanes away and comes by shuffle.  Bound by memory: the next pass is asked for before one is worked on.
+// same channels of a head in every pass, both of each rotary pair among them (rotary.cuh), so it keeps their cosines and sines in registers and
+// exchanges nothing but the maxima of the keys' groups.  Bound by memory: the next pass is asked for before one is worked on.
 template <int TYPE, int KF, int VF, bool HALF>
-__global__ void __launch_bounds__(kRotaryThreads) rotary_append_kernel(const __grid_constant__ RotaryParams p) {
+__global__ void __launch_bounds__(kRotaryThreads, KF == FMT_BF16 ? 8 : 6) rotary_append_kernel(const __grid_constant__ RotaryParams p) {
     constexpr bool kPool = KF == FMT_BF16;
-    __shared__ double2 table[kRotaryThreads / 32][PATCHKV_MAX_ROTARY_DIM / 2];
+    constexpr int kPairs = PATCHKV_MAX_ROTARY_DIM / 2, kWarps = kRotaryThreads / 32;
+    __shared__ double2 exact[kPool ? 1 : kWarps][kPool ? 1 : kPairs];       // of angle 8 u + i at i * Dr / 16 + u
+    __shared__ __align__(16) float cosine[kWarps][kPairs], sine[kWarps][kPairs];
     pdl_trigger();
     const uint32_t wid = (blockIdx.x * kRotaryThreads + threadIdx.x) >> 5;
-    const int r = (int)(wid / (uint32_t)p.parts), part = (int)(wid - (uint32_t)r * p.parts), lane = threadIdx.x & 31;
+    const int r = (int)(wid / (uint32_t)p.parts), part = (int)(wid - (uint32_t)r * p.parts), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (r >= p.b.n_rows) return;
     pdl_wait();
     const int u = lane & ((1 << p.U_shift) - 1), sub = lane >> p.U_shift, total = p.q_passes + 2 * p.kv_passes;
+    const int ch0 = first_run(HALF, p.Dr, u), ch1 = second_run(HALF, p.Dr, u);
     struct Unit { uint4 a, b; };
     // Kind of a pass (0 queries, 1 keys, 2 values) and the lane's head in it.
     auto kind_of = [&](int pass, int* h) {
@@ -102,35 +102,35 @@ __global__ void __launch_bounds__(kRotaryThreads) rotary_append_kernel(const __g
         const uint16_t* from = kind == 0 ? p.q + (long long)r * p.q_stride_row + (long long)h * p.q_stride_head
                              : kind == 1 ? p.k + (long long)r * p.k_stride_row + (long long)h * p.k_stride_head
                                          : p.v + (long long)r * p.v_stride_row + (long long)h * p.v_stride_head;
-        x.a = *(reinterpret_cast<const uint4*>(from + 16 * u));
-        x.b = *(reinterpret_cast<const uint4*>(from + 16 * u) + 1);
+        x.a = *reinterpret_cast<const uint4*>(from + (kind == 2 ? 16 * u : ch0));
+        x.b = *reinterpret_cast<const uint4*>(from + (kind == 2 ? 16 * u + 8 : ch1));
         return x;
     };
     Unit next = load(part);
     int slot = 0, pos = 0;
     const int pg = find_page<true>(p, r, lane == 0 && part == 0, &slot, &pos);
     if (pg >= 0) {
-        double2* tab = table[threadIdx.x >> 5];
         if (part < p.q_passes + p.kv_passes) {              // a warp of values alone needs no angles
             if (p.rope_pos) pos = p.rope_pos[r];
             for (int i = lane; i < p.Dr >> 1; i += 32) {
                 double c, s;
                 cos_sin((double)pos * p.f.theta[i], &c, &s);
-                tab[i] = make_double2(p.factor * c, p.factor * s);
+                c *= p.factor;
+                s *= p.factor;
+                if (!kPool) exact[warp][(i & 7) * (p.Dr >> 4) + (i >> 3)] = make_double2(c, s);
+                cosine[warp][i] = (float)c;
+                sine[warp][i] = (float)s;
             }
         }
         __syncwarp();
-        const int away = p.Dr >> 5;                         // lanes between the channels of a pair
-        const bool turns = 16 * u < p.Dr, upper = HALF && u >= away;
-        const int partner = HALF && turns ? (upper ? lane - away : lane + away) : lane;
-        const double2* mine = tab + (!turns ? 0 : HALF ? 16 * (upper ? u - away : u) : 8 * u);
-        constexpr int kAngles = HALF ? 16 : 8;
-        float cf[kAngles], sf[kAngles];
-#pragma unroll
-        for (int i = 0; i < kAngles; i++) {
-            cf[i] = turns ? (float)mine[i].x : 1.0f;
-            sf[i] = turns ? (float)mine[i].y : 0.0f;
-            if (HALF && !upper) sf[i] = -sf[i];
+        const bool turns = 16 * u < p.Dr;
+        float c[8], s[8];
+        {
+            const float4* a = reinterpret_cast<const float4*>(&cosine[warp][turns ? 8 * u : 0]);
+            const float4* b = reinterpret_cast<const float4*>(&sine[warp][turns ? 8 * u : 0]);
+            const float4 c0 = a[0], c1 = a[1], s0 = b[0], s1 = b[1];
+            c[0] = c0.x; c[1] = c0.y; c[2] = c0.z; c[3] = c0.w; c[4] = c1.x; c[5] = c1.y; c[6] = c1.z; c[7] = c1.w;
+            s[0] = s0.x; s[1] = s0.y; s[2] = s0.z; s[3] = s0.w; s[4] = s1.x; s[5] = s1.y; s[6] = s1.z; s[7] = s1.w;
         }
         const long long row = kPool ? (long long)pg * p.c.stride_page + (long long)slot * p.c.stride_token : (long long)pg * p.c.stride_page;
 #pragma unroll 1
@@ -140,66 +140,64 @@ __global__ void __launch_bounds__(kRotaryThreads) rotary_append_kernel(const __g
             int h;
             const int kind = kind_of(pass, &h);
             const bool live = h < (kind == 0 ? p.Hq : p.c.H);
-            const uint32_t w[8] = {x.a.x, x.a.y, x.a.z, x.a.w, x.b.x, x.b.y, x.b.z, x.b.w};
-            const uint32_t at = ((uint32_t)slot * p.c.H + h) * p.c.D + 16 * u, group = at >> p.G_shift;
-            const bool first = (u & (p.seg - 1)) == 0;
-            if (kind == 2) {
-                if constexpr (kPool) {
-                    if (live) {
-                        uint4* to = reinterpret_cast<uint4*>(p.v_pool + row + (long long)h * p.c.stride_head + 16 * u);
-                        to[0] = x.a;
-                        to[1] = x.b;
-                    }
-                } else {
-                    const uint4 v[2] = {x.a, x.b};
-                    uint8_t* page = p.c.base + row;
-                    encode<TYPE, VF, 16>(v, page + p.c.v_codes + (VF == FMT_INT8 ? at : at >> 1), first ? page + p.c.v_scales + 2 * group : nullptr, p.seg, live);
-                }
-                continue;
-            }
-            uint32_t o[8];                                  // the words of the other channels
-#pragma unroll
-            for (int i = 0; i < 8; i++) o[i] = HALF ? __shfl_sync(0xFFFFFFFFu, w[i], partner) : 0u;
-            if (kPool || kind == 0) {
-                uint32_t y[8];
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const float a = to_float<TYPE>(w[i] & 0xFFFFu), b = to_float<TYPE>(w[i] >> 16);
-                    if (HALF) {
-                        const float a2 = to_float<TYPE>(o[i] & 0xFFFFu), b2 = to_float<TYPE>(o[i] >> 16);
-                        y[i] = pack_pair<TYPE>(fmaf(a2, sf[2 * i], a * cf[2 * i]), fmaf(b2, sf[2 * i + 1], b * cf[2 * i + 1]));
-                    } else {
-                        y[i] = pack_pair<TYPE>(fmaf(-b, sf[i], a * cf[i]), fmaf(b, cf[i], a * sf[i]));
-                    }
-                    if (!turns) y[i] = w[i];
-                }
+            const uint32_t head = ((uint32_t)slot * p.c.H + h) * p.c.D;
+            uint32_t w[8] = {x.a.x, x.a.y, x.a.z, x.a.w, x.b.x, x.b.y, x.b.z, x.b.w};
+            if (!kPool && kind == 2) {
+                const uint4 v[2] = {x.a, x.b};
+                const uint32_t at = head + 16 * u, seg = p.G_shift > 4 ? 1u << (p.G_shift - 4) : 1u;
+                uint8_t* page = p.c.base + row;
+                encode<TYPE, VF, 16>(v, page + p.c.v_codes + (VF == FMT_INT8 ? at : at >> 1), (u & (seg - 1)) == 0 ? page + p.c.v_scales + 2 * (at >> p.G_shift) : nullptr,
+                                     (int)seg, live);
+            } else if (kPool || kind == 0) {
+                if (kind != 2 && turns) turn_words<TYPE, HALF>(w, c, s);
                 if (live) {
                     uint16_t* to = kind == 0 ? p.q_out + (long long)r * p.out_stride_row + (long long)h * p.out_stride_head
-                                             : p.k_pool + row + (long long)h * p.c.stride_head;
-                    reinterpret_cast<uint4*>(to + 16 * u)[0] = make_uint4(y[0], y[1], y[2], y[3]);
-                    reinterpret_cast<uint4*>(to + 16 * u)[1] = make_uint4(y[4], y[5], y[6], y[7]);
+                                             : (kind == 1 ? p.k_pool : p.v_pool) + row + (long long)h * p.c.stride_head;
+                    *reinterpret_cast<uint4*>(to + (kind == 2 ? 16 * u : ch0)) = make_uint4(w[0], w[1], w[2], w[3]);
+                    *reinterpret_cast<uint4*>(to + (kind == 2 ? 16 * u + 8 : ch1)) = make_uint4(w[4], w[5], w[6], w[7]);
                 }
             } else if constexpr (!kPool) {
-                double z[16];
+                double z[16];                               // the runs: 0 .. 7 and 8 .. 15
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    const double a = to_float<TYPE>(w[i] & 0xFFFFu), b = to_float<TYPE>(w[i] >> 16);
-                    if (!turns) {
-                        z[2 * i] = a;
-                        z[2 * i + 1] = b;
-                    } else if (HALF) {
-                        const double a2 = to_float<TYPE>(o[i] & 0xFFFFu), b2 = to_float<TYPE>(o[i] >> 16);
-                        const double2 t0 = mine[2 * i], t1 = mine[2 * i + 1];
-                        z[2 * i] = fma(a2, upper ? t0.y : -t0.y, a * t0.x);
-                        z[2 * i + 1] = fma(b2, upper ? t1.y : -t1.y, b * t1.x);
-                    } else {
-                        const double2 t = mine[i];
-                        z[2 * i] = fma(-b, t.y, a * t.x);
-                        z[2 * i + 1] = fma(b, t.x, a * t.y);
+                    z[2 * i] = low_float<TYPE>(w[i]);
+                    z[2 * i + 1] = high_float<TYPE>(w[i]);
+                }
+                if (turns)
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        const double2 t = exact[warp][i * (p.Dr >> 4) + u];
+                        double& a = z[HALF ? i : 2 * i];
+                        double& b = z[HALF ? 8 + i : 2 * i + 1];
+                        const double y = fma(-b, t.y, a * t.x);
+                        b = fma(b, t.x, a * t.y);
+                        a = y;
+                    }
+                // A group lies in 8 channels of each of G / 8 lanes, or (joint) in all 16 of G / 16: behind the rotary channels, where it has
+                // them all, and in the interleaved layout.
+                const bool joint = !HALF || !turns || p.Dr <= 1 << p.G_shift;
+                double m0 = 0.0, m1 = 0.0;
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    m0 = fmax(m0, fabs(z[i]));
+                    m1 = fmax(m1, fabs(z[8 + i]));
+                }
+                if (joint) m0 = m1 = fmax(m0, m1);
+                const int lanes = 1 << (p.G_shift - (joint ? 4 : 3));
+                for (int d = 1; d < 1 << p.U_shift; d <<= 1) {
+                    const double a = __shfl_xor_sync(0xFFFFFFFFu, m0, d), b = __shfl_xor_sync(0xFFFFFFFFu, m1, d);
+                    if (d < lanes) { m0 = fmax(m0, a); m1 = fmax(m1, b); }
+                }
+                if (live) {
+                    uint8_t* page = p.c.base + row;
+                    const uint32_t s0 = scale64<KF>(m0), s1 = joint ? s0 : scale64<KF>(m1), at0 = head + ch0, at1 = head + ch1;
+                    codes64<KF>(z, s0, page + (KF == FMT_INT8 ? at0 : at0 >> 1));
+                    codes64<KF>(z + 8, s1, page + (KF == FMT_INT8 ? at1 : at1 >> 1));
+                    if ((u & (lanes - 1)) == 0) {
+                        *reinterpret_cast<uint16_t*>(page + p.c.k_scales + 2 * (at0 >> p.G_shift)) = (uint16_t)s0;
+                        if (!joint) *reinterpret_cast<uint16_t*>(page + p.c.k_scales + 2 * (at1 >> p.G_shift)) = (uint16_t)s1;
                     }
                 }
-                uint8_t* page = p.c.base + row;
-                encode64<KF>(z, page + (KF == FMT_INT8 ? at : at >> 1), first ? page + p.c.k_scales + 2 * group : nullptr, p.seg, live);
             }
         }
     }
@@ -354,13 +352,13 @@ extern "C" int patchkv_rotary_append(patchkv_ctx* ctx, const patchkv_geom* g, co
     p.Hq = a->n_q_heads; p.Dr = g->rotary_dim;
     const bool half = g->rope_style == PATCHKV_ROPE_HALF, f16 = a->type == PATCHKV_ROWS_F16;
     const int D = g->head_dim, ds = log2_exact(D), gs = log2_exact(g->group);
-    bool fast = ds >= 4 && ds <= 8 && g->rotary_dim % (half ? 32 : 16) == 0 && vectors(a->k, a->k_stride_row, a->k_stride_head) &&
+    bool fast = ds >= 4 && ds <= 8 && g->rotary_dim % 16 == 0 && vectors(a->k, a->k_stride_row, a->k_stride_head) &&
                 vectors(a->v, a->v_stride_row, a->v_stride_head);
     if (p.Hq) fast = fast && vectors(a->q, a->q_stride_row, a->q_stride_head) && vectors(a->q_out, a->q_out_stride_row, a->q_out_stride_head);
     const long long elems = (long long)g->page_tokens * g->n_kv_heads * D;
     if (pool) fast = fast && p.c.stride_page % 8 == 0 && p.c.stride_token % 8 == 0 && p.c.stride_head % 8 == 0 && pool->stride_layer % 8 == 0;
-    else fast = fast && gs >= 4 && elems % 32 == 0 && (elems / g->group) % 8 == 0;
-    p.seg = fast && !pool ? g->group / 16 : 1;
+    // (a group's channels have to lie in one run of each of its lanes, or in both)
+    else fast = fast && gs >= 4 && elems % 32 == 0 && (elems / g->group) % 8 == 0 && (!half || p.Dr <= g->group || (p.Dr / 2) % g->group == 0);
     p.G_shift = gs < 0 ? 0 : gs;
     p.U_shift = fast ? ds - 4 : 0;
     p.half = half;

@@ -1,6 +1,8 @@
 // Cosines and sines of rotary positions (rotary.cu, evict.cu).
 #pragma once
 
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <math.h>
 
 #include "common.cuh"
@@ -43,6 +45,48 @@ __device__ __forceinline__ void cos_sin(double angle, double* c, double* s) {
     const double a = quarter & 1 ? sn : cs, b = quarter & 1 ? cs : sn;
     *c = (quarter + 1) & 2 ? -a : a;
     *s = quarter & 2 ? -b : b;
+}
+
+// A lane of the fast kernels has 16 channels of a head, two runs of eight, such that it has both channels of its eight rotary pairs: in the
+// half layout the runs lie Dr / 2 apart, in the interleaved one, and behind the rotary channels, side by side.  Angle 8 u + i belongs to pair i
+// of lane u of the head.
+__device__ __forceinline__ int first_run(bool half, int Dr, int u) { return half && 16 * u < Dr ? 8 * u : 16 * u; }
+__device__ __forceinline__ int second_run(bool half, int Dr, int u) { return half && 16 * u < Dr ? Dr / 2 + 8 * u : 16 * u + 8; }
+
+// The runs' eight words in bf16 or fp16 (TYPE), turned by c[i], s[i] in fp32.
+template <int TYPE>
+__device__ __forceinline__ float low_float(uint32_t w) {
+    if (TYPE == PATCHKV_ROWS_F16) return __half2float(__ushort_as_half((unsigned short)(w & 0xFFFFu)));
+    return __uint_as_float(w << 16);
+}
+template <int TYPE>
+__device__ __forceinline__ float high_float(uint32_t w) {
+    if (TYPE == PATCHKV_ROWS_F16) return __half2float(__ushort_as_half((unsigned short)(w >> 16)));
+    return __uint_as_float(w & 0xFFFF0000u);
+}
+template <int TYPE>
+__device__ __forceinline__ uint32_t pack_floats(float lo, float hi) {
+    uint32_t d;
+    if (TYPE == PATCHKV_ROWS_F16) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+template <int TYPE, bool HALF>
+__device__ __forceinline__ void turn_words(uint32_t (&w)[8], const float (&c)[8], const float (&s)[8]) {
+    if (HALF) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const float a0 = low_float<TYPE>(w[i]), a1 = high_float<TYPE>(w[i]), b0 = low_float<TYPE>(w[4 + i]), b1 = high_float<TYPE>(w[4 + i]);
+            w[i] = pack_floats<TYPE>(fmaf(-b0, s[2 * i], a0 * c[2 * i]), fmaf(-b1, s[2 * i + 1], a1 * c[2 * i + 1]));
+            w[4 + i] = pack_floats<TYPE>(fmaf(b0, c[2 * i], a0 * s[2 * i]), fmaf(b1, c[2 * i + 1], a1 * s[2 * i + 1]));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float a = low_float<TYPE>(w[i]), b = high_float<TYPE>(w[i]);
+            w[i] = pack_floats<TYPE>(fmaf(-b, s[i], a * c[i]), fmaf(b, c[i], a * s[i]));
+        }
+    }
 }
 
 }  // namespace patchkv
