@@ -21,11 +21,14 @@ struct RotaryParams {
     double factor;
     int32_t Hq, Dr, half;
     int32_t parts;              // warps that share a row
-    int32_t q_passes, kv_passes;    // passes of a warp over the queries, and over K or V
+    int32_t q_passes, kv_passes;    // passes of a warp over the queries, and over the keys and values
     int32_t U_shift;            // log2 of the 16-channel units of a head
     int32_t G_shift;            // log2 of G
     Frequencies f;
 };
+
+// The larger of two numbers that are not negative: their bit patterns order them.
+__device__ __forceinline__ unsigned long long magnitude(double x) { return __double_as_longlong(x) & 0x7FFFFFFFFFFFFFFFull; }
 
 // Eight channels of keys -> codes and, from the group's first lane, its scale: the quantiser's definition in 64 bits, as a rotated key is not a
 // 16-bit number.  (In fp32 a key within 2^-24 of the border of two codes would fall on either side, and a code is a step of up to a seventh
@@ -50,13 +53,15 @@ __device__ __forceinline__ void codes64(const double* x, uint32_t s16, uint8_t* 
     for (int i = 0; i < 8; i++) {
         double t = x[i] * r;
         t = fma(fma(-t, s, x[i]), r, t);
-        if (s16 < 0x0400u) t = fmin(fmax(t, -qmax), qmax);  // a subnormal scale; else |t| <= qmax (1 + 2^-11)
-        code[i] = usable ? (uint32_t)__double2loint(t + 6755399441055744.0) : 0u;
+        code[i] = (uint32_t)__double2loint(t + 6755399441055744.0);
     }
+    if (s16 < 0x0400u)                                      // a subnormal scale; else |t| <= qmax (1 + 2^-11), which rounds to qmax
+#pragma unroll
+        for (int i = 0; i < 8; i++) code[i] = (uint32_t)min(max((int)code[i], -(int)qmax), (int)qmax);
     uint32_t w[2];
 #pragma unroll
     for (int i = 0; i < 2; i++)
-        w[i] = __byte_perm(__byte_perm(code[4 * i], code[4 * i + 1], 0x0040), __byte_perm(code[4 * i + 2], code[4 * i + 3], 0x0040), 0x5410);
+        w[i] = usable ? __byte_perm(__byte_perm(code[4 * i], code[4 * i + 1], 0x0040), __byte_perm(code[4 * i + 2], code[4 * i + 3], 0x0040), 0x5410) : 0u;
     if (FMT == FMT_INT8) {
         *reinterpret_cast<uint2*>(codes) = make_uint2(w[0], w[1]);
     } else {
@@ -69,9 +74,9 @@ __device__ __forceinline__ void codes64(const double* x, uint32_t s16, uint8_t* 
     }
 }
 
-// A warp takes a row, or every `parts`-th pass of one; a pass is 32 units of 16 channels: queries, then keys, then values.  A lane has the
-// same channels of a head in every pass, both of each rotary pair among them (rotary.cuh), so it keeps their cosines and sines in registers and
-// exchanges nothing but the maxima of the keys' groups.  Bound by memory: the next pass is asked for before one is worked on.
+// A warp takes a row, or every `parts`-th pass of one; a pass is 32 units of 16 channels of the queries, or of the keys and the values.  A lane has
+// the same channels of a head in every pass, both of each rotary pair among them (rotary.cuh), so it keeps their cosines and sines in registers
+// and exchanges nothing but the maxima of the keys' groups.  Two units of a lane are on their way at a time.
 template <int TYPE, int KF, int VF, bool HALF>
 __global__ void __launch_bounds__(kRotaryThreads, KF == FMT_BF16 ? 8 : 6) rotary_append_kernel(const __grid_constant__ RotaryParams p) {
     constexpr bool kPool = KF == FMT_BF16;
@@ -83,44 +88,33 @@ __global__ void __launch_bounds__(kRotaryThreads, KF == FMT_BF16 ? 8 : 6) rotary
     const int r = (int)(wid / (uint32_t)p.parts), part = (int)(wid - (uint32_t)r * p.parts), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (r >= p.b.n_rows) return;
     pdl_wait();
-    const int u = lane & ((1 << p.U_shift) - 1), sub = lane >> p.U_shift, total = p.q_passes + 2 * p.kv_passes;
+    const int u = lane & ((1 << p.U_shift) - 1), sub = lane >> p.U_shift, per_pass = 32 >> p.U_shift;       // unit, head of a pass, heads of a pass
     const int ch0 = first_run(HALF, p.Dr, u), ch1 = second_run(HALF, p.Dr, u);
     struct Unit { uint4 a, b; };
-    // Kind of a pass (0 queries, 1 keys, 2 values) and the lane's head in it.
-    auto kind_of = [&](int pass, int* h) {
-        const int kind = pass < p.q_passes ? 0 : pass < p.q_passes + p.kv_passes ? 1 : 2;
-        pass -= kind == 0 ? 0 : kind == 1 ? p.q_passes : p.q_passes + p.kv_passes;
-        *h = (pass << (5 - p.U_shift)) + sub;
-        return kind;
-    };
-    auto load = [&](int pass) {
+    auto load = [&](const uint16_t* from, int c0, int c1, bool live) {
         Unit x = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-        if (pass >= total) return x;
-        int h;
-        const int kind = kind_of(pass, &h);
-        if (h >= (kind == 0 ? p.Hq : p.c.H)) return x;
-        const uint16_t* from = kind == 0 ? p.q + (long long)r * p.q_stride_row + (long long)h * p.q_stride_head
-                             : kind == 1 ? p.k + (long long)r * p.k_stride_row + (long long)h * p.k_stride_head
-                                         : p.v + (long long)r * p.v_stride_row + (long long)h * p.v_stride_head;
-        x.a = *reinterpret_cast<const uint4*>(from + (kind == 2 ? 16 * u : ch0));
-        x.b = *reinterpret_cast<const uint4*>(from + (kind == 2 ? 16 * u + 8 : ch1));
+        if (live) {
+            x.a = *reinterpret_cast<const uint4*>(from + c0);
+            x.b = *reinterpret_cast<const uint4*>(from + c1);
+        }
         return x;
     };
-    Unit next = load(part);
+    auto store = [&](uint16_t* to, int c0, int c1, const uint32_t (&w)[8]) {
+        *reinterpret_cast<uint4*>(to + c0) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(to + c1) = make_uint4(w[4], w[5], w[6], w[7]);
+    };
     int slot = 0, pos = 0;
     const int pg = find_page<true>(p, r, lane == 0 && part == 0, &slot, &pos);
     if (pg >= 0) {
-        if (part < p.q_passes + p.kv_passes) {              // a warp of values alone needs no angles
-            if (p.rope_pos) pos = p.rope_pos[r];
-            for (int i = lane; i < p.Dr >> 1; i += 32) {
-                double c, s;
-                cos_sin((double)pos * p.f.theta[i], &c, &s);
-                c *= p.factor;
-                s *= p.factor;
-                if (!kPool) exact[warp][(i & 7) * (p.Dr >> 4) + (i >> 3)] = make_double2(c, s);
-                cosine[warp][i] = (float)c;
-                sine[warp][i] = (float)s;
-            }
+        if (p.rope_pos) pos = p.rope_pos[r];
+        for (int i = lane; i < p.Dr >> 1; i += 32) {
+            double c, s;
+            cos_sin((double)pos * p.f.theta[i], &c, &s);
+            c *= p.factor;
+            s *= p.factor;
+            if (!kPool) exact[warp][(i & 7) * (p.Dr >> 4) + (i >> 3)] = make_double2(c, s);
+            cosine[warp][i] = (float)c;
+            sine[warp][i] = (float)s;
         }
         __syncwarp();
         const bool turns = 16 * u < p.Dr;
@@ -132,31 +126,53 @@ __global__ void __launch_bounds__(kRotaryThreads, KF == FMT_BF16 ? 8 : 6) rotary
             c[0] = c0.x; c[1] = c0.y; c[2] = c0.z; c[3] = c0.w; c[4] = c1.x; c[5] = c1.y; c[6] = c1.z; c[7] = c1.w;
             s[0] = s0.x; s[1] = s0.y; s[2] = s0.z; s[3] = s0.w; s[4] = s1.x; s[5] = s1.y; s[6] = s1.z; s[7] = s1.w;
         }
+        int pass = part;
+        {
+            const uint16_t* q = p.q + (long long)r * p.q_stride_row + (long long)(pass * per_pass + sub) * p.q_stride_head;
+            uint16_t* out = p.q_out + (long long)r * p.out_stride_row + (long long)(pass * per_pass + sub) * p.out_stride_head;
+            const long long q_step = (long long)p.parts * per_pass * p.q_stride_head, out_step = (long long)p.parts * per_pass * p.out_stride_head;
+            const int h_step = p.parts * per_pass;
+            int h = pass * per_pass + sub;
+#pragma unroll 1
+            for (; pass < p.q_passes; pass += 2 * p.parts, h += 2 * h_step) {
+                const bool live0 = h < p.Hq, live1 = h + h_step < p.Hq;
+                const Unit x = load(q, ch0, ch1, live0), y = load(q + q_step, ch0, ch1, live1);
+                uint32_t w[8] = {x.a.x, x.a.y, x.a.z, x.a.w, x.b.x, x.b.y, x.b.z, x.b.w};
+                if (turns) turn_words<TYPE, HALF>(w, c, s);
+                if (live0) store(out, ch0, ch1, w);
+                uint32_t v[8] = {y.a.x, y.a.y, y.a.z, y.a.w, y.b.x, y.b.y, y.b.z, y.b.w};
+                if (turns) turn_words<TYPE, HALF>(v, c, s);
+                if (live1) store(out + out_step, ch0, ch1, v);
+                q += 2 * q_step;
+                out += 2 * out_step;
+            }
+            // (a warp whose second unit would have been the first pass behind the queries has not done that one)
+            if (pass - p.parts >= p.q_passes) pass -= p.parts;
+        }
         const long long row = kPool ? (long long)pg * p.c.stride_page + (long long)slot * p.c.stride_token : (long long)pg * p.c.stride_page;
 #pragma unroll 1
-        for (int pass = part; pass < total; pass += p.parts) {
-            const Unit x = next;
-            next = load(pass + p.parts);
-            int h;
-            const int kind = kind_of(pass, &h);
-            const bool live = h < (kind == 0 ? p.Hq : p.c.H);
-            const uint32_t head = ((uint32_t)slot * p.c.H + h) * p.c.D;
+        for (; pass < p.q_passes + p.kv_passes; pass += p.parts) {
+            const int h = (pass - p.q_passes) * per_pass + sub;
+            const bool live = h < p.c.H;
+            const Unit x = load(p.k + (long long)r * p.k_stride_row + (long long)h * p.k_stride_head, ch0, ch1, live);
+            const Unit y = load(p.v + (long long)r * p.v_stride_row + (long long)h * p.v_stride_head, 16 * u, 16 * u + 8, live);
             uint32_t w[8] = {x.a.x, x.a.y, x.a.z, x.a.w, x.b.x, x.b.y, x.b.z, x.b.w};
-            if (!kPool && kind == 2) {
-                const uint4 v[2] = {x.a, x.b};
-                const uint32_t at = head + 16 * u, seg = p.G_shift > 4 ? 1u << (p.G_shift - 4) : 1u;
-                uint8_t* page = p.c.base + row;
-                encode<TYPE, VF, 16>(v, page + p.c.v_codes + (VF == FMT_INT8 ? at : at >> 1), (u & (seg - 1)) == 0 ? page + p.c.v_scales + 2 * (at >> p.G_shift) : nullptr,
-                                     (int)seg, live);
-            } else if (kPool || kind == 0) {
-                if (kind != 2 && turns) turn_words<TYPE, HALF>(w, c, s);
+            if constexpr (kPool) {
+                if (turns) turn_words<TYPE, HALF>(w, c, s);
+                const uint32_t v[8] = {y.a.x, y.a.y, y.a.z, y.a.w, y.b.x, y.b.y, y.b.z, y.b.w};
                 if (live) {
-                    uint16_t* to = kind == 0 ? p.q_out + (long long)r * p.out_stride_row + (long long)h * p.out_stride_head
-                                             : (kind == 1 ? p.k_pool : p.v_pool) + row + (long long)h * p.c.stride_head;
-                    *reinterpret_cast<uint4*>(to + (kind == 2 ? 16 * u : ch0)) = make_uint4(w[0], w[1], w[2], w[3]);
-                    *reinterpret_cast<uint4*>(to + (kind == 2 ? 16 * u + 8 : ch1)) = make_uint4(w[4], w[5], w[6], w[7]);
+                    store(p.k_pool + row + (long long)h * p.c.stride_head, ch0, ch1, w);
+                    store(p.v_pool + row + (long long)h * p.c.stride_head, 16 * u, 16 * u + 8, v);
                 }
-            } else if constexpr (!kPool) {
+            } else {
+                uint8_t* page = p.c.base + row;
+                const uint32_t head = ((uint32_t)slot * p.c.H + h) * p.c.D;
+                {
+                    const uint4 v[2] = {y.a, y.b};
+                    const uint32_t at = head + 16 * u, seg = 1u << (p.G_shift - 4);
+                    encode<TYPE, VF, 16>(v, page + p.c.v_codes + (VF == FMT_INT8 ? at : at >> 1),
+                                         (u & (seg - 1)) == 0 ? page + p.c.v_scales + 2 * (at >> p.G_shift) : nullptr, (int)seg, live);
+                }
                 double z[16];                               // the runs: 0 .. 7 and 8 .. 15
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
@@ -169,28 +185,28 @@ __global__ void __launch_bounds__(kRotaryThreads, KF == FMT_BF16 ? 8 : 6) rotary
                         const double2 t = exact[warp][i * (p.Dr >> 4) + u];
                         double& a = z[HALF ? i : 2 * i];
                         double& b = z[HALF ? 8 + i : 2 * i + 1];
-                        const double y = fma(-b, t.y, a * t.x);
+                        const double e = fma(-b, t.y, a * t.x);
                         b = fma(b, t.x, a * t.y);
-                        a = y;
+                        a = e;
                     }
                 // A group lies in 8 channels of each of G / 8 lanes, or (joint) in all 16 of G / 16: behind the rotary channels, where it has
                 // them all, and in the interleaved layout.
                 const bool joint = !HALF || !turns || p.Dr <= 1 << p.G_shift;
-                double m0 = 0.0, m1 = 0.0;
+                unsigned long long m0 = 0, m1 = 0;
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    m0 = fmax(m0, fabs(z[i]));
-                    m1 = fmax(m1, fabs(z[8 + i]));
+                    m0 = max(m0, magnitude(z[i]));
+                    m1 = max(m1, magnitude(z[8 + i]));
                 }
-                if (joint) m0 = m1 = fmax(m0, m1);
+                if (joint) m0 = m1 = max(m0, m1);
                 const int lanes = 1 << (p.G_shift - (joint ? 4 : 3));
-                for (int d = 1; d < 1 << p.U_shift; d <<= 1) {
-                    const double a = __shfl_xor_sync(0xFFFFFFFFu, m0, d), b = __shfl_xor_sync(0xFFFFFFFFu, m1, d);
-                    if (d < lanes) { m0 = fmax(m0, a); m1 = fmax(m1, b); }
+                for (int d = 1; d < 1 << (p.G_shift - 3) && d < 1 << p.U_shift; d <<= 1) {
+                    const unsigned long long a = __shfl_xor_sync(0xFFFFFFFFu, m0, d), b = __shfl_xor_sync(0xFFFFFFFFu, m1, d);
+                    if (d < lanes) { m0 = max(m0, a); m1 = max(m1, b); }
                 }
                 if (live) {
-                    uint8_t* page = p.c.base + row;
-                    const uint32_t s0 = scale64<KF>(m0), s1 = joint ? s0 : scale64<KF>(m1), at0 = head + ch0, at1 = head + ch1;
+                    const uint32_t s0 = scale64<KF>(__longlong_as_double((long long)m0)), s1 = joint ? s0 : scale64<KF>(__longlong_as_double((long long)m1));
+                    const uint32_t at0 = head + ch0, at1 = head + ch1;
                     codes64<KF>(z, s0, page + (KF == FMT_INT8 ? at0 : at0 >> 1));
                     codes64<KF>(z + 8, s1, page + (KF == FMT_INT8 ? at1 : at1 >> 1));
                     if ((u & (lanes - 1)) == 0) {
@@ -368,7 +384,7 @@ extern "C" int patchkv_rotary_append(patchkv_ctx* ctx, const patchkv_geom* g, co
         p.q_passes = (p.Hq + per_pass - 1) / per_pass;
         p.kv_passes = (g->n_kv_heads + per_pass - 1) / per_pass;
         // Few rows: a warp for each pass of a row.
-        const int passes = p.q_passes + 2 * p.kv_passes;
+        const int passes = p.q_passes + p.kv_passes;
         if ((long long)p.b.n_rows * passes <= 16 * 148) p.parts = passes;
     }
     const long long threads = (long long)p.b.n_rows * (fast ? 32 * p.parts : p.Hq + 2 * g->n_kv_heads);

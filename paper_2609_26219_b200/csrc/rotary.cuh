@@ -76,9 +76,13 @@ __device__ __forceinline__ void turn_words(uint32_t (&w)[8], const float (&c)[8]
     if (HALF) {
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            const float a0 = low_float<TYPE>(w[i]), a1 = high_float<TYPE>(w[i]), b0 = low_float<TYPE>(w[4 + i]), b1 = high_float<TYPE>(w[4 + i]);
-            w[i] = pack_floats<TYPE>(fmaf(-b0, s[2 * i], a0 * c[2 * i]), fmaf(-b1, s[2 * i + 1], a1 * c[2 * i + 1]));
-            w[4 + i] = pack_floats<TYPE>(fmaf(b0, c[2 * i], a0 * s[2 * i]), fmaf(b1, c[2 * i + 1], a1 * s[2 * i + 1]));
+            const f32x2 a = pack2(low_float<TYPE>(w[i]), high_float<TYPE>(w[i])), b = pack2(low_float<TYPE>(w[4 + i]), high_float<TYPE>(w[4 + i]));
+            const f32x2 cc = pack2(c[2 * i], c[2 * i + 1]), ss = pack2(s[2 * i], s[2 * i + 1]);
+            float lo, hi;
+            unpack2(sub2(mul2(a, cc), mul2(b, ss)), lo, hi);
+            w[i] = pack_floats<TYPE>(lo, hi);
+            unpack2(fma2(a, ss, mul2(b, cc)), lo, hi);
+            w[4 + i] = pack_floats<TYPE>(lo, hi);
         }
     } else {
 #pragma unroll
