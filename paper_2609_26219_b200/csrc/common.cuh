@@ -125,6 +125,8 @@ __device__ __forceinline__ uint16_t lds16(uint32_t a) {
     return v;
 }
 
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
 // Programmatic dependent launch (sm_90+).  A kernel launched with launch_pdl may be brought onto the SMs while the kernel
 // in front of it in the stream is still running; it calls pdl_wait() before it touches global memory, which returns
 // once that kernel has completed and its writes are visible.  pdl_trigger() tells the runtime that the kernel behind

@@ -226,6 +226,12 @@ __global__ void __launch_bounds__(kGatherThreads) gather_pool_kernel(const __gri
         x.b = *reinterpret_cast<const uint4*>(a + ch1);
         return x;
     };
+    if (p.parts == 1)
+        for (int c = 0; c < p.c.D; c += 64)                 // 128 bytes
+            for (int h = lane; h < p.c.H; h += 32) {
+                prefetch_l2(p.c.k + from + (long long)h * p.c.stride_head + c);
+                prefetch_l2(p.c.v + from + (long long)h * p.c.stride_head + c);
+            }
     Unit next = load(part);
     const int warp = threadIdx.x >> 5;
     if (rotate && part < p.passes)

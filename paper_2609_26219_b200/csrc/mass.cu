@@ -168,12 +168,12 @@ MassPlan plan_mass(const patchkv_geom* g, int tag, const patchkv_batch* b, int H
     a.nc = cols <= 4 ? 1 : cols <= 8 ? 2 : 4;
     a.cols = (int)cols;
     const int warps = split_warps(pool, a.nc);
-    a.heads = 1;                                // heads of a CTA, and pieces of the batch, as the attention has them
+    a.heads = 1;                                // heads of a CTA, and pieces of the batch, as the attention has them (but for the CTAs an SM)
     for (int h = 2; h <= warps; h *= 2)
         if ((H + h - 1) / h * h <= (H + a.heads - 1) / a.heads * a.heads || h <= H) a.heads = h;
     a.groups = (H + a.heads - 1) / a.heads;
     a.warps_per_head = warps / a.heads;
-    const int slots = std::max(1, kSms / a.groups);
+    const int slots = std::max(1, kWeighCtas * kSms / a.groups);
     a.target = b->n_seqs >= 2 * slots ? 0 : std::max(slots - b->n_seqs, (slots + 1) / 2);
     a.max_items = b->n_seqs + a.target;
     // Tiles that a sequence's rows can see: with a window, and rows one behind the other, not all of them.

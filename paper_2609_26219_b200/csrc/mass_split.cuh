@@ -22,6 +22,9 @@ struct WeighPlan {
 template <int D>
 cudaError_t launch_weigh(const AttentionParams& p, const WeightParams& m, const WeighPlan& pl, int nc, int groups, cudaStream_t s);
 
+// Two CTAs an SM: one leaves the schedulers idle for 40 % of the cycles (8 x 64k tokens of 4-bit pages, 8 columns: KERNELTIMES).
+constexpr int kWeighCtas = 2;
+
 // Sums need no 16-bit weights here: a reference is moved only when fp32 runs short.
 constexpr float kWeighTop = 60.0f;
 
@@ -136,7 +139,7 @@ struct WeighKernel : SplitKernel<KF, KF, D, NC, STAGES, WARPS, G32> {
 };
 
 template <int KF, int D, int NC, int STAGES, int WARPS, bool G32>
-__global__ void __launch_bounds__(WARPS * 32) weigh_split_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ WeighPlan pl) {
+__global__ void __launch_bounds__(WARPS * 32, kWeighCtas) weigh_split_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ WeighPlan pl) {
     using K = WeighKernel<KF, D, NC, STAGES, WARPS, G32>;
     extern __shared__ __align__(16) uint8_t smem[];
     pdl_trigger();
@@ -194,7 +197,10 @@ __global__ void __launch_bounds__(WARPS * 32) weigh_split_kernel(const __grid_co
         auto fetch = [&](int i) {
             const uint32_t flags = __shfl_sync(0xFFFFFFFFu, here.flags, i & 31), row0 = __shfl_sync(0xFFFFFFFFu, here.row0, i & 31);
             const long long at = __shfl_sync(0xFFFFFFFFu, here.at, i & 31);
-            if (i < n) k.fetch_keys(fetch_base, at, row0, flags & 1, flags >> 1, flags & 1 ? 0 : k.first_token(i));
+            if (i < n) {
+                if (flags & 1) k.fetch_keys(fetch_base, at, row0, true, true, 0);
+                else k.fetch_keys(fetch_base, at, row0, false, flags >> 1, k.first_token(i));
+            }
             cp_commit();
             if ((i & 31) == 31) here = place_of(i + 1 + lane);
             whole = whole << 1 | (flags & 1);
@@ -279,76 +285,96 @@ __global__ void __launch_bounds__(WARPS * 32) weigh_split_kernel(const __grid_co
     pl.sums[((long long)blockIdx.x * p.c.H + head) * (4 * NC) + lane] = make_float2(m, l);
 }
 
-// Second pass (grid: 256 tokens, sequence): a thread has four tokens and a quarter of the columns.
-constexpr int kWeighTokens = 256, kWeighThreads = 256, kWeighColumns = 512;
+// Second pass (grid: CTAs of a sequence, sequence): a CTA takes every gridDim.x-th 256 tokens, a thread four tokens and a quarter of the columns.
+// Bound by the logits' bytes; the columns' sums are found once a CTA, so there are no more of those than fill the SMs.
+constexpr int kWeighTokens = 256, kWeighThreads = 256, kWeighColumns = 256;
 template <int NC>
 __global__ void __launch_bounds__(kWeighThreads) weigh_join_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ WeightParams m,
                                                                    const __grid_constant__ WeighPlan pl) {
-    __shared__ float sums[kWeighColumns];                    // log2 of a column's sum
+    __shared__ float2 column[kWeighColumns];                 // log2 of a column's sum, and its place in the logits (a whole number's bits)
+    __shared__ float2 pieces_of[kWeighThreads];
     __shared__ float4 part[3][kWeighTokens / 4];
+    pdl_trigger();
     pdl_wait();
-    const int s = blockIdx.y, t0 = blockIdx.x * kWeighTokens, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int s = blockIdx.y;
     int first, kv, rows, lo, hi, least;
-    if (!sequence_rows(p, s, &first, &kv, &rows) || t0 >= kv) return;
+    if (!sequence_rows(p, s, &first, &kv, &rows) || (int)blockIdx.x * kWeighTokens >= kv) return;
     const int quad = threadIdx.x & (kWeighTokens / 4 - 1), part_of = threadIdx.x / (kWeighTokens / 4);
-    float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     position_range(p, s, first, rows, &lo, &hi, &least);
     const TileRange range = tile_range(p, kv, lo, hi);
     const int all = rows == 0 ? 0 : min(min(rows, p.b.max_rows) * p.share, 4 * NC);
-    // the place of this thread's tokens in the logits
-    const int tile = (t0 + 4 * quad) / kTile, v = tile < range.sink_tiles ? tile : tile - range.first + range.sink_tiles;
-    const bool seen = tile < range.sink_tiles || (tile >= range.first && v < range.count);
-    const float* from = pl.logits + (long long)s * p.c.H * pl.cols * pl.tokens + (long long)v * kTile + (4 * quad & (kTile - 1));
     const int item0 = all ? pl.s.items[2 * s] : 0, pieces = all ? pl.s.items[2 * s + 1] : 0, columns = p.c.H * all;
-    for (int j0 = 0; j0 < columns; j0 += kWeighColumns) {
-        const int n = min(columns - j0, kWeighColumns);
-        if (j0) __syncthreads();
-        for (int j = warp; j < n; j += kWeighThreads / 32) {
-            const int h = (j0 + j) / all, c = (j0 + j) - h * all;
+    const float* logits = pl.logits + (long long)s * p.c.H * pl.cols * pl.tokens;
+    // log2 of the sums of columns j0 .. j0 + n - 1: several threads share a column's pieces.
+    auto sums_of = [&](int j0, int n) {
+        const int shares = kWeighThreads / n, j = (int)threadIdx.x % n, share = (int)threadIdx.x / n;
+        const int h = (j0 + j) / all, c = (j0 + j) - h * all;
+        float top = kNoMax, sum = 0.0f;
+        if (share < shares) {
             const float2* ml = pl.sums + ((long long)item0 * p.c.H + h) * (4 * NC) + c;
-            float top = kNoMax, sum = 0.0f;
-            for (int i = lane; i < pieces; i += 32) {
+#pragma unroll 4
+            for (int i = share; i < pieces; i += shares) {
                 const float2 z = ml[(long long)i * p.c.H * (4 * NC)];
                 const float to = fmaxf(top, z.x);
                 sum = fmaf(sum, fast_exp2(top - to), z.y * fast_exp2(z.x - to));
                 top = to;
             }
-            float best = top;
-#pragma unroll
-            for (int d = 16; d; d >>= 1) best = fmaxf(best, __shfl_xor_sync(0xFFFFFFFFu, best, d));
-            sum *= fast_exp2(top - best);
-#pragma unroll
-            for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-            if (lane == 0) sums[j] = sum == 0.0f ? INFINITY : best + log2f(sum);
+        }
+        __syncthreads();                                     // nobody reads the columns before any more
+        pieces_of[threadIdx.x] = make_float2(top, sum);
+        __syncthreads();
+        if (threadIdx.x < n) {
+            for (int i = 1; i < shares; i++) {
+                const float2 z = pieces_of[i * n + j];
+                const float to = fmaxf(top, z.x);
+                sum = fmaf(sum, fast_exp2(top - to), z.y * fast_exp2(z.x - to));
+                top = to;
+            }
+            column[j] = make_float2(sum == 0.0f ? INFINITY : top + log2f(sum), __int_as_float(h * pl.cols + c));
         }
         __syncthreads();
-        if (seen) {
-#pragma unroll 4
+    };
+    if (columns > 0 && columns <= kWeighColumns) sums_of(0, columns);
+#pragma unroll 1
+    for (int t0 = blockIdx.x * kWeighTokens; t0 < kv; t0 += gridDim.x * kWeighTokens) {
+        // the place of this thread's tokens in the logits
+        const int tile = (t0 + 4 * quad) / kTile, v = tile < range.sink_tiles ? tile : tile - range.first + range.sink_tiles;
+        const bool seen = tile < range.sink_tiles || (tile >= range.first && v < range.count);
+        const float* from = logits + (long long)v * kTile + (4 * quad & (kTile - 1));
+        float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 1
+        for (int j0 = 0; j0 < columns; j0 += kWeighColumns) {
+            const int n = min(columns - j0, kWeighColumns);
+            if (columns > kWeighColumns) sums_of(j0, n);
+            if (!seen) continue;
+            // (a token that the row does not see has no weight, whatever the row's sum is)
+            auto weight = [](float x, float total) { return x == -INFINITY ? 0.0f : fast_exp2(x - total); };
+#pragma unroll 8
             for (int j = part_of; j < n; j += 4) {
-                const int h = (j0 + j) / all, c = (j0 + j) - h * all;
-                const float4 x = *reinterpret_cast<const float4*>(from + ((long long)h * pl.cols + c) * pl.tokens);
-                const float total = sums[j];
-                // (a token that the row does not see has no weight, whatever the row's sum is)
-                y.x += x.x == -INFINITY ? 0.0f : fast_exp2(x.x - total);
-                y.y += x.y == -INFINITY ? 0.0f : fast_exp2(x.y - total);
-                y.z += x.z == -INFINITY ? 0.0f : fast_exp2(x.z - total);
-                y.w += x.w == -INFINITY ? 0.0f : fast_exp2(x.w - total);
+                const float2 z = column[j];
+                const float4 x = *reinterpret_cast<const float4*>(from + (long long)__float_as_int(z.y) * pl.tokens);
+                y.x += weight(x.x, z.x);
+                y.y += weight(x.y, z.x);
+                y.z += weight(x.z, z.x);
+                y.w += weight(x.w, z.x);
             }
         }
-    }
-    if (part_of) part[part_of - 1][quad] = y;
-    __syncthreads();
-    if (part_of) return;
+        if (part_of) part[part_of - 1][quad] = y;
+        __syncthreads();
+        if (!part_of) {
 #pragma unroll
-    for (int i = 0; i < 3; i++) {
-        const float4 z = part[i][quad];
-        y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
+            for (int i = 0; i < 3; i++) {
+                const float4 z = part[i][quad];
+                y.x += z.x; y.y += z.y; y.z += z.z; y.w += z.w;
+            }
+            const int t = t0 + 4 * quad;
+            if (t < kv) store_mass(p, m, s, t, y.x);
+            if (t + 1 < kv) store_mass(p, m, s, t + 1, y.y);
+            if (t + 2 < kv) store_mass(p, m, s, t + 2, y.z);
+            if (t + 3 < kv) store_mass(p, m, s, t + 3, y.w);
+        }
+        __syncthreads();
     }
-    const int t = t0 + 4 * quad;
-    if (t < kv) store_mass(p, m, s, t, y.x);
-    if (t + 1 < kv) store_mass(p, m, s, t + 1, y.y);
-    if (t + 2 < kv) store_mass(p, m, s, t + 2, y.z);
-    if (t + 3 < kv) store_mass(p, m, s, t + 3, y.w);
 }
 
 }  // namespace patchkv

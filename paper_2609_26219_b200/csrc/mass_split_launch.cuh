@@ -1,6 +1,8 @@
 // Launches of the kernels of mass_split.cuh for one head dimension; a translation unit per dimension (mass_split_64.cu, mass_split_128.cu).
 #pragma once
 
+#include <algorithm>
+
 #include "attention_launch.cuh"
 #include "mass_split.cuh"
 
@@ -10,7 +12,7 @@ template <int KF, int D, int NC>
 struct WeighShape {
     static constexpr int kWarps = split_warps(KF == FMT_BF16, NC);
     static constexpr int kBytes = kTile * ((KF == FMT_BF16 ? 2 * D : KF == FMT_INT8 ? D : D / 2) + 24) + 64;
-    static constexpr int kFit = 200 * 1024 / (kWarps * kBytes);
+    static constexpr int kFit = (220 / kWeighCtas - 8) * 1024 / (kWarps * kBytes);
     static constexpr int kStages = kFit > 6 ? 6 : kFit;
     static_assert(kStages >= 2, "the ring needs two stages");
 };
@@ -33,7 +35,8 @@ cudaError_t launch_weigh_columns(const AttentionParams& p, const WeightParams& m
     else if (kf == FMT_INT8) e = p.c.G == 32 ? launch_weigh_one<FMT_INT8, D, NC, true>(p, pl, groups, s) : launch_weigh_one<FMT_INT8, D, NC, false>(p, pl, groups, s);
     else e = p.c.G == 32 ? launch_weigh_one<FMT_INT4, D, NC, true>(p, pl, groups, s) : launch_weigh_one<FMT_INT4, D, NC, false>(p, pl, groups, s);
     if (e != cudaSuccess) return e;
-    return launch_pdl(weigh_join_kernel<NC>, dim3((p.b.max_kv_len + kWeighTokens - 1) / kWeighTokens, p.b.n_seqs), dim3(kWeighThreads), 0, s, p, m, pl);
+    const int blocks = (p.b.max_kv_len + kWeighTokens - 1) / kWeighTokens, ctas = std::max(1, 6 * 148 / p.b.n_seqs);
+    return launch_pdl(weigh_join_kernel<NC>, dim3(std::min(blocks, ctas), p.b.n_seqs), dim3(kWeighThreads), 0, s, p, m, pl);
 }
 template <int D>
 cudaError_t launch_weigh(const AttentionParams& p, const WeightParams& m, const WeighPlan& pl, int nc, int groups, cudaStream_t s) {
