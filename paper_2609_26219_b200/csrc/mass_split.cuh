@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(WARPS * 32, kWeighCtas) weigh_split_kernel(con
 // Bound by the logits' bytes; the columns' sums are found once a CTA, so there are no more of those than fill the SMs.
 constexpr int kWeighTokens = 256, kWeighThreads = 256, kWeighColumns = 256;
 template <int NC>
-__global__ void __launch_bounds__(kWeighThreads) weigh_join_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ WeightParams m,
+__global__ void __launch_bounds__(kWeighThreads, 4) weigh_join_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ WeightParams m,
                                                                    const __grid_constant__ WeighPlan pl) {
     __shared__ float2 column[kWeighColumns];                 // log2 of a column's sum, and its place in the logits (a whole number's bits)
     __shared__ float2 pieces_of[kWeighThreads];
@@ -349,14 +349,22 @@ __global__ void __launch_bounds__(kWeighThreads) weigh_join_kernel(const __grid_
             if (!seen) continue;
             // (a token that the row does not see has no weight, whatever the row's sum is)
             auto weight = [](float x, float total) { return x == -INFINITY ? 0.0f : fast_exp2(x - total); };
-#pragma unroll 8
-            for (int j = part_of; j < n; j += 4) {
-                const float2 z = column[j];
-                const float4 x = *reinterpret_cast<const float4*>(from + (long long)__float_as_int(z.y) * pl.tokens);
-                y.x += weight(x.x, z.x);
-                y.y += weight(x.y, z.x);
-                y.z += weight(x.z, z.x);
-                y.w += weight(x.w, z.x);
+            constexpr int kAtOnce = 8;
+#pragma unroll 1
+            for (int j = part_of; j < n; j += 4 * kAtOnce) {
+                float4 x[kAtOnce];
+#pragma unroll
+                for (int i = 0; i < kAtOnce; i++)
+                    if (j + 4 * i < n) x[i] = *reinterpret_cast<const float4*>(from + (long long)__float_as_int(column[j + 4 * i].y) * pl.tokens);
+#pragma unroll
+                for (int i = 0; i < kAtOnce; i++)
+                    if (j + 4 * i < n) {
+                        const float total = column[j + 4 * i].x;
+                        y.x += weight(x[i].x, total);
+                        y.y += weight(x[i].y, total);
+                        y.z += weight(x[i].z, total);
+                        y.w += weight(x[i].w, total);
+                    }
             }
         }
         if (part_of) part[part_of - 1][quad] = y;
