@@ -151,7 +151,7 @@ MassPlan plan_mass(const patchkv_geom* g, int tag, const patchkv_batch* b, int H
         a.tokens = (int)(steps * kRowTile);
         const uint64_t tile_bytes = (uint64_t)b->n_seqs * H * a.tokens * 4;
         a.chunk = (int)std::min<uint64_t>(tiles, std::max<uint64_t>(1, kMaxMassPartial / std::max<uint64_t>(tile_bytes, 1)));
-        a.sums_bytes = (uint64_t)a.row_splits * weigh_slots(a.one) * b->n_rows * Hq * 8;
+        a.sums_bytes = (uint64_t)a.row_splits * b->n_rows * Hq * 8;
         a.ranges_bytes = (uint64_t)b->n_seqs * tiles * 16;
         a.acc_bytes = a.chunk < tiles ? round16((uint64_t)b->n_seqs * b->max_kv_len * 8) : 0;
         a.partial_bytes = a.chunk * tile_bytes;
@@ -274,7 +274,6 @@ extern "C" int patchkv_attention_mass(patchkv_ctx* ctx, const patchkv_geom* g, c
         pl.acc = reinterpret_cast<double*>(take(plan.acc_bytes));
         pl.partial = reinterpret_cast<float*>(take(plan.partial_bytes));
         pl.tiles = plan.row_tiles; pl.splits = plan.row_splits; pl.one = plan.one;
-        pl.slots = plan.row_splits * weigh_slots(plan.one);
         pl.chunk_tiles = plan.chunk; pl.tokens = plan.tokens; pl.steps = plan.steps;
         PKV_CUDA(ctx, p.c.D == 128 ? launch_weigh_rows<128>(p, m, pl, stream) : launch_weigh_rows<64>(p, m, pl, stream));
         return PATCHKV_OK;

@@ -22,11 +22,10 @@
 namespace patchkv {
 
 struct WeighRowsPlan {
-    float2* sums;               // [slot][n_rows * Hq]: reference and sum of a vector over some of the tokens
+    float2* sums;               // [split][n_rows * Hq]: reference and sum of a vector over a piece of the tokens
     int4* ranges;               // [sequence][tile]: sink steps, first step and count of the steps that a CTA's rows see
     float* partial;             // [sequence][KV head][tile of the chunk][tokens]: what a CTA's vectors give to a token
     int32_t tiles, splits;      // CTAs along the vectors of a sequence, and along the tokens
-    int32_t slots;              // entries of a vector in `sums`
     int32_t chunk, chunk_tiles; // the second pass: first tile, and number of tiles, of this launch
     int32_t one;                // no sequence has more than 128 vectors
     int32_t tokens;             // of a tile in `partial`: 128 for each of its steps
@@ -41,18 +40,33 @@ cudaError_t launch_weigh_rows(const AttentionParams& p, const WeightParams& m, W
 
 constexpr int kWeighConsumers = 512, kWeighProducers = 256;
 __host__ __device__ constexpr int weigh_issuer(bool image) { return kWeighConsumers + (image ? 32 : kWeighProducers); }
-__host__ __device__ constexpr int weigh_slots(bool one) { return one ? 4 : 2; }     // sums of a vector and a piece: a warpgroup each
-__host__ __device__ constexpr int weigh_threads(bool image) { return weigh_issuer(image) + 32; }
+__host__ __device__ constexpr int weigh_threads(bool image) { return weigh_issuer(image) + 64; }        // and the warp that finds the work
 
+// A piece of work: up to 256 vectors of a KV head and some of the tokens that they see.
+struct WeighItem {
+    int32_t ok;                 // 0: there is no more work
+    int32_t seq, head, tile, split, first, kv, m0, m_end, tiles;
+    int32_t lo, least, hi;      // smallest position not below 0, smallest and largest of the rows
+    TileRange range;
+    int32_t begin, end;         // its steps of the range
+};
 struct WeighBars {
-    RowsBars r;
+    uint64_t item_full[2], item_empty[2];
+    uint64_t q_ready[2];                                            // [tile] the queries are there, and what goes with them
+    uint64_t q_free;                                                // the products of an item are done
+    uint64_t mate_done[2];                                          // [pair] its other warpgroups are through with an item
     uint64_t s_full[2][2], s_empty[2][2], k_full[4], k_empty[4];    // [pair][place in TMEM]; stages of the ring of keys
-    uint64_t part_full[2][4];                                       // second pass: [pair][step mod 4] the other warpgroups' sums are there
-    alignas(16) uint32_t absent[8][8];                              // per step (mod 8)
+    uint64_t part_full[4][4];                                       // second pass: [warpgroup][unit mod 4] its sum is there
+    uint64_t drained;
+    alignas(16) uint32_t absent[8][8];                              // per step (mod 8): tokens whose page is out of range
+    WeighItem item[2];
     float factor[256];                                              // of the vectors' logits
     int32_t pos[256];
     alignas(16) float4 column[128];                                 // second pass: of two vectors their factors and -log2 of their sums
-    float part[4][3][kRowTile];                                     // [step mod 4][warpgroup 1 .. 3]
+    float2 sums[4][kRowTile];                                       // first pass: [warpgroup] reference and sum
+    float part[4][4][kRowTile];                                     // second pass: [unit mod 4][warpgroup]
+    uint32_t tmem;
+    int32_t abort;
 };
 template <int D>
 struct WeighSmem {
@@ -80,141 +94,262 @@ __device__ __forceinline__ void weigh_exp2_pair(f32x2 y2, float& a, float& b) {
     unpack2(t, n0, n1);
     unpack2(mul2(e, pack2(__uint_as_float((__float_as_uint(n0) << 23) + 0x3F800000u), __uint_as_float((__float_as_uint(n1) << 23) + 0x3F800000u))), a, b);
 }
-// The threads of the four warpgroups.
-__device__ __forceinline__ void sync_consumers() { asm volatile("bar.sync 1, %0;" ::"n"(kWeighConsumers) : "memory"); }
-
 // KF: format of the keys; IMAGE: they come as images (KF = FMT_INT8 stands for those).  ONE: no sequence has more than one tile of vectors.
-// COLUMNS: the second pass.
+// COLUMNS: the second pass.  A CTA stays on its SM and takes one item after the other: setting one up (12 us of 40 when every
+// item was a CTA of its own) goes on under the products of the one before, but for the queries, which have one place.  Counters run through
+// all items: g steps, u the units (steps of a tile) of a pair.
 template <int KF, int D, bool IMAGE, bool ONE, bool COLUMNS>
-struct WeighRows : RowsKernel<KF, KF, D, IMAGE, KF != FMT_BF16> {
-    static constexpr bool FINE = KF != FMT_BF16;
+struct WeighRows {
+    static constexpr bool FINE = KF != FMT_BF16, kPool = KF == FMT_BF16;
     using B = RowsKernel<KF, KF, D, IMAGE, FINE>;
     using S = RowsSmem<D>;
-    static constexpr int kStages = FINE ? 2 : 4;
+    static constexpr int kStages = FINE ? 2 : 4, kPer = D / 32, kTok = 32 / kPer;
     static constexpr uint32_t kStage = (FINE ? 2 : 1) * S::kMat;
+    const AttentionParams& p;
+    const WeighRowsPlan& pl;
     WeighBars& w;
+    const uint32_t smem;
+    WeighItem it;
+    int last;                                                       // a step up to this token needs no mask
 
-    __device__ __forceinline__ WeighRows(const AttentionParams& p_, WeighBars& b) : B(p_, b.r), w(b) {}
+    __device__ __forceinline__ WeighRows(const AttentionParams& p_, const WeighRowsPlan& pl_, WeighBars& w_, uint32_t smem_) : p(p_), pl(pl_), w(w_), smem(smem_) {}
+    // A wait of a whole warp: all of its lanes go on, or none.
+    __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, &w.abort)); }
+    __device__ __forceinline__ void arrive(uint64_t* bar) {
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
+    }
     __device__ __forceinline__ static uint32_t turn(int n) { return (uint32_t)(n / kStages) & 1u; }
-    __device__ __forceinline__ uint32_t key_stage(int n) const { return this->smem + S::kK + (n % kStages) * kStage; }
+    __device__ __forceinline__ uint32_t key_stage(int n) const { return smem + S::kK + (n % kStages) * kStage; }
+    // Seen by some row (or by none): only then does a token's slot take part.  The same exactly, for what counts as an error.
+    __device__ __forceinline__ bool any_sees(int t) const { return t <= min(it.hi, it.kv - 1) && sees(p, it.lo, t); }
+    __device__ __forceinline__ bool really_seen(int t) const {
+        return any_sees(t) && (!p.b.pos || p.window == 0 || some_row_sees(p, it.first + it.m0 / p.share, it.first + (it.m_end - 1) / p.share, t));
+    }
+    __device__ __forceinline__ bool whole(int t0) const { return whole_step(p, last, it.hi, t0); }
+    __device__ __forceinline__ int steps() const { return it.end - it.begin; }
+
+    // The k-th item, into registers; false when there is none, or after an abort.
+    __device__ __forceinline__ bool next(int k) {
+        if (!wait(&w.item_full[k & 1], (k >> 1) & 1)) return false;
+        it = w.item[k & 1];
+        arrive(&w.item_empty[k & 1]);
+        last = min(it.least, it.kv - 1);
+        return it.ok != 0;
+    }
+
+    // ---- the warp that finds the items: in order of the CTAs, and back again, the last rows (the most tokens) of all heads first
+    __device__ __forceinline__ void find_items() {
+        const int lane = threadIdx.x & 31;
+        const long long total = (long long)pl.chunk_tiles * p.c.H * p.b.n_seqs * pl.splits;
+        int k = 0;
+        for (long long round = 0;; round++) {
+            const long long at = round * gridDim.x + (round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+            const bool more = round * gridDim.x < total;
+            if (more && at >= total) continue;
+            WeighItem x;
+            x.ok = 0;
+            if (more) {
+                long long id = at;
+                x.split = (int)(id % pl.splits); id /= pl.splits;
+                x.head = (int)(id % p.c.H); id /= p.c.H;
+                x.seq = (int)(id % p.b.n_seqs);
+                x.tile = pl.chunk_tiles - 1 - (int)(id / p.b.n_seqs);
+                int rows;
+                const bool ordered = sequence_rows(p, x.seq, &x.first, &x.kv, &rows);
+                if (lane == 0 && (!ordered || rows > p.b.max_rows || p.b.kv_len[x.seq] > x.kv)) latch(p.status);
+                if (!ordered) continue;
+                x.m0 = (pl.chunk + x.tile) * 2 * kRowTile;
+                x.m_end = min(min(rows, p.b.max_rows) * p.share, x.m0 + 2 * kRowTile);
+                if (x.m0 >= x.m_end) continue;
+                x.tiles = !ONE && x.m_end - x.m0 > kRowTile ? 2 : 1;
+                // positions of the rows (one below 0 sees nothing: no window need reach back for it)
+                uint32_t low = 0x7FFFFFFFu;
+                int least = 0x7FFFFFFF, most = -1;
+                for (int r = x.m0 / p.share + lane; r <= (x.m_end - 1) / p.share; r += 32) {
+                    const int pos = row_position(p.b, x.seq, x.first + r);
+                    low = min(low, (uint32_t)pos);
+                    least = min(least, pos);
+                    most = max(most, pos);
+                }
+                x.lo = (int)__reduce_min_sync(0xFFFFFFFFu, low);
+                x.least = __reduce_min_sync(0xFFFFFFFFu, least);
+                x.hi = __reduce_max_sync(0xFFFFFFFFu, most);
+                x.range = step_range(p, x.kv, x.lo, x.hi);
+                x.begin = (int)((long long)x.range.count * x.split / pl.splits);
+                x.end = (int)((long long)x.range.count * (x.split + 1) / pl.splits);
+                x.ok = 1;
+                if (!COLUMNS && x.head == 0 && x.split == 0 && lane == 0)
+                    pl.ranges[(long long)x.seq * pl.tiles + pl.chunk + x.tile] = make_int4(x.range.sink_tiles, x.range.first, x.range.count, 0);
+            }
+            if (!wait(&w.item_empty[k & 1], ((k >> 1) & 1) ^ 1)) return;
+            if (lane == 0) w.item[k & 1] = x;
+            arrive(&w.item_full[k & 1]);
+            k++;
+            if (!more) return;
+        }
+    }
 
     // ---- the warps that bring the keys
-    __device__ __forceinline__ void fetch_images(const WeighRowsPlan& pl) {
+    __device__ __forceinline__ void fetch_images() {
         int n = 0;
-        for (int j = this->begin; j < this->end; j++, n++) {
-            const int st = n % kStages;
-            const long long at = ((long long)this->seq * pl.steps + this->range.tile(j)) * this->p.c.H + this->head;
-            if (!this->wait_warp(&w.k_empty[st], turn(n) ^ 1)) break;
-            if (elect_lane()) {
-                mbar_arrive_expect_tx(&w.k_full[st], kStage + 32);
-                bulk_g2s_at(key_stage(n), pl.images + at * kStage, kStage, &w.k_full[st]);
-                bulk_g2s_at(smem_u32(w.absent[n & 7]), pl.meta + at * 8, 32, &w.k_full[st]);
+        bool good = true;
+        for (int k = 0; good && next(k); k++)
+            for (int j = it.begin; j < it.end; j++) {
+                const int st = n % kStages;
+                const long long at = ((long long)it.seq * pl.steps + it.range.tile(j)) * p.c.H + it.head;
+                if (!wait(&w.k_empty[st], turn(n) ^ 1)) { good = false; break; }
+                if (elect_lane()) {
+                    mbar_arrive_expect_tx(&w.k_full[st], kStage + 32);
+                    bulk_g2s_at(key_stage(n), pl.images + at * kStage, kStage, &w.k_full[st]);
+                    bulk_g2s_at(smem_u32(w.absent[n & 7]), pl.meta + at * 8, 32, &w.k_full[st]);
+                }
+                __syncwarp();
+                n++;
             }
-            __syncwarp();
-        }
         // The last copies (after an abort they may have no reader) must have landed before the CTA goes.
         for (int back = 1; back <= kStages && back <= n; back++)
             for (uint32_t i = 0; i < kWaitLimit && !mbar_try_wait(&w.k_full[(n - back) % kStages], turn(n - back)); i++) __nanosleep(40);
     }
-    __device__ __forceinline__ void produce(int warp) {
-        constexpr int TOK = 16, kPass = TOK / B::kTok;              // tokens of a warp, and passes over them
-        using Pages = typename B::Pages;
-        const int lane = threadIdx.x & 31, c = lane % B::kPer, tok0 = TOK * warp + lane / B::kPer;
+    // Sixteen tokens a warp, kPer lanes to a token.
+    struct Pages { int page, t0; };
+    __device__ __forceinline__ Pages pages_of(int j, int warp) const {
+        Pages g = {-1, 0};
+        if (j >= it.end) return g;
+        g.t0 = it.range.tile(j) * kRowTile;
+        const int t = g.t0 + 16 * warp;
+        if (t >= it.kv) return g;
+        const int pg = p.b.block_table[(long long)it.seq * p.b.table_stride + div_page(p.c, t)];
+        if (pg >= 0 && pg < p.c.n_pages) g.page = pg;
+        return g;
+    }
+    // Address of the thread's token (quantised: its page, and its row in *row); live: some row sees it and it has a page.
+    __device__ __forceinline__ long long token_at(const Pages& g, int tok, uint32_t* row, bool* live) const {
+        const int t = g.t0 + tok, slot = t - div_page(p.c, t) * p.c.P;
+        *live = g.page >= 0 && any_sees(t);
+        *row = (uint32_t)slot * p.c.H + it.head;
+        if (!*live) return 0;
+        return (long long)g.page * p.c.stride_page + (kPool ? (long long)slot * p.c.stride_token + (long long)it.head * p.c.stride_head : 0ll);
+    }
+    // Notes the warp's tokens that some row sees but that have no page.
+    __device__ __forceinline__ void note(const Pages& g, int warp, int n) {
+        const int lane = threadIdx.x & 31;
+        const uint32_t gone = __ballot_sync(0xFFFFFFFFu, lane < 16 && g.page < 0 && any_sees(g.t0 + 16 * warp + lane));
+        if (gone >> lane & 1u && really_seen(g.t0 + 16 * warp + lane)) latch(p.status);
+        if (lane == 0) reinterpret_cast<uint16_t*>(w.absent[n & 7])[warp] = (uint16_t)gone;
+    }
+    __device__ __forceinline__ void load_keys(const Pages& g, int tok, int c, uint32_t (&code)[8], uint32_t& scale) const {
+        uint32_t row;
+        bool live;
+        const uint8_t* pg = p.c.base + token_at(g, tok, &row, &live);
+#pragma unroll
+        for (int i = 0; i < 8; i++) code[i] = 0;
+        scale = 0;
+        if (!live) return;
+        const uint8_t* codes = pg + row * (KF == FMT_INT8 ? D : D / 2) + c * (KF == FMT_INT8 ? 32 : 16);
+        const uint4 a = *reinterpret_cast<const uint4*>(codes);
+        code[0] = a.x; code[1] = a.y; code[2] = a.z; code[3] = a.w;
+        if (KF == FMT_INT8) {
+            const uint4 b = *reinterpret_cast<const uint4*>(codes + 16);
+            code[4] = b.x; code[5] = b.y; code[6] = b.z; code[7] = b.w;
+        }
+        scale = *reinterpret_cast<const uint16_t*>(pg + (row * (D / p.c.G) + c * 32 / p.c.G) * 2 + p.c.k_scales);
+    }
+    __device__ __forceinline__ void produce(B& b, int warp) {
+        constexpr int kPass = 16 / kTok;                            // tokens of a thread
+        const int lane = threadIdx.x & 31, c = lane % kPer, tok0 = 16 * warp + lane / kPer;
         uint32_t m0, m1;
         asm volatile("mov.b32 %0, 0x64086408;" : "=r"(m0));
         asm volatile("mov.b32 %0, 0x64806480;" : "=r"(m1));
-        const int begin = this->begin, end = this->end;
-        if (begin >= end) return;
-        auto pages_of = [&](int j) { return Pages{this->page_of(j, TOK * warp), j < end ? this->range.tile(j) * kRowTile : 0}; };
-        auto note = [&](const Pages& g, int n) {                    // tokens that some row sees but that have no page
-            const uint32_t gone = this->template missing<TOK>(g, warp);
-            if (lane == 0) reinterpret_cast<uint16_t*>(w.absent[n & 7])[warp] = (uint16_t)gone;
-        };
-        Pages now = pages_of(begin), next = pages_of(begin + 1);
-        if constexpr (KF == FMT_BF16) {
-            int n = 0;
+        int n = 0, told = 0;                                        // steps, and those that have been reported
+        for (int k = 0; next(k); k++) {
+            Pages now = pages_of(it.begin, warp), after = pages_of(it.begin + 1, warp);
+            uint32_t code[kPool ? 1 : kPass][8], scale[kPool ? 1 : kPass];
+            if constexpr (!kPool)
+#pragma unroll
+                for (int i = 0; i < kPass; i++) load_keys(now, tok0 + i * kTok, c, code[i], scale[i]);
 #pragma unroll 1
-            for (int j = begin; j < end; j++, n++) {
-                if (!this->wait_warp(&w.k_empty[n % kStages], turn(n) ^ 1)) return;
-                note(now, n);
+            for (int j = it.begin; j < it.end; j++, n++) {
+                if (!wait(&w.k_empty[n % kStages], turn(n) ^ 1)) return;
+                note(now, warp, n);
+                if constexpr (kPool) {
 #pragma unroll
-                for (int i = 0; i < kPass; i++) {
-                    uint32_t row;
-                    bool live;
-                    const uint16_t* x = this->p.c.k + this->template token_at<TOK>(now, tok0 + i * B::kTok, &row, &live) + 8 * c;
+                    for (int i = 0; i < kPass; i++) {
+                        uint32_t row;
+                        bool live;
+                        const uint16_t* x = p.c.k + token_at(now, tok0 + i * kTok, &row, &live) + 8 * c;
 #pragma unroll
-                    for (int q = 0; q < 4; q++)                     // chunks kPer apart: a row's lanes read a contiguous run
-                        cp16(key_stage(n) + swizzled(tok0 + i * B::kTok, q * B::kPer + c), live ? x + 8 * q * B::kPer : this->p.c.k, live);
-                }
-                cp_commit();
-                if (n >= 2) {
-                    cp_wait<2>();
+                        for (int q = 0; q < 4; q++)                 // chunks kPer apart: a row's lanes read a contiguous run
+                            cp16(key_stage(n) + swizzled(tok0 + i * kTok, q * kPer + c), live ? x + 8 * q * kPer : p.c.k, live);
+                    }
+                    cp_commit();
+                    if (told <= n - 2) {                            // two steps behind
+                        cp_wait<2>();
+                        fence_async_smem();
+                        mbar_arrive(&w.k_full[told++ % kStages]);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kPass; i++) {
+                        b.template store_operands<KF, true>(key_stage(n), tok0 + i * kTok, c, code[i], scale[i], m0, m1);
+                        load_keys(after, tok0 + i * kTok, c, code[i], scale[i]);
+                    }
                     fence_async_smem();
-                    mbar_arrive(&w.k_full[(n - 2) % kStages]);
+                    mbar_arrive(&w.k_full[n % kStages]);
                 }
-                now = next;
-                next = pages_of(j + 2);
+                now = after;
+                after = pages_of(j + 2, warp);
             }
-            cp_wait<0>();
-            fence_async_smem();
-            if (n >= 2) mbar_arrive(&w.k_full[(n - 2) % kStages]);
-            mbar_arrive(&w.k_full[(n - 1) % kStages]);
-        } else {
-            uint32_t code[kPass][8], scale[kPass];
-#pragma unroll
-            for (int i = 0; i < kPass; i++) this->template load_piece<KF, TOK>(now, tok0 + i * B::kTok, c, false, code[i], scale[i]);
-            int n = 0;
-#pragma unroll 1
-            for (int j = begin; j < end; j++, n++) {
-                if (!this->wait_warp(&w.k_empty[n % kStages], turn(n) ^ 1)) return;
-                note(now, n);
-#pragma unroll
-                for (int i = 0; i < kPass; i++) {
-                    this->template store_operands<KF, true>(key_stage(n), tok0 + i * B::kTok, c, code[i], scale[i], m0, m1);
-                    this->template load_piece<KF, TOK>(next, tok0 + i * B::kTok, c, false, code[i], scale[i]);
-                }
+            if constexpr (kPool) {                                  // the next item may be long in coming
+                cp_wait<0>();
                 fence_async_smem();
-                mbar_arrive(&w.k_full[n % kStages]);
-                now = next;
-                next = pages_of(j + 2);
+                while (told < n) mbar_arrive(&w.k_full[told++ % kStages]);
             }
         }
     }
 
     // ---- the warp that issues the products.  Step j of tile i goes to pair i, or with one tile to pair j & 1.
-    __device__ __forceinline__ void issue(int tiles, uint32_t tmem) {
+    __device__ __forceinline__ void issue(uint32_t tmem) {
         constexpr uint32_t kDesc = instr_desc(KF == FMT_BF16, false, kRowTile), kMat16 = S::kMat >> 4;
-        const uint64_t q_desc = smem_desc(this->smem + S::kQ, 16), k_desc = smem_desc(this->smem + S::kK, 16);
-        for (int i = 0; i < tiles; i++) if (!this->wait_warp(&w.r.q_ready[i], 0)) return;
-        const int n = this->end - this->begin;
-#pragma unroll 1
-        for (int j = 0; j < n; j++) {
-            const int st = j % kStages;
-            if (!this->wait_warp(&w.k_full[st], turn(j))) return;
-#pragma unroll 1
-            for (int i = 0; i < tiles; i++) {
-                const int pair = ONE ? j & 1 : i, u = ONE ? j >> 1 : j;
-                if (!this->wait_warp(&w.s_empty[pair][u & 1], ((u >> 1) & 1) ^ 1)) return;
-                tc_after();
-                const uint64_t q = q_desc + i * kMat16, k = k_desc + st * (kStage >> 4);
-                const uint32_t d = tmem + (2 * pair + (u & 1)) * kRowTile;
-                if (elect_lane()) {
-#pragma unroll
-                    for (int x = 0; x < D / 16; x++) {              // 16 channels: 32 bytes inside a 128-byte row, then the next half
-                        const uint32_t o = (x >> 2) * (kRowTile * 8) + (x & 3) * 2;
-                        tc_mma_ss(d, COLUMNS ? k + o : q + o, COLUMNS ? q + o : k + o, kDesc, x != 0);
-                        if (FINE) tc_mma_ss(d, COLUMNS ? k + o + kMat16 : q + o, COLUMNS ? q + o : k + o + kMat16, kDesc, true);
-                    }
-                    tc_commit(&w.s_full[pair][u & 1]);
-                    if (i == tiles - 1) tc_commit(&w.k_empty[st]);
-                }
-                __syncwarp();
+        const uint64_t q_desc = smem_desc(smem + S::kQ, 16), k_desc = smem_desc(smem + S::kK, 16);
+        int g = 0, units[2] = {0, 0}, uses[2] = {0, 0};             // steps; units of the pairs; items of the tiles' queries
+        for (int k = 0; next(k); k++) {
+            for (int i = 0; i < it.tiles; i++) {
+                if (!wait(&w.q_ready[i], uses[i] & 1)) return;
+                uses[i]++;
             }
+            const int n = steps();
+#pragma unroll 1
+            for (int j = 0; j < n; j++, g++) {
+                const int st = g % kStages;
+                if (!wait(&w.k_full[st], turn(g))) return;
+#pragma unroll 1
+                for (int i = 0; i < it.tiles; i++) {
+                    const int pair = ONE ? j & 1 : i, u = pair ? units[1]++ : units[0]++;
+                    if (!wait(&w.s_empty[pair][u & 1], ((u >> 1) & 1) ^ 1)) return;
+                    tc_after();
+                    const uint64_t q = q_desc + i * kMat16, key = k_desc + st * (kStage >> 4);
+                    const uint32_t d = tmem + (2 * pair + (u & 1)) * kRowTile;
+                    if (elect_lane()) {
+#pragma unroll
+                        for (int x = 0; x < D / 16; x++) {          // 16 channels: 32 bytes inside a 128-byte row, then the next half
+                            const uint32_t o = (x >> 2) * (kRowTile * 8) + (x & 3) * 2;
+                            tc_mma_ss(d, COLUMNS ? key + o : q + o, COLUMNS ? q + o : key + o, kDesc, x != 0);
+                            if (FINE) tc_mma_ss(d, COLUMNS ? key + o + kMat16 : q + o, COLUMNS ? q + o : key + o + kMat16, kDesc, true);
+                        }
+                        tc_commit(&w.s_full[pair][u & 1]);
+                        if (i == it.tiles - 1) tc_commit(&w.k_empty[st]);
+                    }
+                    __syncwarp();
+                }
+            }
+            if (elect_lane()) tc_commit(&w.q_free);
+            __syncwarp();
         }
     }
 
     // ---- the warpgroups: pair wg >> 1, columns 64 (wg & 1) .. + 63 of a place
-    static constexpr int kOnFma = 5;                                // of 16 pairs of exponentials, those that are computed (0 .. 16)
+    static constexpr int kOnFma = 2;                                // of 16 pairs of exponentials, those that are computed (0 .. 16)
     __device__ __forceinline__ static void exp2_both(int c, f32x2 y, float& a, float& b) {
         if (c * kOnFma % 16 < kOnFma) {
             weigh_exp2_pair(y, a, b);
@@ -232,117 +367,165 @@ struct WeighRows : RowsKernel<KF, KF, D, IMAGE, KF != FMT_BF16> {
             total[c & 1] = add2(total[c & 1], pack2(a, b));
         }
     }
-    // Queries into shared memory, their factors and positions: a tile by the first warpgroup of a pair.
-    __device__ __forceinline__ void queries(int wg, int tiles, int first, int m0, int m_end) {
-        const int i = wg >> 1, r = threadIdx.x & 127;
-        if (!(wg & 1) && i < tiles) {
-            const int m = m0 + 128 * i + r;
-            const bool live = m < m_end;
-            const int row = live ? first + m / this->p.share : first, hq = live ? this->head * this->p.share + m % this->p.share : 0;
-            w.pos[128 * i + r] = live ? max(-1, row_position(this->p.b, this->seq, row)) : -1;
-            w.factor[128 * i + r] = this->load_query(i, r, live, row, hq);
-            fence_async_smem();
-            __syncwarp();
-            if ((threadIdx.x & 31) == 0) mbar_arrive(&w.r.q_ready[i]);
-        }
-        sync_consumers();
+    __device__ __forceinline__ long long vector_index(int m) const {
+        return (long long)(it.first + m / p.share) * p.Hq + it.head * p.share + m % p.share;
     }
     __device__ __forceinline__ void release(int pair, int u) {
         tc_before();
-        __syncwarp();
-        if ((threadIdx.x & 31) == 0) mbar_arrive(&w.s_empty[pair][u & 1]);
+        arrive(&w.s_empty[pair][u & 1]);
     }
-    __device__ __forceinline__ long long vector_index(int first, int m) const {
-        return (long long)(first + m / this->p.share) * this->p.Hq + this->head * this->p.share + m % this->p.share;
+    // Queries into shared memory, their factors and positions: a tile by the first warpgroup of a pair; the others wait for them.
+    // `k` items have been before, `uses` of them with this tile.
+    __device__ __forceinline__ bool queries(B& b, int wg, int i, int k, int uses) {
+        const int r = threadIdx.x & 127;
+        if (wg == 2 * i) {
+            if (k > 0 && !wait(&w.q_free, (k - 1) & 1)) return false;
+            const int m = it.m0 + 128 * i + r;
+            const bool live = m < it.m_end;
+            const int row = live ? it.first + m / p.share : it.first, hq = live ? it.head * p.share + m % p.share : 0;
+            w.pos[128 * i + r] = live ? max(-1, row_position(p.b, it.seq, row)) : -1;
+            float factor = b.load_query(i, r, live, row, hq);
+            w.factor[128 * i + r] = factor;
+            if (COLUMNS) {
+                // -log2 of the row's sum; minus infinity for a row that sees nothing and for vectors behind the last
+                float low = -INFINITY;
+                if (live) {
+                    const long long vec = vector_index(m), step = (long long)p.b.n_rows * p.Hq;
+                    float top = kNoMax, sum = 0.0f;
+#pragma unroll 8
+                    for (int q = 0; q < pl.splits; q++) top = fmaxf(top, pl.sums[q * step + vec].x);
+#pragma unroll 8
+                    for (int q = 0; q < pl.splits; q++) {
+                        const float2 z = pl.sums[q * step + vec];
+                        sum = fmaf(z.y, fast_exp2(z.x - top), sum);
+                    }
+                    if (sum != 0.0f) low = -(top + log2f(sum));
+                }
+                if (!live) factor = 0.0f;
+                if (factor != factor) factor = 1.0f;
+                float* v = reinterpret_cast<float*>(&w.column[64 * i + (r >> 1)]) + (r & 1);
+                v[0] = factor;
+                v[2] = low;
+            }
+            fence_async_smem();
+            arrive(&w.q_ready[i]);
+        }
+        return wait(&w.q_ready[i], uses & 1);
     }
 
     // First pass: a thread per query vector.
-    __device__ __forceinline__ void rows(int wg, int tiles, int first, int m0, int m_end, uint32_t tmem, const WeighRowsPlan& pl, int split) {
-        queries(wg, tiles, first, m0, m_end);
-        const int pair = wg >> 1, half = wg & 1;
-        if (!ONE && pair >= tiles) return;
-        const int r = threadIdx.x & 127, i = ONE ? 0 : pair, m = m0 + 128 * i + r, pos = w.pos[128 * i + r], kv = this->kv;
-        float factor = w.factor[128 * i + r];
-        const bool broken = factor != factor;
-        if (broken) factor = 1.0f;
-        if (factor == 0.0f) factor = 1.17549435e-38f;               // a mask is minus infinity over the factor
+    __device__ __forceinline__ void rows(B& b, int wg, uint32_t tmem) {
+        const int pair = wg >> 1, half = wg & 1, i = ONE ? 0 : pair, r = threadIdx.x & 127;
+        const bool leader = ONE ? wg == 0 : half == 0;              // puts the sums of a vector together
         const uint32_t at = tmem + ((uint32_t)((threadIdx.x >> 5) & 3) << 21) + 64 * half;
-        float ref = kNoMax;
-        f32x2 sum2[2] = {pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)};
-        const f32x2 factor2 = pack2(factor, factor);
-        const int n = this->end - this->begin;
+        int g = 0, u = 0, uses = 0;
+        for (int k = 0; next(k); k++) {
+            const int n = steps();
+            if (i >= it.tiles) { g += n; continue; }
+            if (!queries(b, wg, i, k, uses)) return;
+            const int m = it.m0 + 128 * i + r, pos = w.pos[128 * i + r], kv = it.kv;
+            float factor = w.factor[128 * i + r];
+            const bool broken = factor != factor;
+            if (broken) factor = 1.0f;
+            if (factor == 0.0f) factor = 1.17549435e-38f;           // a mask is minus infinity over the factor
+            float ref = kNoMax;
+            f32x2 sum2[2] = {pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)};
+            const f32x2 factor2 = pack2(factor, factor);
+            bool start = true;
 #pragma unroll 1
-        for (int u = 0, j = ONE ? pair : 0; j < n; u++, j += ONE ? 2 : 1) {
-            const int t0 = this->range.tile(this->begin + j) * kRowTile;
-            const uint32_t s_at = at + (2 * pair + (u & 1)) * kRowTile;
-            if (!this->wait_warp(&w.s_full[pair][u & 1], (u >> 1) & 1)) return;
-            tc_after();
-            const uint4 absent = lds128(smem_u32(w.absent[j & 7]));
-            const bool gaps = (absent.x | absent.y | absent.z | absent.w) != 0;
-            if (gaps || !this->whole(t0)) {                         // what a row does not see becomes minus infinity, in TMEM
-                if (IMAGE && gaps && !half) this->latch_absent(t0, absent);
-                const int c0 = 64 * half, b = min(pos, kv - 1) - t0, a = this->p.window > 0 ? max(pos - this->p.window + 1, 0) - t0 : -t0, s = this->p.sinks - t0;
-                const uint32_t none = factor < 0.0f ? 0x7F800000u : 0xFF800000u;
+            for (int j = ONE ? pair : 0; j < n; u++, j += ONE ? 2 : 1) {
+                const int t0 = it.range.tile(it.begin + j) * kRowTile;
+                const uint32_t s_at = at + (2 * pair + (u & 1)) * kRowTile;
+                if (!wait(&w.s_full[pair][u & 1], (u >> 1) & 1)) return;
+                tc_after();
+                const uint4 absent = lds128(smem_u32(w.absent[(g + j) & 7]));
+                const bool gaps = (absent.x | absent.y | absent.z | absent.w) != 0;
+                if (gaps || !whole(t0)) {                           // what a row does not see becomes minus infinity, in TMEM
+                    if (IMAGE && gaps && !half) latch_absent(t0, absent);
+                    const int x0 = 64 * half, hi = min(pos, kv - 1) - t0, lo = p.window > 0 ? max(pos - p.window + 1, 0) - t0 : -t0, s = p.sinks - t0;
+                    const uint32_t none = factor < 0.0f ? 0x7F800000u : 0xFF800000u;
 #pragma unroll 1
-                for (int k = 0; k < 4; k++) {
-                    const uint32_t gone = (half ? (k < 2 ? absent.z : absent.w) : (k < 2 ? absent.x : absent.y)) >> (16 * (k & 1));
-                    const uint32_t in = B::seen(c0 + 16 * k, a, b, s, gone);
-                    uint32_t x[16];
-                    tc_ld16(x, s_at + 16 * k);
-                    tc_wait_ld();
-#pragma unroll
-                    for (int c = 0; c < 16; c++) x[c] = in >> c & 1u ? x[c] : none;
-                    tc_st16(s_at + 16 * k, x);
-                }
-                tc_wait_st();
-            }
-            // Against the reference as it stands, a row's largest logit in the first step it had tokens in; where the sum shows that it has become
-            // too small (fp32 has room for logits 60 above it) the largest is looked for again and the step done once more.
-            f32x2 total[2];
-            bool search = u == 0;
-            for (;;) {
-                if (search) {
-                    float y = -INFINITY;
-#pragma unroll 1
-                    for (int k = 0; k < 4; k++) {
+                    for (int q = 0; q < 4; q++) {
+                        const uint32_t gone = (half ? (q < 2 ? absent.z : absent.w) : (q < 2 ? absent.x : absent.y)) >> (16 * (q & 1));
+                        const uint32_t in = B::seen(x0 + 16 * q, lo, hi, s, gone);
                         uint32_t x[16];
-                        tc_ld16(x, s_at + 16 * k);
+                        tc_ld16(x, s_at + 16 * q);
                         tc_wait_ld();
 #pragma unroll
-                        for (int c = 0; c < 16; c++) y = fmaxf(y, __uint_as_float(x[c]) * factor);
+                        for (int c = 0; c < 16; c++) x[c] = in >> c & 1u ? x[c] : none;
+                        tc_st16(s_at + 16 * q, x);
                     }
-                    const float to = fmaxf(y, ref), keep = fast_exp2(ref - to);
-                    ref = to;
-                    sum2[0] = mul2(sum2[0], pack2(keep, keep));
-                    sum2[1] = mul2(sum2[1], pack2(keep, keep));
+                    tc_wait_st();
                 }
-                const f32x2 ref2 = pack2(-ref, -ref);
-                total[0] = sum2[0];
-                total[1] = sum2[1];
+                // Against the reference as it stands, a row's largest logit in the first step it had tokens in; where the sum shows that it has
+                // become too small (fp32 has room for logits 60 above it) the largest is looked for again and the step done once more.
+                f32x2 total[2];
+                bool search = start;
+                start = false;
+                for (;;) {
+                    if (search) {
+                        float y = -INFINITY;
+#pragma unroll 1
+                        for (int q = 0; q < 4; q++) {
+                            uint32_t x[16];
+                            tc_ld16(x, s_at + 16 * q);
+                            tc_wait_ld();
 #pragma unroll
-                for (int k = 0; k < 2; k++) {
-                    float x[32];
-                    tc_ld32(x, s_at + 32 * k);
-                    tc_wait_ld();
-                    add_row(x, factor2, ref2, total);
+                            for (int c = 0; c < 16; c++) y = fmaxf(y, __uint_as_float(x[c]) * factor);
+                        }
+                        const float to = fmaxf(y, ref), keep = fast_exp2(ref - to);
+                        ref = to;
+                        sum2[0] = mul2(sum2[0], pack2(keep, keep));
+                        sum2[1] = mul2(sum2[1], pack2(keep, keep));
+                    }
+                    const f32x2 ref2 = pack2(-ref, -ref);
+                    total[0] = sum2[0];
+                    total[1] = sum2[1];
+#pragma unroll
+                    for (int q = 0; q < 2; q++) {
+                        float x[32];
+                        tc_ld32(x, s_at + 32 * q);
+                        tc_wait_ld();
+                        add_row(x, factor2, ref2, total);
+                    }
+                    if (search) break;
+                    float a, c;
+                    unpack2(add2(total[0], total[1]), a, c);
+                    search = __any_sync(0xFFFFFFFFu, a + c > 1.0e18f);
+                    if (!search) break;
                 }
-                if (search) break;
-                float a, b;
-                unpack2(add2(total[0], total[1]), a, b);
-                search = __any_sync(0xFFFFFFFFu, a + b > 1.0e18f);
-                if (!search) break;
+                sum2[0] = total[0];
+                sum2[1] = total[1];
+                release(pair, u);
             }
-            sum2[0] = total[0];
-            sum2[1] = total[1];
-            release(pair, u);
+            g += n;
+            float sum, odd;
+            unpack2(add2(sum2[0], sum2[1]), sum, odd);
+            sum += odd;
+            if (broken && sum != 0.0f) sum = __uint_as_float(0x7FC00000u);
+            if (!leader) {
+                w.sums[wg][r] = make_float2(ref, sum);
+                arrive(&w.mate_done[ONE ? 0 : pair]);
+            } else {
+                if (!wait(&w.mate_done[ONE ? 0 : pair], uses & 1)) return;
+                for (int q = wg + 1; q < (ONE ? 4 : wg + 2); q++) {
+                    const float2 z = w.sums[q][r];
+                    const float to = fmaxf(ref, z.x);
+                    sum = fmaf(sum, fast_exp2(ref - to), z.y * fast_exp2(z.x - to));
+                    ref = to;
+                }
+                if (m < it.m_end) pl.sums[(long long)it.split * p.b.n_rows * p.Hq + vector_index(m)] = make_float2(ref, sum);
+            }
+            uses++;
         }
-        if (m >= m_end) return;
-        float a, b;
-        unpack2(add2(sum2[0], sum2[1]), a, b);
-        a += b;
-        if (broken && a != 0.0f) a = __uint_as_float(0x7FC00000u);
-        const int slot = ONE ? 4 * split + wg : 2 * split + half;
-        pl.sums[(long long)slot * this->p.b.n_rows * this->p.Hq + vector_index(first, m)] = make_float2(ref, a);
+    }
+    // Tokens on pages out of range count when some row sees them (with images nobody has looked at that yet).
+    __device__ __forceinline__ void latch_absent(int t0, const uint4& absent) const {
+        const int lane = threadIdx.x & 31;
+        const uint32_t gone[4] = {absent.x, absent.y, absent.z, absent.w};
+#pragma unroll
+        for (int q = 0; q < 4; q++)
+            if (gone[q] >> lane & 1u && really_seen(t0 + 32 * q + lane)) latch(p.status);
     }
 
     // Second pass: a thread per token, the vectors of a tile along its lane; `in`: the vectors that see it, where not all do.
@@ -364,101 +547,92 @@ struct WeighRows : RowsKernel<KF, KF, D, IMAGE, KF != FMT_BF16> {
     __device__ __forceinline__ float column_sum(uint32_t s_at, int first, unsigned long long in) const {
         f32x2 total[2] = {pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)};
 #pragma unroll
-        for (int k = 0; k < 2; k++) {
+        for (int q = 0; q < 2; q++) {
             float x[32];
-            tc_ld32(x, s_at + 32 * k);
+            tc_ld32(x, s_at + 32 * q);
             tc_wait_ld();
-            add_column<MASK>(x, w.column + first / 2 + 16 * k, (uint32_t)(in >> (32 * k)), total);
+            add_column<MASK>(x, w.column + first / 2 + 16 * q, (uint32_t)(in >> (32 * q)), total);
         }
         float a, b;
         unpack2(add2(total[0], total[1]), a, b);
         return a + b;
     }
-    // Which of 64 vectors from number `first` of the CTA see token t.  A row's vectors lie together.
-    __device__ __forceinline__ unsigned long long seeing(int first, int m0, int t) const {
+    // Which of 64 vectors from number `first` of the item see token t.  A row's vectors lie together.
+    __device__ __forceinline__ unsigned long long seeing(int first, int t) const {
         unsigned long long in = 0;
-        const int share = this->p.share;
-        int left = share - (m0 + first) % share;                    // of the row's vectors, from this one on
+        const int share = p.share;
+        int left = share - (it.m0 + first) % share;                 // of the row's vectors, from this one on
 #pragma unroll 1
         for (int c = 0; c < 64; c += left, left = share) {
             const int pos = w.pos[first + c];
-            if (t <= pos && sees(this->p, pos, t)) in |= (left < 64 ? (1ull << left) - 1ull : ~0ull) << c;
+            if (t <= pos && sees(p, pos, t)) in |= (left < 64 ? (1ull << left) - 1ull : ~0ull) << c;
         }
         return in;
     }
-    __device__ __forceinline__ void columns(int wg, int tiles, int first, int m0, int m_end, uint32_t tmem, const WeighRowsPlan& pl, int tile) {
-        const int pair = wg >> 1, half = wg & 1, r = threadIdx.x & 127, i = ONE ? 0 : pair, kv = this->kv;
-        // -log2 of the rows' sums; minus infinity for a row that sees nothing and for vectors behind the last
-        float low = -INFINITY;
-        const int m = m0 + 128 * pair + r;
-        if (!half && pair < tiles && m < m_end) {
-            const long long vec = vector_index(first, m), step = (long long)this->p.b.n_rows * this->p.Hq;
-            float top = kNoMax, sum = 0.0f;
-            for (int k = 0; k < pl.slots; k++) top = fmaxf(top, pl.sums[k * step + vec].x);
-            for (int k = 0; k < pl.slots; k++) {
-                const float2 z = pl.sums[k * step + vec];
-                sum = fmaf(z.y, fast_exp2(z.x - top), sum);
-            }
-            if (sum != 0.0f) low = -(top + log2f(sum));
-        }
-        queries(wg, tiles, first, m0, m_end);
-        if (!half && pair < tiles) {
-            float factor = w.factor[128 * pair + r];
-            if (!(m < m_end)) factor = 0.0f;
-            if (factor != factor) factor = 1.0f;
-            float* v = reinterpret_cast<float*>(&w.column[64 * pair + (r >> 1)]) + (r & 1);
-            v[0] = factor;
-            v[2] = low;
-        }
-        sync_consumers();
-        if (!ONE && pair >= tiles) return;
-        const uint32_t at = tmem + ((uint32_t)((threadIdx.x >> 5) & 3) << 21) + 64 * half;
-        const int n = this->end - this->begin;
+    __device__ __forceinline__ void columns(B& b, int wg, uint32_t tmem) {
+        const int pair = wg >> 1, half = wg & 1, i = ONE ? 0 : pair, r = threadIdx.x & 127, from = 128 * i + 64 * half;
         const bool leader = ONE ? half == 0 : wg == 0;              // adds up the other warpgroups' sums of a step, one step later
-        float* out = pl.partial + (((long long)this->seq * this->p.c.H + this->head) * pl.chunk_tiles + tile) * pl.tokens + (long long)this->begin * kRowTile + r;
-        float sum = 0.0f;
-        int u = 0, before = -1;                                     // step whose sum the leader still has
-        auto finish = [&]() {
-            const int v = u - 1;
-            if (!this->wait_warp(&w.part_full[ONE ? pair : 0][v & 3], (v >> 2) & 1)) return false;
-            if (ONE) sum += w.part[v & 3][2 * pair][r];
-            else for (int k = 0; k < 2 * tiles - 1; k++) sum += w.part[v & 3][k][r];
-            out[(long long)before * kRowTile] = sum;
-            return true;
-        };
+        const uint32_t at = tmem + ((uint32_t)((threadIdx.x >> 5) & 3) << 21) + 64 * half;
+        int g = 0, u = 0, uses = 0;
+        for (int k = 0; next(k); k++) {
+            const int n = steps();
+            if (i >= it.tiles) { g += n; continue; }
+            if (!queries(b, wg, i, k, uses)) return;
+            const int kv = it.kv;
+            float* out = pl.partial + (((long long)it.seq * p.c.H + it.head) * pl.chunk_tiles + it.tile) * pl.tokens + (long long)it.begin * kRowTile + r;
+            float sum = 0.0f;
+            int before = -1;                                        // step whose sum the leader still has: unit u - 1
+            auto finish = [&]() {
+                const int v = u - 1;
+                for (int q = wg + 1; q < (ONE ? wg + 2 : 2 * it.tiles); q++) {
+                    // (pair 1 has had its own number of units: one for each step of the items with two tiles)
+                    const int x = q < 2 || ONE ? v : u2 - 1;
+                    if (!wait(&w.part_full[q][x & 3], (x >> 2) & 1)) return false;
+                    sum += w.part[x & 3][q][r];
+                }
+                out[(long long)before * kRowTile] = sum;
+                return true;
+            };
 #pragma unroll 1
-        for (int j = ONE ? pair : 0; j < n; u++, j += ONE ? 2 : 1) {
-            const int t0 = this->range.tile(this->begin + j) * kRowTile, t = t0 + r;
-            const uint32_t s_at = at + (2 * pair + (u & 1)) * kRowTile;
-            if (leader && u && !finish()) return;
-            if (!this->wait_warp(&w.s_full[pair][u & 1], (u >> 1) & 1)) return;
-            tc_after();
-            const uint4 absent = lds128(smem_u32(w.absent[j & 7]));
-            const bool gaps = (absent.x | absent.y | absent.z | absent.w) != 0;
-            if (gaps || !this->whole(t0)) {
-                const uint32_t word = r < 32 ? absent.x : r < 64 ? absent.y : r < 96 ? absent.z : absent.w;
-                const bool there = t < kv && !(word >> (r & 31) & 1u);
-                sum = column_sum<true>(s_at, 128 * i + 64 * half, there ? seeing(128 * i + 64 * half, m0, t) : 0ull);
-            } else {
-                sum = column_sum<false>(s_at, 128 * i + 64 * half, 0ull);
+            for (int j = ONE ? pair : 0; j < n; u++, j += ONE ? 2 : 1) {
+                const int t0 = it.range.tile(it.begin + j) * kRowTile, t = t0 + r;
+                const uint32_t s_at = at + (2 * pair + (u & 1)) * kRowTile;
+                if (leader && before >= 0 && !finish()) return;
+                if (it.tiles == 2) u2++;
+                if (!wait(&w.s_full[pair][u & 1], (u >> 1) & 1)) return;
+                tc_after();
+                const uint4 absent = lds128(smem_u32(w.absent[(g + j) & 7]));
+                const bool gaps = (absent.x | absent.y | absent.z | absent.w) != 0;
+                if (gaps || !whole(t0)) {
+                    const uint32_t word = r < 32 ? absent.x : r < 64 ? absent.y : r < 96 ? absent.z : absent.w;
+                    const bool there = t < kv && !(word >> (r & 31) & 1u);
+                    sum = column_sum<true>(s_at, from, there ? seeing(from, t) : 0ull);
+                } else {
+                    sum = column_sum<false>(s_at, from, 0ull);
+                }
+                release(pair, u);
+                if (leader) {
+                    before = j;
+                } else {
+                    w.part[u & 3][wg][r] = sum;
+                    arrive(&w.part_full[wg][u & 3]);
+                }
             }
-            release(pair, u);
-            if (leader) {
-                before = j;
-            } else {
-                w.part[u & 3][ONE ? 2 * pair : wg - 1][r] = sum;
-                __syncwarp();
-                if ((threadIdx.x & 31) == 0) mbar_arrive(&w.part_full[ONE ? pair : 0][u & 3]);
-            }
+            g += n;
+            if (leader && before >= 0 && !finish()) return;
+            // The first warpgroup of a pair writes the next item's numbers over this one's.
+            if (wg != 2 * i) arrive(&w.mate_done[ONE ? 0 : pair]);
+            else if (!wait(&w.mate_done[ONE ? 0 : pair], uses & 1)) return;
+            uses++;
         }
-        if (leader && u) finish();
     }
+    int u2 = 0;                                                     // second pass: units of pair 1, as the leader counts them
 };
 
 template <int KF, int D, bool IMAGE, bool ONE, bool COLUMNS>
 __global__ void __launch_bounds__(weigh_threads(IMAGE), 1) weigh_rows_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ WeighRowsPlan pl) {
     using K = WeighRows<KF, D, IMAGE, ONE, COLUMNS>;
-    constexpr int kIssuer = weigh_issuer(IMAGE), kThreads = weigh_threads(IMAGE);
+    constexpr int kIssuer = weigh_issuer(IMAGE) / 32;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     WeighBars& bars = *reinterpret_cast<WeighBars*>(raw + (base - smem_u32(raw)) + RowsSmem<D>::kBars);
@@ -466,90 +640,59 @@ __global__ void __launch_bounds__(weigh_threads(IMAGE), 1) weigh_rows_kernel(con
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0);
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; i++) {
-            mbar_init(&bars.r.q_ready[i], 4);
+            mbar_init(&bars.item_full[i], 1);
+            mbar_init(&bars.item_empty[i], weigh_threads(IMAGE) / 32 - 1);      // all warps but the one that finds the items
+            mbar_init(&bars.q_ready[i], 4);
+            mbar_init(&bars.mate_done[i], ONE ? 12 : 4);
             for (int k = 0; k < 2; k++) { mbar_init(&bars.s_full[i][k], 1); mbar_init(&bars.s_empty[i][k], 8); }
         }
-        for (int i = 0; i < 4; i++) { mbar_init(&bars.k_full[i], IMAGE ? 1 : kWeighProducers); mbar_init(&bars.k_empty[i], 1); }
-        mbar_init(&bars.r.drained, 1);
-        bars.r.abort = 0; bars.r.lost = 0;
-        bars.r.lo = bars.r.least = 0x7FFFFFFF; bars.r.hi = -1;
+        for (int i = 0; i < 4; i++) {
+            mbar_init(&bars.k_full[i], IMAGE ? 1 : kWeighProducers);
+            mbar_init(&bars.k_empty[i], 1);
+            for (int k = 0; k < 4; k++) mbar_init(&bars.part_full[i][k], 4);
+        }
+        mbar_init(&bars.q_free, 1);
+        mbar_init(&bars.drained, 1);
+        bars.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    pdl_wait();
-    // Block order: the last rows (the most tokens) of all heads first.
-    int id = blockIdx.x;
-    const int split = id % pl.splits; id /= pl.splits;
-    const int head = id % p.c.H; id /= p.c.H;
-    const int seq = id % p.b.n_seqs, local = pl.chunk_tiles - 1 - id / p.b.n_seqs, tile = pl.chunk + local;
-    int first, kv, rows;
-    const bool ordered = sequence_rows(p, seq, &first, &kv, &rows);
-    if (threadIdx.x == 0 && (!ordered || rows > p.b.max_rows || p.b.kv_len[seq] > kv)) latch(p.status);
-    if (!ordered) return;
-    rows = min(rows, p.b.max_rows);
-    const int m0 = tile * 2 * kRowTile, m_end = min(rows * p.share, m0 + 2 * kRowTile);
-    if (m0 >= m_end) return;
-    const int tiles = !ONE && m_end - m0 > kRowTile ? 2 : 1;
-    if (COLUMNS && threadIdx.x == 0) {          // warps of the warpgroups that are not leaders
-        for (int i = 0; i < 2; i++) for (int k = 0; k < 4; k++) mbar_init(&bars.part_full[i][k], ONE ? 4 : 4 * (2 * tiles - 1));
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    __syncthreads();
-    {   // positions of the CTA's rows (one below 0 sees nothing: no window need reach back for it)
-        uint32_t low = 0x7FFFFFFFu;
-        int least = 0x7FFFFFFF, most = -1;
-        for (int r = m0 / p.share + threadIdx.x; r <= (m_end - 1) / p.share; r += kThreads) {
-            const int x = row_position(p.b, seq, first + r);
-            low = min(low, (uint32_t)x);
-            least = min(least, x);
-            most = max(most, x);
-        }
-        low = __reduce_min_sync(0xFFFFFFFFu, low);
-        least = __reduce_min_sync(0xFFFFFFFFu, least);
-        most = __reduce_max_sync(0xFFFFFFFFu, most);
-        if (threadIdx.x == 0) { bars.r.first_row = first + m0 / p.share; bars.r.last_row = first + (m_end - 1) / p.share; }
-        if ((threadIdx.x & 31) == 0) {
-            atomicMin(&bars.r.lo, (int)low);
-            atomicMin(&bars.r.least, least);
-            atomicMax(&bars.r.hi, most);
-        }
-    }
-    if (warp == kIssuer / 32) tc_alloc(&bars.r.tmem, 512);
+    if (warp == kIssuer) tc_alloc(&bars.tmem, 512);
     tc_before();
     __syncthreads();
     tc_after();
-    const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&bars.r.tmem);
-    K k(p, bars);
-    k.smem = base; k.seq = seq; k.head = head; k.kv = kv;
-    k.hi = bars.r.hi;
-    k.last = min(bars.r.least, kv - 1);
-    k.range = step_range(p, kv, bars.r.lo, k.hi);
-    k.begin = (int)((long long)k.range.count * split / pl.splits);
-    k.end = (int)((long long)k.range.count * (split + 1) / pl.splits);
-    if (!COLUMNS && head == 0 && split == 0 && threadIdx.x == 0) pl.ranges[(long long)seq * pl.tiles + tile] = make_int4(k.range.sink_tiles, k.range.first, k.range.count, 0);
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&bars.tmem);
+    pdl_wait();
+    K k(p, pl, bars, base);
+    // The attention's helpers that need no barriers: queries and operands.
+    RowsBars unused;
+    typename K::B b(p, unused);
+    b.smem = base;
     if (warp < kWeighConsumers / 32) {
-        if (COLUMNS) k.columns(warp >> 2, tiles, first, m0, m_end, tmem, pl, local);
-        else k.rows(warp >> 2, tiles, first, m0, m_end, tmem, pl, split);
-    } else if (warp < kIssuer / 32) {
+        if (COLUMNS) k.columns(b, warp >> 2, tmem);
+        else k.rows(b, warp >> 2, tmem);
+    } else if (warp < kIssuer) {
         if constexpr (IMAGE) {
-            k.fetch_images(pl);
+            k.fetch_images();
         } else {
-            k.produce(warp - kWeighConsumers / 32);
+            k.produce(b, warp - kWeighConsumers / 32);
             cp_wait<0>();
         }
-    } else if (k.end > k.begin) {
-        k.issue(tiles, tmem);
-        if (__any_sync(0xFFFFFFFFu, *reinterpret_cast<volatile int32_t*>(&bars.r.abort))) {    // what was issued must have ended before TMEM goes
-            if (elect_lane()) tc_commit(&bars.r.drained);
+    } else if (warp == kIssuer) {
+        k.issue(tmem);
+        if (__any_sync(0xFFFFFFFFu, *reinterpret_cast<volatile int32_t*>(&bars.abort))) {      // what was issued must have ended before TMEM goes
+            if (elect_lane()) tc_commit(&bars.drained);
             __syncwarp();
-            for (uint32_t i = 0; i < kWaitLimit && !mbar_try_wait(&bars.r.drained, 0); i++) __nanosleep(40);
+            for (uint32_t i = 0; i < kWaitLimit && !mbar_try_wait(&bars.drained, 0); i++) __nanosleep(40);
         }
+    } else {
+        k.find_items();
     }
     __syncwarp();
     tc_before();
     __syncthreads();
     tc_after();
-    if (warp == kIssuer / 32) tc_free(tmem, 512);
-    if (threadIdx.x == 0 && bars.r.abort) atomicCAS(p.status, 0, (int)PATCHKV_E_TIMEOUT);
+    if (warp == kIssuer) tc_free(tmem, 512);
+    if (threadIdx.x == 0 && bars.abort) atomicCAS(p.status, 0, (int)PATCHKV_E_TIMEOUT);
 }
 
 // Images of the two matrices of a step's keys (grid: step, KV head, sequence), as attention_image_kernel lays them out.

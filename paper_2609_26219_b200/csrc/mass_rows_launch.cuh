@@ -14,7 +14,8 @@ cudaError_t launch_weigh_rows_kernel(const AttentionParams& p, const WeighRowsPl
     static std::atomic<uint64_t> allowed{0};
     const cudaError_t e = allow_smem((const void*)kernel, WeighSmem<D>::kLaunch, &allowed);
     if (e != cudaSuccess) return e;
-    return launch_pdl(kernel, dim3((unsigned)(pl.chunk_tiles * p.c.H * p.b.n_seqs * pl.splits)), dim3(weigh_threads(IMAGE)), WeighSmem<D>::kLaunch, stream, p, pl);
+    const long long items = (long long)pl.chunk_tiles * p.c.H * p.b.n_seqs * pl.splits;
+    return launch_pdl(kernel, dim3((unsigned)std::min(items, 148ll)), dim3(weigh_threads(IMAGE)), WeighSmem<D>::kLaunch, stream, p, pl);
 }
 template <int KF, int D, bool IMAGE, bool ONE>
 cudaError_t launch_weigh_rows_passes(const AttentionParams& p, const WeightParams& m, WeighRowsPlan pl, cudaStream_t stream) {
