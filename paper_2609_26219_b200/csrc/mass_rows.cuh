@@ -62,7 +62,7 @@ struct WeighBars {
     WeighItem item[2];
     float factor[256];                                              // of the vectors' logits
     int32_t pos[256];
-    alignas(16) float4 column[128];                                 // second pass: of two vectors their factors and -log2 of their sums
+    alignas(16) float scale[256], low[256];                         // second pass: the factors again, and -log2 of the vectors' sums
     float2 sums[4][kRowTile];                                       // first pass: [warpgroup] reference and sum
     float part[4][4][kRowTile];                                     // second pass: [unit mod 4][warpgroup]
     uint32_t tmem;
@@ -401,16 +401,44 @@ struct WeighRows {
                     }
                     if (sum != 0.0f) low = -(top + log2f(sum));
                 }
-                if (!live) factor = 0.0f;
-                if (factor != factor) factor = 1.0f;
-                float* v = reinterpret_cast<float*>(&w.column[64 * i + (r >> 1)]) + (r & 1);
-                v[0] = factor;
-                v[2] = low;
+                if (factor != factor) factor = p.scale_log2;        // (of zeros)
+                w.scale[128 * i + r] = live ? factor : 0.0f;
+                w.low[128 * i + r] = low;
             }
             fence_async_smem();
             arrive(&w.q_ready[i]);
         }
         return wait(&w.q_ready[i], uses & 1);
+    }
+
+    // The sums with a step's 64 columns of the row added.
+    __device__ __forceinline__ static void add_step(uint32_t s_at, f32x2 factor2, float ref, const f32x2 (&sum2)[2], f32x2 (&total)[2]) {
+        const f32x2 ref2 = pack2(-ref, -ref);
+        total[0] = sum2[0];
+        total[1] = sum2[1];
+#pragma unroll
+        for (int q = 0; q < 2; q++) {
+            float x[32];
+            tc_ld32(x, s_at + 32 * q);
+            tc_wait_ld();
+            add_row(x, factor2, ref2, total);
+        }
+    }
+    // The reference at the largest logit so far, and the sums brought to it.
+    __device__ __noinline__ static void move_reference(uint32_t s_at, float factor, float& ref, f32x2 (&sum2)[2]) {
+        float y = ref;
+#pragma unroll 1
+        for (int q = 0; q < 4; q++) {
+            uint32_t x[16];
+            tc_ld16(x, s_at + 16 * q);
+            tc_wait_ld();
+#pragma unroll
+            for (int c = 0; c < 16; c++) y = fmaxf(y, __uint_as_float(x[c]) * factor);
+        }
+        const float keep = fast_exp2(ref - y);
+        ref = y;
+        sum2[0] = mul2(sum2[0], pack2(keep, keep));
+        sum2[1] = mul2(sum2[1], pack2(keep, keep));
     }
 
     // First pass: a thread per query vector.
@@ -459,40 +487,15 @@ struct WeighRows {
                 }
                 // Against the reference as it stands, a row's largest logit in the first step it had tokens in; where the sum shows that it has
                 // become too small (fp32 has room for logits 60 above it) the largest is looked for again and the step done once more.
-                f32x2 total[2];
-                bool search = start;
+                if (start) move_reference(s_at, factor, ref, sum2);
                 start = false;
-                for (;;) {
-                    if (search) {
-                        float y = -INFINITY;
-#pragma unroll 1
-                        for (int q = 0; q < 4; q++) {
-                            uint32_t x[16];
-                            tc_ld16(x, s_at + 16 * q);
-                            tc_wait_ld();
-#pragma unroll
-                            for (int c = 0; c < 16; c++) y = fmaxf(y, __uint_as_float(x[c]) * factor);
-                        }
-                        const float to = fmaxf(y, ref), keep = fast_exp2(ref - to);
-                        ref = to;
-                        sum2[0] = mul2(sum2[0], pack2(keep, keep));
-                        sum2[1] = mul2(sum2[1], pack2(keep, keep));
-                    }
-                    const f32x2 ref2 = pack2(-ref, -ref);
-                    total[0] = sum2[0];
-                    total[1] = sum2[1];
-#pragma unroll
-                    for (int q = 0; q < 2; q++) {
-                        float x[32];
-                        tc_ld32(x, s_at + 32 * q);
-                        tc_wait_ld();
-                        add_row(x, factor2, ref2, total);
-                    }
-                    if (search) break;
-                    float a, c;
-                    unpack2(add2(total[0], total[1]), a, c);
-                    search = __any_sync(0xFFFFFFFFu, a + c > 1.0e18f);
-                    if (!search) break;
+                f32x2 total[2];
+                add_step(s_at, factor2, ref, sum2, total);
+                float a, c;
+                unpack2(add2(total[0], total[1]), a, c);
+                if (__any_sync(0xFFFFFFFFu, a + c > 1.0e18f)) {
+                    move_reference(s_at, factor, ref, sum2);
+                    add_step(s_at, factor2, ref, sum2, total);
                 }
                 sum2[0] = total[0];
                 sum2[1] = total[1];
@@ -528,30 +531,39 @@ struct WeighRows {
             if (gone[q] >> lane & 1u && really_seen(t0 + 32 * q + lane)) latch(p.status);
     }
 
-    // Second pass: a thread per token, the vectors of a tile along its lane; `in`: the vectors that see it, where not all do.
-    template <bool MASK>
-    __device__ __forceinline__ void add_column(const float (&x)[32], const float4* column, uint32_t in, f32x2 (&total)[2]) const {
+    // Second pass: a thread per token, the vectors of a tile along its lane; `in`: the vectors that see it, where not all do.  Where all vectors
+    // have one factor (bf16 pages, fp16 queries) half as much is read along the way.
+    template <bool MASK, bool EVEN>
+    __device__ __forceinline__ void add_column(const float (&x)[32], int first, uint32_t in, f32x2 factor2, f32x2 (&total)[2]) const {
 #pragma unroll
-        for (int c = 0; c < 16; c++) {
-            const uint4 v = lds128(smem_u32(column + c));
-            float a, b;
-            exp2_both(c, fma2(pack2(x[2 * c], x[2 * c + 1]), pack2(__uint_as_float(v.x), __uint_as_float(v.y)), pack2(__uint_as_float(v.z), __uint_as_float(v.w))), a, b);
-            if (MASK) {
-                a = in >> (2 * c) & 1u ? a : 0.0f;
-                b = in >> (2 * c + 1) & 1u ? b : 0.0f;
+        for (int c = 0; c < 16; c += 2) {
+            const uint4 low = lds128(smem_u32(w.low + first + 2 * c));
+            uint4 f = make_uint4(0, 0, 0, 0);
+            if (!EVEN) f = lds128(smem_u32(w.scale + first + 2 * c));
+#pragma unroll
+            for (int e = 0; e < 2; e++) {
+                const f32x2 l = e ? pack2(__uint_as_float(low.z), __uint_as_float(low.w)) : pack2(__uint_as_float(low.x), __uint_as_float(low.y));
+                const f32x2 s = EVEN ? factor2 : e ? pack2(__uint_as_float(f.z), __uint_as_float(f.w)) : pack2(__uint_as_float(f.x), __uint_as_float(f.y));
+                float a, b;
+                exp2_both(c + e, fma2(pack2(x[2 * (c + e)], x[2 * (c + e) + 1]), s, l), a, b);
+                if (MASK) {
+                    a = in >> (2 * (c + e)) & 1u ? a : 0.0f;
+                    b = in >> (2 * (c + e) + 1) & 1u ? b : 0.0f;
+                }
+                total[e] = add2(total[e], pack2(a, b));
             }
-            total[c & 1] = add2(total[c & 1], pack2(a, b));
         }
     }
-    template <bool MASK>
+    template <bool MASK, bool EVEN>
     __device__ __forceinline__ float column_sum(uint32_t s_at, int first, unsigned long long in) const {
         f32x2 total[2] = {pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)};
+        const f32x2 factor2 = pack2(p.scale_log2, p.scale_log2);
 #pragma unroll
         for (int q = 0; q < 2; q++) {
             float x[32];
             tc_ld32(x, s_at + 32 * q);
             tc_wait_ld();
-            add_column<MASK>(x, w.column + first / 2 + 16 * q, (uint32_t)(in >> (32 * q)), total);
+            add_column<MASK, EVEN>(x, first + 32 * q, (uint32_t)(in >> (32 * q)), factor2, total);
         }
         float a, b;
         unpack2(add2(total[0], total[1]), a, b);
@@ -606,9 +618,11 @@ struct WeighRows {
                 if (gaps || !whole(t0)) {
                     const uint32_t word = r < 32 ? absent.x : r < 64 ? absent.y : r < 96 ? absent.z : absent.w;
                     const bool there = t < kv && !(word >> (r & 31) & 1u);
-                    sum = column_sum<true>(s_at, from, there ? seeing(from, t) : 0ull);
+                    sum = column_sum<true, kPool>(s_at, from, there ? seeing(from, t) : 0ull);
+                } else if (kPool || p.f16) {
+                    sum = column_sum<false, true>(s_at, from, 0ull);
                 } else {
-                    sum = column_sum<false>(s_at, from, 0ull);
+                    sum = column_sum<false, false>(s_at, from, 0ull);
                 }
                 release(pair, u);
                 if (leader) {
