@@ -1,7 +1,7 @@
 // Cutting a cache down: which tokens stay (patchkv_evict_select), and their rows' way into other pages (patchkv_cache_gather).
 #include <cooperative_groups.h>
 
-#include "attention_launch.cuh"
+#include "live.cuh"
 #include "rotary.cuh"
 
 namespace patchkv {
@@ -9,7 +9,7 @@ namespace patchkv {
 namespace cg = cooperative_groups;
 
 // ---------------------------------------------------------------- which tokens stay
-constexpr int kSelectThreads = 1024, kSelectWarps = kSelectThreads / 32, kSelectBins = 2048, kSelectCached = 32768;
+constexpr int kSelectThreads = 1024, kSelectWarps = kSelectThreads / 32, kSelectBins = 2048, kSelectKeys = 16, kMaxCluster = 8;
 
 struct EvictParams {
     const float* mass;
@@ -23,22 +23,25 @@ struct EvictParams {
     int32_t* status;
 };
 
-// A cluster takes a sequence, each of its CTAs a run of the tokens, whose masses stay in shared memory as keys: bit patterns, which
-// order numbers that are not negative.  The key of the last token that stays is found digit by digit (11, 11 and 10 bits): every CTA counts
-// its keys by digit, the counts are added up in the first CTA's shared memory, which finds the digit.  Then each warp counts what of its
-// run stays, and a prefix over warps and CTAs gives every kept token its place.  All counts are whole numbers: the order of the
-// atomics does not matter.
+// A cluster takes a sequence, each of its CTAs a run of the tokens, each warp a part of that; masses are keys: bit patterns, which order
+// numbers that are not negative.  The key of the last token that stays is found digit by digit (11, 11 and 10 bits): a CTA counts its
+// keys by digit in shared memory, and every CTA then adds up the counts of all (distributed shared memory) and finds the digit by itself,
+// so that a digit takes one barrier of the cluster.  Then each warp counts what of its part stays, and a prefix over warps and CTAs gives
+// every kept token its place.  All counts are whole numbers: the order of the atomics does not matter.  Bound by the latencies of that
+// chain; HELD: a thread has its keys in registers (runs of up to 16384 tokens), else they are read again each time.
+template <bool HELD>
 __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const EvictParams p) {
-    extern __shared__ uint32_t cached[];
-    __shared__ int bins[kSelectBins];
+    __shared__ __align__(16) int bins[3][kSelectBins];
     __shared__ int warp_sums[33];
-    __shared__ int found[2];                    // digit, and how many keys lie above it (first CTA)
+    __shared__ int found[2];                    // digit, and how many keys lie above it
     __shared__ int2 warp_count[kSelectWarps];   // tokens that stay in any case, and those at the border
-    __shared__ int2 cta_count[16];              // of every CTA of the cluster
+    __shared__ int2 cta_count[kMaxCluster];     // of every CTA of the cluster
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
     const int s = blockIdx.x / ctas, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     pdl_trigger();
+    for (int i = tid; i < 3 * kSelectBins; i += kSelectThreads) bins[0][i] = 0;
+    auto all_there = cluster.barrier_arrive();
     pdl_wait();
     int n = p.kv_len[s], B = p.budget ? p.budget[s] : p.max_keep;
     if (rank == 0 && tid == 0 && (n > p.max_len || B > p.max_keep)) atomicCAS(p.status, 0, (int)PATCHKV_E_BOUNDS);
@@ -46,76 +49,77 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
     B = max(0, min(B, p.max_keep));
     const int kept = min(n, B), last = n <= B ? n : min(p.recent, B), first = n <= B ? 0 : min(p.sinks, B - last);
     const int wanted = kept - last - first;     // of the middle, tokens [first, n - last)
-    // this CTA's run, a whole number of steps of a warp for each warp
-    const int run = (n + ctas * kSelectThreads - 1) / (ctas * kSelectThreads) * kSelectThreads, base = rank * run;
+    // this CTA's run, and this warp's part of it: whole steps of a warp
+    const int run = (n + ctas * kSelectThreads - 1) / (ctas * kSelectThreads) * kSelectThreads, part = run / kSelectWarps;
+    const int begin = rank * run + warp * part + lane, steps = part / 32;
     const float* mass = p.mass + (long long)s * p.mass_stride;
-    auto key_of = [&](int i, bool report) {     // of token base + i
-        const float x = mass[base + i];
-        const uint32_t bits = __float_as_uint(x);
+    auto key_of = [&](int t, bool report) {
+        const uint32_t bits = __float_as_uint(t < n ? mass[t] : 0.0f);
         if (bits < 0x7F800000u) return bits;
         if (bits != 0x80000000u && report) atomicCAS(p.status, 0, (int)PATCHKV_E_BADINPUT);
         return 0u;
     };
-    auto key = [&](int i) { return i < kSelectCached ? cached[i] : key_of(i, false); };
-    for (int i = tid; i < run; i += kSelectThreads) {
-        const uint32_t k = base + i < n ? key_of(i, true) : 0u;
-        if (i < kSelectCached) cached[i] = k;
-    }
+    uint32_t held[HELD ? kSelectKeys : 1];
+    // f(token, key) for every token of the thread; all lanes of a warp come along.
+    auto each = [&](auto&& f, bool report) {
+        if constexpr (HELD) {
+#pragma unroll
+            for (int i = 0; i < kSelectKeys; i++)
+                if (i < steps) f(begin + 32 * i, held[i]);
+        } else {
+#pragma unroll 4
+            for (int i = 0; i < steps; i++) f(begin + 32 * i, key_of(begin + 32 * i, report));
+        }
+    };
+    if constexpr (HELD)
+#pragma unroll
+        for (int i = 0; i < kSelectKeys; i++)
+            if (i < steps) held[i] = key_of(begin + 32 * i, true);
+    cluster.barrier_wait(std::move(all_there));     // all bins are empty, and every CTA is there to be read
     uint32_t border = 0;                        // key of the last token that stays, so far as it is known
     int need = wanted;                          // how many of those keys that agree with it so far stay
     if (wanted > 0) {
 #pragma unroll 1
-        for (int pass = 0; pass < 3; pass++) {
-            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 0 ? 32 : pass == 1 ? 21 : 10;
-            for (int i = tid; i < kSelectBins; i += kSelectThreads) bins[i] = 0;
-            cluster.sync();                     // the keys are there, and all bins are empty
-            for (int i = tid; i < run; i += kSelectThreads) {
-                const int t = base + i;
-                if (t < first || t >= n - last) continue;
-                const uint32_t k = key(i);
-                if (above == 32 || (k >> above) == (border >> above)) atomicAdd(&bins[(k >> shift) & (kSelectBins - 1) & ((1u << (above - shift)) - 1u)], 1);
-            }
-            if (rank != 0) {
-                __syncthreads();
-                int* to = cluster.map_shared_rank(bins, 0);
-                for (int i = tid; i < kSelectBins; i += kSelectThreads)
-                    if (bins[i]) atomicAdd(&to[i], bins[i]);
-            }
+        for (int digit = 0; digit < 3; digit++) {
+            const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, above = digit == 0 ? 32 : digit == 1 ? 21 : 10;
+            const uint32_t mask = (1u << (above - shift)) - 1u, known = digit == 0 ? 0u : ~0u << above;
+            int* mine = bins[digit];
+            each([&](int t, uint32_t k) {
+                if (t >= first && t < n - last && ((k ^ border) & known) == 0) atomicAdd(&mine[k >> shift & mask], 1);
+            }, digit == 0);
             cluster.sync();
-            if (rank == 0) {                    // bins from the top: thread i has the bins 2047 - 2i and 2046 - 2i
-                const int a = bins[kSelectBins - 1 - 2 * tid], b = bins[kSelectBins - 2 - 2 * tid];
-                int total;
-                const int before = cta_exclusive_scan(a + b, warp_sums, &total);
-                if (before < need && need <= before + a + b) {
-                    const bool second = need > before + a;
-                    found[0] = kSelectBins - 1 - 2 * tid - second;
-                    found[1] = before + (second ? a : 0);
-                }
+            // bins from the top: thread i has the bins 2047 - 2i and 2046 - 2i
+            int2 c = make_int2(0, 0);
+            for (int i = 0; i < ctas; i++) {
+                const int2 x = *reinterpret_cast<const int2*>(cluster.map_shared_rank(mine, i) + kSelectBins - 2 - 2 * tid);
+                c.x += x.x;
+                c.y += x.y;
             }
-            cluster.sync();
-            const int* from = cluster.map_shared_rank(found, 0);
-            border |= (uint32_t)from[0] << shift;
-            need -= from[1];
+            int total;
+            const int before = cta_exclusive_scan(c.x + c.y, warp_sums, &total);
+            if (before < need && need <= before + c.x + c.y) {
+                const bool second = need > before + c.y;
+                found[0] = kSelectBins - 1 - 2 * tid - second;
+                found[1] = before + (second ? c.y : 0);
+            }
+            __syncthreads();
+            border |= (uint32_t)found[0] << shift;
+            need -= found[1];
         }
-    } else {
-        __syncthreads();
     }
     // What stays: in any case (bit 0), or if it is among the first `need` at the border (bit 1).
-    auto standing = [&](int i) {
-        const int t = base + i;
+    auto standing = [&](int t, uint32_t k) {
         if (t >= n) return 0;
         if (t < first || t >= n - last) return 1;
         if (wanted == 0) return 0;
-        const uint32_t k = key(i);
         return k > border ? 1 : k == border ? 2 : 0;
     };
-    const int begin = warp * (run / kSelectWarps), end = begin + run / kSelectWarps;
     int2 mine = make_int2(0, 0);
-    for (int i = begin + lane; i < end; i += 32) {
-        const int x = standing(i);
+    each([&](int t, uint32_t k) {
+        const int x = standing(t, k);
         mine.x += __popc(__ballot_sync(0xFFFFFFFFu, x & 1));
         mine.y += __popc(__ballot_sync(0xFFFFFFFFu, x & 2));
-    }
+    }, wanted == 0);
     if (lane == 0) warp_count[warp] = mine;
     __syncthreads();
     if (warp == 0) {
@@ -129,26 +133,25 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
         const int2 all = make_int2(__shfl_sync(0xFFFFFFFFu, sum.x, 31), __shfl_sync(0xFFFFFFFFu, sum.y, 31));
         if (lane < ctas) cluster.map_shared_rank(cta_count, lane)[rank] = all;
     }
-    cluster.sync();
+    cluster.sync();                             // (and behind it nobody reads another CTA's shared memory)
     int2 at = warp_count[warp];
     for (int i = 0; i < rank; i++) { at.x += cta_count[i].x; at.y += cta_count[i].y; }
     int32_t* keep = p.keep + (long long)s * p.keep_stride;
     float* out = p.mass_out ? p.mass_out + (long long)s * p.out_stride : nullptr;
     const uint32_t below = (1u << lane) - 1u;
-    for (int i = begin + lane; i < end; i += 32) {
-        const int x = standing(i);
+    each([&](int t, uint32_t k) {
+        const int x = standing(t, k);
         const uint32_t sure = __ballot_sync(0xFFFFFFFFu, x & 1), edge = __ballot_sync(0xFFFFFFFFu, x & 2);
         const int ties = at.y + __popc(edge & below), place = at.x + __popc(sure & below) + min(ties, need);
         if ((x & 1) || ((x & 2) && ties < need)) {
-            keep[place] = base + i;
-            if (out) out[place] = __uint_as_float(key(i));
+            keep[place] = t;
+            if (out) out[place] = __uint_as_float(k);
         }
         at.x += __popc(sure);
         at.y += __popc(edge);
-    }
+    }, false);
     for (int i = kept + rank * kSelectThreads + tid; i < p.max_keep; i += ctas * kSelectThreads) keep[i] = -1;
     if (rank == 0 && tid == 0) p.kept[s] = kept;
-    cluster.sync();                             // nobody's shared memory goes while it may still be read
 }
 
 // ---------------------------------------------------------------- their rows
@@ -346,23 +349,20 @@ int evict_select(patchkv_ctx* ctx, const patchkv_evict_args* a, cudaStream_t str
                            a->max_len, a->max_keep, a->recent, a->sinks, ctx->d_status};
     // CTAs of a cluster: one for every 4096 tokens, up to eight.
     int ctas = 1;
-    while (ctas < 8 && (long long)ctas * 4096 < a->max_len) ctas *= 2;
-    const int run = (a->max_len + ctas * kSelectThreads - 1) / (ctas * kSelectThreads) * kSelectThreads;
-    const int smem = std::min(run, kSelectCached) * 4;
+    while (ctas < kMaxCluster && (long long)ctas * 4096 < a->max_len) ctas *= 2;
+    const bool held = a->max_len <= ctas * kSelectThreads * kSelectKeys;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return fail(ctx, PATCHKV_E_CUDA, "cudaSetDevice failed");
-    static std::atomic<uint64_t> allowed{0};
-    PKV_CUDA(ctx, allow_smem((const void*)evict_select_kernel, kSelectCached * 4, &allowed));
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
-    cfg.gridDim = dim3(a->n_seqs * ctas); cfg.blockDim = dim3(kSelectThreads); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
+    cfg.gridDim = dim3(a->n_seqs * ctas); cfg.blockDim = dim3(kSelectThreads); cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr; cfg.numAttrs = 2;
-    PKV_CUDA(ctx, cudaLaunchKernelEx(&cfg, evict_select_kernel, p));
+    PKV_CUDA(ctx, held ? cudaLaunchKernelEx(&cfg, evict_select_kernel<true>, p) : cudaLaunchKernelEx(&cfg, evict_select_kernel<false>, p));
     return PATCHKV_OK;
 }
 
