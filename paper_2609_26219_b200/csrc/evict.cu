@@ -1,7 +1,7 @@
 // Cutting a cache down: which tokens stay (patchkv_evict_select), and their rows' way into other pages (patchkv_cache_gather).
 #include <cooperative_groups.h>
 
-#include "live.cuh"
+#include "attention_launch.cuh"
 #include "rotary.cuh"
 
 namespace patchkv {
@@ -9,7 +9,8 @@ namespace patchkv {
 namespace cg = cooperative_groups;
 
 // ---------------------------------------------------------------- which tokens stay
-constexpr int kSelectThreads = 1024, kSelectWarps = kSelectThreads / 32, kSelectBins = 2048, kSelectKeys = 16, kMaxCluster = 8;
+constexpr int kSelectThreads = 1024, kSelectWarps = kSelectThreads / 32, kSelectBins = 2048, kSelectHeld = 16384, kSelectList = 4096, kMaxCluster = 8;
+constexpr int kStays = 0x7FFFFFFF, kAbsent = (int)0x80000000;      // keys of tokens that stay in any case, and of those behind the last
 
 struct EvictParams {
     const float* mass;
@@ -23,24 +24,55 @@ struct EvictParams {
     int32_t* status;
 };
 
-// A cluster takes a sequence, each of its CTAs a run of the tokens, each warp a part of that; masses are keys: bit patterns, which order
-// numbers that are not negative.  The key of the last token that stays is found digit by digit (11, 11 and 10 bits): a CTA counts its
-// keys by digit in shared memory, and every CTA then adds up the counts of all (distributed shared memory) and finds the digit by itself,
-// so that a digit takes one barrier of the cluster.  Then each warp counts what of its part stays, and a prefix over warps and CTAs gives
-// every kept token its place.  All counts are whole numbers: the order of the atomics does not matter.  Bound by the latencies of that
-// chain; HELD: a thread has its keys in registers (runs of up to 16384 tokens), else they are read again each time.
+// A cluster takes a sequence, each of its CTAs a run of the tokens, each lane some that lie together.  Masses are keys, bit patterns, which order
+// numbers that are not negative, with the tokens that stay in any case above all.  The key of the last token that stays is found digit by digit
+// (11, 11 and 10 bits): a CTA counts its keys by digit in shared memory, and every CTA adds up the counts of all (distributed shared memory) and
+// finds the digit by itself.  After the first digit few keys are left as a rule; every CTA then gets the list of them and finds the other
+// two digits without the cluster (where they are many, ties above all, the cluster counts on).  Each lane counts what of its tokens
+// stays, a prefix over lanes, warps and CTAs gives every kept token its place, and the indices leave by way of shared memory, so that they
+// are written side by side.  All counts are whole numbers: the order of the atomics does not matter.  Bound by the latencies of that
+// chain: a barrier of the cluster takes 2000 cycles, counts read from eight CTAs 4000, from sixteen 12000.
+// HELD: keys and indices of a run fit shared memory, else keys are made again each time and indices written one by one.
+struct SelectSmem {
+    alignas(16) int bins[3][kSelectBins];
+    int list[kSelectList];                      // keys that are left after the first digit
+    int sums[kSelectWarps];
+    int found[3];                               // digit, how many keys lie above it, and how many have it
+    int2 warp_count[kSelectWarps];              // tokens above the border, and those at it
+    int2 cta_count[kMaxCluster];                // of every CTA of the cluster
+    int listed[kMaxCluster];                    // keys that every CTA has put on its list
+    int n_list;
+};
+// The bin, from the top, in which the need-th key lies: found = {bin, keys above it, keys in it}.  c: counts of bins 2046 - 2i and 2047 - 2i.
+__device__ __forceinline__ void find_bin(SelectSmem& m, int2 c, int need) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, own = c.x + c.y;
+    int inc = own;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(0xFFFFFFFFu, inc, d);
+        if (lane >= d) inc += o;
+    }
+    if (lane == 31) m.sums[warp] = inc;
+    __syncthreads();
+    const int before = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? m.sums[lane] : 0) + inc - own;
+    if (before < need && need <= before + own) {
+        const bool second = need > before + c.y;
+        m.found[0] = kSelectBins - 1 - 2 * (int)threadIdx.x - second;
+        m.found[1] = before + (second ? c.y : 0);
+        m.found[2] = second ? c.x : c.y;
+    }
+    __syncthreads();
+}
 template <bool HELD>
 __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const EvictParams p) {
-    __shared__ __align__(16) int bins[3][kSelectBins];
-    __shared__ int warp_sums[33];
-    __shared__ int found[2];                    // digit, and how many keys lie above it
-    __shared__ int2 warp_count[kSelectWarps];   // tokens that stay in any case, and those at the border
-    __shared__ int2 cta_count[kMaxCluster];     // of every CTA of the cluster
+    extern __shared__ int held[];               // keys [lane's token][33] of each warp, then the indices of the kept
+    __shared__ SelectSmem m;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
     const int s = blockIdx.x / ctas, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     pdl_trigger();
-    for (int i = tid; i < 3 * kSelectBins; i += kSelectThreads) bins[0][i] = 0;
+    for (int i = tid; i < 3 * kSelectBins / 4; i += kSelectThreads) reinterpret_cast<int4*>(m.bins[0])[i] = make_int4(0, 0, 0, 0);
+    if (tid == 0) m.n_list = 0;
     auto all_there = cluster.barrier_arrive();
     pdl_wait();
     int n = p.kv_len[s], B = p.budget ? p.budget[s] : p.max_keep;
@@ -48,108 +80,149 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const Evic
     n = max(0, min(n, p.max_len));
     B = max(0, min(B, p.max_keep));
     const int kept = min(n, B), last = n <= B ? n : min(p.recent, B), first = n <= B ? 0 : min(p.sinks, B - last);
-    const int wanted = kept - last - first;     // of the middle, tokens [first, n - last)
-    // this CTA's run, and this warp's part of it: whole steps of a warp
-    const int run = (n + ctas * kSelectThreads - 1) / (ctas * kSelectThreads) * kSelectThreads, part = run / kSelectWarps;
-    const int begin = rank * run + warp * part + lane, steps = part / 32;
+    // `steps` tokens a lane
+    const int steps = (n + ctas * kSelectThreads - 1) / (ctas * kSelectThreads), run = steps * kSelectThreads;
+    const int base = rank * run + warp * 32 * steps, begin = base + lane * steps;
+    int* const mine = held + warp * 33 * steps;
+    int* const indices = held + kSelectWarps * 33 * steps;
     const float* mass = p.mass + (long long)s * p.mass_stride;
-    auto key_of = [&](int t, bool report) {
-        const uint32_t bits = __float_as_uint(t < n ? mass[t] : 0.0f);
-        if (bits < 0x7F800000u) return bits;
-        if (bits != 0x80000000u && report) atomicCAS(p.status, 0, (int)PATCHKV_E_BADINPUT);
-        return 0u;
+    auto mass_of = [&](int t) {
+        const uint32_t bits = __float_as_uint(mass[t]);
+        return bits < 0x7F800000u ? (int)bits : 0;
     };
-    uint32_t held[HELD ? kSelectKeys : 1];
-    // f(token, key) for every token of the thread; all lanes of a warp come along.
-    auto each = [&](auto&& f, bool report) {
-        if constexpr (HELD) {
-#pragma unroll
-            for (int i = 0; i < kSelectKeys; i++)
-                if (i < steps) f(begin + 32 * i, held[i]);
-        } else {
+    auto key_of = [&](int t) {
+        if (t >= n) return kAbsent;
+        const uint32_t bits = __float_as_uint(mass[t]);
+        if (bits >= 0x7F800000u && bits != 0x80000000u) atomicCAS(p.status, 0, (int)PATCHKV_E_BADINPUT);
+        return t < first || t >= n - last ? kStays : bits < 0x7F800000u ? (int)bits : 0;
+    };
+    auto key = [&](int i) { return HELD ? mine[33 * i + lane] : key_of(begin + i); };
+    if (HELD)
 #pragma unroll 4
-            for (int i = 0; i < steps; i++) f(begin + 32 * i, key_of(begin + 32 * i, report));
+        for (int i = lane; i < 32 * steps; i += 32) {
+            const int owner = i / steps;
+            mine[33 * (i - owner * steps) + owner] = key_of(base + i);
         }
+    cluster.barrier_wait(std::move(all_there)); // all bins are empty, and every CTA is there to be read
+    auto barrier = [&]() { if (ctas > 1) cluster.sync(); else __syncthreads(); };
+    int border = kept > 0 && first + last < kept ? 0 : kStays;     // key of the last token that stays, so far as it is known
+    int need = kept;                            // how many of those keys that agree with it so far stay
+    auto shift_of = [](int digit) { return digit == 0 ? 21 : digit == 1 ? 10 : 0; };
+    auto mask_of = [](int digit) { return digit == 2 ? 1023u : 2047u; };
+    auto known_of = [](int digit) { return digit == 0 ? 0x80000000u : digit == 1 ? 0xFFE00000u : 0xFFFFFC00u; };
+    auto found = [&](int digit) {
+        border |= m.found[0] << shift_of(digit);
+        need -= m.found[1];
     };
-    if constexpr (HELD)
-#pragma unroll
-        for (int i = 0; i < kSelectKeys; i++)
-            if (i < steps) held[i] = key_of(begin + 32 * i, true);
-    cluster.barrier_wait(std::move(all_there));     // all bins are empty, and every CTA is there to be read
-    uint32_t border = 0;                        // key of the last token that stays, so far as it is known
-    int need = wanted;                          // how many of those keys that agree with it so far stay
-    if (wanted > 0) {
-#pragma unroll 1
-        for (int digit = 0; digit < 3; digit++) {
-            const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, above = digit == 0 ? 32 : digit == 1 ? 21 : 10;
-            const uint32_t mask = (1u << (above - shift)) - 1u, known = digit == 0 ? 0u : ~0u << above;
-            int* mine = bins[digit];
-            each([&](int t, uint32_t k) {
-                if (t >= first && t < n - last && ((k ^ border) & known) == 0) atomicAdd(&mine[k >> shift & mask], 1);
-            }, digit == 0);
-            cluster.sync();
-            // bins from the top: thread i has the bins 2047 - 2i and 2046 - 2i
-            int2 c = make_int2(0, 0);
+    // A digit by the whole cluster.
+    auto count_all = [&](int digit) {
+        const int shift = shift_of(digit);
+        const uint32_t known = known_of(digit), mask = mask_of(digit);
+        int* count = m.bins[digit];
+#pragma unroll 4
+        for (int i = 0; i < steps; i++) {
+            const uint32_t k = (uint32_t)key(i);
+            if (((k ^ (uint32_t)border) & known) == 0) atomicAdd(&count[k >> shift & mask], 1);
+        }
+        barrier();
+        int2 c = make_int2(0, 0);
+        if (digit != 0 || tid >= kSelectThreads / 2)        // the first digit's upper half stands for a sign
+#pragma unroll 8
             for (int i = 0; i < ctas; i++) {
-                const int2 x = *reinterpret_cast<const int2*>(cluster.map_shared_rank(mine, i) + kSelectBins - 2 - 2 * tid);
+                const int2 x = *reinterpret_cast<const int2*>(cluster.map_shared_rank(count, i) + kSelectBins - 2 - 2 * tid);
                 c.x += x.x;
                 c.y += x.y;
             }
-            int total;
-            const int before = cta_exclusive_scan(c.x + c.y, warp_sums, &total);
-            if (before < need && need <= before + c.x + c.y) {
-                const bool second = need > before + c.y;
-                found[0] = kSelectBins - 1 - 2 * tid - second;
-                found[1] = before + (second ? c.y : 0);
+        find_bin(m, c, need);
+        found(digit);
+    };
+    if (border == 0) {
+        count_all(0);
+        const int left = m.found[2];
+        if (left > kSelectList) {
+            count_all(1);
+            count_all(2);
+        } else {
+#pragma unroll 4
+            for (int i = 0; i < steps; i++) {
+                const int k = key(i);
+                if (((uint32_t)(k ^ border) & known_of(1)) == 0) m.list[atomicAdd(&m.n_list, 1)] = k;
             }
             __syncthreads();
-            border |= (uint32_t)found[0] << shift;
-            need -= found[1];
+            if (tid < ctas) cluster.map_shared_rank(m.listed, tid)[rank] = m.n_list;
+            barrier();
+            // The lists of all CTAs, a key to a thread and round: the i-th key is on the list of the CTA whose share of the numbers has i.
+            for (int digit = 1; digit < 3; digit++) {
+                const int shift = shift_of(digit);
+                const uint32_t known = known_of(digit), mask = mask_of(digit);
+                int* count = m.bins[digit];
+                for (int i = tid; i < left; i += kSelectThreads) {
+                    int from = 0, at = i;
+                    while (at >= m.listed[from]) at -= m.listed[from++];
+                    const uint32_t k = (uint32_t)cluster.map_shared_rank(m.list, from)[at];
+                    if (((k ^ (uint32_t)border) & known) == 0) atomicAdd(&count[k >> shift & mask], 1);
+                }
+                __syncthreads();
+                find_bin(m, *reinterpret_cast<const int2*>(count + kSelectBins - 2 - 2 * tid), need);
+                found(digit);
+            }
         }
     }
-    // What stays: in any case (bit 0), or if it is among the first `need` at the border (bit 1).
-    auto standing = [&](int t, uint32_t k) {
-        if (t >= n) return 0;
-        if (t < first || t >= n - last) return 1;
-        if (wanted == 0) return 0;
-        return k > border ? 1 : k == border ? 2 : 0;
-    };
-    int2 mine = make_int2(0, 0);
-    each([&](int t, uint32_t k) {
-        const int x = standing(t, k);
-        mine.x += __popc(__ballot_sync(0xFFFFFFFFu, x & 1));
-        mine.y += __popc(__ballot_sync(0xFFFFFFFFu, x & 2));
-    }, wanted == 0);
-    if (lane == 0) warp_count[warp] = mine;
-    __syncthreads();
-    if (warp == 0) {
-        int2 c = warp_count[lane], sum = c;
+    int2 count = make_int2(0, 0);
+#pragma unroll 4
+    for (int i = 0; i < steps; i++) {
+        const int k = key(i);
+        count.x += k > border;
+        count.y += k == border;
+    }
+    int2 sum = count;
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int a = __shfl_up_sync(0xFFFFFFFFu, sum.x, d), b = __shfl_up_sync(0xFFFFFFFFu, sum.y, d);
-            if (lane >= d) { sum.x += a; sum.y += b; }
-        }
-        warp_count[lane] = make_int2(sum.x - c.x, sum.y - c.y);
-        const int2 all = make_int2(__shfl_sync(0xFFFFFFFFu, sum.x, 31), __shfl_sync(0xFFFFFFFFu, sum.y, 31));
-        if (lane < ctas) cluster.map_shared_rank(cta_count, lane)[rank] = all;
+    for (int d = 1; d < 32; d <<= 1) {
+        const int a = __shfl_up_sync(0xFFFFFFFFu, sum.x, d), b = __shfl_up_sync(0xFFFFFFFFu, sum.y, d);
+        if (lane >= d) { sum.x += a; sum.y += b; }
     }
-    cluster.sync();                             // (and behind it nobody reads another CTA's shared memory)
-    int2 at = warp_count[warp];
-    for (int i = 0; i < rank; i++) { at.x += cta_count[i].x; at.y += cta_count[i].y; }
+    if (lane == 31) m.warp_count[warp] = sum;
+    __syncthreads();
+    int2 at;                                    // of this CTA, in front of the lane's tokens
+    {
+        const int2 c = m.warp_count[lane];
+        at.x = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? c.x : 0) + sum.x - count.x;
+        at.y = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? c.y : 0) + sum.y - count.y;
+        const int2 all = make_int2(__reduce_add_sync(0xFFFFFFFFu, c.x), __reduce_add_sync(0xFFFFFFFFu, c.y));
+        if (warp == 0 && lane < ctas) cluster.map_shared_rank(m.cta_count, lane)[rank] = all;
+    }
+    barrier();                                  // (and behind it nobody reads another CTA's shared memory)
+    int2 front = make_int2(0, 0);               // of the CTAs in front
+    for (int i = 0; i < rank; i++) { front.x += m.cta_count[i].x; front.y += m.cta_count[i].y; }
+    const int2 own = m.cta_count[rank];
+    const int start = front.x + min(front.y, need), end = front.x + own.x + min(front.y + own.y, need);
     int32_t* keep = p.keep + (long long)s * p.keep_stride;
     float* out = p.mass_out ? p.mass_out + (long long)s * p.out_stride : nullptr;
-    const uint32_t below = (1u << lane) - 1u;
-    each([&](int t, uint32_t k) {
-        const int x = standing(t, k);
-        const uint32_t sure = __ballot_sync(0xFFFFFFFFu, x & 1), edge = __ballot_sync(0xFFFFFFFFu, x & 2);
-        const int ties = at.y + __popc(edge & below), place = at.x + __popc(sure & below) + min(ties, need);
-        if ((x & 1) || ((x & 2) && ties < need)) {
-            keep[place] = t;
-            if (out) out[place] = __uint_as_float(k);
+    int place = front.x + at.x + min(front.y + at.y, need), ties = front.y + at.y;
+#pragma unroll 4
+    for (int i = 0; i < steps; i++) {
+        const int k = key(i);
+        const bool stays = k > border || (k == border && ties < need);
+        ties += k == border;
+        if (stays) {
+            if (HELD) {
+                indices[place - start] = begin + i;
+            } else {
+                keep[place] = begin + i;
+                if (out) out[place] = __int_as_float(mass_of(begin + i));
+            }
         }
-        at.x += __popc(sure);
-        at.y += __popc(edge);
-    }, false);
+        place += stays;
+    }
+    if (HELD) {
+        __syncthreads();
+#pragma unroll 4
+        for (int i = start + tid; i < end; i += kSelectThreads) {
+            const int t = indices[i - start];
+            keep[i] = t;
+            if (out) out[i] = __int_as_float(mass_of(t));
+        }
+    }
     for (int i = kept + rank * kSelectThreads + tid; i < p.max_keep; i += ctas * kSelectThreads) keep[i] = -1;
     if (rank == 0 && tid == 0) p.kept[s] = kept;
 }
@@ -350,12 +423,16 @@ int evict_select(patchkv_ctx* ctx, const patchkv_evict_args* a, cudaStream_t str
     // CTAs of a cluster: one for every 4096 tokens, up to eight.
     int ctas = 1;
     while (ctas < kMaxCluster && (long long)ctas * 4096 < a->max_len) ctas *= 2;
-    const bool held = a->max_len <= ctas * kSelectThreads * kSelectKeys;
+    const int run = (a->max_len + ctas * kSelectThreads - 1) / (ctas * kSelectThreads) * kSelectThreads;
+    const bool held = run <= kSelectHeld;
+    auto bytes = [](int tokens) { return tokens / 32 * 33 * 4 + tokens * 4; };
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return fail(ctx, PATCHKV_E_CUDA, "cudaSetDevice failed");
+    static std::atomic<uint64_t> allowed{0};
+    if (held) PKV_CUDA(ctx, allow_smem((const void*)evict_select_kernel<true>, bytes(kSelectHeld), &allowed));
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
-    cfg.gridDim = dim3(a->n_seqs * ctas); cfg.blockDim = dim3(kSelectThreads); cfg.stream = stream;
+    cfg.gridDim = dim3(a->n_seqs * ctas); cfg.blockDim = dim3(kSelectThreads); cfg.dynamicSmemBytes = held ? bytes(run) : 0; cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
