@@ -83,4 +83,6 @@ def test_binding_refuses_what_it_can_see(pk):
         pk._table_rows(torch.zeros((2, 8), dtype=torch.int64), "keep", 2)
     with pytest.raises(ValueError):
         pk._counts(torch.zeros(4, dtype=torch.int32)[::2], "kept", 2)
-    assert pk._table_rows(torch.zeros((3, 8), dtype=torch.int32)[:, :5], "keep", 2) == 8
+    assert pk._table_rows(torch.zeros((3, 8), dtype=torch.int32)[:, :5], "keep", 2) == (8, 5)
+    with pytest.raises(ValueError):
+        pk._table_rows(torch.zeros((3, 8), dtype=torch.int32)[:, :5], "src_table", 2, True)
