@@ -28,7 +28,19 @@ cudaError_t launch_weigh_rows_passes(const AttentionParams& p, const WeightParam
         pl.chunk_tiles = std::min(chunk, pl.tiles - at);
         pl.last = at + chunk >= pl.tiles;
         e = launch_weigh_rows_kernel<KF, D, IMAGE, ONE, true>(p, pl, stream);
-        if (e == cudaSuccess) e = launch_pdl(weigh_rows_join_kernel, dim3((p.b.max_kv_len + kRowTile - 1) / kRowTile, p.b.n_seqs), dim3(kWeighJoin), 0, stream, p, m, pl);
+        if (e != cudaSuccess) break;
+        cudaLaunchConfig_t cfg;
+        memset(&cfg, 0, sizeof(cfg));
+        const unsigned steps = (p.b.max_kv_len + kRowTile - 1) / kRowTile;
+        const unsigned ctas = pl.chunk_tiles > kWeighJoin / 128 && (long long)steps * p.b.n_seqs * kWeighJoinCtas <= 2 * 148 ? kWeighJoinCtas : 1;
+        cfg.gridDim = dim3(steps, p.b.n_seqs, ctas); cfg.blockDim = dim3(kWeighJoin); cfg.stream = stream;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = 1; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = ctas;
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr; cfg.numAttrs = 2;
+        e = cudaLaunchKernelEx(&cfg, weigh_rows_join_kernel, p, m, pl);
     }
     return e;
 }
