@@ -567,7 +567,7 @@ typedef struct {
     int64_t q_stride_head;
     const void* mass_in;          /* DEVICE [n_seqs][mass_stride], optional; may be mass */
     void* mass;                   /* DEVICE [n_seqs][mass_stride] */
-    int64_t mass_stride;          /* elements, at least max_kv_len */
+    int64_t mass_stride;          /* elements, at least max_kv_len or what a sequence's block table has room for, the smaller */
     void* workspace;              /* as for patchkv_attention */
     uint64_t workspace_bytes;     /* at least patchkv_attention_mass_workspace_bytes of the same arguments */
 } patchkv_mass_args;

@@ -306,32 +306,32 @@ _MASS_TYPES = {torch.float32: MASS_F32, torch.int64: MASS_U64}
 def _rows(t: torch.Tensor, name: str):
     """Row type, shape and strides of a tensor [rows][heads][channels]."""
     kind, shape, strides = _ROW_TYPES.get(t.dtype), t.shape, t.stride()
-    if kind is None or len(shape) != 3 or (strides[2] != 1 and shape[2] > 1):
-        raise ValueError(f"{name}: a bfloat16 or float16 tensor [rows][heads][channels] with unit channel stride")
+    if kind is None or not t.is_cuda or len(shape) != 3 or (strides[2] != 1 and shape[2] > 1):
+        raise ValueError(f"{name}: a bfloat16 or float16 device tensor [rows][heads][channels] with unit channel stride")
     return kind, shape, strides
 
 
 def _table_rows(t: torch.Tensor, name: str, rows: int, whole: bool = False):
     """Row stride and entries of an int32 tensor [at least rows][entries] with unit stride on the last axis (whole: without gaps)."""
     shape, strides = t.shape, t.stride()
-    if (t.dtype is not torch.int32 or len(shape) != 2 or shape[0] < rows or (strides[1] != 1 and shape[1] > 1)
+    if (t.dtype is not torch.int32 or not t.is_cuda or len(shape) != 2 or shape[0] < rows or (strides[1] != 1 and shape[1] > 1)
             or (whole and rows > 1 and strides[0] != shape[1])):
-        raise ValueError(f"{name}: {'a contiguous' if whole else 'an'} int32 tensor [n_seqs][entries]{'' if whole else ' with unit stride on the last axis'}")
+        raise ValueError(f"{name}: {'a contiguous' if whole else 'an'} int32 device tensor [n_seqs][entries]{'' if whole else ' with unit stride on the last axis'}")
     return (strides[0] if shape[0] > 1 else shape[1]), shape[1]
 
 
 def _counts(t: torch.Tensor, name: str, n: int) -> int:
     shape = t.shape
-    if t.dtype is not torch.int32 or len(shape) != 1 or shape[0] < n or (n > 1 and t.stride(0) != 1):
-        raise ValueError(f"{name}: a contiguous int32 tensor of {n} entries")
+    if t.dtype is not torch.int32 or not t.is_cuda or len(shape) != 1 or shape[0] < n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name}: a contiguous int32 device tensor of {n} entries")
     return t.data_ptr()
 
 
 def _mass_rows(t: torch.Tensor, name: str, kinds, rows: int):
     """Row stride and entries of a tensor of masses [at least rows][tokens]."""
     shape, strides = t.shape, t.stride()
-    if t.dtype not in kinds or len(shape) != 2 or shape[0] < rows or (strides[1] != 1 and shape[1] > 1):
-        raise ValueError(f"{name}: a tensor [n_seqs][tokens] of {', '.join(str(k) for k in kinds)} with unit stride on the last axis")
+    if t.dtype not in kinds or not t.is_cuda or len(shape) != 2 or shape[0] < rows or (strides[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{name}: a device tensor [n_seqs][tokens] of {', '.join(str(k) for k in kinds)} with unit stride on the last axis")
     return (strides[0] if shape[0] > 1 else shape[1]), shape[1]
 
 
@@ -495,8 +495,8 @@ class Context:
         if shape[0] < batch.n_rows or shape[2] != geom.head_dim:
             raise ValueError("q: [n_rows][n_q_heads][head_dim]")
         stride, tokens = _mass_rows(mass, "mass", _MASS_TYPES, batch.n_seqs)
-        if tokens < batch.max_kv_len:
-            raise ValueError("mass: [n_seqs][at least max_kv_len]")
+        if tokens < batch.max_kv_len and tokens < batch.table_stride * geom.page_tokens:
+            raise ValueError("mass: [n_seqs][at least max_kv_len, or what the block table has room for]")
         before = None
         if mass_in is not None:
             if mass_in is not mass and (mass_in.dtype is not mass.dtype or mass_in.shape != mass.shape or mass_in.stride() != mass.stride()):

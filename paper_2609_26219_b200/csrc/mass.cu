@@ -128,6 +128,11 @@ struct MassPlan {
 constexpr uint64_t kMaxMassImages = 3ull << 29, kMaxMassPartial = 1ull << 28;
 uint64_t round16(uint64_t x) { return (x + 15) / 16 * 16; }
 
+// Tokens that a sequence can have: max_kv_len, or what its block table has room for.
+long long longest_sequence(const patchkv_geom* g, const patchkv_batch* b) {
+    return std::min((long long)b->max_kv_len, (long long)b->table_stride * g->page_tokens);
+}
+
 MassPlan plan_mass(const patchkv_geom* g, int tag, const patchkv_batch* b, int Hq, int window, int sinks) {
     MassPlan a;
     memset(&a, 0, sizeof(a));
@@ -135,13 +140,15 @@ MassPlan plan_mass(const patchkv_geom* g, int tag, const patchkv_batch* b, int H
     const bool pool = tag == PATCHKV_TAG_BF16;
     const bool shape = (D == 64 || D == 128) && g->page_tokens % kTile == 0 && (pool || g->group % 32 == 0);
     const long long cols = (long long)std::min(b->max_rows, b->n_rows) * (Hq / H);
-    a.bytes = round16((uint64_t)b->n_rows * Hq * 4);
-    if (!shape || cols == 0) return a;
+    const uint64_t any_bytes = round16((uint64_t)b->n_rows * Hq * 4);       // of the element-wise kernel, which unaligned queries go to
+    a.bytes = any_bytes;
+    const long long longest = longest_sequence(g, b);
+    if (!shape || cols == 0 || longest > 1 << 30) return a;
     if (cols > 16) {
         // Whole CTAs along the query vectors; where they leave SMs idle the tokens are split, two steps a piece at least.
         const long long tiles = (cols + 2 * kRowTile - 1) / (2 * kRowTile), ctas = tiles * H * b->n_seqs;
         if (ctas > 1 << 24 || cols > 1 << 30) return a;
-        const long long all = ((long long)b->max_kv_len + kRowTile - 1) / kRowTile;
+        const long long all = (longest + kRowTile - 1) / kRowTile;
         long long steps = all;                  // that the rows of a CTA see at most
         const long long cta_rows = std::min((long long)b->max_rows, 2ll * kRowTile / (Hq / H) + 2);
         if (window > 0 && !b->pos) steps = std::min(all, ((long long)window + sinks + cta_rows) / kRowTile + 3);
@@ -153,7 +160,7 @@ MassPlan plan_mass(const patchkv_geom* g, int tag, const patchkv_batch* b, int H
         a.chunk = (int)std::min<uint64_t>(tiles, std::max<uint64_t>(1, kMaxMassPartial / std::max<uint64_t>(tile_bytes, 1)));
         a.sums_bytes = (uint64_t)a.row_splits * b->n_rows * Hq * 8;
         a.ranges_bytes = (uint64_t)b->n_seqs * tiles * 16;
-        a.acc_bytes = a.chunk < tiles ? round16((uint64_t)b->n_seqs * b->max_kv_len * 8) : 0;
+        a.acc_bytes = a.chunk < tiles ? round16((uint64_t)b->n_seqs * longest * 8) : 0;
         a.partial_bytes = a.chunk * tile_bytes;
         // Images pay where several CTAs would make the same operands from codes.
         const uint64_t images = (uint64_t)all * H * b->n_seqs, image = 4ull * kRowTile * D;
@@ -162,7 +169,7 @@ MassPlan plan_mass(const patchkv_geom* g, int tag, const patchkv_batch* b, int H
             a.image_bytes = images * image;
             a.meta_bytes = images * 32;
         }
-        a.bytes = round16(a.sums_bytes) + a.ranges_bytes + a.acc_bytes + a.partial_bytes + a.image_bytes + a.meta_bytes;
+        a.bytes = std::max(any_bytes, round16(a.sums_bytes) + a.ranges_bytes + a.acc_bytes + a.partial_bytes + a.image_bytes + a.meta_bytes);
         return a;
     }
     a.nc = cols <= 4 ? 1 : cols <= 8 ? 2 : 4;
@@ -177,12 +184,12 @@ MassPlan plan_mass(const patchkv_geom* g, int tag, const patchkv_batch* b, int H
     a.target = b->n_seqs >= 2 * slots ? 0 : std::max(slots - b->n_seqs, (slots + 1) / 2);
     a.max_items = b->n_seqs + a.target;
     // Tiles that a sequence's rows can see: with a window, and rows one behind the other, not all of them.
-    long long tiles = ((long long)b->max_kv_len + kTile - 1) / kTile;
+    long long tiles = (longest + kTile - 1) / kTile;
     if (window > 0 && !b->pos) tiles = std::min(tiles, ((long long)window + b->max_rows + kTile - 1) / kTile + 1 + ((long long)sinks + kTile - 1) / kTile);
     a.tokens = (int)(tiles * kTile);
     a.items_bytes = ((uint64_t)b->n_seqs * 8 + 15) / 16 * 16;
     a.sums_bytes = (uint64_t)a.max_items * H * 4 * a.nc * 8;
-    a.bytes = a.items_bytes + a.sums_bytes + (uint64_t)b->n_seqs * H * a.cols * a.tokens * 4;
+    a.bytes = std::max(any_bytes, a.items_bytes + a.sums_bytes + (uint64_t)b->n_seqs * H * a.cols * a.tokens * 4);
     return a;
 }
 
@@ -221,7 +228,7 @@ extern "C" int patchkv_attention_mass(patchkv_ctx* ctx, const patchkv_geom* g, c
     if (a->mass_type == PATCHKV_MASS_U64 && a->decay != 0.0f && a->decay != 1.0f)
         return fail(ctx, PATCHKV_E_INVALID, "attention_mass: decay of whole masses must be 0 or 1");
     if (a->q_stride_row < 0 || a->q_stride_head < 0) return fail(ctx, PATCHKV_E_INVALID, "attention_mass: negative stride");
-    if (a->mass_stride < batch->max_kv_len) return fail(ctx, PATCHKV_E_INVALID, "attention_mass: mass_stride is smaller than max_kv_len");
+    if (a->mass_stride < longest_sequence(g, batch)) return fail(ctx, PATCHKV_E_INVALID, "attention_mass: mass_stride is smaller than the longest sequence");
     if (p.b.n_seqs == 0 || p.b.max_kv_len == 0) return PATCHKV_OK;
     const uintptr_t unit = a->mass_type == PATCHKV_MASS_U64 ? 7 : 3;
     if (!a->mass || (reinterpret_cast<uintptr_t>(a->mass) & unit) || (reinterpret_cast<uintptr_t>(a->mass_in) & unit))
@@ -233,6 +240,8 @@ extern "C" int patchkv_attention_mass(patchkv_ctx* ctx, const patchkv_geom* g, c
     const uint64_t need = patchkv_attention_mass_workspace_bytes(g, p.c.tag, batch, a->n_q_heads, a->window, a->sinks);
     if (need && (!a->workspace || (reinterpret_cast<uintptr_t>(a->workspace) & 15) || a->workspace_bytes < need))
         return fail(ctx, PATCHKV_E_INVALID, "attention_mass: workspace null, misaligned or too small");
+    p.b.max_kv_len = (int)longest_sequence(g, batch);           // sizes the launches
+    if (p.b.max_kv_len == 0) return PATCHKV_OK;
     p.q = static_cast<const uint16_t*>(a->q); p.out = nullptr;
     p.q_stride_row = a->q_stride_row; p.q_stride_head = a->q_stride_head;
     p.out_stride_row = p.out_stride_head = 0;
@@ -283,7 +292,7 @@ extern "C" int patchkv_attention_mass(patchkv_ctx* ctx, const patchkv_geom* g, c
         mass_sums_any_kernel<<<dim3(std::min(p.b.max_rows, p.b.n_rows), p.Hq, p.b.n_seqs), kMassThreads, 0, stream>>>(p, sums);
         PKV_CUDA(ctx, cudaGetLastError());
     }
-    mass_columns_any_kernel<<<dim3((p.b.max_kv_len + kMassThreads - 1) / kMassThreads, p.b.n_seqs), kMassThreads, 0, stream>>>(p, m, sums);
+    mass_columns_any_kernel<<<dim3((unsigned)((p.b.max_kv_len + (long long)kMassThreads - 1) / kMassThreads), p.b.n_seqs), kMassThreads, 0, stream>>>(p, m, sums);
     PKV_CUDA(ctx, cudaGetLastError());
     return PATCHKV_OK;
 }

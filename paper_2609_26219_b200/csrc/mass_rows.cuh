@@ -12,8 +12,7 @@
 // Keys are operands without a rounding: bf16 as they are, quantised ones as the sum of two fp16 matrices (22 bits), for two products per
 // 16 channels.  One fp16 matrix alone would put a logit 2^-12 of its terms off and the masses 1e-4.  With many tiles of vectors the operands are
 // laid out in the workspace first (images), as for the attention; else each CTA makes them from the pages, eight warps of it.
-// A step of two tiles takes 1024 cycles of products (quantised 2048) and as many exponentials as 2048 cycles of the exponential unit, of which
-// a part is computed on the fma pipe instead.
+// A step of two tiles takes 1024 cycles of products (quantised 2048) and 2048 cycles of the exponential unit.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -351,7 +350,9 @@ struct WeighRows {
     }
 
     // ---- the warpgroups: pair wg >> 1, columns 64 (wg & 1) .. + 63 of a place
-    static constexpr int kOnFma = 2;                                // of 16 pairs of exponentials, those that are computed (0 .. 16)
+    // Of 16 pairs of exponentials, those that are computed instead of left to the exponential unit (0 .. 16).  With 0, 2, 4 and 6 of them 8192
+    // rows over 8192 tokens (32 query heads) take 950, 1000, 1015 and 1060 us on 8-bit keys, and 749, 738, 760 and 810 us on bf16 keys.
+    static constexpr int kOnFma = FINE ? 0 : 2;
     __device__ __forceinline__ static void exp2_both(int c, f32x2 y, float& a, float& b) {
         if (c * kOnFma % 16 < kOnFma) {
             weigh_exp2_pair(y, a, b);

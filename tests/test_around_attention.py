@@ -74,15 +74,27 @@ def test_the_reference_turns_by_sums_of_angles():
         assert np.allclose((a ** 2).sum(-1), (x ** 2).sum(-1))
 
 
-def test_binding_refuses_what_it_can_see(pk):
-    with pytest.raises(ValueError):
-        pk._mass_rows(torch.zeros((2, 8), dtype=torch.float64), "mass", (torch.float32,), 2)
-    with pytest.raises(ValueError):
-        pk._mass_rows(torch.zeros((2, 8)), "mass", (torch.float32,), 3)
-    with pytest.raises(ValueError):
-        pk._table_rows(torch.zeros((2, 8), dtype=torch.int64), "keep", 2)
-    with pytest.raises(ValueError):
-        pk._counts(torch.zeros(4, dtype=torch.int32)[::2], "kept", 2)
-    assert pk._table_rows(torch.zeros((3, 8), dtype=torch.int32)[:, :5], "keep", 2) == (8, 5)
-    with pytest.raises(ValueError):
-        pk._table_rows(torch.zeros((3, 8), dtype=torch.int32)[:, :5], "src_table", 2, True)
+def test_workspace_holds_the_sums_of_the_element_wise_kernel(pk):
+    """Calls of one shape go to another kernel when their queries are not aligned: one workspace has to do for both, however loose the
+    bound on the rows is."""
+    lib = pk.lib()
+    for D in (64, 128, 80):
+        g = pk.make_geom(1, 2, D, D, 0, 1e4, 16, 16, 16 if D == 80 else 32)
+        for n_rows, max_rows in ((1, 1), (1000000, 1), (5000, 3), (5000, 900)):
+            assert lib.patchkv_attention_mass_workspace_bytes(g, 3, _batch(pk, 1, n_rows, max_rows, 64), 8, 0, 0) >= n_rows * 8 * 4
+
+
+def test_workspace_goes_by_the_block_table_where_that_is_smaller(pk):
+    g = pk.make_geom(1, 8, 128, 128, 0, 1e4, 16, 16, 32)
+    size = lambda rows, kv: pk.lib().patchkv_attention_mass_workspace_bytes(g, 3, _batch(pk, 1, rows, rows, kv), 32, 0, 0)
+    for rows in (1, 100):
+        assert 0 < size(rows, 64) == size(rows, 2 ** 31 - 1)          # four pages of 16 tokens
+
+
+def test_binding_refuses_host_tensors(pk):
+    """A host address in a kernel would be a fault of the GPU."""
+    f, i = torch.zeros((2, 8)), torch.zeros((2, 8), dtype=torch.int32)
+    for call in (lambda: pk._mass_rows(f, "mass", (torch.float32,), 2), lambda: pk._table_rows(i, "keep", 2), lambda: pk._counts(i[0], "kept", 2),
+                 lambda: pk._rows(torch.zeros((2, 2, 8), dtype=torch.bfloat16), "q")):
+        with pytest.raises(ValueError):
+            call()

@@ -296,6 +296,36 @@ def test_pages_and_lengths_out_of_range(pk, ctx, tag, rows):
     assert torch.all(got == -9)                                 # both sequences' entries are out of order or range
 
 
+@pytest.mark.parametrize("tag", [0, 3])
+@pytest.mark.parametrize("rows", [1, 40])
+def test_loose_bounds(pk, ctx, tag, rows):
+    """Bounds far above what there is: tokens up to 2^31 - 1, and packed rows that no sequence has, with aligned and unaligned queries."""
+    run = Run(pk, tag, 2, 8, 64, 16, 32, Case([150, 130], [rows, rows]), BF16, n_rows=2 * rows + 5000)
+    base = run.call(ctx, tokens=160)
+    run.batch.max_kv_len = 2 ** 31 - 1
+    assert torch.equal(run.call(ctx, tokens=160), base)
+    odd = torch.zeros(run.q.numel() + 1, dtype=BF16, device=DEV)[1:].view(run.q.shape)
+    odd.copy_(run.q)
+    got, (want, tol) = run.call(ctx, q=odd, tokens=160).double().cpu().numpy(), run.want(tokens=160)
+    for b, t in enumerate(run.case.kv):
+        assert np.all(np.abs(got[b, :t] - want[b, :t]) <= tol[b, :t]) and np.all(got[b, t:] == -9.0)
+
+
+def test_many_tiles_in_several_launches(pk, ctx):
+    """So many tiles of vectors, sequences and (by the bound) tokens that what the tiles give to the tokens does not fit the workspace's 256 MiB at
+    once: 100 MiB a tile, so two at a time."""
+    case = Case([500] + [20] * 399, [460] + [1] * 399)
+    run = Run(pk, 0, 1, 64, 64, 16, 32, case, BF16)
+    want, tol = run.want(tokens=500)
+    run.held["wide"] = run.held["table"].repeat(1, 65536 // (16 * run.table.shape[1]))
+    run.batch = pk.make_batch(row_start=run.held["start"], kv_len=run.held["kv"], block_table=run.held["wide"], n_rows=859, max_rows=460, max_kv_len=65536)
+    before = torch.rand((400, 65536), device=DEV)
+    got = run.call(ctx, tokens=65536, mass_in=before, decay=0.5)
+    for b, t in ((0, 500), (1, 20), (399, 20)):
+        x = got[b, :t].double().cpu().numpy() - 0.5 * before[b, :t].double().cpu().numpy()
+        assert np.all(np.abs(x - want[b, :t]) <= tol[b, :t] + 2.0 ** -23 * (np.abs(want[b, :t]) + 1)) and torch.all(got[b, t:] == -9)
+
+
 def test_rows_above_the_bound_are_left_out(pk, ctx):
     for rows in (3, 60):
         run = Run(pk, 0, 2, 4, 64, 16, 32, Case([100, 90], [rows, 2]), BF16)
