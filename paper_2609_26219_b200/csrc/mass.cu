@@ -125,6 +125,8 @@ struct MassPlan {
     uint64_t ranges_bytes, acc_bytes, partial_bytes, image_bytes, meta_bytes;
 };
 
+// Steps of an item of the row kernels: some of their waits take as long as an item (a million tokens, 30 ms), well below the limit of a wait.
+constexpr long long kMaxItemSteps = 8192;
 constexpr uint64_t kMaxMassImages = 3ull << 29, kMaxMassPartial = 1ull << 28;
 uint64_t round16(uint64_t x) { return (x + 15) / 16 * 16; }
 
@@ -144,8 +146,11 @@ MassPlan plan_mass(const patchkv_geom* g, int tag, const patchkv_batch* b, int H
     a.bytes = any_bytes;
     const long long longest = longest_sequence(g, b);
     if (!shape || cols == 0 || longest > 1 << 30) return a;
+    // Up to 16 columns the split kernel: 32 query heads over 8 KV heads, 32k tokens, 1, 2 and 4 rows take 27, 34 and 49 us of it on a bf16 pool
+    // and 22, 28 and 43 us on 4-bit pages; the row kernels take 60 and 68 us for any of them.
     if (cols > 16) {
-        // Whole CTAs along the query vectors; where they leave SMs idle the tokens are split, two steps a piece at least.
+        // Whole CTAs along the query vectors; where they leave SMs idle the tokens are split, two steps a piece at least.  (32 rows of 32 query
+        // heads over 8 KV heads, 32k tokens of a bf16 pool: 62 us split, 492 us on eight SMs.)
         const long long tiles = (cols + 2 * kRowTile - 1) / (2 * kRowTile), ctas = tiles * H * b->n_seqs;
         if (ctas > 1 << 24 || cols > 1 << 30) return a;
         const long long all = (longest + kRowTile - 1) / kRowTile;
@@ -153,7 +158,7 @@ MassPlan plan_mass(const patchkv_geom* g, int tag, const patchkv_batch* b, int H
         const long long cta_rows = std::min((long long)b->max_rows, 2ll * kRowTile / (Hq / H) + 2);
         if (window > 0 && !b->pos) steps = std::min(all, ((long long)window + sinks + cta_rows) / kRowTile + 3);
         a.row_tiles = (int)tiles;
-        a.row_splits = (int)std::max(1ll, std::min((long long)kSms / ctas, steps / 2));
+        a.row_splits = (int)std::max({1ll, std::min((long long)kSms / ctas, steps / 2), (steps + kMaxItemSteps - 1) / kMaxItemSteps});
         a.one = cols <= kRowTile;
         a.tokens = (int)(steps * kRowTile);
         const uint64_t tile_bytes = (uint64_t)b->n_seqs * H * a.tokens * 4;
@@ -162,9 +167,10 @@ MassPlan plan_mass(const patchkv_geom* g, int tag, const patchkv_batch* b, int H
         a.ranges_bytes = (uint64_t)b->n_seqs * tiles * 16;
         a.acc_bytes = a.chunk < tiles ? round16((uint64_t)b->n_seqs * longest * 8) : 0;
         a.partial_bytes = a.chunk * tile_bytes;
-        // Images pay where several CTAs would make the same operands from codes.
+        // Images pay where many CTAs would make the same operands from codes (8-bit keys, 8192 tokens, 32 query heads over 8 KV heads, with images and
+        // without: 74 and 58 us for 2 tiles, 154 and 150 for 8, 260 and 275 for 16, 430 and 465 for 32).
         const uint64_t images = (uint64_t)all * H * b->n_seqs, image = 4ull * kRowTile * D;
-        if (!pool && tiles >= 2 && images > 0 && images <= kMaxMassImages / image) {
+        if (!pool && tiles > 8 && images > 0 && images <= kMaxMassImages / image) {
             a.steps = (int)all;
             a.image_bytes = images * image;
             a.meta_bytes = images * 32;
@@ -175,12 +181,12 @@ MassPlan plan_mass(const patchkv_geom* g, int tag, const patchkv_batch* b, int H
     a.nc = cols <= 4 ? 1 : cols <= 8 ? 2 : 4;
     a.cols = (int)cols;
     const int warps = split_warps(pool, a.nc);
-    a.heads = 1;                                // heads of a CTA, and pieces of the batch, as the attention has them (but for the CTAs an SM)
+    a.heads = 1;                                // heads of a CTA, and pieces of the batch, as the attention has them
     for (int h = 2; h <= warps; h *= 2)
         if ((H + h - 1) / h * h <= (H + a.heads - 1) / a.heads * a.heads || h <= H) a.heads = h;
     a.groups = (H + a.heads - 1) / a.heads;
     a.warps_per_head = warps / a.heads;
-    const int slots = std::max(1, kWeighCtas * kSms / a.groups);
+    const int slots = std::max(1, kSms / a.groups);
     a.target = b->n_seqs >= 2 * slots ? 0 : std::max(slots - b->n_seqs, (slots + 1) / 2);
     a.max_items = b->n_seqs + a.target;
     // Tiles that a sequence's rows can see: with a window, and rows one behind the other, not all of them.

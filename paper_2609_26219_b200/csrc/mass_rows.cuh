@@ -6,13 +6,16 @@
 //   second pass   S = K Q^T, a lane per token; a thread adds up 2^(S - log2 of the row's sum) over the vectors of the CTA
 // In both the sum runs along a thread's own lane, so nothing is exchanged, and nothing comes behind the sums: the products of the next
 // steps run while a step is added up.  Four warpgroups do that, two (a pair) for each tile, half of the columns each, with two places
-// in TMEM for each pair; with one tile of vectors the pairs take turns at the steps.  (Two warpgroups, a tile each, took 3000 cycles a step:
-// two warps a scheduler do not hide one another's latencies.)  The second pass leaves a number for each token, head and CTA, which
+// in TMEM for each pair; with one tile of vectors the pairs take turns at the steps.  (Two warpgroups, a tile each, were as fast in
+// the first pass, where the exponential unit is the bound.)  The second pass leaves a number for each token, head and CTA, which
 // the last kernel adds up in an order that the arguments fix.
 // Keys are operands without a rounding: bf16 as they are, quantised ones as the sum of two fp16 matrices (22 bits), for two products per
 // 16 channels.  One fp16 matrix alone would put a logit 2^-12 of its terms off and the masses 1e-4.  With many tiles of vectors the operands are
 // laid out in the workspace first (images), as for the attention; else each CTA makes them from the pages, eight warps of it.
-// A step of two tiles takes 1024 cycles of products (quantised 2048) and 2048 cycles of the exponential unit.
+// A step of two tiles takes 1024 cycles of products (quantised 2048) and 2048 cycles of the exponential unit.  8192 rows of 32 query heads over
+// 8192 tokens, 8 KV heads of 128 channels: 459 and 478 us for the passes on quantised pages (1.2 PFLOP/s each, both matrices counted, at the
+// 1.67 GHz that the power limit leaves), 15 for the images, 15 for the last sum; 740 us in all on a bf16 pool.  Few rows are bound by the
+// way to the first product and by the keys' bytes: 32 rows over 32k tokens of a pool 22 and 25 us (67 MB each) and 8.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -414,11 +417,10 @@ struct WeighRows {
         return wait(&w.q_ready[i], uses & 1);
     }
 
-    // The sums with a step's 64 columns of the row added.
-    __device__ __forceinline__ static void add_step(uint32_t s_at, f32x2 factor2, float ref, const f32x2 (&sum2)[2], f32x2 (&total)[2]) {
+    // The sums of a step's 64 columns of the row.
+    __device__ __forceinline__ static void add_step(uint32_t s_at, f32x2 factor2, float ref, f32x2 (&total)[2]) {
         const f32x2 ref2 = pack2(-ref, -ref);
-        total[0] = sum2[0];
-        total[1] = sum2[1];
+        total[0] = total[1] = pack2(0.0f, 0.0f);
 #pragma unroll
         for (int q = 0; q < 2; q++) {
             float x[32];
@@ -493,15 +495,15 @@ struct WeighRows {
                 if (start) move_reference(s_at, factor, ref, sum2);
                 start = false;
                 f32x2 total[2];
-                add_step(s_at, factor2, ref, sum2, total);
+                add_step(s_at, factor2, ref, total);
                 float a, c;
                 unpack2(add2(total[0], total[1]), a, c);
                 if (__any_sync(0xFFFFFFFFu, a + c > 1.0e18f)) {
                     move_reference(s_at, factor, ref, sum2);
-                    add_step(s_at, factor2, ref, sum2, total);
+                    add_step(s_at, factor2, ref, total);
                 }
-                sum2[0] = total[0];
-                sum2[1] = total[1];
+                sum2[0] = add2(sum2[0], total[0]);              // (step by step: a long row's 32-bit sum rounds less often)
+                sum2[1] = add2(sum2[1], total[1]);
                 release(pair, u);
             }
             g += n;
@@ -770,8 +772,8 @@ __global__ void __launch_bounds__(kImageThreads) weigh_image_kernel(const __grid
 }
 
 // The sum over heads and tiles of vectors (grid: step of 128 tokens, sequence, CTA of a cluster): a thread per token, the cluster's groups of 128 threads
-// share the tiles, and its first CTA adds up (distributed shared memory): one CTA a step left half of the SMs idle, 37 us for 8192
-// rows over 8192 tokens.  64 bits: tens of thousands of numbers are added one by one.
+// share the tiles, and its first CTA adds up (distributed shared memory): with one CTA a step, and half of the SMs idle, 8192
+// rows over 8192 tokens of a pool take 761 us instead of 743 in all.  64 bits: tens of thousands of numbers are added one by one.
 constexpr int kWeighJoin = 1024, kWeighJoinCtas = 4;
 static __global__ void __launch_bounds__(kWeighJoin) weigh_rows_join_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ WeightParams m,
                                                                             const __grid_constant__ WeighRowsPlan pl) {

@@ -4,6 +4,9 @@
 // without its values: it leaves the logits, in fp32, and of each piece the column's sums.  The second adds the pieces' sums
 // up and, a token at a time, the weights of all heads and rows.  For 4-bit keys and 8 columns a logit written and read back costs 64 bytes
 // for a token and head where reading the keys again costs 72 and turning their codes into operands twice as well.
+// One CTA an SM: two of 64 registers a thread took 130 us where one of 128 takes 120 (8 x 64k tokens of 4-bit pages, 8 KV heads of 128, 64 query heads:
+// 85 us for the first pass, 302 MB of pages read and 134 MB of logits written at 5.1 TB/s, and 35 for the second).  The bound is the
+// instructions: some 225 for 16 tokens of a head and 8 columns, issued in two of three cycles.
 // Sums run in an order that the arguments fix: no atomics.
 #pragma once
 
@@ -21,9 +24,6 @@ struct WeighPlan {
 };
 template <int D>
 cudaError_t launch_weigh(const AttentionParams& p, const WeightParams& m, const WeighPlan& pl, int nc, int groups, cudaStream_t s);
-
-// Two CTAs an SM: one leaves the schedulers idle for 40 % of the cycles (8 x 64k tokens of 4-bit pages, 8 columns: KERNELTIMES).
-constexpr int kWeighCtas = 2;
 
 // Sums need no 16-bit weights here: a reference is moved only when fp32 runs short.
 constexpr float kWeighTop = 60.0f;
@@ -139,7 +139,7 @@ struct WeighKernel : SplitKernel<KF, KF, D, NC, STAGES, WARPS, G32> {
 };
 
 template <int KF, int D, int NC, int STAGES, int WARPS, bool G32>
-__global__ void __launch_bounds__(WARPS * 32, kWeighCtas) weigh_split_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ WeighPlan pl) {
+__global__ void __launch_bounds__(WARPS * 32, 1) weigh_split_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ WeighPlan pl) {
     using K = WeighKernel<KF, D, NC, STAGES, WARPS, G32>;
     extern __shared__ __align__(16) uint8_t smem[];
     pdl_trigger();
@@ -286,7 +286,8 @@ __global__ void __launch_bounds__(WARPS * 32, kWeighCtas) weigh_split_kernel(con
 }
 
 // Second pass (grid: CTAs of a sequence, sequence): a CTA takes every gridDim.x-th 256 tokens, a thread four tokens and a quarter of the columns.
-// Bound by the logits' bytes; the columns' sums are found once a CTA, so there are no more of those than fill the SMs.
+// Bound by the logits' bytes (134 MB in 35 us); the columns' sums are found once a CTA, so there are no more of those than fill the SMs (six
+// an SM).  A thread has eight logits of each token on their way (144 us a call with one, 131 with eight, 143 with sixteen).
 constexpr int kWeighTokens = 256, kWeighThreads = 256, kWeighColumns = 256;
 template <int NC>
 __global__ void __launch_bounds__(kWeighThreads, 4) weigh_join_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ WeightParams m,
@@ -296,7 +297,7 @@ __global__ void __launch_bounds__(kWeighThreads, 4) weigh_join_kernel(const __gr
     __shared__ float4 part[3][kWeighTokens / 4];
     pdl_trigger();
     pdl_wait();
-    const int s = blockIdx.y;
+    const int s = gridDim.y - 1 - blockIdx.y;                 // the last sequences' logits are still in L2 (129.5 for 130.9 us)
     int first, kv, rows, lo, hi, least;
     if (!sequence_rows(p, s, &first, &kv, &rows) || (int)blockIdx.x * kWeighTokens >= kv) return;
     const int quad = threadIdx.x & (kWeighTokens / 4 - 1), part_of = threadIdx.x / (kWeighTokens / 4);

@@ -326,6 +326,32 @@ def test_many_tiles_in_several_launches(pk, ctx):
         assert np.all(np.abs(x - want[b, :t]) <= tol[b, :t] + 2.0 ** -23 * (np.abs(want[b, :t]) + 1)) and torch.all(got[b, t:] == -9)
 
 
+@pytest.mark.parametrize("tag", [0, 3])
+def test_a_million_tokens(pk, ctx, tag):
+    """A block table that names the same eight pages over and over, seen by 38400 vectors: more CTAs along the vectors than SMs, and yet the tokens
+    are split.  Every token of a page then has the same mass each time.  Tolerance: as mass64's, and a row's sum is added up by 64 columns
+    and then step by step (12000 of them), so it is off by at most (64 + 12000) 2^-24."""
+    pages, times, D, share = 8, 2500, 64, 32
+    rows, period = 1200, 8 * 64
+    kv = period * times
+    run = Run(pk, tag, 1, share, D, 64, 32, Case([period], [1]), BF16)
+    q = random_rows(np.random.default_rng(5), rows, share, D, BF16, False).to(DEV)
+    ids = torch.from_numpy(run.table[:1, :pages].astype(np.int32)).to(DEV)
+    held = [torch.tensor([0, rows], dtype=torch.int32, device=DEV), torch.tensor([kv], dtype=torch.int32, device=DEV),
+            torch.full((rows,), kv - 1, dtype=torch.int32, device=DEV), ids.repeat(1, times).contiguous()]
+    run.batch = pk.make_batch(row_start=held[0], kv_len=held[1], block_table=held[3], pos=held[2], n_rows=rows, max_rows=rows, max_kv_len=kv)
+    run.case = Case([kv], [rows])
+    got = run.call(ctx, q=q, tokens=kv)[0].double().view(times, period)
+    run.case = Case([period], [1])
+    K, qq = torch.from_numpy(run.keys(0)[:, 0]).to(DEV), q.double().flatten(0, 1)
+    x = qq @ K.T * D ** -0.5
+    w = torch.softmax(x, 1) / times
+    d = (D + 64) * 2.0 ** -23 * (qq.abs() @ K.abs().T).amax(1, keepdim=True) * D ** -0.5
+    want = w.sum(0)
+    tol = (w * (torch.expm1(2 * d) + 2.0 ** -19)).sum(0) + want * ((rows * share / 64 + 64) + 64 + kv / 128) * 2.0 ** -24
+    assert torch.all((got - want).abs() <= tol)
+
+
 def test_rows_above_the_bound_are_left_out(pk, ctx):
     for rows in (3, 60):
         run = Run(pk, 0, 2, 4, 64, 16, 32, Case([100, 90], [rows, 2]), BF16)
