@@ -35,7 +35,7 @@ cudaError_t launch_weigh_columns(const AttentionParams& p, const WeightParams& m
     else if (kf == FMT_INT8) e = p.c.G == 32 ? launch_weigh_one<FMT_INT8, D, NC, true>(p, pl, groups, s) : launch_weigh_one<FMT_INT8, D, NC, false>(p, pl, groups, s);
     else e = p.c.G == 32 ? launch_weigh_one<FMT_INT4, D, NC, true>(p, pl, groups, s) : launch_weigh_one<FMT_INT4, D, NC, false>(p, pl, groups, s);
     if (e != cudaSuccess) return e;
-    const int blocks = (p.b.max_kv_len + kWeighTokens - 1) / kWeighTokens, ctas = std::max(1, 6 * 148 / p.b.n_seqs);
+    const int blocks = (p.b.max_kv_len + kWeighTokens - 1) / kWeighTokens, ctas = std::max(1, 4 * 148 / p.b.n_seqs);
     return launch_pdl(weigh_join_kernel<NC>, dim3(std::min(blocks, ctas), p.b.n_seqs), dim3(kWeighThreads), 0, s, p, m, pl);
 }
 template <int D>
