@@ -150,7 +150,7 @@ MassPlan plan_mass(const patchkv_geom* g, int tag, const patchkv_batch* b, int H
     // and 22, 28 and 43 us on 4-bit pages; the row kernels take 60 and 68 us for any of them.
     if (cols > 16) {
         // Whole CTAs along the query vectors; where they leave SMs idle the tokens are split, two steps a piece at least.  (32 rows of 32 query
-        // heads over 8 KV heads, 32k tokens of a bf16 pool: 62 us split, 492 us on eight SMs.)
+        // heads over 8 KV heads, 32k tokens of a bf16 pool: 58 us split, 490 us on eight SMs.)
         const long long tiles = (cols + 2 * kRowTile - 1) / (2 * kRowTile), ctas = tiles * H * b->n_seqs;
         if (ctas > 1 << 24 || cols > 1 << 30) return a;
         const long long all = (longest + kRowTile - 1) / kRowTile;

@@ -15,7 +15,7 @@
 // A step of two tiles takes 1024 cycles of products (quantised 2048) and 2048 cycles of the exponential unit.  8192 rows of 32 query heads over
 // 8192 tokens, 8 KV heads of 128 channels: 459 and 478 us for the passes on quantised pages (1.2 PFLOP/s each, both matrices counted, at the
 // 1.67 GHz that the power limit leaves), 15 for the images, 15 for the last sum; 740 us in all on a bf16 pool.  Few rows are bound by the
-// way to the first product and by the keys' bytes: 32 rows over 32k tokens of a pool 22 and 25 us (67 MB each) and 8.
+// way to the first product and by the keys' bytes: 32 rows over 32k tokens of a pool 22 and 25 us (67 MB each), 58 in all.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -771,8 +771,8 @@ __global__ void __launch_bounds__(kImageThreads) weigh_image_kernel(const __grid
     if (threadIdx.x < 8) pl.meta[(((long long)seq * pl.steps + step) * p.c.H + head) * 8 + threadIdx.x] = meta[threadIdx.x];
 }
 
-// The sum over heads and tiles of vectors (grid: step of 128 tokens, sequence, CTA of a cluster): a thread per token, the cluster's groups of 128 threads
-// share the tiles, and its first CTA adds up (distributed shared memory): with one CTA a step, and half of the SMs idle, 8192
+// The sum over heads and tiles of vectors (grid: step of 128 tokens, sequence, CTA of a cluster): a thread per token, the cluster's groups of 128 threads (no
+// more than there are tiles: 58 us for 62 with one tile) share the tiles, and its first CTA adds up (distributed shared memory): with one CTA a step, and half of the SMs idle, 8192
 // rows over 8192 tokens of a pool take 761 us instead of 743 in all.  64 bits: tens of thousands of numbers are added one by one.
 constexpr int kWeighJoin = 1024, kWeighJoinCtas = 4;
 static __global__ void __launch_bounds__(kWeighJoin) weigh_rows_join_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ WeightParams m,
@@ -783,13 +783,13 @@ static __global__ void __launch_bounds__(kWeighJoin) weigh_rows_join_kernel(cons
     pdl_trigger();
     cluster.barrier_arrive();
     pdl_wait();
-    const int s = blockIdx.y, step = blockIdx.x, r = threadIdx.x & 127, group = threadIdx.x >> 7;
+    const int s = blockIdx.y, step = blockIdx.x, r = threadIdx.x & 127, group = threadIdx.x >> 7, groups = blockDim.x >> 7;
     int first, kv, rows;
     const bool ordered = sequence_rows(p, s, &first, &kv, &rows) && step * kRowTile < kv;
     double sum = 0.0;
     if (ordered) {
         const int tiles = (min(rows, p.b.max_rows) * p.share + 2 * kRowTile - 1) / (2 * kRowTile), end = min(tiles, pl.chunk + pl.chunk_tiles);
-        for (int tile = pl.chunk + group + kWeighJoin / 128 * rank; tile < end; tile += kWeighJoin / 128 * ctas) {
+        for (int tile = pl.chunk + group + groups * rank; tile < end; tile += groups * ctas) {
             const int4 range = pl.ranges[(long long)s * pl.tiles + tile];
             const int v = step < range.x ? step : step - range.y + range.x;
             if (!(step < range.x || (step >= range.y && v < range.z))) continue;
@@ -804,7 +804,7 @@ static __global__ void __launch_bounds__(kWeighJoin) weigh_rows_join_kernel(cons
     __syncthreads();
     cluster.barrier_wait();                                     // the first CTA is there to be written to
     if (group == 0) {
-        for (int i = 1; i < kWeighJoin / 128; i++) sum += part[i * 128 + r];
+        for (int i = 1; i < groups; i++) sum += part[i * 128 + r];
         cluster.map_shared_rank(&whole[0][0], 0)[rank * kRowTile + r] = sum;
     }
     cluster.sync();

@@ -33,7 +33,7 @@ cudaError_t launch_weigh_rows_passes(const AttentionParams& p, const WeightParam
         memset(&cfg, 0, sizeof(cfg));
         const unsigned steps = (p.b.max_kv_len + kRowTile - 1) / kRowTile;
         const unsigned ctas = pl.chunk_tiles > kWeighJoin / 128 && (long long)steps * p.b.n_seqs * kWeighJoinCtas <= 2 * 148 ? kWeighJoinCtas : 1;
-        cfg.gridDim = dim3(steps, p.b.n_seqs, ctas); cfg.blockDim = dim3(kWeighJoin); cfg.stream = stream;
+        cfg.gridDim = dim3(steps, p.b.n_seqs, ctas); cfg.blockDim = dim3(128 * std::min(pl.chunk_tiles, kWeighJoin / 128)); cfg.stream = stream;
         cudaLaunchAttribute attr[2];
         attr[0].id = cudaLaunchAttributeClusterDimension;
         attr[0].val.clusterDim.x = 1; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = ctas;
