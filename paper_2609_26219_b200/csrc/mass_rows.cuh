@@ -771,9 +771,10 @@ __global__ void __launch_bounds__(kImageThreads) weigh_image_kernel(const __grid
     if (threadIdx.x < 8) pl.meta[(((long long)seq * pl.steps + step) * p.c.H + head) * 8 + threadIdx.x] = meta[threadIdx.x];
 }
 
-// The sum over heads and tiles of vectors (grid: step of 128 tokens, sequence, CTA of a cluster): a thread per token, the cluster's groups of 128 threads (no
-// more than there are tiles: 58 us for 62 with one tile) share the tiles, and its first CTA adds up (distributed shared memory): with one CTA a step, and half of the SMs idle, 8192
-// rows over 8192 tokens of a pool take 761 us instead of 743 in all.  64 bits: tens of thousands of numbers are added one by one.
+// The sum over heads and tiles of vectors (grid: step of 128 tokens, sequence, CTA of a cluster): a thread per token, the cluster's groups of 128 threads
+// (no more than there are tiles: 58 us for 62 with one tile) share the tiles, and its first CTA adds up (distributed shared memory): with
+// one CTA a step, and half of the SMs idle, 8192 rows over 8192 tokens of a pool take 761 us instead of 743 in all.  64 bits: tens of
+// thousands of numbers are added one by one.
 constexpr int kWeighJoin = 1024, kWeighJoinCtas = 4;
 static __global__ void __launch_bounds__(kWeighJoin) weigh_rows_join_kernel(const __grid_constant__ AttentionParams p, const __grid_constant__ WeightParams m,
                                                                             const __grid_constant__ WeighRowsPlan pl) {

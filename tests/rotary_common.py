@@ -35,9 +35,3 @@ def rotation_tolerance(x: np.ndarray, theta: np.ndarray, style: int, factor: flo
     least = 2.0 ** -25 if out_type == torch.float16 else 1e-38
     rest = np.where(big > 0, u * big * 1.01 + 4 * 2.0 ** -24 * big + least, 0.0)      # channels that are not rotated: exact
     return rest
-
-
-def copies_only(x: np.ndarray, n: int) -> np.ndarray:
-    m = np.ones(x.shape, bool)
-    m[..., :2 * n] = False
-    return m
