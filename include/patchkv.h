@@ -512,6 +512,7 @@ PATCHKV_API uint64_t patchkv_attention_workspace_bytes(const patchkv_geom* geom,
  * is rotated.  Queries, and keys of a bf16 pool, are formed in fp32 with c and s rounded to fp32, and rounded once; channels behind
  * rotary_dim are copied bit for bit.  Keys of quantised pages are formed in double and quantised from there as
  * patchkv_cache_append quantises, without a rounding in between; values are quantised from their 16 bits.
+ * A pool in which two heads, tokens or pages, or K and V, lie in one place is refused, here and by patchkv_cache_gather.
  * Rows, positions and skipped rows as for patchkv_cache_append; the q_out of a skipped row, and of a row of no sequence, is left
  * as it was.  One launch, no allocation, no workspace; can be captured (inv_freq is read by the call, not by its replays).
  * Every geometry is taken.  The fast kernel wants D a power of two from 16 to 256, rotary_dim a multiple of 16,

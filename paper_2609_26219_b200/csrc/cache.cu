@@ -2,6 +2,8 @@
 // live-cache calls share.
 #include <math.h>
 
+#include <algorithm>
+
 #include "cache_rows.cuh"
 
 namespace patchkv {
@@ -253,6 +255,20 @@ int fill_pool(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, const pa
     c->n_pages = q->n_pages; c->H = g->n_kv_heads; c->D = g->head_dim; c->P = g->page_tokens; c->G = g->group;
     c->P_shift = log2_exact(g->page_tokens);
     c->tag = PATCHKV_TAG_BF16;
+    return PATCHKV_OK;
+}
+
+int check_written_pool(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, const patchkv_pool* q) {
+    const std::string w(who);
+    if (q->k_base == q->v_base) return fail(ctx, PATCHKV_E_INVALID, w + ": K and V of the pool are in one place");
+    struct Axis { long long n, stride; } axes[3] = {{g->n_kv_heads, q->stride_head}, {g->page_tokens, q->stride_token}, {q->n_pages, q->stride_page}};
+    std::sort(axes, axes + 3, [](const Axis& a, const Axis& b) { return a.stride < b.stride; });
+    __int128 extent = g->head_dim;                          // of what lies inside an axis
+    for (const Axis& x : axes) {
+        if (x.n == 1) continue;
+        if (x.stride < extent) return fail(ctx, PATCHKV_E_INVALID, w + ": heads, tokens or pages of the pool overlap");
+        extent += (__int128)(x.n - 1) * x.stride;
+    }
     return PATCHKV_OK;
 }
 

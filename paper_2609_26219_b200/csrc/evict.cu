@@ -452,6 +452,7 @@ int cache_gather(patchkv_ctx* ctx, const patchkv_geom* g, const patchkv_pool* po
     if ((pool != nullptr) == (cache != nullptr)) return fail(ctx, PATCHKV_E_INVALID, "cache_gather: give a pool or a cache, one of the two");
     int rc = check_live_geometry(ctx, "cache_gather", g, layer);
     if (rc == PATCHKV_OK) rc = pool ? fill_pool(ctx, "cache_gather", g, pool, layer, &p.c) : fill_cache(ctx, "cache_gather", g, cache, layer, &p.c);
+    if (rc == PATCHKV_OK && pool) rc = check_written_pool(ctx, "cache_gather", g, pool);
     if (rc != PATCHKV_OK) return rc;
     if (!a || a->struct_size != sizeof(patchkv_gather_args)) return fail(ctx, PATCHKV_E_INVALID, "cache_gather: null args or wrong struct_size");
     if (a->n_seqs < 0 || a->max_keep < 0 || a->src_stride < 0 || a->dst_stride < 0) return fail(ctx, PATCHKV_E_INVALID, "cache_gather: negative count");

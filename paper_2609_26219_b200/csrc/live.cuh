@@ -76,6 +76,8 @@ __device__ __forceinline__ float scale_at(const uint8_t* scales, unsigned long l
 int fill_batch(patchkv_ctx* ctx, const char* who, const patchkv_batch* b, BatchDev* out);
 int fill_cache(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, const patchkv_qpool* q, int layer, CacheDev* out);
 int fill_pool(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, const patchkv_pool* q, int layer, CacheDev* out);
+// A pool that is written: no two of its rows in one place.
+int check_written_pool(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, const patchkv_pool* q);
 int check_live_geometry(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, int layer);
 // Whether two of the n * H vectors of D elements at these strides share an element (rows within heads or heads within rows).
 bool rows_overlap(long long n, long long H, long long D, long long stride_row, long long stride_head);

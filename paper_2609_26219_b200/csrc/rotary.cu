@@ -337,6 +337,7 @@ extern "C" int patchkv_rotary_append(patchkv_ctx* ctx, const patchkv_geom* g, co
     if (rc == PATCHKV_OK) rc = fill_frequencies(ctx, "rotary_append", g, &p.f);
     if (rc == PATCHKV_OK) rc = fill_batch(ctx, "rotary_append", batch, &p.b);
     if (rc == PATCHKV_OK) rc = pool ? fill_pool(ctx, "rotary_append", g, pool, layer, &p.c) : fill_cache(ctx, "rotary_append", g, cache, layer, &p.c);
+    if (rc == PATCHKV_OK && pool) rc = check_written_pool(ctx, "rotary_append", g, pool);
     if (rc != PATCHKV_OK) return rc;
     if (!a || a->struct_size != sizeof(patchkv_rotary_args)) return fail(ctx, PATCHKV_E_INVALID, "rotary_append: null args or wrong struct_size");
     if (a->type != PATCHKV_ROWS_BF16 && a->type != PATCHKV_ROWS_F16) return fail(ctx, PATCHKV_E_INVALID, "rotary_append: unknown row type");

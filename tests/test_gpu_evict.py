@@ -281,6 +281,11 @@ def test_gather_refusals(pk, ctx):
         ctx.cache_gather(geom, cache, 0, args[0].long(), *args[1:])
     with pytest.raises(ValueError):
         ctx.cache_gather(geom, cache, 0, args[0], args[1].long(), *args[2:])
+    x = torch.zeros((4, 16, 2, 64), dtype=BF16, device=DEV)
+    for v, strides in ((x, (0, 2048, 128, 64)), (x.clone(), (0, 2048, 64, 64)), (x.clone(), (0, 128, 128, 64))):
+        with pytest.raises(pk.PatchKVError) as e:
+            ctx.cache_gather(geom, pk.make_pool(x, v, 4, strides), 0, *args)
+        assert e.value.code == pk.E_INVALID
     a = pk.GatherArgs(C.sizeof(pk.GatherArgs), 1, 1, 0, 1, 1, None, 1)
     assert pk.lib().patchkv_cache_gather(ctx._h, geom, None, cache, 0, a, None) == pk.E_INVALID
     assert pk.lib().patchkv_cache_gather(ctx._h, geom, None, None, 0, a, None) == pk.E_INVALID

@@ -225,6 +225,9 @@ def test_refusals(pk, ctx):
     for bad in (dict(q=q.half()), dict(q=q, q_out=q[:, :2]), dict(q_out=q), dict(q=q, rope_pos=torch.zeros(1, dtype=torch.int32, device=DEV))):
         with pytest.raises(ValueError):
             ctx.rotary_append(ok(), pool, 0, batch, k, k, **bad)
+    for strides in ((0, P * H * D, H * D, 0), (0, P * H * D, D, D), (0, H * D, H * D, D), (0, 0, H * D, D), (0, P * H * D - 8, H * D, D), (0, D, H * D, 2 * D)):
+        refused(pk.E_INVALID, ok(), pk.make_pool(kp, kp.clone(), n_pages, strides), 0, batch, k, k)
+    refused(pk.E_INVALID, ok(), pk.make_pool(kp, kp, n_pages, (0, P * H * D, H * D, D)), 0, batch, k, k)
     lib = pk.lib()
     a = pk.RotaryArgs(C.sizeof(pk.RotaryArgs))
     assert lib.patchkv_rotary_append(ctx._h, ok(), None, None, 0, batch, a, None) == pk.E_INVALID
