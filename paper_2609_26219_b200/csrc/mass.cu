@@ -63,9 +63,9 @@ __global__ void __launch_bounds__(kMassThreads) mass_sums_any_kernel(const Atten
         if (!sees(p, pos, t)) continue;
         KeyPlace k;
         if (!find_key(p, s, t, h, &k)) { latch(p.status); continue; }
-        const float x = logit(p, k, q), to = fmaxf(m, x);
-        if (to == -INFINITY) continue;
-        l = l * exp2f(m - to) + exp2f(x - to);
+        const float x = logit(p, k, q), to = fmaxf(m, x);      // (a NaN leaves the maximum as it is, and stays in the sum)
+        if (x == -INFINITY) continue;
+        l = x != x ? x : l * exp2f(m - to) + exp2f(x - to);
         m = to;
     }
     red[threadIdx.x] = make_float2(m, l);
@@ -73,8 +73,7 @@ __global__ void __launch_bounds__(kMassThreads) mass_sums_any_kernel(const Atten
     if (threadIdx.x != 0) return;
     for (int i = 0; i < kMassThreads; i++) m = fmaxf(m, red[i].x);
     l = 0.0f;
-    if (m != -INFINITY)
-        for (int i = 0; i < kMassThreads; i++) l += red[i].y * exp2f(red[i].x - m);
+    for (int i = 0; i < kMassThreads; i++) l += red[i].x == m ? red[i].y : red[i].y * exp2f(red[i].x - m);      // (m may be -infinity)
     sums[(long long)r * p.Hq + hq] = l == 0.0f ? INFINITY : m + log2f(l);
 }
 
