@@ -59,6 +59,7 @@ struct WeighBars {
     uint64_t q_ready[2];                                            // [tile] the queries are there, and what goes with them
     uint64_t q_free;                                                // the products of an item are done
     uint64_t mate_done[2];                                          // [pair] its other warpgroups are through with an item
+    uint64_t second_done;                                           // first pass: so is the whole of the second pair, with an item of two tiles
     uint64_t s_full[2][2], s_empty[2][2], k_full[4], k_empty[4];    // [pair][place in TMEM]; stages of the ring of keys
     uint64_t part_full[4][4];                                       // second pass: [warpgroup][unit mod 4] its sum is there
     uint64_t drained;
@@ -322,6 +323,9 @@ struct WeighRows {
                 if (!wait(&w.q_ready[i], uses[i] & 1)) return;
                 uses[i]++;
             }
+            // The steps of an item of one tile go to the first pair alone.  The second may not have read the last steps' `absent` of the
+            // item before, which the producers, eight steps on, write over.  (In the second pass the first pair waits for its sums.)
+            if (!COLUMNS && !ONE && it.tiles == 1 && uses[1] > 0 && !wait(&w.second_done, (uses[1] - 1) & 1)) return;
             const int n = steps();
 #pragma unroll 1
             for (int j = 0; j < n; j++, g++) {
@@ -523,6 +527,7 @@ struct WeighRows {
                     ref = to;
                 }
                 if (m < it.m_end) pl.sums[(long long)it.split * p.b.n_rows * p.Hq + vector_index(m)] = make_float2(ref, sum);
+                if (!ONE && pair == 1) arrive(&w.second_done);
             }
             uses++;
         }
@@ -671,6 +676,7 @@ __global__ void __launch_bounds__(weigh_threads(IMAGE), 1) weigh_rows_kernel(con
             for (int k = 0; k < 4; k++) mbar_init(&bars.part_full[i][k], 4);
         }
         mbar_init(&bars.q_free, 1);
+        mbar_init(&bars.second_done, 4);
         mbar_init(&bars.drained, 1);
         bars.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");

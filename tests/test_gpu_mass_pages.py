@@ -1,0 +1,70 @@
+"""patchkv_attention_mass with pages out of range, by the kernels of many query vectors: tokens that a row sees on such a page are left out of
+its sum, get no weight, and latch PATCHKV_E_BOUNDS; all others have the weights of the 64-bit formula."""
+import numpy as np
+import pytest
+import torch
+
+from live_common import BF16, Case
+from test_gpu_mass import DEV, Run
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def pk():
+    from paper_2609_26219_b200 import build, binding
+    build.build()
+    return binding
+
+
+@pytest.fixture(scope="module")
+def ctx(pk):
+    c = pk.Context(device=0)
+    yield c
+    c.close()
+
+
+def lose(run, pages):
+    """Takes pages (sequence, logical page) out of the block table; the keys of their tokens are not there then."""
+    table = run.held["table"].cpu().numpy()
+    for s, page in pages:
+        table[s, page] = -1 if (s + page) & 1 else 2 ** 30
+    run.held["table"].copy_(torch.from_numpy(table))
+    run.lost = set(pages)
+
+
+def check(run, ctx, window=0, sinks=0, status=0, sequences=None):
+    """Tolerance: as mass64's."""
+    got = run.call(ctx, window, sinks, status=status).double().cpu().numpy()
+    q, share, scale, D, r = run.q.double().cpu().numpy(), run.Hq // run.H, run.D ** -0.5, run.D, 0
+    for s, (t, positions) in enumerate(zip(run.case.kv, run.case.positions())):
+        R = len(positions)
+        assert np.all(got[s, t:] == -9.0)
+        if sequences is None or s in sequences:
+            K, gone = run.keys(s), np.array([(s, j // run.P) in run.lost for j in range(t)])
+            j, p = np.arange(t)[None], np.array(positions).reshape(-1, 1)
+            see = (j <= p) & ((window == 0) | (p - j < window) | (j < sinks)) & ~gone
+            K = np.where((see.any(0))[:, None, None], K, 0.0)
+            live, want, tol = see.any(1), np.zeros(t), np.zeros(t)
+            for h in range(run.Hq):
+                kk, qq = K[:, h // share], q[r:r + R, h]
+                x = np.where(see, qq @ kk.T * scale, -np.inf)
+                w = np.where(see, np.exp(x - np.where(live, x.max(1), 0.0)[:, None]), 0.0)
+                w /= np.where(live, w.sum(1), 1.0)[:, None]
+                big = scale * np.where(see, np.abs(qq) @ np.abs(kk).T, 0.0).max(1)[:, None]
+                want += w.sum(0)
+                tol += (w * (np.expm1(2 * (D + 64) * 2.0 ** -23 * big) + 2.0 ** -19)).sum(0)
+            tol += want * (R * run.Hq / 64 + 64) * 2.0 ** -24 + R * run.Hq * 2.0 ** -120
+            assert np.all(np.abs(got[s, :t] - want) <= tol), (s, np.flatnonzero(np.abs(got[s, :t] - want) > tol))
+            assert np.all(got[s, :t][gone] == 0)
+        r += R
+
+
+@pytest.mark.parametrize("tag", [0, 3])
+def test_one_tile_behind_two(pk, ctx, tag):
+    """More sequences than SMs, so that a CTA takes those of two tiles of vectors first and then those of one, each with other pages missing."""
+    n = 300
+    case = Case([1400] * n, [200] * 148 + [60] * (n - 148))
+    run = Run(pk, tag, 1, 1, 64, 16, 32, case, BF16)
+    lose(run, [(s, page) for s in range(n) for page in ((73, 70, 3) if s < 148 else (0, 20 + s % 40))])
+    check(run, ctx, status=pk.E_BOUNDS, sequences={0, 1, 70, 147, 148, 149, 222, 295, 296, 299})
