@@ -625,14 +625,16 @@ struct WeighRows {
                 tc_after();
                 const uint4 absent = lds128(smem_u32(w.absent[(g + j) & 7]));
                 const bool gaps = (absent.x | absent.y | absent.z | absent.w) != 0;
-                if (gaps || !whole(t0)) {
+                bool masked = gaps || !whole(t0);
+                if (!masked) {
+                    sum = kPool || p.f16 ? column_sum<false, true>(s_at, from, 0ull) : column_sum<false, false>(s_at, from, 0ull);
+                    // (an infinite key times the zeros behind the last vector is NaN, which is nobody's)
+                    masked = __any_sync(0xFFFFFFFFu, sum != sum);
+                }
+                if (masked) {
                     const uint32_t word = r < 32 ? absent.x : r < 64 ? absent.y : r < 96 ? absent.z : absent.w;
                     const bool there = t < kv && !(word >> (r & 31) & 1u);
                     sum = column_sum<true, kPool>(s_at, from, there ? seeing(from, t) : 0ull);
-                } else if (kPool || p.f16) {
-                    sum = column_sum<false, true>(s_at, from, 0ull);
-                } else {
-                    sum = column_sum<false, false>(s_at, from, 0ull);
                 }
                 release(pair, u);
                 if (leader) {

@@ -76,15 +76,17 @@ ROWS = [1, 3, 30, 50]
 @pytest.mark.parametrize("rows", ROWS)
 @pytest.mark.parametrize("geometry", list(GEOMETRIES))
 @pytest.mark.parametrize("token", [3, 130, 299])
-@pytest.mark.parametrize("value", ["inf", "nan"])
+@pytest.mark.parametrize("value", ["inf", "-inf", "nan"])
 def test_keys_of_the_pool(pk, ctx, rows, geometry, token, value):
-    """Queries above zero in the channel: plus infinity gives NaN to all that the row sees, as a NaN does."""
+    """Queries above zero in the channel: plus infinity gives NaN to all that the row sees, minus infinity takes the token's weight away."""
     def spoil(run):
         run.kp[run.table[0, token // run.P], token % run.P, 0, 7] = float(value)
 
     run = Run(pk, 0, *GEOMETRIES[geometry], Case([300, 80], [rows, rows]), BF16, k_edit=spoil)
     run.q[:, :, 7] = run.q[:, :, 7].abs() + 0.5
-    check(run, ctx)
+    want = check(run, ctx)
+    if value == "-inf" and run.H == 1:
+        assert want[0][token] == 0 and not np.isnan(want[0]).any()
 
 
 @pytest.mark.parametrize("tag", [1, 3])
