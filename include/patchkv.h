@@ -546,7 +546,9 @@ PATCHKV_API int patchkv_rotary_append(patchkv_ctx* ctx, const patchkv_geom* geom
  *   mass[b][j] <- decay * mass_in[b][j] + sum over rows and query heads of softmax_j(scale * q . k_j)
  * for every token j < kv_len[b] (a sequence without rows has an empty sum); entries at and behind kv_len[b] are left as they were.
  * What a row sees, and what is left out or skipped, is as for patchkv_attention with the
- * same arguments; a row that sees no token adds nothing; a NaN or an infinity in a query makes the masses that it sees NaN.
+ * same arguments; a row that sees no token adds nothing; a NaN or an infinity in a query makes the masses that it sees NaN.  A key that
+ * gives a row the logit NaN or +infinity does so, too; the logit -infinity is a weight of 0, or NaN where the row has no other (logits
+ * below -3e38 may count as -infinity, and an infinite scale of quantised keys may give NaN either way).
  * Sums are formed in fp32 in an order that the arguments fix, so that equal calls give equal bits.
  *   PATCHKV_MASS_F32: decay any finite number; 0 does not read mass_in, and neither does a null mass_in.
  *   PATCHKV_MASS_U64: units of 2^-24 as patchkv_select_repair_tokens reads them (kind TOKEN_MASS); the call's sum is rounded

@@ -45,8 +45,8 @@ __device__ __forceinline__ void load_query(const AttentionParams& p, int r, int 
     for (int c = threadIdx.x; c < p.c.D; c += kMassThreads) q[c] = p.f16 ? half_bits_to_float(qs[c]) : bf16_bits_to_float(qs[c]);
 }
 
-// One CTA per (row, query head): log2 of the sum of 2^logit over the tokens that the row sees; infinity for a row that sees none, so that
-// its weights are zero.
+// One CTA per (row, query head): log2 of the sum of 2^logit over the tokens that the row sees; NaN for a row whose logits are all minus
+// infinity, infinity for one that sees none.
 __global__ void __launch_bounds__(kMassThreads) mass_sums_any_kernel(const AttentionParams p, float* sums) {
     __shared__ float q[PATCHKV_MAX_ATTENTION_DIM];
     __shared__ float2 red[kMassThreads];
@@ -59,22 +59,24 @@ __global__ void __launch_bounds__(kMassThreads) mass_sums_any_kernel(const Atten
     load_query(p, r, hq, q);
     __syncthreads();
     float m = -INFINITY, l = 0.0f;
+    bool saw = false;
     for (int t = threadIdx.x; t <= min(pos, kv - 1); t += kMassThreads) {
         if (!sees(p, pos, t)) continue;
         KeyPlace k;
         if (!find_key(p, s, t, h, &k)) { latch(p.status); continue; }
         const float x = logit(p, k, q), to = fmaxf(m, x);      // (a NaN leaves the maximum as it is, and stays in the sum)
+        saw = true;
         if (x == -INFINITY) continue;
         l = x != x ? x : l * exp2f(m - to) + exp2f(x - to);
         m = to;
     }
     red[threadIdx.x] = make_float2(m, l);
-    __syncthreads();
+    saw = __syncthreads_or(saw);
     if (threadIdx.x != 0) return;
     for (int i = 0; i < kMassThreads; i++) m = fmaxf(m, red[i].x);
     l = 0.0f;
     for (int i = 0; i < kMassThreads; i++) l += red[i].x == m ? red[i].y : red[i].y * exp2f(red[i].x - m);      // (m may be -infinity)
-    sums[(long long)r * p.Hq + hq] = l == 0.0f ? INFINITY : m + log2f(l);
+    sums[(long long)r * p.Hq + hq] = l != 0.0f ? m + log2f(l) : saw ? NAN : INFINITY;
 }
 
 // A thread per token: the weights of all rows and heads, in order.

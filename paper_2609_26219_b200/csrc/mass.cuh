@@ -14,6 +14,12 @@ struct WeightParams {
     int32_t u64;
 };
 
+// Whether the row at position pos sees a token at all.
+__device__ __forceinline__ bool sees_some(const AttentionParams& p, int pos, int kv) {
+    const int end = min(pos, kv - 1);
+    return end >= 0 && (p.window == 0 || pos - end < p.window || p.sinks > 0);
+}
+
 // The call's sum for token t of sequence s, onto what was there.
 __device__ __forceinline__ void store_mass(const AttentionParams& p, const WeightParams& m, int s, int t, float sum) {
     const long long at = (long long)s * m.stride + t;

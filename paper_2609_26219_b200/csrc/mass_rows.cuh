@@ -397,7 +397,8 @@ struct WeighRows {
             float factor = b.load_query(i, r, live, row, hq);
             w.factor[128 * i + r] = factor;
             if (COLUMNS) {
-                // -log2 of the row's sum; minus infinity for a row that sees nothing and for vectors behind the last
+                // -log2 of the row's sum; NaN where all of its logits are minus infinity, minus infinity for a row that sees nothing and for
+                // vectors behind the last
                 float low = -INFINITY;
                 if (live) {
                     const long long vec = vector_index(m), step = (long long)p.b.n_rows * p.Hq;
@@ -410,6 +411,7 @@ struct WeighRows {
                         sum = fmaf(z.y, fast_exp2(z.x - top), sum);
                     }
                     if (sum != 0.0f) low = -(top + log2f(sum));
+                    else if (sees_some(p, w.pos[128 * i + r], it.kv)) low = __uint_as_float(0x7FC00000u);
                 }
                 if (factor != factor) factor = p.scale_log2;        // (of zeros)
                 w.scale[128 * i + r] = live ? factor : 0.0f;

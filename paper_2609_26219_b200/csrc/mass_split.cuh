@@ -130,7 +130,7 @@ struct WeighKernel : SplitKernel<KF, KF, D, NC, STAGES, WARPS, G32> {
         for (int c = 0; c < NC; c++) { x[c][0] = finite_low(x[c][0] * this->factor[c]); x[c][1] = finite_low(x[c][1] * this->factor[c]); }
     }
     // -infinity stands for a token that the row does not see; one that it sees, of an infinite key or query, has the weight that its
-    // row's sum gives it (NaN where that is NaN).
+    // row's sum gives it (NaN where that is NaN).  A row that has no other logits keeps its first reference: weigh_join_kernel makes its sum NaN.
     __device__ __forceinline__ static float finite_low(float x) {
         float y;
         asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(x), "f"(kNoMax));
@@ -332,7 +332,8 @@ __global__ void __launch_bounds__(kWeighThreads, 4) weigh_join_kernel(const __gr
                 sum = fmaf(sum, fast_exp2(top - to), z.y * fast_exp2(z.x - to));
                 top = to;
             }
-            column[j] = make_float2(sum == 0.0f ? INFINITY : top + log2f(sum), __int_as_float(h * pl.cols + c));
+            const float total = sum == 0.0f ? INFINITY : top == kNoMax ? __uint_as_float(0x7FC00000u) : top + log2f(sum);
+            column[j] = make_float2(total, __int_as_float(h * pl.cols + c));
         }
         __syncthreads();
     };

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from live_common import BF16, Case
+from live_common import BF16, F16, Case
 from test_gpu_mass import DEV, Run
 
 pytestmark = pytest.mark.gpu
@@ -73,6 +73,40 @@ GEOMETRIES = {"fast_64": (1, 4, 64, 16, 32), "fast_128": (2, 8, 128, 16, 32), "a
 ROWS = [1, 3, 30, 50]
 
 
+def one_sign(run):
+    """Every key below zero in every channel, so that an infinite query has logits of minus infinity (or of plus infinity) alone."""
+    if run.tag == 0:
+        run.kp[:] = -run.kp.abs() - 0.25
+    else:
+        for page in run.pages:
+            run.lay.split(page)[0][:] = 0xFF                # code -1
+
+
+@pytest.mark.parametrize("tag", [0, 1, 3])
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("geometry", list(GEOMETRIES))
+@pytest.mark.parametrize("value", ["inf", "-inf", "nan"])
+def test_queries(pk, ctx, tag, rows, geometry, value):
+    for dtype in (BF16, F16) if tag else (BF16,):
+        for edit in (None, one_sign):
+            run = Run(pk, tag, *GEOMETRIES[geometry], Case([300, 80], [rows, rows]), dtype, k_edit=edit)
+            run.q[rows - 1, 2, 5] = float(value)
+            want = check(run, ctx)
+            assert np.isnan(want[0]).all() and not np.isnan(want[1]).any()
+
+
+@pytest.mark.parametrize("tag", [0, 3])
+@pytest.mark.parametrize("geometry", list(GEOMETRIES))
+def test_rows_that_see_one_token(pk, ctx, tag, geometry):
+    """All logits of such a row have one sign."""
+    for case in (Case([1], [1]), Case([1], [30], [[0] * 30]), Case([60, 2], [60, 1], [list(range(60)), [0]])):
+        for sign in (1.0, -1.0):
+            run = Run(pk, tag, *GEOMETRIES[geometry], case, BF16)
+            run.q[0, :, 3] = sign * float("inf")
+            want = check(run, ctx)
+            assert np.isnan(want[0][0]) and not np.isnan(want[0][1:]).any()
+
+
 @pytest.mark.parametrize("rows", ROWS)
 @pytest.mark.parametrize("geometry", list(GEOMETRIES))
 @pytest.mark.parametrize("token", [3, 130, 299])
@@ -87,6 +121,23 @@ def test_keys_of_the_pool(pk, ctx, rows, geometry, token, value):
     want = check(run, ctx)
     if value == "-inf" and run.H == 1:
         assert want[0][token] == 0 and not np.isnan(want[0]).any()
+
+
+@pytest.mark.parametrize("rows", ROWS)
+@pytest.mark.parametrize("geometry", list(GEOMETRIES))
+def test_keys_of_the_pool_that_leave_a_row_nothing(pk, ctx, rows, geometry):
+    """Minus infinity for every token, and for all but one."""
+    for but in (None, 17):
+        def spoil(run):
+            keep = None if but is None else run.kp[run.table[0, but // run.P], but % run.P].clone()
+            run.kp[run.table[0].astype(np.int64), :, :, 7] = float("-inf")
+            if but is not None:
+                run.kp[run.table[0, but // run.P], but % run.P] = keep
+
+        run = Run(pk, 0, *GEOMETRIES[geometry], Case([300, 80], [rows, rows]), BF16, k_edit=spoil)
+        run.q[:, :, 7] = run.q[:, :, 7].abs() + 0.5
+        want = check(run, ctx)
+        assert np.isnan(want[0]).all() == (but is None) and not np.isnan(want[1]).any()
 
 
 @pytest.mark.parametrize("tag", [1, 3])
@@ -112,7 +163,28 @@ def test_unaligned_queries_give_the_same(pk, ctx, rows):
     def spoil(run):
         run.kp[run.table[0, 0], 3, 0, 7] = float("nan")
 
-    run = Run(pk, 0, 1, 4, 64, 16, 32, Case([300, 80], [rows, rows]), BF16, k_edit=spoil)
-    odd = torch.zeros(run.q.numel() + 1, dtype=BF16, device=DEV)[1:].view(run.q.shape)
-    odd.copy_(run.q)
-    assert np.isnan(check(run, ctx, q=odd)[0]).all()
+    for edit, value in ((one_sign, float("inf")), (spoil, 1.0)):
+        run = Run(pk, 0, 1, 4, 64, 16, 32, Case([300, 80], [rows, rows]), BF16, k_edit=edit)
+        run.q[rows - 1, 2, 5] = value
+        odd = torch.zeros(run.q.numel() + 1, dtype=BF16, device=DEV)[1:].view(run.q.shape)
+        odd.copy_(run.q)
+        assert np.isnan(check(run, ctx, q=odd)[0]).all()
+
+
+@pytest.mark.parametrize("rows", [1, 50])
+def test_whole_masses_of_broken_rows_are_zero_and_latched(pk, ctx, rows):
+    run = Run(pk, 0, 1, 4, 64, 16, 32, Case([300, 80], [rows, rows]), BF16, k_edit=one_sign)
+    base = run.call(ctx, dtype=torch.int64)
+    run.q[rows - 1, 2, 5] = float("inf")
+    got = run.call(ctx, dtype=torch.int64, status=pk.E_BADINPUT)
+    assert torch.all(got[0, :300] == 0) and torch.equal(got[1], base[1])
+
+
+@pytest.mark.parametrize("rows", ROWS)
+def test_rows_that_see_nothing_still_add_nothing(pk, ctx, rows):
+    """Beside rows that do: at negative positions, and behind the cache's end by more than the window."""
+    pos = [[-1] * (rows - 1) + [99], [200] * rows]
+    run = Run(pk, 0, 1, 4, 64, 16, 32, Case([100, 80], [rows, rows], pos), BF16)
+    run.q[:rows - 1] = float("inf")
+    want = check(run, ctx, window=20)
+    assert np.all(want[1] == 0) and want[0].sum() == pytest.approx(4.0)
