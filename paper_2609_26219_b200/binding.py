@@ -303,35 +303,36 @@ def attention_mass_workspace_bytes(geom: Geom, cache, batch: Batch, n_q_heads: i
 _MASS_TYPES = {torch.float32: MASS_F32, torch.int64: MASS_U64}
 
 
-def _rows(t: torch.Tensor, name: str):
+# The helpers below refuse a tensor that is not on the GPU `device`: a host address, or another GPU's, in a kernel would be a fault.
+def _rows(t: torch.Tensor, name: str, device: int = 0):
     """Row type, shape and strides of a tensor [rows][heads][channels]."""
     kind, shape, strides = _ROW_TYPES.get(t.dtype), t.shape, t.stride()
-    if kind is None or not t.is_cuda or len(shape) != 3 or (strides[2] != 1 and shape[2] > 1):
-        raise ValueError(f"{name}: a bfloat16 or float16 device tensor [rows][heads][channels] with unit channel stride")
+    if kind is None or t.get_device() != device or len(shape) != 3 or (strides[2] != 1 and shape[2] > 1):
+        raise ValueError(f"{name}: a bfloat16 or float16 tensor [rows][heads][channels] on GPU {device} with unit channel stride")
     return kind, shape, strides
 
 
-def _table_rows(t: torch.Tensor, name: str, rows: int, whole: bool = False):
+def _table_rows(t: torch.Tensor, name: str, rows: int, whole: bool = False, device: int = 0):
     """Row stride and entries of an int32 tensor [at least rows][entries] with unit stride on the last axis (whole: without gaps)."""
     shape, strides = t.shape, t.stride()
-    if (t.dtype is not torch.int32 or not t.is_cuda or len(shape) != 2 or shape[0] < rows or (strides[1] != 1 and shape[1] > 1)
+    if (t.dtype is not torch.int32 or t.get_device() != device or len(shape) != 2 or shape[0] < rows or (strides[1] != 1 and shape[1] > 1)
             or (whole and rows > 1 and strides[0] != shape[1])):
-        raise ValueError(f"{name}: {'a contiguous' if whole else 'an'} int32 device tensor [n_seqs][entries]{'' if whole else ' with unit stride on the last axis'}")
+        raise ValueError(f"{name}: {'a contiguous' if whole else 'an'} int32 tensor [n_seqs][entries] on GPU {device}{'' if whole else ' with unit stride on the last axis'}")
     return (strides[0] if shape[0] > 1 else shape[1]), shape[1]
 
 
-def _counts(t: torch.Tensor, name: str, n: int) -> int:
+def _counts(t: torch.Tensor, name: str, n: int, device: int = 0) -> int:
     shape = t.shape
-    if t.dtype is not torch.int32 or not t.is_cuda or len(shape) != 1 or shape[0] < n or (n > 1 and t.stride(0) != 1):
-        raise ValueError(f"{name}: a contiguous int32 device tensor of {n} entries")
+    if t.dtype is not torch.int32 or t.get_device() != device or len(shape) != 1 or shape[0] < n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name}: a contiguous int32 tensor of {n} entries on GPU {device}")
     return t.data_ptr()
 
 
-def _mass_rows(t: torch.Tensor, name: str, kinds, rows: int):
+def _mass_rows(t: torch.Tensor, name: str, kinds, rows: int, device: int = 0):
     """Row stride and entries of a tensor of masses [at least rows][tokens]."""
     shape, strides = t.shape, t.stride()
-    if t.dtype not in kinds or not t.is_cuda or len(shape) != 2 or shape[0] < rows or (strides[1] != 1 and shape[1] > 1):
-        raise ValueError(f"{name}: a device tensor [n_seqs][tokens] of {', '.join(str(k) for k in kinds)} with unit stride on the last axis")
+    if t.dtype not in kinds or t.get_device() != device or len(shape) != 2 or shape[0] < rows or (strides[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{name}: a tensor [n_seqs][tokens] of {', '.join(str(k) for k in kinds)} on GPU {device} with unit stride on the last axis")
     return (strides[0] if shape[0] > 1 else shape[1]), shape[1]
 
 
@@ -455,20 +456,20 @@ class Context:
         """Rotates q [n_rows][Hq][D] into q_out (None: into q itself) and k [n_rows][H][D], and writes k and v into their
         positions of a QPool or of the bf16 Pool.  rope_pos: int32 [n_rows], the rotary positions where they are not those in
         the cache; rope_factor multiplies cos and sin.  Without q only the cache is written."""
-        kind, shape, ks = _rows(k, "k")
-        v_kind, v_shape, vs = _rows(v, "v")
+        kind, shape, ks = _rows(k, "k", self.device)
+        v_kind, v_shape, vs = _rows(v, "v", self.device)
         if v_kind != kind or v_shape != shape:
             raise ValueError("k and v must agree in type and shape")
         n, dim = batch.n_rows, geom.head_dim
         if shape[0] < n or shape[1] != geom.n_kv_heads or shape[2] != dim:
             raise ValueError("k and v: [n_rows][n_kv_heads][head_dim]")
         if q is not None:
-            q_kind, q_shape, qs = _rows(q, "q")
+            q_kind, q_shape, qs = _rows(q, "q", self.device)
             qp = q.data_ptr()
             if q_out is None:
                 o_kind, o_shape, os_, op = q_kind, q_shape, qs, qp
             else:
-                o_kind, o_shape, os_ = _rows(q_out, "q_out")
+                o_kind, o_shape, os_ = _rows(q_out, "q_out", self.device)
                 op = q_out.data_ptr()
             if q_kind != kind or o_kind != kind or o_shape != q_shape:
                 raise ValueError("q and q_out must agree in shape, and in type with k")
@@ -480,7 +481,7 @@ class Context:
         else:
             heads, qp, op, qs, os_ = 0, None, None, (0, 0), (0, 0)
         a = RotaryArgs(_SIZEOF_ROTARY, kind, heads, rope_factor, qp, op, qs[0], qs[1], os_[0], os_[1], k.data_ptr(), v.data_ptr(),
-                       ks[0], ks[1], vs[0], vs[1], None if rope_pos is None else _counts(rope_pos, "rope_pos", n))
+                       ks[0], ks[1], vs[0], vs[1], None if rope_pos is None else _counts(rope_pos, "rope_pos", n, self.device))
         pool, pages = (None, cache) if isinstance(cache, QPool) else (cache, None)
         rc = (_lib or lib()).patchkv_rotary_append(self._h, geom, pool, pages, layer, batch, a, _stream_of(stream, self.device))
         return rc if rc == OK else self._check(rc, check)
@@ -491,18 +492,23 @@ class Context:
         """mass [n_seqs][tokens] (fp32, or int64 in units of 2^-24) = decay * mass_in + the attention weight that each token gets
         from q [n_rows][Hq][D].  mass_in: like mass (same strides), may be mass; None: zeros.  The rest as for attention, the
         workspace of attention_mass_workspace_bytes(...) bytes."""
-        kind, shape, qs = _rows(q, "q")
+        kind, shape, qs = _rows(q, "q", self.device)
         if shape[0] < batch.n_rows or shape[2] != geom.head_dim:
             raise ValueError("q: [n_rows][n_q_heads][head_dim]")
-        stride, tokens = _mass_rows(mass, "mass", _MASS_TYPES, batch.n_seqs)
+        stride, tokens = _mass_rows(mass, "mass", _MASS_TYPES, batch.n_seqs, self.device)
         if tokens < batch.max_kv_len and tokens < batch.table_stride * geom.page_tokens:
             raise ValueError("mass: [n_seqs][at least max_kv_len, or what the block table has room for]")
         before = None
         if mass_in is not None:
-            if mass_in is not mass and (mass_in.dtype is not mass.dtype or mass_in.shape != mass.shape or mass_in.stride() != mass.stride()):
-                raise ValueError("mass_in must agree with mass in type, shape and strides")
+            if mass_in is not mass and (mass_in.dtype is not mass.dtype or mass_in.shape != mass.shape or mass_in.stride() != mass.stride()
+                                        or mass_in.get_device() != self.device):
+                raise ValueError("mass_in must agree with mass in type, shape, strides and device")
             before = mass_in.data_ptr()
-        ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+        ws, ws_bytes = None, 0
+        if workspace is not None:
+            if workspace.get_device() != self.device or not workspace.is_contiguous():
+                raise ValueError(f"workspace: a contiguous tensor on GPU {self.device}")
+            ws, ws_bytes = workspace.data_ptr(), workspace.nbytes
         a = MassArgs(_SIZEOF_MASS, kind, shape[1], window, sinks, shape[2] ** -0.5 if scale is None else scale, decay,
                      _MASS_TYPES[mass.dtype], q.data_ptr(), qs[0], qs[1], before, mass.data_ptr(), stride, ws, ws_bytes)
         pool, pages = (None, cache) if isinstance(cache, QPool) else (cache, None)
@@ -516,17 +522,17 @@ class Context:
         (ascending, then -1), kept int32 [n_seqs], and mass_out fp32 [n_seqs][max_keep], the masses of the kept.  The
         budget of a sequence is budget[b] (int32), or max_keep; n_seqs is kv_len's size."""
         n = kv_len.numel()
-        mass_stride, tokens = _mass_rows(mass, "mass", _FLOAT_MASS, n)
-        keep_stride, most = _table_rows(keep, "keep", n)
+        mass_stride, tokens = _mass_rows(mass, "mass", _FLOAT_MASS, n, self.device)
+        keep_stride, most = _table_rows(keep, "keep", n, False, self.device)
         out, out_stride = None, 0
         if mass_out is not None:
-            out_stride, room = _mass_rows(mass_out, "mass_out", _FLOAT_MASS, n)
+            out_stride, room = _mass_rows(mass_out, "mass_out", _FLOAT_MASS, n, self.device)
             if room < most:
                 raise ValueError("mass_out: [n_seqs][at least max_keep]")
             out = mass_out.data_ptr()
-        a = EvictArgs(_SIZEOF_EVICT, n, tokens, most, recent, sinks, mass.data_ptr(), mass_stride, _counts(kv_len, "kv_len", n),
-                      None if budget is None else _counts(budget, "budget", n), keep.data_ptr(), keep_stride,
-                      _counts(kept, "kept", n), out, out_stride)
+        a = EvictArgs(_SIZEOF_EVICT, n, tokens, most, recent, sinks, mass.data_ptr(), mass_stride, _counts(kv_len, "kv_len", n, self.device),
+                      None if budget is None else _counts(budget, "budget", n, self.device), keep.data_ptr(), keep_stride,
+                      _counts(kept, "kept", n, self.device), out, out_stride)
         rc = (_lib or lib()).patchkv_evict_select(self._h, a, _stream_of(stream, self.device))
         return rc if rc == OK else self._check(rc, check)
 
@@ -535,10 +541,10 @@ class Context:
         """Moves the rows keep[b][i] (positions by src_table) of a QPool or the bf16 Pool to positions i by dst_table; rotate (Pool
         only) turns K by i - keep[b][i].  int32 tensors; pages of dst_table may not be among those that src_table reads."""
         n = kept.numel()
-        keep_stride, most = _table_rows(keep, "keep", n)
-        a = GatherArgs(_SIZEOF_GATHER, n, most, 1 if rotate else 0, _table_rows(src_table, "src_table", n, True)[1],
-                       _table_rows(dst_table, "dst_table", n, True)[1], keep.data_ptr(), keep_stride, _counts(kept, "kept", n),
-                       _counts(kv_len, "kv_len", n), src_table.data_ptr(), dst_table.data_ptr())
+        keep_stride, most = _table_rows(keep, "keep", n, False, self.device)
+        a = GatherArgs(_SIZEOF_GATHER, n, most, 1 if rotate else 0, _table_rows(src_table, "src_table", n, True, self.device)[1],
+                       _table_rows(dst_table, "dst_table", n, True, self.device)[1], keep.data_ptr(), keep_stride, _counts(kept, "kept", n, self.device),
+                       _counts(kv_len, "kv_len", n, self.device), src_table.data_ptr(), dst_table.data_ptr())
         pool, pages = (None, cache) if isinstance(cache, QPool) else (cache, None)
         rc = (_lib or lib()).patchkv_cache_gather(self._h, geom, pool, pages, layer, a, _stream_of(stream, self.device))
         return rc if rc == OK else self._check(rc, check)
