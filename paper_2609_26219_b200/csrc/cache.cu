@@ -258,10 +258,25 @@ int fill_pool(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, const pa
     return PATCHKV_OK;
 }
 
+namespace {
+struct Axis { long long n, stride; };
+// Whether two rows of D elements, `delta` and some steps (fewer than n each way) along the axes apart, share an element.  Axes ascend, and
+// each strides over all that lies inside it, so that of its steps only the two next to delta come near.
+bool rows_meet(const Axis* axes, int i, __int128 delta, int D) {
+    if (i < 0) return delta > -D && delta < D;
+    const Axis& x = axes[i];
+    if (x.n == 1) return rows_meet(axes, i - 1, delta, D);
+    __int128 a = delta / x.stride;
+    if (a * x.stride > delta) a--;
+    for (int k = 0; k < 2; k++, a++)
+        if (a > -x.n && a < x.n && rows_meet(axes, i - 1, delta - a * x.stride, D)) return true;
+    return false;
+}
+}  // namespace
+
 int check_written_pool(patchkv_ctx* ctx, const char* who, const patchkv_geom* g, const patchkv_pool* q) {
     const std::string w(who);
-    if (q->k_base == q->v_base) return fail(ctx, PATCHKV_E_INVALID, w + ": K and V of the pool are in one place");
-    struct Axis { long long n, stride; } axes[3] = {{g->n_kv_heads, q->stride_head}, {g->page_tokens, q->stride_token}, {q->n_pages, q->stride_page}};
+    Axis axes[3] = {{g->n_kv_heads, q->stride_head}, {g->page_tokens, q->stride_token}, {q->n_pages, q->stride_page}};
     std::sort(axes, axes + 3, [](const Axis& a, const Axis& b) { return a.stride < b.stride; });
     __int128 extent = g->head_dim;                          // of what lies inside an axis
     for (const Axis& x : axes) {
@@ -269,6 +284,8 @@ int check_written_pool(patchkv_ctx* ctx, const char* who, const patchkv_geom* g,
         if (x.stride < extent) return fail(ctx, PATCHKV_E_INVALID, w + ": heads, tokens or pages of the pool overlap");
         extent += (__int128)(x.n - 1) * x.stride;
     }
+    const long long apart = (static_cast<const char*>(q->v_base) - static_cast<const char*>(q->k_base)) / 2;
+    if (rows_meet(axes, 2, apart, g->head_dim)) return fail(ctx, PATCHKV_E_INVALID, w + ": K and V of the pool are in one place");
     return PATCHKV_OK;
 }
 
