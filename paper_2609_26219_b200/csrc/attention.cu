@@ -35,9 +35,9 @@ __global__ void __launch_bounds__(kAnyThreads) attention_any_kernel(const Attent
     const int end = min(pos, kv - 1) + 1;                       // tokens [0, end), those outside the window by `sees`
     float m = -INFINITY, l = 0.0f, acc[2] = {0.0f, 0.0f};
     const int kf = k_format(p.c.tag), vf = v_format(p.c.tag);
-    int t0 = 0;
+    long long t0 = 0;                                           // (of 2^31 - 1 tokens the step behind the last is above 2^31)
     while (t0 < end) {
-        const int t = t0 + threadIdx.x;
+        const int t = (int)min(t0 + threadIdx.x, (long long)end);
         float x = -INFINITY;
         off_v[threadIdx.x] = -1;
         if (t < end && sees(p, pos, t)) {
@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(kAnyThreads) attention_any_kernel(const Attent
         __syncthreads();
         l *= keep;
         acc[0] *= keep; acc[1] *= keep;
-        for (int j = 0; j < min(kAnyThreads, end - t0); j++) {
+        for (int j = 0, n = (int)min((long long)kAnyThreads, end - t0); j < n; j++) {
             const long long o = off_v[j];
             if (o < 0) continue;
             l += w[j];

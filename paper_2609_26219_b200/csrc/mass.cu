@@ -60,7 +60,9 @@ __global__ void __launch_bounds__(kMassThreads) mass_sums_any_kernel(const Atten
     __syncthreads();
     float m = -INFINITY, l = 0.0f;
     bool saw = false;
-    for (int t = threadIdx.x; t <= min(pos, kv - 1); t += kMassThreads) {
+    const int end = min(pos, kv - 1) + 1;
+    for (uint32_t at = threadIdx.x; end > 0 && at < (uint32_t)end; at += kMassThreads) {       // (of 2^31 - 1 tokens the step behind the last is above 2^31)
+        const int t = (int)at;
         if (!sees(p, pos, t)) continue;
         KeyPlace k;
         if (!find_key(p, s, t, h, &k)) { latch(p.status); continue; }
