@@ -33,9 +33,9 @@ def lose(run, pages):
     run.lost = set(pages)
 
 
-def check(run, ctx, window=0, sinks=0, status=0, sequences=None):
+def check(run, ctx, window=0, sinks=0, status=0, sequences=None, tokens=None):
     """Tolerance: as mass64's."""
-    got = run.call(ctx, window, sinks, status=status).double().cpu().numpy()
+    got = run.call(ctx, window, sinks, status=status, tokens=tokens).double().cpu().numpy()
     q, share, scale, D, r = run.q.double().cpu().numpy(), run.Hq // run.H, run.D ** -0.5, run.D, 0
     for s, (t, positions) in enumerate(zip(run.case.kv, run.case.positions())):
         R = len(positions)
@@ -68,3 +68,65 @@ def test_one_tile_behind_two(pk, ctx, tag):
     run = Run(pk, tag, 1, 1, 64, 16, 32, case, BF16)
     lose(run, [(s, page) for s in range(n) for page in ((73, 70, 3) if s < 148 else (0, 20 + s % 40))])
     check(run, ctx, status=pk.E_BOUNDS, sequences={0, 1, 70, 147, 148, 149, 222, 295, 296, 299})
+
+
+# More than eight tiles of 256 vectors over quantised keys: operands come as images.
+MANY = (1, 4, 64, 16, 32), Case([700, 650], [600, 600])
+
+
+@pytest.mark.parametrize("tag", [0, 1, 3])
+def test_many_tiles_of_vectors(pk, ctx, tag):
+    geometry, case = MANY
+    run = Run(pk, tag, *geometry, case, BF16)
+    lose(run, [(0, 2), (0, 40), (1, 0), (1, 17)])
+    check(run, ctx, status=pk.E_BOUNDS)
+    check(run, ctx, window=30, sinks=5, status=pk.E_BOUNDS)
+
+
+@pytest.mark.parametrize("tag", [0, 1, 3])
+def test_many_tiles_of_vectors_do_not_ask_for_pages_that_none_sees(pk, ctx, tag):
+    """Behind the window, between windows that lie apart, and behind the last position."""
+    geometry, case = MANY
+    run = Run(pk, tag, *geometry, case, BF16)
+    lose(run, [(0, 2), (0, 4), (1, 1)])
+    check(run, ctx, window=10, sinks=3)
+    case = Case([700, 650], [600, 600], [[100 + i % 50 if i < 300 else 400 + i % 70 for i in range(600)], [200 + i % 90 for i in range(600)]])
+    run = Run(pk, tag, *geometry, case, BF16)                 # seen: tokens 61 to 149 and 361 to 469, 161 to 289, and the first two
+    lose(run, [(0, 2), (0, 14), (0, 21), (0, 40), (1, 3), (1, 20), (1, 39)])
+    check(run, ctx, window=40, sinks=2)
+    lose(run, [(0, 5), (0, 26), (1, 12)])
+    run.lost |= {(0, 2), (0, 14), (0, 21), (0, 40), (1, 3), (1, 20), (1, 39)}
+    check(run, ctx, window=40, sinks=2, status=pk.E_BOUNDS)
+
+
+@pytest.mark.parametrize("tag", [1, 3])
+def test_many_tiles_of_vectors_and_scales_that_are_not_numbers_where_none_sees(pk, ctx, tag):
+    def spoil(run):
+        for s, t, end in ((0, 700, 704), (1, 650, 656), (0, 20, 90)):
+            for j in range(t, end):
+                ks = run.lay.split(run.pages[run.table[s, j // 16]])[1].view(np.uint16)
+                n = len(ks) // 16
+                ks[j % 16 * n:(j % 16 + 1) * n] = (0x7E00, 0x7C00, 0xFC00)[j % 3]
+
+    geometry, case = MANY
+    run = Run(pk, tag, *geometry, case, BF16, k_edit=spoil)
+    run.lost = set()
+    check(run, ctx, window=10, sinks=3)
+
+
+@pytest.mark.parametrize("tag", [1, 3])
+@pytest.mark.parametrize("images", [False, True])
+def test_many_tiles_in_several_launches_of_quantised_keys(pk, ctx, tag, images):
+    """The tiles' sums do not fit the workspace's 256 MiB at once: by the bound on the tokens 100 MiB a tile, so that two go at a time, without images
+    (they would take more than their share), and 22.5 MiB a tile with them, eleven at a time of thirteen."""
+    n, rows = (90, 50) if images else (400, 460)
+    case = Case([500] + [20] * (n - 1), [rows] + [1] * (n - 1))
+    run = Run(pk, tag, 1, 64, 64, 16, 32, case, BF16)
+    run.held["table"] = run.held["table"].repeat(1, 65536 // (16 * run.table.shape[1]))
+    total = rows + n - 1
+    run.batch = pk.make_batch(row_start=run.held["start"], kv_len=run.held["kv"], block_table=run.held["table"], n_rows=total, max_rows=rows, max_kv_len=65536)
+    assert (pk.attention_mass_workspace_bytes(run.geom, run.cache, run.batch, 64) > 1 << 30) == images
+    run.lost = set()
+    check(run, ctx, sequences={0, 1, n - 1}, tokens=65536)
+    lose(run, [(0, 3), (1, 0)])
+    check(run, ctx, status=pk.E_BOUNDS, sequences={0, 1, n - 1}, tokens=65536)
