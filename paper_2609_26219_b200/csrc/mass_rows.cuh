@@ -392,9 +392,10 @@ struct WeighRows {
             if (k > 0 && !wait(&w.q_free, (k - 1) & 1)) return false;
             const int m = it.m0 + 128 * i + r;
             const bool live = m < it.m_end;
-            const int row = live ? it.first + m / p.share : it.first, hq = live ? it.head * p.share + m % p.share : 0;
+            // Behind the last vector the second pass has the item's first again, with the weight 0: zeros times an infinite key would be NaN.
+            const int from = COLUMNS ? it.m0 : 0, row = it.first + (live ? m : from) / p.share, hq = it.head * p.share + (live ? m : from) % p.share;
             w.pos[128 * i + r] = live ? max(-1, row_position(p.b, it.seq, row)) : -1;
-            float factor = b.load_query(i, r, live, row, hq);
+            float factor = b.load_query(i, r, COLUMNS || live, row, hq);
             w.factor[128 * i + r] = factor;
             if (COLUMNS) {
                 // -log2 of the row's sum; NaN where all of its logits are minus infinity, minus infinity for a row that sees nothing and for
@@ -414,7 +415,7 @@ struct WeighRows {
                     else if (sees_some(p, w.pos[128 * i + r], it.kv)) low = __uint_as_float(0x7FC00000u);
                 }
                 if (factor != factor) factor = p.scale_log2;        // (of zeros)
-                w.scale[128 * i + r] = live ? factor : 0.0f;
+                w.scale[128 * i + r] = factor;
                 w.low[128 * i + r] = low;
             }
             fence_async_smem();
@@ -627,16 +628,14 @@ struct WeighRows {
                 tc_after();
                 const uint4 absent = lds128(smem_u32(w.absent[(g + j) & 7]));
                 const bool gaps = (absent.x | absent.y | absent.z | absent.w) != 0;
-                bool masked = gaps || !whole(t0);
-                if (!masked) {
-                    sum = kPool || p.f16 ? column_sum<false, true>(s_at, from, 0ull) : column_sum<false, false>(s_at, from, 0ull);
-                    // (an infinite key times the zeros behind the last vector is NaN, which is nobody's)
-                    masked = __any_sync(0xFFFFFFFFu, sum != sum);
-                }
-                if (masked) {
+                if (gaps || !whole(t0)) {
                     const uint32_t word = r < 32 ? absent.x : r < 64 ? absent.y : r < 96 ? absent.z : absent.w;
                     const bool there = t < kv && !(word >> (r & 31) & 1u);
                     sum = column_sum<true, kPool>(s_at, from, there ? seeing(from, t) : 0ull);
+                } else if (kPool || p.f16) {
+                    sum = column_sum<false, true>(s_at, from, 0ull);
+                } else {
+                    sum = column_sum<false, false>(s_at, from, 0ull);
                 }
                 release(pair, u);
                 if (leader) {
