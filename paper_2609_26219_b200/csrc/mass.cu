@@ -155,7 +155,7 @@ MassPlan plan_mass(const patchkv_geom* g, int tag, const patchkv_batch* b, int H
         // Whole CTAs along the query vectors; where they leave SMs idle the tokens are split, two steps a piece at least.  (32 rows of 32 query
         // heads over 8 KV heads, 32k tokens of a bf16 pool: 58 us split, 490 us on eight SMs.)
         const long long tiles = (cols + 2 * kRowTile - 1) / (2 * kRowTile), ctas = tiles * H * b->n_seqs;
-        if (ctas > 1 << 24 || cols > 1 << 30) return a;
+        if (ctas == 0 || ctas > 1 << 24 || cols > 1 << 30) return a;
         const long long all = (longest + kRowTile - 1) / kRowTile;
         long long steps = all;                  // that the rows of a CTA see at most
         const long long cta_rows = std::min((long long)b->max_rows, 2ll * kRowTile / (Hq / H) + 2);
