@@ -86,7 +86,10 @@ __global__ void __launch_bounds__(kMassThreads) mass_columns_any_kernel(const At
     __shared__ float q[PATCHKV_MAX_ATTENTION_DIM];
     const int s = blockIdx.y, t = blockIdx.x * kMassThreads + threadIdx.x;
     int first, kv, rows;
-    if (!sequence_rows(p, s, &first, &kv, &rows)) return;
+    if (!sequence_rows(p, s, &first, &kv, &rows)) {
+        if (threadIdx.x == 0) latch(p.status);                  // (of a call without rows nobody has looked)
+        return;
+    }
     rows = min(rows, p.b.max_rows);
     float total = 0.0f;
     for (int hq = 0; hq < p.Hq; hq++) {

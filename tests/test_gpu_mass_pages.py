@@ -130,3 +130,18 @@ def test_many_tiles_in_several_launches_of_quantised_keys(pk, ctx, tag, images):
     check(run, ctx, sequences={0, 1, n - 1}, tokens=65536)
     lose(run, [(0, 3), (1, 0)])
     check(run, ctx, status=pk.E_BOUNDS, sequences={0, 1, n - 1}, tokens=65536)
+
+
+@pytest.mark.parametrize("tag", [0, 3])
+@pytest.mark.parametrize("D", [64, 80])
+def test_batches_without_rows(pk, ctx, tag, D):
+    """Their sums are empty; entries of row_start that are out of order are an error in them, too."""
+    run = Run(pk, tag, 2, 4, D, 16, 16 if D == 80 else 32, Case([40, 33, 0], [0, 0, 0]), BF16)
+    run.q = torch.empty((0, 2, D), dtype=BF16, device=DEV)
+    before = torch.rand((3, 43), device=DEV)
+    got = run.call(ctx, mass_in=before, decay=0.5)
+    for s, t in enumerate(run.case.kv):
+        assert torch.equal(got[s, :t], 0.5 * before[s, :t]) and torch.all(got[s, t:] == -9)
+    run.held["start"].copy_(torch.tensor([0, 0, 2, 1], dtype=torch.int32))
+    got = run.call(ctx, mass_in=before, decay=0.5, status=pk.E_BOUNDS)
+    assert torch.equal(got[0, :40], 0.5 * before[0, :40]) and torch.all(got[1:] == -9)
