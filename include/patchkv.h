@@ -512,7 +512,7 @@ PATCHKV_API uint64_t patchkv_attention_workspace_bytes(const patchkv_geom* geom,
  * is rotated.  Queries, and keys of a bf16 pool, are formed in fp32 with c and s rounded to fp32, and rounded once; channels behind
  * rotary_dim are copied bit for bit.  Keys of quantised pages are formed in double and quantised from there as
  * patchkv_cache_append quantises, without a rounding in between; values are quantised from their 16 bits.
- * A pool in which two heads, tokens or pages, or K and V, lie in one place is refused, here and by patchkv_cache_gather.
+ * A pool in which two heads, tokens or pages, or K and V, share a place is refused, here and by patchkv_cache_gather.
  * Rows, positions and skipped rows as for patchkv_cache_append; the q_out of a skipped row, and of a row of no sequence, is left
  * as it was.  One launch, no allocation, no workspace; can be captured (inv_freq is read by the call, not by its replays).
  * Every geometry is taken.  The fast kernel wants D a power of two from 16 to 256, rotary_dim a multiple of 16,
@@ -554,7 +554,10 @@ PATCHKV_API int patchkv_rotary_append(patchkv_ctx* ctx, const patchkv_geom* geom
  *   PATCHKV_MASS_U64: units of 2^-24 as patchkv_select_repair_tokens reads them (kind TOKEN_MASS); the call's sum is rounded
  *     once, ties to even, and added: decay must be 0 or 1.  A sum that is not finite counts as 0 and latches PATCHKV_E_BADINPUT.
  * Quantised keys enter as they are in calls of up to 16 (row, query head) pairs per KV head and sequence, and with 22 bits in larger
- * ones (a magnitude above 65504 is an infinity to those). */
+ * ones (a magnitude above 65504 is an infinity to those; the masses are up to 2.4e-7 off, relative 2-norm, against 3e-8).
+ * max_rows decides for the whole batch which of the two it is: decode steps beside a prompt's chunk are faster in a call of their own.
+ * The workspace of a small call holds its logits, some 4 * rows * Hq * tokens bytes for each sequence (64 query heads: 134 MB for
+ * eight sequences of one row and 65536 tokens). */
 enum { PATCHKV_MASS_F32 = 0, PATCHKV_MASS_U64 = 1 };
 typedef struct {
     uint32_t struct_size;
@@ -590,7 +593,7 @@ PATCHKV_API uint64_t patchkv_attention_mass_workspace_bytes(const patchkv_geom* 
  *   mass_out[b][i] = mass[b][keep[b][i]], where mass_out is given; the entries behind are left as they were
  * A mass that is negative, infinite or NaN counts as zero and latches PATCHKV_E_BADINPUT.  Lengths above max_len and budgets
  * above max_keep are cut there and latch PATCHKV_E_BOUNDS; those below 0 count as 0.  One launch on `stream`, no allocation, no workspace;
- * can be captured. */
+ * can be captured.  max_len sizes the launch, whatever the lengths are (up to 131072 the keys stay in shared memory): a close bound is faster. */
 typedef struct {
     uint32_t struct_size;
     int32_t n_seqs;

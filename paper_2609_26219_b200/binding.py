@@ -491,7 +491,7 @@ class Context:
                        sinks: int = 0, workspace: Optional[torch.Tensor] = None, stream=None, check: bool = True) -> int:
         """mass [n_seqs][tokens] (fp32, or int64 in units of 2^-24) = decay * mass_in + the attention weight that each token gets
         from q [n_rows][Hq][D].  mass_in: like mass (same strides), may be mass; None: zeros.  The rest as for attention, the
-        workspace of attention_mass_workspace_bytes(...) bytes."""
+        workspace (contiguous) of attention_mass_workspace_bytes(...) bytes.  All tensors are on the context's GPU."""
         kind, shape, qs = _rows(q, "q", self.device)
         if shape[0] < batch.n_rows or shape[2] != geom.head_dim:
             raise ValueError("q: [n_rows][n_q_heads][head_dim]")
@@ -520,7 +520,8 @@ class Context:
                      check: bool = True) -> int:
         """Chooses the tokens that stay: mass fp32 [n_seqs][tokens], kv_len int32 [n_seqs] -> keep int32 [n_seqs][max_keep]
         (ascending, then -1), kept int32 [n_seqs], and mass_out fp32 [n_seqs][max_keep], the masses of the kept.  The
-        budget of a sequence is budget[b] (int32), or max_keep; n_seqs is kv_len's size."""
+        budget of a sequence is budget[b] (int32), or max_keep; n_seqs is kv_len's size.  The width of mass sizes the launch: where it is far
+        above the lengths, pass a narrower view (mass[:, :longest])."""
         n = kv_len.numel()
         mass_stride, tokens = _mass_rows(mass, "mass", _FLOAT_MASS, n, self.device)
         keep_stride, most = _table_rows(keep, "keep", n, False, self.device)

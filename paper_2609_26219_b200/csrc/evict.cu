@@ -30,10 +30,12 @@ struct EvictParams {
 // finds the digit by itself.  After the first digit few keys are left as a rule; every CTA then gets the list of them and finds the other
 // two digits without the cluster (where they are many, ties above all, the cluster counts on).  Each lane counts what of its tokens
 // stays, a prefix over lanes, warps and CTAs gives every kept token its place, and the indices leave by way of shared memory, so that they
-// are written side by side.  All counts are whole numbers: the order of the atomics does not matter.  Bound by the latencies of that
-// chain: a barrier of the cluster takes 2000 cycles, counts read from eight CTAs 4000, from sixteen 12000.  Eight sequences of 128k tokens 22 us, 32
-// of 4096 tokens 9.
-// HELD: keys and indices of a run fit shared memory, else keys are made again each time and indices written one by one.
+// are written side by side.  All counts are whole numbers: the order of the atomics does not matter.  Bound by latencies: a
+// barrier of the cluster takes 2000 cycles, counts read from eight CTAs 4000, from sixteen 12000, which is 5 to 6 of the 21 us that eight sequences
+// of 128k tokens take; the rest, the walks over the keys and the atomics on bins that keys of one scale share, has not been taken apart.
+// 32 sequences of 4096 tokens 7.1 us.
+// HELD: keys and indices of a run fit shared memory, else keys are made again each time and indices written one by one.  The bound on the lengths
+// decides (131072: 21.6 us for eight sequences of that length; 131073: 42.0).
 struct SelectSmem {
     alignas(16) int bins[3][kSelectBins];
     int list[kSelectList];                      // keys that are left after the first digit

@@ -152,6 +152,8 @@ MassPlan plan_mass(const patchkv_geom* g, int tag, const patchkv_batch* b, int H
     a.bytes = any_bytes;
     const long long longest = longest_sequence(g, b);
     if (!shape || cols == 0 || longest > 1 << 30) return a;
+    // The longest run of rows decides for the whole batch: a prompt chunk beside decode steps (2048 rows over 8192 tokens and 7 rows over 65536 each, bf16
+    // pool) takes 1694 us in one call, and 567 in two.
     // Up to 16 columns the split kernel: 32 query heads over 8 KV heads, 32k tokens, 1, 2 and 4 rows take 27, 34 and 49 us of it on a bf16 pool
     // and 22, 28 and 43 us on 4-bit pages; the row kernels take 60 and 68 us for any of them.
     if (cols > 16) {

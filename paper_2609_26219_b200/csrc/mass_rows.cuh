@@ -9,8 +9,7 @@
 // in TMEM for each pair; with one tile of vectors the pairs take turns at the steps.  (Two warpgroups, a tile each, were as fast in
 // the first pass, where the exponential unit is the bound.)  The second pass leaves a number for each token, head and CTA, which
 // the last kernel adds up in an order that the arguments fix.
-// Keys are operands without a rounding: bf16 as they are, quantised ones as the sum of two fp16 matrices (22 bits), for two products per
-// 16 channels.  One fp16 matrix alone would put a logit 2^-12 of its terms off and the masses 1e-4.  With many tiles of vectors the operands are
+// Keys as operands: bf16 as they are, quantised ones as the sum of two fp16 matrices (22 bits), for two products per 16 channels.  One fp16 matrix alone would put a logit 2^-12 of its terms off and the masses 1e-4.  With many tiles of vectors the operands are
 // laid out in the workspace first (images), as for the attention; else each CTA makes them from the pages, eight warps of it.
 // A step of two tiles takes 1024 cycles of products (quantised 2048) and 2048 cycles of the exponential unit.  8192 rows of 32 query heads over
 // 8192 tokens, 8 KV heads of 128 channels: 459 and 478 us for the passes on quantised pages (1.2 PFLOP/s each, both matrices counted, at the

@@ -5,8 +5,9 @@
 // up and, a token at a time, the weights of all heads and rows.  For 4-bit keys and 8 columns a logit written and read back costs 64 bytes
 // for a token and head where reading the keys again costs 72 and turning their codes into operands twice as well.
 // One CTA an SM: two of 64 registers a thread took 130 us where one of 128 takes 120 (8 x 64k tokens of 4-bit pages, 8 KV heads of 128, 64
-// query heads; now 115 in all, 85 of them this pass: 302 MB of keys and scales read and 134 MB of logits written, 5.1 TB/s).  The bound
-// is the instructions: some 225 for 16 tokens of a head and 8 columns, issued in two of three cycles.
+// query heads; now 115 in all, 85 of them this pass: 302 MB of keys and scales read and 134 MB of logits written, 5.1 TB/s).  Neither
+// is full: the instructions, some 225 for 16 tokens of a head and 8 columns, take 63 % of the issue slots.  The workspace holds the logits: 4 bytes
+// for each row, query head and token that the row's sequence may have.
 // Sums run in an order that the arguments fix: no atomics.
 #pragma once
 
@@ -286,8 +287,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) weigh_split_kernel(const __grid
 }
 
 // Second pass (grid: CTAs of a sequence, sequence): a CTA takes every gridDim.x-th 256 tokens, a thread four tokens and a quarter of the columns.
-// Bound by the logits' bytes (134 MB in 31 us); the columns' sums are found once a CTA, so there are no more of those than fill the SMs (four
-// an SM: 114.5 us a call, six 118.3, three 116.9).  A thread has eight logits of each token on their way (144 us a call with one, 131 with
+// Bound by the latency of reading the logits (134 MB in 31 us, some of it from L2; captured 3.2 TB/s of DRAM, warps waiting on loads); the
+// columns' sums are found once a CTA, so there are no more of those than fill the SMs (four an SM: 114.5 us a call, six 118.3, three 116.9).  A thread has eight logits of each token on their way (144 us a call with one, 131 with
 // eight, 143 with sixteen, when it was made).
 constexpr int kWeighTokens = 256, kWeighThreads = 256, kWeighColumns = 256;
 template <int NC>

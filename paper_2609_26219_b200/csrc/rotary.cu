@@ -78,7 +78,8 @@ __device__ __forceinline__ void codes64(const double* x, uint32_t s16, uint8_t* 
 // the same channels of a head in every pass, both of each rotary pair among them (rotary.cuh), so it keeps their cosines and sines in registers
 // and exchanges nothing but the maxima of the keys' groups (with the pairs' other halves brought by shuffles 166 us where this takes 116, 16384
 // rows of 32 query heads and 8 KV heads into 4-bit pages).  Two units of a lane are on their way at a time (95 us for 116).  Bound by
-// memory into a bf16 pool (403 MB in 68 us, 5.9 TB/s); for quantised pages, of 354 MB, by the 64-bit work on the keys beside it, 77 us.
+// memory into a bf16 pool (403 MB in 68 us, 5.9 TB/s); for quantised pages (354 MB in 76 us) by latency beside the 64-bit work on the keys: fp64
+// pipe 12 %, issue slots 49 %, a third of the warps active, most of them waiting on loads.
 template <int TYPE, int KF, int VF, bool HALF>
 __global__ void __launch_bounds__(kRotaryThreads, KF == FMT_BF16 ? 8 : 6) rotary_append_kernel(const __grid_constant__ RotaryParams p) {
     constexpr bool kPool = KF == FMT_BF16;
